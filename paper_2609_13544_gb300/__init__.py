@@ -7,6 +7,7 @@ library has not been built (there is no CPU fallback).
 
 Names follow the C ABI: ``peat_signature_create``, ``peat_compare``,
 ``peat_compare_segmented``, ``peat_pseudo_error_inject``, ``peat_inject_compare``, ``peat_last_error``.
+The playback operators (include/peat_ops.h) are bound in ``ops`` and exported here.
 """
 from __future__ import annotations
 
@@ -16,7 +17,11 @@ from typing import Optional, Sequence
 
 import numpy as np
 
+from . import ops as _ops
 from .buildlib import LIB, build  # noqa: F401
+from .ops import (GRADNORM_BYTES, OPS_EXPORTS, GradList, Linear8, peat_grad_clip, peat_grad_clip_raw,  # noqa: F401
+                  peat_grad_norm, peat_grad_norm_raw, peat_matmul_i8, peat_matmul_i8_raw, peat_quantize_i8,
+                  peat_quantize_i8_raw)
 
 DTYPE_CODES = {"f32": 0, "f16": 1, "bf16": 2}
 CLASSES = ("exact", "within_tol", "mismatch", "nan_inf_asym", "sign_flip")
@@ -135,6 +140,7 @@ def load(path: Optional[Path] = None) -> ctypes.CDLL:
     L.peat_spearman.restype = i32
     L.peat_mean_std.argtypes = [dp, i64, i32, dp, dp]
     L.peat_mean_std.restype = i32
+    _ops.register(L)
     _lib = L
     return L
 

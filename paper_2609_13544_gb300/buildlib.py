@@ -1,4 +1,4 @@
-"""Compile libpeat.so (the CUDA library behind include/peat.h) for sm_103a.
+"""Compile libpeat.so (the CUDA library behind include/peat.h and include/peat_ops.h) for sm_103a.
 
 Each translation unit is compiled in parallel with nvcc, then linked into
 paper_2609_13544_gb300/_build/libpeat.so.  No CMake; a rebuild happens when
@@ -20,9 +20,11 @@ CSRC = PKG / "csrc"
 OUT_DIR = PKG / "_build"
 LIB = OUT_DIR / "libpeat.so"
 LIB_CHECKED = OUT_DIR / "libpeat_checked.so"
-SOURCES = ["compare.cu", "compare8.cu", "compare64.cu", "topk.cu", "tstats.cu", "isclose.cu", "isclose64.cu", "inject.cu", "peat_api.cpp"]
+SOURCES = ["compare.cu", "compare8.cu", "compare64.cu", "topk.cu", "tstats.cu", "isclose.cu", "isclose64.cu", "inject.cu", "quant8.cu",
+           "matmul8.cu", "gradnorm.cu", "peat_api.cpp", "ops_api.cpp"]
 HEADERS = [CSRC / "peat_internal.h", CSRC / "exact.cuh", CSRC / "meanvar.cuh", CSRC / "inject_models.cuh", CSRC / "tol_exact.cuh", CSRC / "exact64.cuh",
-           ROOT / "include" / "peat.h"]
+           CSRC / "peat_handle.h", CSRC / "ops_internal.h", CSRC / "mm8_common.cuh", ROOT / "include" / "peat.h",
+           ROOT / "include" / "peat_ops.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
               f"-I{ROOT / 'include'}", f"-I{CSRC}"]

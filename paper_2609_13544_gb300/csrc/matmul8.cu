@@ -1,0 +1,298 @@
+// 8-bit integer products by the warp-level matrix instructions: few rows, and
+// small products of any shape.
+//
+// Of the two operands "w" is b (its N rows are the 16-row side of the
+// instruction) and "t" is a (its M rows the 8-column side).  A lane holds 16
+// consecutive integers of a row; word j of the 16 makes the lane's four k
+// positions of the j-th of four 16 x 8 x 16 instructions.  Which k a position
+// stands for does not matter as long as both operands agree, so no shuffle and
+// no transposed load is needed.
+#include <cooperative_groups.h>
+
+#include "mm8_common.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace peat {
+namespace {
+
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t word(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
+
+// sums in float32 become integers, added to `sum`
+template <int NT>
+__device__ __forceinline__ void drain(float (&c)[NT][4], int (&sum)[NT][4]) {
+#pragma unroll
+  for (int n = 0; n < NT; n++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      sum[n][i] += __float2int_rn(c[n][i]);
+      c[n][i] = 0.0f;
+    }
+}
+
+// ---- up to 16 rows of a: bound by the bytes of b -----------------------------
+// A CTA of four warps takes 16 rows of b, each warp every fourth run of 64 k
+// (and each CTA of a cluster a share of those runs), straight from global
+// memory: every byte of b is used once, so nothing is gained by staging it.
+constexpr int RT = 128;  // threads
+template <int OUT, int NT, int MODE>
+__global__ void __launch_bounds__(RT) mm8_rows(Mm8Params p) {
+  __shared__ int part[4][NT * 8][17];
+  cg::cluster_group cl = cg::this_cluster();
+  const int S = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int64_t n0 = ((int64_t)blockIdx.x / S) * 16;
+  const int64_t runs = (p.K + 63) / 64;
+  const int8_t *alo = p.a, *ahi = p.a + (p.M - 1) * p.lda + p.K, *blo = p.b, *bhi = p.b + (p.N - 1) * p.ldb + p.K;
+  float c[NT][4];
+  int sum[NT][4];
+#pragma unroll
+  for (int n = 0; n < NT; n++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) c[n][i] = 0.0f, sum[n][i] = 0;
+  const int8_t* w0 = p.b + (n0 + g) * p.ldb + 16 * t;
+  const int8_t* w1 = w0 + 8 * p.ldb;
+  const bool has0 = n0 + g < p.N, has1 = n0 + g + 8 < p.N;
+  const int step = 4 * S;
+  constexpr int U = 4;  // runs in flight
+  int since = 0;
+  for (int64_t r = rank * 4 + warp; r < runs; r += U * step) {
+    uint4 u0[U], u1[U], x[U][NT];
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int64_t k = (r + (int64_t)u * step) * 64, left = p.K - k - 16 * t;
+      u0[u] = load16<MODE>(w0 + k, has0 ? left : 0, blo, bhi);
+      u1[u] = load16<MODE>(w1 + k, has1 ? left : 0, blo, bhi);
+#pragma unroll
+      for (int n = 0; n < NT; n++)
+        x[u][n] = load16<MODE>(p.a + (n * 8 + g) * p.lda + 16 * t + k, n * 8 + g < p.M ? left : 0, alo, ahi);
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        uint32_t a[4];
+        to_half(word(u0[u], j), a[0], a[2]);
+        to_half(word(u1[u], j), a[1], a[3]);
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+          uint32_t b0, b1;
+          to_half(word(x[u][n], j), b0, b1);
+          mma16816(c[n], a, b0, b1);
+        }
+      }
+    }
+    since += U;
+    if (since >= MM8_EXACT_K / 64) {
+      drain(c, sum);
+      since = 0;
+    }
+  }
+  drain(c, sum);
+#pragma unroll
+  for (int n = 0; n < NT; n++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) part[warp][n * 8 + 2 * t + (i & 1)][g + 8 * (i >> 1)] = sum[n][i];
+  cl.sync();
+  // the cluster's CTAs share the tile's elements: 16 b rows of each a row
+  typename Mm8Out<OUT>::T* out = static_cast<typename Mm8Out<OUT>::T*>(p.out);
+  for (int i = rank * RT + threadIdx.x; i < NT * 8 * 16; i += S * RT) {
+    const int m = i >> 4, n = i & 15;
+    if (m >= p.M || n0 + n >= p.N) continue;
+    int v = 0;
+    for (int k = 0; k < S; k++) {
+      const int* q = cl.map_shared_rank(&part[0][m][n], k);
+#pragma unroll
+      for (int w = 0; w < 4; w++) v += q[w * NT * 8 * 17];
+    }
+    const float s = (p.sa ? __ldg(p.sa + m) : 1.0f) * (p.sb ? __ldg(p.sb + n0 + n) : 1.0f);
+    out[m * p.ldo + n0 + n] = Mm8Out<OUT>::make(v, s, p.bias ? __ldg(p.bias + n0 + n) : 0.0f);
+  }
+  cl.sync();  // the others may still read this CTA's part
+}
+
+// ---- tiles --------------------------------------------------------------------
+// A CTA takes 128 rows of b by 64 rows of a, 64 k a stage, staged as bytes;
+// each of its 8 warps 32 x 32, so that an integer that is turned into binary16
+// serves four instructions.
+constexpr int TT = 256, TW = 128, TA = 64, TK = 64, TSTAGES = 4;
+constexpr int TSTAGE_BYTES = (TW + TA) * TK;
+constexpr int T_SMEM = TSTAGES * TSTAGE_BYTES;  // 48 KB; the sums' tile (64 x 132 words) fits in it
+static_assert(T_SMEM >= TA * (TW + 4) * 4, "the sums take the stages' place");
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+
+template <int OUT, int MODE>
+__global__ void __launch_bounds__(TT, 2) mm8_tiles(Mm8Params p, int ntw) {
+  extern __shared__ __align__(128) int8_t smem[];
+  cg::cluster_group cl = cg::this_cluster();
+  const int S = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  const int tile = blockIdx.x / S;
+  const int64_t n0 = (int64_t)(tile % ntw) * TW, m0 = (int64_t)(tile / ntw) * TA;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int wn = (warp & 3) * 32, wm = (warp >> 2) * 32;
+  const int64_t runs = (p.K + TK - 1) / TK, r0 = runs * rank / S, r1 = runs * (rank + 1) / S;
+  const int8_t *alo = p.a, *ahi = p.a + (p.M - 1) * p.lda + p.K, *blo = p.b, *bhi = p.b + (p.N - 1) * p.ldb + p.K;
+  const uint32_t sbase = (uint32_t)__cvta_generic_to_shared(smem);
+
+  // a thread's three pieces of 16 bytes of a stage: rows of b first, then of a
+  const int8_t* src[3];
+  bool has[3];
+#pragma unroll
+  for (int i = 0; i < 3; i++) {
+    const int row = (threadIdx.x >> 2) + 64 * i;
+    const bool isb = row < TW;
+    const int64_t gr = isb ? n0 + row : m0 + row - TW;
+    has[i] = gr < (isb ? p.N : p.M);
+    src[i] = (isb ? p.b + (has[i] ? gr : 0) * p.ldb : p.a + (has[i] ? gr : 0) * p.lda) + 16 * (threadIdx.x & 3);
+  }
+  auto load = [&](int64_t r, int st) {
+    const int64_t k = r * TK, left = p.K - k - 16 * (threadIdx.x & 3);
+#pragma unroll
+    for (int i = 0; i < 3; i++) {
+      const int at = st * TSTAGE_BYTES + 64 * 64 * i + threadIdx.x * 16;
+      if (MODE == 16) {
+        const int bytes = has[i] && left > 0 ? (int)(left < 16 ? left : 16) : 0;
+        cp_async16(sbase + at, bytes ? src[i] + k : p.a, bytes);
+      } else {
+        const bool isb = i < 2;
+        *reinterpret_cast<uint4*>(smem + at) = load16<MODE>(src[i] + k, has[i] ? left : 0, isb ? blo : alo, isb ? bhi : ahi);
+      }
+    }
+  };
+  float c[8][4];
+  int sum[8][4];
+#pragma unroll
+  for (int n = 0; n < 8; n++)
+#pragma unroll
+    for (int i = 0; i < 4; i++) c[n][i] = 0.0f, sum[n][i] = 0;
+
+#pragma unroll
+  for (int s = 0; s < TSTAGES - 1; s++) {
+    if (r0 + s < r1) load(r0 + s, s);
+    if (MODE == 16) asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  int since = 0;
+  for (int64_t r = r0; r < r1; r++) {
+    const int st = (int)((r - r0) % TSTAGES);
+    if (MODE == 16) asm volatile("cp.async.wait_group %0;" ::"n"(TSTAGES - 2) : "memory");
+    __syncthreads();  // the stage is there, and the one before it is free
+    if (r + TSTAGES - 1 < r1) load(r + TSTAGES - 1, (int)((r - r0 + TSTAGES - 1) % TSTAGES));
+    if (MODE == 16) asm volatile("cp.async.commit_group;" ::: "memory");
+    const int8_t* sb = smem + st * TSTAGE_BYTES;
+    const int8_t* sa = sb + TW * TK;
+    uint4 w[4], x[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      w[i] = *reinterpret_cast<const uint4*>(sb + (wn + i * 8 + g) * TK + 16 * t);
+      x[i] = *reinterpret_cast<const uint4*>(sa + (wm + i * 8 + g) * TK + 16 * t);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      uint32_t a[2][4], b[4][2];
+#pragma unroll
+      for (int i = 0; i < 2; i++) {
+        to_half(word(w[2 * i], j), a[i][0], a[i][2]);
+        to_half(word(w[2 * i + 1], j), a[i][1], a[i][3]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; i++) to_half(word(x[i], j), b[i][0], b[i][1]);
+#pragma unroll
+      for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int n = 0; n < 4; n++) mma16816(c[i * 4 + n], a[i], b[n][0], b[n][1]);
+    }
+    if (++since == MM8_EXACT_K / TK) {
+      drain(c, sum);
+      since = 0;
+    }
+  }
+  drain(c, sum);
+  if (MODE == 16) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+  int* tot = reinterpret_cast<int*>(smem);  // [TA][TW + 4]
+  constexpr int P = TW + 4;
+#pragma unroll
+  for (int i = 0; i < 2; i++)
+#pragma unroll
+    for (int n = 0; n < 4; n++)
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        tot[(wm + n * 8 + 2 * t + (e & 1)) * P + wn + i * 16 + g + 8 * (e >> 1)] = sum[i * 4 + n][e];
+  cl.sync();
+  typename Mm8Out<OUT>::T* out = static_cast<typename Mm8Out<OUT>::T*>(p.out);
+  const int col = threadIdx.x & 127;
+  const int64_t n = n0 + col;
+  if (n < p.N) {
+    const float sb = p.sb ? __ldg(p.sb + n) : 1.0f, bias = p.bias ? __ldg(p.bias + n) : 0.0f;
+    for (int row = rank * 2 + (threadIdx.x >> 7); row < TA; row += 2 * S) {
+      const int64_t m = m0 + row;
+      if (m >= p.M) break;
+      int v = 0;
+      for (int k = 0; k < S; k++) v += *cl.map_shared_rank(&tot[row * P + col], k);
+      const float s = (p.sa ? __ldg(p.sa + m) : 1.0f) * sb;
+      out[m * p.ldo + n] = Mm8Out<OUT>::make(v, s, bias);
+    }
+  }
+  cl.sync();  // the others may still read this CTA's sums
+}
+
+template <typename F, typename... A>
+cudaError_t cluster_launch(F kernel, int64_t tiles, int S, int threads, int smem, cudaStream_t s, A... args) {
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)S;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * S));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int OUT, int MODE>
+cudaError_t direct(const Mm8Params& p, int nsm, cudaStream_t s) {
+  const int64_t runs = (p.K + 63) / 64;
+  if (p.M <= 16) {
+    const int64_t tiles = (p.N + 15) / 16;
+    int S = 1;  // share the k runs while the SMs are not filled and every warp keeps a few
+    while (S < 8 && tiles * S < 2 * (int64_t)nsm && runs >= 32 * S) S *= 2;
+    if (p.M <= 8) return cluster_launch(mm8_rows<OUT, 1, MODE>, tiles, S, RT, 0, s, p);
+    return cluster_launch(mm8_rows<OUT, 2, MODE>, tiles, S, RT, 0, s, p);
+  }
+  const int64_t ntw = (p.N + TW - 1) / TW, tiles = ntw * ((p.M + TA - 1) / TA);
+  int S = 1;
+  while (S < 8 && tiles * S < 2 * (int64_t)nsm && runs >= 8 * S) S *= 2;
+  return cluster_launch(mm8_tiles<OUT, MODE>, tiles, S, TT, T_SMEM, s, p, (int)ntw);
+}
+
+template <int OUT>
+cudaError_t direct_out(const Mm8Params& p, int nsm, cudaStream_t s) {
+  const bool al = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | (uintptr_t)p.lda |
+                    (uintptr_t)p.ldb) & 15) == 0;
+  return al ? direct<OUT, 16>(p, nsm, s) : direct<OUT, 1>(p, nsm, s);
+}
+
+}  // namespace
+
+cudaError_t launch_mm8_direct(int out_dtype, const Mm8Params& p, int nsm, cudaStream_t s) {
+  switch (out_dtype) {
+    case PEAT_F32: return direct_out<PEAT_F32>(p, nsm, s);
+    case PEAT_F16: return direct_out<PEAT_F16>(p, nsm, s);
+    case PEAT_BF16: return direct_out<PEAT_BF16>(p, nsm, s);
+    default: return direct_out<PEAT_OUT_I32>(p, nsm, s);
+  }
+}
+
+}  // namespace peat

@@ -1,0 +1,322 @@
+// Host side of the playback operators declared in include/peat_ops.h:
+// argument checks, workspace, launch planning.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <cstring>
+#include <new>
+
+#include "ops_internal.h"
+#include "peat_handle.h"
+
+namespace peat {
+
+// Made by a handle's first call of an operator, freed with it.
+struct OpsState {
+  // gradient lists: device block (entries, then partial sums), and a ring of
+  // pinned copies of the entries, each free again once its event has passed
+  static constexpr int RING = 4;
+  void* d_list = nullptr;
+  size_t d_list_cap = 0;
+  void* h_list[RING] = {};
+  size_t h_list_cap[RING] = {};
+  cudaEvent_t taken[RING] = {};
+  bool pending[RING] = {};
+  int next = 0;
+  unsigned int* done = nullptr;  // zero between calls
+};
+
+void ops_destroy(OpsState* s) {
+  if (!s) return;
+  if (s->d_list) cudaFree(s->d_list);
+  if (s->done) cudaFree(s->done);
+  for (int i = 0; i < OpsState::RING; i++) {
+    if (s->h_list[i]) cudaFreeHost(s->h_list[i]);
+    if (s->taken[i]) cudaEventDestroy(s->taken[i]);
+  }
+  delete s;
+}
+
+}  // namespace peat
+
+namespace {
+
+using peat::cuda_fail;
+using peat::DeviceGuard;
+using peat::fail;
+using peat::OpsState;
+
+constexpr int64_t MAX_DIM = ((int64_t)1 << 31) - 1;
+
+int type_bytes(int dt) { return dt == PEAT_F32 ? 4 : (dt == PEAT_F16 || dt == PEAT_BF16 ? 2 : 0); }
+bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
+
+peat_status_t ops_state(peat_handle_t h, OpsState** out) {
+  if (!h->ops) {
+    OpsState* s = new OpsState();
+    if (cudaMalloc(&s->done, 256) != cudaSuccess || cudaMemset(s->done, 0, 256) != cudaSuccess ||
+        cudaDeviceSynchronize() != cudaSuccess) {
+      cudaGetLastError();
+      peat::ops_destroy(s);
+      return fail(h, PEAT_ERR_ALLOC, "operator workspace allocation failed");
+    }
+    h->ops = s;
+  }
+  *out = h->ops;
+  return PEAT_OK;
+}
+
+// grows a device block; its contents are not kept, and an earlier call that uses it is waited for by cudaFree
+peat_status_t grow(peat_handle_t h, void** p, size_t* cap, size_t need) {
+  if (need <= *cap) return PEAT_OK;
+  if (*p) cudaFree(*p);
+  *p = nullptr;
+  *cap = 0;
+  if (cudaMalloc(p, need) != cudaSuccess) {
+    cudaGetLastError();
+    *p = nullptr;
+    return fail(h, PEAT_ERR_ALLOC, "operator workspace allocation failed");
+  }
+  *cap = need;
+  return PEAT_OK;
+}
+
+peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int axis,
+                       int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv, cudaStream_t st) {
+  const int B = type_bytes(dtype);
+  if (!B) return fail(h, PEAT_ERR_INVALID_ARG, "dtype must be PEAT_F32, PEAT_F16 or PEAT_BF16");
+  if (axis != 0 && axis != 1) return fail(h, PEAT_ERR_INVALID_ARG, "axis must be 0 (rows) or 1 (columns)");
+  if (rows < 0 || cols < 0) return fail(h, PEAT_ERR_INVALID_ARG, "rows or cols < 0");
+  if (rows > MAX_DIM || cols > MAX_DIM) return fail(h, PEAT_ERR_UNSUPPORTED, "rows or cols above 2^31 - 1");
+  if (ldx < cols) return fail(h, PEAT_ERR_INVALID_ARG, "ldx < cols");
+  if (q && ldq < (axis == 0 ? cols : rows)) return fail(h, PEAT_ERR_INVALID_ARG, "ldq is less than a row of q");
+  if (values && ldv < cols) return fail(h, PEAT_ERR_INVALID_ARG, "ldv < cols");
+  const bool any = rows > 0 && cols > 0;
+  if (any && !x) return fail(h, PEAT_ERR_INVALID_ARG, "x is NULL");
+  if (any && !q && !values) return fail(h, PEAT_ERR_INVALID_ARG, "q and values are both NULL");
+  if ((any && !aligned(x, B)) || (values && !aligned(values, B)) || (scale && !aligned(scale, 4)))
+    return fail(h, PEAT_ERR_INVALID_ARG, "a pointer is not aligned to its element type");
+  // nothing to write: no scale either
+  if ((axis == 0 ? rows : cols) == 0) return PEAT_OK;
+  DeviceGuard dg(h->device);
+  if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
+  const int E = 16 / B;
+  peat::QuantParams p;
+  p.x = x;
+  p.rows = rows;
+  p.cols = cols;
+  p.ldx = ldx;
+  p.q = q;
+  p.ldq = ldq;
+  p.scale = scale;
+  p.values = values;
+  p.ldv = ldv;
+  p.vec_x = aligned(x, 16) && (ldx % E == 0 || rows <= 1);
+  const int qa = axis == 0 ? E : 4;
+  p.vec_q = q && aligned(q, qa) && ldq % qa == 0;
+  p.vec_v = values && aligned(values, 16) && (ldv % E == 0 || rows <= 1);
+  cudaError_t e = peat::launch_quant8(dtype, axis, p, h->nsm, st);
+  if (e != cudaSuccess) return cuda_fail(h, e, "8-bit quantisation launch");
+  return PEAT_OK;
+}
+
+peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb,
+                     const float* sb, const float* bias, int64_t M, int64_t N, int64_t K, void* out, int64_t ldo,
+                     int out_dtype, cudaStream_t st) {
+  const int B = out_dtype == PEAT_OUT_I32 ? 4 : type_bytes(out_dtype);
+  if (!B) return fail(h, PEAT_ERR_INVALID_ARG, "out_dtype must be PEAT_F32, PEAT_F16, PEAT_BF16 or PEAT_OUT_I32");
+  if (M < 0 || N < 0 || K < 0) return fail(h, PEAT_ERR_INVALID_ARG, "M, N or K < 0");
+  if (K > 131071) return fail(h, PEAT_ERR_UNSUPPORTED, "K above 131071: the sums may not fit 32 bits");
+  if (lda < K || ldb < K || ldo < N) return fail(h, PEAT_ERR_INVALID_ARG, "lda, ldb or ldo is less than a row");
+  if (out_dtype == PEAT_OUT_I32 && (sa || sb || bias))
+    return fail(h, PEAT_ERR_INVALID_ARG, "PEAT_OUT_I32 takes no scales and no bias");
+  if (M == 0 || N == 0) return PEAT_OK;
+  // tiles are counted in 32 bits
+  if (M > MAX_DIM || N > MAX_DIM || ((M + 63) / 64) * ((N + 127) / 128) > ((int64_t)1 << 27))
+    return fail(h, PEAT_ERR_UNSUPPORTED, "the output is too large for one call");
+  if (!out) return fail(h, PEAT_ERR_INVALID_ARG, "out is NULL");
+  if (K > 0 && (!a || !b)) return fail(h, PEAT_ERR_INVALID_ARG, "a or b is NULL");
+  if (!aligned(out, B) || (sa && !aligned(sa, 4)) || (sb && !aligned(sb, 4)) || (bias && !aligned(bias, 4)))
+    return fail(h, PEAT_ERR_INVALID_ARG, "a pointer is not aligned to its element type");
+  DeviceGuard dg(h->device);
+  if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
+  peat::Mm8Params p;
+  p.a = a;
+  p.b = b;
+  p.lda = lda;
+  p.ldb = ldb;
+  p.sa = sa;
+  p.sb = sb;
+  p.bias = bias;
+  p.out = out;
+  p.ldo = ldo;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  cudaError_t e = peat::launch_mm8_direct(out_dtype, p, h->nsm, st);
+  if (e != cudaSuccess) return cuda_fail(h, e, "8-bit product launch");
+  return PEAT_OK;
+}
+
+peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count, int type, float unscale, bool clip,
+                        float max_norm, float eps, int bad, peat_gradnorm_t* result, float* norms, cudaStream_t st) {
+  if (count < 0 || (count > 0 && !list)) return fail(h, PEAT_ERR_INVALID_ARG, "count < 0, or list is NULL");
+  if (count > ((int64_t)1 << 24)) return fail(h, PEAT_ERR_UNSUPPORTED, "more than 2^24 tensors");
+  if (type != PEAT_NORM_2 && type != PEAT_NORM_1 && type != PEAT_NORM_INF)
+    return fail(h, PEAT_ERR_INVALID_ARG, "type must be one of peat_norm_t");
+  if (!(unscale > 0.0f) || !std::isfinite(unscale))
+    return fail(h, PEAT_ERR_INVALID_ARG, "unscale must be finite and > 0");
+  if (clip && !(max_norm >= 0.0f)) return fail(h, PEAT_ERR_INVALID_ARG, "max_norm must be >= 0");
+  if (clip && (!(eps >= 0.0f) || !std::isfinite(eps)))
+    return fail(h, PEAT_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (clip && bad != PEAT_BAD_PROPAGATE && bad != PEAT_BAD_ZERO && bad != PEAT_BAD_KEEP)
+    return fail(h, PEAT_ERR_INVALID_ARG, "bad must be one of peat_bad_t");
+  if (!result || !aligned(result, 8)) return fail(h, PEAT_ERR_INVALID_ARG, "result is NULL or not 8-byte aligned");
+  if (norms && !aligned(norms, 4)) return fail(h, PEAT_ERR_INVALID_ARG, "norms is not aligned");
+  int64_t units = 0;
+  for (int64_t t = 0; t < count; t++) {
+    const peat_grad_t& e = list[t];
+    const int B = type_bytes(e.dtype);
+    if (!B) return fail(h, PEAT_ERR_INVALID_ARG, "a tensor's dtype must be PEAT_F32, PEAT_F16 or PEAT_BF16");
+    if (e.n < 0 || e.reserved != 0) return fail(h, PEAT_ERR_INVALID_ARG, "a tensor's n < 0, or reserved not 0");
+    if (e.n > ((int64_t)1 << 40)) return fail(h, PEAT_ERR_UNSUPPORTED, "a tensor of more than 2^40 elements");
+    if (e.n == 0) continue;
+    if (!e.g || !aligned(e.g, B)) return fail(h, PEAT_ERR_INVALID_ARG, "a tensor's g is NULL or not aligned to its type");
+    if (clip && (!e.out || !aligned(e.out, B)))
+      return fail(h, PEAT_ERR_INVALID_ARG, "a tensor's out is NULL or not aligned to its type");
+    units += peat::gn_units(e.g, e.n, B);
+  }
+  // units * warps stays inside 64 bits
+  if (units > ((int64_t)1 << 44)) return fail(h, PEAT_ERR_UNSUPPORTED, "the list is too large");
+  DeviceGuard dg(h->device);
+  if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
+  OpsState* s = nullptr;
+  peat_status_t ps = ops_state(h, &s);
+  if (ps != PEAT_OK) return ps;
+
+  // one wave; a warp has at least 64 units
+  const int per = peat::gn_block() / 32;
+  const int64_t warps = std::max<int64_t>(1, std::min<int64_t>((units + 63) / 64, (int64_t)h->nsm * 4 * per));
+  const int nctas = (int)((warps + per - 1) / per);
+  const size_t listed = count > peat::GN_INLINE ? (sizeof(peat::GnEntry) * (size_t)count + 255) / 256 * 256 : 0;
+  ps = grow(h, &s->d_list, &s->d_list_cap, listed + sizeof(peat::GnPartial) * (size_t)(count + warps));
+  if (ps != PEAT_OK) return ps;
+
+  peat::GnInline in;
+  peat::GnEntry* dst = in.e;
+  int slot = -1;
+  if (listed) {
+    slot = s->next;
+    s->next = (s->next + 1) % OpsState::RING;
+    if (!s->taken[slot] && cudaEventCreateWithFlags(&s->taken[slot], cudaEventDisableTiming) != cudaSuccess) {
+      cudaGetLastError();
+      s->taken[slot] = nullptr;
+      return fail(h, PEAT_ERR_ALLOC, "operator staging allocation failed");
+    }
+    if (s->pending[slot]) {
+      cudaError_t e = cudaEventSynchronize(s->taken[slot]);
+      if (e != cudaSuccess) return cuda_fail(h, e, "cudaEventSynchronize");
+      s->pending[slot] = false;
+    }
+    if (listed > s->h_list_cap[slot]) {
+      if (s->h_list[slot]) cudaFreeHost(s->h_list[slot]);
+      s->h_list[slot] = nullptr;
+      s->h_list_cap[slot] = 0;
+      if (cudaMallocHost(&s->h_list[slot], listed) != cudaSuccess) {
+        cudaGetLastError();
+        s->h_list[slot] = nullptr;
+        return fail(h, PEAT_ERR_ALLOC, "operator staging allocation failed");
+      }
+      s->h_list_cap[slot] = listed;
+    }
+    dst = static_cast<peat::GnEntry*>(s->h_list[slot]);
+  }
+  units = 0;
+  for (int64_t t = 0; t < count; t++) {
+    const peat_grad_t& e = list[t];
+    dst[t] = peat::GnEntry{e.g, e.out, e.n, units, e.dtype, 0};
+    units += peat::gn_units(e.g, e.n, type_bytes(e.dtype));
+  }
+  if (listed) {
+    cudaError_t e = cudaMemcpyAsync(s->d_list, dst, sizeof(peat::GnEntry) * (size_t)count, cudaMemcpyHostToDevice, st);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemcpyAsync(list)");
+    e = cudaEventRecord(s->taken[slot], st);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cudaEventRecord");
+    s->pending[slot] = true;
+  }
+  peat::GnParams p;
+  p.list = listed ? static_cast<const peat::GnEntry*>(s->d_list) : nullptr;
+  p.count = (int)count;
+  p.units = units;
+  p.nwarps = (int)warps;
+  p.type = type;
+  p.unscale = unscale;
+  p.max_norm = max_norm;
+  p.eps = eps;
+  p.bad_mode = bad;
+  p.clip = clip ? 1 : 0;
+  p.parts = reinterpret_cast<peat::GnPartial*>(static_cast<char*>(s->d_list) + listed);
+  p.done = s->done;
+  p.result = result;
+  p.norms = norms;
+  cudaError_t e = peat::launch_gradnorm(p, in, nctas, st);
+  if (e == cudaSuccess && clip && units > 0) e = peat::launch_gradscale(p, in, nctas, st);
+  if (e != cudaSuccess) return cuda_fail(h, e, "gradient norm launch");
+  return PEAT_OK;
+}
+
+// nothing is thrown across the C boundary
+template <typename F>
+peat_status_t guarded(peat_handle_t h, F f) {
+  if (!h) return PEAT_ERR_INVALID_ARG;
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return PEAT_ERR_ALLOC;
+  } catch (...) {
+    return PEAT_ERR_INTERNAL;
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+peat_status_t peat_quantize_i8(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx,
+                               peat_dtype_t dtype, int axis, int8_t* q, int64_t ldq, float* scale, void* values,
+                               int64_t ldv, peat_stream_t stream) {
+  return guarded(h, [&] {
+    return quantize(h, x, rows, cols, ldx, dtype, axis, q, ldq, scale, values, ldv,
+                    reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+peat_status_t peat_matmul_i8(peat_handle_t h, const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b,
+                             int64_t ldb, const float* b_scale, const float* bias, int64_t M, int64_t N, int64_t K,
+                             void* out, int64_t ldo, int out_dtype, peat_stream_t stream) {
+  return guarded(h, [&] {
+    return matmul(h, a, lda, a_scale, b, ldb, b_scale, bias, M, N, K, out, ldo, out_dtype,
+                  reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+peat_status_t peat_grad_norm(peat_handle_t h, const peat_grad_t* list, int64_t count, peat_norm_t type,
+                             float unscale, peat_gradnorm_t* result, float* norms, peat_stream_t stream) {
+  return guarded(h, [&] {
+    return grad_pass(h, list, count, type, unscale, false, 0.0f, 0.0f, PEAT_BAD_PROPAGATE, result, norms,
+                     reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+peat_status_t peat_grad_clip(peat_handle_t h, const peat_grad_t* list, int64_t count, peat_norm_t type,
+                             float unscale, float max_norm, float eps, peat_bad_t bad, peat_gradnorm_t* result,
+                             float* norms, peat_stream_t stream) {
+  return guarded(h, [&] {
+    return grad_pass(h, list, count, type, unscale, true, max_norm, eps, bad, result, norms,
+                     reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+}  // extern "C"

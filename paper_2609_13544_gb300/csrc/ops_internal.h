@@ -1,0 +1,82 @@
+// Internal declarations of the playback operators (include/peat_ops.h).
+#pragma once
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "peat.h"
+#include "peat_ops.h"
+
+namespace peat {
+
+// ---- 8-bit quantisation (quant8.cu) ----
+struct QuantParams {
+  const void* x;
+  int64_t rows, cols, ldx;
+  int8_t* q;  // or null
+  int64_t ldq;
+  float* scale;   // or null
+  void* values;  // or null
+  int64_t ldv;
+  int vec_x;  // x's rows start on 16-byte boundaries
+  int vec_q;  // q's rows start on boundaries of a vector's integers (axis 0: 8 or 4 bytes; axis 1: 4 bytes)
+  int vec_v;  // values' rows start on 16-byte boundaries
+};
+cudaError_t launch_quant8(int dtype, int axis, const QuantParams& p, int nsm, cudaStream_t s);
+
+// ---- 8-bit products (matmul8.cu) ----
+struct Mm8Params {
+  const int8_t* a;  // [M, K]
+  const int8_t* b;  // [N, K]
+  int64_t lda, ldb;
+  const float* sa;    // or null
+  const float* sb;    // or null
+  const float* bias;  // or null
+  void* out;
+  int64_t ldo;
+  int64_t M, N, K;
+};
+cudaError_t launch_mm8_direct(int out_dtype, const Mm8Params& p, int nsm, cudaStream_t s);
+
+// ---- gradient lists (gradnorm.cu) ----
+struct GnEntry {
+  const void* g;
+  void* out;
+  int64_t n;
+  int64_t unit0;  // the list's 16-byte units before this tensor's
+  int32_t dtype, pad;
+};
+constexpr int GN_INLINE = 96;  // entries that travel as a kernel argument (40 bytes each, below 4 KB)
+struct GnInline {
+  GnEntry e[GN_INLINE];
+};
+struct GnPartial {
+  double s;          // sum (or maximum) of the piece
+  unsigned int bad;  // its NaN and infinite elements
+  unsigned int nan;  // of them, NaN
+};
+struct GnParams {
+  const GnEntry* list;  // device; null: the inline entries
+  int count;
+  int64_t units;        // of the whole list
+  int nwarps;           // warps of the norm pass
+  int type;             // peat_norm_t
+  float unscale, max_norm, eps;
+  int bad_mode;
+  int clip;             // 0: norm only
+  GnPartial* parts;     // count + nwarps slots: warp w's part of tensor t at t + w
+  unsigned int* done;   // CTAs finished, zero between calls
+  peat_gradnorm_t* result;
+  float* norms;         // or null
+};
+int gn_block();  // threads of a CTA of both passes
+cudaError_t launch_gradnorm(const GnParams& p, const GnInline& in, int nctas, cudaStream_t s);
+cudaError_t launch_gradscale(const GnParams& p, const GnInline& in, int nctas, cudaStream_t s);
+// 16-byte units that hold the n elements of `size` bytes at g
+inline int64_t gn_units(const void* g, int64_t n, int size) {
+  if (n <= 0) return 0;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(g);
+  return (int64_t)((a + (uint64_t)n * size + 15) / 16 - a / 16);
+}
+
+}  // namespace peat

@@ -1,0 +1,299 @@
+"""Binding of the playback operators (include/peat_ops.h), and a linear layer made of them.
+
+``peat_quantize_i8`` and ``peat_matmul_i8`` are a linear layer's products in
+8-bit integers with a scale for each row of either operand; ``peat_grad_norm``
+and ``peat_grad_clip`` the norm over a list of gradient tensors and their
+clipping.  As in the rest of the binding, a ``_raw`` function fills outputs
+that the caller holds; the plain ones allocate them.  All of them only enqueue
+work on the stream (``peat_grad_norm`` and ``peat_grad_clip``, which return
+host numbers, wait for it).
+
+``Linear8`` is the layer as a playback step replays it (Alg. 1's Fwd, InGrad
+and WgGrad at a lower precision): the weight held in 8 bits, the recorded
+tensors rounded on the way in.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+from typing import Optional, Sequence
+
+OUT_I32 = 100
+GRADNORM_BYTES = 16
+NORM_TYPES = {"2": 0, "1": 1, "inf": 2}
+BAD_MODES = {"propagate": 0, "zero": 1, "keep": 2}
+
+OPS_EXPORTS = ("peat_quantize_i8", "peat_matmul_i8", "peat_grad_norm", "peat_grad_clip")
+
+
+class GradEntry(ctypes.Structure):
+    _fields_ = [("g", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+def register(L) -> None:
+    """Argument types of the entry points in a loaded library."""
+    vp, i64, i32, f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
+    L.peat_quantize_i8.argtypes = [vp, vp, i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp]
+    L.peat_matmul_i8.argtypes = [vp, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i64, i32, vp]
+    L.peat_grad_norm.argtypes = [vp, vp, i64, i32, f32, vp, vp, vp]
+    L.peat_grad_clip.argtypes = [vp, vp, i64, i32, f32, f32, f32, i32, vp, vp, vp]
+    for name in OPS_EXPORTS:
+        getattr(L, name).restype = i32
+
+
+def _call(h, name, *args) -> None:
+    from . import _check, load
+    _check(getattr(load(), name)(h.ptr, *args), h)
+
+
+def _stream(h, stream) -> int:
+    import torch
+    return (torch.cuda.current_stream(h.device) if stream is None else stream).cuda_stream
+
+
+def _on(stream):
+    """Allocations belong to the stream that the call runs on."""
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _code(t) -> int:
+    import torch
+    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}: float32, float16 or bfloat16")
+    return code
+
+
+def _matrix(h, t, name: str) -> int:
+    """The row distance of a matrix whose rows are contiguous, on the handle's device."""
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions")
+    if not t.is_cuda or t.device.index != h.device:
+        raise ValueError(f"{name} must be a CUDA tensor on the handle's device")
+    rows, cols = t.shape
+    s0, s1 = t.stride()
+    if cols > 1 and s1 != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    if rows <= 1:
+        return cols
+    if s0 < cols:
+        raise ValueError(f"the rows of {name} overlap")
+    return s0
+
+
+def _vector(h, t, n: int, name: str) -> Optional[int]:
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda or \
+            t.device.index != h.device:
+        raise ValueError(f"{name} must be a contiguous float32 tensor of {n} elements on the handle's device")
+    return t.data_ptr()
+
+
+def _padded(rows: int, cols: int, device):
+    """An int8 matrix whose rows start on 16-byte boundaries, as the products read them fastest."""
+    import torch
+    return torch.empty(rows, (cols + 15) // 16 * 16, dtype=torch.int8, device=device)[:, :cols]
+
+
+def peat_quantize_i8_raw(h, x, axis: int, q=None, scale=None, values=None, stream=None) -> None:
+    """peat_quantize_i8 on preallocated device outputs: q int8 (axis 0: x's shape, axis 1: transposed), scale
+    float32 [rows or cols], values (x's shape and type); each may be None, but not both of q and values."""
+    import torch
+    ldx = _matrix(h, x, "x")
+    rows, cols = x.shape
+    ldq = ldv = 0
+    if q is not None:
+        ldq = _matrix(h, q, "q")
+        if q.dtype != torch.int8 or tuple(q.shape) != ((rows, cols) if axis == 0 else (cols, rows)):
+            raise ValueError("q must be int8 of x's shape (axis 0) or its transpose (axis 1)")
+    if values is not None:
+        ldv = _matrix(h, values, "values")
+        if values.dtype != x.dtype or values.shape != x.shape:
+            raise ValueError("values must have x's shape and type")
+    _call(h, "peat_quantize_i8", x.data_ptr(), rows, cols, ldx, _code(x), axis, None if q is None else q.data_ptr(),
+          ldq, _vector(h, scale, cols if axis else rows, "scale"), None if values is None else values.data_ptr(), ldv,
+          _stream(h, stream))
+
+
+def peat_quantize_i8(h, x, axis: int = 0, stream=None):
+    """x as 8-bit integers with a scale for each row (axis 0) or column (axis 1): (q, scale), for axis 1 q
+    transposed.  q's rows are padded to 16 bytes (a view)."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x must have two dimensions")
+    rows, cols = x.shape if axis == 0 else (x.shape[1], x.shape[0])
+    with _on(stream):
+        q = _padded(rows, cols, x.device)
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+        peat_quantize_i8_raw(h, x, axis, q, scale, None, stream)
+    return q, scale
+
+
+def peat_matmul_i8_raw(h, a, a_scale, b, b_scale, out, bias=None, stream=None) -> None:
+    """peat_matmul_i8 into out [M, N] (float32, float16, bfloat16, or int32 for the sums themselves) from a [M, K]
+    and b [N, K] int8 with their scales (None: 1)."""
+    import torch
+    lda, ldb, ldo = _matrix(h, a, "a"), _matrix(h, b, "b"), _matrix(h, out, "out")
+    (M, K), N = a.shape, b.shape[0]
+    if a.dtype != torch.int8 or b.dtype != torch.int8:
+        raise TypeError("a and b must be int8")
+    if b.shape[1] != K:
+        raise ValueError("a and b differ in their row length")
+    if tuple(out.shape) != (M, N):
+        raise ValueError("out must be [rows of a, rows of b]")
+    _call(h, "peat_matmul_i8", a.data_ptr(), lda, _vector(h, a_scale, M, "a_scale"), b.data_ptr(), ldb,
+          _vector(h, b_scale, N, "b_scale"), _vector(h, bias, N, "bias"), M, N, K, out.data_ptr(), ldo,
+          OUT_I32 if out.dtype == torch.int32 else _code(out), _stream(h, stream))
+
+
+def peat_matmul_i8(h, a, a_scale, b, b_scale, bias=None, out_dtype=None, stream=None):
+    """(sum over k of a[m, k] b[n, k]) a_scale[m] b_scale[n] + bias[n] as out_dtype (float32 unless given)."""
+    import torch
+    with _on(stream):
+        out = torch.empty(a.shape[0], b.shape[0], dtype=out_dtype or torch.float32, device=a.device)
+        peat_matmul_i8_raw(h, a, a_scale, b, b_scale, out, bias, stream)
+    return out
+
+
+class GradList:
+    """A list of gradient tensors (and, for clipping, of as many output tensors; None: in place), made once and
+    passed to every peat_grad_norm or peat_grad_clip.  It holds the tensors: where a program gives a parameter a
+    new gradient tensor, it makes a new list."""
+
+    def __init__(self, tensors: Sequence, outs: Optional[Sequence] = None):
+        import torch
+        self.tensors = list(tensors)
+        self.outs = self.tensors if outs is None else list(outs)
+        if len(self.outs) != len(self.tensors):
+            raise ValueError("as many outputs as tensors are needed")
+        self.entries = (GradEntry * max(len(self.tensors), 1))()
+        self.device = self.tensors[0].device if self.tensors else None
+        for i, (t, o) in enumerate(zip(self.tensors, self.outs)):
+            code = _code(t)
+            if not t.is_cuda or t.device != self.device or o.device != self.device:
+                raise ValueError("gradients and outputs must be CUDA tensors on one device")
+            if o.dtype != t.dtype or o.shape != t.shape:
+                raise ValueError("an output differs from its gradient in type or shape")
+            dense = t.is_contiguous() or (t.dim() == 4 and t.is_contiguous(memory_format=torch.channels_last))
+            if not dense or (o is not t and o.stride() != t.stride()):
+                raise ValueError("gradients must be contiguous (or channels-last), outputs of the same layout")
+            self.entries[i] = GradEntry(t.data_ptr(), o.data_ptr(), t.numel(), code, 0)
+
+    def __len__(self) -> int:
+        return len(self.tensors)
+
+
+def _grad_args(h, grads, record, norms):
+    import torch
+    if not isinstance(grads, GradList):
+        grads = GradList(grads)
+    if len(grads) and grads.device.index != h.device:
+        raise ValueError("the gradients must be on the handle's device")
+    if record.numel() * record.element_size() < GRADNORM_BYTES or not record.is_cuda or not record.is_contiguous() \
+            or record.device.index != h.device:
+        raise ValueError("record must be a contiguous CUDA tensor of 16 bytes on the handle's device")
+    if norms is not None and (norms.dtype != torch.float32 or norms.numel() < len(grads)):
+        raise ValueError("norms must be float32, one element for each tensor")
+    return grads, None if norms is None else _vector(h, norms, norms.numel(), "norms")
+
+
+def peat_grad_norm_raw(h, grads, record, norms=None, norm_type: str = "2", unscale: float = 1.0, stream=None) -> None:
+    """peat_grad_norm of a GradList (or a list of tensors) into record (16 bytes: float32 norm, float32 1, uint64
+    count of NaN and infinite elements) and norms (float32, one a tensor, or None)."""
+    grads, np_ = _grad_args(h, grads, record, norms)
+    _call(h, "peat_grad_norm", grads.entries, len(grads), NORM_TYPES[norm_type], unscale, record.data_ptr(), np_,
+          _stream(h, stream))
+
+
+def peat_grad_clip_raw(h, grads, max_norm: float, record, norms=None, norm_type: str = "2", unscale: float = 1.0,
+                       eps: float = 1e-6, bad: str = "propagate", stream=None) -> None:
+    """peat_grad_clip of a GradList (or, in place, of a list of tensors); record and norms as in peat_grad_norm_raw,
+    record's second float32 the clipping factor."""
+    grads, np_ = _grad_args(h, grads, record, norms)
+    _call(h, "peat_grad_clip", grads.entries, len(grads), NORM_TYPES[norm_type], unscale, max_norm, eps,
+          BAD_MODES[bad], record.data_ptr(), np_, _stream(h, stream))
+
+
+def _grad_record(record, norms, stream) -> dict:
+    from . import _sync
+    import torch
+    _sync(stream)
+    r = record.cpu()
+    f = r.view(torch.float32)
+    return {"norm": f[0].item(), "coef": f[1].item(), "n_bad": r.view(torch.int64)[1].item(),
+            "norms": norms.cpu().numpy()}
+
+
+def _grad_outputs(h, grads):
+    import torch
+    dev = torch.device("cuda", h.device)
+    return (torch.empty(GRADNORM_BYTES, dtype=torch.uint8, device=dev),
+            torch.empty(len(grads), dtype=torch.float32, device=dev))
+
+
+def peat_grad_norm(h, grads, norm_type: str = "2", unscale: float = 1.0, stream=None) -> dict:
+    """Norm of unscale * g over all tensors: dict of norm, n_bad (NaN and infinite elements), coef (1) and norms
+    (numpy float32, one a tensor); synchronises."""
+    with _on(stream):
+        record, norms = _grad_outputs(h, grads)
+        peat_grad_norm_raw(h, grads, record, norms, norm_type, unscale, stream)
+        return _grad_record(record, norms, stream)
+
+
+def peat_grad_clip(h, grads, max_norm: float, norm_type: str = "2", unscale: float = 1.0, eps: float = 1e-6,
+                   bad: str = "propagate", stream=None) -> dict:
+    """Scales the tensors by unscale * min(1, max_norm / (norm + eps)), in place or into the GradList's outputs;
+    the dict of peat_grad_norm with the factor as coef; synchronises."""
+    with _on(stream):
+        record, norms = _grad_outputs(h, grads)
+        peat_grad_clip_raw(h, grads, max_norm, record, norms, norm_type, unscale, eps, bad, stream)
+        return _grad_record(record, norms, stream)
+
+
+class Linear8:
+    """y = x w^T with w [out, in] held in 8-bit integers, by row for the forward product and by column for the
+    input gradient; x and the output gradient are rounded as they come (by row, or, for the weight gradient, by
+    column).  Inputs are float32, float16 or bfloat16 with any leading dimensions; the layer keeps none of them."""
+
+    def __init__(self, h, weight, stream=None):
+        self.h = h
+        self.out_features, self.in_features = weight.shape
+        self.q, self.scale = peat_quantize_i8(h, weight, 0, stream)
+        self.qt, self.scale_t = peat_quantize_i8(h, weight, 1, stream)
+
+    def _rows(self, t, width: int, name: str):
+        if t.dim() < 1 or t.shape[-1] != width:
+            raise ValueError(f"the last dimension of {name} must be {width}")
+        return t.reshape(-1, width)
+
+    def forward(self, x, bias=None, stream=None):
+        """x [..., in] -> [..., out] of x's type."""
+        with _on(stream):
+            q, s = peat_quantize_i8(self.h, self._rows(x, self.in_features, "x"), 0, stream)
+            y = peat_matmul_i8(self.h, q, s, self.q, self.scale, bias, x.dtype, stream)
+        return y.view(*x.shape[:-1], self.out_features)
+
+    def input_grad(self, grad, stream=None):
+        """dL/dx [..., in] of grad's type from grad = dL/dy [..., out]."""
+        with _on(stream):
+            q, s = peat_quantize_i8(self.h, self._rows(grad, self.out_features, "grad"), 0, stream)
+            g = peat_matmul_i8(self.h, q, s, self.qt, self.scale_t, None, grad.dtype, stream)
+        return g.view(*grad.shape[:-1], self.in_features)
+
+    def weight_grad(self, grad, x, stream=None):
+        """dL/dw [out, in] in float32 from grad [..., out] and x [..., in]."""
+        with _on(stream):
+            g, x = self._rows(grad, self.out_features, "grad"), self._rows(x, self.in_features, "x")
+            if g.shape[0] != x.shape[0]:
+                raise ValueError("grad and x differ in their leading dimensions")
+            qg, sg = peat_quantize_i8(self.h, g, 1, stream)
+            qx, sx = peat_quantize_i8(self.h, x, 1, stream)
+            return peat_matmul_i8(self.h, qg, sg, qx, sx, None, None, stream)
+
+    def backward(self, grad, x, stream=None):
+        """(dL/dx, dL/dw)."""
+        return self.input_grad(grad, stream), self.weight_grad(grad, x, stream)
