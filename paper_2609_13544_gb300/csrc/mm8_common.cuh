@@ -35,6 +35,7 @@ __device__ __forceinline__ uint4 load16(const int8_t* p, int64_t left, const int
     v.w = __funnelshift_r(w3, w4, 8 * mis);
   } else {  // the tensor's first and last bytes
     uint32_t t[4] = {0, 0, 0, 0};
+#pragma unroll
     for (int i = 0; i < 16; i++)
       if (i < left) t[i >> 2] |= (uint32_t)(uint8_t)p[i] << (8 * (i & 3));
     v = make_uint4(t[0], t[1], t[2], t[3]);

@@ -1,0 +1,555 @@
+// 8-bit integer products on the fifth-generation tensor cores: many rows.
+//
+// The integers are laid out as binary16 once per call (pack), in the very
+// image that the matrix instruction reads from shared memory: blocks of 128
+// rows by 64 k, 128-byte rows with their 16-byte pieces swizzled, so that a
+// block is one contiguous 16 KB that a TMA copy moves as it lies, and ragged
+// edges are zeros that pack wrote.  Converting inside the product instead would
+// move every block through shared memory twice more than the instruction reads
+// it, and shared memory bandwidth is what the instruction runs against.
+//
+// A cluster of two CTAs makes a tile of 256 x 256 (cta_group::2: each holds
+// 128 rows of a and 128 of b, and the accumulators of its rows), persistent
+// over the tiles.  Warp roles: one thread issues the copies, one (of the even
+// CTA) the matrix instructions, eight warps turn accumulators into results
+// while the other half of the 512 accumulator columns fills.
+//
+// Exactness: float32 holds a sum of products exactly while it stays below
+// 2^24.  pack leaves for every block of 128 rows and 256 k the largest 2-norm
+// of a row; by Cauchy and Schwarz the product of two such norms bounds every
+// partial sum over those 256 k, and the accumulator is drained to int32
+// before the bounds add up to 2^23.  Full-range integers drain every 512 k,
+// normally distributed ones about every 8000.
+#include <cooperative_groups.h>
+#include <cuda.h>
+
+#include "mm8_common.cuh"
+#include "peat_internal.h"
+
+namespace cg = cooperative_groups;
+
+namespace peat {
+namespace {
+
+constexpr int BLK = 128 * 64 * 2;  // bytes of a packed block
+constexpr int KN = 256;            // k of one norm
+
+// ---------------------------------------------------------------------------
+// pack
+// ---------------------------------------------------------------------------
+struct PackParams {
+  const int8_t* x[2];
+  int64_t ld[2], rows[2];
+  __half* out[2];
+  float* norm[2];
+  int64_t K;
+  int kb, kc;        // blocks of 64 and 256 k
+  int64_t first_b;   // CTAs of the first matrix
+};
+
+template <int MODE>
+__global__ void __launch_bounds__(256) mm8_pack(PackParams p) {
+  pdl_trigger();
+  const int which = blockIdx.x >= p.first_b;
+  const int64_t at = blockIdx.x - (which ? p.first_b : 0);
+  const int64_t rb = at / p.kc;
+  const int kc = (int)(at - rb * p.kc);
+  const int8_t* x = which ? p.x[1] : p.x[0];
+  const int64_t ld = which ? p.ld[1] : p.ld[0], rows = which ? p.rows[1] : p.rows[0];
+  const int8_t *lo = x, *hi = x + (rows - 1) * ld + p.K;
+  const int l = threadIdx.x & 15, kb = kc * 4 + (l >> 2);
+  const int64_t k = (int64_t)kc * KN + l * 16, left = p.K - k;
+  char* out = reinterpret_cast<char*>(which ? p.out[1] : p.out[0]) + (rb * p.kb + kb) * (int64_t)BLK;
+  uint4 v[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    const int64_t row = rb * 128 + (threadIdx.x >> 4) + 16 * i;
+    v[i] = load16<MODE>(x + row * ld + k, row < rows ? left : 0, lo, hi);
+  }
+  int most = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    const int r = (threadIdx.x >> 4) + 16 * i;
+    int ss = __dp4a((int)v[i].x, (int)v[i].x, 0);
+    ss = __dp4a((int)v[i].y, (int)v[i].y, ss);
+    ss = __dp4a((int)v[i].z, (int)v[i].z, ss);
+    ss = __dp4a((int)v[i].w, (int)v[i].w, ss);
+#pragma unroll
+    for (int o = 8; o; o /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+    most = max(most, ss);
+    if (kb < p.kb) {
+      uint4 a, b;  // the first and the second 8 of the 16
+      to_half(v[i].x, a.x, a.y);
+      to_half(v[i].y, a.z, a.w);
+      to_half(v[i].z, b.x, b.y);
+      to_half(v[i].w, b.z, b.w);
+      uint4* d = reinterpret_cast<uint4*>(out + r * 128 + (((l & 3) * 2) ^ (r & 6)) * 16);
+      d[0] = r & 1 ? b : a;
+      d[1] = r & 1 ? a : b;
+    }
+  }
+  most = __reduce_max_sync(0xffffffffu, most);
+  __shared__ int part[8];
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+#pragma unroll
+    for (int w = 1; w < 8; w++) most = max(most, part[w]);
+    (which ? p.norm[1] : p.norm[0])[rb * p.kc + kc] = sqrtf((float)most) * 1.00001f;  // (rounded up)
+  }
+}
+
+// ---------------------------------------------------------------------------
+// product
+// ---------------------------------------------------------------------------
+constexpr int STAGES = 6, STAGE = 2 * BLK;  // a CTA's block of a and block of b
+constexpr int EPI_WARPS = 8, THREADS = (EPI_WARPS + 2) * 32;
+constexpr int EPI_BYTES = EPI_WARPS * 32 * 33 * 4;
+constexpr int BARS = 512;
+constexpr int SMEM = STAGES * STAGE + EPI_BYTES + BARS + 1024;
+constexpr float LIMIT = 8388608.0f;  // 2^23
+
+struct TcParams {
+  Mm8Params m;
+  const float* na;  // norms [row blocks][kc]
+  const float* nb;
+  int kb, kc;
+  int mt, nt;       // tiles
+  int splits;       // parts of the k range of a tile
+  int* sums;        // splits > 1: 256 x 256 int32 for each tile, zero between calls
+  unsigned int* tickets;  // splits > 1: one for each result warp of a tile, zero between calls
+  unsigned int* status;
+  uint32_t wait_limit;
+};
+
+__device__ __forceinline__ uint32_t sptr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// arrive on a barrier of the cluster (an address of mapa)
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+// waits for the barrier's phase of this parity; false after `limit` polls
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit) {
+  for (uint32_t i = 0; i < limit; i++) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        " selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    if (ok) return true;
+  }
+  return false;
+}
+// a block into this CTA's shared memory, its bytes counted on the even CTA's barrier
+__device__ __forceinline__ void tma_block(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, "
+      "%3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(row), "r"(bar)
+      : "memory");
+}
+// shared-memory descriptor of a block: K-major, 128-byte swizzle, 8-row groups 1024 bytes apart
+__device__ __forceinline__ uint64_t block_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) |
+         ((uint64_t)2 << 61);
+}
+// float32 accumulators, binary16 operands, both K-major, 256 x 256
+constexpr uint32_t IDESC = (1u << 4) | ((256u / 8) << 17) | ((256u / 16) << 24);
+__device__ __forceinline__ void mma_256(uint32_t d, uint64_t a, uint64_t b, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(IDESC), "r"(accumulate)
+      : "memory");
+}
+// arrives on the barrier at this offset in both CTAs once the instructions issued so far are done
+__device__ __forceinline__ void commit_both(uint32_t bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+      "h"((uint16_t)3)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+      "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(addr));
+}
+
+struct Unit {
+  int mt, nt, tile;
+  int k0, k1;  // blocks of 64 k
+};
+__device__ __forceinline__ Unit unit_at(const TcParams& p, int u) {
+  Unit r;
+  r.tile = u / p.splits;
+  const int s = u - r.tile * p.splits;
+  r.nt = r.tile / p.mt;
+  r.mt = r.tile - r.nt * p.mt;
+  r.k0 = (int)((int64_t)p.kb * s / p.splits);
+  r.k1 = (int)((int64_t)p.kb * (s + 1) / p.splits);
+  return r;
+}
+// the bound of a tile's partial sums over norm block kc (0 past the end)
+__device__ __forceinline__ float bound_of(const TcParams& p, const Unit& t, int kc) {
+  if (kc * 4 >= t.k1) return 0.0f;
+  const float* a = p.na + (int64_t)t.mt * 2 * p.kc + kc;
+  const float* b = p.nb + (int64_t)t.nt * 2 * p.kc + kc;
+  return __fmul_rn(fmaxf(__ldcg(a), __ldcg(a + p.kc)), fmaxf(__ldcg(b), __ldcg(b + p.kc)));
+}
+// Which of 32 norm blocks (lane i holds block i's bound) the accumulator is
+// drained before; `run` is the bound of what it holds, and is carried on.  The
+// instruction warp and the result warps each work this out, so every rounding
+// is spelled out.
+__device__ __forceinline__ uint32_t drains(float mine, float& run) {
+  float all = mine;
+#pragma unroll
+  for (int o = 16; o; o /= 2) all = __fadd_rn(all, __shfl_xor_sync(0xffffffffu, all, o));
+  if (__fadd_rn(run, all) <= LIMIT) {
+    run = __fadd_rn(run, all);
+    return 0;
+  }
+  uint32_t mask = 0;
+  for (int i = 0; i < 32; i++) {
+    const float b = __shfl_sync(0xffffffffu, mine, i);
+    const float sum = __fadd_rn(run, b);
+    if (sum > LIMIT) {
+      if (run > 0.0f) mask |= 1u << i;
+      run = b;
+    } else {
+      run = sum;
+    }
+  }
+  return mask;
+}
+
+template <int OUT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+    mm8_tc(TcParams p, const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb) {
+  extern __shared__ char raw[];
+  char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  int* stage_out = reinterpret_cast<int*>(smem + STAGES * STAGE);
+  const uint32_t bars = sptr(smem + STAGES * STAGE + EPI_BYTES);
+  const uint32_t full = bars, empty = bars + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 16,
+                 last = acc_empty + 16;
+  volatile uint32_t* shared_words = reinterpret_cast<volatile uint32_t*>(smem + STAGES * STAGE + EPI_BYTES + 256);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t rank;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int units = p.mt * p.nt * p.splits, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < STAGES; i++) {
+      mbar_init(full + 8 * i, 1);   // the even CTA's copier; plus the bytes of both
+      mbar_init(empty + 8 * i, 1);  // a commit
+    }
+    for (int i = 0; i < 2; i++) {
+      mbar_init(acc_full + 8 * i, 1);
+      mbar_init(acc_empty + 8 * i, 2 * EPI_WARPS);
+    }
+    mbar_init(last, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == EPI_WARPS + 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sptr((const void*)shared_words))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  cg::this_cluster().sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = shared_words[0];
+  pdl_wait();
+
+  bool ok = true;
+  if (warp == EPI_WARPS) {  // copies
+    if (lane == 0) {
+      int seq = 0;
+      for (int u = first; u < units && ok; u += step) {
+        const Unit t = unit_at(p, u);
+        const int ra = (t.mt * 2 + (int)rank) * p.kb, rb = (t.nt * 2 + (int)rank) * p.kb;
+        for (int k = t.k0; k < t.k1; k++, seq++) {
+          const int s = seq % STAGES;
+          if (!(ok = mbar_wait(empty + 8 * s, (seq / STAGES & 1) ^ 1, p.wait_limit))) break;
+          const uint32_t dst = sptr(smem + s * STAGE), bar = mapa(full + 8 * s, 0);
+          if (rank == 0) mbar_expect(full + 8 * s, 2 * STAGE);
+          tma_block(dst, &ma, (ra + k) * 128, bar);
+          tma_block(dst + BLK, &mb, (rb + k) * 128, bar);
+        }
+      }
+      // a stage's copies have landed when its instructions are done with it
+      for (int i = 0; i < STAGES && i < seq; i++) {
+        const int q = seq - 1 - i;
+        mbar_wait(empty + 8 * (q % STAGES), q / STAGES & 1, p.wait_limit);
+      }
+    }
+  } else if (warp == EPI_WARPS + 1) {  // matrix instructions
+    if (rank == 0) {
+      int seq = 0, chunk = 0;
+      Unit t = unit_at(p, first);
+      float mine = first < units ? bound_of(p, t, t.k0 / 4 + lane) : 0.0f;
+      for (int u = first; u < units && ok; u += step) {
+        const Unit now = t;
+        float run = 0.0f;
+        uint32_t mask = drains(mine, run);
+        if (u + step < units) {  // the next tile's bounds are on their way meanwhile
+          t = unit_at(p, u + step);
+          mine = bound_of(p, t, t.k0 / 4 + lane);
+        }
+        const int c0 = now.k0 / 4;
+        bool fresh = true;  // the accumulator starts anew
+        for (int k = now.k0; k < now.k1 && ok; k++, seq++) {
+          const int c = k / 4 - c0;
+          if ((k & 3) == 0 && c > 0 && (c & 31) == 0) mask = drains(bound_of(p, now, k / 4 + lane), run);
+          if ((k == now.k0 || (k & 3) == 0) && (mask >> (c & 31) & 1)) {
+            if (lane == 0) commit_both(acc_full + 8 * (chunk & 1));
+            chunk++;
+            fresh = true;
+          }
+          if (fresh) {
+            ok = mbar_wait(acc_empty + 8 * (chunk & 1), (chunk / 2 & 1) ^ 1, p.wait_limit);
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          }
+          const int s = seq % STAGES;
+          ok = ok && mbar_wait(full + 8 * s, seq / STAGES & 1, p.wait_limit);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          if (lane == 0) {
+            const uint32_t d = tmem + (chunk & 1) * 256, base = sptr(smem + s * STAGE);
+            const uint64_t a = block_desc(base), b = block_desc(base + BLK);
+#pragma unroll
+            for (int i = 0; i < 4; i++) mma_256(d, a + 2 * i, b + 2 * i, !(fresh && i == 0));
+            commit_both(empty + 8 * s);
+          }
+          __syncwarp();
+          fresh = false;
+        }
+        if (ok && lane == 0) commit_both(acc_full + 8 * (chunk & 1));
+        chunk++;
+      }
+      // whatever was issued is done before the accumulators are given back
+      if (lane == 0) {
+        commit_both(last);
+        mbar_wait(last, 0, p.wait_limit);
+      }
+      __syncwarp();
+    }
+  } else {  // results: a warp has 32 rows and half of the columns
+    int chunk = 0;
+    const int half = warp >> 2, quarter = warp & 3;
+    int* mine = stage_out + warp * 32 * 33;
+    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
+    const uint32_t release0 = mapa(acc_empty, 0);
+    typename Mm8Out<OUT>::T* out = static_cast<typename Mm8Out<OUT>::T*>(p.m.out);
+    for (int u = first; u < units && ok; u += step) {
+      const Unit t = unit_at(p, u);
+      int acc[128];
+      // pieces that the accumulator is drained in
+      int pieces = 1;
+      {
+        float run = 0.0f;
+        for (int c = t.k0 / 4; c * 4 < t.k1; c += 32) pieces += __popc(drains(bound_of(p, t, c + lane), run));
+      }
+      for (int q = 0; q < pieces; q++, chunk++) {
+        if (!(ok = mbar_wait(acc_full + 8 * (chunk & 1), chunk / 2 & 1, p.wait_limit))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+          uint32_t v[32];
+          tmem_load32(taddr + (chunk & 1) * 256 + g * 32, v);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+          for (int i = 0; i < 32; i++) {
+            const int x = __float2int_rn(__uint_as_float(v[i]));
+            acc[g * 32 + i] = q ? acc[g * 32 + i] + x : x;
+          }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(release0 + 8 * (chunk & 1));
+      }
+      if (!ok) break;
+      if (p.splits > 1) {
+        // integer sums meet in global memory (their order does not matter); the last to come takes the total
+        const int64_t part = ((int64_t)t.tile * 2 + rank) * EPI_WARPS + warp;
+        int* sums = p.sums + part * (32 * 128) + lane;
+#pragma unroll
+        for (int i = 0; i < 128; i++) atomicAdd(sums + i * 32, acc[i]);
+        __threadfence();
+        __syncwarp();
+        unsigned int n = 0;
+        if (lane == 0) {
+          n = atomicAdd(p.tickets + part, 1u);
+          if (n == (unsigned)p.splits - 1) p.tickets[part] = 0;
+        }
+        if (__shfl_sync(0xffffffffu, n, 0) != (unsigned)p.splits - 1) continue;
+        __threadfence();
+#pragma unroll
+        for (int i = 0; i < 128; i++) {
+          acc[i] = __ldcg(sums + i * 32);
+          __stcg(sums + i * 32, 0);
+        }
+      }
+      const int64_t row0 = (int64_t)t.mt * 256 + rank * 128 + quarter * 32;
+      const int64_t col0 = (int64_t)t.nt * 256 + half * 128;
+      const float sa = p.m.sa && row0 + lane < p.m.M ? __ldg(p.m.sa + row0 + lane) : 1.0f;
+      const int rows = (int)min((int64_t)32, p.m.M - row0);
+#pragma unroll
+      for (int g = 0; g < 4; g++) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 32; i++) mine[lane * 33 + i] = acc[g * 32 + i];
+        __syncwarp();
+        const int64_t col = col0 + g * 32 + lane;
+        const bool has = col < p.m.N;
+        const float sb = p.m.sb && has ? __ldg(p.m.sb + col) : 1.0f;
+        const float bias = p.m.bias && has ? __ldg(p.m.bias + col) : 0.0f;
+        typename Mm8Out<OUT>::T* o = out + row0 * p.m.ldo + col;
+#pragma unroll 8
+        for (int r = 0; r < rows; r++) {
+          const float s = __shfl_sync(0xffffffffu, sa, r) * sb;
+          if (has) o[r * p.m.ldo] = Mm8Out<OUT>::make(mine[r * 33 + lane], s, bias);
+        }
+      }
+    }
+  }
+  if (!ok) atomicOr_system(p.status, 1u);
+  __syncwarp();
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  cg::this_cluster().sync();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == EPI_WARPS + 1)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+  static EncodeFn fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<EncodeFn>(f);
+  }();
+  return fn;
+}
+// packed blocks as rows of 64 binary16 values; a box is one block
+bool block_map(CUtensorMap* m, void* base, int64_t blocks) {
+  EncodeFn f = encode_fn();
+  if (!f) return false;
+  const cuuint64_t dims[2] = {64, (cuuint64_t)blocks * 128}, strides[1] = {128};
+  const cuuint32_t box[2] = {64, 128}, elem[2] = {1, 1};
+  return f(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+           CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+         CUDA_SUCCESS;
+}
+
+template <int OUT>
+cudaError_t tc_launch(const TcParams& p, const CUtensorMap& ma, const CUtensorMap& mb, int nsm, cudaStream_t s) {
+  static cudaError_t ready = cudaFuncSetAttribute(mm8_tc<OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+  if (ready != cudaSuccess) return ready;
+  const int64_t units = (int64_t)p.mt * p.nt * p.splits;
+  const int clusters = (int)(units < nsm / 2 ? units : nsm / 2);
+  return launch_dependent(mm8_tc<OUT>, (unsigned)(clusters * 2), THREADS, SMEM, s, p, ma, mb);
+}
+
+}  // namespace
+
+Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm) {
+  Mm8TcPlan r;
+  r.kb = (int)((K + 63) / 64);
+  r.kc = (r.kb + 3) / 4;
+  r.mt = (M + 255) / 256;
+  r.nt = (N + 255) / 256;
+  r.splits = 1;
+  const int64_t tiles = r.mt * r.nt, clusters = nsm / 2;
+  // Time of a split in blocks of 64 k: the blocks of the waves, and for a split
+  // tile what adding up its parts costs (about 12 blocks each).
+  double best = 0.0;
+  for (int s = 1; s <= 16 && s <= r.kb / 4; s++) {
+    const double t = (double)((tiles * s + clusters - 1) / clusters) * ((double)r.kb / s + (s > 1 ? 14 : 4));
+    if (s == 1 || t < 0.95 * best) best = t, r.splits = s;
+  }
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  size_t at = 0;
+  r.a_off = at;
+  at += up((size_t)r.mt * 2 * r.kb * BLK);
+  r.b_off = at;
+  at += up((size_t)r.nt * 2 * r.kb * BLK);
+  r.na_off = at;
+  at += up((size_t)r.mt * 2 * r.kc * sizeof(float));
+  r.nb_off = at;
+  at += up((size_t)r.nt * 2 * r.kc * sizeof(float));
+  r.bytes = at;
+  r.sum_bytes = r.splits > 1 ? (size_t)tiles * (256 * 256 * sizeof(int) + 2 * EPI_WARPS * sizeof(unsigned int)) : 0;
+  return r;
+}
+
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, char* sums,
+                          unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s) {
+  PackParams k;
+  k.x[0] = m.a;
+  k.x[1] = m.b;
+  k.ld[0] = m.lda;
+  k.ld[1] = m.ldb;
+  k.rows[0] = m.M;
+  k.rows[1] = m.N;
+  k.out[0] = reinterpret_cast<__half*>(ws + plan.a_off);
+  k.out[1] = reinterpret_cast<__half*>(ws + plan.b_off);
+  k.norm[0] = reinterpret_cast<float*>(ws + plan.na_off);
+  k.norm[1] = reinterpret_cast<float*>(ws + plan.nb_off);
+  k.K = m.K;
+  k.kb = plan.kb;
+  k.kc = plan.kc;
+  k.first_b = plan.mt * 2 * plan.kc;
+  const int64_t ctas = k.first_b + plan.nt * 2 * plan.kc;
+  const bool al = ((reinterpret_cast<uintptr_t>(m.a) | reinterpret_cast<uintptr_t>(m.b) | (uintptr_t)m.lda |
+                    (uintptr_t)m.ldb) & 15) == 0;
+  if (al) mm8_pack<16><<<(unsigned)ctas, 256, 0, s>>>(k);
+  else mm8_pack<1><<<(unsigned)ctas, 256, 0, s>>>(k);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  CUtensorMap ma, mb;
+  if (!block_map(&ma, ws + plan.a_off, plan.mt * 2 * plan.kb) || !block_map(&mb, ws + plan.b_off, plan.nt * 2 * plan.kb))
+    return cudaErrorNotSupported;
+  TcParams p;
+  p.m = m;
+  p.na = k.norm[0];
+  p.nb = k.norm[1];
+  p.kb = plan.kb;
+  p.kc = plan.kc;
+  p.mt = (int)plan.mt;
+  p.nt = (int)plan.nt;
+  p.splits = plan.splits;
+  p.sums = reinterpret_cast<int*>(sums);
+  p.tickets = reinterpret_cast<unsigned int*>(sums + (size_t)plan.mt * plan.nt * 256 * 256 * sizeof(int));
+  p.status = status;
+  p.wait_limit = wait_limit;
+  switch (out_dtype) {
+    case PEAT_F32: return tc_launch<PEAT_F32>(p, ma, mb, nsm, s);
+    case PEAT_F16: return tc_launch<PEAT_F16>(p, ma, mb, nsm, s);
+    case PEAT_BF16: return tc_launch<PEAT_BF16>(p, ma, mb, nsm, s);
+    default: return tc_launch<PEAT_OUT_I32>(p, ma, mb, nsm, s);
+  }
+}
+
+}  // namespace peat
