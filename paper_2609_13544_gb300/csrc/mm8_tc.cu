@@ -18,8 +18,8 @@
 // 2^24.  pack leaves for every block of 128 rows and 256 k the largest 2-norm
 // of a row; by Cauchy and Schwarz the product of two such norms bounds every
 // partial sum over those 256 k, and the accumulator is drained to int32
-// before the bounds add up to 2^23.  Full-range integers drain every 512 k,
-// normally distributed ones about every 8000.
+// before the bounds add up to more than 2^24.  Full-range integers drain every
+// 768 k, normally distributed ones about every 16 000.
 #include <cooperative_groups.h>
 #include <cuda.h>
 
@@ -104,10 +104,13 @@ __global__ void __launch_bounds__(256) mm8_pack(PackParams p) {
 // ---------------------------------------------------------------------------
 constexpr int STAGES = 6, STAGE = 2 * BLK;  // a CTA's block of a and block of b
 constexpr int EPI_WARPS = 8, THREADS = (EPI_WARPS + 2) * 32;
-constexpr int EPI_BYTES = EPI_WARPS * 32 * 33 * 4;
+// of each result warp: 64 bytes of each of its 32 rows on their way out, and
+// the scales and biases of its 128 columns
+constexpr int EPI_ROWS = 32 * 64, EPI_COLS = 2 * 128 * 4;
+constexpr int EPI_BYTES = EPI_WARPS * (EPI_ROWS + EPI_COLS);
 constexpr int BARS = 512;
 constexpr int SMEM = STAGES * STAGE + EPI_BYTES + BARS + 1024;
-constexpr float LIMIT = 8388608.0f;  // 2^23
+constexpr float LIMIT = 16777216.0f;  // 2^24
 
 struct TcParams {
   Mm8Params m;
@@ -116,8 +119,9 @@ struct TcParams {
   int kb, kc;
   int mt, nt;       // tiles
   int splits;       // parts of the k range of a tile
-  int* sums;        // splits > 1: 256 x 256 int32 for each tile, zero between calls
+  int* sums;        // 128 x 256 int32 for each CTA, or (splits > 1) for each half of a tile, then zero between calls
   unsigned int* tickets;  // splits > 1: one for each result warp of a tile, zero between calls
+  int vec_out;      // out's rows start on 16-byte boundaries
   unsigned int* status;
   uint32_t wait_limit;
 };
@@ -192,6 +196,81 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
       : "r"(addr));
 }
 
+// 16 bytes of a row's results
+template <int OUT>
+struct Piece {
+  static constexpr int E = 16 / (int)sizeof(typename Mm8Out<OUT>::T);
+  static __device__ __forceinline__ uint4 make(const float* v, float sa, const float* sb, const float* bias) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      if (OUT == PEAT_F32) {
+        w[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], __fmul_rn(sa, sb[i])), bias[i]));
+      } else if (OUT == PEAT_OUT_I32) {
+        w[i] = __float_as_uint(v[i]);  // (holds the integer's bits)
+      } else {
+        const float x = __fadd_rn(__fmul_rn(v[2 * i], __fmul_rn(sa, sb[2 * i])), bias[2 * i]);
+        const float y = __fadd_rn(__fmul_rn(v[2 * i + 1], __fmul_rn(sa, sb[2 * i + 1])), bias[2 * i + 1]);
+        if (OUT == PEAT_BF16) {
+          __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+          w[i] = *reinterpret_cast<uint32_t*>(&h);
+        } else {
+          __half2 h = __floats2half2_rn(x, y);
+          w[i] = *reinterpret_cast<uint32_t*>(&h);
+        }
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+// 32 columns of a warp's 32 rows, a row a lane: results into shared memory 64
+// bytes of a row at a time (pieces swizzled against bank conflicts), and from
+// there to global memory, four lanes a row
+template <int OUT>
+__device__ __forceinline__ void put_columns(const TcParams& p, const float (&v)[32], float sa, const float* scol,
+                                            char* stage, int64_t row0, int rows, int64_t col0) {
+  using T = typename Mm8Out<OUT>::T;
+  constexpr int E = Piece<OUT>::E, STEP = 4 * E;  // columns of 64 bytes
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int c = 0; c < 32; c += STEP) {
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      float sb[E], bias[E];
+      if (OUT != PEAT_OUT_I32) {
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+          *reinterpret_cast<float4*>(sb + i) = *reinterpret_cast<const float4*>(scol + c + j * E + i);
+          *reinterpret_cast<float4*>(bias + i) = *reinterpret_cast<const float4*>(scol + 128 + c + j * E + i);
+        }
+      }
+      *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1 & 3)) * 16)) =
+          Piece<OUT>::make(v + c + j * E, sa, sb, bias);
+    }
+    __syncwarp();
+    T* out = static_cast<T*>(p.m.out) + row0 * p.m.ldo + col0 + c;
+    const int64_t left = p.m.N - col0 - c;  // columns
+    if (p.vec_out && left >= STEP) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int r = i * 8 + (lane >> 2);
+        const uint4 u = *reinterpret_cast<const uint4*>(stage + r * 64 + (((lane & 3) ^ (r >> 1 & 3)) * 16));
+        if (r < rows) *reinterpret_cast<uint4*>(out + r * p.m.ldo + (lane & 3) * E) = u;
+      }
+    } else {  // element by element, a row (or two) a step
+      constexpr int R = 32 / STEP;
+      const int e = lane % STEP;
+      if (e < left) {
+#pragma unroll 8
+        for (int r = lane / STEP; r < rows; r += R)
+          out[r * p.m.ldo + e] = *reinterpret_cast<const T*>(stage + r * 64 + (((e / E) ^ (r >> 1 & 3)) * 16) +
+                                                             (e % E) * sizeof(T));
+      }
+    }
+  }
+}
+
 struct Unit {
   int mt, nt, tile;
   int k0, k1;  // blocks of 64 k
@@ -244,7 +323,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     mm8_tc(TcParams p, const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb) {
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  int* stage_out = reinterpret_cast<int*>(smem + STAGES * STAGE);
   const uint32_t bars = sptr(smem + STAGES * STAGE + EPI_BYTES);
   const uint32_t full = bars, empty = bars + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 16,
                  last = acc_empty + 16;
@@ -353,79 +431,98 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   } else {  // results: a warp has 32 rows and half of the columns
     int chunk = 0;
     const int half = warp >> 2, quarter = warp & 3;
-    int* mine = stage_out + warp * 32 * 33;
+    char* rows_out = smem + STAGES * STAGE + warp * (EPI_ROWS + EPI_COLS);
+    float* scol = reinterpret_cast<float*>(rows_out + EPI_ROWS);
     const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
     const uint32_t release0 = mapa(acc_empty, 0);
-    typename Mm8Out<OUT>::T* out = static_cast<typename Mm8Out<OUT>::T*>(p.m.out);
     for (int u = first; u < units && ok; u += step) {
       const Unit t = unit_at(p, u);
-      int acc[128];
+      const int64_t row0 = (int64_t)t.mt * 256 + rank * 128 + quarter * 32;
+      const int64_t col0 = (int64_t)t.nt * 256 + half * 128;
+      const int rows = (int)max((int64_t)0, min((int64_t)32, p.m.M - row0));
+      const float sa = p.m.sa && lane < rows ? __ldg(p.m.sa + row0 + lane) : 1.0f;
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int64_t col = col0 + i * 32 + lane;
+        scol[i * 32 + lane] = p.m.sb && col < p.m.N ? __ldg(p.m.sb + col) : 1.0f;
+        scol[128 + i * 32 + lane] = p.m.bias && col < p.m.N ? __ldg(p.m.bias + col) : 0.0f;
+      }
       // pieces that the accumulator is drained in
       int pieces = 1;
       {
         float run = 0.0f;
         for (int c = t.k0 / 4; c * 4 < t.k1; c += 32) pieces += __popc(drains(bound_of(p, t, c + lane), run));
       }
-      for (int q = 0; q < pieces; q++, chunk++) {
+      // One piece that is the whole sum goes straight from the accumulator to
+      // the output.  Otherwise pieces are added up as integers in memory: in a
+      // place of this CTA's, or, for a tile whose k range is split, in the
+      // tile's, by atomics (whose order does not matter); the last to come has
+      // the total there.
+      const bool split = p.splits > 1;
+      const int64_t part = (split ? (int64_t)t.tile * 2 + rank : (int64_t)blockIdx.x) * EPI_WARPS + warp;
+      int* sums = p.sums + part * (32 * 128) + lane;
+      for (int q = 0; q < pieces && ok; q++, chunk++) {
         if (!(ok = mbar_wait(acc_full + 8 * (chunk & 1), chunk / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-#pragma unroll
+#pragma unroll 1
         for (int g = 0; g < 4; g++) {
           uint32_t v[32];
+          float f[32];
           tmem_load32(taddr + (chunk & 1) * 256 + g * 32, v);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-          for (int i = 0; i < 32; i++) {
-            const int x = __float2int_rn(__uint_as_float(v[i]));
-            acc[g * 32 + i] = q ? acc[g * 32 + i] + x : x;
+          if (g == 3) {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(release0 + 8 * (chunk & 1));
           }
+#pragma unroll
+          for (int i = 0; i < 32; i++) f[i] = __uint_as_float(v[i]);
+          if (split) {
+#pragma unroll
+            for (int i = 0; i < 32; i++) atomicAdd(sums + (g * 32 + i) * 32, __float2int_rn(f[i]));
+            continue;
+          }
+          if (pieces > 1) {
+            int x[32];
+#pragma unroll
+            for (int i = 0; i < 32; i++) x[i] = q ? __ldcg(sums + (g * 32 + i) * 32) : 0;
+#pragma unroll
+            for (int i = 0; i < 32; i++) x[i] += __float2int_rn(f[i]);
+            if (q < pieces - 1) {
+#pragma unroll
+              for (int i = 0; i < 32; i++) __stcg(sums + (g * 32 + i) * 32, x[i]);
+              continue;
+            }
+#pragma unroll
+            for (int i = 0; i < 32; i++) f[i] = OUT == PEAT_OUT_I32 ? __int_as_float(x[i]) : __int2float_rn(x[i]);
+          } else if (OUT == PEAT_OUT_I32) {
+#pragma unroll
+            for (int i = 0; i < 32; i++) f[i] = __int_as_float(__float2int_rn(f[i]));
+          }
+          put_columns<OUT>(p, f, sa, scol + g * 32, rows_out, row0, rows, col0 + g * 32);
         }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(release0 + 8 * (chunk & 1));
       }
-      if (!ok) break;
-      if (p.splits > 1) {
-        // integer sums meet in global memory (their order does not matter); the last to come takes the total
-        const int64_t part = ((int64_t)t.tile * 2 + rank) * EPI_WARPS + warp;
-        int* sums = p.sums + part * (32 * 128) + lane;
-#pragma unroll
-        for (int i = 0; i < 128; i++) atomicAdd(sums + i * 32, acc[i]);
-        __threadfence();
-        __syncwarp();
-        unsigned int n = 0;
-        if (lane == 0) {
-          n = atomicAdd(p.tickets + part, 1u);
-          if (n == (unsigned)p.splits - 1) p.tickets[part] = 0;
-        }
-        if (__shfl_sync(0xffffffffu, n, 0) != (unsigned)p.splits - 1) continue;
-        __threadfence();
-#pragma unroll
-        for (int i = 0; i < 128; i++) {
-          acc[i] = __ldcg(sums + i * 32);
-          __stcg(sums + i * 32, 0);
-        }
+      if (!ok || !split) continue;
+      __threadfence();
+      __syncwarp();
+      unsigned int n = 0;
+      if (lane == 0) {
+        n = atomicAdd(p.tickets + part, 1u);
+        if (n == (unsigned)p.splits - 1) p.tickets[part] = 0;
       }
-      const int64_t row0 = (int64_t)t.mt * 256 + rank * 128 + quarter * 32;
-      const int64_t col0 = (int64_t)t.nt * 256 + half * 128;
-      const float sa = p.m.sa && row0 + lane < p.m.M ? __ldg(p.m.sa + row0 + lane) : 1.0f;
-      const int rows = (int)min((int64_t)32, p.m.M - row0);
-#pragma unroll
+      if (__shfl_sync(0xffffffffu, n, 0) != (unsigned)p.splits - 1) continue;
+      __threadfence();
+#pragma unroll 1
       for (int g = 0; g < 4; g++) {
-        __syncwarp();
+        float f[32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) mine[lane * 33 + i] = acc[g * 32 + i];
-        __syncwarp();
-        const int64_t col = col0 + g * 32 + lane;
-        const bool has = col < p.m.N;
-        const float sb = p.m.sb && has ? __ldg(p.m.sb + col) : 1.0f;
-        const float bias = p.m.bias && has ? __ldg(p.m.bias + col) : 0.0f;
-        typename Mm8Out<OUT>::T* o = out + row0 * p.m.ldo + col;
-#pragma unroll 8
-        for (int r = 0; r < rows; r++) {
-          const float s = __shfl_sync(0xffffffffu, sa, r) * sb;
-          if (has) o[r * p.m.ldo] = Mm8Out<OUT>::make(mine[r * 33 + lane], s, bias);
+        for (int i = 0; i < 32; i++) {
+          const int x = __ldcg(sums + (g * 32 + i) * 32);
+          f[i] = OUT == PEAT_OUT_I32 ? __int_as_float(x) : __int2float_rn(x);
         }
+#pragma unroll
+        for (int i = 0; i < 32; i++) __stcg(sums + (g * 32 + i) * 32, 0);
+        put_columns<OUT>(p, f, sa, scol + g * 32, rows_out, row0, rows, col0 + g * 32);
       }
     }
   }
@@ -500,11 +597,14 @@ Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm) {
   r.nb_off = at;
   at += up((size_t)r.nt * 2 * r.kc * sizeof(float));
   r.bytes = at;
-  r.sum_bytes = r.splits > 1 ? (size_t)tiles * (256 * 256 * sizeof(int) + 2 * EPI_WARPS * sizeof(unsigned int)) : 0;
+  // the two kinds of sums lie apart: one is left as it is, the other zero
+  r.sum_off = at;
+  if (r.splits == 1) r.bytes = at + (size_t)nsm * (128 * 256 * sizeof(int));
+  r.zero_bytes = r.splits > 1 ? (size_t)tiles * (256 * 256 * sizeof(int) + 2 * EPI_WARPS * sizeof(unsigned int)) : 0;
   return r;
 }
 
-cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, char* sums,
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, char* zeros,
                           unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s) {
   PackParams k;
   k.x[0] = m.a;
@@ -540,8 +640,10 @@ cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& pl
   p.mt = (int)plan.mt;
   p.nt = (int)plan.nt;
   p.splits = plan.splits;
-  p.sums = reinterpret_cast<int*>(sums);
-  p.tickets = reinterpret_cast<unsigned int*>(sums + (size_t)plan.mt * plan.nt * 256 * 256 * sizeof(int));
+  p.sums = reinterpret_cast<int*>(plan.splits > 1 ? zeros : ws + plan.sum_off);
+  p.tickets = reinterpret_cast<unsigned int*>(zeros + (size_t)plan.mt * plan.nt * 256 * 256 * sizeof(int));
+  p.vec_out = reinterpret_cast<uintptr_t>(m.out) % 16 == 0 &&
+              m.ldo * (out_dtype == PEAT_F16 || out_dtype == PEAT_BF16 ? 2 : 4) % 16 == 0;
   p.status = status;
   p.wait_limit = wait_limit;
   switch (out_dtype) {

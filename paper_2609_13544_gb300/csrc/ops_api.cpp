@@ -29,8 +29,8 @@ struct OpsState {
   // products: packed operands; integer sums of split tiles, zero between calls
   void* mm = nullptr;
   size_t mm_cap = 0;
-  void* sums = nullptr;
-  size_t sums_cap = 0;
+  void* zeros = nullptr;
+  size_t zeros_cap = 0;
 };
 
 void ops_destroy(OpsState* s) {
@@ -38,7 +38,7 @@ void ops_destroy(OpsState* s) {
   if (s->d_list) cudaFree(s->d_list);
   if (s->done) cudaFree(s->done);
   if (s->mm) cudaFree(s->mm);
-  if (s->sums) cudaFree(s->sums);
+  if (s->zeros) cudaFree(s->zeros);
   for (int i = 0; i < OpsState::RING; i++) {
     if (s->h_list[i]) cudaFreeHost(s->h_list[i]);
     if (s->taken[i]) cudaEventDestroy(s->taken[i]);
@@ -165,7 +165,7 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
   if (h->status_host && *(volatile unsigned int*)h->status_host) {
     *(volatile unsigned int*)h->status_host = 0;
     // what the call left of its split sums is cleared
-    if (h->ops && h->ops->sums) cudaMemsetAsync(h->ops->sums, 0, h->ops->sums_cap, st);
+    if (h->ops && h->ops->zeros) cudaMemsetAsync(h->ops->zeros, 0, h->ops->zeros_cap, st);
     return fail(h, PEAT_ERR_TIMEOUT,
                 "a bounded device-side wait expired in an earlier call on this handle; its outputs are invalid");
   }
@@ -179,14 +179,14 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
     peat_status_t ps = ops_state(h, &s);
     if (ps == PEAT_OK) ps = grow(h, &s->mm, &s->mm_cap, plan.bytes);
     if (ps != PEAT_OK) return ps;
-    if (plan.sum_bytes > s->sums_cap) {
-      ps = grow(h, &s->sums, &s->sums_cap, plan.sum_bytes);
+    if (plan.zero_bytes > s->zeros_cap) {
+      ps = grow(h, &s->zeros, &s->zeros_cap, plan.zero_bytes);
       if (ps != PEAT_OK) return ps;
-      e = cudaMemsetAsync(s->sums, 0, plan.sum_bytes, st);
-      if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(sums)");
+      e = cudaMemsetAsync(s->zeros, 0, plan.zero_bytes, st);
+      if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(zeros)");
     }
     const unsigned int limit = std::min(h->wait_limit, 1u << 22);
-    e = peat::launch_mm8_tc(out_dtype, p, plan, static_cast<char*>(s->mm), static_cast<char*>(s->sums), h->status_dev,
+    e = peat::launch_mm8_tc(out_dtype, p, plan, static_cast<char*>(s->mm), static_cast<char*>(s->zeros), h->status_dev,
                             limit, h->nsm, st);
   } else {
     e = peat::launch_mm8_direct(out_dtype, p, h->nsm, st);

@@ -42,11 +42,11 @@ struct Mm8TcPlan {
   int kb, kc;      // blocks of 64 k, and of 256
   int64_t mt, nt;  // tiles
   int splits;      // parts of a tile's k range
-  size_t a_off, b_off, na_off, nb_off, bytes;  // workspace
-  size_t sum_bytes;  // a second one, zero between calls (0: not needed)
+  size_t a_off, b_off, na_off, nb_off, sum_off, bytes;  // workspace
+  size_t zero_bytes;  // a second one, zero between calls (0: not needed)
 };
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm);
-cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, char* sums,
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, char* zeros,
                           unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s);
 
 // ---- gradient lists (gradnorm.cu) ----
