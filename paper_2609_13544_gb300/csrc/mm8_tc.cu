@@ -12,7 +12,9 @@
 // 128 rows of a and 128 of b, and the accumulators of its rows), persistent
 // over the tiles.  Warp roles: one thread issues the copies, one (of the even
 // CTA) the matrix instructions, eight warps turn accumulators into results
-// while the other half of the 512 accumulator columns fills.
+// while the other half of the 512 accumulator columns fills, and one warp
+// plans: a few tiles ahead it works out each tile's place and drains and
+// fetches its scales, so that nobody else waits for global memory.
 //
 // Exactness: float32 holds a sum of products exactly while it stays below
 // 2^24.  pack leaves for every block of 128 rows and 256 k the largest 2-norm
@@ -103,13 +105,22 @@ __global__ void __launch_bounds__(256) mm8_pack(PackParams p) {
 // product
 // ---------------------------------------------------------------------------
 constexpr int STAGES = 6, STAGE = 2 * BLK;  // a CTA's block of a and block of b
-constexpr int EPI_WARPS = 8, THREADS = (EPI_WARPS + 2) * 32;
-// of each result warp: 64 bytes of each of its 32 rows on their way out, and
-// the scales and biases of its 128 columns
-constexpr int EPI_ROWS = 32 * 64, EPI_COLS = 2 * 128 * 4;
-constexpr int EPI_BYTES = EPI_WARPS * (EPI_ROWS + EPI_COLS);
-constexpr int BARS = 512;
-constexpr int SMEM = STAGES * STAGE + EPI_BYTES + BARS + 1024;
+constexpr int EPI_WARPS = 8, COPY_WARP = EPI_WARPS, MMA_WARP = COPY_WARP + 1, PLAN_WARP = MMA_WARP + 1;
+constexpr int THREADS = (PLAN_WARP + 1) * 32;
+constexpr int EPI_ROWS = 32 * 64;  // a result warp's 64 bytes of each of its rows, for outputs off the vector grid
+constexpr int MAX_GROUPS = 16;     // of 32 norm blocks: K up to 131072
+struct Slot {                      // a planned tile
+  int tile, mt, nt, k0, k1;        // its place; its part of the k range in blocks of 64
+  int pieces;                      // times its accumulator is read
+  uint32_t drain[MAX_GROUPS];      // bit i of word g: drained before norm block k0 / 4 + 32 g + i
+  alignas(16) float sb[256];
+  float bias[256];
+};
+constexpr int SLOTS = 4;
+constexpr int AT_ROWS = STAGES * STAGE, AT_SLOTS = AT_ROWS + EPI_WARPS * EPI_ROWS,
+              AT_BARS = AT_SLOTS + SLOTS * (int)sizeof(Slot), BARS = 256;
+static_assert(AT_BARS % 16 == 0, "barriers are aligned");
+constexpr int SMEM = AT_BARS + BARS + 1024;
 constexpr float LIMIT = 16777216.0f;  // 2^24
 
 struct TcParams {
@@ -121,7 +132,7 @@ struct TcParams {
   int splits;       // parts of the k range of a tile
   int* sums;        // 128 x 256 int32 for each CTA, or (splits > 1) for each half of a tile, then zero between calls
   unsigned int* tickets;  // splits > 1: one for each result warp of a tile, zero between calls
-  int vec_out;      // out's rows start on 16-byte boundaries
+  int vec_out;      // out's rows start on 32-byte boundaries
   unsigned int* status;
   uint32_t wait_limit;
 };
@@ -132,6 +143,9 @@ __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
 }
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // arrive on a barrier of the cluster (an address of mapa)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
@@ -147,7 +161,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
   for (uint32_t i = 0; i < limit; i++) {
     uint32_t ok;
     asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
         " selp.u32 %0, 1, 0, p;\n}"
         : "=r"(ok)
         : "r"(bar), "r"(parity)
@@ -155,6 +169,13 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
     if (ok) return true;
   }
   return false;
+}
+// one lane of the warp; unlike a test of the lane's number, the compiler knows
+// that it is one (with the test a tile took 843 cycles per 64 k, with this 600)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(p));
+  return p != 0;
 }
 // a block into this CTA's shared memory, its bytes counted on the even CTA's barrier
 __device__ __forceinline__ void tma_block(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar) {
@@ -196,126 +217,148 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
       : "r"(addr));
 }
 
-// 16 bytes of a row's results
-template <int OUT>
-struct Piece {
-  static constexpr int E = 16 / (int)sizeof(typename Mm8Out<OUT>::T);
-  static __device__ __forceinline__ uint4 make(const float* v, float sa, const float* sb, const float* bias) {
-    uint32_t w[4];
+// N consecutive results of a row, packed
+template <int OUT, int N>
+__device__ __forceinline__ void results(const float* v, float sa, const float* sb, const float* bias, bool biased,
+                                        uint32_t* w) {
+  constexpr int B = (int)sizeof(typename Mm8Out<OUT>::T);
+  if constexpr (OUT == PEAT_OUT_I32) {  // (v holds the integers' bits)
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      if (OUT == PEAT_F32) {
-        w[i] = __float_as_uint(__fadd_rn(__fmul_rn(v[i], __fmul_rn(sa, sb[i])), bias[i]));
-      } else if (OUT == PEAT_OUT_I32) {
-        w[i] = __float_as_uint(v[i]);  // (holds the integer's bits)
-      } else {
-        const float x = __fadd_rn(__fmul_rn(v[2 * i], __fmul_rn(sa, sb[2 * i])), bias[2 * i]);
-        const float y = __fadd_rn(__fmul_rn(v[2 * i + 1], __fmul_rn(sa, sb[2 * i + 1])), bias[2 * i + 1]);
-        if (OUT == PEAT_BF16) {
-          __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-          w[i] = *reinterpret_cast<uint32_t*>(&h);
-        } else {
-          __half2 h = __floats2half2_rn(x, y);
-          w[i] = *reinterpret_cast<uint32_t*>(&h);
-        }
+    for (int i = 0; i < N; i++) w[i] = __float_as_uint(v[i]);
+  } else {
+    float y[N];
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const float4 s = *reinterpret_cast<const float4*>(sb + i);
+      y[i] = __fmul_rn(v[i], __fmul_rn(sa, s.x));
+      y[i + 1] = __fmul_rn(v[i + 1], __fmul_rn(sa, s.y));
+      y[i + 2] = __fmul_rn(v[i + 2], __fmul_rn(sa, s.z));
+      y[i + 3] = __fmul_rn(v[i + 3], __fmul_rn(sa, s.w));
+      if (biased) {
+        const float4 b = *reinterpret_cast<const float4*>(bias + i);
+        y[i] = __fadd_rn(y[i], b.x);
+        y[i + 1] = __fadd_rn(y[i + 1], b.y);
+        y[i + 2] = __fadd_rn(y[i + 2], b.z);
+        y[i + 3] = __fadd_rn(y[i + 3], b.w);
       }
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+    for (int i = 0; i < N * B / 4; i++) {
+      if (OUT == PEAT_F32) {
+        w[i] = __float_as_uint(y[i]);
+      } else if (OUT == PEAT_BF16) {
+        __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+        w[i] = *reinterpret_cast<uint32_t*>(&h);
+      } else {
+        __half2 h = __floats2half2_rn(y[2 * i], y[2 * i + 1]);
+        w[i] = *reinterpret_cast<uint32_t*>(&h);
+      }
+    }
   }
-};
-// 32 columns of a warp's 32 rows, a row a lane: results into shared memory 64
-// bytes of a row at a time (pieces swizzled against bank conflicts), and from
-// there to global memory, four lanes a row
+}
+// a whole 32-byte sector
+__device__ __forceinline__ void store_sector(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+// 32 columns of a warp's 32 rows, a row a lane.  Where the rows lie on 32-byte
+// boundaries each lane writes its sectors itself; elsewhere they go through
+// shared memory, 64 bytes of a row at a time (pieces swizzled against bank
+// conflicts), and out element by element along the rows.
 template <int OUT>
-__device__ __forceinline__ void put_columns(const TcParams& p, const float (&v)[32], float sa, const float* scol,
-                                            char* stage, int64_t row0, int rows, int64_t col0) {
+__device__ __forceinline__ void put_columns(const TcParams& p, const float (&v)[32], float sa, const float* sb,
+                                            const float* bias, char* stage, int64_t row0, int rows, int64_t col0) {
   using T = typename Mm8Out<OUT>::T;
-  constexpr int E = Piece<OUT>::E, STEP = 4 * E;  // columns of 64 bytes
+  constexpr int B = (int)sizeof(T);
   const int lane = threadIdx.x & 31;
+  const bool biased = p.m.bias != nullptr;
+  T* out = static_cast<T*>(p.m.out) + row0 * p.m.ldo + col0;
+  const int64_t left = p.m.N - col0;  // columns
+  if (p.vec_out && left >= 32) {
+    T* o = out + lane * p.m.ldo;
+#pragma unroll
+    for (int c = 0; c < 32; c += 32 / B) {
+      uint32_t w[8];
+      results<OUT, 32 / B>(v + c, sa, sb + c, bias + c, biased, w);
+      if (lane < rows) store_sector(o + c, w);
+    }
+    return;
+  }
+  constexpr int E = 16 / B, STEP = 4 * E, R = 32 / STEP;
 #pragma unroll
   for (int c = 0; c < 32; c += STEP) {
     __syncwarp();
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-      float sb[E], bias[E];
-      if (OUT != PEAT_OUT_I32) {
-#pragma unroll
-        for (int i = 0; i < E; i += 4) {
-          *reinterpret_cast<float4*>(sb + i) = *reinterpret_cast<const float4*>(scol + c + j * E + i);
-          *reinterpret_cast<float4*>(bias + i) = *reinterpret_cast<const float4*>(scol + 128 + c + j * E + i);
-        }
-      }
-      *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1 & 3)) * 16)) =
-          Piece<OUT>::make(v + c + j * E, sa, sb, bias);
+      uint32_t w[4];
+      results<OUT, E>(v + c + j * E, sa, sb + c + j * E, bias + c + j * E, biased, w);
+      *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1 & 3)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
     __syncwarp();
-    T* out = static_cast<T*>(p.m.out) + row0 * p.m.ldo + col0 + c;
-    const int64_t left = p.m.N - col0 - c;  // columns
-    if (p.vec_out && left >= STEP) {
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const int r = i * 8 + (lane >> 2);
-        const uint4 u = *reinterpret_cast<const uint4*>(stage + r * 64 + (((lane & 3) ^ (r >> 1 & 3)) * 16));
-        if (r < rows) *reinterpret_cast<uint4*>(out + r * p.m.ldo + (lane & 3) * E) = u;
-      }
-    } else {  // element by element, a row (or two) a step
-      constexpr int R = 32 / STEP;
-      const int e = lane % STEP;
-      if (e < left) {
+    const int e = lane % STEP;
+    if (c + e < left) {
 #pragma unroll 8
-        for (int r = lane / STEP; r < rows; r += R)
-          out[r * p.m.ldo + e] = *reinterpret_cast<const T*>(stage + r * 64 + (((e / E) ^ (r >> 1 & 3)) * 16) +
-                                                             (e % E) * sizeof(T));
-      }
+      for (int r = lane / STEP; r < rows; r += R)
+        out[r * p.m.ldo + c + e] = *reinterpret_cast<const T*>(stage + r * 64 + (((e / E) ^ (r >> 1 & 3)) * 16) +
+                                                               (e % E) * B);
     }
   }
 }
 
-struct Unit {
-  int mt, nt, tile;
-  int k0, k1;  // blocks of 64 k
-};
-__device__ __forceinline__ Unit unit_at(const TcParams& p, int u) {
-  Unit r;
-  r.tile = u / p.splits;
-  const int s = u - r.tile * p.splits;
-  r.nt = r.tile / p.mt;
-  r.mt = r.tile - r.nt * p.mt;
-  r.k0 = (int)((int64_t)p.kb * s / p.splits);
-  r.k1 = (int)((int64_t)p.kb * (s + 1) / p.splits);
-  return r;
-}
-// the bound of a tile's partial sums over norm block kc (0 past the end)
-__device__ __forceinline__ float bound_of(const TcParams& p, const Unit& t, int kc) {
-  if (kc * 4 >= t.k1) return 0.0f;
-  const float* a = p.na + (int64_t)t.mt * 2 * p.kc + kc;
-  const float* b = p.nb + (int64_t)t.nt * 2 * p.kc + kc;
-  return __fmul_rn(fmaxf(__ldcg(a), __ldcg(a + p.kc)), fmaxf(__ldcg(b), __ldcg(b + p.kc)));
-}
-// Which of 32 norm blocks (lane i holds block i's bound) the accumulator is
-// drained before; `run` is the bound of what it holds, and is carried on.  The
-// instruction warp and the result warps each work this out, so every rounding
-// is spelled out.
-__device__ __forceinline__ uint32_t drains(float mine, float& run) {
-  float all = mine;
+constexpr int GROUP = 8;
+// Plans a tile into a slot, by a warp.
+__device__ void plan_tile(const TcParams& p, int u, Slot* slot) {
+  const int lane = threadIdx.x & 31;
+  const int tile = u / p.splits, part = u - tile * p.splits;
+  // groups of GROUP rows of tiles, column by column: the clusters at work at
+  // any time share few blocks of a and few of b
+  const int per = GROUP * p.nt, g = tile / per, in = tile - g * per, wide = min(GROUP, p.mt - g * GROUP);
+  const int nt = in / wide, mt = g * GROUP + in - nt * wide;
+  const int k0 = (int)((int64_t)p.kb * part / p.splits), k1 = (int)((int64_t)p.kb * (part + 1) / p.splits);
 #pragma unroll
-  for (int o = 16; o; o /= 2) all = __fadd_rn(all, __shfl_xor_sync(0xffffffffu, all, o));
-  if (__fadd_rn(run, all) <= LIMIT) {
-    run = __fadd_rn(run, all);
-    return 0;
+  for (int i = 0; i < 8; i++) {
+    const int64_t col = (int64_t)nt * 256 + i * 32 + lane;
+    slot->sb[i * 32 + lane] = p.m.sb && col < p.m.N ? __ldg(p.m.sb + col) : 1.0f;
+    if (p.m.bias) slot->bias[i * 32 + lane] = col < p.m.N ? __ldg(p.m.bias + col) : 0.0f;
   }
-  uint32_t mask = 0;
-  for (int i = 0; i < 32; i++) {
-    const float b = __shfl_sync(0xffffffffu, mine, i);
-    const float sum = __fadd_rn(run, b);
-    if (sum > LIMIT) {
-      if (run > 0.0f) mask |= 1u << i;
-      run = b;
+  const float* na = p.na + (int64_t)mt * 2 * p.kc;
+  const float* nb = p.nb + (int64_t)nt * 2 * p.kc;
+  int pieces = 1;
+  float run = 0.0f;  // the bound of what the accumulator holds
+  for (int c0 = k0 / 4, w = 0; c0 * 4 < k1; c0 += 32, w++) {
+    const int c = c0 + lane;
+    float mine = 0.0f;
+    if (c * 4 < k1)
+      mine = fmaxf(__ldcg(na + c), __ldcg(na + p.kc + c)) * fmaxf(__ldcg(nb + c), __ldcg(nb + p.kc + c));
+    float all = mine;
+#pragma unroll
+    for (int o = 16; o; o /= 2) all += __shfl_xor_sync(0xffffffffu, all, o);
+    uint32_t mask = 0;
+    if (run + all <= LIMIT) {
+      run += all;
     } else {
-      run = sum;
+      for (int i = 0; i < 32; i++) {
+        const float b = __shfl_sync(0xffffffffu, mine, i);
+        if (run + b > LIMIT) {
+          if (run > 0.0f) mask |= 1u << i;
+          run = b;
+        } else {
+          run += b;
+        }
+      }
     }
+    pieces += __popc(mask);
+    if (lane == 0) slot->drain[w] = mask;
   }
-  return mask;
+  if (lane == 0) {
+    slot->tile = tile;
+    slot->mt = mt;
+    slot->nt = nt;
+    slot->k0 = k0;
+    slot->k1 = k1;
+    slot->pieces = pieces;
+  }
 }
 
 template <int OUT>
@@ -323,10 +366,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     mm8_tc(TcParams p, const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb) {
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t bars = sptr(smem + STAGES * STAGE + EPI_BYTES);
-  const uint32_t full = bars, empty = bars + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 16,
-                 last = acc_empty + 16;
-  volatile uint32_t* shared_words = reinterpret_cast<volatile uint32_t*>(smem + STAGES * STAGE + EPI_BYTES + 256);
+  Slot* slots = reinterpret_cast<Slot*>(smem + AT_SLOTS);
+  const uint32_t full = sptr(smem + AT_BARS), empty = full + 8 * STAGES, acc_full = empty + 8 * STAGES,
+                 acc_empty = acc_full + 16, last = acc_empty + 16, planned = last + 8, unplanned = planned + 8 * SLOTS;
+  volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(smem + AT_BARS + 8 * (2 * STAGES + 5 + 2 * SLOTS));
+  static_assert(8 * (2 * STAGES + 5 + 2 * SLOTS) + 4 <= BARS, "the barriers fit");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t rank;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -342,124 +386,124 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       mbar_init(acc_empty + 8 * i, 2 * EPI_WARPS);
     }
     mbar_init(last, 1);
+    for (int i = 0; i < SLOTS; i++) {
+      mbar_init(planned + 8 * i, 1);
+      mbar_init(unplanned + 8 * i, EPI_WARPS + 1 + (rank == 0));  // results, copies, and the instructions' warp
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == EPI_WARPS + 1) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sptr((const void*)shared_words))
+  if (warp == MMA_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sptr((const void*)tmem_at))
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   cg::this_cluster().sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const uint32_t tmem = shared_words[0];
+  const uint32_t tmem = *tmem_at;
   pdl_wait();
 
   bool ok = true;
-  if (warp == EPI_WARPS) {  // copies
-    if (lane == 0) {
-      int seq = 0;
-      for (int u = first; u < units && ok; u += step) {
-        const Unit t = unit_at(p, u);
-        const int ra = (t.mt * 2 + (int)rank) * p.kb, rb = (t.nt * 2 + (int)rank) * p.kb;
-        for (int k = t.k0; k < t.k1; k++, seq++) {
+  if (warp == PLAN_WARP) {
+    int i = 0;
+    for (int u = first; u < units && ok; u += step, i++) {
+      ok = mbar_wait(unplanned + 8 * (i % SLOTS), (i / SLOTS & 1) ^ 1, p.wait_limit);
+      if (!ok) break;
+      plan_tile(p, u, slots + i % SLOTS);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(planned + 8 * (i % SLOTS));
+    }
+  } else if (warp == COPY_WARP) {
+    if (elect_one()) {
+      int seq = 0, i = 0;
+      for (int u = first; u < units && ok; u += step, i++) {
+        const Slot* t = slots + i % SLOTS;
+        if (!(ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
+        const int k0 = t->k0, k1 = t->k1;
+        const int ra = (t->mt * 2 + (int)rank) * p.kb, rb = (t->nt * 2 + (int)rank) * p.kb;
+        mbar_arrive(unplanned + 8 * (i % SLOTS));
+        for (int k = k0; k < k1; k++, seq++) {
           const int s = seq % STAGES;
           if (!(ok = mbar_wait(empty + 8 * s, (seq / STAGES & 1) ^ 1, p.wait_limit))) break;
           const uint32_t dst = sptr(smem + s * STAGE), bar = mapa(full + 8 * s, 0);
           if (rank == 0) mbar_expect(full + 8 * s, 2 * STAGE);
-          tma_block(dst, &ma, (ra + k) * 128, bar);
-          tma_block(dst + BLK, &mb, (rb + k) * 128, bar);
+          tma_block(dst, &ma, (ra + k) * 16, bar);
+          tma_block(dst + BLK, &mb, (rb + k) * 16, bar);
         }
       }
       // a stage's copies have landed when its instructions are done with it
-      for (int i = 0; i < STAGES && i < seq; i++) {
-        const int q = seq - 1 - i;
+      for (int j = 0; j < STAGES && j < seq; j++) {
+        const int q = seq - 1 - j;
         mbar_wait(empty + 8 * (q % STAGES), q / STAGES & 1, p.wait_limit);
       }
     }
-  } else if (warp == EPI_WARPS + 1) {  // matrix instructions
+  } else if (warp == MMA_WARP) {
     if (rank == 0) {
-      int seq = 0, chunk = 0;
-      Unit t = unit_at(p, first);
-      float mine = first < units ? bound_of(p, t, t.k0 / 4 + lane) : 0.0f;
-      for (int u = first; u < units && ok; u += step) {
-        const Unit now = t;
-        float run = 0.0f;
-        uint32_t mask = drains(mine, run);
-        if (u + step < units) {  // the next tile's bounds are on their way meanwhile
-          t = unit_at(p, u + step);
-          mine = bound_of(p, t, t.k0 / 4 + lane);
-        }
-        const int c0 = now.k0 / 4;
+      int seq = 0, chunk = 0, i = 0;
+      for (int u = first; u < units && ok; u += step, i++) {
+        const Slot* t = slots + i % SLOTS;
+        if (!(ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
+        const int k0 = t->k0, k1 = t->k1;
+        uint32_t mask = 0;
         bool fresh = true;  // the accumulator starts anew
-        for (int k = now.k0; k < now.k1 && ok; k++, seq++) {
-          const int c = k / 4 - c0;
-          if ((k & 3) == 0 && c > 0 && (c & 31) == 0) mask = drains(bound_of(p, now, k / 4 + lane), run);
-          if ((k == now.k0 || (k & 3) == 0) && (mask >> (c & 31) & 1)) {
-            if (lane == 0) commit_both(acc_full + 8 * (chunk & 1));
-            chunk++;
-            fresh = true;
+        for (int k = k0; k < k1; k++, seq++) {
+          if (k == k0 || (k & 3) == 0) {
+            const int c = k / 4 - k0 / 4;
+            if ((c & 31) == 0) mask = t->drain[c >> 5];
+            if (mask >> (c & 31) & 1) {
+              if (elect_one()) commit_both(acc_full + 8 * (chunk & 1));
+              chunk++;
+              fresh = true;
+            }
           }
           if (fresh) {
             ok = mbar_wait(acc_empty + 8 * (chunk & 1), (chunk / 2 & 1) ^ 1, p.wait_limit);
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (!ok) break;
           }
           const int s = seq % STAGES;
-          ok = ok && mbar_wait(full + 8 * s, seq / STAGES & 1, p.wait_limit);
-          if (!ok) break;
+          if (!(ok = mbar_wait(full + 8 * s, seq / STAGES & 1, p.wait_limit))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          if (lane == 0) {
+          if (elect_one()) {
             const uint32_t d = tmem + (chunk & 1) * 256, base = sptr(smem + s * STAGE);
             const uint64_t a = block_desc(base), b = block_desc(base + BLK);
 #pragma unroll
-            for (int i = 0; i < 4; i++) mma_256(d, a + 2 * i, b + 2 * i, !(fresh && i == 0));
+            for (int j = 0; j < 4; j++) mma_256(d, a + 2 * j, b + 2 * j, !(fresh && j == 0));
             commit_both(empty + 8 * s);
+            if (k == k1 - 1) commit_both(acc_full + 8 * (chunk & 1));
           }
           __syncwarp();
           fresh = false;
         }
-        if (ok && lane == 0) commit_both(acc_full + 8 * (chunk & 1));
         chunk++;
+        if (lane == 0) mbar_arrive(unplanned + 8 * (i % SLOTS));
       }
       // whatever was issued is done before the accumulators are given back
-      if (lane == 0) {
-        commit_both(last);
-        mbar_wait(last, 0, p.wait_limit);
-      }
+      if (elect_one()) commit_both(last);
+      mbar_wait(last, 0, p.wait_limit);
       __syncwarp();
     }
   } else {  // results: a warp has 32 rows and half of the columns
-    int chunk = 0;
+    int chunk = 0, i = 0;
     const int half = warp >> 2, quarter = warp & 3;
-    char* rows_out = smem + STAGES * STAGE + warp * (EPI_ROWS + EPI_COLS);
-    float* scol = reinterpret_cast<float*>(rows_out + EPI_ROWS);
+    char* stage = smem + AT_ROWS + warp * EPI_ROWS;
     const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
     const uint32_t release0 = mapa(acc_empty, 0);
-    for (int u = first; u < units && ok; u += step) {
-      const Unit t = unit_at(p, u);
-      const int64_t row0 = (int64_t)t.mt * 256 + rank * 128 + quarter * 32;
-      const int64_t col0 = (int64_t)t.nt * 256 + half * 128;
+    const bool split = p.splits > 1;
+    for (int u = first; u < units && ok; u += step, i++) {
+      const Slot* t = slots + i % SLOTS;
+      if (!(ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
+      const int pieces = t->pieces;
+      const int64_t row0 = (int64_t)t->mt * 256 + rank * 128 + quarter * 32;
+      const int64_t col0 = (int64_t)t->nt * 256 + half * 128;
+      const float *sb = t->sb + half * 128, *bias = t->bias + half * 128;
       const int rows = (int)max((int64_t)0, min((int64_t)32, p.m.M - row0));
       const float sa = p.m.sa && lane < rows ? __ldg(p.m.sa + row0 + lane) : 1.0f;
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        const int64_t col = col0 + i * 32 + lane;
-        scol[i * 32 + lane] = p.m.sb && col < p.m.N ? __ldg(p.m.sb + col) : 1.0f;
-        scol[128 + i * 32 + lane] = p.m.bias && col < p.m.N ? __ldg(p.m.bias + col) : 0.0f;
-      }
-      // pieces that the accumulator is drained in
-      int pieces = 1;
-      {
-        float run = 0.0f;
-        for (int c = t.k0 / 4; c * 4 < t.k1; c += 32) pieces += __popc(drains(bound_of(p, t, c + lane), run));
-      }
       // One piece that is the whole sum goes straight from the accumulator to
       // the output.  Otherwise pieces are added up as integers in memory: in a
       // place of this CTA's, or, for a tile whose k range is split, in the
       // tile's, by atomics (whose order does not matter); the last to come has
       // the total there.
-      const bool split = p.splits > 1;
-      const int64_t part = (split ? (int64_t)t.tile * 2 + rank : (int64_t)blockIdx.x) * EPI_WARPS + warp;
+      const int64_t part = (split ? (int64_t)t->tile * 2 + rank : (int64_t)blockIdx.x) * EPI_WARPS + warp;
       int* sums = p.sums + part * (32 * 128) + lane;
       for (int q = 0; q < pieces && ok; q++, chunk++) {
         if (!(ok = mbar_wait(acc_full + 8 * (chunk & 1), chunk / 2 & 1, p.wait_limit))) break;
@@ -499,31 +543,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 #pragma unroll
             for (int i = 0; i < 32; i++) f[i] = __int_as_float(__float2int_rn(f[i]));
           }
-          put_columns<OUT>(p, f, sa, scol + g * 32, rows_out, row0, rows, col0 + g * 32);
+          put_columns<OUT>(p, f, sa, sb + g * 32, bias + g * 32, stage, row0, rows, col0 + g * 32);
         }
       }
-      if (!ok || !split) continue;
-      __threadfence();
-      __syncwarp();
-      unsigned int n = 0;
-      if (lane == 0) {
-        n = atomicAdd(p.tickets + part, 1u);
-        if (n == (unsigned)p.splits - 1) p.tickets[part] = 0;
-      }
-      if (__shfl_sync(0xffffffffu, n, 0) != (unsigned)p.splits - 1) continue;
-      __threadfence();
+      if (!ok) break;
+      if (split) {
+        __threadfence();
+        __syncwarp();
+        unsigned int n = 0;
+        if (lane == 0) {
+          n = atomicAdd(p.tickets + part, 1u);
+          if (n == (unsigned)p.splits - 1) p.tickets[part] = 0;
+        }
+        if (__shfl_sync(0xffffffffu, n, 0) == (unsigned)p.splits - 1) {
+          __threadfence();
 #pragma unroll 1
-      for (int g = 0; g < 4; g++) {
-        float f[32];
+          for (int g = 0; g < 4; g++) {
+            float f[32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) {
-          const int x = __ldcg(sums + (g * 32 + i) * 32);
-          f[i] = OUT == PEAT_OUT_I32 ? __int_as_float(x) : __int2float_rn(x);
+            for (int j = 0; j < 32; j++) {
+              const int x = __ldcg(sums + (g * 32 + j) * 32);
+              f[j] = OUT == PEAT_OUT_I32 ? __int_as_float(x) : __int2float_rn(x);
+            }
+#pragma unroll
+            for (int j = 0; j < 32; j++) __stcg(sums + (g * 32 + j) * 32, 0);
+            put_columns<OUT>(p, f, sa, sb + g * 32, bias + g * 32, stage, row0, rows, col0 + g * 32);
+          }
         }
-#pragma unroll
-        for (int i = 0; i < 32; i++) __stcg(sums + (g * 32 + i) * 32, 0);
-        put_columns<OUT>(p, f, sa, scol + g * 32, rows_out, row0, rows, col0 + g * 32);
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(unplanned + 8 * (i % SLOTS));
     }
   }
   if (!ok) atomicOr_system(p.status, 1u);
@@ -531,7 +580,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   cg::this_cluster().sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  if (warp == EPI_WARPS + 1)
+  if (warp == MMA_WARP)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
@@ -549,13 +598,13 @@ EncodeFn encode_fn() {
   }();
   return fn;
 }
-// packed blocks as rows of 64 binary16 values; a box is one block
+// packed blocks as rows of 1 KB; a box of 16 of them is one block
 bool block_map(CUtensorMap* m, void* base, int64_t blocks) {
   EncodeFn f = encode_fn();
   if (!f) return false;
-  const cuuint64_t dims[2] = {64, (cuuint64_t)blocks * 128}, strides[1] = {128};
-  const cuuint32_t box[2] = {64, 128}, elem[2] = {1, 1};
-  return f(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, base, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint64_t dims[2] = {256, (cuuint64_t)blocks * 16}, strides[1] = {1024};
+  const cuuint32_t box[2] = {256, 16}, elem[2] = {1, 1};
+  return f(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, base, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE,
            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
          CUDA_SUCCESS;
 }
@@ -642,8 +691,8 @@ cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& pl
   p.splits = plan.splits;
   p.sums = reinterpret_cast<int*>(plan.splits > 1 ? zeros : ws + plan.sum_off);
   p.tickets = reinterpret_cast<unsigned int*>(zeros + (size_t)plan.mt * plan.nt * 256 * 256 * sizeof(int));
-  p.vec_out = reinterpret_cast<uintptr_t>(m.out) % 16 == 0 &&
-              m.ldo * (out_dtype == PEAT_F16 || out_dtype == PEAT_BF16 ? 2 : 4) % 16 == 0;
+  p.vec_out = reinterpret_cast<uintptr_t>(m.out) % 32 == 0 &&
+              m.ldo * (out_dtype == PEAT_F16 || out_dtype == PEAT_BF16 ? 2 : 4) % 32 == 0;
   p.status = status;
   p.wait_limit = wait_limit;
   switch (out_dtype) {
