@@ -23,7 +23,8 @@ LIB_CHECKED = OUT_DIR / "libpeat_checked.so"
 SOURCES = ["compare.cu", "compare8.cu", "compare64.cu", "topk.cu", "tstats.cu", "isclose.cu", "isclose64.cu", "inject.cu", "quant8.cu",
            "matmul8.cu", "mm8_tc.cu", "gradnorm.cu", "peat_api.cpp", "ops_api.cpp"]
 HEADERS = [CSRC / "peat_internal.h", CSRC / "exact.cuh", CSRC / "meanvar.cuh", CSRC / "inject_models.cuh", CSRC / "tol_exact.cuh", CSRC / "exact64.cuh",
-           CSRC / "peat_handle.h", CSRC / "ops_internal.h", CSRC / "mm8_common.cuh", ROOT / "include" / "peat.h",
+           CSRC / "peat_handle.h", CSRC / "ops_internal.h", CSRC / "mm8_common.cuh",
+           CSRC / "vec16.cuh", ROOT / "include" / "peat.h",
            ROOT / "include" / "peat_ops.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",

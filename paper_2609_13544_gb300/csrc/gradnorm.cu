@@ -16,52 +16,17 @@
 // Bound by memory: the norm reads the list once; clipping reads it again and
 // writes it, in the opposite order, so that what the norm read last is still
 // in L2.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include "ops_internal.h"
+#include "peat_internal.h"
+#include "vec16.cuh"
 
 namespace peat {
 namespace {
 
-constexpr int GB = 256;
+constexpr int GB = 256;        // threads of a CTA
+constexpr int GB_SMALL = 1024;  // of the one CTA that takes a small list
 
 __device__ __forceinline__ int elem_size(int dt) { return dt == PEAT_F32 ? 4 : 2; }
-
-template <int DT>
-__device__ __forceinline__ void unpack(uint4 u, float (&x)[DT == PEAT_F32 ? 4 : 8]) {
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    if (DT == PEAT_F32) {
-      x[i] = __uint_as_float(w[i]);
-    } else if (DT == PEAT_BF16) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    } else {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      x[2 * i] = f.x;
-      x[2 * i + 1] = f.y;
-    }
-  }
-}
-template <int DT>
-__device__ __forceinline__ uint4 pack(const float (&x)[DT == PEAT_F32 ? 4 : 8]) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    if (DT == PEAT_F32) {
-      w[i] = __float_as_uint(x[i]);
-    } else if (DT == PEAT_BF16) {
-      __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<uint32_t*>(&b);
-    } else {
-      __half2 b = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<uint32_t*>(&b);
-    }
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 
 // A tensor's bytes on the grid of 16-byte units: unit j is [base + 16 j, + 16);
 // only the first and the last may hold bytes that are not the tensor's.
@@ -120,22 +85,21 @@ __device__ __forceinline__ float unit_sum(uint4 u) {
     return a + b;
   }
 }
-template <int DT>
-__device__ __forceinline__ uint32_t unit_max(uint32_t m, uint4 u) {  // patterns without sign: one word, or two half-words
-  if (DT == PEAT_F32) {
-    return max(max(m, u.x & 0x7fffffffu), max(max(u.y & 0x7fffffffu, u.z & 0x7fffffffu), u.w & 0x7fffffffu));
-  } else {
-    const uint32_t a = __vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), b = __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu);
-    return __vmaxu2(m, __vmaxu2(a, b));
-  }
+// the largest magnitude of a unit; a NaN stays
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
-// the largest pattern as float32 bits (infinities and NaNs at or above 0x7f800000)
 template <int DT>
-__device__ __forceinline__ uint32_t max_bits(uint32_t m) {
-  if (DT == PEAT_F32) return m;
-  m = max(m & 0xffffu, m >> 16);
-  if (DT == PEAT_BF16) return m << 16;
-  return __float_as_uint(__half2float(__ushort_as_half((unsigned short)m)));
+__device__ __forceinline__ float unit_max(uint4 u) {
+  constexpr int E = DT == PEAT_F32 ? 4 : 8;
+  float x[E];
+  unpack<DT>(u, x);
+  float m = fabsf(x[0]);
+#pragma unroll
+  for (int e = 1; e < E; e++) m = max_nan(m, fabsf(x[e]));
+  return m;
 }
 
 __device__ __forceinline__ double warp_sum(double v) {
@@ -151,23 +115,21 @@ __device__ GnPartial piece(const Span& s, int64_t j0, int64_t j1) {
   const uint4* v = reinterpret_cast<const uint4*>(s.base);
   constexpr int U = 8;
   Sum sum;
-  uint32_t m = 0;
+  float m = 0.0f;     // the largest magnitude (the maximum norm alone)
+  uint32_t any = 0;   // the elements' bits
+  auto take = [&](uint4 u) {
+    any |= u.x | u.y | u.z | u.w;
+    if (NORM == PEAT_NORM_INF) m = max_nan(m, unit_max<DT>(u));
+    else sum.add(unit_sum<DT, NORM>(u));
+  };
   int64_t j = j0;
   if (j < j1 && !s.full(j)) {  // the tensor's first unit
-    if (lane == 0) {
-      const uint4 u = edge_unit<DT>(s, j);
-      if (NORM != PEAT_NORM_INF) sum.add(unit_sum<DT, NORM>(u));
-      m = unit_max<DT>(m, u);
-    }
+    if (lane == 0) take(edge_unit<DT>(s, j));
     j++;
   }
   int64_t je = j1;
   if (j < je && !s.full(je - 1)) {  // and its last
-    if (lane == 1) {
-      const uint4 u = edge_unit<DT>(s, je - 1);
-      if (NORM != PEAT_NORM_INF) sum.add(unit_sum<DT, NORM>(u));
-      m = unit_max<DT>(m, u);
-    }
+    if (lane == 1) take(edge_unit<DT>(s, je - 1));
     je--;
   }
   for (; j + 32 * U <= je; j += 32 * U) {
@@ -177,27 +139,29 @@ __device__ GnPartial piece(const Span& s, int64_t j0, int64_t j1) {
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int i = 0; i < U; i += 2) {
-      if (NORM != PEAT_NORM_INF) a += unit_sum<DT, NORM>(u[i]), b += unit_sum<DT, NORM>(u[i + 1]);
-      m = unit_max<DT>(unit_max<DT>(m, u[i]), u[i + 1]);
+      any |= u[i].x | u[i].y | u[i].z | u[i].w;
+      any |= u[i + 1].x | u[i + 1].y | u[i + 1].z | u[i + 1].w;
+      if (NORM == PEAT_NORM_INF) m = max_nan(m, max_nan(unit_max<DT>(u[i]), unit_max<DT>(u[i + 1])));
+      else a += unit_sum<DT, NORM>(u[i]), b += unit_sum<DT, NORM>(u[i + 1]);
     }
     if (NORM != PEAT_NORM_INF) sum.add(a + b);
   }
-  for (j += lane; j < je; j += 32) {
-    const uint4 u = __ldcg(v + j);
-    if (NORM != PEAT_NORM_INF) sum.add(unit_sum<DT, NORM>(u));
-    m = unit_max<DT>(m, u);
-  }
-  const uint32_t top = __reduce_max_sync(0xffffffffu, max_bits<DT>(m));
+  for (j += lane; j < je; j += 32) take(__ldcg(v + j));
   GnPartial r;
-  r.bad = r.nan = 0;
-  const float big = __uint_as_float(top);
-  // squares of numbers between 2^-40 and 2^50 and their sums stay well inside
-  // float32's range; below, a number 2^23 times smaller than the largest may
-  // lose its square, which is then below 2^-46 of the sum
-  const bool fine = top < 0x7f800000u && (NORM == PEAT_NORM_INF || (NORM == PEAT_NORM_1 ? big < 0x1p100f : (big < 0x1p50f && (big >= 0x1p-40f || top == 0))));
-  if (fine) {
-    r.s = NORM == PEAT_NORM_INF ? (double)big : warp_sum((double)sum.hi + (double)sum.lo);
-    return r;
+  r.bad = 0;
+  any = __reduce_or_sync(0xffffffffu, any);
+  if (NORM == PEAT_NORM_INF) {
+    r.s = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m) & 0x7fffffffu));
+    if (__double2float_rn(r.s) < __uint_as_float(0x7f800000u)) return r;  // (not for a NaN)
+  } else {
+    const double total = warp_sum((double)sum.hi + (double)sum.lo);
+    r.s = total;
+    // No element was infinite or NaN, and no square too large, if the total is
+    // finite.  A square below 2^-126 may be off by 2^-150: with a total of
+    // 2^-70 the fewer than 2^40 of them are off by less than 2^-40 of it.
+    const float t = __double2float_rn(total);
+    const bool zeros = (any & (DT == PEAT_F32 ? 0x7fffffffu : 0x7fff7fffu)) == 0;
+    if (t < 0x1p120f && (NORM == PEAT_NORM_1 || t >= 0x1p-70f || zeros)) return r;
   }
   // again: scaled so that the largest finite magnitude is near 1, and counted
   constexpr int E = DT == PEAT_F32 ? 4 : 8;
@@ -209,18 +173,18 @@ __device__ GnPartial piece(const Span& s, int64_t j0, int64_t j1) {
     for (int e = 0; e < E; e++) {
       const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
       bad += b >= 0x7f800000u;
-      nan += b > 0x7f800000u;
+      nan |= b > 0x7f800000u;
       if (b < 0x7f800000u) most = max(most, b);
     }
   }
   most = __reduce_max_sync(0xffffffffu, most);
   r.bad = __reduce_add_sync(0xffffffffu, bad);
-  r.nan = __reduce_add_sync(0xffffffffu, nan);
+  nan = __reduce_or_sync(0xffffffffu, nan);
   if (r.bad) {
-    r.s = r.nan ? __longlong_as_double(0x7ff8000000000000ll) : __longlong_as_double(0x7ff0000000000000ll);
+    r.s = nan ? __longlong_as_double(0x7ff8000000000000ll) : __longlong_as_double(0x7ff0000000000000ll);
     return r;
   }
-  const int k = ilogbf(__uint_as_float(most));  // (not zero here)
+  const int k = ilogbf(__uint_as_float(most));  // (there is a number that is not zero here)
   const float f1 = ldexpf(1.0f, -(k / 2)), f2 = ldexpf(1.0f, -(k - k / 2));
   Sum again;
   for (j = j0 + lane; j < j1; j += 32) {
@@ -255,92 +219,146 @@ __device__ __forceinline__ int find_tensor(const GnEntry* list, int count, int64
   }
   return lo;
 }
-// warp w of n owns units [first(w), first(w + 1)); owner(u) has unit u
-__device__ __forceinline__ int64_t first_unit(int64_t w, int64_t n, int64_t units) { return units * w / n; }
-__device__ __forceinline__ int64_t owner(int64_t u, int64_t n, int64_t units) { return ((u + 1) * n - 1) / units; }
+// warp w of n owns units [first(w), first(w + 1)); owner(u) has unit u (in 32
+// bits where the numbers fit: a 64-bit division is a hundred instructions)
+template <typename I>
+__device__ __forceinline__ I first_unit(I w, I n, I units) {
+  return units * w / n;
+}
+template <typename I>
+__device__ __forceinline__ I owner(I u, I n, I units) {
+  return ((u + 1) * n - 1) / units;
+}
 
 // the norm of a sum, times unscale, once rounded
 template <int NORM>
 __device__ __forceinline__ float to_norm(double s, float unscale) {
-  return (float)((NORM == PEAT_NORM_2 ? sqrt(s) : s) * (double)unscale);
+  if (NORM == PEAT_NORM_2) {
+    // the root in float32 of s = f 4^k, 1 <= f < 4 (a binary64 root is slow here)
+    const long long b = __double_as_longlong(s);
+    const int e = (int)(b >> 52 & 0x7ff) - 1023, k = e >> 1;  // (no subnormal s: squares of float32 values)
+    if (!(s > 0.0) || e == 1024) return (float)(s * (double)unscale);
+    const float f = (float)__longlong_as_double((b & 0x000fffffffffffffll) | (long long)(1023 + (e & 1)) << 52);
+    return (float)((double)__fsqrt_rn(f) * (double)unscale * __longlong_as_double((long long)(1023 + k) << 52));
+  }
+  return (float)(s * (double)unscale);
 }
 
-// the pieces of every tensor, in order, by the CTA that finished last
-template <int NORM>
-__device__ void finish(const GnParams& p, const GnEntry* list) {
-  __shared__ double wsum[GB / 32];
-  __shared__ unsigned long long wbad[GB / 32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  double all = 0.0;
+// totals of one tensor or of several
+struct Total {
+  double s = 0.0;
   unsigned long long bad = 0;
-  for (int t = warp; t < p.count; t += GB / 32) {
-    const int64_t u0 = list[t].unit0, u1 = t + 1 < p.count ? list[t + 1].unit0 : p.units;
-    double s = 0.0;
-    unsigned long long nb = 0;
-    if (u1 > u0) {
-      const int64_t w0 = owner(u0, p.nwarps, p.units), w1 = owner(u1 - 1, p.nwarps, p.units);
-      for (int64_t w = w0 + lane; w <= w1; w += 32) {
-        const double v = __ldcg(&p.parts[t + w].s);
-        s = NORM == PEAT_NORM_INF ? (v > s || isnan(v) ? v : s) : s + v;  // (a NaN stays: nothing is above it)
-        nb += __ldcg(&p.parts[t + w].bad);
-      }
-    }
-    if (NORM == PEAT_NORM_INF) {
-#pragma unroll
-      for (int o = 16; o; o /= 2) {
-        const double v = __shfl_xor_sync(0xffffffffu, s, o);
-        s = v > s || isnan(v) ? v : s;
-      }
-    } else {
-      s = warp_sum(s);
-    }
-#pragma unroll
-    for (int o = 16; o; o /= 2) nb += __shfl_xor_sync(0xffffffffu, nb, o);
-    bad += nb;
-    all = NORM == PEAT_NORM_INF ? (s > all || isnan(s) ? s : all) : all + s;
-    if (lane == 0 && p.norms) p.norms[t] = to_norm<NORM>(s, p.unscale);
+  template <int NORM>
+  __device__ __forceinline__ void add(double v, unsigned long long b) {
+    s = NORM == PEAT_NORM_INF ? (v > s || isnan(v) ? v : s) : s + v;  // (a NaN stays: nothing is above it)
+    bad += b;
   }
-  if (lane == 0) wsum[warp] = all, wbad[warp] = bad;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < GB / 32; w++) {
-      const double s = wsum[w];
-      all = NORM == PEAT_NORM_INF ? (s > all || isnan(s) ? s : all) : all + s;
-      bad += wbad[w];
+  template <int NORM>
+  __device__ __forceinline__ void warp() {
+#pragma unroll
+    for (int o = 16; o; o /= 2) {
+      const double v = __shfl_xor_sync(0xffffffffu, s, o);
+      const unsigned long long b = __shfl_xor_sync(0xffffffffu, bad, o);
+      add<NORM>(v, b);
     }
-    peat_gradnorm_t r;
-    r.norm = to_norm<NORM>(all, p.unscale);
-    r.n_bad = bad;
+  }
+};
+
+// the record from the tensors' sums, by a CTA of NT threads; thread 0 returns it
+template <int NORM, int NT, typename F>
+__device__ peat_gradnorm_t finish(const GnParams& p, F tensor) {
+  __shared__ Total part[NT / 32];
+  Total all;
+  for (int t = threadIdx.x; t < p.count; t += NT) {
+    const GnPartial r = tensor(t);
+    if (p.norms) p.norms[t] = to_norm<NORM>(r.s, p.unscale);
+    all.add<NORM>(r.s, r.bad);
+  }
+  all.warp<NORM>();
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = all;
+  __syncthreads();
+  peat_gradnorm_t r = {};
+  if (threadIdx.x < 32) {
+    all = Total();
+    if (threadIdx.x < NT / 32) all = part[threadIdx.x];
+    all.warp<NORM>();
+    r.norm = to_norm<NORM>(all.s, p.unscale);
+    r.n_bad = all.bad;
     float c = 1.0f;
     if (p.clip) {
       const float q = __fdiv_rn(p.max_norm, __fadd_rn(r.norm, p.eps));
       c = q >= 1.0f ? 1.0f : q;  // (a NaN stays one)
-      if (bad && p.bad_mode == PEAT_BAD_ZERO) c = 0.0f;
-      if (bad && p.bad_mode == PEAT_BAD_KEEP) c = 1.0f;
+      if (r.n_bad && p.bad_mode == PEAT_BAD_ZERO) c = 0.0f;
+      if (r.n_bad && p.bad_mode == PEAT_BAD_KEEP) c = 1.0f;
     }
     r.coef = c;
-    *p.result = r;
-    *p.done = 0;
+    if (threadIdx.x == 0) *p.result = r;
   }
+  return r;
+}
+
+// the pieces w0..w1 of a tensor, in a fixed order, by a warp
+template <int NORM>
+__device__ __forceinline__ GnPartial gather(const GnPartial* parts, int t, int64_t w0, int64_t w1, bool global) {
+  Total all;
+  for (int64_t w = w0 + (threadIdx.x & 31); w <= w1; w += 32) {
+    const GnPartial* q = parts + t + w;
+    all.add<NORM>(global ? __ldcg(&q->s) : q->s, global ? __ldcg(&q->bad) : q->bad);
+  }
+  all.warp<NORM>();
+  GnPartial r;
+  r.s = all.s;
+  r.bad = all.bad;
+  return r;
+}
+
+// Warp w's pieces.  A tensor that lies in one warp's share is done with that;
+// one of several pieces is added up by the warp that comes last to it.
+template <int NORM>
+__device__ __forceinline__ void pieces_of(const GnParams& p, const GnEntry* list, int64_t w) {
+  if (w >= p.nwarps || p.units == 0) return;
+  const int lane = threadIdx.x & 31;
+  int64_t u = first_unit<int64_t>(w, p.nwarps, p.units);
+  const int64_t begin = u, end = first_unit<int64_t>(w + 1, p.nwarps, p.units);
+  if (u >= end) return;
+  for (int t = find_tensor(list, p.count, u); u < end; t++) {
+    const GnEntry e = list[t];
+    const int64_t next = t + 1 < p.count ? list[t + 1].unit0 : p.units, stop = min(end, next);
+    if (stop <= u) continue;
+    const GnPartial r = piece_of<NORM>(e, u - e.unit0, stop - e.unit0);
+    u = stop;
+    if (e.unit0 >= begin && next <= end) {
+      if (lane == 0) p.sums[t] = r;
+      continue;
+    }
+    const int64_t w0 = owner<int64_t>(e.unit0, p.nwarps, p.units), w1 = owner<int64_t>(next - 1, p.nwarps, p.units);
+    unsigned int n = 0;
+    if (lane == 0) {
+      p.parts[t + w] = r;
+      __threadfence();
+      n = atomicAdd(p.tickets + t, 1u);
+    }
+    if (__shfl_sync(0xffffffffu, n, 0) != (unsigned)(w1 - w0)) continue;
+    __threadfence();
+    const GnPartial all = gather<NORM>(p.parts, t, w0, w1, true);
+    if (lane == 0) {
+      p.sums[t] = all;
+      p.tickets[t] = 0;
+    }
+  }
+}
+__device__ __forceinline__ GnPartial load_sum(const GnPartial* q) {
+  GnPartial r;
+  r.s = __ldcg(&q->s);
+  r.bad = __ldcg(&q->bad);
+  return r;
 }
 
 template <int NORM>
 __global__ void __launch_bounds__(GB) gn_norm(GnParams p, const __grid_constant__ GnInline in) {
+  pdl_trigger();
   const GnEntry* list = p.list ? p.list : in.e;
-  const int64_t w = (int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5);
-  if (w < p.nwarps && p.units > 0) {
-    int64_t u = first_unit(w, p.nwarps, p.units);
-    const int64_t end = first_unit(w + 1, p.nwarps, p.units);
-    for (int t = find_tensor(list, p.count, u); u < end; t++) {
-      const GnEntry e = list[t];
-      const int64_t stop = min(end, t + 1 < p.count ? list[t + 1].unit0 : p.units);
-      if (stop > u) {
-        const GnPartial r = piece_of<NORM>(e, u - e.unit0, stop - e.unit0);
-        if ((threadIdx.x & 31) == 0) p.parts[t + w] = r;
-        u = stop;
-      }
-    }
-  }
+  pieces_of<NORM>(p, list, (int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5));
   __shared__ bool last;
   __threadfence();
   __syncthreads();
@@ -348,7 +366,11 @@ __global__ void __launch_bounds__(GB) gn_norm(GnParams p, const __grid_constant_
   __syncthreads();
   if (!last) return;
   __threadfence();
-  finish<NORM>(p, list);
+  finish<NORM, GB>(p, [&](int t) {
+    const int64_t next = t + 1 < p.count ? list[t + 1].unit0 : p.units;
+    return next > list[t].unit0 ? load_sum(p.sums + t) : GnPartial{0.0, 0ull};  // (an empty tensor has no sum)
+  });
+  if (threadIdx.x == 0) *p.done = 0;
 }
 
 template <int DT>
@@ -405,14 +427,11 @@ __device__ void scale_piece(const GnEntry& e, int64_t j0, int64_t j1, float f, b
   }
 }
 
-__global__ void __launch_bounds__(GB) gn_scale(GnParams p, const __grid_constant__ GnInline in) {
-  const GnEntry* list = p.list ? p.list : in.e;
-  const int64_t n = (int64_t)gridDim.x * (GB / 32);
-  const int64_t w = n - 1 - ((int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5));
-  const float f = __fmul_rn(p.unscale, __ldcg(&p.result->coef));
-  const bool zero = p.bad_mode == PEAT_BAD_ZERO && __ldcg(&p.result->n_bad) != 0;
-  int64_t u = first_unit(w, n, p.units);
-  const int64_t end = first_unit(w + 1, n, p.units);
+// warp w's share of n of the list, scaled by f (or set to zero)
+template <typename I>
+__device__ __forceinline__ void scale_share(const GnParams& p, const GnEntry* list, I w, I n, float f, bool zero) {
+  int64_t u = first_unit<I>(w, n, (I)p.units);
+  const int64_t end = first_unit<I>(w + 1, n, (I)p.units);
   if (u >= end) return;
   for (int t = find_tensor(list, p.count, u); u < end; t++) {
     const GnEntry e = list[t];
@@ -426,6 +445,56 @@ __global__ void __launch_bounds__(GB) gn_scale(GnParams p, const __grid_constant
     u = stop;
   }
 }
+__global__ void __launch_bounds__(GB) gn_scale(GnParams p, const __grid_constant__ GnInline in) {
+  pdl_wait();
+  const GnEntry* list = p.list ? p.list : in.e;
+  const int64_t n = (int64_t)gridDim.x * (GB / 32);
+  const float f = __fmul_rn(p.unscale, __ldcg(&p.result->coef));
+  const bool zero = p.bad_mode == PEAT_BAD_ZERO && __ldcg(&p.result->n_bad) != 0;
+  scale_share<int64_t>(p, list, n - 1 - ((int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5)), n, f, zero);
+}
+
+// A small list by one CTA, norm and clipping in one launch: a launch and the
+// meeting of CTAs in global memory cost more than its bytes. 
+template <int NORM>
+__global__ void __launch_bounds__(GB_SMALL) gn_small(GnParams p, const __grid_constant__ GnInline in) {
+  constexpr int W = GB_SMALL / 32;
+  __shared__ GnPartial parts[GN_INLINE + W], sums[GN_INLINE];
+  __shared__ float f;
+  __shared__ bool zero;
+  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const GnEntry* list = in.e;
+  // every warp that counts has a unit, so every part that is gathered was written
+  const uint32_t units = (uint32_t)p.units, n = min((uint32_t)W, max(units, 1u));
+  if (w < n && units > 0) {
+    int64_t u = first_unit<uint32_t>(w, n, units);
+    const int64_t end = first_unit<uint32_t>(w + 1, n, units);
+    for (int t = find_tensor(list, p.count, u); u < end; t++) {
+      const GnEntry e = list[t];
+      const int64_t stop = min(end, t + 1 < p.count ? list[t + 1].unit0 : p.units);
+      if (stop <= u) continue;
+      const GnPartial r = piece_of<NORM>(e, u - e.unit0, stop - e.unit0);
+      if (lane == 0) parts[t + w] = r;
+      u = stop;
+    }
+  }
+  __syncthreads();
+  for (int t = w; t < p.count; t += W) {
+    const int64_t u0 = list[t].unit0, u1 = t + 1 < p.count ? list[t + 1].unit0 : p.units;
+    GnPartial r{0.0, 0ull};
+    if (u1 > u0) r = gather<NORM>(parts, t, owner<uint32_t>((uint32_t)u0, n, units), owner<uint32_t>((uint32_t)u1 - 1, n, units), false);
+    if (lane == 0) sums[t] = r;
+  }
+  __syncthreads();
+  const peat_gradnorm_t r = finish<NORM, GB_SMALL>(p, [&](int t) { return sums[t]; });
+  if (!p.clip) return;
+  if (threadIdx.x == 0) {
+    f = __fmul_rn(p.unscale, r.coef);
+    zero = p.bad_mode == PEAT_BAD_ZERO && r.n_bad != 0;
+  }
+  __syncthreads();
+  if (p.units > 0) scale_share<uint32_t>(p, list, w, W, f, zero);
+}
 
 }  // namespace
 
@@ -435,10 +504,14 @@ cudaError_t launch_gradnorm(const GnParams& p, const GnInline& in, int nctas, cu
   if (p.type == PEAT_NORM_1) gn_norm<PEAT_NORM_1><<<nctas, GB, 0, s>>>(p, in);
   else if (p.type == PEAT_NORM_INF) gn_norm<PEAT_NORM_INF><<<nctas, GB, 0, s>>>(p, in);
   else gn_norm<PEAT_NORM_2><<<nctas, GB, 0, s>>>(p, in);
-  return cudaGetLastError();
+  cudaError_t e = cudaGetLastError();
+  if (e == cudaSuccess && p.clip && p.units > 0) e = launch_dependent(gn_scale, (unsigned)nctas, GB, 0, s, p, in);
+  return e;
 }
-cudaError_t launch_gradscale(const GnParams& p, const GnInline& in, int nctas, cudaStream_t s) {
-  gn_scale<<<nctas, GB, 0, s>>>(p, in);
+cudaError_t launch_gradnorm_small(const GnParams& p, const GnInline& in, cudaStream_t s) {
+  if (p.type == PEAT_NORM_1) gn_small<PEAT_NORM_1><<<1, GB_SMALL, 0, s>>>(p, in);
+  else if (p.type == PEAT_NORM_INF) gn_small<PEAT_NORM_INF><<<1, GB_SMALL, 0, s>>>(p, in);
+  else gn_small<PEAT_NORM_2><<<1, GB_SMALL, 0, s>>>(p, in);
   return cudaGetLastError();
 }
 

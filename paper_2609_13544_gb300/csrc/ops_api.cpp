@@ -26,6 +26,13 @@ struct OpsState {
   bool pending[RING] = {};
   int next = 0;
   unsigned int* done = nullptr;  // zero between calls
+  void* tickets = nullptr;       // one for each tensor of a list, zero between calls
+  size_t tickets_cap = 0;
+  // column maxima: two buffers in turn; a call clears the other one's last use
+  void* colmax = nullptr;
+  size_t colmax_cap = 0;  // bytes of both
+  int64_t colmax_used[2] = {0, 0};
+  int colmax_at = 0;
   // products: packed operands; integer sums of split tiles, zero between calls
   void* mm = nullptr;
   size_t mm_cap = 0;
@@ -37,6 +44,8 @@ void ops_destroy(OpsState* s) {
   if (!s) return;
   if (s->d_list) cudaFree(s->d_list);
   if (s->done) cudaFree(s->done);
+  if (s->tickets) cudaFree(s->tickets);
+  if (s->colmax) cudaFree(s->colmax);
   if (s->mm) cudaFree(s->mm);
   if (s->zeros) cudaFree(s->zeros);
   for (int i = 0; i < OpsState::RING; i++) {
@@ -124,8 +133,38 @@ peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t col
   const int qa = axis == 0 ? E : 4;
   p.vec_q = q && aligned(q, qa) && ldq % qa == 0;
   p.vec_v = values && aligned(values, 16) && (ldv % E == 0 || rows <= 1);
-  cudaError_t e = peat::launch_quant8(dtype, axis, p, h->nsm, st);
-  if (e != cudaSuccess) return cuda_fail(h, e, "8-bit quantisation launch");
+  p.colmax = p.zero = nullptr;
+  p.zero_n = 0;
+  OpsState* s = nullptr;
+  cudaError_t e;
+  if (axis == 1) {
+    peat_status_t ps = ops_state(h, &s);
+    if (ps != PEAT_OK) return ps;
+    const size_t need = 2 * sizeof(unsigned int) * (size_t)std::max<int64_t>(cols, 16384);
+    if (need > s->colmax_cap) {
+      ps = grow(h, &s->colmax, &s->colmax_cap, need);
+      if (ps != PEAT_OK) return ps;
+      s->colmax_used[0] = s->colmax_used[1] = 0;
+      e = cudaMemsetAsync(s->colmax, 0, need, st);
+      if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(maxima)");
+    }
+    unsigned int* both = static_cast<unsigned int*>(s->colmax);
+    const size_t half = s->colmax_cap / 2 / sizeof(unsigned int);
+    const int at = s->colmax_at;
+    p.colmax = both + at * half;
+    p.zero = both + (at ^ 1) * half;
+    p.zero_n = s->colmax_used[at ^ 1];
+  }
+  e = peat::launch_quant8(dtype, axis, p, h->nsm, st);
+  if (e != cudaSuccess) {
+    if (s) s->colmax_cap = 0;  // (made anew by the next call: a launch may have left maxima)
+    return cuda_fail(h, e, "8-bit quantisation launch");
+  }
+  if (s) {
+    s->colmax_used[s->colmax_at] = cols;
+    s->colmax_used[s->colmax_at ^ 1] = 0;
+    s->colmax_at ^= 1;
+  }
   return PEAT_OK;
 }
 
@@ -236,8 +275,16 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   const int64_t warps = std::max<int64_t>(1, std::min<int64_t>((units + 63) / 64, (int64_t)h->nsm * 4 * per));
   const int nctas = (int)((warps + per - 1) / per);
   const size_t listed = count > peat::GN_INLINE ? (sizeof(peat::GnEntry) * (size_t)count + 255) / 256 * 256 : 0;
-  ps = grow(h, &s->d_list, &s->d_list_cap, listed + sizeof(peat::GnPartial) * (size_t)(count + warps));
+  const size_t parted = sizeof(peat::GnPartial) * (size_t)(count + warps);
+  ps = grow(h, &s->d_list, &s->d_list_cap, listed + parted + sizeof(peat::GnPartial) * (size_t)count);
   if (ps != PEAT_OK) return ps;
+  const size_t tickets = sizeof(unsigned int) * (size_t)std::max<int64_t>(count, 1024);
+  if (tickets > s->tickets_cap) {
+    ps = grow(h, &s->tickets, &s->tickets_cap, tickets);
+    if (ps != PEAT_OK) return ps;
+    cudaError_t e = cudaMemsetAsync(s->tickets, 0, tickets, st);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(tickets)");
+  }
 
   peat::GnInline in;
   peat::GnEntry* dst = in.e;
@@ -293,11 +340,13 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   p.bad_mode = bad;
   p.clip = clip ? 1 : 0;
   p.parts = reinterpret_cast<peat::GnPartial*>(static_cast<char*>(s->d_list) + listed);
+  p.sums = reinterpret_cast<peat::GnPartial*>(static_cast<char*>(s->d_list) + listed + parted);
+  p.tickets = static_cast<unsigned int*>(s->tickets);
   p.done = s->done;
   p.result = result;
   p.norms = norms;
-  cudaError_t e = peat::launch_gradnorm(p, in, nctas, st);
-  if (e == cudaSuccess && clip && units > 0) e = peat::launch_gradscale(p, in, nctas, st);
+  cudaError_t e = !listed && units <= peat::GN_SMALL ? peat::launch_gradnorm_small(p, in, st)
+                                                     : peat::launch_gradnorm(p, in, nctas, st);
   if (e != cudaSuccess) return cuda_fail(h, e, "gradient norm launch");
   return PEAT_OK;
 }

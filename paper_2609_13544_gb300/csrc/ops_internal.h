@@ -21,6 +21,10 @@ struct QuantParams {
   int vec_x;  // x's rows start on 16-byte boundaries
   int vec_q;  // q's rows start on boundaries of a vector's integers (axis 0: 8 or 4 bytes; axis 1: 4 bytes)
   int vec_v;  // values' rows start on 16-byte boundaries
+  // columns: their largest patterns, zero before the call, and what to clear for a later one
+  unsigned int* colmax;
+  unsigned int* zero;
+  int64_t zero_n;
 };
 cudaError_t launch_quant8(int dtype, int axis, const QuantParams& p, int nsm, cudaStream_t s);
 
@@ -62,9 +66,8 @@ struct GnInline {
   GnEntry e[GN_INLINE];
 };
 struct GnPartial {
-  double s;          // sum (or maximum) of the piece
-  unsigned int bad;  // its NaN and infinite elements
-  unsigned int nan;  // of them, NaN
+  double s;                // sum (or maximum)
+  unsigned long long bad;  // NaN and infinite elements
 };
 struct GnParams {
   const GnEntry* list;  // device; null: the inline entries
@@ -76,13 +79,17 @@ struct GnParams {
   int bad_mode;
   int clip;             // 0: norm only
   GnPartial* parts;     // count + nwarps slots: warp w's part of tensor t at t + w
+  GnPartial* sums;      // one for each tensor
+  unsigned int* tickets;  // pieces finished, one for each tensor, zero between calls
   unsigned int* done;   // CTAs finished, zero between calls
   peat_gradnorm_t* result;
   float* norms;         // or null
 };
 int gn_block();  // threads of a CTA of both passes
 cudaError_t launch_gradnorm(const GnParams& p, const GnInline& in, int nctas, cudaStream_t s);
-cudaError_t launch_gradscale(const GnParams& p, const GnInline& in, int nctas, cudaStream_t s);
+// the whole call in one CTA, for an inline list of at most GN_SMALL units
+constexpr int64_t GN_SMALL = 8192;
+cudaError_t launch_gradnorm_small(const GnParams& p, const GnInline& in, cudaStream_t s);
 // 16-byte units that hold the n elements of `size` bytes at g
 inline int64_t gn_units(const void* g, int64_t n, int size) {
   if (n <= 0) return 0;

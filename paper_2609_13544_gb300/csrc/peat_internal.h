@@ -22,13 +22,13 @@ namespace peat {
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <typename... KA, typename... A>
-inline cudaError_t launch_dependent(void (*kernel)(KA...), unsigned grid, unsigned block, size_t smem,
+inline cudaError_t launch_dependent(void (*kernel)(KA...), dim3 grid, unsigned block, size_t smem,
                                     cudaStream_t s, A... args) {
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(block);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;

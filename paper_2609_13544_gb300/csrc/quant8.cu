@@ -1,21 +1,18 @@
 // Rounding of a matrix to 8-bit integers with one scale for each row or column.
 //
 // Over a row (or column): amax = max |x|, scale = amax / 127, r = 127 / amax,
-// q = rint(x r), all float32.  The maximum is taken on the bit patterns
-// without their sign, which order as the magnitudes do and put infinities and
-// NaNs above every number, so one integer maximum finds both amax and whether
-// the row is finite.
+// q = rint(x r), all float32.  The maximum is one that keeps NaNs, so it finds
+// both amax and whether the row is finite; it is handed on as a bit pattern
+// without sign, which order as the magnitudes do, infinities and NaNs on top.
 //
 // Bound by memory: a row is read once and kept in registers between the
-// maximum and the rounding; a strip of columns is read twice, the second time
-// from L2.
-#include <cooperative_groups.h>
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
+// maximum and the rounding; columns are read twice, as far as they fit from L2
+// the second time.
+#include <algorithm>
 
 #include "ops_internal.h"
-
-namespace cg = cooperative_groups;
+#include "peat_internal.h"
+#include "vec16.cuh"
 
 namespace peat {
 namespace {
@@ -61,22 +58,36 @@ union Vec {
   __device__ Vec() {}
 };
 
-// elementwise maximum of the magnitudes' bit patterns: four words, or eight half-words
+// elementwise maximum of the magnitudes; a NaN on either side stays (as a NaN
+// pattern, above every number's).  The types' own maxima: the packed integer
+// ones are several instructions each on this GPU.
+__device__ __forceinline__ uint32_t max_f32(uint32_t m, uint32_t v) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(m)), "f"(fabsf(__uint_as_float(v))));
+  return __float_as_uint(r) & 0x7fffffffu;
+}
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t m, uint32_t v) {
+  uint32_t r;
+  asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(v & 0x7fff7fffu));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t m, uint32_t v) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(v & 0x7fff7fffu));
+  return r;
+}
+template <int DT>
+__device__ __forceinline__ uint32_t max_word(uint32_t m, uint32_t v) {
+  return DT == PEAT_F32 ? max_f32(m, v) : (DT == PEAT_F16 ? max_f16x2(m, v) : max_bf16x2(m, v));
+}
 template <int DT>
 __device__ __forceinline__ uint4 mag_max(uint4 m, uint4 v) {
-  if (DT == PEAT_F32) {
-    return make_uint4(max(m.x, v.x & 0x7fffffffu), max(m.y, v.y & 0x7fffffffu), max(m.z, v.z & 0x7fffffffu),
-                      max(m.w, v.w & 0x7fffffffu));
-  } else {
-    return make_uint4(__vmaxu2(m.x, v.x & 0x7fff7fffu), __vmaxu2(m.y, v.y & 0x7fff7fffu),
-                      __vmaxu2(m.z, v.z & 0x7fff7fffu), __vmaxu2(m.w, v.w & 0x7fff7fffu));
-  }
+  return make_uint4(max_word<DT>(m.x, v.x), max_word<DT>(m.y, v.y), max_word<DT>(m.z, v.z), max_word<DT>(m.w, v.w));
 }
 template <int DT>
 __device__ __forceinline__ uint32_t mag_fold(uint4 m) {  // the largest of the vector
-  if (DT == PEAT_F32) return max(max(m.x, m.y), max(m.z, m.w));
-  const uint32_t a = __vmaxu2(__vmaxu2(m.x, m.y), __vmaxu2(m.z, m.w));
-  return max(a & 0xffffu, a >> 16);
+  const uint32_t a = max_word<DT>(max_word<DT>(m.x, m.y), max_word<DT>(m.z, m.w));
+  return DT == PEAT_F32 ? a : max(a & 0xffffu, a >> 16);
 }
 
 // r and scale of a row from its largest pattern
@@ -92,38 +103,63 @@ __device__ __forceinline__ void factors(uint32_t m, float& r, float& scale) {
   scale = __fdiv_rn(amax, 127.0f);
   if (!(r <= 3.402823466e38f)) r = scale = 0.0f;  // amax 0, or too small for a finite r
 }
-// the integer of x; a non-finite row has r = 0, and 0 x NaN must not get through
-template <int DT>
-__device__ __forceinline__ int whole(float x, float r, bool finite) {
-  return finite ? __float2int_rn(__fmul_rn(x, r)) : 0;
+// The integer of x: the float32 product x r, added to 1.5 2^23, has it in its
+// low bits, rounded to nearest even (conversion instructions run at an eighth of
+// the additions' rate).  A row that is not finite has r = 0, and 0 x NaN must
+// not get through.
+constexpr float MAGIC = 12582912.0f;
+__device__ __forceinline__ float whole(float x, float r, bool finite) {
+  return finite ? __fadd_rn(__fmul_rn(x, r), MAGIC) : MAGIC;
 }
-__device__ __forceinline__ uint32_t pack4(int a, int b, int c, int d) {
-  return __byte_perm(__byte_perm((uint32_t)a, (uint32_t)b, 0x0040), __byte_perm((uint32_t)c, (uint32_t)d, 0x0040), 0x5410);
+__device__ __forceinline__ float number(float w) { return __fsub_rn(w, MAGIC); }
+__device__ __forceinline__ int8_t byte_of(float w) { return (int8_t)__float_as_uint(w); }
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+  return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
+                     __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
 }
 
 // the first `left` elements of a vector at p (left < E: one by one, zero beyond)
 template <int DT, bool VEC>
-__device__ __forceinline__ Vec<DT> load_vec(const typename Elem<DT>::T* p, int64_t left) {
+__device__ __forceinline__ uint4 load_vec(const typename Elem<DT>::T* p, int64_t left) {
+  if (VEC && left >= Elem<DT>::E) return __ldg(reinterpret_cast<const uint4*>(p));
   Vec<DT> v;
-  if (VEC && left >= Elem<DT>::E) {
-    v.u = __ldg(reinterpret_cast<const uint4*>(p));
-    return v;
-  }
   v.u = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int e = 0; e < Elem<DT>::E; e++)
     if (e < left) v.e[e] = p[e];
-  return v;
+  return v.u;
+}
+
+// a vector's integers (in float32, see whole) from its row's or its columns' factors
+template <int DT, bool FINITE>
+__device__ __forceinline__ void wholes(uint4 v, float r, float (&w)[Elem<DT>::E]) {
+  float x[Elem<DT>::E];
+  unpack<DT>(v, x);
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::E; e++) w[e] = whole(x[e], r, FINITE);
+}
+// a vector's values at o, of which `left` exist
+template <int DT>
+__device__ __forceinline__ void store_values(typename Elem<DT>::T* o, const float (&y)[Elem<DT>::E], bool vec, int64_t left) {
+  Vec<DT> v;
+  v.u = pack<DT>(y);
+  if (vec && left >= Elem<DT>::E) {
+    __stcs(reinterpret_cast<uint4*>(o), v.u);
+  } else {
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::E; e++)
+      if (e < left) o[e] = v.e[e];
+  }
 }
 
 // integers and values of one vector of a row
 template <int DT>
-__device__ __forceinline__ void store_row_vec(const QuantParams& p, const Vec<DT>& v, int64_t row, int64_t col,
-                                              int64_t left, float r, float scale, bool finite) {
+__device__ __forceinline__ void store_row_vec(const QuantParams& p, uint4 v, int64_t row, int64_t col, int64_t left,
+                                              float r, float scale, bool finite) {
   using L = Elem<DT>;
-  int w[L::E];
-#pragma unroll
-  for (int e = 0; e < L::E; e++) w[e] = whole<DT>(L::up(v.e[e]), r, finite);
+  float w[L::E];
+  if (finite) wholes<DT, true>(v, r, w);
+  else wholes<DT, false>(v, r, w);
   if (p.q) {
     int8_t* q = p.q + row * p.ldq + col;
     if (p.vec_q && left >= L::E) {
@@ -134,21 +170,14 @@ __device__ __forceinline__ void store_row_vec(const QuantParams& p, const Vec<DT
     } else {
 #pragma unroll
       for (int e = 0; e < L::E; e++)
-        if (e < left) q[e] = (int8_t)w[e];
+        if (e < left) q[e] = byte_of(w[e]);
     }
   }
   if (p.values) {
-    typename L::T* o = static_cast<typename L::T*>(p.values) + row * p.ldv + col;
-    Vec<DT> y;
+    float y[L::E];
 #pragma unroll
-    for (int e = 0; e < L::E; e++) y.e[e] = L::down(__fmul_rn((float)w[e], scale));
-    if (p.vec_v && left >= L::E) {
-      *reinterpret_cast<uint4*>(o) = y.u;
-    } else {
-#pragma unroll
-      for (int e = 0; e < L::E; e++)
-        if (e < left) o[e] = y.e[e];
-    }
+    for (int e = 0; e < L::E; e++) y[e] = __fmul_rn(number(w[e]), scale);
+    store_values<DT>(static_cast<typename L::T*>(p.values) + row * p.ldv + col, y, p.vec_v, left);
   }
 }
 
@@ -174,16 +203,23 @@ __global__ void __launch_bounds__(QT) quant_rows(QuantParams p) {
   const int64_t row = (int64_t)blockIdx.x * (QT / TPR) + threadIdx.x / TPR;
   if (row >= p.rows) return;  // (whole warps; with TPR = QT there is a row for every CTA)
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + row * p.ldx;
-  Vec<DT> v[NV];
+  uint4 v[NV];
   uint4 m = make_uint4(0, 0, 0, 0);
 #pragma unroll
   for (int i = 0; i < NV; i++) {
     const int64_t col = (int64_t)(i * TPR + lane) * L::E;
-    v[i].u = make_uint4(0, 0, 0, 0);
-    if (col < p.cols) v[i] = load_vec<DT, true>(x + col, p.cols - col);
+    v[i] = make_uint4(0, 0, 0, 0);
+    if (col + L::E <= p.cols) v[i] = __ldg(reinterpret_cast<const uint4*>(x + col));
+  }
+  if (p.cols % L::E) {  // the row's last vector
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int64_t col = (int64_t)(i * TPR + lane) * L::E;
+      if (col < p.cols && col + L::E > p.cols) v[i] = load_vec<DT, false>(x + col, p.cols - col);
+    }
   }
 #pragma unroll
-  for (int i = 0; i < NV; i++) m = mag_max<DT>(m, v[i].u);
+  for (int i = 0; i < NV; i++) m = mag_max<DT>(m, v[i]);
   const uint32_t top = row_max<TPR>(mag_fold<DT>(m));
   float r, scale;
   factors<DT>(top, r, scale);
@@ -208,7 +244,7 @@ __global__ void __launch_bounds__(QT) quant_rows_twice(QuantParams p) {
     uint4 m = make_uint4(0, 0, 0, 0);
 #pragma unroll 4
     for (int64_t col = (int64_t)threadIdx.x * L::E; col < p.cols; col += QT * L::E)
-      m = mag_max<DT>(m, load_vec<DT, true>(x + col, p.cols - col).u);
+      m = mag_max<DT>(m, load_vec<DT, true>(x + col, p.cols - col));
     top = mag_fold<DT>(m);
   } else {
 #pragma unroll 8
@@ -228,103 +264,151 @@ __global__ void __launch_bounds__(QT) quant_rows_twice(QuantParams p) {
     typename L::T* o = p.values ? static_cast<typename L::T*>(p.values) + row * p.ldv : nullptr;
 #pragma unroll 4
     for (int64_t col = threadIdx.x; col < p.cols; col += QT) {
-      const int w = whole<DT>(L::up(x[col]), r, finite);
-      if (q) q[col] = (int8_t)w;
-      if (o) o[col] = L::down(__fmul_rn((float)w, scale));
+      const float w = whole(L::up(x[col]), r, finite);
+      if (q) q[col] = byte_of(w);
+      if (o) o[col] = L::down(__fmul_rn(number(w), scale));
     }
   }
 }
 
-// Columns: a cluster takes a strip of 128 bytes of columns (64 or 32), its
-// CTAs a share of the rows each.  The maxima meet in distributed shared memory;
-// then each CTA reads its share again (from L2: it has just been read) in
-// tiles of 128 rows and writes the integers transposed through shared memory,
-// 128 contiguous ones a column.
-constexpr int TR = 128;  // rows of a tile
+// Columns, in two launches.  The first finds each column's maximum: a thread
+// has a 16-byte vector of columns (VEC false: one column) and walks down a
+// share of the rows, the shares meet by atomic maxima of the patterns.  The
+// second reads the matrix again, last rows first, so that it finds in L2 what
+// the first read last, in tiles of 128 rows by 128 bytes, and writes the
+// integers transposed through shared memory, 128 contiguous ones of a column
+// at a time.  (One launch of clusters that keep a strip of columns to
+// themselves, meet in distributed shared memory and read the strip again from
+// L2 took 101 us for 16384 x 4096 bfloat16 values where these take CCC: its
+// phases wait for each other.)
 template <int DT, bool VEC>
-__global__ void __launch_bounds__(QT) quant_cols(QuantParams p) {
+__global__ void __launch_bounds__(QT) quant_colmax(QuantParams p, int vl, int64_t rows_each) {
   using L = Elem<DT>;
-  constexpr int CW = 8 * L::E;  // columns of a strip
-  __shared__ uint4 part[QT / 32][8];
-  __shared__ uint4 mine[8];
-  __shared__ uint32_t tile[CW][TR / 4 + 1];
-  cg::cluster_group cl = cg::this_cluster();
-  const int S = (int)cl.num_blocks(), rank = (int)cl.block_rank();
-  const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3;
-  const int64_t col = ((int64_t)blockIdx.x / S) * CW + tx * L::E;
-  const int64_t left = p.cols - col;  // may be <= 0
-  const int64_t tiles = (p.rows + TR - 1) / TR;
-  const int64_t r0 = tiles * rank / S * TR, r1 = min(p.rows, tiles * (rank + 1) / S * TR);
+  pdl_trigger();
+  __shared__ uint4 part[QT];
+  const int lx = threadIdx.x % vl, ly = threadIdx.x / vl, nl = QT / vl;
+  const int64_t r0 = (int64_t)blockIdx.y * rows_each, r1 = min(p.rows, r0 + rows_each);
+  const int64_t col = ((int64_t)blockIdx.x * vl + lx) * (VEC ? L::E : 1), left = p.cols - col;
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + col;
-
   uint4 m = make_uint4(0, 0, 0, 0);
   if (left > 0) {
-#pragma unroll 8
-    for (int64_t r = r0 + ty; r < r1; r += 32) m = mag_max<DT>(m, load_vec<DT, VEC>(x + r * p.ldx, left).u);
-  }
+    constexpr int U = 8;  // rows in flight; past the end the last row again, which changes no maximum
+    if (VEC && left >= L::E) {
+      for (int64_t r = r0 + ly; r < r1; r += U * nl) {
+        uint4 u[U];
 #pragma unroll
-  for (int o = 8; o <= 16; o *= 2) {
-    uint4 t;
-    t.x = __shfl_xor_sync(0xffffffffu, m.x, o);
-    t.y = __shfl_xor_sync(0xffffffffu, m.y, o);
-    t.z = __shfl_xor_sync(0xffffffffu, m.z, o);
-    t.w = __shfl_xor_sync(0xffffffffu, m.w, o);
-    m = mag_max<DT>(m, t);
+        for (int i = 0; i < U; i++) u[i] = __ldg(reinterpret_cast<const uint4*>(x + min(r + i * nl, r1 - 1) * p.ldx));
+#pragma unroll
+        for (int i = 0; i < U; i++) m = mag_max<DT>(m, u[i]);
+      }
+    } else if (VEC) {
+      for (int64_t r = r0 + ly; r < r1; r += nl) m = mag_max<DT>(m, load_vec<DT, false>(x + r * p.ldx, left));
+    } else {
+      for (int64_t r = r0 + ly; r < r1; r += U * nl) {
+        uint32_t u[U];
+#pragma unroll
+        for (int i = 0; i < U; i++) u[i] = L::bits(x[min(r + i * nl, r1 - 1) * p.ldx]);
+#pragma unroll
+        for (int i = 0; i < U; i++) m.x = max(m.x, u[i]);
+      }
+    }
   }
-  if ((threadIdx.x & 31) < 8) part[threadIdx.x >> 5][tx] = m;
+  part[threadIdx.x] = m;
   __syncthreads();
-  if (threadIdx.x < 8) {
+  if (ly > 0 || left <= 0) return;
+  for (int k = 1; k < nl; k++) {
+    if (VEC) m = mag_max<DT>(m, part[k * vl + lx]);
+    else m.x = max(m.x, part[k * vl + lx].x);
+  }
+  if (VEC) {
+    const uint32_t w[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
-    for (int w = 0; w < QT / 32; w++) m = mag_max<DT>(m, part[w][tx]);
-    mine[tx] = m;
+    for (int e = 0; e < L::E; e++) {
+      const uint32_t b = L::E == 4 ? w[e % 4] : (e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu);
+      if (e < left) atomicMax(p.colmax + col + e, b);
+    }
+  } else {
+    atomicMax(p.colmax + col, m.x);
   }
-  cl.sync();
-  m = mine[tx];
-  for (int k = 1; k < S; k++) {
-    int o = rank + k;
-    o = o < S ? o : o - S;
-    m = mag_max<DT>(m, *cl.map_shared_rank(&mine[tx], o));
+}
+
+constexpr int TR = 128;  // rows of a tile
+template <int DT, bool VEC>
+__global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_each) {
+  using L = Elem<DT>;
+  constexpr int CW = 8 * L::E;  // columns of a tile
+  __shared__ __align__(16) float rs[CW], ss[CW];
+  __shared__ uint32_t bads[2];
+  __shared__ uint32_t tile[CW][TR / 4 + 1];
+  const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3;
+  const int64_t c0 = (int64_t)blockIdx.x * CW, col = c0 + tx * L::E;
+  const int64_t left = p.cols - col;  // may be <= 0
+  const int64_t r0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * rows_each, r1 = min(p.rows, r0 + rows_each);
+  const typename L::T* x = static_cast<const typename L::T*>(p.x) + col;
+  pdl_wait();
+  // the other buffer of maxima is the next call's: zero again
+  {
+    const int64_t n = (int64_t)gridDim.x * gridDim.y * QT;
+    for (int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * QT + threadIdx.x; i < p.zero_n; i += n) p.zero[i] = 0;
   }
+  auto load = [&](int64_t t0, uint4 (&v)[4]) {
+    const typename L::T* q = x + (t0 + ty * 4) * p.ldx;
+    if (VEC && left >= L::E && t0 + TR <= r1) {
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[j] = __ldg(reinterpret_cast<const uint4*>(q + j * p.ldx));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        v[j] = make_uint4(0, 0, 0, 0);
+        if (t0 + ty * 4 + j < r1 && left > 0) v[j] = load_vec<DT, VEC>(q + j * p.ldx, left);
+      }
+    }
+  };
+  uint4 v[4];
+  load(r0, v);
+  if (threadIdx.x < CW) {
+    const int c = threadIdx.x;
+    const uint32_t top = c0 + c < p.cols ? __ldcg(p.colmax + c0 + c) : 0;
+    float r, scale;
+    factors<DT>(top, r, scale);
+    rs[c] = r;
+    ss[c] = scale;
+    const uint32_t vote = __ballot_sync(0xffffffffu, top >= L::INF);
+    if ((c & 31) == 0) bads[c >> 5] = vote;
+    if (p.scale && blockIdx.y == 0 && c0 + c < p.cols) p.scale[c0 + c] = scale;
+  }
+  __syncthreads();
   float r[L::E], scale[L::E];
-  uint32_t bad = 0;
 #pragma unroll
-  for (int e = 0; e < L::E; e++) {
-    const uint32_t w = e < 2 * (L::E / 4) ? (e < L::E / 4 ? m.x : m.y) : (e < 3 * (L::E / 4) ? m.z : m.w);
-    const uint32_t b = L::E == 4 ? w : (e & 1 ? w >> 16 : w & 0xffffu);
-    factors<DT>(b, r[e], scale[e]);
-    if (b >= L::INF) bad |= 1u << e;
-    if (p.scale && rank == 0 && ty == 0 && e < left) p.scale[col + e] = scale[e];
+  for (int e = 0; e < L::E; e += 4) {
+    *reinterpret_cast<float4*>(r + e) = *reinterpret_cast<const float4*>(rs + tx * L::E + e);
+    *reinterpret_cast<float4*>(scale + e) = *reinterpret_cast<const float4*>(ss + tx * L::E + e);
   }
+  const uint32_t bad = bads[tx * L::E >> 5] >> (tx * L::E & 31) & ((1u << L::E) - 1u);
 
   for (int64_t t0 = r0; t0 < r1; t0 += TR) {
-    Vec<DT> v[4];
+    float w[4][L::E];
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-      const int64_t row = t0 + ty * 4 + j;
-      v[j].u = make_uint4(0, 0, 0, 0);
-      if (row < r1 && left > 0) v[j] = load_vec<DT, VEC>(x + row * p.ldx, left);
+      unpack<DT>(v[j], w[j]);
+      if (bad) {
+#pragma unroll
+        for (int e = 0; e < L::E; e++) w[j][e] = whole(w[j][e], r[e], !(bad >> e & 1));
+      } else {
+#pragma unroll
+        for (int e = 0; e < L::E; e++) w[j][e] = whole(w[j][e], r[e], true);
+      }
     }
-    int w[4][L::E];
-#pragma unroll
-    for (int j = 0; j < 4; j++)
-#pragma unroll
-      for (int e = 0; e < L::E; e++) w[j][e] = whole<DT>(L::up(v[j].e[e]), r[e], !(bad >> e & 1));
+    if (t0 + TR < r1) load(t0 + TR, v);  // the next tile is on its way
     if (p.values) {
 #pragma unroll
       for (int j = 0; j < 4; j++) {
         const int64_t row = t0 + ty * 4 + j;
         if (row >= r1 || left <= 0) continue;
-        typename L::T* o = static_cast<typename L::T*>(p.values) + row * p.ldv + col;
-        Vec<DT> y;
+        float y[L::E];
 #pragma unroll
-        for (int e = 0; e < L::E; e++) y.e[e] = L::down(__fmul_rn((float)w[j][e], scale[e]));
-        if (p.vec_v && left >= L::E) {
-          *reinterpret_cast<uint4*>(o) = y.u;
-        } else {
-#pragma unroll
-          for (int e = 0; e < L::E; e++)
-            if (e < left) o[e] = y.e[e];
-        }
+        for (int e = 0; e < L::E; e++) y[e] = __fmul_rn(number(w[j][e]), scale[e]);
+        store_values<DT>(static_cast<typename L::T*>(p.values) + row * p.ldv + col, y, p.vec_v, left);
       }
     }
     if (p.q) {
@@ -334,7 +418,6 @@ __global__ void __launch_bounds__(QT) quant_cols(QuantParams p) {
       __syncthreads();
       const int lane = threadIdx.x & 31;
       const int64_t row = t0 + lane * 4;
-      const int64_t c0 = ((int64_t)blockIdx.x / S) * CW;
       for (int c = threadIdx.x >> 5; c < CW; c += QT / 32) {
         if (c0 + c >= p.cols || row >= p.rows) continue;
         const uint32_t u = tile[c][lane];
@@ -349,7 +432,6 @@ __global__ void __launch_bounds__(QT) quant_cols(QuantParams p) {
       }
     }
   }
-  cl.sync();  // the others may still read this CTA's maxima
 }
 
 template <int DT>
@@ -374,22 +456,28 @@ cudaError_t rows_launch(const QuantParams& p, cudaStream_t s) {
 
 template <int DT, bool VEC>
 cudaError_t cols_launch(const QuantParams& p, int nsm, cudaStream_t s) {
-  constexpr int CW = 8 * Elem<DT>::E;
-  const int64_t strips = (p.cols + CW - 1) / CW, tiles = (p.rows + TR - 1) / TR;
-  // split the rows until there are a few CTAs for each SM, two tiles or more each
-  int S = 1;
-  while (S < 8 && strips * S < 4 * (int64_t)nsm && tiles >= 4 * S) S *= 2;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)S;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(strips * S));
-  cfg.blockDim = dim3(QT);
-  cfg.stream = s;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, quant_cols<DT, VEC>, p);
+  constexpr int E = Elem<DT>::E, CW = 8 * E;
+  const int64_t per = VEC ? E : 1, nv = (p.cols + per - 1) / per;
+  int vl = 8;
+  while (vl < 32 && vl < nv) vl *= 2;  // wider CTAs would mean more shares of the rows, and atomics for each
+  const int64_t wide = (nv + vl - 1) / vl, lanes = QT / vl;
+  // one wave of as many CTAs as an SM holds, `least` rows or more for each
+  auto shares = [&](int64_t across, int64_t least, int64_t rows_unit, int64_t resident, int64_t* each) {
+    int64_t n = std::min(resident * nsm / across, (p.rows + least - 1) / least);
+    n = std::max<int64_t>(1, std::min<int64_t>(n, 65535));
+    *each = ((p.rows + n - 1) / n + rows_unit - 1) / rows_unit * rows_unit;
+    return (unsigned)std::max<int64_t>(1, (p.rows + *each - 1) / std::max<int64_t>(*each, 1));
+  };
+  int64_t each = 1;
+  const unsigned ny = shares(wide, 8 * lanes, 1, 5, &each);
+  if (p.rows > 0) {
+    quant_colmax<DT, VEC><<<dim3((unsigned)wide, ny), QT, 0, s>>>(p, vl, std::max<int64_t>(each, 1));
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  const int64_t strips = (p.cols + CW - 1) / CW;
+  const unsigned ty = shares(strips, TR, TR, 3, &each);
+  return launch_dependent(quant_cols<DT, VEC>, dim3((unsigned)strips, ty), QT, 0, s, p, std::max<int64_t>(each, TR));
 }
 
 template <int DT>

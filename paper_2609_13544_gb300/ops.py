@@ -42,9 +42,18 @@ def register(L) -> None:
         getattr(L, name).restype = i32
 
 
+_entry = {}
+
+
 def _call(h, name, *args) -> None:
-    from . import _check, load
-    _check(getattr(load(), name)(h.ptr, *args), h)
+    f = _entry.get(name)
+    if f is None:
+        from . import load
+        f = _entry[name] = getattr(load(), name)
+    rc = f(h.ptr, *args)
+    if rc:
+        from . import _check
+        _check(rc, h)
 
 
 def _stream(h, stream) -> int:
@@ -60,21 +69,25 @@ def _on(stream):
 
 def _code(t) -> int:
     import torch
-    code = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}.get(t.dtype)
-    if code is None:
-        raise TypeError(f"unsupported dtype {t.dtype}: float32, float16 or bfloat16")
-    return code
+    d = t.dtype
+    if d is torch.float32:
+        return 0
+    if d is torch.bfloat16:
+        return 2
+    if d is torch.float16:
+        return 1
+    raise TypeError(f"unsupported dtype {d}: float32, float16 or bfloat16")
 
 
 def _matrix(h, t, name: str) -> int:
     """The row distance of a matrix whose rows are contiguous, on the handle's device."""
     if t.dim() != 2:
         raise ValueError(f"{name} must have two dimensions")
-    if not t.is_cuda or t.device.index != h.device:
+    if t.get_device() != h.device:
         raise ValueError(f"{name} must be a CUDA tensor on the handle's device")
     rows, cols = t.shape
     s0, s1 = t.stride()
-    if cols > 1 and s1 != 1:
+    if s1 != 1 and cols > 1:
         raise ValueError(f"the rows of {name} must be contiguous")
     if rows <= 1:
         return cols
@@ -87,8 +100,7 @@ def _vector(h, t, n: int, name: str) -> Optional[int]:
     import torch
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda or \
-            t.device.index != h.device:
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != h.device:
         raise ValueError(f"{name} must be a contiguous float32 tensor of {n} elements on the handle's device")
     return t.data_ptr()
 
@@ -191,10 +203,9 @@ def _grad_args(h, grads, record, norms):
     import torch
     if not isinstance(grads, GradList):
         grads = GradList(grads)
-    if len(grads) and grads.device.index != h.device:
+    if grads.device is not None and grads.device.index != h.device:
         raise ValueError("the gradients must be on the handle's device")
-    if record.numel() * record.element_size() < GRADNORM_BYTES or not record.is_cuda or not record.is_contiguous() \
-            or record.device.index != h.device:
+    if record.nbytes < GRADNORM_BYTES or not record.is_contiguous() or record.get_device() != h.device:
         raise ValueError("record must be a contiguous CUDA tensor of 16 bytes on the handle's device")
     if norms is not None and (norms.dtype != torch.float32 or norms.numel() < len(grads)):
         raise ValueError("norms must be float32, one element for each tensor")
