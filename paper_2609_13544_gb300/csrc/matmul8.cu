@@ -9,6 +9,8 @@
 // no transposed load is needed.
 #include <cooperative_groups.h>
 
+#include <algorithm>
+
 #include "mm8_common.cuh"
 
 namespace cg = cooperative_groups;
@@ -35,6 +37,8 @@ __device__ __forceinline__ void drain(float (&c)[NT][4], int (&sum)[NT][4]) {
       c[n][i] = 0.0f;
     }
 }
+
+constexpr int64_t MM8_STREAM_N = 8192;  // rows of b from which every SM has a warp tile or more of its own
 
 // ---- up to 16 rows of a: bound by the bytes of b -----------------------------
 // A CTA of four warps takes 16 rows of b, each warp every fourth run of 64 k
@@ -115,6 +119,98 @@ __global__ void __launch_bounds__(RT) mm8_rows(Mm8Params p) {
     out[m * p.ldo + n0 + n] = Mm8Out<OUT>::make(v, s, p.bias ? __ldg(p.bias + n0 + n) : 0.0f);
   }
   cl.sync();  // the others may still read this CTA's part
+}
+
+// ---- up to 64 rows of a and many of b: a stream over b ------------------------
+// The rows of a are turned into binary16 once per CTA, in the very registers'
+// order, and stay in shared memory (a run of 1024 k of them at a time where
+// they are longer); every warp then streams 16 rows of b past them, so a byte
+// of b costs its load, its conversion and its share of the instructions.
+constexpr int ST = 512;
+template <int OUT, int NT, int MODE>
+__global__ void __launch_bounds__(ST, NT <= 2 ? 2 : 1) mm8_stream(Mm8Params p, int runs_held) {
+  extern __shared__ __align__(16) uint2 held[];  // [run][n][j][lane]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int64_t runs = (p.K + 63) / 64, tiles = (p.N + 15) / 16;
+  const int8_t *alo = p.a, *ahi = p.a + (p.M - 1) * p.lda + p.K, *blo = p.b, *bhi = p.b + (p.N - 1) * p.ldb + p.K;
+  const int64_t t0 = tiles * blockIdx.x / gridDim.x, t1 = tiles * (blockIdx.x + 1) / gridDim.x;
+  typename Mm8Out<OUT>::T* out = static_cast<typename Mm8Out<OUT>::T*>(p.out);
+  constexpr int U = NT <= 2 ? 2 : 4;  // runs of b in flight
+  for (int64_t round = t0; round < t1; round += ST / 32) {
+    const int64_t tile = round + warp, n0 = tile * 16;
+    const bool mine = tile < t1;
+    float c[NT][4];
+    int sum[NT][4];
+#pragma unroll
+    for (int n = 0; n < NT; n++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) c[n][i] = 0.0f, sum[n][i] = 0;
+    const int8_t* w0 = p.b + (n0 + g) * p.ldb + 16 * t;
+    const int8_t* w1 = w0 + 8 * p.ldb;
+    const bool has0 = mine && n0 + g < p.N, has1 = mine && n0 + g + 8 < p.N;
+    for (int64_t k0 = 0; k0 < runs; k0 += runs_held) {
+      const int here = (int)min((int64_t)runs_held, runs - k0);
+      if (round == t0 || runs > runs_held) {
+        __syncthreads();  // the last readers are done
+        for (int i = warp; i < here * NT; i += ST / 32) {
+          const int n = i % NT, m = n * 8 + g;
+          const int64_t k = (k0 + i / NT) * 64 + 16 * t;
+          const uint4 x = load16<MODE>(p.a + m * p.lda + k, m < p.M ? p.K - k : 0, alo, ahi);
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            uint2 h;
+            to_half(word(x, j), h.x, h.y);
+            held[(i * 4 + j) * 32 + lane] = h;
+          }
+        }
+        __syncthreads();
+      }
+      if (mine) {
+        int since = 0;
+        for (int r = 0; r < here; r += U) {
+          uint4 u0[U], u1[U];
+#pragma unroll
+          for (int u = 0; u < U; u++) {
+            const int64_t k = (k0 + r + u) * 64, left = r + u < here ? p.K - k - 16 * t : 0;
+            u0[u] = load16<MODE>(w0 + k, has0 ? left : 0, blo, bhi);
+            u1[u] = load16<MODE>(w1 + k, has1 ? left : 0, blo, bhi);
+          }
+#pragma unroll
+          for (int u = 0; u < U; u++) {
+            if (r + u >= here) break;
+            const uint2* x = held + (size_t)(r + u) * NT * 4 * 32 + lane;
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+              uint32_t a[4];
+              to_half(word(u0[u], j), a[0], a[2]);
+              to_half(word(u1[u], j), a[1], a[3]);
+#pragma unroll
+              for (int n = 0; n < NT; n++) {
+                const uint2 b = x[(n * 4 + j) * 32];
+                mma16816(c[n], a, b.x, b.y);
+              }
+            }
+          }
+          since += U;
+          if (since >= MM8_EXACT_K / 64) {
+            drain(c, sum);
+            since = 0;
+          }
+        }
+        drain(c, sum);
+      }
+    }
+    if (!mine) continue;
+#pragma unroll
+    for (int n = 0; n < NT; n++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int64_t m = n * 8 + 2 * t + (i & 1), col = n0 + g + 8 * (i >> 1);
+        if (m >= p.M || col >= p.N) continue;
+        const float s = (p.sa ? __ldg(p.sa + m) : 1.0f) * (p.sb ? __ldg(p.sb + col) : 1.0f);
+        out[m * p.ldo + col] = Mm8Out<OUT>::make(sum[n][i], s, p.bias ? __ldg(p.bias + col) : 0.0f);
+      }
+  }
 }
 
 // ---- tiles --------------------------------------------------------------------
@@ -261,9 +357,28 @@ cudaError_t cluster_launch(F kernel, int64_t tiles, int S, int threads, int smem
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+template <int OUT, int NT, int MODE>
+cudaError_t stream(const Mm8Params& p, int nsm, cudaStream_t s) {
+  const int64_t runs = (p.K + 63) / 64, tiles = (p.N + 15) / 16;
+  constexpr int RUN = NT * 1024, CTAS = NT <= 2 ? 2 : 1, MOST = 16 * 8 * 1024;  // bytes of a held run; of all of them
+  const int held = (int)std::min<int64_t>(runs, (CTAS == 2 ? MOST / 2 : MOST) / RUN);
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = allow_smem(mm8_stream<OUT, NT, MODE>, MOST, allowed);
+  if (e != cudaSuccess) return e;
+  const unsigned ctas = (unsigned)std::min<int64_t>(CTAS * (int64_t)nsm, tiles);
+  mm8_stream<OUT, NT, MODE><<<ctas, ST, (size_t)held * RUN, s>>>(p, held);
+  return cudaGetLastError();
+}
+
 template <int OUT, int MODE>
 cudaError_t direct(const Mm8Params& p, int nsm, cudaStream_t s) {
   const int64_t runs = (p.K + 63) / 64;
+  if (p.M <= 64 && p.K > 0 && p.N >= MM8_STREAM_N) {
+    if (p.M <= 8) return stream<OUT, 1, MODE>(p, nsm, s);
+    if (p.M <= 16) return stream<OUT, 2, MODE>(p, nsm, s);
+    if (p.M <= 32) return stream<OUT, 4, MODE>(p, nsm, s);
+    return stream<OUT, 8, MODE>(p, nsm, s);
+  }
   if (p.M <= 16) {
     const int64_t tiles = (p.N + 15) / 16;
     int S = 1;  // share the k runs while the SMs are not filled and every warp keeps a few

@@ -14,7 +14,8 @@
 // CTA) the matrix instructions, eight warps turn accumulators into results
 // while the other half of the 512 accumulator columns fills, and one warp
 // plans: a few tiles ahead it works out each tile's place and drains and
-// fetches its scales, so that nobody else waits for global memory.
+// fetches its scales, so that neither instructions nor results wait for global
+// memory.
 //
 // Exactness: float32 holds a sum of products exactly while it stays below
 // 2^24.  pack leaves for every block of 128 rows and 256 k the largest 2-norm
@@ -130,7 +131,7 @@ struct TcParams {
   int kb, kc;
   int mt, nt;       // tiles
   int splits;       // parts of the k range of a tile
-  int* sums;        // 128 x 256 int32 for each CTA, or (splits > 1) for each half of a tile, then zero between calls
+  int4* sums;       // 128 x 256 int32 for each CTA, or (splits > 1) for each half of each part of a tile
   unsigned int* tickets;  // splits > 1: one for each result warp of a tile, zero between calls
   int vec_out;      // out's rows start on 32-byte boundaries
   unsigned int* status;
@@ -147,9 +148,12 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-// arrive on a barrier of the cluster (an address of mapa)
+// Arrive on a barrier of the cluster (an address of mapa).  What it tells the
+// other CTA is that accumulators have been read, which the tcgen05 fence
+// before it orders; a release at cluster scope would wait for this thread's
+// stores to global memory, 2000 cycles of every tile.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
   uint32_t r;
@@ -306,30 +310,63 @@ __device__ __forceinline__ void put_columns(const TcParams& p, const float (&v)[
   }
 }
 
+// integer sums as put_columns takes them
+template <int OUT>
+__device__ __forceinline__ void as_results(const int4 (&x)[8], float (&f)[32]) {
+#pragma unroll
+  for (int j = 0; j < 8; j++) {
+    const int v[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
+#pragma unroll
+    for (int i = 0; i < 4; i++) f[4 * j + i] = OUT == PEAT_OUT_I32 ? __int_as_float(v[i]) : __int2float_rn(v[i]);
+  }
+}
+
 constexpr int GROUP = 8;
-// Plans a tile into a slot, by a warp.
-__device__ void plan_tile(const TcParams& p, int u, Slot* slot) {
-  const int lane = threadIdx.x & 31;
-  const int tile = u / p.splits, part = u - tile * p.splits;
+// a tile, and its part of the k range in blocks of 64
+struct Place {
+  int tile, mt, nt, k0, k1;
+};
+__device__ __forceinline__ Place place_of(const TcParams& p, int u) {
+  Place r;
+  r.tile = u / p.splits;
+  const int part = u - r.tile * p.splits;
   // groups of GROUP rows of tiles, column by column: the clusters at work at
   // any time share few blocks of a and few of b
-  const int per = GROUP * p.nt, g = tile / per, in = tile - g * per, wide = min(GROUP, p.mt - g * GROUP);
-  const int nt = in / wide, mt = g * GROUP + in - nt * wide;
-  const int k0 = (int)((int64_t)p.kb * part / p.splits), k1 = (int)((int64_t)p.kb * (part + 1) / p.splits);
+  const int per = GROUP * p.nt, g = r.tile / per, in = r.tile - g * per, wide = min(GROUP, p.mt - g * GROUP);
+  r.nt = in / wide;
+  r.mt = g * GROUP + in - r.nt * wide;
+  // (kb < 2^12, splits <= 16)
+  r.k0 = p.kb * part / p.splits;
+  r.k1 = p.kb * (part + 1) / p.splits;
+  return r;
+}
+// a tile's scales into its slot, by a warp
+__device__ __forceinline__ void plan_scales(const TcParams& p, const Place& t, Slot* slot) {
+  const int lane = threadIdx.x & 31;
+  float sb[8], bias[8];
 #pragma unroll
   for (int i = 0; i < 8; i++) {
-    const int64_t col = (int64_t)nt * 256 + i * 32 + lane;
-    slot->sb[i * 32 + lane] = p.m.sb && col < p.m.N ? __ldg(p.m.sb + col) : 1.0f;
-    if (p.m.bias) slot->bias[i * 32 + lane] = col < p.m.N ? __ldg(p.m.bias + col) : 0.0f;
+    const int64_t col = (int64_t)t.nt * 256 + i * 32 + lane;
+    sb[i] = p.m.sb && col < p.m.N ? __ldg(p.m.sb + col) : 1.0f;
+    bias[i] = p.m.bias && col < p.m.N ? __ldg(p.m.bias + col) : 0.0f;
   }
-  const float* na = p.na + (int64_t)mt * 2 * p.kc;
-  const float* nb = p.nb + (int64_t)nt * 2 * p.kc;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    slot->sb[i * 32 + lane] = sb[i];
+    slot->bias[i * 32 + lane] = bias[i];
+  }
+}
+// a tile's place and drains into its slot, by a warp
+__device__ void plan_drains(const TcParams& p, const Place& t, Slot* slot) {
+  const int lane = threadIdx.x & 31;
+  const float* na = p.na + (int64_t)t.mt * 2 * p.kc;
+  const float* nb = p.nb + (int64_t)t.nt * 2 * p.kc;
   int pieces = 1;
   float run = 0.0f;  // the bound of what the accumulator holds
-  for (int c0 = k0 / 4, w = 0; c0 * 4 < k1; c0 += 32, w++) {
+  for (int c0 = t.k0 / 4, w = 0; c0 * 4 < t.k1; c0 += 32, w++) {
     const int c = c0 + lane;
     float mine = 0.0f;
-    if (c * 4 < k1)
+    if (c * 4 < t.k1)
       mine = fmaxf(__ldcg(na + c), __ldcg(na + p.kc + c)) * fmaxf(__ldcg(nb + c), __ldcg(nb + p.kc + c));
     float all = mine;
 #pragma unroll
@@ -352,11 +389,11 @@ __device__ void plan_tile(const TcParams& p, int u, Slot* slot) {
     if (lane == 0) slot->drain[w] = mask;
   }
   if (lane == 0) {
-    slot->tile = tile;
-    slot->mt = mt;
-    slot->nt = nt;
-    slot->k0 = k0;
-    slot->k1 = k1;
+    slot->tile = t.tile;
+    slot->mt = t.mt;
+    slot->nt = t.nt;
+    slot->k0 = t.k0;
+    slot->k1 = t.k1;
     slot->pieces = pieces;
   }
 }
@@ -388,7 +425,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     mbar_init(last, 1);
     for (int i = 0; i < SLOTS; i++) {
       mbar_init(planned + 8 * i, 1);
-      mbar_init(unplanned + 8 * i, EPI_WARPS + 1 + (rank == 0));  // results, copies, and the instructions' warp
+      mbar_init(unplanned + 8 * i, EPI_WARPS + (rank == 0));  // results, and the instructions' warp
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -401,7 +438,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   cg::this_cluster().sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_at;
-  pdl_wait();
 
   bool ok = true;
   if (warp == PLAN_WARP) {
@@ -409,20 +445,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     for (int u = first; u < units && ok; u += step, i++) {
       ok = mbar_wait(unplanned + 8 * (i % SLOTS), (i / SLOTS & 1) ^ 1, p.wait_limit);
       if (!ok) break;
-      plan_tile(p, u, slots + i % SLOTS);
+      const Place t = place_of(p, u);
+      // (the scales are not pack's: they were there before it began)
+      plan_scales(p, t, slots + i % SLOTS);
+      if (i == 0) pdl_wait();
+      plan_drains(p, t, slots + i % SLOTS);
       __syncwarp();
       if (lane == 0) mbar_arrive(planned + 8 * (i % SLOTS));
     }
   } else if (warp == COPY_WARP) {
     if (elect_one()) {
-      int seq = 0, i = 0;
-      for (int u = first; u < units && ok; u += step, i++) {
-        const Slot* t = slots + i % SLOTS;
-        if (!(ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
-        const int k0 = t->k0, k1 = t->k1;
-        const int ra = (t->mt * 2 + (int)rank) * p.kb, rb = (t->nt * 2 + (int)rank) * p.kb;
-        mbar_arrive(unplanned + 8 * (i % SLOTS));
-        for (int k = k0; k < k1; k++, seq++) {
+      pdl_wait();
+      int seq = 0;
+      for (int u = first; u < units && ok; u += step) {
+        const Place t = place_of(p, u);
+        const int ra = (t.mt * 2 + (int)rank) * p.kb, rb = (t.nt * 2 + (int)rank) * p.kb;
+        for (int k = t.k0; k < t.k1; k++, seq++) {
           const int s = seq % STAGES;
           if (!(ok = mbar_wait(empty + 8 * s, (seq / STAGES & 1) ^ 1, p.wait_limit))) break;
           const uint32_t dst = sptr(smem + s * STAGE), bar = mapa(full + 8 * s, 0);
@@ -499,12 +537,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       const int rows = (int)max((int64_t)0, min((int64_t)32, p.m.M - row0));
       const float sa = p.m.sa && lane < rows ? __ldg(p.m.sa + row0 + lane) : 1.0f;
       // One piece that is the whole sum goes straight from the accumulator to
-      // the output.  Otherwise pieces are added up as integers in memory: in a
-      // place of this CTA's, or, for a tile whose k range is split, in the
-      // tile's, by atomics (whose order does not matter); the last to come has
-      // the total there.
-      const int64_t part = (split ? (int64_t)t->tile * 2 + rank : (int64_t)blockIdx.x) * EPI_WARPS + warp;
-      int* sums = p.sums + part * (32 * 128) + lane;
+      // the output.  Otherwise pieces are added up as integers in memory, in a
+      // place of this CTA's, or, for a tile whose k range is split, of this
+      // part's; the last part to come adds up all of them.
+      const bool whole = pieces == 1 && !split;
+      const int64_t area = (int64_t)EPI_WARPS * 8 * 128;  // int4 values of a CTA's half tile
+      int4* sums = p.sums + (split ? ((int64_t)u * 2 + rank) : (int64_t)blockIdx.x) * area + warp * (8 * 128) + lane;
       for (int q = 0; q < pieces && ok; q++, chunk++) {
         if (!(ok = mbar_wait(acc_full + 8 * (chunk & 1), chunk / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -520,28 +558,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             if (lane == 0) mbar_arrive_cluster(release0 + 8 * (chunk & 1));
           }
 #pragma unroll
-          for (int i = 0; i < 32; i++) f[i] = __uint_as_float(v[i]);
-          if (split) {
+          for (int j = 0; j < 32; j++) f[j] = __uint_as_float(v[j]);
+          if (!whole) {
+            int4* s4 = sums + g * 8 * 32;
+            int4 x[8];
 #pragma unroll
-            for (int i = 0; i < 32; i++) atomicAdd(sums + (g * 32 + i) * 32, __float2int_rn(f[i]));
-            continue;
-          }
-          if (pieces > 1) {
-            int x[32];
-#pragma unroll
-            for (int i = 0; i < 32; i++) x[i] = q ? __ldcg(sums + (g * 32 + i) * 32) : 0;
-#pragma unroll
-            for (int i = 0; i < 32; i++) x[i] += __float2int_rn(f[i]);
-            if (q < pieces - 1) {
-#pragma unroll
-              for (int i = 0; i < 32; i++) __stcg(sums + (g * 32 + i) * 32, x[i]);
-              continue;
+            for (int j = 0; j < 8; j++) {
+              x[j] = q ? __ldcg(s4 + j * 32) : make_int4(0, 0, 0, 0);
             }
 #pragma unroll
-            for (int i = 0; i < 32; i++) f[i] = OUT == PEAT_OUT_I32 ? __int_as_float(x[i]) : __int2float_rn(x[i]);
+            for (int j = 0; j < 8; j++) {
+              x[j].x += __float2int_rn(f[4 * j]);
+              x[j].y += __float2int_rn(f[4 * j + 1]);
+              x[j].z += __float2int_rn(f[4 * j + 2]);
+              x[j].w += __float2int_rn(f[4 * j + 3]);
+            }
+            if (split || q < pieces - 1) {
+#pragma unroll
+              for (int j = 0; j < 8; j++) __stcg(s4 + j * 32, x[j]);
+              continue;
+            }
+            as_results<OUT>(x, f);
           } else if (OUT == PEAT_OUT_I32) {
 #pragma unroll
-            for (int i = 0; i < 32; i++) f[i] = __int_as_float(__float2int_rn(f[i]));
+            for (int j = 0; j < 32; j++) f[j] = __int_as_float(__float2int_rn(f[j]));
           }
           put_columns<OUT>(p, f, sa, sb + g * 32, bias + g * 32, stage, row0, rows, col0 + g * 32);
         }
@@ -551,22 +591,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         __threadfence();
         __syncwarp();
         unsigned int n = 0;
+        unsigned int* ticket = p.tickets + ((int64_t)t->tile * 2 + rank) * EPI_WARPS + warp;
         if (lane == 0) {
-          n = atomicAdd(p.tickets + part, 1u);
-          if (n == (unsigned)p.splits - 1) p.tickets[part] = 0;
+          n = atomicAdd(ticket, 1u);
+          if (n == (unsigned)p.splits - 1) *ticket = 0;
         }
         if (__shfl_sync(0xffffffffu, n, 0) == (unsigned)p.splits - 1) {
           __threadfence();
+          const int4* all = p.sums + ((int64_t)t->tile * p.splits * 2 + rank) * area + warp * (8 * 128) + lane;
 #pragma unroll 1
           for (int g = 0; g < 4; g++) {
+            int4 x[8];
             float f[32];
 #pragma unroll
-            for (int j = 0; j < 32; j++) {
-              const int x = __ldcg(sums + (g * 32 + j) * 32);
-              f[j] = OUT == PEAT_OUT_I32 ? __int_as_float(x) : __int2float_rn(x);
-            }
+            for (int j = 0; j < 8; j++) x[j] = __ldcg(all + (g * 8 + j) * 32);
+            for (int k = 1; k < p.splits; k++) {
 #pragma unroll
-            for (int j = 0; j < 32; j++) __stcg(sums + (g * 32 + j) * 32, 0);
+              for (int j = 0; j < 8; j++) {
+                const int4 y = __ldcg(all + k * 2 * area + (g * 8 + j) * 32);
+                x[j].x += y.x;
+                x[j].y += y.y;
+                x[j].z += y.z;
+                x[j].w += y.w;
+              }
+            }
+            as_results<OUT>(x, f);
             put_columns<OUT>(p, f, sa, sb + g * 32, bias + g * 32, stage, row0, rows, col0 + g * 32);
           }
         }
@@ -611,8 +660,9 @@ bool block_map(CUtensorMap* m, void* base, int64_t blocks) {
 
 template <int OUT>
 cudaError_t tc_launch(const TcParams& p, const CUtensorMap& ma, const CUtensorMap& mb, int nsm, cudaStream_t s) {
-  static cudaError_t ready = cudaFuncSetAttribute(mm8_tc<OUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-  if (ready != cudaSuccess) return ready;
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = allow_smem(mm8_tc<OUT>, SMEM, allowed);
+  if (e != cudaSuccess) return e;
   const int64_t units = (int64_t)p.mt * p.nt * p.splits;
   const int clusters = (int)(units < nsm / 2 ? units : nsm / 2);
   return launch_dependent(mm8_tc<OUT>, (unsigned)(clusters * 2), THREADS, SMEM, s, p, ma, mb);
@@ -646,14 +696,13 @@ Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm) {
   r.nb_off = at;
   at += up((size_t)r.nt * 2 * r.kc * sizeof(float));
   r.bytes = at;
-  // the two kinds of sums lie apart: one is left as it is, the other zero
   r.sum_off = at;
-  if (r.splits == 1) r.bytes = at + (size_t)nsm * (128 * 256 * sizeof(int));
-  r.zero_bytes = r.splits > 1 ? (size_t)tiles * (256 * 256 * sizeof(int) + 2 * EPI_WARPS * sizeof(unsigned int)) : 0;
+  r.bytes = at + (size_t)(r.splits > 1 ? tiles * r.splits * 2 : nsm) * (128 * 256 * sizeof(int));
+  r.tickets = r.splits > 1 ? (size_t)tiles * 2 * EPI_WARPS : 0;
   return r;
 }
 
-cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, char* zeros,
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* tickets,
                           unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s) {
   PackParams k;
   k.x[0] = m.a;
@@ -689,8 +738,8 @@ cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& pl
   p.mt = (int)plan.mt;
   p.nt = (int)plan.nt;
   p.splits = plan.splits;
-  p.sums = reinterpret_cast<int*>(plan.splits > 1 ? zeros : ws + plan.sum_off);
-  p.tickets = reinterpret_cast<unsigned int*>(zeros + (size_t)plan.mt * plan.nt * 256 * 256 * sizeof(int));
+  p.sums = reinterpret_cast<int4*>(ws + plan.sum_off);
+  p.tickets = tickets;
   p.vec_out = reinterpret_cast<uintptr_t>(m.out) % 32 == 0 &&
               m.ldo * (out_dtype == PEAT_F16 || out_dtype == PEAT_BF16 ? 2 : 4) % 32 == 0;
   p.status = status;

@@ -26,18 +26,16 @@ struct OpsState {
   bool pending[RING] = {};
   int next = 0;
   unsigned int* done = nullptr;  // zero between calls
-  void* tickets = nullptr;       // one for each tensor of a list, zero between calls
+  void* tickets = nullptr;       // counters of finished parts, zero between calls
   size_t tickets_cap = 0;
   // column maxima: two buffers in turn; a call clears the other one's last use
   void* colmax = nullptr;
   size_t colmax_cap = 0;  // bytes of both
   int64_t colmax_used[2] = {0, 0};
   int colmax_at = 0;
-  // products: packed operands; integer sums of split tiles, zero between calls
+  // products: packed operands and partial sums
   void* mm = nullptr;
   size_t mm_cap = 0;
-  void* zeros = nullptr;
-  size_t zeros_cap = 0;
 };
 
 void ops_destroy(OpsState* s) {
@@ -47,7 +45,6 @@ void ops_destroy(OpsState* s) {
   if (s->tickets) cudaFree(s->tickets);
   if (s->colmax) cudaFree(s->colmax);
   if (s->mm) cudaFree(s->mm);
-  if (s->zeros) cudaFree(s->zeros);
   for (int i = 0; i < OpsState::RING; i++) {
     if (s->h_list[i]) cudaFreeHost(s->h_list[i]);
     if (s->taken[i]) cudaEventDestroy(s->taken[i]);
@@ -97,6 +94,16 @@ peat_status_t grow(peat_handle_t h, void** p, size_t* cap, size_t need) {
   }
   *cap = need;
   return PEAT_OK;
+}
+
+// n counters, zero
+peat_status_t tickets(peat_handle_t h, OpsState* s, size_t n, cudaStream_t st) {
+  const size_t need = sizeof(unsigned int) * std::max(n, (size_t)4096);
+  if (need <= s->tickets_cap) return PEAT_OK;
+  peat_status_t ps = grow(h, &s->tickets, &s->tickets_cap, need);
+  if (ps != PEAT_OK) return ps;
+  cudaError_t e = cudaMemsetAsync(s->tickets, 0, need, st);
+  return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "cudaMemsetAsync(counters)");
 }
 
 peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int axis,
@@ -203,8 +210,8 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
   p.K = K;
   if (h->status_host && *(volatile unsigned int*)h->status_host) {
     *(volatile unsigned int*)h->status_host = 0;
-    // what the call left of its split sums is cleared
-    if (h->ops && h->ops->zeros) cudaMemsetAsync(h->ops->zeros, 0, h->ops->zeros_cap, st);
+    // what the call left of its counters is cleared
+    if (h->ops && h->ops->tickets) cudaMemsetAsync(h->ops->tickets, 0, h->ops->tickets_cap, st);
     return fail(h, PEAT_ERR_TIMEOUT,
                 "a bounded device-side wait expired in an earlier call on this handle; its outputs are invalid");
   }
@@ -217,16 +224,11 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
     OpsState* s = nullptr;
     peat_status_t ps = ops_state(h, &s);
     if (ps == PEAT_OK) ps = grow(h, &s->mm, &s->mm_cap, plan.bytes);
+    if (ps == PEAT_OK) ps = tickets(h, s, plan.tickets, st);
     if (ps != PEAT_OK) return ps;
-    if (plan.zero_bytes > s->zeros_cap) {
-      ps = grow(h, &s->zeros, &s->zeros_cap, plan.zero_bytes);
-      if (ps != PEAT_OK) return ps;
-      e = cudaMemsetAsync(s->zeros, 0, plan.zero_bytes, st);
-      if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(zeros)");
-    }
     const unsigned int limit = std::min(h->wait_limit, 1u << 22);
-    e = peat::launch_mm8_tc(out_dtype, p, plan, static_cast<char*>(s->mm), static_cast<char*>(s->zeros), h->status_dev,
-                            limit, h->nsm, st);
+    e = peat::launch_mm8_tc(out_dtype, p, plan, static_cast<char*>(s->mm), static_cast<unsigned int*>(s->tickets),
+                            h->status_dev, limit, h->nsm, st);
   } else {
     e = peat::launch_mm8_direct(out_dtype, p, h->nsm, st);
   }
@@ -278,13 +280,8 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   const size_t parted = sizeof(peat::GnPartial) * (size_t)(count + warps);
   ps = grow(h, &s->d_list, &s->d_list_cap, listed + parted + sizeof(peat::GnPartial) * (size_t)count);
   if (ps != PEAT_OK) return ps;
-  const size_t tickets = sizeof(unsigned int) * (size_t)std::max<int64_t>(count, 1024);
-  if (tickets > s->tickets_cap) {
-    ps = grow(h, &s->tickets, &s->tickets_cap, tickets);
-    if (ps != PEAT_OK) return ps;
-    cudaError_t e = cudaMemsetAsync(s->tickets, 0, tickets, st);
-    if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(tickets)");
-  }
+  ps = tickets(h, s, (size_t)count, st);
+  if (ps != PEAT_OK) return ps;
 
   peat::GnInline in;
   peat::GnEntry* dst = in.e;

@@ -1,5 +1,6 @@
 // Internal declarations of the playback operators (include/peat_ops.h).
 #pragma once
+#include <atomic>
 #include <cstdint>
 
 #include <cuda_runtime.h>
@@ -8,6 +9,19 @@
 #include "peat_ops.h"
 
 namespace peat {
+
+// a kernel's dynamic shared memory limit, raised once on each device (done: ordinals below 64)
+template <typename K>
+inline cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 // ---- 8-bit quantisation (quant8.cu) ----
 struct QuantParams {
@@ -47,10 +61,10 @@ struct Mm8TcPlan {
   int64_t mt, nt;  // tiles
   int splits;      // parts of a tile's k range
   size_t a_off, b_off, na_off, nb_off, sum_off, bytes;  // workspace
-  size_t zero_bytes;  // a second one, zero between calls (0: not needed)
+  size_t tickets;  // counters, zero between calls
 };
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm);
-cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, char* zeros,
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, unsigned int* tickets,
                           unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s);
 
 // ---- gradient lists (gradnorm.cu) ----
