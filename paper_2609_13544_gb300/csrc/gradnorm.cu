@@ -356,6 +356,7 @@ __device__ __forceinline__ GnPartial load_sum(const GnPartial* q) {
 
 template <int NORM>
 __global__ void __launch_bounds__(GB) gn_norm(GnParams p, const __grid_constant__ GnInline in) {
+  pdl_wait();
   pdl_trigger();
   const GnEntry* list = p.list ? p.list : in.e;
   pieces_of<NORM>(p, list, (int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5));
@@ -447,6 +448,7 @@ __device__ __forceinline__ void scale_share(const GnParams& p, const GnEntry* li
 }
 __global__ void __launch_bounds__(GB) gn_scale(GnParams p, const __grid_constant__ GnInline in) {
   pdl_wait();
+  pdl_trigger();
   const GnEntry* list = p.list ? p.list : in.e;
   const int64_t n = (int64_t)gridDim.x * (GB / 32);
   const float f = __fmul_rn(p.unscale, __ldcg(&p.result->coef));
@@ -464,6 +466,8 @@ __global__ void __launch_bounds__(GB_SMALL) gn_small(GnParams p, const __grid_co
   __shared__ bool zero;
   const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const GnEntry* list = in.e;
+  pdl_wait();
+  pdl_trigger();
   // every warp that counts has a unit, so every part that is gathered was written
   const uint32_t units = (uint32_t)p.units, n = min((uint32_t)W, max(units, 1u));
   if (w < n && units > 0) {
@@ -501,18 +505,16 @@ __global__ void __launch_bounds__(GB_SMALL) gn_small(GnParams p, const __grid_co
 int gn_block() { return GB; }
 
 cudaError_t launch_gradnorm(const GnParams& p, const GnInline& in, int nctas, cudaStream_t s) {
-  if (p.type == PEAT_NORM_1) gn_norm<PEAT_NORM_1><<<nctas, GB, 0, s>>>(p, in);
-  else if (p.type == PEAT_NORM_INF) gn_norm<PEAT_NORM_INF><<<nctas, GB, 0, s>>>(p, in);
-  else gn_norm<PEAT_NORM_2><<<nctas, GB, 0, s>>>(p, in);
-  cudaError_t e = cudaGetLastError();
+  auto kernel = p.type == PEAT_NORM_1 ? gn_norm<PEAT_NORM_1>
+                                      : (p.type == PEAT_NORM_INF ? gn_norm<PEAT_NORM_INF> : gn_norm<PEAT_NORM_2>);
+  cudaError_t e = launch_dependent(kernel, (unsigned)nctas, GB, 0, s, p, in);
   if (e == cudaSuccess && p.clip && p.units > 0) e = launch_dependent(gn_scale, (unsigned)nctas, GB, 0, s, p, in);
   return e;
 }
 cudaError_t launch_gradnorm_small(const GnParams& p, const GnInline& in, cudaStream_t s) {
-  if (p.type == PEAT_NORM_1) gn_small<PEAT_NORM_1><<<1, GB_SMALL, 0, s>>>(p, in);
-  else if (p.type == PEAT_NORM_INF) gn_small<PEAT_NORM_INF><<<1, GB_SMALL, 0, s>>>(p, in);
-  else gn_small<PEAT_NORM_2><<<1, GB_SMALL, 0, s>>>(p, in);
-  return cudaGetLastError();
+  auto kernel = p.type == PEAT_NORM_1 ? gn_small<PEAT_NORM_1>
+                                      : (p.type == PEAT_NORM_INF ? gn_small<PEAT_NORM_INF> : gn_small<PEAT_NORM_2>);
+  return launch_dependent(kernel, 1, GB_SMALL, 0, s, p, in);
 }
 
 }  // namespace peat

@@ -12,6 +12,7 @@
 #include <algorithm>
 
 #include "mm8_common.cuh"
+#include "peat_internal.h"
 
 namespace cg = cooperative_groups;
 
@@ -47,6 +48,8 @@ constexpr int64_t MM8_STREAM_N = 8192;  // rows of b from which every SM has a w
 constexpr int RT = 128;  // threads
 template <int OUT, int NT, int MODE>
 __global__ void __launch_bounds__(RT) mm8_rows(Mm8Params p) {
+  pdl_wait();
+  pdl_trigger();
   __shared__ int part[4][NT * 8][17];
   cg::cluster_group cl = cg::this_cluster();
   const int S = (int)cl.num_blocks(), rank = (int)cl.block_rank();
@@ -129,6 +132,8 @@ __global__ void __launch_bounds__(RT) mm8_rows(Mm8Params p) {
 constexpr int ST = 512;
 template <int OUT, int NT, int MODE>
 __global__ void __launch_bounds__(ST, NT <= 2 ? 2 : 1) mm8_stream(Mm8Params p, int runs_held) {
+  pdl_wait();
+  pdl_trigger();
   extern __shared__ __align__(16) uint2 held[];  // [run][n][j][lane]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int64_t runs = (p.K + 63) / 64, tiles = (p.N + 15) / 16;
@@ -228,6 +233,8 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, int by
 
 template <int OUT, int MODE>
 __global__ void __launch_bounds__(TT, 2) mm8_tiles(Mm8Params p, int ntw) {
+  pdl_wait();
+  pdl_trigger();
   extern __shared__ __align__(128) int8_t smem[];
   cg::cluster_group cl = cg::this_cluster();
   const int S = (int)cl.num_blocks(), rank = (int)cl.block_rank();
@@ -343,17 +350,19 @@ __global__ void __launch_bounds__(TT, 2) mm8_tiles(Mm8Params p, int ntw) {
 
 template <typename F, typename... A>
 cudaError_t cluster_launch(F kernel, int64_t tiles, int S, int threads, int smem, cudaStream_t s, A... args) {
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = (unsigned)S;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * S));
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cfg.attrs = at;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -366,8 +375,7 @@ cudaError_t stream(const Mm8Params& p, int nsm, cudaStream_t s) {
   cudaError_t e = allow_smem(mm8_stream<OUT, NT, MODE>, MOST, allowed);
   if (e != cudaSuccess) return e;
   const unsigned ctas = (unsigned)std::min<int64_t>(CTAS * (int64_t)nsm, tiles);
-  mm8_stream<OUT, NT, MODE><<<ctas, ST, (size_t)held * RUN, s>>>(p, held);
-  return cudaGetLastError();
+  return launch_dependent(mm8_stream<OUT, NT, MODE>, ctas, ST, (size_t)held * RUN, s, p, held);
 }
 
 template <int OUT, int MODE>

@@ -22,9 +22,12 @@
 // of a row; by Cauchy and Schwarz the product of two such norms bounds every
 // partial sum over those 256 k, and the accumulator is drained to int32
 // before the bounds add up to more than 2^24.  Full-range integers drain every
-// 768 k, normally distributed ones about every 16 000.
+// 768 k, normally distributed ones about every 16 000; up to 1024 k nothing can
+// add up to more, and no norms are made.
 #include <cooperative_groups.h>
 #include <cuda.h>
+
+#include <algorithm>
 
 #include "mm8_common.cuh"
 #include "peat_internal.h"
@@ -36,7 +39,14 @@ namespace {
 
 constexpr int BLK = 128 * 64 * 2;  // bytes of a packed block
 constexpr int KN = 256;            // k of one norm
+constexpr int64_t FREE_K = 1024;   // products of any integers whose sum is at most 2^24
 
+// a whole 32-byte sector
+__device__ __forceinline__ void store_sector(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
 // ---------------------------------------------------------------------------
 // pack
 // ---------------------------------------------------------------------------
@@ -52,6 +62,7 @@ struct PackParams {
 
 template <int MODE>
 __global__ void __launch_bounds__(256) mm8_pack(PackParams p) {
+  pdl_wait();
   pdl_trigger();
   const int which = blockIdx.x >= p.first_b;
   const int64_t at = blockIdx.x - (which ? p.first_b : 0);
@@ -69,28 +80,40 @@ __global__ void __launch_bounds__(256) mm8_pack(PackParams p) {
     const int64_t row = rb * 128 + (threadIdx.x >> 4) + 16 * i;
     v[i] = load16<MODE>(x + row * ld + k, row < rows ? left : 0, lo, hi);
   }
-  int most = 0;
+  const bool odd = threadIdx.x >> 4 & 1;  // of the thread's rows: there the two 16-byte pieces change places
+  if (kb < p.kb) {
+    char* d = out + (threadIdx.x >> 4) * 128 + (((l & 3) * 2) ^ ((threadIdx.x >> 4) & 6)) * 16;
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    const int r = (threadIdx.x >> 4) + 16 * i;
-    int ss = __dp4a((int)v[i].x, (int)v[i].x, 0);
-    ss = __dp4a((int)v[i].y, (int)v[i].y, ss);
-    ss = __dp4a((int)v[i].z, (int)v[i].z, ss);
-    ss = __dp4a((int)v[i].w, (int)v[i].w, ss);
-#pragma unroll
-    for (int o = 8; o; o /= 2) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-    most = max(most, ss);
-    if (kb < p.kb) {
-      uint4 a, b;  // the first and the second 8 of the 16
-      to_half(v[i].x, a.x, a.y);
-      to_half(v[i].y, a.z, a.w);
-      to_half(v[i].z, b.x, b.y);
-      to_half(v[i].w, b.z, b.w);
-      uint4* d = reinterpret_cast<uint4*>(out + r * 128 + (((l & 3) * 2) ^ (r & 6)) * 16);
-      d[0] = r & 1 ? b : a;
-      d[1] = r & 1 ? a : b;
+    for (int i = 0; i < 8; i++) {
+      uint32_t w[8];
+      to_half(odd ? v[i].z : v[i].x, w[0], w[1]);
+      to_half(odd ? v[i].w : v[i].y, w[2], w[3]);
+      to_half(odd ? v[i].x : v[i].z, w[4], w[5]);
+      to_half(odd ? v[i].y : v[i].w, w[6], w[7]);
+      store_sector(d + i * (16 * 128), w);
     }
   }
+  if (p.K <= FREE_K) return;  // no norms are needed
+  // sums of squares of the thread's part of 8 rows; 16 lanes have a row: two
+  // values change hands a step while there are several (8 shuffles, not 32)
+  int ss[8];
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    ss[i] = __dp4a((int)v[i].x, (int)v[i].x, 0);
+    ss[i] = __dp4a((int)v[i].y, (int)v[i].y, ss[i]);
+    ss[i] = __dp4a((int)v[i].z, (int)v[i].z, ss[i]);
+    ss[i] = __dp4a((int)v[i].w, (int)v[i].w, ss[i]);
+  }
+#pragma unroll
+  for (int n = 4; n; n /= 2) {
+    const bool high = l & n;
+#pragma unroll
+    for (int i = 0; i < n; i++) {
+      const int give = high ? ss[i] : ss[i + n], keep = high ? ss[i + n] : ss[i];
+      ss[i] = keep + __shfl_xor_sync(0xffffffffu, give, n);
+    }
+  }
+  int most = ss[0] + __shfl_xor_sync(0xffffffffu, ss[0], 8);
   most = __reduce_max_sync(0xffffffffu, most);
   __shared__ int part[8];
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = most;
@@ -130,9 +153,8 @@ struct TcParams {
   const float* nb;
   int kb, kc;
   int mt, nt;       // tiles
-  int splits;       // parts of the k range of a tile
-  int4* sums;       // 128 x 256 int32 for each CTA, or (splits > 1) for each half of each part of a tile
-  unsigned int* tickets;  // splits > 1: one for each result warp of a tile, zero between calls
+  int splits;       // parts of the k range of a tile: 1, 2 or 4; split tiles have a cluster each
+  int4* sums;       // 128 x 256 int32 for each CTA
   int vec_out;      // out's rows start on 32-byte boundaries
   unsigned int* status;
   uint32_t wait_limit;
@@ -159,6 +181,11 @@ __device__ __forceinline__ uint32_t mapa(uint32_t addr, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
+}
+__device__ __forceinline__ int4 load_cluster(uint32_t addr) {
+  int4 v;
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+  return v;
 }
 // waits for the barrier's phase of this parity; false after `limit` polls
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit) {
@@ -203,11 +230,12 @@ __device__ __forceinline__ void mma_256(uint32_t d, uint64_t a, uint64_t b, uint
       "l"(a), "l"(b), "r"(IDESC), "r"(accumulate)
       : "memory");
 }
-// arrives on the barrier at this offset in both CTAs once the instructions issued so far are done
-__device__ __forceinline__ void commit_both(uint32_t bar) {
+// arrives on the barrier at this offset in both CTAs of the pair (their ranks'
+// bits: pair) once the instructions issued so far are done
+__device__ __forceinline__ void commit_both(uint32_t bar, uint16_t pair) {
   asm volatile(
       "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-      "h"((uint16_t)3)
+      "h"(pair)
       : "memory");
 }
 __device__ __forceinline__ void tmem_load32(uint32_t addr, uint32_t (&v)[32]) {
@@ -260,12 +288,6 @@ __device__ __forceinline__ void results(const float* v, float sa, const float* s
     }
   }
 }
-// a whole 32-byte sector
-__device__ __forceinline__ void store_sector(void* p, const uint32_t* w) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
-               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
 // 32 columns of a warp's 32 rows, a row a lane.  Where the rows lie on 32-byte
 // boundaries each lane writes its sectors itself; elsewhere they go through
 // shared memory, 64 bytes of a row at a time (pieces swizzled against bank
@@ -289,7 +311,7 @@ __device__ __forceinline__ void put_columns(const TcParams& p, const float (&v)[
     }
     return;
   }
-  constexpr int E = 16 / B, STEP = 4 * E, R = 32 / STEP;
+  constexpr int E = 16 / B, STEP = 4 * E;
 #pragma unroll
   for (int c = 0; c < 32; c += STEP) {
     __syncwarp();
@@ -300,12 +322,13 @@ __device__ __forceinline__ void put_columns(const TcParams& p, const float (&v)[
       *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1 & 3)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
     __syncwarp();
+    auto at = [&](int r, int e) {  // element e of row r
+      return reinterpret_cast<const T*>(stage + r * 64 + (((e / E) ^ (r >> 1 & 3)) * 16) + (e % E) * B);
+    };
     const int e = lane % STEP;
     if (c + e < left) {
 #pragma unroll 8
-      for (int r = lane / STEP; r < rows; r += R)
-        out[r * p.m.ldo + c + e] = *reinterpret_cast<const T*>(stage + r * 64 + (((e / E) ^ (r >> 1 & 3)) * 16) +
-                                                               (e % E) * B);
+      for (int r = lane / STEP; r < rows; r += 32 / STEP) out[r * p.m.ldo + c + e] = *at(r, e);
     }
   }
 }
@@ -326,16 +349,15 @@ constexpr int GROUP = 8;
 struct Place {
   int tile, mt, nt, k0, k1;
 };
-__device__ __forceinline__ Place place_of(const TcParams& p, int u) {
+__device__ __forceinline__ Place place_of(const TcParams& p, int u, int part) {
   Place r;
-  r.tile = u / p.splits;
-  const int part = u - r.tile * p.splits;
+  r.tile = u;
   // groups of GROUP rows of tiles, column by column: the clusters at work at
   // any time share few blocks of a and few of b
   const int per = GROUP * p.nt, g = r.tile / per, in = r.tile - g * per, wide = min(GROUP, p.mt - g * GROUP);
   r.nt = in / wide;
   r.mt = g * GROUP + in - r.nt * wide;
-  // (kb < 2^12, splits <= 16)
+  // (kb <= 2048, splits <= 4)
   r.k0 = p.kb * part / p.splits;
   r.k1 = p.kb * (part + 1) / p.splits;
   return r;
@@ -347,8 +369,8 @@ __device__ __forceinline__ void plan_scales(const TcParams& p, const Place& t, S
 #pragma unroll
   for (int i = 0; i < 8; i++) {
     const int64_t col = (int64_t)t.nt * 256 + i * 32 + lane;
-    sb[i] = p.m.sb && col < p.m.N ? __ldg(p.m.sb + col) : 1.0f;
-    bias[i] = p.m.bias && col < p.m.N ? __ldg(p.m.bias + col) : 0.0f;
+    sb[i] = p.m.sb && col < p.m.N ? __ldcg(p.m.sb + col) : 1.0f;
+    bias[i] = p.m.bias && col < p.m.N ? __ldcg(p.m.bias + col) : 0.0f;
   }
 #pragma unroll
   for (int i = 0; i < 8; i++) {
@@ -363,7 +385,8 @@ __device__ void plan_drains(const TcParams& p, const Place& t, Slot* slot) {
   const float* nb = p.nb + (int64_t)t.nt * 2 * p.kc;
   int pieces = 1;
   float run = 0.0f;  // the bound of what the accumulator holds
-  for (int c0 = t.k0 / 4, w = 0; c0 * 4 < t.k1; c0 += 32, w++) {
+  if (p.m.K <= FREE_K && lane == 0) slot->drain[0] = 0;
+  for (int c0 = t.k0 / 4, w = 0; p.m.K > FREE_K && c0 * 4 < t.k1; c0 += 32, w++) {
     const int c = c0 + lane;
     float mine = 0.0f;
     if (c * 4 < t.k1)
@@ -399,7 +422,7 @@ __device__ void plan_drains(const TcParams& p, const Place& t, Slot* slot) {
 }
 
 template <int OUT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(THREADS, 1)
     mm8_tc(TcParams p, const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb) {
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
@@ -409,10 +432,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(smem + AT_BARS + 8 * (2 * STAGES + 5 + 2 * SLOTS));
   static_assert(8 * (2 * STAGES + 5 + 2 * SLOTS) + 4 <= BARS, "the barriers fit");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint32_t rank;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  const int units = p.mt * p.nt * p.splits, first = blockIdx.x >> 1, step = gridDim.x >> 1;
+  // a pair's CTAs differ in the last bit of their rank; the parts of a split
+  // tile's k range are the pairs of one cluster
+  uint32_t in_cluster;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(in_cluster));
+  const uint32_t rank = in_cluster & 1, part = in_cluster >> 1, even = in_cluster & ~1u;
+  const uint16_t pair = (uint16_t)(3u << even);
+  const int units = p.mt * p.nt, first = blockIdx.x / (2 * p.splits), step = gridDim.x / (2 * p.splits);
+  const bool split = p.splits > 1;
 
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&ma) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mb) : "memory");
+  }
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; i++) {
       mbar_init(full + 8 * i, 1);   // the even CTA's copier; plus the bytes of both
@@ -438,6 +470,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
   cg::this_cluster().sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_at;
+  pdl_trigger();
 
   bool ok = true;
   if (warp == PLAN_WARP) {
@@ -445,8 +478,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     for (int u = first; u < units && ok; u += step, i++) {
       ok = mbar_wait(unplanned + 8 * (i % SLOTS), (i / SLOTS & 1) ^ 1, p.wait_limit);
       if (!ok) break;
-      const Place t = place_of(p, u);
-      // (the scales are not pack's: they were there before it began)
+      const Place t = place_of(p, u, part);
+      // (the scales are not pack's: what is older than pack was complete before
+      // it let this kernel start)
       plan_scales(p, t, slots + i % SLOTS);
       if (i == 0) pdl_wait();
       plan_drains(p, t, slots + i % SLOTS);
@@ -458,12 +492,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       pdl_wait();
       int seq = 0;
       for (int u = first; u < units && ok; u += step) {
-        const Place t = place_of(p, u);
+        const Place t = place_of(p, u, part);
         const int ra = (t.mt * 2 + (int)rank) * p.kb, rb = (t.nt * 2 + (int)rank) * p.kb;
         for (int k = t.k0; k < t.k1; k++, seq++) {
           const int s = seq % STAGES;
           if (!(ok = mbar_wait(empty + 8 * s, (seq / STAGES & 1) ^ 1, p.wait_limit))) break;
-          const uint32_t dst = sptr(smem + s * STAGE), bar = mapa(full + 8 * s, 0);
+          const uint32_t dst = sptr(smem + s * STAGE), bar = mapa(full + 8 * s, even);
           if (rank == 0) mbar_expect(full + 8 * s, 2 * STAGE);
           tma_block(dst, &ma, (ra + k) * 16, bar);
           tma_block(dst + BLK, &mb, (rb + k) * 16, bar);
@@ -489,7 +523,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             const int c = k / 4 - k0 / 4;
             if ((c & 31) == 0) mask = t->drain[c >> 5];
             if (mask >> (c & 31) & 1) {
-              if (elect_one()) commit_both(acc_full + 8 * (chunk & 1));
+              if (elect_one()) commit_both(acc_full + 8 * (chunk & 1), pair);
               chunk++;
               fresh = true;
             }
@@ -506,8 +540,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
             const uint64_t a = block_desc(base), b = block_desc(base + BLK);
 #pragma unroll
             for (int j = 0; j < 4; j++) mma_256(d, a + 2 * j, b + 2 * j, !(fresh && j == 0));
-            commit_both(empty + 8 * s);
-            if (k == k1 - 1) commit_both(acc_full + 8 * (chunk & 1));
+            commit_both(empty + 8 * s, pair);
+            if (k == k1 - 1) commit_both(acc_full + 8 * (chunk & 1), pair);
           }
           __syncwarp();
           fresh = false;
@@ -516,7 +550,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
         if (lane == 0) mbar_arrive(unplanned + 8 * (i % SLOTS));
       }
       // whatever was issued is done before the accumulators are given back
-      if (elect_one()) commit_both(last);
+      if (elect_one()) commit_both(last, pair);
       mbar_wait(last, 0, p.wait_limit);
       __syncwarp();
     }
@@ -525,8 +559,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
     const int half = warp >> 2, quarter = warp & 3;
     char* stage = smem + AT_ROWS + warp * EPI_ROWS;
     const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
-    const uint32_t release0 = mapa(acc_empty, 0);
-    const bool split = p.splits > 1;
+    const uint32_t release0 = mapa(acc_empty, even);
     for (int u = first; u < units && ok; u += step, i++) {
       const Slot* t = slots + i % SLOTS;
       if (!(ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
@@ -535,14 +568,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
       const int64_t col0 = (int64_t)t->nt * 256 + half * 128;
       const float *sb = t->sb + half * 128, *bias = t->bias + half * 128;
       const int rows = (int)max((int64_t)0, min((int64_t)32, p.m.M - row0));
-      const float sa = p.m.sa && lane < rows ? __ldg(p.m.sa + row0 + lane) : 1.0f;
+      const float sa = p.m.sa && lane < rows ? __ldcg(p.m.sa + row0 + lane) : 1.0f;
       // One piece that is the whole sum goes straight from the accumulator to
-      // the output.  Otherwise pieces are added up as integers in memory, in a
-      // place of this CTA's, or, for a tile whose k range is split, of this
-      // part's; the last part to come adds up all of them.
+      // the output.  Several are added up as integers in memory, in a place of
+      // this CTA's.  The sum of a split tile's part (its CTA's only one) goes to
+      // the stages' place in shared memory, where the other parts find it; the
+      // last piece is there when the instructions are done with the stages.
       const bool whole = pieces == 1 && !split;
-      const int64_t area = (int64_t)EPI_WARPS * 8 * 128;  // int4 values of a CTA's half tile
-      int4* sums = p.sums + (split ? ((int64_t)u * 2 + rank) : (int64_t)blockIdx.x) * area + warp * (8 * 128) + lane;
+      const int mine = warp * (8 * 128) + lane;
+      int4* sums = p.sums + (int64_t)blockIdx.x * (EPI_WARPS * 8 * 128) + mine;
+      int4* shared_sums = reinterpret_cast<int4*>(smem) + mine;
       for (int q = 0; q < pieces && ok; q++, chunk++) {
         if (!(ok = mbar_wait(acc_full + 8 * (chunk & 1), chunk / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -560,12 +595,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int j = 0; j < 32; j++) f[j] = __uint_as_float(v[j]);
           if (!whole) {
-            int4* s4 = sums + g * 8 * 32;
             int4 x[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-              x[j] = q ? __ldcg(s4 + j * 32) : make_int4(0, 0, 0, 0);
-            }
+            for (int j = 0; j < 8; j++) x[j] = q ? sums[(g * 8 + j) * 32] : make_int4(0, 0, 0, 0);
 #pragma unroll
             for (int j = 0; j < 8; j++) {
               x[j].x += __float2int_rn(f[4 * j]);
@@ -573,9 +605,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
               x[j].z += __float2int_rn(f[4 * j + 2]);
               x[j].w += __float2int_rn(f[4 * j + 3]);
             }
-            if (split || q < pieces - 1) {
+            if (q < pieces - 1) {
 #pragma unroll
-              for (int j = 0; j < 8; j++) __stcg(s4 + j * 32, x[j]);
+              for (int j = 0; j < 8; j++) sums[(g * 8 + j) * 32] = x[j];
+              continue;
+            }
+            if (split) {
+#pragma unroll
+              for (int j = 0; j < 8; j++) shared_sums[(g * 8 + j) * 32] = x[j];
               continue;
             }
             as_results<OUT>(x, f);
@@ -586,42 +623,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
           put_columns<OUT>(p, f, sa, sb + g * 32, bias + g * 32, stage, row0, rows, col0 + g * 32);
         }
       }
-      if (!ok) break;
-      if (split) {
-        __threadfence();
-        __syncwarp();
-        unsigned int n = 0;
-        unsigned int* ticket = p.tickets + ((int64_t)t->tile * 2 + rank) * EPI_WARPS + warp;
-        if (lane == 0) {
-          n = atomicAdd(ticket, 1u);
-          if (n == (unsigned)p.splits - 1) *ticket = 0;
-        }
-        if (__shfl_sync(0xffffffffu, n, 0) == (unsigned)p.splits - 1) {
-          __threadfence();
-          const int4* all = p.sums + ((int64_t)t->tile * p.splits * 2 + rank) * area + warp * (8 * 128) + lane;
-#pragma unroll 1
-          for (int g = 0; g < 4; g++) {
-            int4 x[8];
-            float f[32];
-#pragma unroll
-            for (int j = 0; j < 8; j++) x[j] = __ldcg(all + (g * 8 + j) * 32);
-            for (int k = 1; k < p.splits; k++) {
-#pragma unroll
-              for (int j = 0; j < 8; j++) {
-                const int4 y = __ldcg(all + k * 2 * area + (g * 8 + j) * 32);
-                x[j].x += y.x;
-                x[j].y += y.y;
-                x[j].z += y.z;
-                x[j].w += y.w;
-              }
-            }
-            as_results<OUT>(x, f);
-            put_columns<OUT>(p, f, sa, sb + g * 32, bias + g * 32, stage, row0, rows, col0 + g * 32);
-          }
-        }
-      }
+      if (!ok || split) break;  // (a split tile's slot is still needed)
       __syncwarp();
       if (lane == 0) mbar_arrive(unplanned + 8 * (i % SLOTS));
+    }
+  }
+  __syncwarp();
+  if (split) {
+    // The parts meet: each CTA adds up its share of the columns over the pairs.
+    cg::this_cluster().sync();
+    if (warp < EPI_WARPS && ok) {
+      const Slot* t = slots;
+      const int half = warp >> 2, quarter = warp & 3;
+      const int64_t row0 = (int64_t)t->mt * 256 + rank * 128 + quarter * 32, col0 = (int64_t)t->nt * 256 + half * 128;
+      const int rows = (int)max((int64_t)0, min((int64_t)32, p.m.M - row0));
+      const float sa = p.m.sa && lane < rows ? __ldcg(p.m.sa + row0 + lane) : 1.0f;
+#pragma unroll 1
+      for (int g = part; g < 4; g += p.splits) {
+        const uint32_t at = sptr(smem) + (uint32_t)(((warp * 4 + g) * 8 * 32 + lane) * 16);
+        int4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) x[j] = make_int4(0, 0, 0, 0);
+#pragma unroll 2
+        for (int k = 0; k < p.splits; k++) {
+          const uint32_t from = mapa(at, rank + 2 * k);
+#pragma unroll
+          for (int j = 0; j < 8; j++) {
+            const int4 y = load_cluster(from + j * 512);
+            x[j].x += y.x;
+            x[j].y += y.y;
+            x[j].z += y.z;
+            x[j].w += y.w;
+          }
+        }
+        float f[32];
+        as_results<OUT>(x, f);
+        put_columns<OUT>(p, f, sa, t->sb + half * 128 + g * 32, t->bias + half * 128 + g * 32,
+                         smem + AT_ROWS + warp * EPI_ROWS, row0, rows, col0 + g * 32);
+      }
     }
   }
   if (!ok) atomicOr_system(p.status, 1u);
@@ -663,9 +702,22 @@ cudaError_t tc_launch(const TcParams& p, const CUtensorMap& ma, const CUtensorMa
   static std::atomic<uint64_t> allowed{0};
   cudaError_t e = allow_smem(mm8_tc<OUT>, SMEM, allowed);
   if (e != cudaSuccess) return e;
-  const int64_t units = (int64_t)p.mt * p.nt * p.splits;
-  const int clusters = (int)(units < nsm / 2 ? units : nsm / 2);
-  return launch_dependent(mm8_tc<OUT>, (unsigned)(clusters * 2), THREADS, SMEM, s, p, ma, mb);
+  const int64_t tiles = (int64_t)p.mt * p.nt;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = 2 * (unsigned)p.splits;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  // persistent pairs, or a cluster for each split tile
+  cfg.gridDim = dim3((unsigned)(p.splits > 1 ? tiles * 2 * p.splits : 2 * std::min<int64_t>(tiles, nsm / 2)));
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = SMEM;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, mm8_tc<OUT>, p, ma, mb);
 }
 
 }  // namespace
@@ -677,13 +729,15 @@ Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm) {
   r.mt = (M + 255) / 256;
   r.nt = (N + 255) / 256;
   r.splits = 1;
-  const int64_t tiles = r.mt * r.nt, clusters = nsm / 2;
-  // Time of a split in blocks of 64 k: the blocks of the waves, and for a split
-  // tile what adding up its parts costs (about 12 blocks each).
+  const int64_t tiles = r.mt * r.nt;
+  // Time of a split in blocks of 64 k (about 520 cycles): those of the waves,
+  // and what each tile pays once. Clusters of 8 do not fill the GPU (15 of them
+  // run at once, of 152 SMs), those of 4 nearly do.
   double best = 0.0;
-  for (int s = 1; s <= 16 && s <= r.kb / 4; s++) {
-    const double t = (double)((tiles * s + clusters - 1) / clusters) * ((double)r.kb / s + (s > 1 ? 14 : 4));
-    if (s == 1 || t < 0.95 * best) best = t, r.splits = s;
+  for (int s = 1; s <= 4 && s <= r.kb; s *= 2) {
+    const int64_t clusters = s == 1 ? nsm / 2 : (s == 2 ? nsm / 4 - 1 : nsm / 10);
+    const double t = (double)((tiles + clusters - 1) / clusters) * ((double)r.kb / s + (s == 1 ? 2 : (s == 2 ? 10 : 8))) + 14;
+    if (s == 1 || t < best) best = t, r.splits = s;
   }
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   size_t at = 0;
@@ -697,13 +751,13 @@ Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm) {
   at += up((size_t)r.nt * 2 * r.kc * sizeof(float));
   r.bytes = at;
   r.sum_off = at;
-  r.bytes = at + (size_t)(r.splits > 1 ? tiles * r.splits * 2 : nsm) * (128 * 256 * sizeof(int));
-  r.tickets = r.splits > 1 ? (size_t)tiles * 2 * EPI_WARPS : 0;
+  if (K > FREE_K) at += (size_t)(r.splits > 1 ? tiles * 2 * r.splits : nsm) * (128 * 256 * sizeof(int));
+  r.bytes = at;
   return r;
 }
 
-cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* tickets,
-                          unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s) {
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* status,
+                          unsigned int wait_limit, int nsm, cudaStream_t s) {
   PackParams k;
   k.x[0] = m.a;
   k.x[1] = m.b;
@@ -722,9 +776,7 @@ cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& pl
   const int64_t ctas = k.first_b + plan.nt * 2 * plan.kc;
   const bool al = ((reinterpret_cast<uintptr_t>(m.a) | reinterpret_cast<uintptr_t>(m.b) | (uintptr_t)m.lda |
                     (uintptr_t)m.ldb) & 15) == 0;
-  if (al) mm8_pack<16><<<(unsigned)ctas, 256, 0, s>>>(k);
-  else mm8_pack<1><<<(unsigned)ctas, 256, 0, s>>>(k);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = launch_dependent(al ? mm8_pack<16> : mm8_pack<1>, (unsigned)ctas, 256, 0, s, k);
   if (e != cudaSuccess) return e;
   CUtensorMap ma, mb;
   if (!block_map(&ma, ws + plan.a_off, plan.mt * 2 * plan.kb) || !block_map(&mb, ws + plan.b_off, plan.nt * 2 * plan.kb))
@@ -739,7 +791,6 @@ cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& pl
   p.nt = (int)plan.nt;
   p.splits = plan.splits;
   p.sums = reinterpret_cast<int4*>(ws + plan.sum_off);
-  p.tickets = tickets;
   p.vec_out = reinterpret_cast<uintptr_t>(m.out) % 32 == 0 &&
               m.ldo * (out_dtype == PEAT_F16 || out_dtype == PEAT_BF16 ? 2 : 4) % 32 == 0;
   p.status = status;

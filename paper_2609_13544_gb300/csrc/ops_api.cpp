@@ -210,8 +210,6 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
   p.K = K;
   if (h->status_host && *(volatile unsigned int*)h->status_host) {
     *(volatile unsigned int*)h->status_host = 0;
-    // what the call left of its counters is cleared
-    if (h->ops && h->ops->tickets) cudaMemsetAsync(h->ops->tickets, 0, h->ops->tickets_cap, st);
     return fail(h, PEAT_ERR_TIMEOUT,
                 "a bounded device-side wait expired in an earlier call on this handle; its outputs are invalid");
   }
@@ -224,11 +222,9 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
     OpsState* s = nullptr;
     peat_status_t ps = ops_state(h, &s);
     if (ps == PEAT_OK) ps = grow(h, &s->mm, &s->mm_cap, plan.bytes);
-    if (ps == PEAT_OK) ps = tickets(h, s, plan.tickets, st);
     if (ps != PEAT_OK) return ps;
     const unsigned int limit = std::min(h->wait_limit, 1u << 22);
-    e = peat::launch_mm8_tc(out_dtype, p, plan, static_cast<char*>(s->mm), static_cast<unsigned int*>(s->tickets),
-                            h->status_dev, limit, h->nsm, st);
+    e = peat::launch_mm8_tc(out_dtype, p, plan, static_cast<char*>(s->mm), h->status_dev, limit, h->nsm, st);
   } else {
     e = peat::launch_mm8_direct(out_dtype, p, h->nsm, st);
   }

@@ -59,13 +59,12 @@ cudaError_t launch_mm8_direct(int out_dtype, const Mm8Params& p, int nsm, cudaSt
 struct Mm8TcPlan {
   int kb, kc;      // blocks of 64 k, and of 256
   int64_t mt, nt;  // tiles
-  int splits;      // parts of a tile's k range
+  int splits;      // parts of a tile's k range: 1, 2 or 4
   size_t a_off, b_off, na_off, nb_off, sum_off, bytes;  // workspace
-  size_t tickets;  // counters, zero between calls
 };
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm);
-cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, unsigned int* tickets,
-                          unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s);
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, unsigned int* status,
+                          unsigned int wait_limit, int nsm, cudaStream_t s);
 
 // ---- gradient lists (gradnorm.cu) ----
 struct GnEntry {

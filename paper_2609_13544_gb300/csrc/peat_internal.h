@@ -23,7 +23,7 @@ __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;"
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <typename... KA, typename... A>
 inline cudaError_t launch_dependent(void (*kernel)(KA...), dim3 grid, unsigned block, size_t smem,
-                                    cudaStream_t s, A... args) {
+                                    cudaStream_t s, const A&... args) {
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;

@@ -199,6 +199,8 @@ __device__ __forceinline__ uint32_t row_max(uint32_t m) {
 template <int DT, int TPR, int NV>
 __global__ void __launch_bounds__(QT) quant_rows(QuantParams p) {
   using L = Elem<DT>;
+  pdl_wait();
+  pdl_trigger();
   const int lane = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * (QT / TPR) + threadIdx.x / TPR;
   if (row >= p.rows) return;  // (whole warps; with TPR = QT there is a row for every CTA)
@@ -237,6 +239,8 @@ __global__ void __launch_bounds__(QT) quant_rows(QuantParams p) {
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(QT) quant_rows_twice(QuantParams p) {
   using L = Elem<DT>;
+  pdl_wait();
+  pdl_trigger();
   const int64_t row = blockIdx.x;
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + row * p.ldx;
   uint32_t top = 0;
@@ -284,6 +288,7 @@ __global__ void __launch_bounds__(QT) quant_rows_twice(QuantParams p) {
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(QT) quant_colmax(QuantParams p, int vl, int64_t rows_each) {
   using L = Elem<DT>;
+  pdl_wait();
   pdl_trigger();
   __shared__ uint4 part[QT];
   const int lx = threadIdx.x % vl, ly = threadIdx.x / vl, nl = QT / vl;
@@ -346,6 +351,7 @@ __global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_
   const int64_t r0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * rows_each, r1 = min(p.rows, r0 + rows_each);
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + col;
   pdl_wait();
+  pdl_trigger();
   // the other buffer of maxima is the next call's: zero again
   {
     const int64_t n = (int64_t)gridDim.x * gridDim.y * QT;
@@ -437,21 +443,19 @@ __global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_
 template <int DT>
 cudaError_t rows_launch(const QuantParams& p, cudaStream_t s) {
   constexpr int E = Elem<DT>::E;
-  if (!p.vec_x) {
-    quant_rows_twice<DT, false><<<(unsigned)p.rows, QT, 0, s>>>(p);
-    return cudaGetLastError();
-  }
+  if (!p.vec_x) return launch_dependent(quant_rows_twice<DT, false>, (unsigned)p.rows, QT, 0, s, p);
   const int64_t nv = (p.cols + E - 1) / E;
-  auto grid = [&](int tpr) { return (unsigned)((p.rows + QT / tpr - 1) / (QT / tpr)); };
-  if (nv <= 32) quant_rows<DT, 32, 1><<<grid(32), QT, 0, s>>>(p);
-  else if (nv <= 64) quant_rows<DT, 32, 2><<<grid(32), QT, 0, s>>>(p);
-  else if (nv <= 128) quant_rows<DT, 32, 4><<<grid(32), QT, 0, s>>>(p);
-  else if (nv <= 256) quant_rows<DT, QT, 1><<<grid(QT), QT, 0, s>>>(p);
-  else if (nv <= 512) quant_rows<DT, QT, 2><<<grid(QT), QT, 0, s>>>(p);
-  else if (nv <= 1024) quant_rows<DT, QT, 4><<<grid(QT), QT, 0, s>>>(p);
-  else if (nv <= 2048) quant_rows<DT, QT, 8><<<grid(QT), QT, 0, s>>>(p);
-  else quant_rows_twice<DT, true><<<(unsigned)p.rows, QT, 0, s>>>(p);
-  return cudaGetLastError();
+  auto go = [&](void (*kernel)(QuantParams), int tpr) {
+    return launch_dependent(kernel, (unsigned)((p.rows + QT / tpr - 1) / (QT / tpr)), QT, 0, s, p);
+  };
+  if (nv <= 32) return go(quant_rows<DT, 32, 1>, 32);
+  if (nv <= 64) return go(quant_rows<DT, 32, 2>, 32);
+  if (nv <= 128) return go(quant_rows<DT, 32, 4>, 32);
+  if (nv <= 256) return go(quant_rows<DT, QT, 1>, QT);
+  if (nv <= 512) return go(quant_rows<DT, QT, 2>, QT);
+  if (nv <= 1024) return go(quant_rows<DT, QT, 4>, QT);
+  if (nv <= 2048) return go(quant_rows<DT, QT, 8>, QT);
+  return go(quant_rows_twice<DT, true>, QT);
 }
 
 template <int DT, bool VEC>
@@ -471,8 +475,7 @@ cudaError_t cols_launch(const QuantParams& p, int nsm, cudaStream_t s) {
   int64_t each = 1;
   const unsigned ny = shares(wide, 8 * lanes, 1, 5, &each);
   if (p.rows > 0) {
-    quant_colmax<DT, VEC><<<dim3((unsigned)wide, ny), QT, 0, s>>>(p, vl, std::max<int64_t>(each, 1));
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = launch_dependent(quant_colmax<DT, VEC>, dim3((unsigned)wide, ny), QT, 0, s, p, vl, std::max<int64_t>(each, 1));
     if (e != cudaSuccess) return e;
   }
   const int64_t strips = (p.cols + CW - 1) / CW;
