@@ -8,7 +8,7 @@
  * (activation, weight, output gradient), and scores them against the golden
  * ones.  Here the lower precision is 8-bit integers with one scale for each
  * row of either operand: peat_quantize_i8 makes the operands,
- * peat_matmul_i8 multiplies them.  A training step ends with the norm over
+ * peat_matmul_i8 multiplies them, peat_product_i8 does both.  A training step ends with the norm over
  * all its gradient tensors, by which they are clipped: peat_grad_norm and
  * peat_grad_clip.
  *
@@ -74,6 +74,30 @@ peat_status_t peat_quantize_i8(peat_handle_t h, const void* x, int64_t rows, int
 peat_status_t peat_matmul_i8(peat_handle_t h, const int8_t* a, int64_t lda, const float* a_scale, const int8_t* b,
                              int64_t ldb, const float* b_scale, const float* bias, int64_t M, int64_t N, int64_t K,
                              void* out, int64_t ldo, int out_dtype, peat_stream_t stream);
+
+/* An operand of peat_product_i8: a matrix [rows, cols], row r at data + r * ld
+ * elements (ld >= cols).  dtype PEAT_INT8: 8-bit integers with their scales
+ * (scale: float32 [rows], NULL: 1), axis 0.  dtype PEAT_F32, PEAT_F16 or
+ * PEAT_BF16: rounded to such integers as peat_quantize_i8 does, with a scale
+ * for each row (axis 0), or for each column (axis 1, whose transpose is then
+ * the operand); scale is not read. */
+#define PEAT_INT8 101
+typedef struct {
+  const void* data;
+  const float* scale;
+  int64_t rows, cols, ld;
+  int32_t dtype;
+  int32_t axis;
+} peat_operand_t;
+
+/* peat_matmul_i8 of two operands that are rounded on the way where they are
+ * not integers yet: a's M x K is rows x cols (axis 0) or cols x rows (axis 1),
+ * b's N x K likewise, the two K equal.  The results are those of
+ * peat_quantize_i8 followed by peat_matmul_i8, in one call and without the
+ * integers' detour through the caller.  out_dtype PEAT_F32, PEAT_F16 or
+ * PEAT_BF16. */
+peat_status_t peat_product_i8(peat_handle_t h, const peat_operand_t* a, const peat_operand_t* b, const float* bias,
+                              void* out, int64_t ldo, peat_dtype_t out_dtype, peat_stream_t stream);
 
 /* One tensor of a gradient list (a HOST array, copied before the call
  * returns): n contiguous elements of type dtype (PEAT_F32, PEAT_F16,

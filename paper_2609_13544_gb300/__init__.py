@@ -20,8 +20,8 @@ import numpy as np
 from . import ops as _ops
 from .buildlib import LIB, build  # noqa: F401
 from .ops import (GRADNORM_BYTES, OPS_EXPORTS, GradList, Linear8, peat_grad_clip, peat_grad_clip_raw,  # noqa: F401
-                  peat_grad_norm, peat_grad_norm_raw, peat_matmul_i8, peat_matmul_i8_raw, peat_quantize_i8,
-                  peat_quantize_i8_raw)
+                  peat_grad_norm, peat_grad_norm_raw, peat_matmul_i8, peat_matmul_i8_raw, peat_product_i8,
+                  peat_product_i8_raw, peat_quantize_i8, peat_quantize_i8_raw)
 
 DTYPE_CODES = {"f32": 0, "f16": 1, "bf16": 2}
 CLASSES = ("exact", "within_tol", "mismatch", "nan_inf_asym", "sign_flip")

@@ -33,6 +33,9 @@ struct OpsState {
   size_t colmax_cap = 0;  // bytes of both
   int64_t colmax_used[2] = {0, 0};
   int colmax_at = 0;
+  // operands that a product rounds, and their scales
+  void* rounded = nullptr;
+  size_t rounded_cap = 0;
   // products: packed operands and partial sums
   void* mm = nullptr;
   size_t mm_cap = 0;
@@ -45,6 +48,7 @@ void ops_destroy(OpsState* s) {
   if (s->tickets) cudaFree(s->tickets);
   if (s->colmax) cudaFree(s->colmax);
   if (s->mm) cudaFree(s->mm);
+  if (s->rounded) cudaFree(s->rounded);
   for (int i = 0; i < OpsState::RING; i++) {
     if (s->h_list[i]) cudaFreeHost(s->h_list[i]);
     if (s->taken[i]) cudaEventDestroy(s->taken[i]);
@@ -232,6 +236,67 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
   return PEAT_OK;
 }
 
+// Rounds a float operand into the handle's workspace at *at, which moves on.
+// Before a pass with ws NULL only the place is counted.
+struct Operand {
+  const int8_t* q;
+  const float* scale;
+  int64_t rows, K, ld;
+};
+bool operand_ok(const peat_operand_t* o) {
+  if (!o || o->rows < 0 || o->cols < 0 || o->ld < o->cols) return false;
+  if (o->dtype == PEAT_INT8) return o->axis == 0;
+  return type_bytes(o->dtype) != 0 && (o->axis == 0 || o->axis == 1);
+}
+Operand operand_of(const peat_operand_t& o, char* ws, size_t* at) {
+  Operand r;
+  r.rows = o.axis ? o.cols : o.rows;
+  r.K = o.axis ? o.rows : o.cols;
+  if (o.dtype == PEAT_INT8) {
+    r.q = static_cast<const int8_t*>(o.data);
+    r.scale = o.scale;
+    r.ld = o.ld;
+    return r;
+  }
+  r.ld = (r.K + 15) / 16 * 16;
+  r.scale = reinterpret_cast<const float*>(ws + *at);
+  *at += ((size_t)r.rows * sizeof(float) + 255) / 256 * 256;
+  r.q = reinterpret_cast<const int8_t*>(ws + *at);
+  *at += ((size_t)r.rows * (size_t)r.ld + 255) / 256 * 256;
+  return r;
+}
+
+peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_operand_t* b, const float* bias, void* out,
+                      int64_t ldo, int out_dtype, cudaStream_t st) {
+  if (!operand_ok(a) || !operand_ok(b))
+    return fail(h, PEAT_ERR_INVALID_ARG, "an operand is NULL, or its sizes, dtype or axis are not valid");
+  if (!type_bytes(out_dtype)) return fail(h, PEAT_ERR_INVALID_ARG, "out_dtype must be PEAT_F32, PEAT_F16 or PEAT_BF16");
+  size_t need = 0;
+  Operand x = operand_of(*a, nullptr, &need), y = operand_of(*b, nullptr, &need);
+  if (x.K != y.K) return fail(h, PEAT_ERR_INVALID_ARG, "the operands differ in K");
+  if (x.K > 131071) return fail(h, PEAT_ERR_UNSUPPORTED, "K above 131071: the sums may not fit 32 bits");
+  if (x.rows == 0 || y.rows == 0) return PEAT_OK;
+  DeviceGuard dg(h->device);
+  if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
+  OpsState* s = nullptr;
+  peat_status_t ps = ops_state(h, &s);
+  if (ps == PEAT_OK) ps = grow(h, &s->rounded, &s->rounded_cap, need);
+  if (ps != PEAT_OK) return ps;
+  char* ws = static_cast<char*>(s->rounded);
+  size_t at = 0;
+  x = operand_of(*a, ws, &at);
+  y = operand_of(*b, ws, &at);
+  const peat_operand_t* in[2] = {a, b};
+  const Operand* op[2] = {&x, &y};
+  for (int i = 0; i < 2; i++) {
+    if (in[i]->dtype == PEAT_INT8) continue;
+    ps = quantize(h, in[i]->data, in[i]->rows, in[i]->cols, in[i]->ld, in[i]->dtype, in[i]->axis,
+                  const_cast<int8_t*>(op[i]->q), op[i]->ld, const_cast<float*>(op[i]->scale), nullptr, 0, st);
+    if (ps != PEAT_OK) return ps;
+  }
+  return matmul(h, x.q, x.ld, x.scale, y.q, y.ld, y.scale, bias, x.rows, y.rows, x.K, out, ldo, out_dtype, st);
+}
+
 peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count, int type, float unscale, bool clip,
                         float max_norm, float eps, int bad, peat_gradnorm_t* result, float* norms, cudaStream_t st) {
   if (count < 0 || (count > 0 && !list)) return fail(h, PEAT_ERR_INVALID_ARG, "count < 0, or list is NULL");
@@ -376,6 +441,13 @@ peat_status_t peat_matmul_i8(peat_handle_t h, const int8_t* a, int64_t lda, cons
   return guarded(h, [&] {
     return matmul(h, a, lda, a_scale, b, ldb, b_scale, bias, M, N, K, out, ldo, out_dtype,
                   reinterpret_cast<cudaStream_t>(stream));
+  });
+}
+
+peat_status_t peat_product_i8(peat_handle_t h, const peat_operand_t* a, const peat_operand_t* b, const float* bias,
+                              void* out, int64_t ldo, peat_dtype_t out_dtype, peat_stream_t stream) {
+  return guarded(h, [&] {
+    return product(h, a, b, bias, out, ldo, out_dtype, reinterpret_cast<cudaStream_t>(stream));
   });
 }
 

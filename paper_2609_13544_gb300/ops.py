@@ -1,7 +1,8 @@
 """Binding of the playback operators (include/peat_ops.h), and a linear layer made of them.
 
-``peat_quantize_i8`` and ``peat_matmul_i8`` are a linear layer's products in
-8-bit integers with a scale for each row of either operand; ``peat_grad_norm``
+``peat_quantize_i8`` and ``peat_matmul_i8`` (in one call: ``peat_product_i8``)
+are a linear layer's products in 8-bit integers with a scale for each row of
+either operand; ``peat_grad_norm``
 and ``peat_grad_clip`` the norm over a list of gradient tensors and their
 clipping.  As in the rest of the binding, a ``_raw`` function fills outputs
 that the caller holds; the plain ones allocate them.  All of them only enqueue
@@ -23,7 +24,8 @@ GRADNORM_BYTES = 16
 NORM_TYPES = {"2": 0, "1": 1, "inf": 2}
 BAD_MODES = {"propagate": 0, "zero": 1, "keep": 2}
 
-OPS_EXPORTS = ("peat_quantize_i8", "peat_matmul_i8", "peat_grad_norm", "peat_grad_clip")
+OPS_EXPORTS = ("peat_quantize_i8", "peat_matmul_i8", "peat_product_i8", "peat_grad_norm", "peat_grad_clip")
+INT8 = 101
 
 
 class GradEntry(ctypes.Structure):
@@ -31,11 +33,18 @@ class GradEntry(ctypes.Structure):
                 ("reserved", ctypes.c_int32)]
 
 
+class Operand8(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("axis", ctypes.c_int32)]
+
+
 def register(L) -> None:
     """Argument types of the entry points in a loaded library."""
     vp, i64, i32, f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
     L.peat_quantize_i8.argtypes = [vp, vp, i64, i64, i64, i32, i32, vp, i64, vp, vp, i64, vp]
     L.peat_matmul_i8.argtypes = [vp, vp, i64, vp, vp, i64, vp, vp, i64, i64, i64, vp, i64, i32, vp]
+    op = ctypes.POINTER(Operand8)
+    L.peat_product_i8.argtypes = [vp, op, op, vp, vp, i64, i32, vp]
     L.peat_grad_norm.argtypes = [vp, vp, i64, i32, f32, vp, vp, vp]
     L.peat_grad_clip.argtypes = [vp, vp, i64, i32, f32, f32, f32, i32, vp, vp, vp]
     for name in OPS_EXPORTS:
@@ -171,6 +180,47 @@ def peat_matmul_i8(h, a, a_scale, b, b_scale, bias=None, out_dtype=None, stream=
     return out
 
 
+def _operand(h, t, axis: int, scale, name: str):
+    """(structure, rows of the operand, its K) of a matrix that is 8-bit integers or is rounded to them."""
+    import torch
+    ld = _matrix(h, t, name)
+    rows, cols = t.shape
+    if t.dtype is torch.int8:
+        if axis != 0:
+            raise ValueError(f"{name} is integers already: axis 0")
+        return Operand8(t.data_ptr(), _vector(h, scale, rows, name + "'s scale"), rows, cols, ld, INT8, 0), rows, cols
+    if scale is not None:
+        raise ValueError(f"{name} is not integers: it has no scale yet")
+    op = Operand8(t.data_ptr(), None, rows, cols, ld, _code(t), axis)
+    return (op, cols, rows) if axis else (op, rows, cols)
+
+
+def peat_product_i8_raw(h, a, b, out, a_axis: int = 0, b_axis: int = 0, a_scale=None, b_scale=None, bias=None,
+                        stream=None) -> None:
+    """peat_product_i8 into out [M, N] (float32, float16 or bfloat16): each operand int8 with its scale, or a float
+    matrix that is rounded with a scale for each row (axis 0) or column (axis 1; its transpose is the operand)."""
+    x, M, K = _operand(h, a, a_axis, a_scale, "a")
+    y, N, K2 = _operand(h, b, b_axis, b_scale, "b")
+    if K != K2:
+        raise ValueError("a and b differ in their row length")
+    ldo = _matrix(h, out, "out")
+    if out.shape[0] != M or out.shape[1] != N:
+        raise ValueError("out must be [rows of a, rows of b]")
+    _call(h, "peat_product_i8", ctypes.byref(x), ctypes.byref(y), _vector(h, bias, N, "bias"), out.data_ptr(), ldo,
+          _code(out), _stream(h, stream))
+
+
+def peat_product_i8(h, a, b, a_axis: int = 0, b_axis: int = 0, a_scale=None, b_scale=None, bias=None, out_dtype=None,
+                    stream=None):
+    """The product as a new tensor of out_dtype (float32 unless given)."""
+    import torch
+    with _on(stream):
+        out = torch.empty(a.shape[1 if a_axis else 0], b.shape[1 if b_axis else 0], dtype=out_dtype or torch.float32,
+                          device=a.device)
+        peat_product_i8_raw(h, a, b, out, a_axis, b_axis, a_scale, b_scale, bias, stream)
+    return out
+
+
 class GradList:
     """A list of gradient tensors (and, for clipping, of as many output tensors; None: in place), made once and
     passed to every peat_grad_norm or peat_grad_clip.  It holds the tensors: where a program gives a parameter a
@@ -279,31 +329,26 @@ class Linear8:
     def _rows(self, t, width: int, name: str):
         if t.dim() < 1 or t.shape[-1] != width:
             raise ValueError(f"the last dimension of {name} must be {width}")
-        return t.reshape(-1, width)
+        return t if t.dim() == 2 else t.reshape(-1, width)
 
     def forward(self, x, bias=None, stream=None):
         """x [..., in] -> [..., out] of x's type."""
-        with _on(stream):
-            q, s = peat_quantize_i8(self.h, self._rows(x, self.in_features, "x"), 0, stream)
-            y = peat_matmul_i8(self.h, q, s, self.q, self.scale, bias, x.dtype, stream)
-        return y.view(*x.shape[:-1], self.out_features)
+        y = peat_product_i8(self.h, self._rows(x, self.in_features, "x"), self.q, 0, 0, None, self.scale, bias, x.dtype,
+                            stream)
+        return y if x.dim() == 2 else y.view(*x.shape[:-1], self.out_features)
 
     def input_grad(self, grad, stream=None):
         """dL/dx [..., in] of grad's type from grad = dL/dy [..., out]."""
-        with _on(stream):
-            q, s = peat_quantize_i8(self.h, self._rows(grad, self.out_features, "grad"), 0, stream)
-            g = peat_matmul_i8(self.h, q, s, self.qt, self.scale_t, None, grad.dtype, stream)
-        return g.view(*grad.shape[:-1], self.in_features)
+        g = peat_product_i8(self.h, self._rows(grad, self.out_features, "grad"), self.qt, 0, 0, None, self.scale_t, None,
+                            grad.dtype, stream)
+        return g if grad.dim() == 2 else g.view(*grad.shape[:-1], self.in_features)
 
     def weight_grad(self, grad, x, stream=None):
         """dL/dw [out, in] in float32 from grad [..., out] and x [..., in]."""
-        with _on(stream):
-            g, x = self._rows(grad, self.out_features, "grad"), self._rows(x, self.in_features, "x")
-            if g.shape[0] != x.shape[0]:
-                raise ValueError("grad and x differ in their leading dimensions")
-            qg, sg = peat_quantize_i8(self.h, g, 1, stream)
-            qx, sx = peat_quantize_i8(self.h, x, 1, stream)
-            return peat_matmul_i8(self.h, qg, sg, qx, sx, None, None, stream)
+        g, x = self._rows(grad, self.out_features, "grad"), self._rows(x, self.in_features, "x")
+        if g.shape[0] != x.shape[0]:
+            raise ValueError("grad and x differ in their leading dimensions")
+        return peat_product_i8(self.h, g, x, 1, 1, stream=stream)
 
     def backward(self, grad, x, stream=None):
         """(dL/dx, dL/dw)."""

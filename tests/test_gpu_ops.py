@@ -535,3 +535,75 @@ def test_refusals(peat_gpu, h):
     assert quant(rows=1 << 31, cols=8) == 2
     assert L.peat_grad_norm(None, None, 0, 0, 1.0, rec, None, None) == 1
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("axes", [(0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("mnk", [(1, 64, 128), (33, 70, 129), (300, 270, 520), (512, 256, 1500), (700, 300, 3100)])
+@pytest.mark.parametrize("dtypes", [("f32", "bf16"), ("f16", "f16"), ("bf16", "int8"), ("int8", "f32")])
+def test_product(peat_gpu, h, axes, mnk, dtypes):
+    """Operands rounded on the way give what rounding and multiplying them one after the other gives."""
+    import torch
+    M, N, K = mnk
+    g = rng(M + K)
+    args, want = [], []
+    for rows, axis, d in ((M, axes[0], dtypes[0]), (N, axes[1], dtypes[1])):
+        if d == "int8":
+            q, s = ints(rows, K, "gauss", g, 1), torch.rand(rows, generator=g, device="cuda")
+            args.append((q, 0, s))
+            want.append((q, s))
+            continue
+        x = torch.randn(rows, K, generator=g, device="cuda").to(dt(d))
+        x[rows // 2] = 0.0
+        x = x.t().contiguous() if axis else x
+        for pad in (0, 3):
+            x = torch.nn.functional.pad(x, (0, pad))[:, : x.shape[1]] if pad and rows % 2 else x
+        args.append((x, axis, None))
+        want.append(quant_definition(x, axis)[:2])
+    (a, ax, sa), (b, bx, sb) = args
+    bias = torch.randn(N, generator=g, device="cuda")
+    exact = sums(want[0][0], want[1][0]).float() * (want[0][1][:, None] * want[1][1][None, :])
+    for bv, out in ((None, "f32"), (bias, "bf16"), (None, "f16")):
+        w = exact if bv is None else exact + bv
+        got = peat_gpu.peat_product_i8(h, a, b, ax, bx, sa, sb, bv, dt(out))
+        assert same_bits(got, w.to(dt(out)))
+
+
+def test_product_passes_bad_values_on(peat_gpu, h):
+    """NaN and infinities make their row of the operand NaN, whichever kernel takes it."""
+    import torch
+    for M, K in ((5, 100), (300, 200), (300, 2000)):
+        x = torch.randn(M, K, generator=rng(1), device="cuda").to(torch.bfloat16)
+        w = torch.randn(260, K, generator=rng(2), device="cuda").to(torch.bfloat16)
+        x[M // 2, K - 1] = float("inf")
+        w[77, 0] = float("nan")
+        for axis in (0, 1):
+            u, v = (x, w) if axis == 0 else (x.t().contiguous(), w.t().contiguous())
+            y = torch.isnan(peat_gpu.peat_product_i8(h, u, v, axis, axis))
+            assert bool(y[M // 2].all()) and bool(y[:, 77].all()) and int(y.sum()) == M + 260 - 1
+
+
+def test_product_refusals(peat_gpu, h):
+    import torch
+    P, x, q = peat_gpu, torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, dtype=torch.int8, device="cuda")
+    for call in (lambda: P.peat_product_i8(h, q, x, 1), lambda: P.peat_product_i8(h, x, x, a_scale=x[0, :4].contiguous()),
+                 lambda: P.peat_product_i8(h, x, x[:, :7]), lambda: P.peat_product_i8(h, x, x, 0, 1),
+                 lambda: P.peat_product_i8_raw(h, x, x, torch.zeros(4, 5, device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        P.peat_product_i8(h, x.double(), x)
+    L, O = P.load(), P.ops.Operand8
+
+    def op(data=x.data_ptr(), rows=4, cols=8, ld=8, dtype=0, axis=0):
+        return O(data, None, rows, cols, ld, dtype, axis)
+
+    def call(a, b, t=0):
+        import ctypes
+        return L.peat_product_i8(h.ptr, None if a is None else ctypes.byref(a), None if b is None else ctypes.byref(b),
+                                 None, x.data_ptr(), 4, t, None)
+    assert call(op(), op()) == 0
+    for a, b, t in ((None, op(), 0), (op(rows=-1), op(), 0), (op(ld=7), op(), 0), (op(dtype=5), op(), 0),
+                    (op(axis=2), op(), 0), (op(q.data_ptr(), dtype=101, axis=1), op(), 0), (op(cols=7, ld=8), op(), 0),
+                    (op(data=None), op(), 0), (op(), op(), 100), (op(), op(), 3)):
+        assert call(a, b, t) == 1 and P.peat_last_error(h)
+    torch.cuda.synchronize()
