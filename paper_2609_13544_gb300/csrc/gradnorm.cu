@@ -14,8 +14,10 @@
 // counts.
 //
 // Bound by memory: the norm reads the list once; clipping reads it again and
-// writes it, in the opposite order, so that what the norm read last is still
-// in L2.
+// writes it, each warp's share from its end, so that what the norm read last is
+// still in L2.
+#include <algorithm>
+
 #include "ops_internal.h"
 #include "peat_internal.h"
 #include "vec16.cuh"
@@ -132,10 +134,7 @@ __device__ GnPartial piece(const Span& s, int64_t j0, int64_t j1) {
     if (lane == 1) take(edge_unit<DT>(s, je - 1));
     je--;
   }
-  for (; j + 32 * U <= je; j += 32 * U) {
-    uint4 u[U];
-#pragma unroll
-    for (int i = 0; i < U; i++) u[i] = __ldcg(v + j + 32 * i + lane);
+  auto batch = [&](const uint4 (&u)[U]) {
     float a = 0.0f, b = 0.0f;
 #pragma unroll
     for (int i = 0; i < U; i += 2) {
@@ -145,8 +144,21 @@ __device__ GnPartial piece(const Span& s, int64_t j0, int64_t j1) {
       else a += unit_sum<DT, NORM>(u[i]), b += unit_sum<DT, NORM>(u[i + 1]);
     }
     if (NORM != PEAT_NORM_INF) sum.add(a + b);
+  };
+  uint4 u[U];
+  for (; j + 32 * U <= je; j += 32 * U) {
+#pragma unroll
+    for (int i = 0; i < U; i++) u[i] = __ldcg(v + j + 32 * i + lane);
+    batch(u);
   }
-  for (j += lane; j < je; j += 32) take(__ldcg(v + j));
+  if (j < je) {  // the rest, its loads under way at once too; zeros past the end change nothing
+#pragma unroll
+    for (int i = 0; i < U; i++) {
+      u[i] = make_uint4(0, 0, 0, 0);
+      if (j + 32 * i + lane < je) u[i] = __ldcg(v + j + 32 * i + lane);
+    }
+    batch(u);
+  }
   GnPartial r;
   r.bad = 0;
   any = __reduce_or_sync(0xffffffffu, any);
@@ -209,13 +221,16 @@ __device__ GnPartial piece_of(const GnEntry& e, int64_t j0, int64_t j1) {
   return piece<PEAT_BF16, NORM>(s, j0, j1);
 }
 
-// the last tensor whose units start at or before u (one with units, for u below the total)
+// the last tensor whose units start at or before u (one with units, for u
+// below the total), by a warp: 32 tensors are looked at together
 __device__ __forceinline__ int find_tensor(const GnEntry* list, int count, int64_t u) {
-  int lo = 0, hi = count - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (list[mid].unit0 <= u) lo = mid;
-    else hi = mid - 1;
+  int lo = 0, n = count;  // it is one of [lo, lo + n)
+  while (n > 1) {
+    const int step = (n + 31) / 32, at = lo + step * (threadIdx.x & 31);
+    const uint32_t before = __ballot_sync(0xffffffffu, at < lo + n && list[min(at, count - 1)].unit0 <= u);
+    const int k = 31 - __clz(before);  // (lane 0's is)
+    n = min(step, lo + n - (lo + k * step));
+    lo += k * step;
   }
   return lo;
 }
@@ -324,14 +339,15 @@ __device__ __forceinline__ void pieces_of(const GnParams& p, const GnEntry* list
   for (int t = find_tensor(list, p.count, u); u < end; t++) {
     const GnEntry e = list[t];
     const int64_t next = t + 1 < p.count ? list[t + 1].unit0 : p.units, stop = min(end, next);
-    if (stop <= u) continue;
-    const GnPartial r = piece_of<NORM>(e, u - e.unit0, stop - e.unit0);
-    u = stop;
-    if (e.unit0 >= begin && next <= end) {
+    const int64_t data = e.unit0 + p.lead, from = max(u, data);
+    u = max(u, stop);
+    if (stop <= from) continue;
+    const GnPartial r = piece_of<NORM>(e, from - data, stop - data);
+    if (data >= begin && next <= end) {
       if (lane == 0) p.sums[t] = r;
       continue;
     }
-    const int64_t w0 = owner<int64_t>(e.unit0, p.nwarps, p.units), w1 = owner<int64_t>(next - 1, p.nwarps, p.units);
+    const int64_t w0 = owner<int64_t>(data, p.nwarps, p.units), w1 = owner<int64_t>(next - 1, p.nwarps, p.units);
     unsigned int n = 0;
     if (lane == 0) {
       p.parts[t + w] = r;
@@ -354,8 +370,8 @@ __device__ __forceinline__ GnPartial load_sum(const GnPartial* q) {
   return r;
 }
 
-template <int NORM>
-__global__ void __launch_bounds__(GB) gn_norm(GnParams p, const __grid_constant__ GnInline in) {
+template <int NORM, typename IN>
+__global__ void __launch_bounds__(GB, 5) gn_norm(GnParams p, const __grid_constant__ IN in) {
   pdl_wait();
   pdl_trigger();
   const GnEntry* list = p.list ? p.list : in.e;
@@ -369,7 +385,7 @@ __global__ void __launch_bounds__(GB) gn_norm(GnParams p, const __grid_constant_
   __threadfence();
   finish<NORM, GB>(p, [&](int t) {
     const int64_t next = t + 1 < p.count ? list[t + 1].unit0 : p.units;
-    return next > list[t].unit0 ? load_sum(p.sums + t) : GnPartial{0.0, 0ull};  // (an empty tensor has no sum)
+    return next > list[t].unit0 + p.lead ? load_sum(p.sums + t) : GnPartial{0.0, 0ull};  // (an empty tensor has no sum)
   });
   if (threadIdx.x == 0) *p.done = 0;
 }
@@ -414,15 +430,16 @@ __device__ void scale_piece(const GnEntry& e, int64_t j0, int64_t j1, float f, b
       if (lane == 1) put_elements<DT>(s, out, je - 1, scaled<DT>(edge_unit<DT>(s, je - 1), f, zero));
       je--;
     }
+    // last units first: they are what the norm pass read last, and the first to be found in L2
     uint4* o = reinterpret_cast<uint4*>(out);
-    for (; j + 32 * U <= je; j += 32 * U) {
+    for (int64_t k = je - 1 - lane; k + lane >= j; k -= 32 * U) {
       uint4 u[U];
 #pragma unroll
-      for (int i = 0; i < U; i++) u[i] = __ldcg(v + j + 32 * i + lane);
+      for (int i = 0; i < U; i++) u[i] = k - 32 * i >= j ? __ldcs(v + k - 32 * i) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-      for (int i = 0; i < U; i++) __stcs(o + j + 32 * i + lane, scaled<DT>(u[i], f, zero));
+      for (int i = 0; i < U; i++)
+        if (k - 32 * i >= j) __stcs(o + k - 32 * i, scaled<DT>(u[i], f, zero));
     }
-    for (j += lane; j < je; j += 32) __stcs(o + j, scaled<DT>(__ldcg(v + j), f, zero));
   } else {
     for (j += lane; j < je; j += 32) put_elements<DT>(s, out, j, scaled<DT>(edge_unit<DT>(s, j), f, zero));
   }
@@ -431,29 +448,29 @@ __device__ void scale_piece(const GnEntry& e, int64_t j0, int64_t j1, float f, b
 // warp w's share of n of the list, scaled by f (or set to zero)
 template <typename I>
 __device__ __forceinline__ void scale_share(const GnParams& p, const GnEntry* list, I w, I n, float f, bool zero) {
-  int64_t u = first_unit<I>(w, n, (I)p.units);
-  const int64_t end = first_unit<I>(w + 1, n, (I)p.units);
+  const int64_t u = first_unit<I>(w, n, (I)p.units);
+  int64_t end = first_unit<I>(w + 1, n, (I)p.units);
   if (u >= end) return;
-  for (int t = find_tensor(list, p.count, u); u < end; t++) {
+  for (int t = find_tensor(list, p.count, end - 1); end > u; t--) {
     const GnEntry e = list[t];
-    const int64_t stop = min(end, t + 1 < p.count ? list[t + 1].unit0 : p.units);
-    if (stop <= u) continue;
-    if (!(f == 1.0f && !zero && e.out == e.g)) {
-      if (e.dtype == PEAT_F32) scale_piece<PEAT_F32>(e, u - e.unit0, stop - e.unit0, f, zero);
-      else if (e.dtype == PEAT_F16) scale_piece<PEAT_F16>(e, u - e.unit0, stop - e.unit0, f, zero);
-      else scale_piece<PEAT_BF16>(e, u - e.unit0, stop - e.unit0, f, zero);
+    const int64_t data = e.unit0 + p.lead, start = max(u, data);
+    if (start < end && !(f == 1.0f && !zero && e.out == e.g)) {
+      if (e.dtype == PEAT_F32) scale_piece<PEAT_F32>(e, start - data, end - data, f, zero);
+      else if (e.dtype == PEAT_F16) scale_piece<PEAT_F16>(e, start - data, end - data, f, zero);
+      else scale_piece<PEAT_BF16>(e, start - data, end - data, f, zero);
     }
-    u = stop;
+    end = min(end, max(u, e.unit0));
   }
 }
-__global__ void __launch_bounds__(GB) gn_scale(GnParams p, const __grid_constant__ GnInline in) {
+template <typename IN>
+__global__ void __launch_bounds__(GB) gn_scale(GnParams p, const __grid_constant__ IN in) {
   pdl_wait();
   pdl_trigger();
   const GnEntry* list = p.list ? p.list : in.e;
   const int64_t n = (int64_t)gridDim.x * (GB / 32);
   const float f = __fmul_rn(p.unscale, __ldcg(&p.result->coef));
   const bool zero = p.bad_mode == PEAT_BAD_ZERO && __ldcg(&p.result->n_bad) != 0;
-  scale_share<int64_t>(p, list, n - 1 - ((int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5)), n, f, zero);
+  scale_share<int64_t>(p, list, (int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5), n, f, zero);
 }
 
 // A small list by one CTA, norm and clipping in one launch: a launch and the
@@ -504,14 +521,29 @@ __global__ void __launch_bounds__(GB_SMALL) gn_small(GnParams p, const __grid_co
 
 int gn_block() { return GB; }
 
-cudaError_t launch_gradnorm(const GnParams& p, const GnInline& in, int nctas, cudaStream_t s) {
-  auto kernel = p.type == PEAT_NORM_1 ? gn_norm<PEAT_NORM_1>
-                                      : (p.type == PEAT_NORM_INF ? gn_norm<PEAT_NORM_INF> : gn_norm<PEAT_NORM_2>);
+template <typename IN>
+static cudaError_t norm_and_scale(const GnParams& p, const IN& in, int nctas, cudaStream_t s) {
+  auto kernel = p.type == PEAT_NORM_1
+                    ? gn_norm<PEAT_NORM_1, IN>
+                    : (p.type == PEAT_NORM_INF ? gn_norm<PEAT_NORM_INF, IN> : gn_norm<PEAT_NORM_2, IN>);
   cudaError_t e = launch_dependent(kernel, (unsigned)nctas, GB, 0, s, p, in);
-  if (e == cudaSuccess && p.clip && p.units > 0) e = launch_dependent(gn_scale, (unsigned)nctas, GB, 0, s, p, in);
+  if (e == cudaSuccess && p.clip && p.units > 0) e = launch_dependent(gn_scale<IN>, (unsigned)nctas, GB, 0, s, p, in);
   return e;
 }
-cudaError_t launch_gradnorm_small(const GnParams& p, const GnInline& in, cudaStream_t s) {
+cudaError_t launch_gradnorm(const GnParams& p, const GnEntry* host, int nctas, cudaStream_t s) {
+  if (p.list) return norm_and_scale(p, GnInlineOf<1>{}, nctas, s);
+  if (p.count <= GN_INLINE) {
+    GnInline in;
+    std::copy(host, host + p.count, in.e);
+    return norm_and_scale(p, in, nctas, s);
+  }
+  GnInlineOf<GN_INLINE_MOST> in;
+  std::copy(host, host + p.count, in.e);
+  return norm_and_scale(p, in, nctas, s);
+}
+cudaError_t launch_gradnorm_small(const GnParams& p, const GnEntry* host, cudaStream_t s) {
+  GnInline in;
+  std::copy(host, host + p.count, in.e);
   auto kernel = p.type == PEAT_NORM_1 ? gn_small<PEAT_NORM_1>
                                       : (p.type == PEAT_NORM_INF ? gn_small<PEAT_NORM_INF> : gn_small<PEAT_NORM_2>);
   return launch_dependent(kernel, 1, GB_SMALL, 0, s, p, in);

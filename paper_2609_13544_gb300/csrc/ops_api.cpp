@@ -333,19 +333,23 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   peat_status_t ps = ops_state(h, &s);
   if (ps != PEAT_OK) return ps;
 
+  const bool small = count <= peat::GN_INLINE && units <= peat::GN_SMALL;
+  // a piece's own time is about that of 256 units
+  const int64_t lead = small ? 0 : 256;
+  for (int64_t t = 0; t < count; t++) units += list[t].n > 0 ? lead : 0;
   // one wave; a warp has at least 64 units
   const int per = peat::gn_block() / 32;
-  const int64_t warps = std::max<int64_t>(1, std::min<int64_t>((units + 63) / 64, (int64_t)h->nsm * 4 * per));
+  const int64_t warps = std::max<int64_t>(1, std::min<int64_t>((units + 63) / 64, (int64_t)h->nsm * 5 * per));
   const int nctas = (int)((warps + per - 1) / per);
-  const size_t listed = count > peat::GN_INLINE ? (sizeof(peat::GnEntry) * (size_t)count + 255) / 256 * 256 : 0;
+  const size_t listed = count > peat::GN_INLINE_MOST ? (sizeof(peat::GnEntry) * (size_t)count + 255) / 256 * 256 : 0;
   const size_t parted = sizeof(peat::GnPartial) * (size_t)(count + warps);
   ps = grow(h, &s->d_list, &s->d_list_cap, listed + parted + sizeof(peat::GnPartial) * (size_t)count);
   if (ps != PEAT_OK) return ps;
   ps = tickets(h, s, (size_t)count, st);
   if (ps != PEAT_OK) return ps;
 
-  peat::GnInline in;
-  peat::GnEntry* dst = in.e;
+  peat::GnEntry inline_list[peat::GN_INLINE_MOST];
+  peat::GnEntry* dst = inline_list;
   int slot = -1;
   if (listed) {
     slot = s->next;
@@ -377,7 +381,7 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   for (int64_t t = 0; t < count; t++) {
     const peat_grad_t& e = list[t];
     dst[t] = peat::GnEntry{e.g, e.out, e.n, units, e.dtype, 0};
-    units += peat::gn_units(e.g, e.n, type_bytes(e.dtype));
+    units += peat::gn_units(e.g, e.n, type_bytes(e.dtype)) + (e.n > 0 ? lead : 0);
   }
   if (listed) {
     cudaError_t e = cudaMemcpyAsync(s->d_list, dst, sizeof(peat::GnEntry) * (size_t)count, cudaMemcpyHostToDevice, st);
@@ -403,8 +407,9 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   p.done = s->done;
   p.result = result;
   p.norms = norms;
-  cudaError_t e = !listed && units <= peat::GN_SMALL ? peat::launch_gradnorm_small(p, in, st)
-                                                     : peat::launch_gradnorm(p, in, nctas, st);
+  p.lead = lead;
+  cudaError_t e = small ? peat::launch_gradnorm_small(p, inline_list, st)
+                        : peat::launch_gradnorm(p, inline_list, nctas, st);
   if (e != cudaSuccess) return cuda_fail(h, e, "gradient norm launch");
   return PEAT_OK;
 }

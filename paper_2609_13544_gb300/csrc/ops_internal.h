@@ -71,21 +71,26 @@ struct GnEntry {
   const void* g;
   void* out;
   int64_t n;
-  int64_t unit0;  // the list's 16-byte units before this tensor's
+  int64_t unit0;  // the list's 16-byte units before this tensor's (each tensor that has any leads with GnParams::lead empty ones)
   int32_t dtype, pad;
 };
-constexpr int GN_INLINE = 96;  // entries that travel as a kernel argument (40 bytes each, below 4 KB)
-struct GnInline {
-  GnEntry e[GN_INLINE];
+// Entries that travel as a kernel argument, which takes up to 32 764 bytes: a
+// list in memory would first have to be copied there (4 us).
+constexpr int GN_INLINE = 96, GN_INLINE_MOST = 800;
+template <int N>
+struct GnInlineOf {
+  GnEntry e[N];
 };
+using GnInline = GnInlineOf<GN_INLINE>;
 struct GnPartial {
   double s;                // sum (or maximum)
   unsigned long long bad;  // NaN and infinite elements
 };
 struct GnParams {
-  const GnEntry* list;  // device; null: the inline entries
+  const GnEntry* list;  // device; null: the entries are a kernel argument
   int count;
   int64_t units;        // of the whole list
+  int64_t lead;         // empty units before each tensor's: what a piece costs beside its bytes
   int nwarps;           // warps of the norm pass
   int type;             // peat_norm_t
   float unscale, max_norm, eps;
@@ -99,10 +104,11 @@ struct GnParams {
   float* norms;         // or null
 };
 int gn_block();  // threads of a CTA of both passes
-cudaError_t launch_gradnorm(const GnParams& p, const GnInline& in, int nctas, cudaStream_t s);
-// the whole call in one CTA, for an inline list of at most GN_SMALL units
+// host: the entries, where p.list is null
+cudaError_t launch_gradnorm(const GnParams& p, const GnEntry* host, int nctas, cudaStream_t s);
+// the whole call in one CTA, for at most GN_INLINE tensors and GN_SMALL units (lead 0)
 constexpr int64_t GN_SMALL = 8192;
-cudaError_t launch_gradnorm_small(const GnParams& p, const GnInline& in, cudaStream_t s);
+cudaError_t launch_gradnorm_small(const GnParams& p, const GnEntry* host, cudaStream_t s);
 // 16-byte units that hold the n elements of `size` bytes at g
 inline int64_t gn_units(const void* g, int64_t n, int size) {
   if (n <= 0) return 0;
