@@ -10,6 +10,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "mm8_common.cuh"
 #include "peat_internal.h"
@@ -271,6 +272,8 @@ __global__ void __launch_bounds__(TT, 2) mm8_tiles(Mm8Params p, int ntw) {
       }
     }
   };
+  __shared__ float sas[TA];  // the rows' scales
+  if (threadIdx.x < TA) sas[threadIdx.x] = p.sa && m0 + threadIdx.x < p.M ? __ldg(p.sa + m0 + threadIdx.x) : 1.0f;
   float c[8][4];
   int sum[8][4];
 #pragma unroll
@@ -336,13 +339,17 @@ __global__ void __launch_bounds__(TT, 2) mm8_tiles(Mm8Params p, int ntw) {
   const int64_t n = n0 + col;
   if (n < p.N) {
     const float sb = p.sb ? __ldg(p.sb + n) : 1.0f, bias = p.bias ? __ldg(p.bias + n) : 0.0f;
-    for (int row = rank * 2 + (threadIdx.x >> 7); row < TA; row += 2 * S) {
-      const int64_t m = m0 + row;
-      if (m >= p.M) break;
-      int v = 0;
-      for (int k = 0; k < S; k++) v += *cl.map_shared_rank(&tot[row * P + col], k);
-      const float s = (p.sa ? __ldg(p.sa + m) : 1.0f) * sb;
-      out[m * p.ldo + n] = Mm8Out<OUT>::make(v, s, bias);
+    const int rows = (int)min((int64_t)TA, p.M - m0), row0 = rank * 2 + (threadIdx.x >> 7);
+    if (S == 1) {
+#pragma unroll 8
+      for (int row = row0; row < rows; row += 2)
+        out[(m0 + row) * p.ldo + n] = Mm8Out<OUT>::make(tot[row * P + col], sas[row] * sb, bias);
+    } else {
+      for (int row = row0; row < rows; row += 2 * S) {
+        int v = 0;
+        for (int k = 0; k < S; k++) v += *cl.map_shared_rank(&tot[row * P + col], k);
+        out[(m0 + row) * p.ldo + n] = Mm8Out<OUT>::make(v, sas[row] * sb, bias);
+      }
     }
   }
   cl.sync();  // the others may still read this CTA's sums
@@ -364,6 +371,13 @@ cudaError_t cluster_launch(F kernel, int64_t tiles, int S, int threads, int smem
   cfg.attrs = at;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// parts of the k range of a tile: until the SMs have two each, 8 runs of 64 k or more to start from
+int tile_parts(int64_t tiles, int64_t runs, int nsm) {
+  int S = 1;
+  while (S < 8 && tiles * S < 2 * (int64_t)nsm && runs >= 8 * S) S *= 2;
+  return S;
 }
 
 template <int OUT, int NT, int MODE>
@@ -395,8 +409,11 @@ cudaError_t direct(const Mm8Params& p, int nsm, cudaStream_t s) {
     return cluster_launch(mm8_rows<OUT, 2, MODE>, tiles, S, RT, 0, s, p);
   }
   const int64_t ntw = (p.N + TW - 1) / TW, tiles = ntw * ((p.M + TA - 1) / TA);
-  int S = 1;
-  while (S < 8 && tiles * S < 2 * (int64_t)nsm && runs >= 8 * S) S *= 2;
+  const int S = tile_parts(tiles, runs, nsm);
+  // (with the static part a little above the 48 KB that need no leave)
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = allow_smem(mm8_tiles<OUT, MODE>, T_SMEM, allowed);
+  if (e != cudaSuccess) return e;
   return cluster_launch(mm8_tiles<OUT, MODE>, tiles, S, TT, T_SMEM, s, p, (int)ntw);
 }
 
@@ -408,6 +425,16 @@ cudaError_t direct_out(const Mm8Params& p, int nsm, cudaStream_t s) {
 }
 
 }  // namespace
+
+// Microseconds of a call, fitted to those measured for M from 32 to 1024, N to
+// 16 384 and K to 16 384: one run of 64 k of a tile takes 0.8, an SM's CTAs share it.
+double mm8_direct_time(int64_t M, int64_t N, int64_t K, int nsm) {
+  if (M <= 16 || (M <= 64 && N >= MM8_STREAM_N)) return 0.0;  // bound by b's bytes: nothing is faster
+  const int64_t tiles = ((N + TW - 1) / TW) * ((M + TA - 1) / TA), runs = (K + TK - 1) / TK;
+  const int S = tile_parts(tiles, runs, nsm);
+  const double share = std::max(1.0, 1.1 * (double)(tiles * S) / nsm);
+  return 6.5 + 0.8 * std::ceil((double)runs / S) * share;
+}
 
 cudaError_t launch_mm8_direct(int out_dtype, const Mm8Params& p, int nsm, cudaStream_t s) {
   switch (out_dtype) {

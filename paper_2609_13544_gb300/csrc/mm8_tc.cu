@@ -756,6 +756,15 @@ Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm) {
   return r;
 }
 
+// Microseconds of a call, fitted as mm8_direct_time is: a fixed time, the waves'
+// blocks, the meeting of parts, and packing beyond what the fixed time hides.
+double mm8_tc_time(const Mm8TcPlan& p, int64_t K, int nsm) {
+  const int64_t tiles = p.mt * p.nt, at_once = p.splits == 1 ? nsm / 2 : (p.splits == 2 ? nsm / 4 - 1 : nsm / 10);
+  const double waves = (double)((tiles + at_once - 1) / at_once);
+  return 10.5 + 0.27 * waves * ((double)p.kb / p.splits) + (p.splits > 1 ? 2.0 : 0.0) + (K > FREE_K ? 2.5 : 0.0) +
+         std::max(0.0, (double)(p.mt + p.nt) * 256 * K * 3 / 5e6 - 3.0);
+}
+
 cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* status,
                           unsigned int wait_limit, int nsm, cudaStream_t s) {
   PackParams k;

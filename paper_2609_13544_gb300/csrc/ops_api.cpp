@@ -217,10 +217,10 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
     return fail(h, PEAT_ERR_TIMEOUT,
                 "a bounded device-side wait expired in an earlier call on this handle; its outputs are invalid");
   }
-  const bool wide = M >= 192 && N >= 128 && K >= 128;
   const peat::Mm8TcPlan plan = peat::mm8_tc_plan(M, N, K, h->nsm);
   // the packed blocks' rows are 32-bit coordinates
   const bool fits = (plan.mt + plan.nt) * 2 * plan.kb < ((int64_t)1 << 24);
+  const bool wide = K > 0 && peat::mm8_tc_time(plan, K, h->nsm) < peat::mm8_direct_time(M, N, K, h->nsm);
   cudaError_t e;
   if (wide && fits) {
     OpsState* s = nullptr;

@@ -62,7 +62,9 @@ struct Mm8TcPlan {
   int splits;      // parts of a tile's k range: 1, 2 or 4
   size_t a_off, b_off, na_off, nb_off, sum_off, bytes;  // workspace
 };
+double mm8_direct_time(int64_t M, int64_t N, int64_t K, int nsm);  // expected microseconds
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm);
+double mm8_tc_time(const Mm8TcPlan& p, int64_t K, int nsm);
 cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, unsigned int* status,
                           unsigned int wait_limit, int nsm, cudaStream_t s);
 
