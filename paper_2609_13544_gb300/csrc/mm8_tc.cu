@@ -18,9 +18,10 @@
 // memory.
 //
 // Exactness: float32 holds a sum of products exactly while it stays below
-// 2^24.  pack leaves for every block of 128 rows and 256 k the largest 2-norm
-// of a row; by Cauchy and Schwarz the product of two such norms bounds every
-// partial sum over those 256 k, and the accumulator is drained to int32
+// 2^24.  pack (or the quantiser that writes the blocks itself) leaves for every
+// block of 128 rows and 256 k the largest sum of squares of a row, in one word
+// or as one for each half; by Cauchy and Schwarz the product of two roots
+// bounds every partial sum over those 256 k, and the accumulator is drained to int32
 // before the bounds add up to more than 2^24.  Full-range integers drain every
 // 768 k, normally distributed ones about every 16 000; up to 1024 k nothing can
 // add up to more, and no norms are made.
@@ -54,7 +55,7 @@ struct PackParams {
   const int8_t* x[2];
   int64_t ld[2], rows[2];
   __half* out[2];
-  float* norm[2];
+  unsigned int* norm[2];
   int64_t K;
   int kb, kc;        // blocks of 64 and 256 k
   int64_t first_b;   // CTAs of the first matrix
@@ -121,7 +122,7 @@ __global__ void __launch_bounds__(256) mm8_pack(PackParams p) {
   if (threadIdx.x == 0) {
 #pragma unroll
     for (int w = 1; w < 8; w++) most = max(most, part[w]);
-    (which ? p.norm[1] : p.norm[0])[rb * p.kc + kc] = sqrtf((float)most) * 1.00001f;  // (rounded up)
+    reinterpret_cast<uint2*>(which ? p.norm[1] : p.norm[0])[rb * p.kc + kc] = make_uint2((unsigned)most, 0u);
   }
 }
 
@@ -149,8 +150,9 @@ constexpr float LIMIT = 16777216.0f;  // 2^24
 
 struct TcParams {
   Mm8Params m;
-  const float* na;  // norms [row blocks][kc]
-  const float* nb;
+  const uint2* na;  // sums of squares [row blocks][kc]
+  const uint2* nb;
+  int scales_late;  // the scales may come from the kernel before this one
   int kb, kc;
   int mt, nt;       // tiles
   int splits;       // parts of the k range of a tile: 1, 2 or 4; split tiles have a cluster each
@@ -381,16 +383,19 @@ __device__ __forceinline__ void plan_scales(const TcParams& p, const Place& t, S
 // a tile's place and drains into its slot, by a warp
 __device__ void plan_drains(const TcParams& p, const Place& t, Slot* slot) {
   const int lane = threadIdx.x & 31;
-  const float* na = p.na + (int64_t)t.mt * 2 * p.kc;
-  const float* nb = p.nb + (int64_t)t.nt * 2 * p.kc;
+  const uint2* na = p.na + (int64_t)t.mt * 2 * p.kc;
+  const uint2* nb = p.nb + (int64_t)t.nt * 2 * p.kc;
   int pieces = 1;
   float run = 0.0f;  // the bound of what the accumulator holds
   if (p.m.K <= FREE_K && lane == 0) slot->drain[0] = 0;
   for (int c0 = t.k0 / 4, w = 0; p.m.K > FREE_K && c0 * 4 < t.k1; c0 += 32, w++) {
     const int c = c0 + lane;
     float mine = 0.0f;
-    if (c * 4 < t.k1)
-      mine = fmaxf(__ldcg(na + c), __ldcg(na + p.kc + c)) * fmaxf(__ldcg(nb + c), __ldcg(nb + p.kc + c));
+    if (c * 4 < t.k1) {
+      const uint2 a0 = __ldcg(na + c), a1 = __ldcg(na + p.kc + c), b0 = __ldcg(nb + c), b1 = __ldcg(nb + p.kc + c);
+      const unsigned a = max(a0.x + a0.y, a1.x + a1.y), b = max(b0.x + b0.y, b1.x + b1.y);
+      mine = sqrtf((float)a) * sqrtf((float)b) * 1.00001f;  // (rounded up)
+    }
     float all = mine;
 #pragma unroll
     for (int o = 16; o; o /= 2) all += __shfl_xor_sync(0xffffffffu, all, o);
@@ -479,8 +484,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       ok = mbar_wait(unplanned + 8 * (i % SLOTS), (i / SLOTS & 1) ^ 1, p.wait_limit);
       if (!ok) break;
       const Place t = place_of(p, u, part);
-      // (the scales are not pack's: what is older than pack was complete before
-      // it let this kernel start)
+      // (where the kernel before is pack, the scales are older: complete before
+      // pack let this kernel start)
+      if (i == 0 && p.scales_late) pdl_wait();
       plan_scales(p, t, slots + i % SLOTS);
       if (i == 0) pdl_wait();
       plan_drains(p, t, slots + i % SLOTS);
@@ -745,11 +751,8 @@ Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm) {
   at += up((size_t)r.mt * 2 * r.kb * BLK);
   r.b_off = at;
   at += up((size_t)r.nt * 2 * r.kb * BLK);
-  r.na_off = at;
-  at += up((size_t)r.mt * 2 * r.kc * sizeof(float));
-  r.nb_off = at;
-  at += up((size_t)r.nt * 2 * r.kc * sizeof(float));
-  r.bytes = at;
+  r.na_words = K > FREE_K ? r.mt * 2 * r.kc * 2 : 0;
+  r.nb_words = K > FREE_K ? r.nt * 2 * r.kc * 2 : 0;
   r.sum_off = at;
   if (K > FREE_K) at += (size_t)(r.splits > 1 ? tiles * 2 * r.splits : nsm) * (128 * 256 * sizeof(int));
   r.bytes = at;
@@ -765,35 +768,41 @@ double mm8_tc_time(const Mm8TcPlan& p, int64_t K, int nsm) {
          std::max(0.0, (double)(p.mt + p.nt) * 256 * K * 3 / 5e6 - 3.0);
 }
 
-cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* status,
-                          unsigned int wait_limit, int nsm, cudaStream_t s) {
-  PackParams k;
-  k.x[0] = m.a;
-  k.x[1] = m.b;
-  k.ld[0] = m.lda;
-  k.ld[1] = m.ldb;
-  k.rows[0] = m.M;
-  k.rows[1] = m.N;
-  k.out[0] = reinterpret_cast<__half*>(ws + plan.a_off);
-  k.out[1] = reinterpret_cast<__half*>(ws + plan.b_off);
-  k.norm[0] = reinterpret_cast<float*>(ws + plan.na_off);
-  k.norm[1] = reinterpret_cast<float*>(ws + plan.nb_off);
-  k.K = m.K;
-  k.kb = plan.kb;
-  k.kc = plan.kc;
-  k.first_b = plan.mt * 2 * plan.kc;
-  const int64_t ctas = k.first_b + plan.nt * 2 * plan.kc;
-  const bool al = ((reinterpret_cast<uintptr_t>(m.a) | reinterpret_cast<uintptr_t>(m.b) | (uintptr_t)m.lda |
-                    (uintptr_t)m.ldb) & 15) == 0;
-  cudaError_t e = launch_dependent(al ? mm8_pack<16> : mm8_pack<1>, (unsigned)ctas, 256, 0, s, k);
-  if (e != cudaSuccess) return e;
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* norms,
+                          int packed, unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s) {
+  unsigned int* na = norms;
+  unsigned int* nb = norms + plan.na_words;
+  if (packed != 3) {
+    PackParams k;
+    k.x[0] = m.a;
+    k.x[1] = m.b;
+    k.ld[0] = m.lda;
+    k.ld[1] = m.ldb;
+    k.rows[0] = m.M;
+    k.rows[1] = m.N;
+    k.out[0] = reinterpret_cast<__half*>(ws + plan.a_off);
+    k.out[1] = reinterpret_cast<__half*>(ws + plan.b_off);
+    k.norm[0] = na;
+    k.norm[1] = nb;
+    k.K = m.K;
+    k.kb = plan.kb;
+    k.kc = plan.kc;
+    // (a matrix that is packed already has no CTAs)
+    k.first_b = packed & 1 ? 0 : plan.mt * 2 * plan.kc;
+    const int64_t ctas = k.first_b + (packed & 2 ? 0 : plan.nt * 2 * plan.kc);
+    const uintptr_t a = packed & 1 ? 0 : reinterpret_cast<uintptr_t>(m.a) | (uintptr_t)m.lda;
+    const uintptr_t b = packed & 2 ? 0 : reinterpret_cast<uintptr_t>(m.b) | (uintptr_t)m.ldb;
+    cudaError_t e = launch_dependent(((a | b) & 15) == 0 ? mm8_pack<16> : mm8_pack<1>, (unsigned)ctas, 256, 0, s, k);
+    if (e != cudaSuccess) return e;
+  }
   CUtensorMap ma, mb;
   if (!block_map(&ma, ws + plan.a_off, plan.mt * 2 * plan.kb) || !block_map(&mb, ws + plan.b_off, plan.nt * 2 * plan.kb))
     return cudaErrorNotSupported;
   TcParams p;
   p.m = m;
-  p.na = k.norm[0];
-  p.nb = k.norm[1];
+  p.na = reinterpret_cast<const uint2*>(na);
+  p.nb = reinterpret_cast<const uint2*>(nb);
+  p.scales_late = packed != 0;
   p.kb = plan.kb;
   p.kc = plan.kc;
   p.mt = (int)plan.mt;

@@ -36,6 +36,11 @@ struct OpsState {
   // operands that a product rounds, and their scales
   void* rounded = nullptr;
   size_t rounded_cap = 0;
+  // sums of squares of operands packed on the way: two buffers in turn
+  void* norms = nullptr;
+  size_t norms_cap = 0;  // bytes of both
+  int64_t norms_used[2] = {0, 0};
+  int norms_at = 0;
   // products: packed operands and partial sums
   void* mm = nullptr;
   size_t mm_cap = 0;
@@ -49,6 +54,7 @@ void ops_destroy(OpsState* s) {
   if (s->colmax) cudaFree(s->colmax);
   if (s->mm) cudaFree(s->mm);
   if (s->rounded) cudaFree(s->rounded);
+  if (s->norms) cudaFree(s->norms);
   for (int i = 0; i < OpsState::RING; i++) {
     if (s->h_list[i]) cudaFreeHost(s->h_list[i]);
     if (s->taken[i]) cudaEventDestroy(s->taken[i]);
@@ -110,8 +116,19 @@ peat_status_t tickets(peat_handle_t h, OpsState* s, size_t n, cudaStream_t st) {
   return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "cudaMemsetAsync(counters)");
 }
 
+// A packed operand as a quantisation's output: its place, and in the plan's norms.
+struct Packed {
+  void* blocks;
+  int kb, kc;
+  int64_t rows;
+  unsigned int* norms;
+  unsigned int* zero;
+  int64_t zero_n;
+  bool made;  // out: whether it was made (else the integers were asked for in q and stand there)
+};
 peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int axis,
-                       int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv, cudaStream_t st) {
+                       int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv, cudaStream_t st,
+                       Packed* packed = nullptr) {
   const int B = type_bytes(dtype);
   if (!B) return fail(h, PEAT_ERR_INVALID_ARG, "dtype must be PEAT_F32, PEAT_F16 or PEAT_BF16");
   if (axis != 0 && axis != 1) return fail(h, PEAT_ERR_INVALID_ARG, "axis must be 0 (rows) or 1 (columns)");
@@ -146,6 +163,17 @@ peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t col
   p.vec_v = values && aligned(values, 16) && (ldv % E == 0 || rows <= 1);
   p.colmax = p.zero = nullptr;
   p.zero_n = 0;
+  p.packed = nullptr;
+  if (packed) {
+    p.kb = packed->kb;
+    p.kc = packed->kc;
+    p.prows = packed->rows;
+    p.norms = packed->norms;
+    p.zero2 = packed->zero;
+    p.zero2_n = packed->zero_n;
+    packed->made = peat::quant8_packs(dtype, axis, p);
+    if (packed->made) p.packed = packed->blocks;
+  }
   OpsState* s = nullptr;
   cudaError_t e;
   if (axis == 1) {
@@ -179,56 +207,61 @@ peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t col
   return PEAT_OK;
 }
 
-peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb,
-                     const float* sb, const float* bias, int64_t M, int64_t N, int64_t K, void* out, int64_t ldo,
-                     int out_dtype, cudaStream_t st) {
+// checks of a product's output and inner size
+peat_status_t output_ok(peat_handle_t h, const float* sa, const float* sb, const float* bias, int64_t M, int64_t N,
+                        int64_t K, const void* out, int64_t ldo, int out_dtype) {
   const int B = out_dtype == PEAT_OUT_I32 ? 4 : type_bytes(out_dtype);
-  if (!B) return fail(h, PEAT_ERR_INVALID_ARG, "out_dtype must be PEAT_F32, PEAT_F16, PEAT_BF16 or PEAT_OUT_I32");
-  if (M < 0 || N < 0 || K < 0) return fail(h, PEAT_ERR_INVALID_ARG, "M, N or K < 0");
   if (K > 131071) return fail(h, PEAT_ERR_UNSUPPORTED, "K above 131071: the sums may not fit 32 bits");
-  if (lda < K || ldb < K || ldo < N) return fail(h, PEAT_ERR_INVALID_ARG, "lda, ldb or ldo is less than a row");
-  if (out_dtype == PEAT_OUT_I32 && (sa || sb || bias))
-    return fail(h, PEAT_ERR_INVALID_ARG, "PEAT_OUT_I32 takes no scales and no bias");
+  if (ldo < N) return fail(h, PEAT_ERR_INVALID_ARG, "ldo is less than a row");
   if (M == 0 || N == 0) return PEAT_OK;
   // tiles are counted in 32 bits
   if (M > MAX_DIM || N > MAX_DIM || ((M + 63) / 64) * ((N + 127) / 128) > ((int64_t)1 << 27))
     return fail(h, PEAT_ERR_UNSUPPORTED, "the output is too large for one call");
   if (!out) return fail(h, PEAT_ERR_INVALID_ARG, "out is NULL");
-  if (K > 0 && (!a || !b)) return fail(h, PEAT_ERR_INVALID_ARG, "a or b is NULL");
   if (!aligned(out, B) || (sa && !aligned(sa, 4)) || (sb && !aligned(sb, 4)) || (bias && !aligned(bias, 4)))
     return fail(h, PEAT_ERR_INVALID_ARG, "a pointer is not aligned to its element type");
-  DeviceGuard dg(h->device);
-  if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
-  peat::Mm8Params p;
-  p.a = a;
-  p.b = b;
-  p.lda = lda;
-  p.ldb = ldb;
-  p.sa = sa;
-  p.sb = sb;
-  p.bias = bias;
-  p.out = out;
-  p.ldo = ldo;
-  p.M = M;
-  p.N = N;
-  p.K = K;
   if (h->status_host && *(volatile unsigned int*)h->status_host) {
     *(volatile unsigned int*)h->status_host = 0;
     return fail(h, PEAT_ERR_TIMEOUT,
                 "a bounded device-side wait expired in an earlier call on this handle; its outputs are invalid");
   }
-  const peat::Mm8TcPlan plan = peat::mm8_tc_plan(M, N, K, h->nsm);
+  return PEAT_OK;
+}
+// whether the tensor-core path takes a product
+bool wide_product(peat_handle_t h, const peat::Mm8TcPlan& plan, int64_t M, int64_t N, int64_t K) {
   // the packed blocks' rows are 32-bit coordinates
   const bool fits = (plan.mt + plan.nt) * 2 * plan.kb < ((int64_t)1 << 24);
-  const bool wide = K > 0 && peat::mm8_tc_time(plan, K, h->nsm) < peat::mm8_direct_time(M, N, K, h->nsm);
+  return K > 0 && fits && peat::mm8_tc_time(plan, K, h->nsm) < peat::mm8_direct_time(M, N, K, h->nsm);
+}
+unsigned int wait_limit(peat_handle_t h) { return std::min(h->wait_limit, 1u << 22); }
+
+peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float* sa, const int8_t* b, int64_t ldb,
+                     const float* sb, const float* bias, int64_t M, int64_t N, int64_t K, void* out, int64_t ldo,
+                     int out_dtype, cudaStream_t st) {
+  if (out_dtype != PEAT_OUT_I32 && !type_bytes(out_dtype))
+    return fail(h, PEAT_ERR_INVALID_ARG, "out_dtype must be PEAT_F32, PEAT_F16, PEAT_BF16 or PEAT_OUT_I32");
+  if (M < 0 || N < 0 || K < 0) return fail(h, PEAT_ERR_INVALID_ARG, "M, N or K < 0");
+  if (lda < K || ldb < K) return fail(h, PEAT_ERR_INVALID_ARG, "lda or ldb is less than a row");
+  if (out_dtype == PEAT_OUT_I32 && (sa || sb || bias))
+    return fail(h, PEAT_ERR_INVALID_ARG, "PEAT_OUT_I32 takes no scales and no bias");
+  peat_status_t ps = output_ok(h, sa, sb, bias, M, N, K, out, ldo, out_dtype);
+  if (ps != PEAT_OK || M == 0 || N == 0) return ps;
+  if (K > 0 && (!a || !b)) return fail(h, PEAT_ERR_INVALID_ARG, "a or b is NULL");
+  DeviceGuard dg(h->device);
+  if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
+  const peat::Mm8Params p{a, b, lda, ldb, sa, sb, bias, out, ldo, M, N, K};
+  const peat::Mm8TcPlan plan = peat::mm8_tc_plan(M, N, K, h->nsm);
   cudaError_t e;
-  if (wide && fits) {
+  if (wide_product(h, plan, M, N, K)) {
     OpsState* s = nullptr;
-    peat_status_t ps = ops_state(h, &s);
-    if (ps == PEAT_OK) ps = grow(h, &s->mm, &s->mm_cap, plan.bytes);
+    ps = ops_state(h, &s);
+    const size_t norms = (plan.bytes + 255) / 256 * 256;
+    if (ps == PEAT_OK)
+      ps = grow(h, &s->mm, &s->mm_cap, norms + sizeof(unsigned int) * (size_t)(plan.na_words + plan.nb_words));
     if (ps != PEAT_OK) return ps;
-    const unsigned int limit = std::min(h->wait_limit, 1u << 22);
-    e = peat::launch_mm8_tc(out_dtype, p, plan, static_cast<char*>(s->mm), h->status_dev, limit, h->nsm, st);
+    char* ws = static_cast<char*>(s->mm);
+    e = peat::launch_mm8_tc(out_dtype, p, plan, ws, reinterpret_cast<unsigned int*>(ws + norms), 0, h->status_dev,
+                            wait_limit(h), h->nsm, st);
   } else {
     e = peat::launch_mm8_direct(out_dtype, p, h->nsm, st);
   }
@@ -274,27 +307,71 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
   size_t need = 0;
   Operand x = operand_of(*a, nullptr, &need), y = operand_of(*b, nullptr, &need);
   if (x.K != y.K) return fail(h, PEAT_ERR_INVALID_ARG, "the operands differ in K");
-  if (x.K > 131071) return fail(h, PEAT_ERR_UNSUPPORTED, "K above 131071: the sums may not fit 32 bits");
-  if (x.rows == 0 || y.rows == 0) return PEAT_OK;
+  const int64_t M = x.rows, N = y.rows, K = x.K;
+  peat_status_t ps = output_ok(h, x.scale, y.scale, bias, M, N, K, out, ldo, out_dtype);
+  if (ps != PEAT_OK || M == 0 || N == 0) return ps;
+  if (K > 0 && (!a->data || !b->data)) return fail(h, PEAT_ERR_INVALID_ARG, "an operand's data is NULL");
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
   OpsState* s = nullptr;
-  peat_status_t ps = ops_state(h, &s);
+  ps = ops_state(h, &s);
   if (ps == PEAT_OK) ps = grow(h, &s->rounded, &s->rounded_cap, need);
   if (ps != PEAT_OK) return ps;
-  char* ws = static_cast<char*>(s->rounded);
+  char* rounded = static_cast<char*>(s->rounded);
   size_t at = 0;
-  x = operand_of(*a, ws, &at);
-  y = operand_of(*b, ws, &at);
+  x = operand_of(*a, rounded, &at);
+  y = operand_of(*b, rounded, &at);
+  const peat::Mm8TcPlan plan = peat::mm8_tc_plan(M, N, K, h->nsm);
+  const bool wide = wide_product(h, plan, M, N, K);
+  char* ws = nullptr;
+  unsigned int *norms = nullptr, *stale = nullptr;
+  int64_t stale_n = 0;
+  const int64_t words = plan.na_words + plan.nb_words;
+  if (wide) {
+    ps = grow(h, &s->mm, &s->mm_cap, plan.bytes);
+    // the sums of squares: two buffers in turn, one cleared while the other is in use
+    const size_t both = 2 * sizeof(unsigned int) * (size_t)words;
+    if (ps == PEAT_OK && both > s->norms_cap) {
+      ps = grow(h, &s->norms, &s->norms_cap, both);
+      s->norms_used[0] = s->norms_used[1] = 0;
+      if (ps == PEAT_OK && cudaMemsetAsync(s->norms, 0, both, st) != cudaSuccess)
+        ps = cuda_fail(h, cudaGetLastError(), "cudaMemsetAsync(norms)");
+    }
+    if (ps != PEAT_OK) return ps;
+    ws = static_cast<char*>(s->mm);
+    if (words) {
+      const size_t half = s->norms_cap / 2 / sizeof(unsigned int);
+      norms = static_cast<unsigned int*>(s->norms) + s->norms_at * half;
+      stale = static_cast<unsigned int*>(s->norms) + (s->norms_at ^ 1) * half;
+      stale_n = s->norms_used[s->norms_at ^ 1];
+    }
+  }
   const peat_operand_t* in[2] = {a, b};
   const Operand* op[2] = {&x, &y};
+  int packed = 0;
   for (int i = 0; i < 2; i++) {
     if (in[i]->dtype == PEAT_INT8) continue;
+    Packed to{ws + (i ? plan.b_off : plan.a_off), plan.kb, plan.kc, (i ? plan.nt : plan.mt) * 256,
+              norms ? norms + (i ? plan.na_words : 0) : nullptr, stale, packed ? 0 : stale_n, false};
     ps = quantize(h, in[i]->data, in[i]->rows, in[i]->cols, in[i]->ld, in[i]->dtype, in[i]->axis,
-                  const_cast<int8_t*>(op[i]->q), op[i]->ld, const_cast<float*>(op[i]->scale), nullptr, 0, st);
-    if (ps != PEAT_OK) return ps;
+                  const_cast<int8_t*>(op[i]->q), op[i]->ld, const_cast<float*>(op[i]->scale), nullptr, 0, st,
+                  wide ? &to : nullptr);
+    if (ps != PEAT_OK) {
+      s->norms_cap = 0;  // (made anew by the next call)
+      return ps;
+    }
+    if (to.made) packed |= 1 << i;
   }
-  return matmul(h, x.q, x.ld, x.scale, y.q, y.ld, y.scale, bias, x.rows, y.rows, x.K, out, ldo, out_dtype, st);
+  if (!packed) return matmul(h, x.q, x.ld, x.scale, y.q, y.ld, y.scale, bias, M, N, K, out, ldo, out_dtype, st);
+  if (words) {
+    s->norms_used[s->norms_at] = words;
+    s->norms_used[s->norms_at ^ 1] = 0;
+    s->norms_at ^= 1;
+  }
+  const peat::Mm8Params p{x.q, y.q, x.ld, y.ld, x.scale, y.scale, bias, out, ldo, M, N, K};
+  cudaError_t e = peat::launch_mm8_tc(out_dtype, p, plan, ws, norms, packed, h->status_dev, wait_limit(h), h->nsm, st);
+  if (e != cudaSuccess) return cuda_fail(h, e, "8-bit product launch");
+  return PEAT_OK;
 }
 
 peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count, int type, float unscale, bool clip,

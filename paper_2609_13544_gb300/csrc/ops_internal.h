@@ -39,7 +39,16 @@ struct QuantParams {
   unsigned int* colmax;
   unsigned int* zero;
   int64_t zero_n;
+  // the integers as a product's packed operand (mm8_tc.cu) in place of q; null: not
+  void* packed;
+  int kb, kc;        // its blocks of 64 k, and of 256
+  int64_t prows;     // its rows, a multiple of 256
+  unsigned int* norms;  // its sums of squares, zero before (null: not needed)
+  unsigned int* zero2;  // those of an earlier call, cleared for a later one
+  int64_t zero2_n;
 };
+// whether a packed operand can be made (the matrix's rows lie on the vector grid, and fit a CTA's registers)
+bool quant8_packs(int dtype, int axis, const QuantParams& p);
 cudaError_t launch_quant8(int dtype, int axis, const QuantParams& p, int nsm, cudaStream_t s);
 
 // ---- 8-bit products (matmul8.cu) ----
@@ -60,13 +69,15 @@ struct Mm8TcPlan {
   int kb, kc;      // blocks of 64 k, and of 256
   int64_t mt, nt;  // tiles
   int splits;      // parts of a tile's k range: 1, 2 or 4
-  size_t a_off, b_off, na_off, nb_off, sum_off, bytes;  // workspace
+  size_t a_off, b_off, sum_off, bytes;  // workspace
+  int64_t na_words, nb_words;            // sums of squares of a's and of b's blocks (0: not needed)
 };
 double mm8_direct_time(int64_t M, int64_t N, int64_t K, int nsm);  // expected microseconds
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm);
 double mm8_tc_time(const Mm8TcPlan& p, int64_t K, int nsm);
-cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, unsigned int* status,
-                          unsigned int wait_limit, int nsm, cudaStream_t s);
+// norms: na_words, then nb_words; packed: bit 0 a, bit 1 b is packed already (its scales may be from the kernel before)
+cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, unsigned int* norms,
+                          int packed, unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s);
 
 // ---- gradient lists (gradnorm.cu) ----
 struct GnEntry {

@@ -234,6 +234,109 @@ __global__ void __launch_bounds__(QT) quant_rows(QuantParams p) {
   }
 }
 
+// where the integers of operand row `row`, k on, lie in a packed operand (see
+// mm8_tc.cu): 16 KB blocks of 128 rows by 64 k, 16-byte pieces of 8 k swizzled
+__device__ __forceinline__ char* packed_at(const QuantParams& p, int64_t row, int64_t k) {
+  const int r = (int)(row & 127);
+  return static_cast<char*>(p.packed) + ((row >> 7) * p.kb + (k >> 6)) * 16384 + r * 128 +
+         ((((int)k >> 3 & 7) ^ (r & 7)) * 16) + ((int)k & 7) * 2;
+}
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+  const __half2 h = __floats2half2_rn(number(a), number(b));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void clear_earlier(const QuantParams& p) {
+  const int64_t n = (int64_t)gridDim.x * gridDim.y * QT;
+  for (int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * QT + threadIdx.x; i < p.zero2_n; i += n) p.zero2[i] = 0;
+}
+
+// quant_rows with a packed operand for its output, zeros in its margins.  A
+// group of threads takes `each` rows one after another, the next one's vectors
+// on their way, and hands on the largest sums of squares of all of them.
+template <int DT, int TPR, int NV>
+__global__ void __launch_bounds__(QT) quant_rows_packed(QuantParams p, int each) {
+  using L = Elem<DT>;
+  pdl_wait();
+  pdl_trigger();
+  clear_earlier(p);
+  __shared__ uint32_t part[2][QT / 32];
+  const int lane = threadIdx.x % TPR;
+  const int64_t row0 = ((int64_t)blockIdx.x * (QT / TPR) + threadIdx.x / TPR) * each;
+  const bool ragged = p.cols % L::E != 0;
+  auto load = [&](int64_t row, uint4 (&v)[NV]) {
+    const bool real = row < p.rows;
+    const typename L::T* x = static_cast<const typename L::T*>(p.x) + row * p.ldx;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int64_t col = (int64_t)(i * TPR + lane) * L::E;
+      v[i] = make_uint4(0, 0, 0, 0);
+      if (real && col + L::E <= p.cols) v[i] = __ldg(reinterpret_cast<const uint4*>(x + col));
+    }
+    if (real && ragged) {  // the row's last vector
+#pragma unroll
+      for (int i = 0; i < NV; i++) {
+        const int64_t col = (int64_t)(i * TPR + lane) * L::E;
+        if (col < p.cols && col + L::E > p.cols) v[i] = load_vec<DT, false>(x + col, p.cols - col);
+      }
+    }
+  };
+  unsigned most[NV];
+#pragma unroll
+  for (int i = 0; i < NV; i++) most[i] = 0;
+  uint4 next[NV];
+  load(row0, next);
+  for (int it = 0; it < each; it++) {
+    const int64_t row = row0 + it;
+    uint4 v[NV];
+    uint4 m = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      v[i] = next[i];
+      m = mag_max<DT>(m, v[i]);
+    }
+    if (it + 1 < each) load(row + 1, next);
+    uint32_t top = __reduce_max_sync(0xffffffffu, mag_fold<DT>(m));
+    if (TPR > 32) {
+      if ((threadIdx.x & 31) == 0) part[it & 1][threadIdx.x >> 5] = top;
+      __syncthreads();
+      top = __reduce_max_sync(0xffffffffu, part[it & 1][threadIdx.x & (QT / 32 - 1)]);
+    }
+    float r, scale;
+    factors<DT>(top, r, scale);
+    const bool finite = top < L::INF;
+    if (lane == 0 && row < p.rows) p.scale[row] = scale;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int64_t k = (int64_t)(i * TPR + lane) * L::E;
+      float w[L::E];
+      if (finite) wholes<DT, true>(v[i], r, w);
+      else wholes<DT, false>(v[i], r, w);
+      if (k < (int64_t)p.kb * 64) {
+        char* d = packed_at(p, row, k);
+        if (L::E == 8)
+          *reinterpret_cast<uint4*>(d) = make_uint4(half_pair(w[0], w[1]), half_pair(w[2], w[3]), half_pair(w[4 % L::E], w[5 % L::E]),
+                                                    half_pair(w[6 % L::E], w[7 % L::E]));
+        else
+          *reinterpret_cast<uint2*>(d) = make_uint2(half_pair(w[0], w[1]), half_pair(w[2], w[3]));
+      }
+      if (p.norms) {  // a warp's vectors are 256 k, or half of them
+        float ss = 0.0f;  // (exact: below 2^17)
+#pragma unroll
+        for (int e = 0; e < L::E; e++) ss = fmaf(number(w[e]), number(w[e]), ss);
+        most[i] = max(most[i], __reduce_add_sync(0xffffffffu, (unsigned)ss));
+      }
+    }
+  }
+  if (p.norms && (threadIdx.x & 31) == 0) {
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int64_t first = (int64_t)(i * TPR + (lane & ~31)) * L::E;
+      if (first < (int64_t)p.kb * 64)
+        atomicMax(p.norms + (row0 >> 7) * p.kc * 2 + (L::E == 8 ? first / 256 * 2 : first / 128), most[i]);
+    }
+  }
+}
+
 // A row by a CTA, read twice: rows too long for the registers, and (VEC false) rows off the 16-byte grid,
 // which are taken element by element.
 template <int DT, bool VEC>
@@ -283,7 +386,7 @@ __global__ void __launch_bounds__(QT) quant_rows_twice(QuantParams p) {
 // integers transposed through shared memory, 128 contiguous ones of a column
 // at a time.  (One launch of clusters that keep a strip of columns to
 // themselves, meet in distributed shared memory and read the strip again from
-// L2 took 101 us for 16384 x 4096 bfloat16 values where these take CCC: its
+// L2 took 101 us for 16384 x 4096 bfloat16 values where these take 75: its
 // phases wait for each other.)
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(QT) quant_colmax(QuantParams p, int vl, int64_t rows_each) {
@@ -338,20 +441,24 @@ __global__ void __launch_bounds__(QT) quant_colmax(QuantParams p, int vl, int64_
 }
 
 constexpr int TR = 128;  // rows of a tile
-template <int DT, bool VEC>
-__global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_each) {
+template <int DT, bool VEC, bool PACK>
+__global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, int64_t rows_each) {
   using L = Elem<DT>;
   constexpr int CW = 8 * L::E;  // columns of a tile
   __shared__ __align__(16) float rs[CW], ss[CW];
   __shared__ uint32_t bads[2];
-  __shared__ uint32_t tile[CW][TR / 4 + 1];
+  __shared__ __align__(16) uint32_t tile[CW * (PACK ? TR / 2 : TR / 4 + 1)];  // integers: bytes, or packed binary16
+  __shared__ float squares[PACK ? QT / 32 : 1][CW];
   const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3;
   const int64_t c0 = (int64_t)blockIdx.x * CW, col = c0 + tx * L::E;
   const int64_t left = p.cols - col;  // may be <= 0
-  const int64_t r0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * rows_each, r1 = min(p.rows, r0 + rows_each);
+  // (a packed operand's k go on to a whole block: zeros)
+  const int64_t r0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * rows_each,
+                r1 = min(PACK ? (int64_t)p.kb * 64 : p.rows, r0 + rows_each);
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + col;
   pdl_wait();
   pdl_trigger();
+  if (PACK) clear_earlier(p);
   // the other buffer of maxima is the next call's: zero again
   {
     const int64_t n = (int64_t)gridDim.x * gridDim.y * QT;
@@ -359,14 +466,14 @@ __global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_
   }
   auto load = [&](int64_t t0, uint4 (&v)[4]) {
     const typename L::T* q = x + (t0 + ty * 4) * p.ldx;
-    if (VEC && left >= L::E && t0 + TR <= r1) {
+    if (VEC && left >= L::E && t0 + TR <= min(r1, p.rows)) {
 #pragma unroll
       for (int j = 0; j < 4; j++) v[j] = __ldg(reinterpret_cast<const uint4*>(q + j * p.ldx));
     } else {
 #pragma unroll
       for (int j = 0; j < 4; j++) {
         v[j] = make_uint4(0, 0, 0, 0);
-        if (t0 + ty * 4 + j < r1 && left > 0) v[j] = load_vec<DT, VEC>(q + j * p.ldx, left);
+        if (t0 + ty * 4 + j < min(r1, p.rows) && left > 0) v[j] = load_vec<DT, VEC>(q + j * p.ldx, left);
       }
     }
   };
@@ -406,7 +513,7 @@ __global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_
       }
     }
     if (t0 + TR < r1) load(t0 + TR, v);  // the next tile is on its way
-    if (p.values) {
+    if (!PACK && p.values) {
 #pragma unroll
       for (int j = 0; j < 4; j++) {
         const int64_t row = t0 + ty * 4 + j;
@@ -417,16 +524,54 @@ __global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_
         store_values<DT>(static_cast<typename L::T*>(p.values) + row * p.ldv + col, y, p.vec_v, left);
       }
     }
-    if (p.q) {
+    if constexpr (PACK) {
+      // k pairs of a column side by side, its 16-byte pieces swizzled by the
+      // thread column against bank conflicts; then 8 lanes write a row of a block
+      __syncthreads();  // the tile's last readers are done
+      char* bytes = reinterpret_cast<char*>(tile);
+#pragma unroll
+      for (int e = 0; e < L::E; e++)
+        *reinterpret_cast<uint2*>(bytes + (tx * L::E + e) * (TR * 2) + ((ty >> 1 ^ tx) * 16) + (ty & 1) * 8) =
+            make_uint2(half_pair(w[0][e], w[1][e]), half_pair(w[2][e], w[3][e]));
+      if (p.norms) {
+#pragma unroll
+        for (int e = 0; e < L::E; e++) {
+          float ss = 0.0f;
+#pragma unroll
+          for (int j = 0; j < 4; j++) ss = fmaf(number(w[j][e]), number(w[j][e]), ss);
+          ss += __shfl_xor_sync(0xffffffffu, ss, 8);
+          ss += __shfl_xor_sync(0xffffffffu, ss, 16);
+          if ((threadIdx.x & 31) < 8) squares[threadIdx.x >> 5][tx * L::E + e] = ss;
+        }
+      }
+      __syncthreads();
+      const int piece = threadIdx.x & 7;
+#pragma unroll
+      for (int i = threadIdx.x >> 3; i < CW * 2; i += QT / 8) {
+        const int c = i >> 1, block = i & 1;
+        const int64_t k = t0 + block * 64 + piece * 8;
+        if (k >= (int64_t)p.kb * 64) continue;
+        const uint4 u = *reinterpret_cast<const uint4*>(bytes + c * (TR * 2) + (block * 8 + (piece ^ (c / L::E))) * 16);
+        *reinterpret_cast<uint4*>(packed_at(p, c0 + c, k)) = u;
+      }
+      if (p.norms && threadIdx.x < CW) {  // (exact: below 2^22)
+        float ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < QT / 32; i++) ss += squares[i][threadIdx.x];
+        const unsigned most = __reduce_max_sync(0xffffffffu, (unsigned)ss);
+        if ((threadIdx.x & 31) == 0) atomicMax(p.norms + (c0 >> 7) * p.kc * 2 + t0 / 128, most);
+      }
+    } else if (p.q) {
+      constexpr int TP = TR / 4 + 1;
       __syncthreads();  // the tile's last readers are done
 #pragma unroll
-      for (int e = 0; e < L::E; e++) tile[tx * L::E + e][ty] = pack4(w[0][e], w[1][e], w[2][e], w[3][e]);
+      for (int e = 0; e < L::E; e++) tile[(tx * L::E + e) * TP + ty] = pack4(w[0][e], w[1][e], w[2][e], w[3][e]);
       __syncthreads();
       const int lane = threadIdx.x & 31;
       const int64_t row = t0 + lane * 4;
       for (int c = threadIdx.x >> 5; c < CW; c += QT / 32) {
         if (c0 + c >= p.cols || row >= p.rows) continue;
-        const uint32_t u = tile[c][lane];
+        const uint32_t u = tile[c * TP + lane];
         int8_t* q = p.q + (c0 + c) * p.ldq + row;
         if (p.vec_q && row + 4 <= p.rows) {
           *reinterpret_cast<uint32_t*>(q) = u;
@@ -441,13 +586,29 @@ __global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_
 }
 
 template <int DT>
-cudaError_t rows_launch(const QuantParams& p, cudaStream_t s) {
+cudaError_t rows_launch(const QuantParams& p, int nsm, cudaStream_t s) {
   constexpr int E = Elem<DT>::E;
   if (!p.vec_x) return launch_dependent(quant_rows_twice<DT, false>, (unsigned)p.rows, QT, 0, s, p);
   const int64_t nv = (p.cols + E - 1) / E;
   auto go = [&](void (*kernel)(QuantParams), int tpr) {
     return launch_dependent(kernel, (unsigned)((p.rows + QT / tpr - 1) / (QT / tpr)), QT, 0, s, p);
   };
+  if (p.packed) {
+    const int64_t pv = (int64_t)p.kb * 64 / E;
+    auto pack = [&](void (*kernel)(QuantParams, int), int tpr) {
+      const int64_t groups = p.prows / (QT / tpr);
+      int each = 1;  // rows of a thread group (of one block of 128): up to 8, while every SM has 4 CTAs
+      while (each < 8 && groups / (2 * each) >= 4 * nsm) each *= 2;
+      return launch_dependent(kernel, (unsigned)(groups / each), QT, 0, s, p, each);
+    };
+    if (pv <= 32) return pack(quant_rows_packed<DT, 32, 1>, 32);
+    if (pv <= 64) return pack(quant_rows_packed<DT, 32, 2>, 32);
+    if (pv <= 128) return pack(quant_rows_packed<DT, 32, 4>, 32);
+    if (pv <= 256) return pack(quant_rows_packed<DT, QT, 1>, QT);
+    if (pv <= 512) return pack(quant_rows_packed<DT, QT, 2>, QT);
+    if (pv <= 1024) return pack(quant_rows_packed<DT, QT, 4>, QT);
+    return pack(quant_rows_packed<DT, QT, 8>, QT);
+  }
   if (nv <= 32) return go(quant_rows<DT, 32, 1>, 32);
   if (nv <= 64) return go(quant_rows<DT, 32, 2>, 32);
   if (nv <= 128) return go(quant_rows<DT, 32, 4>, 32);
@@ -478,18 +639,29 @@ cudaError_t cols_launch(const QuantParams& p, int nsm, cudaStream_t s) {
     cudaError_t e = launch_dependent(quant_colmax<DT, VEC>, dim3((unsigned)wide, ny), QT, 0, s, p, vl, std::max<int64_t>(each, 1));
     if (e != cudaSuccess) return e;
   }
+  if (p.packed) {
+    const int64_t strips = p.prows / CW, K = (int64_t)p.kb * 64;
+    int64_t n = std::max<int64_t>(1, std::min(std::min<int64_t>(2 * nsm / strips, (K + TR - 1) / TR), (int64_t)65535));
+    each = ((K + n - 1) / n + TR - 1) / TR * TR;
+    n = (K + each - 1) / each;
+    return launch_dependent(quant_cols<DT, VEC, true>, dim3((unsigned)strips, (unsigned)n), QT, 0, s, p, each);
+  }
   const int64_t strips = (p.cols + CW - 1) / CW;
   const unsigned ty = shares(strips, TR, TR, 3, &each);
-  return launch_dependent(quant_cols<DT, VEC>, dim3((unsigned)strips, ty), QT, 0, s, p, std::max<int64_t>(each, TR));
+  return launch_dependent(quant_cols<DT, VEC, false>, dim3((unsigned)strips, ty), QT, 0, s, p, std::max<int64_t>(each, TR));
 }
 
 template <int DT>
 cudaError_t quant_launch(int axis, const QuantParams& p, int nsm, cudaStream_t s) {
-  if (axis == 0) return rows_launch<DT>(p, s);
+  if (axis == 0) return rows_launch<DT>(p, nsm, s);
   return p.vec_x ? cols_launch<DT, true>(p, nsm, s) : cols_launch<DT, false>(p, nsm, s);
 }
 
 }  // namespace
+
+bool quant8_packs(int dtype, int axis, const QuantParams& p) {
+  return p.vec_x && (axis == 1 || (int64_t)p.kb * 64 / (dtype == PEAT_F32 ? 4 : 8) <= 8 * QT);
+}
 
 cudaError_t launch_quant8(int dtype, int axis, const QuantParams& p, int nsm, cudaStream_t s) {
   if (dtype == PEAT_F32) return quant_launch<PEAT_F32>(axis, p, nsm, s);
