@@ -768,41 +768,39 @@ double mm8_tc_time(const Mm8TcPlan& p, int64_t K, int nsm) {
          std::max(0.0, (double)(p.mt + p.nt) * 256 * K * 3 / 5e6 - 3.0);
 }
 
+cudaError_t launch_mm8_pack(const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* norms, int which,
+                            cudaStream_t s) {
+  PackParams k;
+  k.x[0] = m.a;
+  k.x[1] = m.b;
+  k.ld[0] = m.lda;
+  k.ld[1] = m.ldb;
+  k.rows[0] = m.M;
+  k.rows[1] = m.N;
+  k.out[0] = reinterpret_cast<__half*>(ws + plan.a_off);
+  k.out[1] = reinterpret_cast<__half*>(ws + plan.b_off);
+  k.norm[0] = norms;
+  k.norm[1] = norms + plan.na_words;
+  k.K = m.K;
+  k.kb = plan.kb;
+  k.kc = plan.kc;
+  k.first_b = which & 1 ? plan.mt * 2 * plan.kc : 0;  // (a matrix that is not asked for has no CTAs)
+  const int64_t ctas = k.first_b + (which & 2 ? plan.nt * 2 * plan.kc : 0);
+  const uintptr_t a = which & 1 ? reinterpret_cast<uintptr_t>(m.a) | (uintptr_t)m.lda : 0;
+  const uintptr_t b = which & 2 ? reinterpret_cast<uintptr_t>(m.b) | (uintptr_t)m.ldb : 0;
+  return launch_dependent(((a | b) & 15) == 0 ? mm8_pack<16> : mm8_pack<1>, (unsigned)ctas, 256, 0, s, k);
+}
+
 cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* norms,
-                          int packed, unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s) {
-  unsigned int* na = norms;
-  unsigned int* nb = norms + plan.na_words;
-  if (packed != 3) {
-    PackParams k;
-    k.x[0] = m.a;
-    k.x[1] = m.b;
-    k.ld[0] = m.lda;
-    k.ld[1] = m.ldb;
-    k.rows[0] = m.M;
-    k.rows[1] = m.N;
-    k.out[0] = reinterpret_cast<__half*>(ws + plan.a_off);
-    k.out[1] = reinterpret_cast<__half*>(ws + plan.b_off);
-    k.norm[0] = na;
-    k.norm[1] = nb;
-    k.K = m.K;
-    k.kb = plan.kb;
-    k.kc = plan.kc;
-    // (a matrix that is packed already has no CTAs)
-    k.first_b = packed & 1 ? 0 : plan.mt * 2 * plan.kc;
-    const int64_t ctas = k.first_b + (packed & 2 ? 0 : plan.nt * 2 * plan.kc);
-    const uintptr_t a = packed & 1 ? 0 : reinterpret_cast<uintptr_t>(m.a) | (uintptr_t)m.lda;
-    const uintptr_t b = packed & 2 ? 0 : reinterpret_cast<uintptr_t>(m.b) | (uintptr_t)m.ldb;
-    cudaError_t e = launch_dependent(((a | b) & 15) == 0 ? mm8_pack<16> : mm8_pack<1>, (unsigned)ctas, 256, 0, s, k);
-    if (e != cudaSuccess) return e;
-  }
+                          bool scales_late, unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s) {
   CUtensorMap ma, mb;
   if (!block_map(&ma, ws + plan.a_off, plan.mt * 2 * plan.kb) || !block_map(&mb, ws + plan.b_off, plan.nt * 2 * plan.kb))
     return cudaErrorNotSupported;
   TcParams p;
   p.m = m;
-  p.na = reinterpret_cast<const uint2*>(na);
-  p.nb = reinterpret_cast<const uint2*>(nb);
-  p.scales_late = packed != 0;
+  p.na = reinterpret_cast<const uint2*>(norms);
+  p.nb = reinterpret_cast<const uint2*>(norms + plan.na_words);
+  p.scales_late = scales_late;
   p.kb = plan.kb;
   p.kc = plan.kc;
   p.mt = (int)plan.mt;

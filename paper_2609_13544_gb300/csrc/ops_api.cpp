@@ -13,6 +13,15 @@
 
 namespace peat {
 
+// Words that a call finds zero and the next one clears: two halves, in turn.
+struct Halves {
+  void* p = nullptr;
+  size_t cap = 0;  // bytes of both
+  int64_t used[2] = {0, 0};
+  int at = 0;
+  bool lost = false;  // a launch failed: what they hold is not known
+};
+
 // Made by a handle's first call of an operator, freed with it.
 struct OpsState {
   // gradient lists: device block (entries, then partial sums), and a ring of
@@ -28,19 +37,11 @@ struct OpsState {
   unsigned int* done = nullptr;  // zero between calls
   void* tickets = nullptr;       // counters of finished parts, zero between calls
   size_t tickets_cap = 0;
-  // column maxima: two buffers in turn; a call clears the other one's last use
-  void* colmax = nullptr;
-  size_t colmax_cap = 0;  // bytes of both
-  int64_t colmax_used[2] = {0, 0};
-  int colmax_at = 0;
+  Halves colmax;  // column maxima
+  Halves norms;   // sums of squares of operands packed on the way
   // operands that a product rounds, and their scales
   void* rounded = nullptr;
   size_t rounded_cap = 0;
-  // sums of squares of operands packed on the way: two buffers in turn
-  void* norms = nullptr;
-  size_t norms_cap = 0;  // bytes of both
-  int64_t norms_used[2] = {0, 0};
-  int norms_at = 0;
   // products: packed operands and partial sums
   void* mm = nullptr;
   size_t mm_cap = 0;
@@ -51,10 +52,10 @@ void ops_destroy(OpsState* s) {
   if (s->d_list) cudaFree(s->d_list);
   if (s->done) cudaFree(s->done);
   if (s->tickets) cudaFree(s->tickets);
-  if (s->colmax) cudaFree(s->colmax);
+  if (s->colmax.p) cudaFree(s->colmax.p);
   if (s->mm) cudaFree(s->mm);
   if (s->rounded) cudaFree(s->rounded);
-  if (s->norms) cudaFree(s->norms);
+  if (s->norms.p) cudaFree(s->norms.p);
   for (int i = 0; i < OpsState::RING; i++) {
     if (s->h_list[i]) cudaFreeHost(s->h_list[i]);
     if (s->taken[i]) cudaEventDestroy(s->taken[i]);
@@ -116,19 +117,9 @@ peat_status_t tickets(peat_handle_t h, OpsState* s, size_t n, cudaStream_t st) {
   return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "cudaMemsetAsync(counters)");
 }
 
-// A packed operand as a quantisation's output: its place, and in the plan's norms.
-struct Packed {
-  void* blocks;
-  int kb, kc;
-  int64_t rows;
-  unsigned int* norms;
-  unsigned int* zero;
-  int64_t zero_n;
-  bool made;  // out: whether it was made (else the integers were asked for in q and stand there)
-};
-peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int axis,
-                       int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv, cudaStream_t st,
-                       Packed* packed = nullptr) {
+// the checks of a quantisation, and its launches' parameters but for the workspace
+peat_status_t quant_params(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int axis,
+                           int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv, peat::QuantParams* p) {
   const int B = type_bytes(dtype);
   if (!B) return fail(h, PEAT_ERR_INVALID_ARG, "dtype must be PEAT_F32, PEAT_F16 or PEAT_BF16");
   if (axis != 0 && axis != 1) return fail(h, PEAT_ERR_INVALID_ARG, "axis must be 0 (rows) or 1 (columns)");
@@ -142,68 +133,70 @@ peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t col
   if (any && !q && !values) return fail(h, PEAT_ERR_INVALID_ARG, "q and values are both NULL");
   if ((any && !aligned(x, B)) || (values && !aligned(values, B)) || (scale && !aligned(scale, 4)))
     return fail(h, PEAT_ERR_INVALID_ARG, "a pointer is not aligned to its element type");
+  const int E = 16 / B;
+  std::memset(p, 0, sizeof(*p));
+  p->x = x;
+  p->rows = rows;
+  p->cols = cols;
+  p->ldx = ldx;
+  p->q = q;
+  p->ldq = ldq;
+  p->scale = scale;
+  p->values = values;
+  p->ldv = ldv;
+  p->vec_x = aligned(x, 16) && (ldx % E == 0 || rows <= 1);
+  const int qa = axis == 0 ? E : 4;
+  p->vec_q = q && aligned(q, qa) && ldq % qa == 0;
+  p->vec_v = values && aligned(values, 16) && (ldv % E == 0 || rows <= 1);
+  return PEAT_OK;
+}
+
+// n zeroed words out of a buffer of two halves, used in turn by the calls that
+// take some: a call also clears (*zero, *zero_n) what the one before it used.
+peat_status_t take(peat_handle_t h, peat::Halves* b, int64_t n, int64_t least, unsigned int** words, unsigned int** zero,
+                   int64_t* zero_n, cudaStream_t st) {
+  const size_t need = 2 * sizeof(unsigned int) * (size_t)((std::max(n, least) + 3) / 4 * 4);
+  if (need > b->cap || b->lost) {
+    b->lost = false;
+    peat_status_t ps = grow(h, &b->p, &b->cap, need);
+    if (ps != PEAT_OK) return ps;
+    b->used[0] = b->used[1] = 0;
+    cudaError_t e = cudaMemsetAsync(b->p, 0, b->cap, st);
+    if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(workspace)");
+  }
+  const size_t half = b->cap / 2 / sizeof(unsigned int);
+  unsigned int* base = static_cast<unsigned int*>(b->p);
+  *words = base + b->at * half;
+  *zero = base + (b->at ^ 1) * half;
+  *zero_n = b->used[b->at ^ 1];
+  b->used[b->at] = n;
+  b->used[b->at ^ 1] = 0;
+  b->at ^= 1;
+  return PEAT_OK;
+}
+
+peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int axis,
+                       int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv, cudaStream_t st) {
+  peat::QuantParams p;
+  peat_status_t ps = quant_params(h, x, rows, cols, ldx, dtype, axis, q, ldq, scale, values, ldv, &p);
+  if (ps != PEAT_OK) return ps;
   // nothing to write: no scale either
   if ((axis == 0 ? rows : cols) == 0) return PEAT_OK;
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
-  const int E = 16 / B;
-  peat::QuantParams p;
-  p.x = x;
-  p.rows = rows;
-  p.cols = cols;
-  p.ldx = ldx;
-  p.q = q;
-  p.ldq = ldq;
-  p.scale = scale;
-  p.values = values;
-  p.ldv = ldv;
-  p.vec_x = aligned(x, 16) && (ldx % E == 0 || rows <= 1);
-  const int qa = axis == 0 ? E : 4;
-  p.vec_q = q && aligned(q, qa) && ldq % qa == 0;
-  p.vec_v = values && aligned(values, 16) && (ldv % E == 0 || rows <= 1);
-  p.colmax = p.zero = nullptr;
-  p.zero_n = 0;
-  p.packed = nullptr;
-  if (packed) {
-    p.kb = packed->kb;
-    p.kc = packed->kc;
-    p.prows = packed->rows;
-    p.norms = packed->norms;
-    p.zero2 = packed->zero;
-    p.zero2_n = packed->zero_n;
-    packed->made = peat::quant8_packs(dtype, axis, p);
-    if (packed->made) p.packed = packed->blocks;
-  }
-  OpsState* s = nullptr;
   cudaError_t e;
-  if (axis == 1) {
-    peat_status_t ps = ops_state(h, &s);
+  if (axis == 0) {
+    e = peat::launch_quant8(dtype, peat::QUANT_ROWS, p, h->nsm, st);
+  } else {
+    OpsState* s = nullptr;
+    ps = ops_state(h, &s);
+    if (ps == PEAT_OK) ps = take(h, &s->colmax, cols, 8192, &p.colmax, &p.zero, &p.zero_n, st);
     if (ps != PEAT_OK) return ps;
-    const size_t need = 2 * sizeof(unsigned int) * (size_t)std::max<int64_t>(cols, 16384);
-    if (need > s->colmax_cap) {
-      ps = grow(h, &s->colmax, &s->colmax_cap, need);
-      if (ps != PEAT_OK) return ps;
-      s->colmax_used[0] = s->colmax_used[1] = 0;
-      e = cudaMemsetAsync(s->colmax, 0, need, st);
-      if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(maxima)");
-    }
-    unsigned int* both = static_cast<unsigned int*>(s->colmax);
-    const size_t half = s->colmax_cap / 2 / sizeof(unsigned int);
-    const int at = s->colmax_at;
-    p.colmax = both + at * half;
-    p.zero = both + (at ^ 1) * half;
-    p.zero_n = s->colmax_used[at ^ 1];
+    e = peat::launch_quant8(dtype, peat::QUANT_MAXIMA, p, h->nsm, st);
+    if (e == cudaSuccess) e = peat::launch_quant8(dtype, peat::QUANT_COLUMNS, p, h->nsm, st);
+    if (e != cudaSuccess) s->colmax.lost = true;
   }
-  e = peat::launch_quant8(dtype, axis, p, h->nsm, st);
-  if (e != cudaSuccess) {
-    if (s) s->colmax_cap = 0;  // (made anew by the next call: a launch may have left maxima)
-    return cuda_fail(h, e, "8-bit quantisation launch");
-  }
-  if (s) {
-    s->colmax_used[s->colmax_at] = cols;
-    s->colmax_used[s->colmax_at ^ 1] = 0;
-    s->colmax_at ^= 1;
-  }
+  if (e != cudaSuccess) return cuda_fail(h, e, "8-bit quantisation launch");
   return PEAT_OK;
 }
 
@@ -260,8 +253,10 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
       ps = grow(h, &s->mm, &s->mm_cap, norms + sizeof(unsigned int) * (size_t)(plan.na_words + plan.nb_words));
     if (ps != PEAT_OK) return ps;
     char* ws = static_cast<char*>(s->mm);
-    e = peat::launch_mm8_tc(out_dtype, p, plan, ws, reinterpret_cast<unsigned int*>(ws + norms), 0, h->status_dev,
-                            wait_limit(h), h->nsm, st);
+    unsigned int* sums = reinterpret_cast<unsigned int*>(ws + norms);
+    e = peat::launch_mm8_pack(p, plan, ws, sums, 3, st);
+    if (e == cudaSuccess)
+      e = peat::launch_mm8_tc(out_dtype, p, plan, ws, sums, false, h->status_dev, wait_limit(h), h->nsm, st);
   } else {
     e = peat::launch_mm8_direct(out_dtype, p, h->nsm, st);
   }
@@ -323,54 +318,89 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
   y = operand_of(*b, rounded, &at);
   const peat::Mm8TcPlan plan = peat::mm8_tc_plan(M, N, K, h->nsm);
   const bool wide = wide_product(h, plan, M, N, K);
-  char* ws = nullptr;
-  unsigned int *norms = nullptr, *stale = nullptr;
-  int64_t stale_n = 0;
-  const int64_t words = plan.na_words + plan.nb_words;
-  if (wide) {
-    ps = grow(h, &s->mm, &s->mm_cap, plan.bytes);
-    // the sums of squares: two buffers in turn, one cleared while the other is in use
-    const size_t both = 2 * sizeof(unsigned int) * (size_t)words;
-    if (ps == PEAT_OK && both > s->norms_cap) {
-      ps = grow(h, &s->norms, &s->norms_cap, both);
-      s->norms_used[0] = s->norms_used[1] = 0;
-      if (ps == PEAT_OK && cudaMemsetAsync(s->norms, 0, both, st) != cudaSuccess)
-        ps = cuda_fail(h, cudaGetLastError(), "cudaMemsetAsync(norms)");
-    }
-    if (ps != PEAT_OK) return ps;
-    ws = static_cast<char*>(s->mm);
-    if (words) {
-      const size_t half = s->norms_cap / 2 / sizeof(unsigned int);
-      norms = static_cast<unsigned int*>(s->norms) + s->norms_at * half;
-      stale = static_cast<unsigned int*>(s->norms) + (s->norms_at ^ 1) * half;
-      stale_n = s->norms_used[s->norms_at ^ 1];
-    }
-  }
+
+  // Which operands are rounded, and which of them straight into packed blocks
   const peat_operand_t* in[2] = {a, b};
   const Operand* op[2] = {&x, &y};
-  int packed = 0;
+  peat::QuantParams q[2];
+  int rounded_ops = 0, packed = 0;
+  int64_t columns = 0;
   for (int i = 0; i < 2; i++) {
     if (in[i]->dtype == PEAT_INT8) continue;
-    Packed to{ws + (i ? plan.b_off : plan.a_off), plan.kb, plan.kc, (i ? plan.nt : plan.mt) * 256,
-              norms ? norms + (i ? plan.na_words : 0) : nullptr, stale, packed ? 0 : stale_n, false};
-    ps = quantize(h, in[i]->data, in[i]->rows, in[i]->cols, in[i]->ld, in[i]->dtype, in[i]->axis,
-                  const_cast<int8_t*>(op[i]->q), op[i]->ld, const_cast<float*>(op[i]->scale), nullptr, 0, st,
-                  wide ? &to : nullptr);
-    if (ps != PEAT_OK) {
-      s->norms_cap = 0;  // (made anew by the next call)
-      return ps;
+    ps = quant_params(h, in[i]->data, in[i]->rows, in[i]->cols, in[i]->ld, in[i]->dtype, in[i]->axis,
+                      const_cast<int8_t*>(op[i]->q), op[i]->ld, const_cast<float*>(op[i]->scale), nullptr, 0, &q[i]);
+    if (ps != PEAT_OK) return ps;
+    rounded_ops |= 1 << i;
+    if (in[i]->axis) columns += in[i]->cols;
+    q[i].kb = plan.kb;
+    q[i].kc = plan.kc;
+    if (wide && peat::quant8_packs(in[i]->dtype, in[i]->axis, q[i])) packed |= 1 << i;
+  }
+  char* ws = nullptr;
+  unsigned int *norms = nullptr, *stale = nullptr, *maxima = nullptr, *zero = nullptr;
+  int64_t stale_n = 0, zero_n = 0;
+  const int64_t words = plan.na_words + plan.nb_words;
+  if (packed) {
+    ps = grow(h, &s->mm, &s->mm_cap, plan.bytes);
+    if (ps != PEAT_OK) return ps;
+    ws = static_cast<char*>(s->mm);
+    if (words) ps = take(h, &s->norms, words, 4096, &norms, &stale, &stale_n, st);
+    if (ps != PEAT_OK) return ps;
+  }
+  if (columns) {
+    ps = take(h, &s->colmax, columns, 8192, &maxima, &zero, &zero_n, st);
+    if (ps != PEAT_OK) return ps;
+  }
+  // A launch that needs nothing of the one before it runs beside it: the
+  // packing of one operand and the rounding of the other, both operands'
+  // column maxima, both operands' columns.
+  const peat::Mm8Params p{x.q, y.q, x.ld, y.ld, x.scale, y.scale, bias, out, ldo, M, N, K};
+  cudaError_t e = cudaSuccess;
+  bool beside = false;
+  const int as_is = packed ? 3 & ~rounded_ops : 0;
+  if (as_is) {
+    e = peat::launch_mm8_pack(p, plan, ws, norms, as_is, st);
+    beside = true;
+  }
+  int64_t at_column = 0;
+  for (int i = 0; i < 2; i++) {
+    if (!(rounded_ops >> i & 1) || !in[i]->axis) continue;
+    q[i].colmax = maxima + at_column;
+    at_column += in[i]->cols;
+    q[i].overlap = beside;
+    if (e == cudaSuccess) e = peat::launch_quant8(in[i]->dtype, peat::QUANT_MAXIMA, q[i], h->nsm, st);
+    beside = true;
+  }
+  if (columns) beside = false;  // the columns need their maxima
+  for (int i = 0; i < 2; i++) {
+    if (!(rounded_ops >> i & 1)) continue;
+    if (packed >> i & 1) {
+      q[i].packed = ws + (i ? plan.b_off : plan.a_off);
+      q[i].prows = (i ? plan.nt : plan.mt) * 256;
+      q[i].norms = norms ? norms + (i ? plan.na_words : 0) : nullptr;
+      q[i].zero2 = stale;
+      q[i].zero2_n = stale_n;
+      stale_n = 0;
     }
-    if (to.made) packed |= 1 << i;
+    if (in[i]->axis) {
+      q[i].zero = zero;
+      q[i].zero_n = zero_n;
+      zero_n = 0;
+    }
+    q[i].overlap = beside && (packed >> i & 1 || in[i]->axis);
+    if (e == cudaSuccess)
+      e = peat::launch_quant8(in[i]->dtype, in[i]->axis ? peat::QUANT_COLUMNS : peat::QUANT_ROWS, q[i], h->nsm, st);
+    beside = true;
+  }
+  // (a rounded operand that could not be packed on the way)
+  if (e == cudaSuccess && packed && (rounded_ops & ~packed)) e = peat::launch_mm8_pack(p, plan, ws, norms, rounded_ops & ~packed, st);
+  if (e == cudaSuccess && packed)
+    e = peat::launch_mm8_tc(out_dtype, p, plan, ws, norms, true, h->status_dev, wait_limit(h), h->nsm, st);
+  if (e != cudaSuccess) {
+    s->norms.lost = s->colmax.lost = true;
+    return cuda_fail(h, e, "8-bit product launch");
   }
   if (!packed) return matmul(h, x.q, x.ld, x.scale, y.q, y.ld, y.scale, bias, M, N, K, out, ldo, out_dtype, st);
-  if (words) {
-    s->norms_used[s->norms_at] = words;
-    s->norms_used[s->norms_at ^ 1] = 0;
-    s->norms_at ^= 1;
-  }
-  const peat::Mm8Params p{x.q, y.q, x.ld, y.ld, x.scale, y.scale, bias, out, ldo, M, N, K};
-  cudaError_t e = peat::launch_mm8_tc(out_dtype, p, plan, ws, norms, packed, h->status_dev, wait_limit(h), h->nsm, st);
-  if (e != cudaSuccess) return cuda_fail(h, e, "8-bit product launch");
   return PEAT_OK;
 }
 

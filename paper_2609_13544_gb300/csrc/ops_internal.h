@@ -46,10 +46,13 @@ struct QuantParams {
   unsigned int* norms;  // its sums of squares, zero before (null: not needed)
   unsigned int* zero2;  // those of an earlier call, cleared for a later one
   int64_t zero2_n;
+  int overlap;  // the kernel before this one on the stream is nothing to it
 };
 // whether a packed operand can be made (the matrix's rows lie on the vector grid, and fit a CTA's registers)
 bool quant8_packs(int dtype, int axis, const QuantParams& p);
-cudaError_t launch_quant8(int dtype, int axis, const QuantParams& p, int nsm, cudaStream_t s);
+// rows; or for columns first their maxima, then the integers
+enum { QUANT_ROWS, QUANT_MAXIMA, QUANT_COLUMNS };
+cudaError_t launch_quant8(int dtype, int step, const QuantParams& p, int nsm, cudaStream_t s);
 
 // ---- 8-bit products (matmul8.cu) ----
 struct Mm8Params {
@@ -75,9 +78,12 @@ struct Mm8TcPlan {
 double mm8_direct_time(int64_t M, int64_t N, int64_t K, int nsm);  // expected microseconds
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm);
 double mm8_tc_time(const Mm8TcPlan& p, int64_t K, int nsm);
-// norms: na_words, then nb_words; packed: bit 0 a, bit 1 b is packed already (its scales may be from the kernel before)
+// norms: na_words, then nb_words; which: bit 0 a, bit 1 b
+cudaError_t launch_mm8_pack(const Mm8Params& p, const Mm8TcPlan& plan, char* ws, unsigned int* norms, int which,
+                            cudaStream_t s);
+// scales_late: the scales may be made by the kernel before
 cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& p, const Mm8TcPlan& plan, char* ws, unsigned int* norms,
-                          int packed, unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s);
+                          bool scales_late, unsigned int* status, unsigned int wait_limit, int nsm, cudaStream_t s);
 
 // ---- gradient lists (gradnorm.cu) ----
 struct GnEntry {

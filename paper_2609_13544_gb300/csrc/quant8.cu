@@ -183,6 +183,17 @@ __device__ __forceinline__ void store_row_vec(const QuantParams& p, uint4 v, int
 
 constexpr int QT = 256;  // threads of a CTA
 
+// A kernel that needs nothing of the one before it (QuantParams::overlap) runs
+// beside it, and waits for it at its end, so that whoever waits for this one
+// has waited for both.
+__device__ __forceinline__ void begin(const QuantParams& p) {
+  if (!p.overlap) pdl_wait();
+  pdl_trigger();
+}
+__device__ __forceinline__ void end(const QuantParams& p) {
+  if (p.overlap) pdl_wait();
+}
+
 // the largest pattern over the TPR threads of a row (32: a warp, QT: the CTA)
 template <int TPR>
 __device__ __forceinline__ uint32_t row_max(uint32_t m) {
@@ -256,8 +267,7 @@ __device__ __forceinline__ void clear_earlier(const QuantParams& p) {
 template <int DT, int TPR, int NV>
 __global__ void __launch_bounds__(QT) quant_rows_packed(QuantParams p, int each) {
   using L = Elem<DT>;
-  pdl_wait();
-  pdl_trigger();
+  begin(p);
   clear_earlier(p);
   __shared__ uint32_t part[2][QT / 32];
   const int lane = threadIdx.x % TPR;
@@ -335,6 +345,7 @@ __global__ void __launch_bounds__(QT) quant_rows_packed(QuantParams p, int each)
         atomicMax(p.norms + (row0 >> 7) * p.kc * 2 + (L::E == 8 ? first / 256 * 2 : first / 128), most[i]);
     }
   }
+  end(p);
 }
 
 // A row by a CTA, read twice: rows too long for the registers, and (VEC false) rows off the 16-byte grid,
@@ -391,8 +402,7 @@ __global__ void __launch_bounds__(QT) quant_rows_twice(QuantParams p) {
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(QT) quant_colmax(QuantParams p, int vl, int64_t rows_each) {
   using L = Elem<DT>;
-  pdl_wait();
-  pdl_trigger();
+  begin(p);
   __shared__ uint4 part[QT];
   const int lx = threadIdx.x % vl, ly = threadIdx.x / vl, nl = QT / vl;
   const int64_t r0 = (int64_t)blockIdx.y * rows_each, r1 = min(p.rows, r0 + rows_each);
@@ -423,21 +433,23 @@ __global__ void __launch_bounds__(QT) quant_colmax(QuantParams p, int vl, int64_
   }
   part[threadIdx.x] = m;
   __syncthreads();
-  if (ly > 0 || left <= 0) return;
-  for (int k = 1; k < nl; k++) {
-    if (VEC) m = mag_max<DT>(m, part[k * vl + lx]);
-    else m.x = max(m.x, part[k * vl + lx].x);
-  }
-  if (VEC) {
-    const uint32_t w[4] = {m.x, m.y, m.z, m.w};
-#pragma unroll
-    for (int e = 0; e < L::E; e++) {
-      const uint32_t b = L::E == 4 ? w[e % 4] : (e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu);
-      if (e < left) atomicMax(p.colmax + col + e, b);
+  if (ly == 0 && left > 0) {
+    for (int k = 1; k < nl; k++) {
+      if (VEC) m = mag_max<DT>(m, part[k * vl + lx]);
+      else m.x = max(m.x, part[k * vl + lx].x);
     }
-  } else {
-    atomicMax(p.colmax + col, m.x);
+    if (VEC) {
+      const uint32_t w[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+      for (int e = 0; e < L::E; e++) {
+        const uint32_t b = L::E == 4 ? w[e % 4] : (e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu);
+        if (e < left) atomicMax(p.colmax + col + e, b);
+      }
+    } else {
+      atomicMax(p.colmax + col, m.x);
+    }
   }
+  end(p);
 }
 
 constexpr int TR = 128;  // rows of a tile
@@ -456,8 +468,7 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
   const int64_t r0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * rows_each,
                 r1 = min(PACK ? (int64_t)p.kb * 64 : p.rows, r0 + rows_each);
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + col;
-  pdl_wait();
-  pdl_trigger();
+  begin(p);
   if (PACK) clear_earlier(p);
   // the other buffer of maxima is the next call's: zero again
   {
@@ -583,6 +594,7 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
       }
     }
   }
+  end(p);
 }
 
 template <int DT>
@@ -620,7 +632,7 @@ cudaError_t rows_launch(const QuantParams& p, int nsm, cudaStream_t s) {
 }
 
 template <int DT, bool VEC>
-cudaError_t cols_launch(const QuantParams& p, int nsm, cudaStream_t s) {
+cudaError_t cols_launch(const QuantParams& p, bool maxima, int nsm, cudaStream_t s) {
   constexpr int E = Elem<DT>::E, CW = 8 * E;
   const int64_t per = VEC ? E : 1, nv = (p.cols + per - 1) / per;
   int vl = 8;
@@ -634,10 +646,10 @@ cudaError_t cols_launch(const QuantParams& p, int nsm, cudaStream_t s) {
     return (unsigned)std::max<int64_t>(1, (p.rows + *each - 1) / std::max<int64_t>(*each, 1));
   };
   int64_t each = 1;
-  const unsigned ny = shares(wide, 8 * lanes, 1, 5, &each);
-  if (p.rows > 0) {
-    cudaError_t e = launch_dependent(quant_colmax<DT, VEC>, dim3((unsigned)wide, ny), QT, 0, s, p, vl, std::max<int64_t>(each, 1));
-    if (e != cudaSuccess) return e;
+  if (maxima) {
+    const unsigned ny = shares(wide, 8 * lanes, 1, 5, &each);
+    if (p.rows == 0) return cudaSuccess;
+    return launch_dependent(quant_colmax<DT, VEC>, dim3((unsigned)wide, ny), QT, 0, s, p, vl, std::max<int64_t>(each, 1));
   }
   if (p.packed) {
     const int64_t strips = p.prows / CW, K = (int64_t)p.kb * 64;
@@ -652,9 +664,10 @@ cudaError_t cols_launch(const QuantParams& p, int nsm, cudaStream_t s) {
 }
 
 template <int DT>
-cudaError_t quant_launch(int axis, const QuantParams& p, int nsm, cudaStream_t s) {
-  if (axis == 0) return rows_launch<DT>(p, nsm, s);
-  return p.vec_x ? cols_launch<DT, true>(p, nsm, s) : cols_launch<DT, false>(p, nsm, s);
+cudaError_t quant_launch(int step, const QuantParams& p, int nsm, cudaStream_t s) {
+  if (step == QUANT_ROWS) return rows_launch<DT>(p, nsm, s);
+  const bool maxima = step == QUANT_MAXIMA;
+  return p.vec_x ? cols_launch<DT, true>(p, maxima, nsm, s) : cols_launch<DT, false>(p, maxima, nsm, s);
 }
 
 }  // namespace
@@ -663,10 +676,10 @@ bool quant8_packs(int dtype, int axis, const QuantParams& p) {
   return p.vec_x && (axis == 1 || (int64_t)p.kb * 64 / (dtype == PEAT_F32 ? 4 : 8) <= 8 * QT);
 }
 
-cudaError_t launch_quant8(int dtype, int axis, const QuantParams& p, int nsm, cudaStream_t s) {
-  if (dtype == PEAT_F32) return quant_launch<PEAT_F32>(axis, p, nsm, s);
-  if (dtype == PEAT_F16) return quant_launch<PEAT_F16>(axis, p, nsm, s);
-  return quant_launch<PEAT_BF16>(axis, p, nsm, s);
+cudaError_t launch_quant8(int dtype, int step, const QuantParams& p, int nsm, cudaStream_t s) {
+  if (dtype == PEAT_F32) return quant_launch<PEAT_F32>(step, p, nsm, s);
+  if (dtype == PEAT_F16) return quant_launch<PEAT_F16>(step, p, nsm, s);
+  return quant_launch<PEAT_BF16>(step, p, nsm, s);
 }
 
 }  // namespace peat
