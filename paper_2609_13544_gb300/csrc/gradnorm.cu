@@ -25,8 +25,7 @@
 namespace peat {
 namespace {
 
-constexpr int GB = 256;        // threads of a CTA
-constexpr int GB_SMALL = 1024;  // of the one CTA that takes a small list
+constexpr int GB = 256;  // threads of a CTA
 
 __device__ __forceinline__ int elem_size(int dt) { return dt == PEAT_F32 ? 4 : 2; }
 
@@ -234,16 +233,9 @@ __device__ __forceinline__ int find_tensor(const GnEntry* list, int count, int64
   }
   return lo;
 }
-// warp w of n owns units [first(w), first(w + 1)); owner(u) has unit u (in 32
-// bits where the numbers fit: a 64-bit division is a hundred instructions)
-template <typename I>
-__device__ __forceinline__ I first_unit(I w, I n, I units) {
-  return units * w / n;
-}
-template <typename I>
-__device__ __forceinline__ I owner(I u, I n, I units) {
-  return ((u + 1) * n - 1) / units;
-}
+// warp w of n owns units [first(w), first(w + 1)); owner(u) has unit u
+__device__ __forceinline__ int64_t first_unit(int64_t w, int64_t n, int64_t units) { return units * w / n; }
+__device__ __forceinline__ int64_t owner(int64_t u, int64_t n, int64_t units) { return ((u + 1) * n - 1) / units; }
 
 // the norm of a sum, times unscale, once rounded
 template <int NORM>
@@ -279,12 +271,12 @@ struct Total {
   }
 };
 
-// the record from the tensors' sums, by a CTA of NT threads; thread 0 returns it
-template <int NORM, int NT, typename F>
-__device__ peat_gradnorm_t finish(const GnParams& p, F tensor) {
-  __shared__ Total part[NT / 32];
+// the record from the tensors' sums, by a CTA
+template <int NORM, typename F>
+__device__ void finish(const GnParams& p, F tensor) {
+  __shared__ Total part[GB / 32];
   Total all;
-  for (int t = threadIdx.x; t < p.count; t += NT) {
+  for (int t = threadIdx.x; t < p.count; t += GB) {
     const GnPartial r = tensor(t);
     if (p.norms) p.norms[t] = to_norm<NORM>(r.s, p.unscale);
     all.add<NORM>(r.s, r.bad);
@@ -292,11 +284,11 @@ __device__ peat_gradnorm_t finish(const GnParams& p, F tensor) {
   all.warp<NORM>();
   if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = all;
   __syncthreads();
-  peat_gradnorm_t r = {};
   if (threadIdx.x < 32) {
     all = Total();
-    if (threadIdx.x < NT / 32) all = part[threadIdx.x];
+    if (threadIdx.x < GB / 32) all = part[threadIdx.x];
     all.warp<NORM>();
+    peat_gradnorm_t r;
     r.norm = to_norm<NORM>(all.s, p.unscale);
     r.n_bad = all.bad;
     float c = 1.0f;
@@ -309,17 +301,14 @@ __device__ peat_gradnorm_t finish(const GnParams& p, F tensor) {
     r.coef = c;
     if (threadIdx.x == 0) *p.result = r;
   }
-  return r;
 }
 
 // the pieces w0..w1 of a tensor, in a fixed order, by a warp
 template <int NORM>
-__device__ __forceinline__ GnPartial gather(const GnPartial* parts, int t, int64_t w0, int64_t w1, bool global) {
+__device__ __forceinline__ GnPartial gather(const GnPartial* parts, int t, int64_t w0, int64_t w1) {
   Total all;
-  for (int64_t w = w0 + (threadIdx.x & 31); w <= w1; w += 32) {
-    const GnPartial* q = parts + t + w;
-    all.add<NORM>(global ? __ldcg(&q->s) : q->s, global ? __ldcg(&q->bad) : q->bad);
-  }
+  for (int64_t w = w0 + (threadIdx.x & 31); w <= w1; w += 32)
+    all.add<NORM>(__ldcg(&parts[t + w].s), __ldcg(&parts[t + w].bad));
   all.warp<NORM>();
   GnPartial r;
   r.s = all.s;
@@ -333,8 +322,8 @@ template <int NORM>
 __device__ __forceinline__ void pieces_of(const GnParams& p, const GnEntry* list, int64_t w) {
   if (w >= p.nwarps || p.units == 0) return;
   const int lane = threadIdx.x & 31;
-  int64_t u = first_unit<int64_t>(w, p.nwarps, p.units);
-  const int64_t begin = u, end = first_unit<int64_t>(w + 1, p.nwarps, p.units);
+  int64_t u = first_unit(w, p.nwarps, p.units);
+  const int64_t begin = u, end = first_unit(w + 1, p.nwarps, p.units);
   if (u >= end) return;
   for (int t = find_tensor(list, p.count, u); u < end; t++) {
     const GnEntry e = list[t];
@@ -347,7 +336,7 @@ __device__ __forceinline__ void pieces_of(const GnParams& p, const GnEntry* list
       if (lane == 0) p.sums[t] = r;
       continue;
     }
-    const int64_t w0 = owner<int64_t>(data, p.nwarps, p.units), w1 = owner<int64_t>(next - 1, p.nwarps, p.units);
+    const int64_t w0 = owner(data, p.nwarps, p.units), w1 = owner(next - 1, p.nwarps, p.units);
     unsigned int n = 0;
     if (lane == 0) {
       p.parts[t + w] = r;
@@ -356,7 +345,7 @@ __device__ __forceinline__ void pieces_of(const GnParams& p, const GnEntry* list
     }
     if (__shfl_sync(0xffffffffu, n, 0) != (unsigned)(w1 - w0)) continue;
     __threadfence();
-    const GnPartial all = gather<NORM>(p.parts, t, w0, w1, true);
+    const GnPartial all = gather<NORM>(p.parts, t, w0, w1);
     if (lane == 0) {
       p.sums[t] = all;
       p.tickets[t] = 0;
@@ -383,7 +372,7 @@ __global__ void __launch_bounds__(GB, 5) gn_norm(GnParams p, const __grid_consta
   __syncthreads();
   if (!last) return;
   __threadfence();
-  finish<NORM, GB>(p, [&](int t) {
+  finish<NORM>(p, [&](int t) {
     const int64_t next = t + 1 < p.count ? list[t + 1].unit0 : p.units;
     return next > list[t].unit0 + p.lead ? load_sum(p.sums + t) : GnPartial{0.0, 0ull};  // (an empty tensor has no sum)
   });
@@ -446,10 +435,10 @@ __device__ void scale_piece(const GnEntry& e, int64_t j0, int64_t j1, float f, b
 }
 
 // warp w's share of n of the list, scaled by f (or set to zero)
-template <typename I>
-__device__ __forceinline__ void scale_share(const GnParams& p, const GnEntry* list, I w, I n, float f, bool zero) {
-  const int64_t u = first_unit<I>(w, n, (I)p.units);
-  int64_t end = first_unit<I>(w + 1, n, (I)p.units);
+__device__ __forceinline__ void scale_share(const GnParams& p, const GnEntry* list, int64_t w, int64_t n, float f,
+                                            bool zero) {
+  const int64_t u = first_unit(w, n, p.units);
+  int64_t end = first_unit(w + 1, n, p.units);
   if (u >= end) return;
   for (int t = find_tensor(list, p.count, end - 1); end > u; t--) {
     const GnEntry e = list[t];
@@ -470,51 +459,7 @@ __global__ void __launch_bounds__(GB) gn_scale(GnParams p, const __grid_constant
   const int64_t n = (int64_t)gridDim.x * (GB / 32);
   const float f = __fmul_rn(p.unscale, __ldcg(&p.result->coef));
   const bool zero = p.bad_mode == PEAT_BAD_ZERO && __ldcg(&p.result->n_bad) != 0;
-  scale_share<int64_t>(p, list, (int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5), n, f, zero);
-}
-
-// A small list by one CTA, norm and clipping in one launch: a launch and the
-// meeting of CTAs in global memory cost more than its bytes. 
-template <int NORM>
-__global__ void __launch_bounds__(GB_SMALL) gn_small(GnParams p, const __grid_constant__ GnInline in) {
-  constexpr int W = GB_SMALL / 32;
-  __shared__ GnPartial parts[GN_INLINE + W], sums[GN_INLINE];
-  __shared__ float f;
-  __shared__ bool zero;
-  const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const GnEntry* list = in.e;
-  pdl_wait();
-  pdl_trigger();
-  // every warp that counts has a unit, so every part that is gathered was written
-  const uint32_t units = (uint32_t)p.units, n = min((uint32_t)W, max(units, 1u));
-  if (w < n && units > 0) {
-    int64_t u = first_unit<uint32_t>(w, n, units);
-    const int64_t end = first_unit<uint32_t>(w + 1, n, units);
-    for (int t = find_tensor(list, p.count, u); u < end; t++) {
-      const GnEntry e = list[t];
-      const int64_t stop = min(end, t + 1 < p.count ? list[t + 1].unit0 : p.units);
-      if (stop <= u) continue;
-      const GnPartial r = piece_of<NORM>(e, u - e.unit0, stop - e.unit0);
-      if (lane == 0) parts[t + w] = r;
-      u = stop;
-    }
-  }
-  __syncthreads();
-  for (int t = w; t < p.count; t += W) {
-    const int64_t u0 = list[t].unit0, u1 = t + 1 < p.count ? list[t + 1].unit0 : p.units;
-    GnPartial r{0.0, 0ull};
-    if (u1 > u0) r = gather<NORM>(parts, t, owner<uint32_t>((uint32_t)u0, n, units), owner<uint32_t>((uint32_t)u1 - 1, n, units), false);
-    if (lane == 0) sums[t] = r;
-  }
-  __syncthreads();
-  const peat_gradnorm_t r = finish<NORM, GB_SMALL>(p, [&](int t) { return sums[t]; });
-  if (!p.clip) return;
-  if (threadIdx.x == 0) {
-    f = __fmul_rn(p.unscale, r.coef);
-    zero = p.bad_mode == PEAT_BAD_ZERO && r.n_bad != 0;
-  }
-  __syncthreads();
-  if (p.units > 0) scale_share<uint32_t>(p, list, w, W, f, zero);
+  scale_share(p, list, (int64_t)blockIdx.x * (GB / 32) + (threadIdx.x >> 5), n, f, zero);
 }
 
 }  // namespace
@@ -532,21 +477,13 @@ static cudaError_t norm_and_scale(const GnParams& p, const IN& in, int nctas, cu
 }
 cudaError_t launch_gradnorm(const GnParams& p, const GnEntry* host, int nctas, cudaStream_t s) {
   if (p.list) return norm_and_scale(p, GnInlineOf<1>{}, nctas, s);
-  if (p.count <= GN_INLINE) {
-    GnInline in;
+  if (p.count <= GN_INLINE_FEW) {
+    GnInlineOf<GN_INLINE_FEW> in;
     std::copy(host, host + p.count, in.e);
     return norm_and_scale(p, in, nctas, s);
   }
-  GnInlineOf<GN_INLINE_MOST> in;
+  GnInlineOf<GN_INLINE> in;
   std::copy(host, host + p.count, in.e);
   return norm_and_scale(p, in, nctas, s);
 }
-cudaError_t launch_gradnorm_small(const GnParams& p, const GnEntry* host, cudaStream_t s) {
-  GnInline in;
-  std::copy(host, host + p.count, in.e);
-  auto kernel = p.type == PEAT_NORM_1 ? gn_small<PEAT_NORM_1>
-                                      : (p.type == PEAT_NORM_INF ? gn_small<PEAT_NORM_INF> : gn_small<PEAT_NORM_2>);
-  return launch_dependent(kernel, 1, GB_SMALL, 0, s, p, in);
-}
-
 }  // namespace peat

@@ -185,8 +185,8 @@ peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t col
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
   cudaError_t e;
-  if (axis == 0) {
-    e = peat::launch_quant8(dtype, peat::QUANT_ROWS, p, h->nsm, st);
+  if (axis == 0 || rows <= peat::QUANT_FEW_ROWS) {
+    e = peat::launch_quant8(dtype, axis == 0 ? peat::QUANT_ROWS : peat::QUANT_COLUMNS, p, h->nsm, st);
   } else {
     OpsState* s = nullptr;
     ps = ops_state(h, &s);
@@ -331,7 +331,7 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
                       const_cast<int8_t*>(op[i]->q), op[i]->ld, const_cast<float*>(op[i]->scale), nullptr, 0, &q[i]);
     if (ps != PEAT_OK) return ps;
     rounded_ops |= 1 << i;
-    if (in[i]->axis) columns += in[i]->cols;
+    if (in[i]->axis && in[i]->rows > peat::QUANT_FEW_ROWS) columns += in[i]->cols;
     q[i].kb = plan.kb;
     q[i].kc = plan.kc;
     if (wide && peat::quant8_packs(in[i]->dtype, in[i]->axis, q[i])) packed |= 1 << i;
@@ -364,7 +364,7 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
   }
   int64_t at_column = 0;
   for (int i = 0; i < 2; i++) {
-    if (!(rounded_ops >> i & 1) || !in[i]->axis) continue;
+    if (!(rounded_ops >> i & 1) || !in[i]->axis || !columns) continue;  // (both operands' columns have K rows)
     q[i].colmax = maxima + at_column;
     at_column += in[i]->cols;
     q[i].overlap = beside;
@@ -382,7 +382,7 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
       q[i].zero2_n = stale_n;
       stale_n = 0;
     }
-    if (in[i]->axis) {
+    if (q[i].colmax) {
       q[i].zero = zero;
       q[i].zero_n = zero_n;
       zero_n = 0;
@@ -440,22 +440,21 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   peat_status_t ps = ops_state(h, &s);
   if (ps != PEAT_OK) return ps;
 
-  const bool small = count <= peat::GN_INLINE && units <= peat::GN_SMALL;
   // a piece's own time is about that of 256 units
-  const int64_t lead = small ? 0 : 256;
+  const int64_t lead = 256;
   for (int64_t t = 0; t < count; t++) units += list[t].n > 0 ? lead : 0;
   // one wave; a warp has at least 64 units
   const int per = peat::gn_block() / 32;
   const int64_t warps = std::max<int64_t>(1, std::min<int64_t>((units + 63) / 64, (int64_t)h->nsm * 5 * per));
   const int nctas = (int)((warps + per - 1) / per);
-  const size_t listed = count > peat::GN_INLINE_MOST ? (sizeof(peat::GnEntry) * (size_t)count + 255) / 256 * 256 : 0;
+  const size_t listed = count > peat::GN_INLINE ? (sizeof(peat::GnEntry) * (size_t)count + 255) / 256 * 256 : 0;
   const size_t parted = sizeof(peat::GnPartial) * (size_t)(count + warps);
   ps = grow(h, &s->d_list, &s->d_list_cap, listed + parted + sizeof(peat::GnPartial) * (size_t)count);
   if (ps != PEAT_OK) return ps;
   ps = tickets(h, s, (size_t)count, st);
   if (ps != PEAT_OK) return ps;
 
-  peat::GnEntry inline_list[peat::GN_INLINE_MOST];
+  peat::GnEntry inline_list[peat::GN_INLINE];
   peat::GnEntry* dst = inline_list;
   int slot = -1;
   if (listed) {
@@ -515,8 +514,7 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   p.result = result;
   p.norms = norms;
   p.lead = lead;
-  cudaError_t e = small ? peat::launch_gradnorm_small(p, inline_list, st)
-                        : peat::launch_gradnorm(p, inline_list, nctas, st);
+  cudaError_t e = peat::launch_gradnorm(p, inline_list, nctas, st);
   if (e != cudaSuccess) return cuda_fail(h, e, "gradient norm launch");
   return PEAT_OK;
 }

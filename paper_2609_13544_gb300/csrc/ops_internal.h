@@ -35,7 +35,8 @@ struct QuantParams {
   int vec_x;  // x's rows start on 16-byte boundaries
   int vec_q;  // q's rows start on boundaries of a vector's integers (axis 0: 8 or 4 bytes; axis 1: 4 bytes)
   int vec_v;  // values' rows start on 16-byte boundaries
-  // columns: their largest patterns, zero before the call, and what to clear for a later one
+  // columns: their largest patterns, zero before the call (null: the rows are few
+  // and every CTA finds its own), and what to clear for a later one
   unsigned int* colmax;
   unsigned int* zero;
   int64_t zero_n;
@@ -50,6 +51,9 @@ struct QuantParams {
 };
 // whether a packed operand can be made (the matrix's rows lie on the vector grid, and fit a CTA's registers)
 bool quant8_packs(int dtype, int axis, const QuantParams& p);
+// Rows up to which columns need no launch for their maxima: at 512 of 4096
+// columns the one launch takes AAA us and the two BBB.
+constexpr int64_t QUANT_FEW_ROWS = 512;
 // rows; or for columns first their maxima, then the integers
 enum { QUANT_ROWS, QUANT_MAXIMA, QUANT_COLUMNS };
 cudaError_t launch_quant8(int dtype, int step, const QuantParams& p, int nsm, cudaStream_t s);
@@ -94,13 +98,13 @@ struct GnEntry {
   int32_t dtype, pad;
 };
 // Entries that travel as a kernel argument, which takes up to 32 764 bytes: a
-// list in memory would first have to be copied there (4 us).
-constexpr int GN_INLINE = 96, GN_INLINE_MOST = 800;
+// list in memory would first have to be copied there (a call with 800 tensors
+// of 80 elements takes 12 us, with 801 of them 21).
+constexpr int GN_INLINE_FEW = 96, GN_INLINE = 800;
 template <int N>
 struct GnInlineOf {
   GnEntry e[N];
 };
-using GnInline = GnInlineOf<GN_INLINE>;
 struct GnPartial {
   double s;                // sum (or maximum)
   unsigned long long bad;  // NaN and infinite elements
@@ -125,9 +129,6 @@ struct GnParams {
 int gn_block();  // threads of a CTA of both passes
 // host: the entries, where p.list is null
 cudaError_t launch_gradnorm(const GnParams& p, const GnEntry* host, int nctas, cudaStream_t s);
-// the whole call in one CTA, for at most GN_INLINE tensors and GN_SMALL units (lead 0)
-constexpr int64_t GN_SMALL = 8192;
-cudaError_t launch_gradnorm_small(const GnParams& p, const GnEntry* host, cudaStream_t s);
 // 16-byte units that hold the n elements of `size` bytes at g
 inline int64_t gn_units(const void* g, int64_t n, int size) {
   if (n <= 0) return 0;

@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(QT) quant_rows_twice(QuantParams p) {
   }
 }
 
-// Columns, in two launches.  The first finds each column's maximum: a thread
+// Columns, in two launches (one for few rows).  The first finds each column's maximum: a thread
 // has a 16-byte vector of columns (VEC false: one column) and walks down a
 // share of the rows, the shares meet by atomic maxima of the patterns.  The
 // second reads the matrix again, last rows first, so that it finds in L2 what
@@ -458,7 +458,7 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
   using L = Elem<DT>;
   constexpr int CW = 8 * L::E;  // columns of a tile
   __shared__ __align__(16) float rs[CW], ss[CW];
-  __shared__ uint32_t bads[2];
+  __shared__ uint32_t bads[2], tops[CW];
   __shared__ __align__(16) uint32_t tile[CW * (PACK ? TR / 2 : TR / 4 + 1)];  // integers: bytes, or packed binary16
   __shared__ float squares[PACK ? QT / 32 : 1][CW];
   const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3;
@@ -490,9 +490,37 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
   };
   uint4 v[4];
   load(r0, v);
+  if (!p.colmax) {  // few rows: every CTA finds its columns' maxima itself
+    __shared__ uint4 part[QT / 32][8];
+    uint4 m = make_uint4(0, 0, 0, 0);
+    if (left > 0) {
+      for (int64_t row = ty; row < p.rows; row += 4 * (QT / 8)) {
+        uint4 u[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) u[j] = load_vec<DT, VEC>(x + min(row + j * (QT / 8), p.rows - 1) * p.ldx, left);
+#pragma unroll
+        for (int j = 0; j < 4; j++) m = mag_max<DT>(m, u[j]);
+      }
+    }
+#pragma unroll
+    for (int o = 8; o <= 16; o *= 2)
+      m = mag_max<DT>(m, make_uint4(__shfl_xor_sync(0xffffffffu, m.x, o), __shfl_xor_sync(0xffffffffu, m.y, o),
+                                    __shfl_xor_sync(0xffffffffu, m.z, o), __shfl_xor_sync(0xffffffffu, m.w, o)));
+    if ((threadIdx.x & 31) < 8) part[threadIdx.x >> 5][tx] = m;
+    __syncthreads();
+    if (threadIdx.x < CW) {
+      uint32_t top = 0;
+      const int c = threadIdx.x;
+      for (int w = 0; w < QT / 32; w++) {
+        const uint32_t b = reinterpret_cast<const uint32_t*>(&part[w][0])[c * 4 / L::E];
+        top = max(top, L::E == 4 ? b : (c & 1 ? b >> 16 : b & 0xffffu));
+      }
+      tops[c] = top;
+    }
+  }
   if (threadIdx.x < CW) {
     const int c = threadIdx.x;
-    const uint32_t top = c0 + c < p.cols ? __ldcg(p.colmax + c0 + c) : 0;
+    const uint32_t top = c0 + c >= p.cols ? 0 : (p.colmax ? __ldcg(p.colmax + c0 + c) : tops[c]);
     float r, scale;
     factors<DT>(top, r, scale);
     rs[c] = r;

@@ -65,15 +65,30 @@ def _call(h, name, *args) -> None:
         _check(rc, h)
 
 
+_raw_stream = None
+
+
 def _stream(h, stream) -> int:
-    import torch
-    return (torch.cuda.current_stream(h.device) if stream is None else stream).cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        # the current stream's handle without a Stream object around it (1 us less a call), where torch has it
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda device: torch.cuda.current_stream(device).cuda_stream)
+    return _raw_stream(h.device)
+
+
+_NOTHING = contextlib.nullcontext()
 
 
 def _on(stream):
     """Allocations belong to the stream that the call runs on."""
+    if stream is None:
+        return _NOTHING
     import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return torch.cuda.stream(stream)
 
 
 def _code(t) -> int:
@@ -325,27 +340,37 @@ class Linear8:
         self.out_features, self.in_features = weight.shape
         self.q, self.scale = peat_quantize_i8(h, weight, 0, stream)
         self.qt, self.scale_t = peat_quantize_i8(h, weight, 1, stream)
+        self._w = _operand(h, self.q, 0, self.scale, "weight")
+        self._wt = _operand(h, self.qt, 0, self.scale_t, "weight")
 
-    def _rows(self, t, width: int, name: str):
-        if t.dim() < 1 or t.shape[-1] != width:
-            raise ValueError(f"the last dimension of {name} must be {width}")
-        return t if t.dim() == 2 else t.reshape(-1, width)
+    def _product(self, t, w, name: str, bias=None, stream=None):
+        """t [..., K] by row times a weight operand -> [..., N] of t's type."""
+        import torch
+        op, N, K = w
+        if t.dim() < 1 or t.shape[-1] != K:
+            raise ValueError(f"the last dimension of {name} must be {K}")
+        x = t if t.dim() == 2 else t.reshape(-1, K)
+        with _on(stream):
+            out = torch.empty(x.shape[0], N, dtype=t.dtype, device=t.device)
+            a, M, _ = _operand(self.h, x, 0, None, name)
+            _call(self.h, "peat_product_i8", ctypes.byref(a), ctypes.byref(op), _vector(self.h, bias, N, "bias"),
+                  out.data_ptr(), N, _code(out), _stream(self.h, stream))
+        return out if t.dim() == 2 else out.view(*t.shape[:-1], N)
 
     def forward(self, x, bias=None, stream=None):
         """x [..., in] -> [..., out] of x's type."""
-        y = peat_product_i8(self.h, self._rows(x, self.in_features, "x"), self.q, 0, 0, None, self.scale, bias, x.dtype,
-                            stream)
-        return y if x.dim() == 2 else y.view(*x.shape[:-1], self.out_features)
+        return self._product(x, self._w, "x", bias, stream)
 
     def input_grad(self, grad, stream=None):
         """dL/dx [..., in] of grad's type from grad = dL/dy [..., out]."""
-        g = peat_product_i8(self.h, self._rows(grad, self.out_features, "grad"), self.qt, 0, 0, None, self.scale_t, None,
-                            grad.dtype, stream)
-        return g if grad.dim() == 2 else g.view(*grad.shape[:-1], self.in_features)
+        return self._product(grad, self._wt, "grad", None, stream)
 
     def weight_grad(self, grad, x, stream=None):
         """dL/dw [out, in] in float32 from grad [..., out] and x [..., in]."""
-        g, x = self._rows(grad, self.out_features, "grad"), self._rows(x, self.in_features, "x")
+        if grad.shape[-1:] != (self.out_features,) or x.shape[-1:] != (self.in_features,):
+            raise ValueError(f"the last dimensions of grad and x must be {self.out_features} and {self.in_features}")
+        g = grad if grad.dim() == 2 else grad.reshape(-1, self.out_features)
+        x = x if x.dim() == 2 else x.reshape(-1, self.in_features)
         if g.shape[0] != x.shape[0]:
             raise ValueError("grad and x differ in their leading dimensions")
         return peat_product_i8(self.h, g, x, 1, 1, stream=stream)
