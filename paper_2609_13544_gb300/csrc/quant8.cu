@@ -24,30 +24,21 @@ struct Elem<PEAT_F32> {
   using T = float;
   static constexpr int E = 4;  // elements of a 16-byte vector
   static constexpr uint32_t INF = 0x7f800000u;
-  static __device__ __forceinline__ uint32_t bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
   static __device__ __forceinline__ float mag(uint32_t b) { return __uint_as_float(b); }
-  static __device__ __forceinline__ float up(float v) { return v; }
-  static __device__ __forceinline__ float down(float v) { return v; }
 };
 template <>
 struct Elem<PEAT_F16> {
   using T = __half;
   static constexpr int E = 8;
   static constexpr uint32_t INF = 0x7c00u;
-  static __device__ __forceinline__ uint32_t bits(__half v) { return __half_as_ushort(v) & 0x7fffu; }
   static __device__ __forceinline__ float mag(uint32_t b) { return __half2float(__ushort_as_half((unsigned short)b)); }
-  static __device__ __forceinline__ float up(__half v) { return __half2float(v); }
-  static __device__ __forceinline__ __half down(float v) { return __float2half_rn(v); }
 };
 template <>
 struct Elem<PEAT_BF16> {
   using T = __nv_bfloat16;
   static constexpr int E = 8;
   static constexpr uint32_t INF = 0x7f80u;
-  static __device__ __forceinline__ uint32_t bits(__nv_bfloat16 v) { return __bfloat16_as_ushort(v) & 0x7fffu; }
   static __device__ __forceinline__ float mag(uint32_t b) { return __uint_as_float(b << 16); }
-  static __device__ __forceinline__ float up(__nv_bfloat16 v) { return __bfloat162float(v); }
-  static __device__ __forceinline__ __nv_bfloat16 down(float v) { return __float2bfloat16_rn(v); }
 };
 
 // a 16-byte vector as its elements
@@ -118,10 +109,48 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
                      __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
 }
 
-// the first `left` elements of a vector at p (left < E: one by one, zero beyond)
-template <int DT, bool VEC>
-__device__ __forceinline__ uint4 load_vec(const typename Elem<DT>::T* p, int64_t left) {
-  if (VEC && left >= Elem<DT>::E) return __ldg(reinterpret_cast<const uint4*>(p));
+// bytes [by, by + 16) of the 32 of a and b
+__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int by) {
+  uint32_t t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  const bool one = by & 4, two = by & 8;
+#pragma unroll
+  for (int i = 0; i < 7; i++) t[i] = one ? t[i + 1] : t[i];
+#pragma unroll
+  for (int i = 0; i < 5; i++) t[i] = two ? t[i + 2] : t[i];
+  const int bits = (by & 3) * 8;
+  return make_uint4(__funnelshift_r(t[0], t[1], bits), __funnelshift_r(t[1], t[2], bits),
+                    __funnelshift_r(t[2], t[3], bits), __funnelshift_r(t[3], t[4], bits));
+}
+// Vectors of E elements at any multiple of the element's size.  On the 16-byte
+// grid one load; off it the two aligned vectors that hold it, shifted together.
+// A vector that is not whole (`left` elements exist), or whose aligned vectors
+// reach beyond the matrix, is left for load_edge.
+template <int DT, bool GRID>
+struct Source {
+  using T = typename Elem<DT>::T;
+  uintptr_t lo, hi;  // the matrix's bytes
+  __device__ explicit Source(const QuantParams& p) {
+    const T* x = static_cast<const T*>(p.x);
+    lo = reinterpret_cast<uintptr_t>(x);
+    hi = reinterpret_cast<uintptr_t>(x + (p.rows - 1) * p.ldx + p.cols);
+  }
+  __device__ __forceinline__ bool whole(const T* p, int64_t left) const {
+    if (left < Elem<DT>::E) return false;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15;
+    return GRID || (a >= lo && a + 32 <= hi);
+  }
+  __device__ __forceinline__ uint4 load(const T* p) const {
+    if (GRID) return __ldg(reinterpret_cast<const uint4*>(p));
+    const uint4* a = on_grid(p);
+    return shifted(__ldg(a), __ldg(a + 1), (int)(reinterpret_cast<uintptr_t>(p) & 15));
+  }
+  static __device__ __forceinline__ const uint4* on_grid(const T* p) {
+    return reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+  }
+};
+// the first `left` elements of a vector, one by one, zeros beyond
+template <int DT>
+__device__ __forceinline__ uint4 load_edge(const typename Elem<DT>::T* p, int64_t left) {
   Vec<DT> v;
   v.u = make_uint4(0, 0, 0, 0);
 #pragma unroll
@@ -130,7 +159,7 @@ __device__ __forceinline__ uint4 load_vec(const typename Elem<DT>::T* p, int64_t
   return v.u;
 }
 
-// a vector's integers (in float32, see whole) from its row's or its columns' factors
+// a vector's integers (in float32, see whole) from its row's factor
 template <int DT, bool FINITE>
 __device__ __forceinline__ void wholes(uint4 v, float r, float (&w)[Elem<DT>::E]) {
   float x[Elem<DT>::E];
@@ -138,28 +167,111 @@ __device__ __forceinline__ void wholes(uint4 v, float r, float (&w)[Elem<DT>::E]
 #pragma unroll
   for (int e = 0; e < Elem<DT>::E; e++) w[e] = whole(x[e], r, FINITE);
 }
-// a vector's values at o, of which `left` exist
-template <int DT>
-__device__ __forceinline__ void store_values(typename Elem<DT>::T* o, const float (&y)[Elem<DT>::E], bool vec, int64_t left) {
+// A vector's values at o, of which `left` (any number) exist, by G lanes that
+// have consecutive vectors of a row.  Where the row is off the 16-byte grid a
+// lane writes the aligned vector that ends inside its own, the last elements of
+// the vector before in front: the lane before's, or for lane 0 `carry`, the last
+// lane's of the call before, unless this is the first.  What no vector of the
+// group precedes or follows goes one by one.  All lanes of a group call it.
+template <int DT, int G>
+__device__ __forceinline__ void store_values(typename Elem<DT>::T* o, const float (&y)[Elem<DT>::E], bool on_grid,
+                                             int64_t left, uint4& carry, bool first, bool last) {
+  constexpr int E = Elem<DT>::E, B = 16 / E;
   Vec<DT> v;
   v.u = pack<DT>(y);
-  if (vec && left >= Elem<DT>::E) {
-    __stcs(reinterpret_cast<uint4*>(o), v.u);
+  if (on_grid) {
+    if (left >= E) {
+      __stcs(reinterpret_cast<uint4*>(o), v.u);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e++)
+        if (e < left) o[e] = v.e[e];
+    }
+    return;
+  }
+  const int lane = threadIdx.x % G;
+  // (a rotation: lane 0 receives the last lane's, for the next call)
+  auto turned = [&](uint32_t x, uint32_t& kept) {
+    const uint32_t t = __shfl_sync(0xffffffffu, x, (lane + G - 1) % G, G);
+    const uint32_t before = lane == 0 ? kept : t;
+    kept = t;
+    return before;
+  };
+  const uint4 before = make_uint4(turned(v.u.x, carry.x), turned(v.u.y, carry.y), turned(v.u.z, carry.z), turned(v.u.w, carry.w));
+  const int s = (int)(reinterpret_cast<uintptr_t>(o) & 15) / B;  // elements from the grid to o
+  const bool alone = first && lane == 0;
+  Vec<DT> w;
+  w.u = s ? shifted(before, v.u, 16 - s * B) : v.u;
+  if ((!alone || s == 0) && left >= E - s) {
+    __stcs(reinterpret_cast<uint4*>(o - s), w.u);
   } else {
 #pragma unroll
-    for (int e = 0; e < Elem<DT>::E; e++)
-      if (e < left) o[e] = v.e[e];
+    for (int e = 0; e < E; e++)
+      if ((!alone || e >= s) && e - s < left) o[e - s] = w.e[e];
+  }
+  if (last && lane == G - 1) {  // its own last elements
+#pragma unroll
+    for (int e = 0; e < E; e++)
+      if (e >= E - s && e < left) o[e] = v.e[e];
   }
 }
 
-// integers and values of one vector of a row
-template <int DT>
-__device__ __forceinline__ void store_row_vec(const QuantParams& p, uint4 v, int64_t row, int64_t col, int64_t left,
-                                              float r, float scale, bool finite) {
+constexpr int QT = 256;  // threads of a CTA
+
+// A kernel that needs nothing of the one before it (QuantParams::overlap) runs
+// beside it, and waits for it at its end, so that whoever waits for this one
+// has waited for both.
+__device__ __forceinline__ void begin(const QuantParams& p) {
+  if (!p.overlap) pdl_wait();
+  pdl_trigger();
+}
+__device__ __forceinline__ void end(const QuantParams& p) {
+  if (p.overlap) pdl_wait();
+}
+__device__ __forceinline__ void clear_earlier(const QuantParams& p) {
+  const int64_t n = (int64_t)gridDim.x * gridDim.y * QT;
+  for (int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * QT + threadIdx.x; i < p.zero2_n; i += n) p.zero2[i] = 0;
+}
+
+// where the integers of operand row `row`, k on, lie in a packed operand (see
+// mm8_tc.cu): 16 KB blocks of 128 rows by 64 k, 16-byte pieces of 8 k swizzled
+__device__ __forceinline__ char* packed_at(const QuantParams& p, int64_t row, int64_t k) {
+  const int r = (int)(row & 127);
+  return static_cast<char*>(p.packed) + ((row >> 7) * p.kb + (k >> 6)) * 16384 + r * 128 +
+         ((((int)k >> 3 & 7) ^ (r & 7)) * 16) + ((int)k & 7) * 2;
+}
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+  const __half2 h = __floats2half2_rn(number(a), number(b));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// integers (q, or the packed operand), values and the sum of squares of one
+// vector of a row; all lanes of a warp together
+template <int DT, bool PACK, int G>
+__device__ __forceinline__ void put_row_vec(const QuantParams& p, uint4 v, int64_t row, int64_t col, float r,
+                                            float scale, bool finite, unsigned& most, uint4& carry, bool first, bool last) {
   using L = Elem<DT>;
   float w[L::E];
   if (finite) wholes<DT, true>(v, r, w);
   else wholes<DT, false>(v, r, w);
+  if (PACK) {
+    if (col < (int64_t)p.kb * 64) {
+      char* d = packed_at(p, row, col);
+      if (L::E == 8)
+        *reinterpret_cast<uint4*>(d) = make_uint4(half_pair(w[0], w[1]), half_pair(w[2], w[3]),
+                                                  half_pair(w[4 % L::E], w[5 % L::E]), half_pair(w[6 % L::E], w[7 % L::E]));
+      else
+        *reinterpret_cast<uint2*>(d) = make_uint2(half_pair(w[0], w[1]), half_pair(w[2], w[3]));
+    }
+    if (p.norms) {  // a warp's vectors are 256 k, or half of them
+      float ss = 0.0f;  // (exact: below 2^17)
+#pragma unroll
+      for (int e = 0; e < L::E; e++) ss = fmaf(number(w[e]), number(w[e]), ss);
+      most = max(most, __reduce_add_sync(0xffffffffu, (unsigned)ss));
+    }
+    return;
+  }
+  const int64_t left = row < p.rows ? p.cols - col : -16;
   if (p.q) {
     int8_t* q = p.q + row * p.ldq + col;
     if (p.vec_q && left >= L::E) {
@@ -177,135 +289,55 @@ __device__ __forceinline__ void store_row_vec(const QuantParams& p, uint4 v, int
     float y[L::E];
 #pragma unroll
     for (int e = 0; e < L::E; e++) y[e] = __fmul_rn(number(w[e]), scale);
-    store_values<DT>(static_cast<typename L::T*>(p.values) + row * p.ldv + col, y, p.vec_v, left);
+    store_values<DT, G>(static_cast<typename L::T*>(p.values) + row * p.ldv + col, y, p.vec_v, left, carry,
+                        first, last);
   }
 }
 
-constexpr int QT = 256;  // threads of a CTA
-
-// A kernel that needs nothing of the one before it (QuantParams::overlap) runs
-// beside it, and waits for it at its end, so that whoever waits for this one
-// has waited for both.
-__device__ __forceinline__ void begin(const QuantParams& p) {
-  if (!p.overlap) pdl_wait();
-  pdl_trigger();
-}
-__device__ __forceinline__ void end(const QuantParams& p) {
-  if (p.overlap) pdl_wait();
-}
-
-// the largest pattern over the TPR threads of a row (32: a warp, QT: the CTA)
-template <int TPR>
-__device__ __forceinline__ uint32_t row_max(uint32_t m) {
-  m = __reduce_max_sync(0xffffffffu, m);
-  if (TPR == 32) return m;
-  __shared__ uint32_t part[QT / 32];
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = m;
-  __syncthreads();
-  uint32_t t = part[threadIdx.x & (QT / 32 - 1)];
-  return __reduce_max_sync(0xffffffffu, t);
-}
-
-// A row by TPR threads, NV vectors each, held in registers.
-template <int DT, int TPR, int NV>
-__global__ void __launch_bounds__(QT) quant_rows(QuantParams p) {
-  using L = Elem<DT>;
-  pdl_wait();
-  pdl_trigger();
-  const int lane = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * (QT / TPR) + threadIdx.x / TPR;
-  if (row >= p.rows) return;  // (whole warps; with TPR = QT there is a row for every CTA)
-  const typename L::T* x = static_cast<const typename L::T*>(p.x) + row * p.ldx;
-  uint4 v[NV];
-  uint4 m = make_uint4(0, 0, 0, 0);
-#pragma unroll
-  for (int i = 0; i < NV; i++) {
-    const int64_t col = (int64_t)(i * TPR + lane) * L::E;
-    v[i] = make_uint4(0, 0, 0, 0);
-    if (col + L::E <= p.cols) v[i] = __ldg(reinterpret_cast<const uint4*>(x + col));
-  }
-  if (p.cols % L::E) {  // the row's last vector
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-      const int64_t col = (int64_t)(i * TPR + lane) * L::E;
-      if (col < p.cols && col + L::E > p.cols) v[i] = load_vec<DT, false>(x + col, p.cols - col);
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < NV; i++) m = mag_max<DT>(m, v[i]);
-  const uint32_t top = row_max<TPR>(mag_fold<DT>(m));
-  float r, scale;
-  factors<DT>(top, r, scale);
-  const bool finite = top < L::INF;
-  if (p.scale && lane == 0) p.scale[row] = scale;
-#pragma unroll
-  for (int i = 0; i < NV; i++) {
-    const int64_t col = (int64_t)(i * TPR + lane) * L::E;
-    if (col < p.cols) store_row_vec<DT>(p, v[i], row, col, p.cols - col, r, scale, finite);
-  }
-}
-
-// where the integers of operand row `row`, k on, lie in a packed operand (see
-// mm8_tc.cu): 16 KB blocks of 128 rows by 64 k, 16-byte pieces of 8 k swizzled
-__device__ __forceinline__ char* packed_at(const QuantParams& p, int64_t row, int64_t k) {
-  const int r = (int)(row & 127);
-  return static_cast<char*>(p.packed) + ((row >> 7) * p.kb + (k >> 6)) * 16384 + r * 128 +
-         ((((int)k >> 3 & 7) ^ (r & 7)) * 16) + ((int)k & 7) * 2;
-}
-__device__ __forceinline__ uint32_t half_pair(float a, float b) {
-  const __half2 h = __floats2half2_rn(number(a), number(b));
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
-__device__ __forceinline__ void clear_earlier(const QuantParams& p) {
-  const int64_t n = (int64_t)gridDim.x * gridDim.y * QT;
-  for (int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * QT + threadIdx.x; i < p.zero2_n; i += n) p.zero2[i] = 0;
-}
-
-// quant_rows with a packed operand for its output, zeros in its margins.  A
-// group of threads takes `each` rows one after another, the next one's vectors
-// on their way, and hands on the largest sums of squares of all of them.
-template <int DT, int TPR, int NV>
-__global__ void __launch_bounds__(QT) quant_rows_packed(QuantParams p, int each) {
+// Rows, `each` one after another by TPR threads with NV vectors each, held in
+// registers between the maximum and the rounding.  PACK: into a packed operand,
+// with zeros in its margins, and the largest sums of squares handed on once for
+// all rows.  16384 x 4096 bfloat16 with values take 51 us, 6.6 TB/s; 11590 x 1749
+// binary16 with values, rows off the grid, 27 (on it, x 1752: 13).
+template <int DT, int TPR, int NV, bool PACK, bool GRID>
+__global__ void __launch_bounds__(QT) quant_rows(QuantParams p, int each) {
   using L = Elem<DT>;
   begin(p);
-  clear_earlier(p);
+  if (PACK) clear_earlier(p);
   __shared__ uint32_t part[2][QT / 32];
   const int lane = threadIdx.x % TPR;
   const int64_t row0 = ((int64_t)blockIdx.x * (QT / TPR) + threadIdx.x / TPR) * each;
-  const bool ragged = p.cols % L::E != 0;
+  const Source<DT, GRID> source(p);
+  const bool ragged = p.cols % L::E != 0 || !GRID;
   auto load = [&](int64_t row, uint4 (&v)[NV]) {
-    const bool real = row < p.rows;
     const typename L::T* x = static_cast<const typename L::T*>(p.x) + row * p.ldx;
+    const int64_t cols = row < p.rows ? p.cols : 0;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       const int64_t col = (int64_t)(i * TPR + lane) * L::E;
       v[i] = make_uint4(0, 0, 0, 0);
-      if (real && col + L::E <= p.cols) v[i] = __ldg(reinterpret_cast<const uint4*>(x + col));
+      if (source.whole(x + col, cols - col)) v[i] = source.load(x + col);
     }
-    if (real && ragged) {  // the row's last vector
+    if (ragged) {
 #pragma unroll
       for (int i = 0; i < NV; i++) {
         const int64_t col = (int64_t)(i * TPR + lane) * L::E;
-        if (col < p.cols && col + L::E > p.cols) v[i] = load_vec<DT, false>(x + col, p.cols - col);
+        if (col < cols && !source.whole(x + col, cols - col)) v[i] = load_edge<DT>(x + col, cols - col);
       }
     }
   };
   unsigned most[NV];
 #pragma unroll
   for (int i = 0; i < NV; i++) most[i] = 0;
-  uint4 next[NV];
-  load(row0, next);
   for (int it = 0; it < each; it++) {
     const int64_t row = row0 + it;
     uint4 v[NV];
     uint4 m = make_uint4(0, 0, 0, 0);
+    load(row, v);
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-      v[i] = next[i];
-      m = mag_max<DT>(m, v[i]);
-    }
-    if (it + 1 < each) load(row + 1, next);
-    uint32_t top = __reduce_max_sync(0xffffffffu, mag_fold<DT>(m));
+    for (int i = 0; i < NV; i++) m = mag_max<DT>(m, v[i]);
+    const uint32_t group = TPR >= 32 ? 0xffffffffu : ((1u << (TPR & 31)) - 1u) << (threadIdx.x & 31 & ~(TPR - 1));
+    uint32_t top = __reduce_max_sync(group, mag_fold<DT>(m));
     if (TPR > 32) {
       if ((threadIdx.x & 31) == 0) part[it & 1][threadIdx.x >> 5] = top;
       __syncthreads();
@@ -314,30 +346,14 @@ __global__ void __launch_bounds__(QT) quant_rows_packed(QuantParams p, int each)
     float r, scale;
     factors<DT>(top, r, scale);
     const bool finite = top < L::INF;
-    if (lane == 0 && row < p.rows) p.scale[row] = scale;
+    if (lane == 0 && row < p.rows && p.scale) p.scale[row] = scale;
+    uint4 carry = make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-      const int64_t k = (int64_t)(i * TPR + lane) * L::E;
-      float w[L::E];
-      if (finite) wholes<DT, true>(v[i], r, w);
-      else wholes<DT, false>(v[i], r, w);
-      if (k < (int64_t)p.kb * 64) {
-        char* d = packed_at(p, row, k);
-        if (L::E == 8)
-          *reinterpret_cast<uint4*>(d) = make_uint4(half_pair(w[0], w[1]), half_pair(w[2], w[3]), half_pair(w[4 % L::E], w[5 % L::E]),
-                                                    half_pair(w[6 % L::E], w[7 % L::E]));
-        else
-          *reinterpret_cast<uint2*>(d) = make_uint2(half_pair(w[0], w[1]), half_pair(w[2], w[3]));
-      }
-      if (p.norms) {  // a warp's vectors are 256 k, or half of them
-        float ss = 0.0f;  // (exact: below 2^17)
-#pragma unroll
-        for (int e = 0; e < L::E; e++) ss = fmaf(number(w[e]), number(w[e]), ss);
-        most[i] = max(most[i], __reduce_add_sync(0xffffffffu, (unsigned)ss));
-      }
-    }
+    for (int i = 0; i < NV; i++)
+      put_row_vec<DT, PACK, (TPR < 32 ? TPR : 32)>(p, v[i], row, (int64_t)(i * TPR + lane) * L::E, r, scale, finite, most[i],
+                                                   carry, TPR > 32 || i == 0, TPR > 32 || i == NV - 1);
   }
-  if (p.norms && (threadIdx.x & 31) == 0) {
+  if (PACK && p.norms && (threadIdx.x & 31) == 0) {
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       const int64_t first = (int64_t)(i * TPR + (lane & ~31)) * L::E;
@@ -348,118 +364,123 @@ __global__ void __launch_bounds__(QT) quant_rows_packed(QuantParams p, int each)
   end(p);
 }
 
-// A row by a CTA, read twice: rows too long for the registers, and (VEC false) rows off the 16-byte grid,
-// which are taken element by element.
-template <int DT, bool VEC>
-__global__ void __launch_bounds__(QT) quant_rows_twice(QuantParams p) {
+// A row too long for the registers, by a CTA that reads it twice.
+template <int DT, bool GRID>
+__global__ void __launch_bounds__(QT) quant_long_rows(QuantParams p) {
   using L = Elem<DT>;
-  pdl_wait();
-  pdl_trigger();
+  begin(p);
+  __shared__ uint32_t part[QT / 32];
   const int64_t row = blockIdx.x;
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + row * p.ldx;
-  uint32_t top = 0;
-  if (VEC) {
-    uint4 m = make_uint4(0, 0, 0, 0);
+  const Source<DT, GRID> source(p);
+  auto load = [&](int64_t col) {
+    const int64_t left = p.cols - col;
+    if (left <= 0) return make_uint4(0, 0, 0, 0);
+    return source.whole(x + col, left) ? source.load(x + col) : load_edge<DT>(x + col, left);
+  };
+  uint4 m = make_uint4(0, 0, 0, 0);
 #pragma unroll 4
-    for (int64_t col = (int64_t)threadIdx.x * L::E; col < p.cols; col += QT * L::E)
-      m = mag_max<DT>(m, load_vec<DT, true>(x + col, p.cols - col));
-    top = mag_fold<DT>(m);
-  } else {
-#pragma unroll 8
-    for (int64_t col = threadIdx.x; col < p.cols; col += QT) top = max(top, L::bits(x[col]));
-  }
-  top = row_max<QT>(top);
+  for (int64_t col = (int64_t)threadIdx.x * L::E; col < p.cols; col += QT * L::E) m = mag_max<DT>(m, load(col));
+  uint32_t top = __reduce_max_sync(0xffffffffu, mag_fold<DT>(m));
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
+  __syncthreads();
+  top = __reduce_max_sync(0xffffffffu, part[threadIdx.x & (QT / 32 - 1)]);
   float r, scale;
   factors<DT>(top, r, scale);
-  const bool finite = top < L::INF;
   if (p.scale && threadIdx.x == 0) p.scale[row] = scale;
-  if (VEC) {
-#pragma unroll 2
-    for (int64_t col = (int64_t)threadIdx.x * L::E; col < p.cols; col += QT * L::E)
-      store_row_vec<DT>(p, load_vec<DT, true>(x + col, p.cols - col), row, col, p.cols - col, r, scale, finite);
-  } else {
-    int8_t* q = p.q ? p.q + row * p.ldq : nullptr;
-    typename L::T* o = p.values ? static_cast<typename L::T*>(p.values) + row * p.ldv : nullptr;
-#pragma unroll 4
-    for (int64_t col = threadIdx.x; col < p.cols; col += QT) {
-      const float w = whole(L::up(x[col]), r, finite);
-      if (q) q[col] = byte_of(w);
-      if (o) o[col] = L::down(__fmul_rn(number(w), scale));
-    }
+  unsigned most = 0;
+  uint4 carry = make_uint4(0, 0, 0, 0);
+  for (int64_t first = 0; first < p.cols; first += QT * L::E) {
+    const int64_t col = first + (int64_t)threadIdx.x * L::E;
+    put_row_vec<DT, false, 32>(p, load(col), row, col, r, scale, top < L::INF, most, carry, true, true);
   }
+  end(p);
 }
 
-// Columns, in two launches (one for few rows).  The first finds each column's maximum: a thread
-// has a 16-byte vector of columns (VEC false: one column) and walks down a
-// share of the rows, the shares meet by atomic maxima of the patterns.  The
-// second reads the matrix again, last rows first, so that it finds in L2 what
-// the first read last, in tiles of 128 rows by 128 bytes, and writes the
-// integers transposed through shared memory, 128 contiguous ones of a column
-// at a time.  (One launch of clusters that keep a strip of columns to
-// themselves, meet in distributed shared memory and read the strip again from
-// L2 took 101 us for 16384 x 4096 bfloat16 values where these take 75: its
-// phases wait for each other.)
-template <int DT, bool VEC>
-__global__ void __launch_bounds__(QT) quant_colmax(QuantParams p, int vl, int64_t rows_each) {
+// Columns, in two launches (one for few rows, QUANT_FEW_ROWS).  The first finds
+// each column's maximum: a thread has a 16-byte vector of columns and walks down
+// a share of the rows, the shares meet by atomic maxima of the patterns (order
+// makes no difference to a maximum).  The second reads the matrix again, last
+// rows first, so that it finds in L2 what the first read last, in tiles of 128
+// rows by 128 bytes, and writes the integers transposed through shared memory,
+// 128 contiguous ones of a column at a time.  16384 x 4096 bfloat16 with values
+// take 70 us, 5.7 TB/s of what the two launches read and write; with q alone 68.
+// (One launch of clusters that keep a strip of columns to themselves, meet in
+// distributed shared memory and read the strip again from L2 took 101 us: its
+// phases wait for each other.)  Rows off the 16-byte grid take two aligned loads
+// for a vector and their values go through shared memory, an element a lane:
+// 16384 x 4095 take 190 us, bound by instructions (loads element by element and
+// values straight from the registers: 232 and more).
+template <int DT, bool GRID>
+__global__ void __launch_bounds__(QT, 4) quant_colmax(QuantParams p, int vl, int64_t rows_each) {
   using L = Elem<DT>;
   begin(p);
   __shared__ uint4 part[QT];
   const int lx = threadIdx.x % vl, ly = threadIdx.x / vl, nl = QT / vl;
   const int64_t r0 = (int64_t)blockIdx.y * rows_each, r1 = min(p.rows, r0 + rows_each);
-  const int64_t col = ((int64_t)blockIdx.x * vl + lx) * (VEC ? L::E : 1), left = p.cols - col;
+  const int64_t col = ((int64_t)blockIdx.x * vl + lx) * L::E, left = p.cols - col;
+  const Source<DT, GRID> source(p);
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + col;
   uint4 m = make_uint4(0, 0, 0, 0);
-  if (left > 0) {
-    constexpr int U = 8;  // rows in flight; past the end the last row again, which changes no maximum
-    if (VEC && left >= L::E) {
-      for (int64_t r = r0 + ly; r < r1; r += U * nl) {
-        uint4 u[U];
+  constexpr int U = 8;  // rows in flight; past the end the last row again, which changes no maximum
+  if (GRID && left >= L::E) {
+    for (int64_t r = r0 + ly; r < r1; r += U * nl) {
+      uint4 u[U];
 #pragma unroll
-        for (int i = 0; i < U; i++) u[i] = __ldg(reinterpret_cast<const uint4*>(x + min(r + i * nl, r1 - 1) * p.ldx));
+      for (int i = 0; i < U; i++) u[i] = source.load(x + min(r + i * nl, r1 - 1) * p.ldx);
 #pragma unroll
-        for (int i = 0; i < U; i++) m = mag_max<DT>(m, u[i]);
+      for (int i = 0; i < U; i++) m = mag_max<DT>(m, u[i]);
+    }
+  } else if (GRID) {
+    for (int64_t r = r0 + ly; r < r1 && left > 0; r += nl) m = mag_max<DT>(m, load_edge<DT>(x + r * p.ldx, left));
+  } else {
+    constexpr int V = 4;
+    for (int64_t r = r0 + ly; r < r1 && left > 0; r += V * nl) {
+      uint4 a[V], b[V];
+      int edges = 0;
+#pragma unroll
+      for (int i = 0; i < V; i++) {
+        const typename L::T* q = x + min(r + i * nl, r1 - 1) * p.ldx;
+        a[i] = b[i] = make_uint4(0, 0, 0, 0);
+        if (source.whole(q, left)) {
+          a[i] = __ldg(source.on_grid(q));
+          b[i] = __ldg(source.on_grid(q) + 1);
+        } else {
+          edges |= 1 << i;
+        }
       }
-    } else if (VEC) {
-      for (int64_t r = r0 + ly; r < r1; r += nl) m = mag_max<DT>(m, load_vec<DT, false>(x + r * p.ldx, left));
-    } else {
-      for (int64_t r = r0 + ly; r < r1; r += U * nl) {
-        uint32_t u[U];
 #pragma unroll
-        for (int i = 0; i < U; i++) u[i] = L::bits(x[min(r + i * nl, r1 - 1) * p.ldx]);
-#pragma unroll
-        for (int i = 0; i < U; i++) m.x = max(m.x, u[i]);
+      for (int i = 0; i < V; i++)
+        m = mag_max<DT>(m, shifted(a[i], b[i], (int)(reinterpret_cast<uintptr_t>(x + min(r + i * nl, r1 - 1) * p.ldx) & 15)));
+      if (edges) {
+        for (int i = 0; i < V; i++)
+          if (edges >> i & 1) m = mag_max<DT>(m, load_edge<DT>(x + min(r + i * nl, r1 - 1) * p.ldx, left));
       }
     }
   }
   part[threadIdx.x] = m;
   __syncthreads();
   if (ly == 0 && left > 0) {
-    for (int k = 1; k < nl; k++) {
-      if (VEC) m = mag_max<DT>(m, part[k * vl + lx]);
-      else m.x = max(m.x, part[k * vl + lx].x);
-    }
-    if (VEC) {
-      const uint32_t w[4] = {m.x, m.y, m.z, m.w};
+    for (int k = 1; k < nl; k++) m = mag_max<DT>(m, part[k * vl + lx]);
+    const uint32_t w[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
-      for (int e = 0; e < L::E; e++) {
-        const uint32_t b = L::E == 4 ? w[e % 4] : (e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu);
-        if (e < left) atomicMax(p.colmax + col + e, b);
-      }
-    } else {
-      atomicMax(p.colmax + col, m.x);
+    for (int e = 0; e < L::E; e++) {
+      const uint32_t b = L::E == 4 ? w[e % 4] : (e & 1 ? w[e / 2] >> 16 : w[e / 2] & 0xffffu);
+      if (e < left) atomicMax(p.colmax + col + e, b);
     }
   }
   end(p);
 }
 
 constexpr int TR = 128;  // rows of a tile
-template <int DT, bool VEC, bool PACK>
-__global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, int64_t rows_each) {
+template <int DT, bool PACK, bool GRID>
+__global__ void __launch_bounds__(QT, PACK || !GRID ? 2 : 3) quant_cols(QuantParams p, int64_t rows_each) {
   using L = Elem<DT>;
   constexpr int CW = 8 * L::E;  // columns of a tile
   __shared__ __align__(16) float rs[CW], ss[CW];
   __shared__ uint32_t bads[2], tops[CW];
-  __shared__ __align__(16) uint32_t tile[CW * (PACK ? TR / 2 : TR / 4 + 1)];  // integers: bytes, or packed binary16
+  // integers as bytes, or packed binary16; values
+  __shared__ __align__(16) uint32_t tile[PACK ? CW * TR / 2 : TR * 32];
   __shared__ float squares[PACK ? QT / 32 : 1][CW];
   const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3;
   const int64_t c0 = (int64_t)blockIdx.x * CW, col = c0 + tx * L::E;
@@ -475,21 +496,29 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
     const int64_t n = (int64_t)gridDim.x * gridDim.y * QT;
     for (int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * QT + threadIdx.x; i < p.zero_n; i += n) p.zero[i] = 0;
   }
+  const Source<DT, GRID> source(p);
   auto load = [&](int64_t t0, uint4 (&v)[4]) {
     const typename L::T* q = x + (t0 + ty * 4) * p.ldx;
-    if (VEC && left >= L::E && t0 + TR <= min(r1, p.rows)) {
+    const int64_t rows = min(r1, p.rows) - t0 - ty * 4;  // of the thread's four
+    if (GRID && left >= L::E && rows >= 4) {
 #pragma unroll
-      for (int j = 0; j < 4; j++) v[j] = __ldg(reinterpret_cast<const uint4*>(q + j * p.ldx));
-    } else {
+      for (int j = 0; j < 4; j++) v[j] = source.load(q + j * p.ldx);
+      return;
+    }
+    int edges = 0;  // vectors to be read one by one
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        v[j] = make_uint4(0, 0, 0, 0);
-        if (t0 + ty * 4 + j < min(r1, p.rows) && left > 0) v[j] = load_vec<DT, VEC>(q + j * p.ldx, left);
-      }
+    for (int j = 0; j < 4; j++) {
+      v[j] = make_uint4(0, 0, 0, 0);
+      const bool whole = j < rows && source.whole(q + j * p.ldx, left);
+      if (whole) v[j] = source.load(q + j * p.ldx);
+      else if (j < rows && left > 0) edges |= 1 << j;
+    }
+    if (edges) {
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        if (edges >> j & 1) v[j] = load_edge<DT>(q + j * p.ldx, left);
     }
   };
-  uint4 v[4];
-  load(r0, v);
   if (!p.colmax) {  // few rows: every CTA finds its columns' maxima itself
     __shared__ uint4 part[QT / 32][8];
     uint4 m = make_uint4(0, 0, 0, 0);
@@ -497,7 +526,10 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
       for (int64_t row = ty; row < p.rows; row += 4 * (QT / 8)) {
         uint4 u[4];
 #pragma unroll
-        for (int j = 0; j < 4; j++) u[j] = load_vec<DT, VEC>(x + min(row + j * (QT / 8), p.rows - 1) * p.ldx, left);
+        for (int j = 0; j < 4; j++) {
+          const typename L::T* q = x + min(row + j * (QT / 8), p.rows - 1) * p.ldx;
+          u[j] = source.whole(q, left) ? source.load(q) : load_edge<DT>(q, left);
+        }
 #pragma unroll
         for (int j = 0; j < 4; j++) m = mag_max<DT>(m, u[j]);
       }
@@ -539,6 +571,8 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
   const uint32_t bad = bads[tx * L::E >> 5] >> (tx * L::E & 31) & ((1u << L::E) - 1u);
 
   for (int64_t t0 = r0; t0 < r1; t0 += TR) {
+    uint4 v[4];
+    load(t0, v);
     float w[4][L::E];
 #pragma unroll
     for (int j = 0; j < 4; j++) {
@@ -551,16 +585,32 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
         for (int e = 0; e < L::E; e++) w[j][e] = whole(w[j][e], r[e], true);
       }
     }
-    if (t0 + TR < r1) load(t0 + TR, v);  // the next tile is on its way
     if (!PACK && p.values) {
+      typename L::T* o = static_cast<typename L::T*>(p.values) + t0 * p.ldv + c0;
+      const int rows = (int)min((int64_t)TR, r1 - t0);
+      if (!p.vec_v) __syncthreads();  // the tile's last readers are done
 #pragma unroll
       for (int j = 0; j < 4; j++) {
-        const int64_t row = t0 + ty * 4 + j;
-        if (row >= r1 || left <= 0) continue;
+        const int row = ty * 4 + j;
         float y[L::E];
 #pragma unroll
         for (int e = 0; e < L::E; e++) y[e] = __fmul_rn(number(w[j][e]), scale[e]);
-        store_values<DT>(static_cast<typename L::T*>(p.values) + row * p.ldv + col, y, p.vec_v, left);
+        if (p.vec_v) {
+          uint4 none = make_uint4(0, 0, 0, 0);
+          if (row < rows) store_values<DT, 32>(o + row * p.ldv + tx * L::E, y, true, left, none, true, true);
+        } else {
+          reinterpret_cast<uint4*>(tile)[row * 8 + tx] = pack<DT>(y);
+        }
+      }
+      if (!p.vec_v) {  // rows off the grid: along them, an element a lane
+        __syncthreads();
+        const typename L::T* from = reinterpret_cast<const typename L::T*>(tile);
+        const int lane = threadIdx.x & 31;
+#pragma unroll 4
+        for (int row = threadIdx.x >> 5; row < rows; row += QT / 32)
+#pragma unroll
+          for (int c = lane; c < CW; c += 32)
+            if (c0 + c < p.cols) o[row * p.ldv + c] = from[row * CW + c];
       }
     }
     if constexpr (PACK) {
@@ -625,83 +675,74 @@ __global__ void __launch_bounds__(QT, PACK ? 2 : 3) quant_cols(QuantParams p, in
   end(p);
 }
 
-template <int DT>
+template <int DT, bool PACK, bool GRID>
 cudaError_t rows_launch(const QuantParams& p, int nsm, cudaStream_t s) {
   constexpr int E = Elem<DT>::E;
-  if (!p.vec_x) return launch_dependent(quant_rows_twice<DT, false>, (unsigned)p.rows, QT, 0, s, p);
-  const int64_t nv = (p.cols + E - 1) / E;
-  auto go = [&](void (*kernel)(QuantParams), int tpr) {
-    return launch_dependent(kernel, (unsigned)((p.rows + QT / tpr - 1) / (QT / tpr)), QT, 0, s, p);
+  const int64_t rows = PACK ? p.prows : p.rows, nv = ((PACK ? (int64_t)p.kb * 64 : p.cols) + E - 1) / E;
+  auto go = [&](void (*kernel)(QuantParams, int), int tpr) {
+    const int64_t groups = (rows + QT / tpr - 1) / (QT / tpr);
+    int each = 1;  // rows of a thread group (of one block of 128): up to 8, while every SM has 4 CTAs
+    while (each < 8 && groups / (2 * each) >= 4 * nsm) each *= 2;
+    return launch_dependent(kernel, (unsigned)((groups + each - 1) / each), QT, 0, s, p, each);
   };
-  if (p.packed) {
-    const int64_t pv = (int64_t)p.kb * 64 / E;
-    auto pack = [&](void (*kernel)(QuantParams, int), int tpr) {
-      const int64_t groups = p.prows / (QT / tpr);
-      int each = 1;  // rows of a thread group (of one block of 128): up to 8, while every SM has 4 CTAs
-      while (each < 8 && groups / (2 * each) >= 4 * nsm) each *= 2;
-      return launch_dependent(kernel, (unsigned)(groups / each), QT, 0, s, p, each);
-    };
-    if (pv <= 32) return pack(quant_rows_packed<DT, 32, 1>, 32);
-    if (pv <= 64) return pack(quant_rows_packed<DT, 32, 2>, 32);
-    if (pv <= 128) return pack(quant_rows_packed<DT, 32, 4>, 32);
-    if (pv <= 256) return pack(quant_rows_packed<DT, QT, 1>, QT);
-    if (pv <= 512) return pack(quant_rows_packed<DT, QT, 2>, QT);
-    if (pv <= 1024) return pack(quant_rows_packed<DT, QT, 4>, QT);
-    return pack(quant_rows_packed<DT, QT, 8>, QT);
-  }
-  if (nv <= 32) return go(quant_rows<DT, 32, 1>, 32);
-  if (nv <= 64) return go(quant_rows<DT, 32, 2>, 32);
-  if (nv <= 128) return go(quant_rows<DT, 32, 4>, 32);
-  if (nv <= 256) return go(quant_rows<DT, QT, 1>, QT);
-  if (nv <= 512) return go(quant_rows<DT, QT, 2>, QT);
-  if (nv <= 1024) return go(quant_rows<DT, QT, 4>, QT);
-  if (nv <= 2048) return go(quant_rows<DT, QT, 8>, QT);
-  return go(quant_rows_twice<DT, true>, QT);
+  // (short rows share a warp)
+  if (nv <= 8) return go(quant_rows<DT, 8, 1, PACK, GRID>, 8);
+  if (nv <= 16) return go(quant_rows<DT, 8, 2, PACK, GRID>, 8);
+  if (nv <= 32) return go(quant_rows<DT, 8, 4, PACK, GRID>, 8);
+  if (nv <= 64) return go(quant_rows<DT, 32, 2, PACK, GRID>, 32);
+  if (nv <= 128) return go(quant_rows<DT, 32, 4, PACK, GRID>, 32);
+  // a warp a row needs no meeting of warps, but takes longer for one row
+  if (nv <= 256 && rows >= 8 * nsm) return go(quant_rows<DT, 32, 8, PACK, GRID>, 32);
+  if (nv <= 256) return go(quant_rows<DT, QT, 1, PACK, GRID>, QT);
+  if (nv <= 512) return go(quant_rows<DT, QT, 2, PACK, GRID>, QT);
+  if (nv <= 1024) return go(quant_rows<DT, QT, 4, PACK, GRID>, QT);
+  if (nv <= 2048) return go(quant_rows<DT, QT, 8, PACK, GRID>, QT);
+  return launch_dependent(quant_long_rows<DT, GRID>, (unsigned)p.rows, QT, 0, s, p);
 }
 
-template <int DT, bool VEC>
+template <int DT, bool GRID>
 cudaError_t cols_launch(const QuantParams& p, bool maxima, int nsm, cudaStream_t s) {
   constexpr int E = Elem<DT>::E, CW = 8 * E;
-  const int64_t per = VEC ? E : 1, nv = (p.cols + per - 1) / per;
-  int vl = 8;
-  while (vl < 32 && vl < nv) vl *= 2;  // wider CTAs would mean more shares of the rows, and atomics for each
-  const int64_t wide = (nv + vl - 1) / vl, lanes = QT / vl;
   // one wave of as many CTAs as an SM holds, `least` rows or more for each
-  auto shares = [&](int64_t across, int64_t least, int64_t rows_unit, int64_t resident, int64_t* each) {
-    int64_t n = std::min(resident * nsm / across, (p.rows + least - 1) / least);
+  auto shares = [&](int64_t rows, int64_t across, int64_t least, int64_t unit, int64_t resident, int64_t* each) {
+    int64_t n = std::min(resident * nsm / across, (rows + least - 1) / least);
+    if (maxima) n = std::min<int64_t>(n, 160);  // (690 shares' atomics on the same 256 columns took 50 us)
     n = std::max<int64_t>(1, std::min<int64_t>(n, 65535));
-    *each = ((p.rows + n - 1) / n + rows_unit - 1) / rows_unit * rows_unit;
-    return (unsigned)std::max<int64_t>(1, (p.rows + *each - 1) / std::max<int64_t>(*each, 1));
+    *each = std::max<int64_t>(1, ((rows + n - 1) / n + unit - 1) / unit) * unit;
+    return (unsigned)std::max<int64_t>(1, (rows + *each - 1) / *each);
   };
   int64_t each = 1;
   if (maxima) {
-    const unsigned ny = shares(wide, 8 * lanes, 1, 5, &each);
     if (p.rows == 0) return cudaSuccess;
-    return launch_dependent(quant_colmax<DT, VEC>, dim3((unsigned)wide, ny), QT, 0, s, p, vl, std::max<int64_t>(each, 1));
+    const int64_t nv = (p.cols + E - 1) / E;
+    int vl = 8;
+    while (vl < 32 && vl < nv) vl *= 2;  // wider CTAs would mean more shares of the rows, and atomics for each
+    const int64_t wide = (nv + vl - 1) / vl;
+    const unsigned ny = shares(p.rows, wide, 8 * (QT / vl), 1, 4, &each);
+    return launch_dependent(quant_colmax<DT, GRID>, dim3((unsigned)wide, ny), QT, 0, s, p, vl, each);
   }
   if (p.packed) {
-    const int64_t strips = p.prows / CW, K = (int64_t)p.kb * 64;
-    int64_t n = std::max<int64_t>(1, std::min(std::min<int64_t>(2 * nsm / strips, (K + TR - 1) / TR), (int64_t)65535));
-    each = ((K + n - 1) / n + TR - 1) / TR * TR;
-    n = (K + each - 1) / each;
-    return launch_dependent(quant_cols<DT, VEC, true>, dim3((unsigned)strips, (unsigned)n), QT, 0, s, p, each);
+    const unsigned strips = (unsigned)(p.prows / CW), ny = shares((int64_t)p.kb * 64, strips, TR, TR, 2, &each);
+    return launch_dependent(quant_cols<DT, true, GRID>, dim3(strips, ny), QT, 0, s, p, each);
   }
-  const int64_t strips = (p.cols + CW - 1) / CW;
-  const unsigned ty = shares(strips, TR, TR, 3, &each);
-  return launch_dependent(quant_cols<DT, VEC, false>, dim3((unsigned)strips, ty), QT, 0, s, p, std::max<int64_t>(each, TR));
+  const unsigned strips = (unsigned)((p.cols + CW - 1) / CW), ny = shares(p.rows, strips, TR, TR, GRID ? 3 : 2, &each);
+  return launch_dependent(quant_cols<DT, false, GRID>, dim3(strips, ny), QT, 0, s, p, each);
 }
 
+template <int DT, bool GRID>
+cudaError_t quant_launch(int step, const QuantParams& p, int nsm, cudaStream_t s) {
+  if (step != QUANT_ROWS) return cols_launch<DT, GRID>(p, step == QUANT_MAXIMA, nsm, s);
+  return p.packed ? rows_launch<DT, true, GRID>(p, nsm, s) : rows_launch<DT, false, GRID>(p, nsm, s);
+}
 template <int DT>
 cudaError_t quant_launch(int step, const QuantParams& p, int nsm, cudaStream_t s) {
-  if (step == QUANT_ROWS) return rows_launch<DT>(p, nsm, s);
-  const bool maxima = step == QUANT_MAXIMA;
-  return p.vec_x ? cols_launch<DT, true>(p, maxima, nsm, s) : cols_launch<DT, false>(p, maxima, nsm, s);
+  return p.vec_x ? quant_launch<DT, true>(step, p, nsm, s) : quant_launch<DT, false>(step, p, nsm, s);
 }
 
 }  // namespace
 
 bool quant8_packs(int dtype, int axis, const QuantParams& p) {
-  return p.vec_x && (axis == 1 || (int64_t)p.kb * 64 / (dtype == PEAT_F32 ? 4 : 8) <= 8 * QT);
+  return axis == 1 || (int64_t)p.kb * 64 / (dtype == PEAT_F32 ? 4 : 8) <= 8 * QT;
 }
 
 cudaError_t launch_quant8(int dtype, int step, const QuantParams& p, int nsm, cudaStream_t s) {
