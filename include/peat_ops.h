@@ -8,20 +8,24 @@
  * (activation, weight, output gradient), and scores them against the golden
  * ones.  Here the lower precision is 8-bit integers with one scale for each
  * row of either operand: peat_quantize_i8 makes the operands,
- * peat_matmul_i8 multiplies them, peat_product_i8 does both.  A training step ends with the norm over
- * all its gradient tensors, by which they are clipped: peat_grad_norm and
- * peat_grad_clip.
+ * peat_matmul_i8 multiplies them, peat_product_i8 does both.  A training step
+ * ends with the norm over all its gradient tensors, by which they are clipped:
+ * peat_grad_norm and peat_grad_clip.
  *
  * The conventions of peat.h hold: device pointers unless said otherwise,
  * every call asynchronous on `stream`, errors as peat_status_t with the text
  * in peat_last_error(h), nothing thrown, one handle per host thread and its
  * calls in order on the GPU (its workspace is reused call after call).  The
- * workspace grows on demand, up to 2 (M + N + 384) (K + 64) bytes plus 10 MB
- * for a product; a call that has to grow it waits for the device.  After a
- * first call of the same sizes, the calls of this header do not allocate.
+ * workspace grows on demand; a call that has to grow it waits for the device.
+ * After a first call of the same sizes, the calls of this header do not
+ * allocate.  A product of many rows takes, with M and N rounded up to 256 and K
+ * to 64, 2 (M + N) K bytes, and for K above 1024 20 MB, or where that is more 4
+ * M N bytes for each of the 1, 2 or 4 parts in which K is taken; operands that
+ * peat_product_i8 rounds add a byte for each element.  A gradient list takes
+ * 32 bytes for each tensor and 100 KB, and 40 more for each of more than 800.
  *
- * The wait of a pipeline inside a product is bounded; should one expire, that
- * call's outputs are invalid and the next call of this header on the handle
+ * The waits inside a product of many rows are bounded; should one expire, that
+ * call's outputs are invalid, and the next product or compare on the handle
  * returns PEAT_ERR_TIMEOUT once.
  */
 #ifndef PEAT_OPS_H
@@ -138,15 +142,17 @@ typedef enum {
  * that with a compensation, in a fixed order: the same list gives the same
  * bits on every call.  Neither squares nor sums overflow or underflow at any
  * magnitude of g.  An infinite element makes its tensor's norm and the whole
- * norm +inf, a NaN makes them NaN.  An empty list has norm 0. */
+ * norm +inf, a NaN makes them NaN.  An empty list has norm 0.  A list of more
+ * than 800 tensors is staged in pinned memory that later calls use again: such
+ * a call cannot be captured in a CUDA graph. */
 peat_status_t peat_grad_norm(peat_handle_t h, const peat_grad_t* list, int64_t count, peat_norm_t type,
                              float unscale, peat_gradnorm_t* result, float* norms, peat_stream_t stream);
 
 /* The same, and every tensor scaled: out = g * (unscale * c), one float32
  * product of each element, rounded once to its type, with
  *   c = min(1, max_norm / (norm + eps))     (float32; NaN stays NaN)
- * max_norm >= 0 (may be +inf), eps >= 0.  With unscale * c = 1 an in-place tensor is not
- * touched (its values would not change). */
+ * max_norm >= 0 (may be +inf), eps >= 0.  With unscale * c = 1 an in-place
+ * tensor is not touched (its values would not change). */
 peat_status_t peat_grad_clip(peat_handle_t h, const peat_grad_t* list, int64_t count, peat_norm_t type,
                              float unscale, float max_norm, float eps, peat_bad_t bad, peat_gradnorm_t* result,
                              float* norms, peat_stream_t stream);

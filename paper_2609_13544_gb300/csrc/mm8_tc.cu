@@ -346,6 +346,9 @@ __device__ __forceinline__ void as_results(const int4 (&x)[8], float (&f)[32]) {
   }
 }
 
+// Polls for what a CTA has under way before it ends, whether or not an earlier
+// wait of its expired.
+constexpr uint32_t END_LIMIT = 1u << 22;
 constexpr int GROUP = 8;
 // a tile, and its part of the k range in blocks of 64
 struct Place {
@@ -512,7 +515,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       // a stage's copies have landed when its instructions are done with it
       for (int j = 0; j < STAGES && j < seq; j++) {
         const int q = seq - 1 - j;
-        mbar_wait(empty + 8 * (q % STAGES), q / STAGES & 1, p.wait_limit);
+        mbar_wait(empty + 8 * (q % STAGES), q / STAGES & 1, END_LIMIT);
       }
     }
   } else if (warp == MMA_WARP) {
@@ -557,7 +560,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
       // whatever was issued is done before the accumulators are given back
       if (elect_one()) commit_both(last, pair);
-      mbar_wait(last, 0, p.wait_limit);
+      mbar_wait(last, 0, END_LIMIT);
       __syncwarp();
     }
   } else {  // results: a warp has 32 rows and half of the columns
@@ -674,6 +677,9 @@ __global__ void __launch_bounds__(THREADS, 1)
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   cg::this_cluster().sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  // (the last arrival in the odd CTA's shared memory, before it goes)
+  if (warp == MMA_WARP && rank) mbar_wait(last, 0, END_LIMIT);
+  __syncwarp();
   if (warp == MMA_WARP)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }

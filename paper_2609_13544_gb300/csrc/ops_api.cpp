@@ -349,7 +349,10 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
   }
   if (columns) {
     ps = take(h, &s->colmax, columns, 8192, &maxima, &zero, &zero_n, st);
-    if (ps != PEAT_OK) return ps;
+    if (ps != PEAT_OK) {
+      s->norms.lost = true;  // (what it was to clear)
+      return ps;
+    }
   }
   // A launch that needs nothing of the one before it runs beside it: the
   // packing of one operand and the rounding of the other, both operands'

@@ -2,9 +2,8 @@
 
 ``peat_quantize_i8`` and ``peat_matmul_i8`` (in one call: ``peat_product_i8``)
 are a linear layer's products in 8-bit integers with a scale for each row of
-either operand; ``peat_grad_norm``
-and ``peat_grad_clip`` the norm over a list of gradient tensors and their
-clipping.  As in the rest of the binding, a ``_raw`` function fills outputs
+either operand; ``peat_grad_norm`` and ``peat_grad_clip`` the norm over a list
+of gradient tensors and their clipping.  As in the rest of the binding, a ``_raw`` function fills outputs
 that the caller holds; the plain ones allocate them.  All of them only enqueue
 work on the stream (``peat_grad_norm`` and ``peat_grad_clip``, which return
 host numbers, wait for it).
@@ -349,8 +348,8 @@ class Linear8:
         op, N, K = w
         if t.dim() < 1 or t.shape[-1] != K:
             raise ValueError(f"the last dimension of {name} must be {K}")
-        x = t if t.dim() == 2 else t.reshape(-1, K)
         with _on(stream):
+            x = t if t.dim() == 2 else t.reshape(-1, K)
             out = torch.empty(x.shape[0], N, dtype=t.dtype, device=t.device)
             a, M, _ = _operand(self.h, x, 0, None, name)
             _call(self.h, "peat_product_i8", ctypes.byref(a), ctypes.byref(op), _vector(self.h, bias, N, "bias"),
@@ -369,8 +368,9 @@ class Linear8:
         """dL/dw [out, in] in float32 from grad [..., out] and x [..., in]."""
         if grad.shape[-1:] != (self.out_features,) or x.shape[-1:] != (self.in_features,):
             raise ValueError(f"the last dimensions of grad and x must be {self.out_features} and {self.in_features}")
-        g = grad if grad.dim() == 2 else grad.reshape(-1, self.out_features)
-        x = x if x.dim() == 2 else x.reshape(-1, self.in_features)
+        with _on(stream):
+            g = grad if grad.dim() == 2 else grad.reshape(-1, self.out_features)
+            x = x if x.dim() == 2 else x.reshape(-1, self.in_features)
         if g.shape[0] != x.shape[0]:
             raise ValueError("grad and x differ in their leading dimensions")
         return peat_product_i8(self.h, g, x, 1, 1, stream=stream)

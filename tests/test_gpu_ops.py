@@ -607,3 +607,110 @@ def test_product_refusals(peat_gpu, h):
                     (op(data=None), op(), 0), (op(), op(), 100), (op(), op(), 3)):
         assert call(a, b, t) == 1 and P.peat_last_error(h)
     torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------------------
+# sizes at which another launch shape takes over
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("axis,shape", [(0, (6001, 60)), (0, (3001, 63)), (0, (2500, 1001)), (0, (40, 1001)), (0, (3, 33001)),
+                                        (1, (700, 65)), (1, (9001, 31)), (1, (513, 300)), (1, (512, 301))])
+@pytest.mark.parametrize("pad", [0, 1, 5])
+def test_quantize_rows_off_the_grid(peat_gpu, h, dtype, axis, shape, pad):
+    """Row distances and first elements off the 16-byte grid, with few and with many rows of every length class;
+    values with row distances of their own."""
+    import torch
+    rows, cols = shape
+    g = rng(rows + cols + pad)
+    off = 3 if pad else 0
+    buf = torch.randn(rows * (cols + pad) + off, generator=g, device="cuda").to(dt(dtype))
+    x = buf[off:].view(rows, cols + pad)[:, :cols]
+    x[rows // 2, cols - 1] = float("nan")
+    x[rows - 1, 0] = float("-inf")
+    check_quant(peat_gpu, h, x, axis, pad, 2 * pad)
+
+
+@pytest.mark.parametrize("axes", [(0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("mnk", [(300, 513, 257), (600, 260, 2111), (1025, 300, 600)])
+def test_product_off_the_grid(peat_gpu, h, axes, mnk):
+    """Operands off the 16-byte grid that are rounded into the tensor cores' layout on the way."""
+    import torch
+    M, N, K = mnk
+    g = rng(M + N + K)
+    ops = []
+    for rows, axis in ((M, axes[0]), (N, axes[1])):
+        shape = (K, rows) if axis else (rows, K)
+        buf = torch.randn(shape[0] * (shape[1] + 3) + 1, generator=g, device="cuda").to(torch.bfloat16)
+        ops.append(buf[1:].view(shape[0], shape[1] + 3)[:, : shape[1]])
+    want = [quant_definition(x, axis)[:2] for x, axis in zip(ops, axes)]
+    exact = sums(want[0][0], want[1][0]).float() * (want[0][1][:, None] * want[1][1][None, :])
+    out = torch.full((M, N + 3), 7.0, device="cuda")
+    peat_gpu.peat_product_i8_raw(h, ops[0], ops[1], out[:, :N], *axes)
+    assert same_bits(out[:, :N], exact) and bool((out[:, N:] == 7).all())
+
+
+def test_quantize_and_product_sizes_in_turn(peat_gpu, h):
+    """Column maxima and sums of squares live in two halves of a workspace, used and cleared in turn by calls of
+    different sizes: a large matrix leaves nothing behind for a small one."""
+    import torch
+    g = rng(77)
+    xs = [(torch.randn(r, c, generator=g, device="cuda") * s).to(torch.bfloat16)
+          for r, c, s in ((600, 900, 1e4), (2000, 40, 1e-3), (700, 20000, 1e3), (515, 9, 1.0), (600, 900, 1e-2))]
+    pairs = [(torch.randn(M, K, generator=g, device="cuda") * s, torch.randn(N, K, generator=g, device="cuda"))
+             for M, N, K, s in ((600, 300, 5000, 1.0), (300, 260, 1500, 1e-3), (900, 500, 9000, 1.0))]
+    for _ in range(3):
+        got = []
+        for i, x in enumerate(xs):
+            got.append(peat_gpu.peat_quantize_i8(h, x, 1))
+            a, b = pairs[i % 3]
+            got.append(peat_gpu.peat_product_i8(h, a, b))
+        for i, x in enumerate(xs):
+            q, s, _ = quant_definition(x, 1)
+            assert torch.equal(got[2 * i][0], q) and same_bits(got[2 * i][1], s)
+            a, b = (quant_definition(t, 0)[:2] for t in pairs[i % 3])
+            assert same_bits(got[2 * i + 1], sums(a[0], b[0]).float() * (a[1][:, None] * b[1][None, :]))
+
+
+# ---------------------------------------------------------------------------
+# lists longer than a kernel argument holds, waits that expire
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("count", [96, 97, 800, 801, 2500])
+def test_grad_long_lists(peat_gpu, h, count):
+    """As many tensors as travel with the launch, one more, and many more, clipped in place and elsewhere."""
+    import torch
+    ts = grads([(i * 37) % 301 for i in range(count)], ("bf16", "f32", "f16"), count, 0.1)
+    check_list(peat_gpu, h, ts, max_norm=0.5, outs=[torch.empty_like(t) for t in ts])
+    check_list(peat_gpu, h, ts, max_norm=0.5)
+
+
+def test_grad_long_lists_in_a_row(peat_gpu, h):
+    """More calls than staging buffers, the lists growing and shrinking, with nothing waiting between them."""
+    import torch
+    lists = [grads([20 + i] * (801 + 300 * (i % 5)), ("f32",), i) for i in range(11)]
+    recs = [torch.zeros(16, dtype=torch.uint8, device="cuda") for _ in lists]
+    glists = [peat_gpu.GradList(ts) for ts in lists]
+    torch.cuda._sleep(20_000_000)
+    for ts, r in zip(glists, recs):
+        peat_gpu.peat_grad_norm_raw(h, ts, r)
+    for ts, r in zip(lists, recs):
+        w = norm64(torch.cat(ts), "2")
+        assert abs(r.view(torch.float32)[0].item() - w) <= TOL["2"] * w
+
+
+def test_expired_wait_is_reported(peat_gpu, h):
+    """A handle whose bounded waits give up at once: the product returns, the next one reports it, and other handles
+    go on."""
+    import torch
+    g = rng(3)
+    a, b = ints(2100, 1024, "uniform", g), ints(2060, 1024, "uniform", g)
+    out = torch.empty(2100, 2060, dtype=torch.int32, device="cuda")
+    bad = peat_gpu.Handle(0, flags=peat_gpu.PEAT_FLAG_TEST_EXPIRE_WAITS)
+    for _ in range(2):
+        peat_gpu.peat_matmul_i8_raw(bad, a, None, b, None, out)
+        torch.cuda.synchronize()
+        with pytest.raises(peat_gpu.PeatError) as e:
+            peat_gpu.peat_matmul_i8_raw(bad, a, None, b, None, out)
+        assert e.value.status == 5
+    bad.close()
+    peat_gpu.peat_matmul_i8_raw(h, a, None, b, None, out)
+    assert torch.equal(out.to(torch.int64), sums(a, b))
