@@ -132,18 +132,17 @@ __global__ void __launch_bounds__(256) mm8_pack(PackParams p) {
 constexpr int STAGES = 6, STAGE = 2 * BLK;  // a CTA's block of a and block of b
 constexpr int EPI_WARPS = 8, COPY_WARP = EPI_WARPS, MMA_WARP = COPY_WARP + 1, PLAN_WARP = MMA_WARP + 1;
 constexpr int THREADS = (PLAN_WARP + 1) * 32;
-constexpr int EPI_ROWS = 32 * 64;  // a result warp's 64 bytes of each of its rows, for outputs off the vector grid
 constexpr int MAX_GROUPS = 16;     // of 32 norm blocks: K up to 131072
 struct Slot {                      // a planned tile
   int tile, mt, nt, k0, k1;        // its place; its part of the k range in blocks of 64
   int pieces;                      // times its accumulator is read
+  int exact;                       // float32 holds the whole sum, over all parts of the k range
   uint32_t drain[MAX_GROUPS];      // bit i of word g: drained before norm block k0 / 4 + 32 g + i
   alignas(16) float sb[256];
   float bias[256];
 };
 constexpr int SLOTS = 4;
-constexpr int AT_ROWS = STAGES * STAGE, AT_SLOTS = AT_ROWS + EPI_WARPS * EPI_ROWS,
-              AT_BARS = AT_SLOTS + SLOTS * (int)sizeof(Slot), BARS = 256;
+constexpr int AT_SLOTS = STAGES * STAGE, AT_BARS = AT_SLOTS + SLOTS * (int)sizeof(Slot), BARS = 256;
 static_assert(AT_BARS % 16 == 0, "barriers are aligned");
 constexpr int SMEM = AT_BARS + BARS + 1024;
 constexpr float LIMIT = 16777216.0f;  // 2^24
@@ -290,60 +289,111 @@ __device__ __forceinline__ void results(const float* v, float sa, const float* s
     }
   }
 }
-// 32 columns of a warp's 32 rows, a row a lane.  Where the rows lie on 32-byte
-// boundaries each lane writes its sectors itself; elsewhere they go through
-// shared memory, 64 bytes of a row at a time (pieces swizzled against bank
-// conflicts), and out element by element along the rows.
+// The elements [lo, hi) of a 32-byte sector: aligned pieces, each as large as fits.
+template <int OUT>
+__device__ __forceinline__ void store_part(void* sector, const uint32_t (&w)[8], int lo, int hi) {
+  constexpr int B = (int)sizeof(typename Mm8Out<OUT>::T), E = 32 / B;
+  if (lo <= 0 && hi >= E) return store_sector(sector, w);
+  char* d = static_cast<char*>(sector);
+  auto in = [&](int from, int n) { return from >= lo && from + n <= hi; };
+#pragma unroll
+  for (int i = 0; i < 8; i += 4)
+    if (in(i * 4 / B, 16 / B)) *reinterpret_cast<uint4*>(d + 4 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
+#pragma unroll
+  for (int i = 0; i < 8; i += 2)
+    if (in(i * 4 / B, 8 / B) && !in((i & ~3) * 4 / B, 16 / B)) *reinterpret_cast<uint2*>(d + 4 * i) = make_uint2(w[i], w[i + 1]);
+#pragma unroll
+  for (int i = 0; i < 8; i++)
+    if (in(i * 4 / B, 4 / B) && !in((i & ~1) * 4 / B, 8 / B)) *reinterpret_cast<uint32_t*>(d + 4 * i) = w[i];
+  if (B == 2) {
+#pragma unroll
+    for (int i = 0; i < 16; i++)
+      if (in(i, 1) && !in(i & ~1, 2)) *reinterpret_cast<uint16_t*>(d + 2 * i) = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+  }
+}
+// A sector's words where the row is `s` elements off the sectors: x holds the
+// words before the sector's place in the row, then the eight from there on.
+template <int OUT>
+__device__ __forceinline__ void sector_at(const uint32_t (&x)[16], int s, uint32_t (&w)[8]) {
+  constexpr int B = (int)sizeof(typename Mm8Out<OUT>::T);
+  const int words = s * B / 4;
+  uint32_t y[16];
+  y[0] = x[0];
+#pragma unroll
+  for (int i = 1; i < 16; i++) y[i] = B == 2 ? __funnelshift_l(x[i - 1], x[i], 16 * (s & 1)) : x[i];
+#pragma unroll
+  for (int by = 4; by; by /= 2)
+#pragma unroll
+    for (int i = 15; i >= 9 - by; i--) y[i] = words & by ? y[max(i - by, 0)] : y[i];
+#pragma unroll
+  for (int i = 0; i < 8; i++) w[i] = y[8 + i];
+}
+// 32 columns of a warp's 32 rows, a row a lane, in a run of such calls from left
+// to right.  Each lane writes whole 32-byte sectors of its row: where the row is
+// off them, its words are shifted by what it is off, the last ones of the call
+// before (carry) in front, and the ends of the run go in smaller pieces.
+// (Through shared memory and out along the rows, 64 bytes of a row at a time,
+// half of the sectors are written in two parts: 1024 x 50257 x 1024 to binary16
+// took 102 us.)
 template <int OUT>
 __device__ __forceinline__ void put_columns(const TcParams& p, const float (&v)[32], float sa, const float* sb,
-                                            const float* bias, char* stage, int64_t row0, int rows, int64_t col0) {
+                                            const float* bias, int64_t row0, int rows, int64_t col0, bool first,
+                                            bool last, uint32_t (&carry)[8]) {
   using T = typename Mm8Out<OUT>::T;
-  constexpr int B = (int)sizeof(T);
+  constexpr int B = (int)sizeof(T), E = 32 / B;
   const int lane = threadIdx.x & 31;
   const bool biased = p.m.bias != nullptr;
-  T* out = static_cast<T*>(p.m.out) + row0 * p.m.ldo + col0;
   const int64_t left = p.m.N - col0;  // columns
+  if (left <= 0) return;
+  T* o = static_cast<T*>(p.m.out) + (row0 + lane) * p.m.ldo + col0;
   if (p.vec_out && left >= 32) {
-    T* o = out + lane * p.m.ldo;
 #pragma unroll
-    for (int c = 0; c < 32; c += 32 / B) {
+    for (int c = 0; c < 32; c += E) {
       uint32_t w[8];
-      results<OUT, 32 / B>(v + c, sa, sb + c, bias + c, biased, w);
+      results<OUT, E>(v + c, sa, sb + c, bias + c, biased, w);
       if (lane < rows) store_sector(o + c, w);
     }
     return;
   }
-  constexpr int E = 16 / B, STEP = 4 * E;
+  const int s = (int)(reinterpret_cast<uintptr_t>(o) & 31) / B;
+  const int n = lane < rows ? (int)min(left, (int64_t)32) : -32;  // the lane's columns
+  o -= s;
+  uint32_t x[16], w[8];
 #pragma unroll
-  for (int c = 0; c < 32; c += STEP) {
-    __syncwarp();
+  for (int i = 0; i < 8; i++) x[i] = carry[i];
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      uint32_t w[4];
-      results<OUT, E>(v + c + j * E, sa, sb + c + j * E, bias + c + j * E, biased, w);
-      *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ (lane >> 1 & 3)) * 16)) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    __syncwarp();
-    auto at = [&](int r, int e) {  // element e of row r
-      return reinterpret_cast<const T*>(stage + r * 64 + (((e / E) ^ (r >> 1 & 3)) * 16) + (e % E) * B);
-    };
-    const int e = lane % STEP;
-    if (c + e < left) {
-#pragma unroll 8
-      for (int r = lane / STEP; r < rows; r += 32 / STEP) out[r * p.m.ldo + c + e] = *at(r, e);
-    }
+  for (int c = 0; c < 32; c += E) {
+    results<OUT, E>(v + c, sa, sb + c, bias + c, biased, w);
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[8 + i] = w[i];
+    sector_at<OUT>(x, s, w);
+    store_part<OUT>(o + c, w, first && c == 0 ? s : 0, s + n - c);
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[i] = x[8 + i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i++) carry[i] = x[i];
+  if (last || left <= 32) {
+    sector_at<OUT>(x, s, w);
+    store_part<OUT>(o + 32, w, 0, s + n - 32);
   }
 }
 
-// integer sums as put_columns takes them
+// integer sums (exact: in float32) as put_columns takes them
 template <int OUT>
-__device__ __forceinline__ void as_results(const int4 (&x)[8], float (&f)[32]) {
+__device__ __forceinline__ void as_results(const int4 (&x)[8], bool exact, float (&f)[32]) {
 #pragma unroll
   for (int j = 0; j < 8; j++) {
     const int v[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
 #pragma unroll
-    for (int i = 0; i < 4; i++) f[4 * j + i] = OUT == PEAT_OUT_I32 ? __int_as_float(v[i]) : __int2float_rn(v[i]);
+    for (int i = 0; i < 4; i++) {
+      if (OUT == PEAT_OUT_I32) f[4 * j + i] = __int_as_float(exact ? __float2int_rn(__int_as_float(v[i])) : v[i]);
+      else f[4 * j + i] = exact ? __int_as_float(v[i]) : __int2float_rn(v[i]);
+    }
   }
+}
+__device__ __forceinline__ int add_sum(int a, int b, bool exact) {
+  return exact ? __float_as_int(__fadd_rn(__int_as_float(a), __int_as_float(b))) : a + b;
 }
 
 // Polls for what a CTA has under way before it ends, whether or not an earlier
@@ -390,18 +440,28 @@ __device__ void plan_drains(const TcParams& p, const Place& t, Slot* slot) {
   const uint2* nb = p.nb + (int64_t)t.nt * 2 * p.kc;
   int pieces = 1;
   float run = 0.0f;  // the bound of what the accumulator holds
-  if (p.m.K <= FREE_K && lane == 0) slot->drain[0] = 0;
-  for (int c0 = t.k0 / 4, w = 0; p.m.K > FREE_K && c0 * 4 < t.k1; c0 += 32, w++) {
-    const int c = c0 + lane;
-    float mine = 0.0f;
-    if (c * 4 < t.k1) {
-      const uint2 a0 = __ldcg(na + c), a1 = __ldcg(na + p.kc + c), b0 = __ldcg(nb + c), b1 = __ldcg(nb + p.kc + c);
-      const unsigned a = max(a0.x + a0.y, a1.x + a1.y), b = max(b0.x + b0.y, b1.x + b1.y);
-      mine = sqrtf((float)a) * sqrtf((float)b) * 1.00001f;  // (rounded up)
-    }
-    float all = mine;
+  bool exact = true;
+  auto bound = [&](int c, int end) {  // of the products of norm block c
+    if (c >= end) return 0.0f;
+    const uint2 a0 = __ldcg(na + c), a1 = __ldcg(na + p.kc + c), b0 = __ldcg(nb + c), b1 = __ldcg(nb + p.kc + c);
+    const unsigned a = max(a0.x + a0.y, a1.x + a1.y), b = max(b0.x + b0.y, b1.x + b1.y);
+    return sqrtf((float)a) * sqrtf((float)b) * 1.00001f;  // (rounded up)
+  };
+  auto over_warp = [](float x) {
 #pragma unroll
-    for (int o = 16; o; o /= 2) all += __shfl_xor_sync(0xffffffffu, all, o);
+    for (int o = 16; o; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+  };
+  if (p.m.K > FREE_K && p.splits > 1) {
+    float all = 0.0f;
+    for (int c = lane; c < p.kc; c += 32) all += bound(c, p.kc);
+    exact = over_warp(all) <= LIMIT;
+  } else if (p.m.K > FREE_K) {
+    exact = false;
+  }
+  if (exact && lane < MAX_GROUPS) slot->drain[lane] = 0;
+  for (int c0 = t.k0 / 4, w = 0; !exact && c0 * 4 < t.k1; c0 += 32, w++) {
+    const float mine = bound(c0 + lane, (t.k1 + 3) / 4), all = over_warp(mine);
     uint32_t mask = 0;
     if (run + all <= LIMIT) {
       run += all;
@@ -426,6 +486,7 @@ __device__ void plan_drains(const TcParams& p, const Place& t, Slot* slot) {
     slot->k0 = t.k0;
     slot->k1 = t.k1;
     slot->pieces = pieces;
+    slot->exact = exact;
   }
 }
 
@@ -481,6 +542,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   pdl_trigger();
 
   bool ok = true;
+  float sa = 1.0f;  // of the lane's row of results
   if (warp == PLAN_WARP) {
     int i = 0;
     for (int u = first; u < units && ok; u += step, i++) {
@@ -523,14 +585,17 @@ __global__ void __launch_bounds__(THREADS, 1)
       int seq = 0, chunk = 0, i = 0;
       for (int u = first; u < units && ok; u += step, i++) {
         const Slot* t = slots + i % SLOTS;
-        if (!(ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
-        const int k0 = t->k0, k1 = t->k1;
+        const Place at = place_of(p, u, part);
+        const int k0 = at.k0, k1 = at.k1;
         uint32_t mask = 0;
-        bool fresh = true;  // the accumulator starts anew
+        bool fresh = true, known = false;  // the accumulator starts anew; the plan is there
         for (int k = k0; k < k1; k++, seq++) {
-          if (k == k0 || (k & 3) == 0) {
-            const int c = k / 4 - k0 / 4;
-            if ((c & 31) == 0) mask = t->drain[c >> 5];
+          const int c = k / 4 - k0 / 4;
+          // (no drain comes before the fourth norm block: three hold less than 2^24)
+          if (c >= 3 && (k & 3) == 0) {
+            if (!known && !(ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
+            if (!known || (c & 31) == 0) mask = t->drain[c >> 5];
+            known = true;
             if (mask >> (c & 31) & 1) {
               if (elect_one()) commit_both(acc_full + 8 * (chunk & 1), pair);
               chunk++;
@@ -556,6 +621,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           fresh = false;
         }
         chunk++;
+        if (ok && !known) ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit);
         if (lane == 0) mbar_arrive(unplanned + 8 * (i % SLOTS));
       }
       // whatever was issued is done before the accumulators are given back
@@ -566,7 +632,6 @@ __global__ void __launch_bounds__(THREADS, 1)
   } else {  // results: a warp has 32 rows and half of the columns
     int chunk = 0, i = 0;
     const int half = warp >> 2, quarter = warp & 3;
-    char* stage = smem + AT_ROWS + warp * EPI_ROWS;
     const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + half * 128;
     const uint32_t release0 = mapa(acc_empty, even);
     for (int u = first; u < units && ok; u += step, i++) {
@@ -577,16 +642,17 @@ __global__ void __launch_bounds__(THREADS, 1)
       const int64_t col0 = (int64_t)t->nt * 256 + half * 128;
       const float *sb = t->sb + half * 128, *bias = t->bias + half * 128;
       const int rows = (int)max((int64_t)0, min((int64_t)32, p.m.M - row0));
-      const float sa = p.m.sa && lane < rows ? __ldcg(p.m.sa + row0 + lane) : 1.0f;
+      sa = p.m.sa && lane < rows ? __ldcg(p.m.sa + row0 + lane) : 1.0f;
       // One piece that is the whole sum goes straight from the accumulator to
       // the output.  Several are added up as integers in memory, in a place of
       // this CTA's.  The sum of a split tile's part (its CTA's only one) goes to
       // the stages' place in shared memory, where the other parts find it; the
       // last piece is there when the instructions are done with the stages.
-      const bool whole = pieces == 1 && !split;
+      const bool whole = pieces == 1 && !split, exact = t->exact;
       const int mine = warp * (8 * 128) + lane;
       int4* sums = p.sums + (int64_t)blockIdx.x * (EPI_WARPS * 8 * 128) + mine;
       int4* shared_sums = reinterpret_cast<int4*>(smem) + mine;
+      uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
       for (int q = 0; q < pieces && ok; q++, chunk++) {
         if (!(ok = mbar_wait(acc_full + 8 * (chunk & 1), chunk / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -604,6 +670,11 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int j = 0; j < 32; j++) f[j] = __uint_as_float(v[j]);
           if (!whole) {
+            if (exact) {  // (a split tile's)
+#pragma unroll
+              for (int j = 0; j < 8; j++) shared_sums[(g * 8 + j) * 32] = make_int4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+              continue;
+            }
             int4 x[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) x[j] = q ? sums[(g * 8 + j) * 32] : make_int4(0, 0, 0, 0);
@@ -624,12 +695,12 @@ __global__ void __launch_bounds__(THREADS, 1)
               for (int j = 0; j < 8; j++) shared_sums[(g * 8 + j) * 32] = x[j];
               continue;
             }
-            as_results<OUT>(x, f);
+            as_results<OUT>(x, false, f);
           } else if (OUT == PEAT_OUT_I32) {
 #pragma unroll
             for (int j = 0; j < 32; j++) f[j] = __int_as_float(__float2int_rn(f[j]));
           }
-          put_columns<OUT>(p, f, sa, sb + g * 32, bias + g * 32, stage, row0, rows, col0 + g * 32);
+          put_columns<OUT>(p, f, sa, sb + g * 32, bias + g * 32, row0, rows, col0 + g * 32, g == 0, g == 3, carry);
         }
       }
       if (!ok || split) break;  // (a split tile's slot is still needed)
@@ -639,36 +710,44 @@ __global__ void __launch_bounds__(THREADS, 1)
   }
   __syncwarp();
   if (split) {
-    // The parts meet: each CTA adds up its share of the columns over the pairs.
+    // The parts meet: each CTA adds up its share of the columns over the pairs,
+    // the other parts' next ones under way while it writes.
     cg::this_cluster().sync();
     if (warp < EPI_WARPS && ok) {
       const Slot* t = slots;
+      const bool exact = t->exact;
       const int half = warp >> 2, quarter = warp & 3;
       const int64_t row0 = (int64_t)t->mt * 256 + rank * 128 + quarter * 32, col0 = (int64_t)t->nt * 256 + half * 128;
       const int rows = (int)max((int64_t)0, min((int64_t)32, p.m.M - row0));
-      const float sa = p.m.sa && lane < rows ? __ldcg(p.m.sa + row0 + lane) : 1.0f;
+      const int4* own = reinterpret_cast<const int4*>(smem) + warp * (8 * 128) + lane;
+      auto other = [&](int g, int k, int4 (&y)[8]) {  // the sums of part + k
+        const uint32_t from = mapa(sptr(own + g * 8 * 32), rank + 2 * ((part + k) & (p.splits - 1)));
+#pragma unroll
+        for (int j = 0; j < 8; j++) y[j] = load_cluster(from + j * 512);
+      };
+      int4 x[8], y[8];
+      auto add = [&]() {
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+          x[j] = make_int4(add_sum(x[j].x, y[j].x, exact), add_sum(x[j].y, y[j].y, exact), add_sum(x[j].z, y[j].z, exact),
+                           add_sum(x[j].w, y[j].w, exact));
+      };
+      other(part, 1, y);
 #pragma unroll 1
       for (int g = part; g < 4; g += p.splits) {
-        const uint32_t at = sptr(smem) + (uint32_t)(((warp * 4 + g) * 8 * 32 + lane) * 16);
-        int4 x[8];
 #pragma unroll
-        for (int j = 0; j < 8; j++) x[j] = make_int4(0, 0, 0, 0);
-#pragma unroll 2
-        for (int k = 0; k < p.splits; k++) {
-          const uint32_t from = mapa(at, rank + 2 * k);
-#pragma unroll
-          for (int j = 0; j < 8; j++) {
-            const int4 y = load_cluster(from + j * 512);
-            x[j].x += y.x;
-            x[j].y += y.y;
-            x[j].z += y.z;
-            x[j].w += y.w;
-          }
+        for (int j = 0; j < 8; j++) x[j] = own[(g * 8 + j) * 32];
+        add();
+        for (int k = 2; k < p.splits; k++) {
+          other(g, k, y);
+          add();
         }
+        if (g + p.splits < 4) other(g + p.splits, 1, y);
         float f[32];
-        as_results<OUT>(x, f);
-        put_columns<OUT>(p, f, sa, t->sb + half * 128 + g * 32, t->bias + half * 128 + g * 32,
-                         smem + AT_ROWS + warp * EPI_ROWS, row0, rows, col0 + g * 32);
+        as_results<OUT>(x, exact, f);
+        uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        put_columns<OUT>(p, f, sa, t->sb + half * 128 + g * 32, t->bias + half * 128 + g * 32, row0, rows, col0 + g * 32,
+                         true, true, carry);
       }
     }
   }
