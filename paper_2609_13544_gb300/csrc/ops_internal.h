@@ -105,7 +105,7 @@ template <int N>
 struct GnInlineOf {
   GnEntry e[N];
 };
-struct GnPartial {
+struct alignas(16) GnPartial {
   double s;                // sum (or maximum)
   unsigned long long bad;  // NaN and infinite elements
 };
