@@ -46,6 +46,7 @@ constexpr int64_t MM8_STREAM_N = 8192;  // rows of b from which every SM has a w
 // A CTA of four warps takes 16 rows of b, each warp every fourth run of 64 k
 // (and each CTA of a cluster a share of those runs), straight from global
 // memory: every byte of b is used once, so nothing is gained by staging it.
+// 1 x 4096 x 1024 takes 8 us a call, as long as the host takes to make it.
 constexpr int RT = 128;  // threads
 template <int OUT, int NT, int MODE>
 __global__ void __launch_bounds__(RT) mm8_rows(Mm8Params p) {
@@ -129,21 +130,29 @@ __global__ void __launch_bounds__(RT) mm8_rows(Mm8Params p) {
 // The rows of a are turned into binary16 once per CTA, in the very registers'
 // order, and stay in shared memory (a run of 1024 k of them at a time where
 // they are longer); every warp then streams 16 rows of b past them, so a byte
-// of b costs its load, its conversion and its share of the instructions.
+// of b costs its load, its conversion and its share of the instructions.  Where
+// a CTA has few such tiles, 2 to 16 warps (`1 << shift`) share the runs of one
+// and meet in shared memory; not where that takes more rounds (two warps a tile
+// and three rounds for one and two: 29.8 us for 32 x 50257 x 1024, not 27.5).
+// 16 x 50257 x 1024 to binary16 takes 17 us, 3.1 TB/s, two thirds of it the
+// chain of a warp's 8 loads and of starting; 8 x 16384 x 4096 19 us, 3.6 TB/s
+// (a warp a tile: 36); rows off the 16-byte grid, 13 x 30001 x 2050, 33 us (49).
 constexpr int ST = 512;
 template <int OUT, int NT, int MODE>
-__global__ void __launch_bounds__(ST, NT <= 2 ? 2 : 1) mm8_stream(Mm8Params p, int runs_held) {
+__global__ void __launch_bounds__(ST, NT <= 2 ? 2 : 1) mm8_stream(Mm8Params p, int runs_held, int shift) {
   pdl_wait();
   pdl_trigger();
   extern __shared__ __align__(16) uint2 held[];  // [run][n][j][lane]
+  int* met = reinterpret_cast<int*>(held + (size_t)runs_held * NT * 4 * 32) + threadIdx.x;  // [n][i][thread]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int64_t runs = (p.K + 63) / 64, tiles = (p.N + 15) / 16;
   const int8_t *alo = p.a, *ahi = p.a + (p.M - 1) * p.lda + p.K, *blo = p.b, *bhi = p.b + (p.N - 1) * p.ldb + p.K;
   const int64_t t0 = tiles * blockIdx.x / gridDim.x, t1 = tiles * (blockIdx.x + 1) / gridDim.x;
   typename Mm8Out<OUT>::T* out = static_cast<typename Mm8Out<OUT>::T*>(p.out);
   constexpr int U = NT <= 2 ? 2 : 4;  // runs of b in flight
-  for (int64_t round = t0; round < t1; round += ST / 32) {
-    const int64_t tile = round + warp, n0 = tile * 16;
+  const int parts = 1 << shift, part = warp & (parts - 1);
+  for (int64_t round = t0; round < t1; round += ST / 32 >> shift) {
+    const int64_t tile = round + (warp >> shift), n0 = tile * 16;
     const bool mine = tile < t1;
     float c[NT][4];
     int sum[NT][4];
@@ -156,6 +165,17 @@ __global__ void __launch_bounds__(ST, NT <= 2 ? 2 : 1) mm8_stream(Mm8Params p, i
     const bool has0 = mine && n0 + g < p.N, has1 = mine && n0 + g + 8 < p.N;
     for (int64_t k0 = 0; k0 < runs; k0 += runs_held) {
       const int here = (int)min((int64_t)runs_held, runs - k0);
+      const int first = here * part >> shift, end = here * (part + 1) >> shift;  // of the warp
+      uint4 u0[U], u1[U];
+      auto load = [&](int r) {
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+          const int64_t k = (k0 + r + u) * 64, left = r + u < end ? p.K - k - 16 * t : 0;
+          u0[u] = load16<MODE>(w0 + k, has0 ? left : 0, blo, bhi);
+          u1[u] = load16<MODE>(w1 + k, has1 ? left : 0, blo, bhi);
+        }
+      };
+      if (NT <= 2) load(first);  // under way while the rows of a are turned (more rows take the registers)
       if (round == t0 || runs > runs_held) {
         __syncthreads();  // the last readers are done
         for (int i = warp; i < here * NT; i += ST / 32) {
@@ -173,17 +193,11 @@ __global__ void __launch_bounds__(ST, NT <= 2 ? 2 : 1) mm8_stream(Mm8Params p, i
       }
       if (mine) {
         int since = 0;
-        for (int r = 0; r < here; r += U) {
-          uint4 u0[U], u1[U];
+        for (int r = first; r < end; r += U) {
+          if (NT > 2 || r > first) load(r);
 #pragma unroll
           for (int u = 0; u < U; u++) {
-            const int64_t k = (k0 + r + u) * 64, left = r + u < here ? p.K - k - 16 * t : 0;
-            u0[u] = load16<MODE>(w0 + k, has0 ? left : 0, blo, bhi);
-            u1[u] = load16<MODE>(w1 + k, has1 ? left : 0, blo, bhi);
-          }
-#pragma unroll
-          for (int u = 0; u < U; u++) {
-            if (r + u >= here) break;
+            if (r + u >= end) break;
             const uint2* x = held + (size_t)(r + u) * NT * 4 * 32 + lane;
 #pragma unroll
             for (int j = 0; j < 4; j++) {
@@ -206,7 +220,21 @@ __global__ void __launch_bounds__(ST, NT <= 2 ? 2 : 1) mm8_stream(Mm8Params p, i
         drain(c, sum);
       }
     }
-    if (!mine) continue;
+    if (parts > 1) {
+      if (part)
+#pragma unroll
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+          for (int i = 0; i < 4; i++) met[(n * 4 + i) * ST] = sum[n][i];
+      __syncthreads();
+      for (int k = 1; k < parts && part == 0; k++)
+#pragma unroll
+        for (int n = 0; n < NT; n++)
+#pragma unroll
+          for (int i = 0; i < 4; i++) sum[n][i] += met[(n * 4 + i) * ST + k * 32];
+      __syncthreads();
+    }
+    if (!mine || part) continue;
 #pragma unroll
     for (int n = 0; n < NT; n++)
 #pragma unroll
@@ -385,11 +413,15 @@ cudaError_t stream(const Mm8Params& p, int nsm, cudaStream_t s) {
   const int64_t runs = (p.K + 63) / 64, tiles = (p.N + 15) / 16;
   constexpr int RUN = NT * 1024, CTAS = NT <= 2 ? 2 : 1, MOST = 16 * 8 * 1024;  // bytes of a held run; of all of them
   const int held = (int)std::min<int64_t>(runs, (CTAS == 2 ? MOST / 2 : MOST) / RUN);
+  constexpr int MET = NT * 4 * ST * 4;  // what the parts of tiles meet in
   static std::atomic<uint64_t> allowed{0};
-  cudaError_t e = allow_smem(mm8_stream<OUT, NT, MODE>, MOST, allowed);
+  cudaError_t e = allow_smem(mm8_stream<OUT, NT, MODE>, MOST + MET, allowed);
   if (e != cudaSuccess) return e;
   const unsigned ctas = (unsigned)std::min<int64_t>(CTAS * (int64_t)nsm, tiles);
-  return launch_dependent(mm8_stream<OUT, NT, MODE>, ctas, ST, (size_t)held * RUN, s, p, held);
+  const int64_t most = (tiles + ctas - 1) / ctas;  // tiles of a CTA
+  int shift = 0;  // 2^shift parts of two runs or more
+  while ((2 * most << shift) <= ST / 32 && runs >= 4 << shift) shift++;
+  return launch_dependent(mm8_stream<OUT, NT, MODE>, ctas, ST, (size_t)held * RUN + (shift ? MET : 0), s, p, held, shift);
 }
 
 template <int OUT, int MODE>

@@ -11,28 +11,26 @@
 #include <cuda_fp16.h>
 
 #include "ops_internal.h"
+#include "vec16.cuh"
 
 namespace peat {
 
 constexpr int MM8_EXACT_K = 512;  // products whose float32 sum is exact
 
 // 16 integers of a row from p on, of which `left` (may be <= 0) exist; zeros
-// beyond.  MODE 16: p is 16-byte aligned; else any alignment, by the 4-byte
-// words that lie inside [lo, hi), the tensor's span.
+// beyond.  MODE 16: p is 16-byte aligned; else any alignment, by the two aligned
+// vectors that hold them where those lie inside [lo, hi), the tensor's span.
 template <int MODE>
 __device__ __forceinline__ uint4 load16(const int8_t* p, int64_t left, const int8_t* lo, const int8_t* hi) {
   if (left <= 0) return make_uint4(0, 0, 0, 0);
   uint4 v;
   if (MODE == 16 && left >= 16) return __ldg(reinterpret_cast<const uint4*>(p));
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3;
-  const uint32_t* w = reinterpret_cast<const uint32_t*>(a);
-  const int mis = (int)(reinterpret_cast<uintptr_t>(p) & 3);
-  if (a >= reinterpret_cast<uintptr_t>(lo) && a + 20 <= reinterpret_cast<uintptr_t>(hi)) {
-    const uint32_t w0 = __ldg(w), w1 = __ldg(w + 1), w2 = __ldg(w + 2), w3 = __ldg(w + 3), w4 = __ldg(w + 4);
-    v.x = __funnelshift_r(w0, w1, 8 * mis);
-    v.y = __funnelshift_r(w1, w2, 8 * mis);
-    v.z = __funnelshift_r(w2, w3, 8 * mis);
-    v.w = __funnelshift_r(w3, w4, 8 * mis);
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15;
+  if (MODE == 16 && p + 16 <= hi) {
+    v = __ldg(reinterpret_cast<const uint4*>(p));
+  } else if (MODE != 16 && a >= reinterpret_cast<uintptr_t>(lo) && a + 32 <= reinterpret_cast<uintptr_t>(hi)) {
+    const uint4* w = reinterpret_cast<const uint4*>(a);
+    v = shifted(__ldg(w), __ldg(w + 1), (int)(reinterpret_cast<uintptr_t>(p) & 15));
   } else {  // the tensor's first and last bytes
     uint32_t t[4] = {0, 0, 0, 0};
 #pragma unroll

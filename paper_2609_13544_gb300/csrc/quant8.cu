@@ -109,18 +109,6 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
                      __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
 }
 
-// bytes [by, by + 16) of the 32 of a and b
-__device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, int by) {
-  uint32_t t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-  const bool one = by & 4, two = by & 8;
-#pragma unroll
-  for (int i = 0; i < 7; i++) t[i] = one ? t[i + 1] : t[i];
-#pragma unroll
-  for (int i = 0; i < 5; i++) t[i] = two ? t[i + 2] : t[i];
-  const int bits = (by & 3) * 8;
-  return make_uint4(__funnelshift_r(t[0], t[1], bits), __funnelshift_r(t[1], t[2], bits),
-                    __funnelshift_r(t[2], t[3], bits), __funnelshift_r(t[3], t[4], bits));
-}
 // Vectors of E elements at any multiple of the element's size.  On the 16-byte
 // grid one load; off it the two aligned vectors that hold it, shifted together.
 // A vector that is not whole (`left` elements exist), or whose aligned vectors

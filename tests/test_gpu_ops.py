@@ -714,3 +714,17 @@ def test_expired_wait_is_reported(peat_gpu, h):
     bad.close()
     peat_gpu.peat_matmul_i8_raw(h, a, None, b, None, out)
     assert torch.equal(out.to(torch.int64), sums(a, b))
+
+
+@pytest.mark.parametrize("mnk", [(1, 8192, 64), (5, 8200, 700), (9, 9001, 131), (16, 20000, 260), (17, 8193, 1025), (33, 8192, 1500),
+                                 (64, 8210, 4200)])
+def test_matmul_few_rows_past_many(peat_gpu, h, mnk):
+    """Few rows of a past many of b, the runs of a tile shared by several warps, with rows on the 16-byte grid and off it."""
+    import torch
+    M, N, K = mnk
+    g = rng(sum(mnk))
+    for pad in (-K % 16, 3 - K % 2):
+        a, b = ints(M, K, "uniform", g, pad), ints(N, K, "uniform", g, pad)
+        out = torch.empty(M, N, dtype=torch.int32, device="cuda")
+        peat_gpu.peat_matmul_i8_raw(h, a, None, b, None, out)
+        assert torch.equal(out.to(torch.int64), sums(a, b))
