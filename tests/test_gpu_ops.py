@@ -630,6 +630,16 @@ def test_quantize_rows_off_the_grid(peat_gpu, h, dtype, axis, shape, pad):
     check_quant(peat_gpu, h, x, axis, pad, 2 * pad)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("cols", [1100, 2048, 2500, 4096])
+def test_quantize_many_long_rows(peat_gpu, h, dtype, cols):
+    """Rows enough for a warp each, longer than the shorter kernels hold."""
+    import torch
+    x = torch.randn(1601, cols, generator=rng(cols), device="cuda").to(dt(dtype))
+    x[800, cols // 2] = float("inf")
+    check_quant(peat_gpu, h, x, 0)
+
+
 @pytest.mark.parametrize("axes", [(0, 0), (0, 1), (1, 0), (1, 1)])
 @pytest.mark.parametrize("mnk", [(300, 513, 257), (600, 260, 2111), (1025, 300, 600)])
 def test_product_off_the_grid(peat_gpu, h, axes, mnk):
