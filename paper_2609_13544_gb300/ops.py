@@ -90,16 +90,29 @@ def _on(stream):
     return torch.cuda.stream(stream)
 
 
+_codes = {}  # by torch type; filled by the first use (an import of torch within each call would take 0.3 us)
+
+
+def _code_or_int8(t) -> Optional[int]:
+    """A tensor's type code, INT8's among them; None for other types."""
+    c = _codes.get(t.dtype)
+    if c is None and not _codes:
+        import torch
+        _codes.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.int8: INT8, torch.int32: OUT_I32})
+        c = _codes.get(t.dtype)
+    return c if c != OUT_I32 else None
+
+
 def _code(t) -> int:
-    import torch
-    d = t.dtype
-    if d is torch.float32:
-        return 0
-    if d is torch.bfloat16:
-        return 2
-    if d is torch.float16:
-        return 1
-    raise TypeError(f"unsupported dtype {d}: float32, float16 or bfloat16")
+    c = _code_or_int8(t)
+    if c is None or c == INT8:
+        raise TypeError(f"unsupported dtype {t.dtype}: float32, float16 or bfloat16")
+    return c
+
+
+def _is_int32(t) -> bool:
+    _code_or_int8(t)
+    return _codes.get(t.dtype) == OUT_I32
 
 
 def _matrix(h, t, name: str) -> int:
@@ -120,10 +133,9 @@ def _matrix(h, t, name: str) -> int:
 
 
 def _vector(h, t, n: int, name: str) -> Optional[int]:
-    import torch
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous() or t.get_device() != h.device:
+    if _code_or_int8(t) != 0 or t.numel() != n or not t.is_contiguous() or t.get_device() != h.device:
         raise ValueError(f"{name} must be a contiguous float32 tensor of {n} elements on the handle's device")
     return t.data_ptr()
 
@@ -137,13 +149,12 @@ def _padded(rows: int, cols: int, device):
 def peat_quantize_i8_raw(h, x, axis: int, q=None, scale=None, values=None, stream=None) -> None:
     """peat_quantize_i8 on preallocated device outputs: q int8 (axis 0: x's shape, axis 1: transposed), scale
     float32 [rows or cols], values (x's shape and type); each may be None, but not both of q and values."""
-    import torch
     ldx = _matrix(h, x, "x")
     rows, cols = x.shape
     ldq = ldv = 0
     if q is not None:
         ldq = _matrix(h, q, "q")
-        if q.dtype != torch.int8 or tuple(q.shape) != ((rows, cols) if axis == 0 else (cols, rows)):
+        if _code_or_int8(q) != INT8 or tuple(q.shape) != ((rows, cols) if axis == 0 else (cols, rows)):
             raise ValueError("q must be int8 of x's shape (axis 0) or its transpose (axis 1)")
     if values is not None:
         ldv = _matrix(h, values, "values")
@@ -171,10 +182,9 @@ def peat_quantize_i8(h, x, axis: int = 0, stream=None):
 def peat_matmul_i8_raw(h, a, a_scale, b, b_scale, out, bias=None, stream=None) -> None:
     """peat_matmul_i8 into out [M, N] (float32, float16, bfloat16, or int32 for the sums themselves) from a [M, K]
     and b [N, K] int8 with their scales (None: 1)."""
-    import torch
     lda, ldb, ldo = _matrix(h, a, "a"), _matrix(h, b, "b"), _matrix(h, out, "out")
     (M, K), N = a.shape, b.shape[0]
-    if a.dtype != torch.int8 or b.dtype != torch.int8:
+    if _code_or_int8(a) != INT8 or _code_or_int8(b) != INT8:
         raise TypeError("a and b must be int8")
     if b.shape[1] != K:
         raise ValueError("a and b differ in their row length")
@@ -182,7 +192,7 @@ def peat_matmul_i8_raw(h, a, a_scale, b, b_scale, out, bias=None, stream=None) -
         raise ValueError("out must be [rows of a, rows of b]")
     _call(h, "peat_matmul_i8", a.data_ptr(), lda, _vector(h, a_scale, M, "a_scale"), b.data_ptr(), ldb,
           _vector(h, b_scale, N, "b_scale"), _vector(h, bias, N, "bias"), M, N, K, out.data_ptr(), ldo,
-          OUT_I32 if out.dtype == torch.int32 else _code(out), _stream(h, stream))
+          OUT_I32 if _is_int32(out) else _code(out), _stream(h, stream))
 
 
 def peat_matmul_i8(h, a, a_scale, b, b_scale, bias=None, out_dtype=None, stream=None):
@@ -196,10 +206,10 @@ def peat_matmul_i8(h, a, a_scale, b, b_scale, bias=None, out_dtype=None, stream=
 
 def _operand(h, t, axis: int, scale, name: str):
     """(structure, rows of the operand, its K) of a matrix that is 8-bit integers or is rounded to them."""
-    import torch
     ld = _matrix(h, t, name)
     rows, cols = t.shape
-    if t.dtype is torch.int8:
+    code = _code_or_int8(t)
+    if code == INT8:
         if axis != 0:
             raise ValueError(f"{name} is integers already: axis 0")
         return Operand8(t.data_ptr(), _vector(h, scale, rows, name + "'s scale"), rows, cols, ld, INT8, 0), rows, cols
@@ -209,14 +219,20 @@ def _operand(h, t, axis: int, scale, name: str):
     return (op, cols, rows) if axis else (op, rows, cols)
 
 
-def peat_product_i8_raw(h, a, b, out, a_axis: int = 0, b_axis: int = 0, a_scale=None, b_scale=None, bias=None,
-                        stream=None) -> None:
-    """peat_product_i8 into out [M, N] (float32, float16 or bfloat16): each operand int8 with its scale, or a float
-    matrix that is rounded with a scale for each row (axis 0) or column (axis 1; its transpose is the operand)."""
+def _operands(h, a, b, a_axis: int, b_axis: int, a_scale, b_scale):
+    """The structures of both operands, and M and N."""
     x, M, K = _operand(h, a, a_axis, a_scale, "a")
     y, N, K2 = _operand(h, b, b_axis, b_scale, "b")
     if K != K2:
         raise ValueError("a and b differ in their row length")
+    return x, y, M, N
+
+
+def peat_product_i8_raw(h, a, b, out, a_axis: int = 0, b_axis: int = 0, a_scale=None, b_scale=None, bias=None,
+                        stream=None) -> None:
+    """peat_product_i8 into out [M, N] (float32, float16 or bfloat16): each operand int8 with its scale, or a float
+    matrix that is rounded with a scale for each row (axis 0) or column (axis 1; its transpose is the operand)."""
+    x, y, M, N = _operands(h, a, b, a_axis, b_axis, a_scale, b_scale)
     ldo = _matrix(h, out, "out")
     if out.shape[0] != M or out.shape[1] != N:
         raise ValueError("out must be [rows of a, rows of b]")
@@ -227,11 +243,14 @@ def peat_product_i8_raw(h, a, b, out, a_axis: int = 0, b_axis: int = 0, a_scale=
 def peat_product_i8(h, a, b, a_axis: int = 0, b_axis: int = 0, a_scale=None, b_scale=None, bias=None, out_dtype=None,
                     stream=None):
     """The product as a new tensor of out_dtype (float32 unless given)."""
+    if stream is not None:
+        with _on(stream):
+            return peat_product_i8(h, a, b, a_axis, b_axis, a_scale, b_scale, bias, out_dtype)
     import torch
-    with _on(stream):
-        out = torch.empty(a.shape[1 if a_axis else 0], b.shape[1 if b_axis else 0], dtype=out_dtype or torch.float32,
-                          device=a.device)
-        peat_product_i8_raw(h, a, b, out, a_axis, b_axis, a_scale, b_scale, bias, stream)
+    x, y, M, N = _operands(h, a, b, a_axis, b_axis, a_scale, b_scale)
+    out = torch.empty(M, N, dtype=out_dtype or torch.float32, device=a.device)
+    _call(h, "peat_product_i8", ctypes.byref(x), ctypes.byref(y), _vector(h, bias, N, "bias"), out.data_ptr(), N,
+          _code(out), _stream(h, None))
     return out
 
 
@@ -344,17 +363,21 @@ class Linear8:
 
     def _product(self, t, w, name: str, bias=None, stream=None):
         """t [..., K] by row times a weight operand -> [..., N] of t's type."""
+        if stream is not None:
+            with _on(stream):
+                return self._product(t, w, name, bias)
         import torch
         op, N, K = w
-        if t.dim() < 1 or t.shape[-1] != K:
+        shape = t.shape
+        if not shape or shape[-1] != K:
             raise ValueError(f"the last dimension of {name} must be {K}")
-        with _on(stream):
-            x = t if t.dim() == 2 else t.reshape(-1, K)
-            out = torch.empty(x.shape[0], N, dtype=t.dtype, device=t.device)
-            a, M, _ = _operand(self.h, x, 0, None, name)
-            _call(self.h, "peat_product_i8", ctypes.byref(a), ctypes.byref(op), _vector(self.h, bias, N, "bias"),
-                  out.data_ptr(), N, _code(out), _stream(self.h, stream))
-        return out if t.dim() == 2 else out.view(*t.shape[:-1], N)
+        flat = len(shape) == 2
+        x = t if flat else t.reshape(-1, K)
+        a, M, _ = _operand(self.h, x, 0, None, name)
+        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
+        _call(self.h, "peat_product_i8", ctypes.byref(a), ctypes.byref(op), _vector(self.h, bias, N, "bias"),
+              out.data_ptr(), N, _code(out), _stream(self.h, None))
+        return out if flat else out.view(*shape[:-1], N)
 
     def forward(self, x, bias=None, stream=None):
         """x [..., in] -> [..., out] of x's type."""
@@ -366,14 +389,16 @@ class Linear8:
 
     def weight_grad(self, grad, x, stream=None):
         """dL/dw [out, in] in float32 from grad [..., out] and x [..., in]."""
+        if stream is not None:
+            with _on(stream):
+                return self.weight_grad(grad, x)
         if grad.shape[-1:] != (self.out_features,) or x.shape[-1:] != (self.in_features,):
             raise ValueError(f"the last dimensions of grad and x must be {self.out_features} and {self.in_features}")
-        with _on(stream):
-            g = grad if grad.dim() == 2 else grad.reshape(-1, self.out_features)
-            x = x if x.dim() == 2 else x.reshape(-1, self.in_features)
+        g = grad if grad.dim() == 2 else grad.reshape(-1, self.out_features)
+        x = x if x.dim() == 2 else x.reshape(-1, self.in_features)
         if g.shape[0] != x.shape[0]:
             raise ValueError("grad and x differ in their leading dimensions")
-        return peat_product_i8(self.h, g, x, 1, 1, stream=stream)
+        return peat_product_i8(self.h, g, x, 1, 1)
 
     def backward(self, grad, x, stream=None):
         """(dL/dx, dL/dw)."""
