@@ -396,10 +396,10 @@ __global__ void __launch_bounds__(QT) quant_long_rows(QuantParams p) {
 // (One launch of clusters that keep a strip of columns to themselves, meet in
 // distributed shared memory and read the strip again from L2 took 101 us: its
 // phases wait for each other.)  Rows off the 16-byte grid take two aligned loads
-// for a vector and their values go through shared memory, an element a lane:
-// 16384 x 4095 take 190 us, bound by instructions (loads element by element and
-// values straight from the registers: 232 and more).
-template <int DT, bool GRID>
+// for a vector in the second launch, and their values go through shared memory,
+// an element a lane: 16384 x 4095 take 173 us, with q alone 123, bound by
+// instructions (two elements a lane: 202; values from the registers: 232).
+template <int DT>
 __global__ void __launch_bounds__(QT, 4) quant_colmax(QuantParams p, int vl, int64_t rows_each) {
   using L = Elem<DT>;
   begin(p);
@@ -407,11 +407,11 @@ __global__ void __launch_bounds__(QT, 4) quant_colmax(QuantParams p, int vl, int
   const int lx = threadIdx.x % vl, ly = threadIdx.x / vl, nl = QT / vl;
   const int64_t r0 = (int64_t)blockIdx.y * rows_each, r1 = min(p.rows, r0 + rows_each);
   const int64_t col = ((int64_t)blockIdx.x * vl + lx) * L::E, left = p.cols - col;
-  const Source<DT, GRID> source(p);
+  const Source<DT, true> source(p);
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + col;
   uint4 m = make_uint4(0, 0, 0, 0);
   constexpr int U = 8;  // rows in flight; past the end the last row again, which changes no maximum
-  if (GRID && left >= L::E) {
+  if (left >= L::E) {
     for (int64_t r = r0 + ly; r < r1; r += U * nl) {
       uint4 u[U];
 #pragma unroll
@@ -419,32 +419,8 @@ __global__ void __launch_bounds__(QT, 4) quant_colmax(QuantParams p, int vl, int
 #pragma unroll
       for (int i = 0; i < U; i++) m = mag_max<DT>(m, u[i]);
     }
-  } else if (GRID) {
-    for (int64_t r = r0 + ly; r < r1 && left > 0; r += nl) m = mag_max<DT>(m, load_edge<DT>(x + r * p.ldx, left));
   } else {
-    constexpr int V = 4;
-    for (int64_t r = r0 + ly; r < r1 && left > 0; r += V * nl) {
-      uint4 a[V], b[V];
-      int edges = 0;
-#pragma unroll
-      for (int i = 0; i < V; i++) {
-        const typename L::T* q = x + min(r + i * nl, r1 - 1) * p.ldx;
-        a[i] = b[i] = make_uint4(0, 0, 0, 0);
-        if (source.whole(q, left)) {
-          a[i] = __ldg(source.on_grid(q));
-          b[i] = __ldg(source.on_grid(q) + 1);
-        } else {
-          edges |= 1 << i;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < V; i++)
-        m = mag_max<DT>(m, shifted(a[i], b[i], (int)(reinterpret_cast<uintptr_t>(x + min(r + i * nl, r1 - 1) * p.ldx) & 15)));
-      if (edges) {
-        for (int i = 0; i < V; i++)
-          if (edges >> i & 1) m = mag_max<DT>(m, load_edge<DT>(x + min(r + i * nl, r1 - 1) * p.ldx, left));
-      }
-    }
+    for (int64_t r = r0 + ly; r < r1 && left > 0; r += nl) m = mag_max<DT>(m, load_edge<DT>(x + r * p.ldx, left));
   }
   part[threadIdx.x] = m;
   __syncthreads();
@@ -459,10 +435,40 @@ __global__ void __launch_bounds__(QT, 4) quant_colmax(QuantParams p, int vl, int
   }
   end(p);
 }
+// The same where rows are off the 16-byte grid: a thread has a column, an
+// element a load (shifting vectors together takes more instructions: 48 us for
+// 16384 x 4095 bfloat16, this 33).
+template <int DT>
+__global__ void __launch_bounds__(QT, 8) quant_colmax_off(QuantParams p, int64_t rows_each) {
+  using T = typename Elem<DT>::T;
+  begin(p);
+  const int64_t r0 = (int64_t)blockIdx.y * rows_each, r1 = min(p.rows, r0 + rows_each);
+  const int64_t col = (int64_t)blockIdx.x * QT + threadIdx.x;
+  if (col < p.cols && r0 < r1) {
+    const T* x = static_cast<const T*>(p.x) + col;
+    constexpr int U = 16;
+    uint32_t m = 0;
+    auto bits = [](T v) {
+      if constexpr (DT == PEAT_F32) return __float_as_uint(v);
+      else return (uint32_t)*reinterpret_cast<const unsigned short*>(&v);
+    };
+    int64_t r = r0;
+    for (; r + U <= r1; r += U) {
+      uint32_t v[U];
+#pragma unroll
+      for (int i = 0; i < U; i++) v[i] = bits(__ldg(x + (r + i) * p.ldx));
+#pragma unroll
+      for (int i = 0; i < U; i++) m = max_word<DT>(m, v[i]);
+    }
+    for (; r < r1; r++) m = max_word<DT>(m, bits(__ldg(x + r * p.ldx)));
+    atomicMax(p.colmax + col, m);
+  }
+  end(p);
+}
 
 constexpr int TR = 128;  // rows of a tile
 template <int DT, bool PACK, bool GRID>
-__global__ void __launch_bounds__(QT, PACK || !GRID ? 2 : 3) quant_cols(QuantParams p, int64_t rows_each) {
+__global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_each) {
   using L = Elem<DT>;
   constexpr int CW = 8 * L::E;  // columns of a tile
   __shared__ __align__(16) float rs[CW], ss[CW];
@@ -706,18 +712,23 @@ cudaError_t cols_launch(const QuantParams& p, bool maxima, int nsm, cudaStream_t
   int64_t each = 1;
   if (maxima) {
     if (p.rows == 0) return cudaSuccess;
+    if constexpr (!GRID) {
+      const int64_t wide = (p.cols + QT - 1) / QT;
+      const unsigned ny = shares(p.rows, wide, 32, 16, 8, &each);
+      return launch_dependent(quant_colmax_off<DT>, dim3((unsigned)wide, ny), QT, 0, s, p, each);
+    }
     const int64_t nv = (p.cols + E - 1) / E;
     int vl = 8;
     while (vl < 32 && vl < nv) vl *= 2;  // wider CTAs would mean more shares of the rows, and atomics for each
     const int64_t wide = (nv + vl - 1) / vl;
     const unsigned ny = shares(p.rows, wide, 8 * (QT / vl), 1, 4, &each);
-    return launch_dependent(quant_colmax<DT, GRID>, dim3((unsigned)wide, ny), QT, 0, s, p, vl, each);
+    return launch_dependent(quant_colmax<DT>, dim3((unsigned)wide, ny), QT, 0, s, p, vl, each);
   }
   if (p.packed) {
-    const unsigned strips = (unsigned)(p.prows / CW), ny = shares((int64_t)p.kb * 64, strips, TR, TR, 2, &each);
+    const unsigned strips = (unsigned)(p.prows / CW), ny = shares((int64_t)p.kb * 64, strips, TR, TR, 3, &each);
     return launch_dependent(quant_cols<DT, true, GRID>, dim3(strips, ny), QT, 0, s, p, each);
   }
-  const unsigned strips = (unsigned)((p.cols + CW - 1) / CW), ny = shares(p.rows, strips, TR, TR, GRID ? 3 : 2, &each);
+  const unsigned strips = (unsigned)((p.cols + CW - 1) / CW), ny = shares(p.rows, strips, TR, TR, 3, &each);
   return launch_dependent(quant_cols<DT, false, GRID>, dim3(strips, ny), QT, 0, s, p, each);
 }
 
