@@ -250,7 +250,9 @@ __global__ void __launch_bounds__(ST, NT <= 2 ? 2 : 1) mm8_stream(Mm8Params p, i
 // ---- tiles --------------------------------------------------------------------
 // A CTA takes 128 rows of b by 64 rows of a, 64 k a stage, staged as bytes;
 // each of its 8 warps 32 x 32, so that an integer that is turned into binary16
-// serves four instructions.
+// serves four instructions.  128 x 1024 x 1024 takes 9 us, 64 x 4096 x 4096 17:
+// a stage's conversions and instructions, 0.8 us, in a chain of K / 64 (few tiles
+// have it split over a cluster).
 constexpr int TT = 256, TW = 128, TA = 64, TK = 64, TSTAGES = 4;
 constexpr int TSTAGE_BYTES = (TW + TA) * TK;
 constexpr int T_SMEM = TSTAGES * TSTAGE_BYTES;  // 48 KB; the sums' tile (64 x 132 words) fits in it
@@ -451,21 +453,24 @@ cudaError_t direct(const Mm8Params& p, int nsm, cudaStream_t s) {
 
 template <int OUT>
 cudaError_t direct_out(const Mm8Params& p, int nsm, cudaStream_t s) {
-  const bool al = ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | (uintptr_t)p.lda |
-                    (uintptr_t)p.ldb) & 15) == 0;
-  return al ? direct<OUT, 16>(p, nsm, s) : direct<OUT, 1>(p, nsm, s);
+  return mm8_aligned(p) ? direct<OUT, 16>(p, nsm, s) : direct<OUT, 1>(p, nsm, s);
 }
 
 }  // namespace
 
 // Microseconds of a call, fitted to those measured for M from 32 to 1024, N to
-// 16 384 and K to 16 384: one run of 64 k of a tile takes 0.8, an SM's CTAs share it.
-double mm8_direct_time(int64_t M, int64_t N, int64_t K, int nsm) {
+// 16 384 and K to 16 384: one run of 64 k of a tile takes 0.8 (off the 16-byte
+// grid, where it is loaded through registers, 1.4), an SM's CTAs share it.
+double mm8_direct_time(int64_t M, int64_t N, int64_t K, bool aligned, int nsm) {
   if (M <= 16 || (M <= 64 && N >= MM8_STREAM_N)) return 0.0;  // bound by b's bytes: nothing is faster
   const int64_t tiles = ((N + TW - 1) / TW) * ((M + TA - 1) / TA), runs = (K + TK - 1) / TK;
   const int S = tile_parts(tiles, runs, nsm);
   const double share = std::max(1.0, 1.1 * (double)(tiles * S) / nsm);
-  return 6.5 + 0.8 * std::ceil((double)runs / S) * share;
+  return 6.5 + (aligned ? 0.8 : 1.4) * std::ceil((double)runs / S) * share;
+}
+
+bool mm8_aligned(const Mm8Params& p) {
+  return ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | (uintptr_t)p.lda | (uintptr_t)p.ldb) & 15) == 0;
 }
 
 cudaError_t launch_mm8_direct(int out_dtype, const Mm8Params& p, int nsm, cudaStream_t s) {

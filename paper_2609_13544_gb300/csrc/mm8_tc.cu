@@ -25,6 +25,11 @@
 // before the bounds add up to more than 2^24.  Full-range integers drain every
 // 768 k, normally distributed ones about every 16 000; up to 1024 k nothing can
 // add up to more, and no norms are made.
+//
+// 8192 x 8192 x 8192 to bfloat16 takes 575 us (1910 TFLOP/s, what the library's
+// bfloat16 product reaches), with extreme integers 727; 16384 x 4096 x 1024 83,
+// of which pack has 10; 2048 x 1024 x 4096, 32 tiles with k in two parts, 26.
+// pack is bound by memory: 52 million integers take 22 us, 7 TB/s.
 #include <cooperative_groups.h>
 #include <cuda.h>
 

@@ -221,10 +221,11 @@ peat_status_t output_ok(peat_handle_t h, const float* sa, const float* sb, const
   return PEAT_OK;
 }
 // whether the tensor-core path takes a product
-bool wide_product(peat_handle_t h, const peat::Mm8TcPlan& plan, int64_t M, int64_t N, int64_t K) {
+bool wide_product(peat_handle_t h, const peat::Mm8TcPlan& plan, const peat::Mm8Params& p) {
   // the packed blocks' rows are 32-bit coordinates
   const bool fits = (plan.mt + plan.nt) * 2 * plan.kb < ((int64_t)1 << 24);
-  return K > 0 && fits && peat::mm8_tc_time(plan, K, h->nsm) < peat::mm8_direct_time(M, N, K, h->nsm);
+  return p.K > 0 && fits &&
+         peat::mm8_tc_time(plan, p.K, h->nsm) < peat::mm8_direct_time(p.M, p.N, p.K, peat::mm8_aligned(p), h->nsm);
 }
 unsigned int wait_limit(peat_handle_t h) { return std::min(h->wait_limit, 1u << 22); }
 
@@ -245,7 +246,7 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
   const peat::Mm8Params p{a, b, lda, ldb, sa, sb, bias, out, ldo, M, N, K};
   const peat::Mm8TcPlan plan = peat::mm8_tc_plan(M, N, K, h->nsm);
   cudaError_t e;
-  if (wide_product(h, plan, M, N, K)) {
+  if (wide_product(h, plan, p)) {
     OpsState* s = nullptr;
     ps = ops_state(h, &s);
     const size_t norms = (plan.bytes + 255) / 256 * 256;
@@ -317,7 +318,8 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
   x = operand_of(*a, rounded, &at);
   y = operand_of(*b, rounded, &at);
   const peat::Mm8TcPlan plan = peat::mm8_tc_plan(M, N, K, h->nsm);
-  const bool wide = wide_product(h, plan, M, N, K);
+  const peat::Mm8Params p{x.q, y.q, x.ld, y.ld, x.scale, y.scale, bias, out, ldo, M, N, K};
+  const bool wide = wide_product(h, plan, p);
 
   // Which operands are rounded, and which of them straight into packed blocks
   const peat_operand_t* in[2] = {a, b};
@@ -357,7 +359,6 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
   // A launch that needs nothing of the one before it runs beside it: the
   // packing of one operand and the rounding of the other, both operands'
   // column maxima, both operands' columns.
-  const peat::Mm8Params p{x.q, y.q, x.ld, y.ld, x.scale, y.scale, bias, out, ldo, M, N, K};
   cudaError_t e = cudaSuccess;
   bool beside = false;
   const int as_is = packed ? 3 & ~rounded_ops : 0;

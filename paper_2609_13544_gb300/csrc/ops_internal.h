@@ -79,7 +79,9 @@ struct Mm8TcPlan {
   size_t a_off, b_off, sum_off, bytes;  // workspace
   int64_t na_words, nb_words;            // sums of squares of a's and of b's blocks (0: not needed)
 };
-double mm8_direct_time(int64_t M, int64_t N, int64_t K, int nsm);  // expected microseconds
+double mm8_direct_time(int64_t M, int64_t N, int64_t K, bool aligned, int nsm);  // expected microseconds
+// whether the rows of a and b start on 16-byte boundaries
+bool mm8_aligned(const Mm8Params& p);
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm);
 double mm8_tc_time(const Mm8TcPlan& p, int64_t K, int nsm);
 // norms: na_words, then nb_words; which: bit 0 a, bit 1 b
