@@ -24,6 +24,12 @@
  * peat_product_i8 rounds add a byte for each element.  A gradient list takes
  * 32 bytes for each tensor and 100 KB, and 40 more for each of more than 800.
  *
+ * The calls can be captured into a CUDA graph, once a call of the same sizes has
+ * been made before (a call that would have to allocate, and a gradient list of
+ * more than 800 tensors, which the host stages, return PEAT_ERR_UNSUPPORTED).
+ * The graph uses the handle's workspace: it lives as long as the handle, and its
+ * launches and the handle's calls stay in order on the GPU.
+ *
  * The waits inside a product of many rows are bounded; should one expire, that
  * call's outputs are invalid, and the next product or compare on the handle
  * returns PEAT_ERR_TIMEOUT once.
@@ -142,9 +148,7 @@ typedef enum {
  * that with a compensation, in a fixed order: the same list gives the same
  * bits on every call.  Neither squares nor sums overflow or underflow at any
  * magnitude of g.  An infinite element makes its tensor's norm and the whole
- * norm +inf, a NaN makes them NaN.  An empty list has norm 0.  A list of more
- * than 800 tensors is staged in pinned memory that later calls use again: such
- * a call cannot be captured in a CUDA graph. */
+ * norm +inf, a NaN makes them NaN.  An empty list has norm 0. */
 peat_status_t peat_grad_norm(peat_handle_t h, const peat_grad_t* list, int64_t count, peat_norm_t type,
                              float unscale, peat_gradnorm_t* result, float* norms, peat_stream_t stream);
 

@@ -7,16 +7,19 @@
 #include <cstdint>
 #include <cstring>
 #include <new>
+#include <vector>
 
 #include "ops_internal.h"
 #include "peat_handle.h"
 
 namespace peat {
 
-// Words that a call finds zero and the next one clears: two halves, in turn.
+// Words that a call finds zero and the next one clears: two halves, in turn.  A
+// call that is captured into a graph has a third part, which it clears itself,
+// because the graph does not run in turn with the calls after it.
 struct Halves {
   void* p = nullptr;
-  size_t cap = 0;  // bytes of both
+  size_t cap = 0;  // bytes of the three parts
   int64_t used[2] = {0, 0};
   int at = 0;
   bool lost = false;  // a launch failed: what they hold is not known
@@ -24,6 +27,9 @@ struct Halves {
 
 // Made by a handle's first call of an operator, freed with it.
 struct OpsState {
+  bool capturing = false;  // the call at work is being captured
+  bool captured = false;   // some call was: blocks that a graph may use are kept
+  std::vector<void*> kept;
   // gradient lists: device block (entries, then partial sums), and a ring of
   // pinned copies of the entries, each free again once its event has passed
   static constexpr int RING = 4;
@@ -56,6 +62,7 @@ void ops_destroy(OpsState* s) {
   if (s->mm) cudaFree(s->mm);
   if (s->rounded) cudaFree(s->rounded);
   if (s->norms.p) cudaFree(s->norms.p);
+  for (void* p : s->kept) cudaFree(p);
   for (int i = 0; i < OpsState::RING; i++) {
     if (s->h_list[i]) cudaFreeHost(s->h_list[i]);
     if (s->taken[i]) cudaEventDestroy(s->taken[i]);
@@ -77,8 +84,15 @@ constexpr int64_t MAX_DIM = ((int64_t)1 << 31) - 1;
 int type_bytes(int dt) { return dt == PEAT_F32 ? 4 : (dt == PEAT_F16 || dt == PEAT_BF16 ? 2 : 0); }
 bool aligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
-peat_status_t ops_state(peat_handle_t h, OpsState** out) {
+peat_status_t ops_state(peat_handle_t h, cudaStream_t st, OpsState** out) {
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(st, &capture) != cudaSuccess) {
+    cudaGetLastError();
+    capture = cudaStreamCaptureStatusNone;
+  }
+  const bool capturing = capture != cudaStreamCaptureStatusNone;
   if (!h->ops) {
+    if (capturing) return fail(h, PEAT_ERR_UNSUPPORTED, "a handle's first operator call cannot be captured");
     OpsState* s = new OpsState();
     if (cudaMalloc(&s->done, 256) != cudaSuccess || cudaMemset(s->done, 0, 256) != cudaSuccess ||
         cudaDeviceSynchronize() != cudaSuccess) {
@@ -88,6 +102,8 @@ peat_status_t ops_state(peat_handle_t h, OpsState** out) {
     }
     h->ops = s;
   }
+  h->ops->capturing = capturing;
+  h->ops->captured |= capturing;
   *out = h->ops;
   return PEAT_OK;
 }
@@ -95,7 +111,10 @@ peat_status_t ops_state(peat_handle_t h, OpsState** out) {
 // grows a device block; its contents are not kept, and an earlier call that uses it is waited for by cudaFree
 peat_status_t grow(peat_handle_t h, void** p, size_t* cap, size_t need) {
   if (need <= *cap) return PEAT_OK;
-  if (*p) cudaFree(*p);
+  if (h->ops->capturing)
+    return fail(h, PEAT_ERR_UNSUPPORTED, "the workspace would have to grow: make the call once before it is captured");
+  if (*p && h->ops->captured) h->ops->kept.push_back(*p);
+  else if (*p) cudaFree(*p);
   *p = nullptr;
   *cap = 0;
   if (cudaMalloc(p, need) != cudaSuccess) {
@@ -155,8 +174,8 @@ peat_status_t quant_params(peat_handle_t h, const void* x, int64_t rows, int64_t
 // take some: a call also clears (*zero, *zero_n) what the one before it used.
 peat_status_t take(peat_handle_t h, peat::Halves* b, int64_t n, int64_t least, unsigned int** words, unsigned int** zero,
                    int64_t* zero_n, cudaStream_t st) {
-  const size_t need = 2 * sizeof(unsigned int) * (size_t)((std::max(n, least) + 3) / 4 * 4);
-  if (need > b->cap || b->lost) {
+  const size_t need = 3 * sizeof(unsigned int) * (size_t)((std::max(n, least) + 3) / 4 * 4);
+  if (need > b->cap || (b->lost && !h->ops->capturing)) {
     b->lost = false;
     peat_status_t ps = grow(h, &b->p, &b->cap, need);
     if (ps != PEAT_OK) return ps;
@@ -164,8 +183,14 @@ peat_status_t take(peat_handle_t h, peat::Halves* b, int64_t n, int64_t least, u
     cudaError_t e = cudaMemsetAsync(b->p, 0, b->cap, st);
     if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(workspace)");
   }
-  const size_t half = b->cap / 2 / sizeof(unsigned int);
+  const size_t half = b->cap / 3 / sizeof(unsigned int);
   unsigned int* base = static_cast<unsigned int*>(b->p);
+  if (h->ops->capturing) {
+    *words = *zero = base + 2 * half;
+    *zero_n = 0;
+    cudaError_t e = cudaMemsetAsync(*words, 0, sizeof(unsigned int) * (size_t)n, st);
+    return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "cudaMemsetAsync(workspace)");
+  }
   *words = base + b->at * half;
   *zero = base + (b->at ^ 1) * half;
   *zero_n = b->used[b->at ^ 1];
@@ -189,7 +214,7 @@ peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t col
     e = peat::launch_quant8(dtype, axis == 0 ? peat::QUANT_ROWS : peat::QUANT_COLUMNS, p, h->nsm, st);
   } else {
     OpsState* s = nullptr;
-    ps = ops_state(h, &s);
+    ps = ops_state(h, st, &s);
     if (ps == PEAT_OK) ps = take(h, &s->colmax, cols, 8192, &p.colmax, &p.zero, &p.zero_n, st);
     if (ps != PEAT_OK) return ps;
     e = peat::launch_quant8(dtype, peat::QUANT_MAXIMA, p, h->nsm, st);
@@ -248,7 +273,7 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
   cudaError_t e;
   if (wide_product(h, plan, p)) {
     OpsState* s = nullptr;
-    ps = ops_state(h, &s);
+    ps = ops_state(h, st, &s);
     const size_t norms = (plan.bytes + 255) / 256 * 256;
     if (ps == PEAT_OK)
       ps = grow(h, &s->mm, &s->mm_cap, norms + sizeof(unsigned int) * (size_t)(plan.na_words + plan.nb_words));
@@ -310,7 +335,7 @@ peat_status_t product(peat_handle_t h, const peat_operand_t* a, const peat_opera
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
   OpsState* s = nullptr;
-  ps = ops_state(h, &s);
+  ps = ops_state(h, st, &s);
   if (ps == PEAT_OK) ps = grow(h, &s->rounded, &s->rounded_cap, need);
   if (ps != PEAT_OK) return ps;
   char* rounded = static_cast<char*>(s->rounded);
@@ -441,7 +466,7 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
   OpsState* s = nullptr;
-  peat_status_t ps = ops_state(h, &s);
+  peat_status_t ps = ops_state(h, st, &s);
   if (ps != PEAT_OK) return ps;
 
   // a piece's own time is about that of 256 units
@@ -461,6 +486,8 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   peat::GnEntry inline_list[peat::GN_INLINE];
   peat::GnEntry* dst = inline_list;
   int slot = -1;
+  if (listed && s->capturing)
+    return fail(h, PEAT_ERR_UNSUPPORTED, "a list of more than 800 tensors cannot be captured: it is staged by the host");
   if (listed) {
     slot = s->next;
     s->next = (s->next + 1) % OpsState::RING;

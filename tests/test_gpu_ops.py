@@ -738,3 +738,100 @@ def test_matmul_few_rows_past_many(peat_gpu, h, mnk):
         out = torch.empty(M, N, dtype=torch.int32, device="cuda")
         peat_gpu.peat_matmul_i8_raw(h, a, None, b, None, out)
         assert torch.equal(out.to(torch.int64), sums(a, b))
+
+
+# ---------------------------------------------------------------------------
+# graphs
+# ---------------------------------------------------------------------------
+def test_captured_calls(peat_gpu):
+    """Calls captured into a graph and replayed on new inputs, between calls that are not, and after the workspace has
+    grown."""
+    import torch
+    P, g = peat_gpu, rng(21)
+    with P.Handle(0) as h:
+        x = torch.empty(900, 700, device="cuda", dtype=torch.bfloat16)
+        a, b = torch.empty(600, 2100, device="cuda"), torch.empty(300, 2100, device="cuda")
+        at, bt = torch.empty(1300, 270, device="cuda"), torch.empty(1300, 280, device="cuda")
+        grads_in = [torch.empty(n, device="cuda") for n in (5, 70000, 1000)]
+        grads_out = [torch.empty_like(t) for t in grads_in]
+        q, s = torch.empty(700, 900, dtype=torch.int8, device="cuda"), torch.empty(700, device="cuda")
+        y, yt = torch.empty(600, 300, device="cuda"), torch.empty(270, 280, device="cuda")
+        rec, norms = torch.empty(16, dtype=torch.uint8, device="cuda"), torch.empty(3, device="cuda")
+        glist = P.GradList(grads_in, grads_out)
+
+        def refill(scale):
+            for t in (x, a, b, at, bt, *grads_in):
+                t.copy_(torch.randn(t.shape, generator=g, device="cuda") * scale)
+
+        def calls():
+            P.peat_quantize_i8_raw(h, x, 1, q, s)
+            P.peat_product_i8_raw(h, a, b, y)
+            P.peat_product_i8_raw(h, at, bt, yt, 1, 1)
+            P.peat_grad_clip_raw(h, glist, 0.5, rec, norms)
+
+        def check():
+            torch.cuda.synchronize()
+            eq, es, _ = quant_definition(x, 1)
+            assert torch.equal(q, eq) and same_bits(s, es)
+            for u, v, w, axis in ((a, b, y, 0), (at, bt, yt, 1)):
+                (qu, su, _), (qv, sv, _) = quant_definition(u, axis), quant_definition(v, axis)
+                assert same_bits(w, sums(qu, qv).float() * (su[:, None] * sv[None, :]))
+            r = rec.view(torch.float32)
+            want = norm64(torch.cat(grads_in), "2")
+            assert abs(r[0].item() - want) <= TOL["2"] * want
+            for t, o in zip(grads_in, grads_out):
+                assert same_bits(o, t * r[1])
+
+        refill(1.0)
+        calls()
+        check()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls()
+        for scale in (100.0, 1e-3, 5.0):
+            refill(scale)
+            graph.replay()
+            check()
+            refill(scale * 3)
+            calls()
+            check()
+        big = torch.randn(1100, 40000, generator=g, device="cuda")  # larger than any call before
+        P.peat_quantize_i8(h, big, 1)
+        P.peat_product_i8(h, big, big[:300])
+        P.peat_grad_norm(h, [torch.ones(10, device="cuda")] * 5000)
+        for scale in (7.0, 1e-2):
+            refill(scale)
+            graph.replay()
+            check()
+
+
+def test_capture_refusals(peat_gpu):
+    """A capture that would have to allocate is refused, and the handle works on."""
+    import torch
+    P = peat_gpu
+    x = torch.randn(700, 64, generator=rng(4), device="cuda")
+    q, s = torch.empty(64, 700, dtype=torch.int8, device="cuda"), torch.empty(64, device="cuda")
+    rec = torch.empty(16, dtype=torch.uint8, device="cuda")
+    long = P.GradList([torch.ones(3, device="cuda") for _ in range(801)])
+    with P.Handle(0) as h:
+        for warm in (False, True):
+            if warm:
+                P.peat_quantize_i8_raw(h, x, 1, q, s)
+                P.peat_grad_norm_raw(h, long, rec)
+                torch.cuda.synchronize()
+            done = torch.zeros(1, device="cuda")
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                done.add_(1)
+                if not warm:
+                    with pytest.raises(P.PeatError) as e:
+                        P.peat_quantize_i8_raw(h, x, 1, q, s)
+                    assert e.value.status == 2
+                with pytest.raises(P.PeatError) as e:
+                    P.peat_grad_norm_raw(h, long, rec)
+                assert e.value.status == 2
+            graph.replay()
+            torch.cuda.synchronize()
+            assert done.item() == 1
+        check_quant(P, h, x, 1)
+        assert abs(P.peat_grad_norm(h, long)["norm"] - 2403 ** 0.5) <= 1e-4
