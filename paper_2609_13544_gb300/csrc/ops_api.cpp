@@ -176,12 +176,12 @@ peat_status_t take(peat_handle_t h, peat::Halves* b, int64_t n, int64_t least, u
                    int64_t* zero_n, cudaStream_t st) {
   const size_t need = 3 * sizeof(unsigned int) * (size_t)((std::max(n, least) + 3) / 4 * 4);
   if (need > b->cap || (b->lost && !h->ops->capturing)) {
-    b->lost = false;
     peat_status_t ps = grow(h, &b->p, &b->cap, need);
     if (ps != PEAT_OK) return ps;
     b->used[0] = b->used[1] = 0;
     cudaError_t e = cudaMemsetAsync(b->p, 0, b->cap, st);
     if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(workspace)");
+    b->lost = false;  // (a refused growth leaves them as they are)
   }
   const size_t half = b->cap / 3 / sizeof(unsigned int);
   unsigned int* base = static_cast<unsigned int*>(b->p);

@@ -1,0 +1,186 @@
+// The host side of the playback operators (csrc/ops_api.cpp) against a runtime of
+// plain host memory, in which calls fail, launches are refused and streams are
+// being captured as a check asks for it.  No GPU: the kernels are stand-ins that
+// look at the words they are given.
+//
+//   ops_host NAME     runs one check; exit code 0 if it holds
+#include <cuda_runtime.h>
+
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <map>
+#include <vector>
+
+#include "ops_internal.h"
+#include "peat_handle.h"
+
+namespace {
+
+struct Runtime {
+  bool capturing = false;
+  bool fail_memset = false;
+  int fail_step = -1;        // the quantiser's launch that fails
+  int dirty = 0;             // words that a kernel should have found zero
+  int allocations = 0;       // device, pinned and event allocations
+  std::map<void*, size_t> device;
+  peat::QuantParams quant;   // of the last quantiser launch
+  size_t live() const {
+    size_t n = 0;
+    for (auto& b : device) n += b.second;
+    return n;
+  }
+} rt;
+
+void zero_or_count(const unsigned int* w, int64_t n) {
+  for (int64_t i = 0; i < n; i++) rt.dirty += w[i] != 0;
+}
+
+int failures = 0;
+void check(bool ok, const char* what, int line) {
+  if (ok) return;
+  std::printf("line %d: %s\n", line, what);
+  failures++;
+}
+#define CHECK(x) check((x), #x, __LINE__)
+
+}  // namespace
+
+// ---- the runtime ----
+extern "C" {
+cudaError_t cudaGetDevice(int* d) { return *d = 0, cudaSuccess; }
+cudaError_t cudaSetDevice(int) { return cudaSuccess; }
+cudaError_t cudaGetLastError() { return cudaSuccess; }
+const char* cudaGetErrorString(cudaError_t) { return "made to fail"; }
+cudaError_t cudaDeviceSynchronize() { return cudaSuccess; }
+cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus* s) {
+  *s = rt.capturing ? cudaStreamCaptureStatusActive : cudaStreamCaptureStatusNone;
+  return cudaSuccess;
+}
+cudaError_t cudaMalloc(void** p, size_t n) {
+  *p = std::malloc(n ? n : 1);
+  std::memset(*p, 0xab, n);
+  rt.device[*p] = n;
+  rt.allocations++;
+  return cudaSuccess;
+}
+cudaError_t cudaFree(void* p) {
+  rt.device.erase(p);
+  std::free(p);
+  return cudaSuccess;
+}
+cudaError_t cudaMallocHost(void** p, size_t n) { return rt.allocations++, *p = std::malloc(n), cudaSuccess; }
+cudaError_t cudaFreeHost(void* p) { return std::free(p), cudaSuccess; }
+cudaError_t cudaMemset(void* p, int v, size_t n) { return std::memset(p, v, n), cudaSuccess; }
+cudaError_t cudaMemsetAsync(void* p, int v, size_t n, cudaStream_t) {
+  if (rt.fail_memset) return cudaErrorUnknown;
+  return std::memset(p, v, n), cudaSuccess;
+}
+cudaError_t cudaMemcpyAsync(void* d, const void* s, size_t n, cudaMemcpyKind, cudaStream_t) {
+  return std::memcpy(d, s, n), cudaSuccess;
+}
+cudaError_t cudaEventCreateWithFlags(cudaEvent_t* e, unsigned) {
+  rt.allocations++;
+  *e = reinterpret_cast<cudaEvent_t>(std::malloc(1));
+  return cudaSuccess;
+}
+cudaError_t cudaEventDestroy(cudaEvent_t e) { return std::free(e), cudaSuccess; }
+cudaError_t cudaEventRecord(cudaEvent_t, cudaStream_t) { return cudaSuccess; }
+cudaError_t cudaEventSynchronize(cudaEvent_t) { return cudaSuccess; }
+}
+
+// ---- the kernels ----
+namespace peat {
+cudaError_t launch_quant8(int, int step, const QuantParams& p, int, cudaStream_t) {
+  rt.quant = p;
+  if (step == rt.fail_step) return cudaErrorLaunchFailure;
+  if (step == QUANT_MAXIMA) {
+    zero_or_count(p.colmax, p.cols);
+    for (int64_t i = 0; i < p.cols; i++) p.colmax[i] = 1;
+  } else {
+    for (int64_t i = 0; i < p.zero_n; i++) p.zero[i] = 0;
+    for (int64_t i = 0; i < p.zero2_n; i++) p.zero2[i] = 0;
+  }
+  return cudaSuccess;
+}
+bool quant8_packs(int, int, const QuantParams&) { return false; }
+cudaError_t launch_mm8_direct(int, const Mm8Params&, int, cudaStream_t) { return cudaSuccess; }
+double mm8_direct_time(int64_t, int64_t, int64_t, bool, int) { return 1e30; }
+bool mm8_aligned(const Mm8Params&) { return true; }
+Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int) {
+  Mm8TcPlan p = {};
+  p.bytes = 2 * (size_t)(M + N) * K;
+  return p;
+}
+double mm8_tc_time(const Mm8TcPlan&, int64_t, int) { return 1.0; }
+cudaError_t launch_mm8_pack(const Mm8Params&, const Mm8TcPlan&, char*, unsigned int*, int, cudaStream_t) {
+  return cudaSuccess;
+}
+cudaError_t launch_mm8_tc(int, const Mm8Params&, const Mm8TcPlan&, char*, unsigned int*, bool, unsigned int*,
+                          unsigned int, int, cudaStream_t) {
+  return cudaSuccess;
+}
+int gn_block() { return 256; }
+cudaError_t launch_gradnorm(const GnParams& p, const GnEntry*, int, cudaStream_t) {
+  zero_or_count(p.tickets, p.count);
+  zero_or_count(p.done, 1);
+  return cudaSuccess;
+}
+}  // namespace peat
+
+namespace {
+
+struct Host {
+  peat_handle_s h;
+  std::vector<char> space = std::vector<char>(1 << 20);  // stands for the caller's tensors: no kernel touches them
+  Host() { h.nsm = 152; }
+  ~Host() { peat::ops_destroy(h.ops); }
+  void* data() { return reinterpret_cast<void*>((reinterpret_cast<uintptr_t>(space.data()) + 255) & ~(uintptr_t)255); }
+  peat_status_t columns(int64_t cols) {
+    return peat_quantize_i8(&h, data(), 1000, cols, cols, PEAT_F32, 1, static_cast<int8_t*>(data()), 1000, nullptr,
+                            nullptr, 0, nullptr);
+  }
+  peat_status_t norm(int64_t count) {
+    std::vector<peat_grad_t> list(count, peat_grad_t{data(), nullptr, 3, PEAT_F32, 0});
+    return peat_grad_norm(&h, list.data(), count, PEAT_NORM_2, 1.0f, static_cast<peat_gradnorm_t*>(data()), nullptr,
+                          nullptr);
+  }
+};
+
+// Words that a failed launch left as they were are cleared before the next call
+// takes them, a capture that was refused in between or not.
+void words_after_a_failed_launch() {
+  for (bool refused : {false, true}) {
+    Host u;
+    CHECK(u.columns(100) == PEAT_OK);
+    rt.fail_step = peat::QUANT_COLUMNS;
+    CHECK(u.columns(100) == PEAT_ERR_CUDA);
+    rt.fail_step = -1;
+    if (refused) {
+      rt.capturing = true;
+      CHECK(u.columns(100000) == PEAT_ERR_UNSUPPORTED);
+      rt.capturing = false;
+    }
+    for (int i = 0; i < 3; i++) CHECK(u.columns(100) == PEAT_OK);
+    CHECK(rt.dirty == 0);
+  }
+}
+
+const struct {
+  const char* name;
+  void (*run)();
+} CHECKS[] = {
+    {"words_after_a_failed_launch", words_after_a_failed_launch},
+};
+
+}  // namespace
+
+int main(int argc, char** argv) {
+  for (auto& c : CHECKS)
+    if (argc == 2 && !std::strcmp(argv[1], c.name)) {
+      c.run();
+      return failures != 0;
+    }
+  for (auto& c : CHECKS) std::printf("%s\n", c.name);
+  return argc == 1 ? 0 : 2;
+}
