@@ -22,7 +22,7 @@ struct Halves {
   size_t cap = 0;  // bytes of the three parts
   int64_t used[2] = {0, 0};
   int at = 0;
-  bool lost = false;  // a launch failed: what they hold is not known
+  bool lost = false;  // a launch or a clearing failed: what they hold is not known
 };
 
 // Made by a handle's first call of an operator, freed with it.
@@ -133,7 +133,9 @@ peat_status_t tickets(peat_handle_t h, OpsState* s, size_t n, cudaStream_t st) {
   peat_status_t ps = grow(h, &s->tickets, &s->tickets_cap, need);
   if (ps != PEAT_OK) return ps;
   cudaError_t e = cudaMemsetAsync(s->tickets, 0, need, st);
-  return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "cudaMemsetAsync(counters)");
+  if (e == cudaSuccess) return PEAT_OK;
+  s->tickets_cap = 0;  // the next call tries again
+  return cuda_fail(h, e, "cudaMemsetAsync(counters)");
 }
 
 // the checks of a quantisation, and its launches' parameters but for the workspace
@@ -178,10 +180,11 @@ peat_status_t take(peat_handle_t h, peat::Halves* b, int64_t n, int64_t least, u
   if (need > b->cap || (b->lost && !h->ops->capturing)) {
     peat_status_t ps = grow(h, &b->p, &b->cap, need);
     if (ps != PEAT_OK) return ps;
+    b->lost = true;
     b->used[0] = b->used[1] = 0;
     cudaError_t e = cudaMemsetAsync(b->p, 0, b->cap, st);
     if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(workspace)");
-    b->lost = false;  // (a refused growth leaves them as they are)
+    b->lost = false;  // (a growth that was refused leaves them as they are)
   }
   const size_t half = b->cap / 3 / sizeof(unsigned int);
   unsigned int* base = static_cast<unsigned int*>(b->p);

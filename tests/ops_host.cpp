@@ -166,11 +166,26 @@ void words_after_a_failed_launch() {
   }
 }
 
+// New workspace whose clearing failed is cleared by the next call that takes it.
+void words_after_a_failed_clear() {
+  Host u;
+  CHECK(u.columns(0) == PEAT_OK && u.norm(1) == PEAT_OK);
+  rt.fail_memset = true;
+  CHECK(u.columns(10000) == PEAT_ERR_CUDA);
+  CHECK(u.norm(5000) == PEAT_ERR_CUDA);
+  rt.fail_memset = false;
+  CHECK(u.columns(10000) == PEAT_OK);
+  CHECK(rt.dirty == 0);
+  CHECK(u.norm(5000) == PEAT_OK);
+  CHECK(rt.dirty == 0);
+}
+
 const struct {
   const char* name;
   void (*run)();
 } CHECKS[] = {
     {"words_after_a_failed_launch", words_after_a_failed_launch},
+    {"words_after_a_failed_clear", words_after_a_failed_clear},
 };
 
 }  // namespace
