@@ -16,7 +16,8 @@
  * every call asynchronous on `stream`, errors as peat_status_t with the text
  * in peat_last_error(h), nothing thrown, one handle per host thread and its
  * calls in order on the GPU (its workspace is reused call after call).  The
- * workspace grows on demand; a call that has to grow it waits for the device.
+ * workspace grows on demand; a call that has to grow it waits for the device, and
+ * a block that is outgrown becomes half as large again, where there is room.
  * After a first call of the same sizes, the calls of this header do not
  * allocate.  A product of many rows takes, with M and N rounded up to 256 and K
  * to 64, 2 (M + N) K bytes, and for K above 1024 20 MB, or where that is more 4

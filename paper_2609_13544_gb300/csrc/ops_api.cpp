@@ -108,21 +108,32 @@ peat_status_t ops_state(peat_handle_t h, cudaStream_t st, OpsState** out) {
   return PEAT_OK;
 }
 
-// grows a device block; its contents are not kept, and an earlier call that uses it is waited for by cudaFree
+// Grows a device block; its contents are not kept, and an earlier call that uses
+// it is waited for by cudaFree.  A block that is outgrown is followed by one half
+// as large again at least, where there is room: sizes that grow call by call
+// allocate seldom, and blocks that are kept for a graph add up to at most twice
+// the last one.
 peat_status_t grow(peat_handle_t h, void** p, size_t* cap, size_t need) {
   if (need <= *cap) return PEAT_OK;
   if (h->ops->capturing)
     return fail(h, PEAT_ERR_UNSUPPORTED, "the workspace would have to grow: make the call once before it is captured");
+  size_t room = std::max(need, *cap + *cap / 2);
   if (*p && h->ops->captured) h->ops->kept.push_back(*p);
   else if (*p) cudaFree(*p);
   *p = nullptr;
   *cap = 0;
-  if (cudaMalloc(p, need) != cudaSuccess) {
+  cudaError_t e = cudaMalloc(p, room);
+  if (e != cudaSuccess && room > need) {
+    cudaGetLastError();
+    room = need;
+    e = cudaMalloc(p, room);
+  }
+  if (e != cudaSuccess) {
     cudaGetLastError();
     *p = nullptr;
     return fail(h, PEAT_ERR_ALLOC, "operator workspace allocation failed");
   }
-  *cap = need;
+  *cap = room;
   return PEAT_OK;
 }
 
@@ -132,7 +143,7 @@ peat_status_t tickets(peat_handle_t h, OpsState* s, size_t n, cudaStream_t st) {
   if (need <= s->tickets_cap) return PEAT_OK;
   peat_status_t ps = grow(h, &s->tickets, &s->tickets_cap, need);
   if (ps != PEAT_OK) return ps;
-  cudaError_t e = cudaMemsetAsync(s->tickets, 0, need, st);
+  cudaError_t e = cudaMemsetAsync(s->tickets, 0, s->tickets_cap, st);
   if (e == cudaSuccess) return PEAT_OK;
   s->tickets_cap = 0;  // the next call tries again
   return cuda_fail(h, e, "cudaMemsetAsync(counters)");
@@ -186,7 +197,7 @@ peat_status_t take(peat_handle_t h, peat::Halves* b, int64_t n, int64_t least, u
     if (e != cudaSuccess) return cuda_fail(h, e, "cudaMemsetAsync(workspace)");
     b->lost = false;  // (a growth that was refused leaves them as they are)
   }
-  const size_t half = b->cap / 3 / sizeof(unsigned int);
+  const size_t half = b->cap / 3 / sizeof(unsigned int) / 4 * 4;  // (sums of squares are read in pairs)
   unsigned int* base = static_cast<unsigned int*>(b->p);
   if (h->ops->capturing) {
     *words = *zero = base + 2 * half;

@@ -20,6 +20,7 @@ namespace {
 struct Runtime {
   bool capturing = false;
   bool fail_memset = false;
+  size_t largest = (size_t)-1;  // block that can be had
   int fail_step = -1;        // the quantiser's launch that fails
   int dirty = 0;             // words that a kernel should have found zero
   int allocations = 0;       // device, pinned and event allocations
@@ -58,6 +59,7 @@ cudaError_t cudaStreamIsCapturing(cudaStream_t, cudaStreamCaptureStatus* s) {
   return cudaSuccess;
 }
 cudaError_t cudaMalloc(void** p, size_t n) {
+  if (n > rt.largest) return cudaErrorMemoryAllocation;
   *p = std::malloc(n ? n : 1);
   std::memset(*p, 0xab, n);
   rt.device[*p] = n;
@@ -140,6 +142,10 @@ struct Host {
     return peat_quantize_i8(&h, data(), 1000, cols, cols, PEAT_F32, 1, static_cast<int8_t*>(data()), 1000, nullptr,
                             nullptr, 0, nullptr);
   }
+  peat_status_t product(int64_t rows) {
+    const int8_t* x = static_cast<int8_t*>(data());
+    return peat_matmul_i8(&h, x, 500, nullptr, x, 500, nullptr, nullptr, rows, 1000, 500, data(), 1000, PEAT_F32, nullptr);
+  }
   peat_status_t norm(int64_t count) {
     std::vector<peat_grad_t> list(count, peat_grad_t{data(), nullptr, 3, PEAT_F32, 0});
     return peat_grad_norm(&h, list.data(), count, PEAT_NORM_2, 1.0f, static_cast<peat_gradnorm_t*>(data()), nullptr,
@@ -180,12 +186,46 @@ void words_after_a_failed_clear() {
   CHECK(rt.dirty == 0);
 }
 
+// Sizes that grow call by call: few allocations, and blocks that a graph may use
+// do not add up to a multiple of the sizes.  Where memory is short, a call gets
+// by with what it needs.
+void growing_sizes() {
+  for (bool captured : {false, true}) {
+    rt.allocations = 0;
+    Host u;
+    CHECK(u.product(1000) == PEAT_OK);
+    if (captured) {
+      rt.capturing = true;
+      CHECK(u.product(1000) == PEAT_OK);
+      rt.capturing = false;
+    }
+    for (int64_t m = 1000; m <= 20000; m += 100) CHECK(u.product(m) == PEAT_OK);
+    const size_t need = 2 * (20000 + 1000) * (size_t)500;
+    CHECK(rt.live() <= (captured ? 5 : 2) * need);
+    CHECK(rt.allocations <= 16);
+  }
+  Host u;
+  CHECK(u.product(1000) == PEAT_OK);
+  rt.largest = 2 * (1100 + 1000) * (size_t)500 + 1000;
+  CHECK(u.product(1100) == PEAT_OK);
+  CHECK(u.product(1200) == PEAT_ERR_ALLOC);
+  rt.largest = (size_t)-1;
+  CHECK(u.product(1200) == PEAT_OK);
+  // zeroed words: all of a block that grew by more than its call needs, on boundaries of 16 bytes
+  for (int64_t n = 5000; n <= 20000; n += 501) {
+    CHECK(u.norm(n) == PEAT_OK && u.columns(2 * n) == PEAT_OK);
+    CHECK(reinterpret_cast<uintptr_t>(rt.quant.colmax) % 16 == 0);
+  }
+  CHECK(rt.dirty == 0);
+}
+
 const struct {
   const char* name;
   void (*run)();
 } CHECKS[] = {
     {"words_after_a_failed_launch", words_after_a_failed_launch},
     {"words_after_a_failed_clear", words_after_a_failed_clear},
+    {"growing_sizes", growing_sizes},
 };
 
 }  // namespace

@@ -18,7 +18,7 @@ def program(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("name", ["words_after_a_failed_launch", "words_after_a_failed_clear"])
+@pytest.mark.parametrize("name", ["words_after_a_failed_launch", "words_after_a_failed_clear", "growing_sizes"])
 def test_host(program, name):
     r = subprocess.run([str(program), name], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
