@@ -18,16 +18,18 @@
  * calls in order on the GPU (its workspace is reused call after call).  The
  * workspace grows on demand; a call that has to grow it waits for the device, and
  * a block that is outgrown becomes half as large again, where there is room.
- * After a first call of the same sizes, the calls of this header do not
- * allocate.  A product of many rows takes, with M and N rounded up to 256 and K
- * to 64, 2 (M + N) K bytes, and for K above 1024 20 MB, or where that is more 4
- * M N bytes for each of the 1, 2 or 4 parts in which K is taken; operands that
- * peat_product_i8 rounds add a byte for each element.  A gradient list takes
- * 32 bytes for each tensor and 100 KB, and 40 more for each of more than 800.
+ * After a first call of the same sizes, types and alignment (of data and row
+ * distances to 16 bytes, which the choice of a product's kernel counts in), the
+ * calls of this header do not allocate.  A product of many rows takes, with M and
+ * N rounded up to 256 and K to 64, 2 (M + N) K bytes, and for K above 1024 20 MB,
+ * or where that is more 4 M N bytes for each of the 1, 2 or 4 parts in which K is
+ * taken; operands that peat_product_i8 rounds add a byte for each element.  A
+ * gradient list takes 32 bytes for each tensor and 100 KB; one of more than 800
+ * takes 40 more for each, and 160 of pinned host memory.
  *
- * The calls can be captured into a CUDA graph, once a call of the same sizes has
- * been made before (a call that would have to allocate, and a gradient list of
- * more than 800 tensors, which the host stages, return PEAT_ERR_UNSUPPORTED).
+ * The calls can be captured into a CUDA graph, once such a first call has been
+ * made (a call that would have to allocate, and a gradient list of more than 800
+ * tensors, which the host stages, return PEAT_ERR_UNSUPPORTED).
  * The graph uses the handle's workspace: it lives as long as the handle, and its
  * launches and the handle's calls stay in order on the GPU.
  *

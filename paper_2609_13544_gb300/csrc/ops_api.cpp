@@ -149,6 +149,40 @@ peat_status_t tickets(peat_handle_t h, OpsState* s, size_t n, cudaStream_t st) {
   return cuda_fail(h, e, "cudaMemsetAsync(counters)");
 }
 
+// a staging buffer whose last copy has been taken
+peat_status_t slot_free(peat_handle_t h, OpsState* s, int slot) {
+  if (!s->pending[slot]) return PEAT_OK;
+  cudaError_t e = cudaEventSynchronize(s->taken[slot]);
+  if (e != cudaSuccess) return cuda_fail(h, e, "cudaEventSynchronize");
+  s->pending[slot] = false;
+  return PEAT_OK;
+}
+// Staging buffers of `bytes` at least: all of the ring at once, so that only a
+// first call of its size allocates; outgrown ones as `grow` has it.
+peat_status_t staging(peat_handle_t h, OpsState* s, size_t bytes) {
+  for (int i = 0; i < OpsState::RING; i++) {
+    if (!s->taken[i] && cudaEventCreateWithFlags(&s->taken[i], cudaEventDisableTiming) != cudaSuccess) {
+      cudaGetLastError();
+      s->taken[i] = nullptr;
+      return fail(h, PEAT_ERR_ALLOC, "operator staging allocation failed");
+    }
+    if (bytes <= s->h_list_cap[i]) continue;
+    peat_status_t ps = slot_free(h, s, i);
+    if (ps != PEAT_OK) return ps;
+    const size_t room = std::max(bytes, s->h_list_cap[i] + s->h_list_cap[i] / 2);
+    if (s->h_list[i]) cudaFreeHost(s->h_list[i]);
+    s->h_list[i] = nullptr;
+    s->h_list_cap[i] = 0;
+    if (cudaMallocHost(&s->h_list[i], room) != cudaSuccess) {
+      cudaGetLastError();
+      s->h_list[i] = nullptr;
+      return fail(h, PEAT_ERR_ALLOC, "operator staging allocation failed");
+    }
+    s->h_list_cap[i] = room;
+  }
+  return PEAT_OK;
+}
+
 // the checks of a quantisation, and its launches' parameters but for the workspace
 peat_status_t quant_params(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int axis,
                            int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv, peat::QuantParams* p) {
@@ -503,29 +537,12 @@ peat_status_t grad_pass(peat_handle_t h, const peat_grad_t* list, int64_t count,
   if (listed && s->capturing)
     return fail(h, PEAT_ERR_UNSUPPORTED, "a list of more than 800 tensors cannot be captured: it is staged by the host");
   if (listed) {
+    ps = staging(h, s, listed);
+    if (ps != PEAT_OK) return ps;
     slot = s->next;
     s->next = (s->next + 1) % OpsState::RING;
-    if (!s->taken[slot] && cudaEventCreateWithFlags(&s->taken[slot], cudaEventDisableTiming) != cudaSuccess) {
-      cudaGetLastError();
-      s->taken[slot] = nullptr;
-      return fail(h, PEAT_ERR_ALLOC, "operator staging allocation failed");
-    }
-    if (s->pending[slot]) {
-      cudaError_t e = cudaEventSynchronize(s->taken[slot]);
-      if (e != cudaSuccess) return cuda_fail(h, e, "cudaEventSynchronize");
-      s->pending[slot] = false;
-    }
-    if (listed > s->h_list_cap[slot]) {
-      if (s->h_list[slot]) cudaFreeHost(s->h_list[slot]);
-      s->h_list[slot] = nullptr;
-      s->h_list_cap[slot] = 0;
-      if (cudaMallocHost(&s->h_list[slot], listed) != cudaSuccess) {
-        cudaGetLastError();
-        s->h_list[slot] = nullptr;
-        return fail(h, PEAT_ERR_ALLOC, "operator staging allocation failed");
-      }
-      s->h_list_cap[slot] = listed;
-    }
+    ps = slot_free(h, s, slot);
+    if (ps != PEAT_OK) return ps;
     dst = static_cast<peat::GnEntry*>(s->h_list[slot]);
   }
   units = 0;

@@ -21,6 +21,7 @@ struct Runtime {
   bool capturing = false;
   bool fail_memset = false;
   size_t largest = (size_t)-1;  // block that can be had
+  int fail_pinned = 0;          // the pinned allocation from here on that fails (1: the next)
   int fail_step = -1;        // the quantiser's launch that fails
   int dirty = 0;             // words that a kernel should have found zero
   int allocations = 0;       // device, pinned and event allocations
@@ -71,7 +72,12 @@ cudaError_t cudaFree(void* p) {
   std::free(p);
   return cudaSuccess;
 }
-cudaError_t cudaMallocHost(void** p, size_t n) { return rt.allocations++, *p = std::malloc(n), cudaSuccess; }
+cudaError_t cudaMallocHost(void** p, size_t n) {
+  if (rt.fail_pinned && --rt.fail_pinned == 0) return cudaErrorMemoryAllocation;
+  rt.allocations++;
+  *p = std::malloc(n);
+  return cudaSuccess;
+}
 cudaError_t cudaFreeHost(void* p) { return std::free(p), cudaSuccess; }
 cudaError_t cudaMemset(void* p, int v, size_t n) { return std::memset(p, v, n), cudaSuccess; }
 cudaError_t cudaMemsetAsync(void* p, int v, size_t n, cudaStream_t) {
@@ -219,6 +225,22 @@ void growing_sizes() {
   CHECK(rt.dirty == 0);
 }
 
+// After a first call of its size a gradient list allocates nothing, a long one
+// neither, whichever staging buffer its turn brings.
+void lists_allocate_once() {
+  Host u;
+  for (int64_t n : {5, 801, 2500, 900, 6000}) {
+    CHECK(u.norm(n) == PEAT_OK);
+    const int before = rt.allocations;
+    for (int i = 0; i < 9; i++) CHECK(u.norm(n) == PEAT_OK);
+    CHECK(rt.allocations == before);
+  }
+  // staging that could not be had: the call says so, and the next one tries again
+  rt.fail_pinned = 2;
+  CHECK(u.norm(20000) == PEAT_ERR_ALLOC);
+  for (int i = 0; i < 9; i++) CHECK(u.norm(20000) == PEAT_OK);
+}
+
 const struct {
   const char* name;
   void (*run)();
@@ -226,6 +248,7 @@ const struct {
     {"words_after_a_failed_launch", words_after_a_failed_launch},
     {"words_after_a_failed_clear", words_after_a_failed_clear},
     {"growing_sizes", growing_sizes},
+    {"lists_allocate_once", lists_allocate_once},
 };
 
 }  // namespace

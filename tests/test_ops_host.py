@@ -18,7 +18,8 @@ def program(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("name", ["words_after_a_failed_launch", "words_after_a_failed_clear", "growing_sizes"])
+@pytest.mark.parametrize("name", ["words_after_a_failed_launch", "words_after_a_failed_clear", "growing_sizes",
+                                  "lists_allocate_once"])
 def test_host(program, name):
     r = subprocess.run([str(program), name], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
