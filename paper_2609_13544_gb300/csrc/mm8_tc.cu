@@ -193,7 +193,7 @@ __device__ __forceinline__ int4 load_cluster(uint32_t addr) {
   asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
   return v;
 }
-// waits for the barrier's phase of this parity; false after `limit` polls
+// waits for the barrier's phase of this parity; false after `limit` polls (a thread by itself)
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit) {
   for (uint32_t i = 0; i < limit; i++) {
     uint32_t ok;
@@ -206,6 +206,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
     if (ok) return true;
   }
   return false;
+}
+// The same by all lanes of a warp, with one outcome: a wait may expire for some
+// lanes just as the phase completes for the others, and the warp must not part
+// before an instruction that takes all of it (tcgen05.ld, shuffles).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint32_t limit) {
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
 }
 // one lane of the warp; unlike a test of the lane's number, the compiler knows
 // that it is one (with the test a tile took 843 cycles per 64 k, with this 600)
@@ -551,7 +557,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (warp == PLAN_WARP) {
     int i = 0;
     for (int u = first; u < units && ok; u += step, i++) {
-      ok = mbar_wait(unplanned + 8 * (i % SLOTS), (i / SLOTS & 1) ^ 1, p.wait_limit);
+      ok = warp_wait(unplanned + 8 * (i % SLOTS), (i / SLOTS & 1) ^ 1, p.wait_limit);
       if (!ok) break;
       const Place t = place_of(p, u, part);
       // (where the kernel before is pack, the scales are older: complete before
@@ -586,7 +592,9 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
   } else if (warp == MMA_WARP) {
-    if (rank == 0) {
+    // (one thread for the whole loop: with all lanes waiting and voting on the
+    // outcome 16384 x 4096 x 1024 took 92.0 us, not 89.5)
+    if (rank == 0 && elect_one()) {
       int seq = 0, chunk = 0, i = 0;
       for (int u = first; u < units && ok; u += step, i++) {
         const Slot* t = slots + i % SLOTS;
@@ -602,7 +610,7 @@ __global__ void __launch_bounds__(THREADS, 1)
             if (!known || (c & 31) == 0) mask = t->drain[c >> 5];
             known = true;
             if (mask >> (c & 31) & 1) {
-              if (elect_one()) commit_both(acc_full + 8 * (chunk & 1), pair);
+              commit_both(acc_full + 8 * (chunk & 1), pair);
               chunk++;
               fresh = true;
             }
@@ -614,25 +622,21 @@ __global__ void __launch_bounds__(THREADS, 1)
           const int s = seq % STAGES;
           if (!(ok = mbar_wait(full + 8 * s, seq / STAGES & 1, p.wait_limit))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          if (elect_one()) {
-            const uint32_t d = tmem + (chunk & 1) * 256, base = sptr(smem + s * STAGE);
-            const uint64_t a = block_desc(base), b = block_desc(base + BLK);
+          const uint32_t d = tmem + (chunk & 1) * 256, base = sptr(smem + s * STAGE);
+          const uint64_t a = block_desc(base), b = block_desc(base + BLK);
 #pragma unroll
-            for (int j = 0; j < 4; j++) mma_256(d, a + 2 * j, b + 2 * j, !(fresh && j == 0));
-            commit_both(empty + 8 * s, pair);
-            if (k == k1 - 1) commit_both(acc_full + 8 * (chunk & 1), pair);
-          }
-          __syncwarp();
+          for (int j = 0; j < 4; j++) mma_256(d, a + 2 * j, b + 2 * j, !(fresh && j == 0));
+          commit_both(empty + 8 * s, pair);
+          if (k == k1 - 1) commit_both(acc_full + 8 * (chunk & 1), pair);
           fresh = false;
         }
         chunk++;
         if (ok && !known) ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit);
-        if (lane == 0) mbar_arrive(unplanned + 8 * (i % SLOTS));
+        mbar_arrive(unplanned + 8 * (i % SLOTS));
       }
       // whatever was issued is done before the accumulators are given back
-      if (elect_one()) commit_both(last, pair);
+      commit_both(last, pair);
       mbar_wait(last, 0, END_LIMIT);
-      __syncwarp();
     }
   } else {  // results: a warp has 32 rows and half of the columns
     int chunk = 0, i = 0;
@@ -641,7 +645,7 @@ __global__ void __launch_bounds__(THREADS, 1)
     const uint32_t release0 = mapa(acc_empty, even);
     for (int u = first; u < units && ok; u += step, i++) {
       const Slot* t = slots + i % SLOTS;
-      if (!(ok = mbar_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
+      if (!(ok = warp_wait(planned + 8 * (i % SLOTS), i / SLOTS & 1, p.wait_limit))) break;
       const int pieces = t->pieces;
       const int64_t row0 = (int64_t)t->mt * 256 + rank * 128 + quarter * 32;
       const int64_t col0 = (int64_t)t->nt * 256 + half * 128;
@@ -659,7 +663,7 @@ __global__ void __launch_bounds__(THREADS, 1)
       int4* shared_sums = reinterpret_cast<int4*>(smem) + mine;
       uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
       for (int q = 0; q < pieces && ok; q++, chunk++) {
-        if (!(ok = mbar_wait(acc_full + 8 * (chunk & 1), chunk / 2 & 1, p.wait_limit))) break;
+        if (!(ok = warp_wait(acc_full + 8 * (chunk & 1), chunk / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
         for (int g = 0; g < 4; g++) {
@@ -762,7 +766,7 @@ __global__ void __launch_bounds__(THREADS, 1)
   cg::this_cluster().sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   // (the last arrival in the odd CTA's shared memory, before it goes)
-  if (warp == MMA_WARP && rank) mbar_wait(last, 0, END_LIMIT);
+  if (warp == MMA_WARP && rank) warp_wait(last, 0, END_LIMIT);
   __syncwarp();
   if (warp == MMA_WARP)
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");

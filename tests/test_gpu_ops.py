@@ -835,3 +835,23 @@ def test_capture_refusals(peat_gpu):
             assert done.item() == 1
         check_quant(P, h, x, 1)
         assert abs(P.peat_grad_norm(h, long)["norm"] - 2403 ** 0.5) <= 1e-4
+
+
+@pytest.mark.parametrize("mnk", [(777, 1000, 2049), (600, 520, 20000)])
+def test_expired_wait_in_split_tiles(peat_gpu, h, mnk):
+    """The same where two or four CTA pairs of a cluster share a tile: all of them meet and end."""
+    import torch
+    M, N, K = mnk
+    g = rng(4)
+    a, b = ints(M, K, "uniform", g, -K % 16), ints(N, K, "uniform", g, -K % 16)
+    out = torch.empty(M, N, dtype=torch.int32, device="cuda")
+    bad = peat_gpu.Handle(0, flags=peat_gpu.PEAT_FLAG_TEST_EXPIRE_WAITS)
+    for _ in range(2):
+        peat_gpu.peat_matmul_i8_raw(bad, a, None, b, None, out)
+        torch.cuda.synchronize()
+        with pytest.raises(peat_gpu.PeatError) as e:
+            peat_gpu.peat_matmul_i8_raw(bad, a, None, b, None, out)
+        assert e.value.status == 5
+    bad.close()
+    peat_gpu.peat_matmul_i8_raw(h, a, None, b, None, out)
+    assert torch.equal(out.to(torch.int64), sums(a, b))
