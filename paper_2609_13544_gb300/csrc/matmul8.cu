@@ -469,10 +469,6 @@ double mm8_direct_time(int64_t M, int64_t N, int64_t K, bool aligned, int nsm) {
   return 6.5 + (aligned ? 0.8 : 1.4) * std::ceil((double)runs / S) * share;
 }
 
-bool mm8_aligned(const Mm8Params& p) {
-  return ((reinterpret_cast<uintptr_t>(p.a) | reinterpret_cast<uintptr_t>(p.b) | (uintptr_t)p.lda | (uintptr_t)p.ldb) & 15) == 0;
-}
-
 cudaError_t launch_mm8_direct(int out_dtype, const Mm8Params& p, int nsm, cudaStream_t s) {
   switch (out_dtype) {
     case PEAT_F32: return direct_out<PEAT_F32>(p, nsm, s);

@@ -880,9 +880,8 @@ cudaError_t launch_mm8_pack(const Mm8Params& m, const Mm8TcPlan& plan, char* ws,
   k.kc = plan.kc;
   k.first_b = which & 1 ? plan.mt * 2 * plan.kc : 0;  // (a matrix that is not asked for has no CTAs)
   const int64_t ctas = k.first_b + (which & 2 ? plan.nt * 2 * plan.kc : 0);
-  const uintptr_t a = which & 1 ? reinterpret_cast<uintptr_t>(m.a) | (uintptr_t)m.lda : 0;
-  const uintptr_t b = which & 2 ? reinterpret_cast<uintptr_t>(m.b) | (uintptr_t)m.ldb : 0;
-  return launch_dependent(((a | b) & 15) == 0 ? mm8_pack<16> : mm8_pack<1>, (unsigned)ctas, 256, 0, s, k);
+  const bool aligned = (!(which & 1) || mm8_rows_aligned(m.a, m.lda, m.M)) && (!(which & 2) || mm8_rows_aligned(m.b, m.ldb, m.N));
+  return launch_dependent(aligned ? mm8_pack<16> : mm8_pack<1>, (unsigned)ctas, 256, 0, s, k);
 }
 
 cudaError_t launch_mm8_tc(int out_dtype, const Mm8Params& m, const Mm8TcPlan& plan, char* ws, unsigned int* norms,

@@ -212,7 +212,7 @@ peat_status_t quant_params(peat_handle_t h, const void* x, int64_t rows, int64_t
   p->ldv = ldv;
   p->vec_x = aligned(x, 16) && (ldx % E == 0 || rows <= 1);
   const int qa = axis == 0 ? E : 4;
-  p->vec_q = q && aligned(q, qa) && ldq % qa == 0;
+  p->vec_q = q && aligned(q, qa) && (ldq % qa == 0 || (axis == 0 ? rows : cols) <= 1);
   p->vec_v = values && aligned(values, 16) && (ldv % E == 0 || rows <= 1);
   return PEAT_OK;
 }

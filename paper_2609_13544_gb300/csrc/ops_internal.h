@@ -80,8 +80,13 @@ struct Mm8TcPlan {
   int64_t na_words, nb_words;            // sums of squares of a's and of b's blocks (0: not needed)
 };
 double mm8_direct_time(int64_t M, int64_t N, int64_t K, bool aligned, int nsm);  // expected microseconds
-// whether the rows of a and b start on 16-byte boundaries
-bool mm8_aligned(const Mm8Params& p);
+// whether the rows of an operand start on 16-byte boundaries (one row has no use for a distance)
+inline bool mm8_rows_aligned(const int8_t* x, int64_t ld, int64_t rows) {
+  return reinterpret_cast<uintptr_t>(x) % 16 == 0 && (ld % 16 == 0 || rows <= 1);
+}
+inline bool mm8_aligned(const Mm8Params& p) {
+  return mm8_rows_aligned(p.a, p.lda, p.M) && mm8_rows_aligned(p.b, p.ldb, p.N);
+}
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int nsm);
 double mm8_tc_time(const Mm8TcPlan& p, int64_t K, int nsm);
 // norms: na_words, then nb_words; which: bit 0 a, bit 1 b

@@ -114,7 +114,6 @@ cudaError_t launch_quant8(int, int step, const QuantParams& p, int, cudaStream_t
 bool quant8_packs(int, int, const QuantParams&) { return false; }
 cudaError_t launch_mm8_direct(int, const Mm8Params&, int, cudaStream_t) { return cudaSuccess; }
 double mm8_direct_time(int64_t, int64_t, int64_t, bool, int) { return 1e30; }
-bool mm8_aligned(const Mm8Params&) { return true; }
 Mm8TcPlan mm8_tc_plan(int64_t M, int64_t N, int64_t K, int) {
   Mm8TcPlan p = {};
   p.bytes = 2 * (size_t)(M + N) * K;
@@ -241,6 +240,30 @@ void lists_allocate_once() {
   for (int i = 0; i < 9; i++) CHECK(u.norm(20000) == PEAT_OK);
 }
 
+// The row distance of a matrix of one row is not used: it does not keep its
+// kernel from whole vectors.
+void one_row_is_aligned() {
+  Host u;
+  int8_t* q = static_cast<int8_t*>(u.data());
+  auto quantize = [&](int64_t rows, int64_t ldq, int64_t at) {
+    CHECK(peat_quantize_i8(&u.h, u.data(), rows, 1001, 1008, PEAT_F16, 0, q + at, ldq, nullptr, nullptr, 0, nullptr) == PEAT_OK);
+    return rt.quant.vec_q;
+  };
+  CHECK(quantize(1, 1001, 0) && quantize(2, 1008, 0) && quantize(2, 1008, 8));
+  CHECK(!quantize(2, 1001, 0) && !quantize(1, 1001, 3));
+  auto transpose = [&](int64_t cols, int64_t ldq, int64_t at) {
+    CHECK(peat_quantize_i8(&u.h, u.data(), 11, cols, 1008, PEAT_F16, 1, q + at, ldq, nullptr, nullptr, 0, nullptr) == PEAT_OK);
+    return rt.quant.vec_q;
+  };
+  CHECK(transpose(1, 11, 0) && transpose(2, 12, 4) && !transpose(2, 11, 0) && !transpose(1, 11, 2));
+  auto aligned = [&](int64_t at, int64_t M, int64_t lda, int64_t N, int64_t ldb) {
+    return peat::mm8_aligned(peat::Mm8Params{q + at, q, lda, ldb, nullptr, nullptr, nullptr, nullptr, 0, M, N, 1001});
+  };
+  CHECK(aligned(0, 1, 1001, 5, 1008) && aligned(0, 5, 1008, 1, 1001) && aligned(0, 1, 1001, 1, 1001) &&
+        aligned(16, 5, 1008, 5, 1008));
+  CHECK(!aligned(0, 2, 1001, 5, 1008) && !aligned(0, 5, 1008, 2, 1001) && !aligned(8, 1, 1001, 5, 1008));
+}
+
 const struct {
   const char* name;
   void (*run)();
@@ -249,6 +272,7 @@ const struct {
     {"words_after_a_failed_clear", words_after_a_failed_clear},
     {"growing_sizes", growing_sizes},
     {"lists_allocate_once", lists_allocate_once},
+    {"one_row_is_aligned", one_row_is_aligned},
 };
 
 }  // namespace

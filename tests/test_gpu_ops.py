@@ -855,3 +855,27 @@ def test_expired_wait_in_split_tiles(peat_gpu, h, mnk):
     bad.close()
     peat_gpu.peat_matmul_i8_raw(h, a, None, b, None, out)
     assert torch.equal(out.to(torch.int64), sums(a, b))
+
+
+@pytest.mark.parametrize("K", [1, 15, 63, 1001, 4099])
+def test_one_row_against_many(peat_gpu, h, K):
+    """One row, whose distance to the next is nothing to go by, against padded rows, on either side; its integers from a
+    buffer of exactly their length."""
+    import torch
+    g = rng(K)
+    x = torch.randn(1, K, generator=g, device="cuda")
+    guard = torch.full((K + 16,), 55, dtype=torch.int8, device="cuda")
+    q, scale = guard[:K].view(1, K), torch.empty(1, device="cuda")
+    peat_gpu.peat_quantize_i8_raw(h, x, 0, q, scale)
+    eq, es, _ = quant_definition(x, 0)
+    assert torch.equal(q, eq) and same_bits(scale, es) and bool((guard[K:] == 55).all())
+    peat_gpu.peat_quantize_i8_raw(h, x.view(K, 1), 1, q, scale)
+    assert torch.equal(q, eq) and same_bits(scale, es) and bool((guard[K:] == 55).all())
+    for rows in (1, 7, 600, 9000):
+        b = ints(rows, K, "uniform", g, -K % 16)
+        for u, v in ((q, b), (b, q)):
+            buf = torch.full((u.shape[0] + 1, v.shape[0] + 3), -5, dtype=torch.int32, device="cuda")
+            out = buf[: u.shape[0], : v.shape[0]]
+            peat_gpu.peat_matmul_i8_raw(h, u, None, v, None, out)
+            assert torch.equal(out.to(torch.int64), sums(u, v))
+            assert bool((buf[u.shape[0]:] == -5).all()) and bool((buf[:, v.shape[0]:] == -5).all())
