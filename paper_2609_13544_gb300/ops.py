@@ -372,7 +372,7 @@ class Linear8:
         if not shape or shape[-1] != K:
             raise ValueError(f"the last dimension of {name} must be {K}")
         flat = len(shape) == 2
-        x = t if flat else t.reshape(-1, K)
+        x = t if flat else t.reshape(shape[:-1].numel(), K)
         a, M, _ = _operand(self.h, x, 0, None, name)
         out = torch.empty((M, N), dtype=x.dtype, device=x.device)
         _call(self.h, "peat_product_i8", ctypes.byref(a), ctypes.byref(op), _vector(self.h, bias, N, "bias"),
@@ -394,8 +394,8 @@ class Linear8:
                 return self.weight_grad(grad, x)
         if grad.shape[-1:] != (self.out_features,) or x.shape[-1:] != (self.in_features,):
             raise ValueError(f"the last dimensions of grad and x must be {self.out_features} and {self.in_features}")
-        g = grad if grad.dim() == 2 else grad.reshape(-1, self.out_features)
-        x = x if x.dim() == 2 else x.reshape(-1, self.in_features)
+        g = grad if grad.dim() == 2 else grad.reshape(grad.shape[:-1].numel(), self.out_features)
+        x = x if x.dim() == 2 else x.reshape(x.shape[:-1].numel(), self.in_features)
         if g.shape[0] != x.shape[0]:
             raise ValueError("grad and x differ in their leading dimensions")
         return peat_product_i8(self.h, g, x, 1, 1)

@@ -879,3 +879,17 @@ def test_one_row_against_many(peat_gpu, h, K):
             peat_gpu.peat_matmul_i8_raw(h, u, None, v, None, out)
             assert torch.equal(out.to(torch.int64), sums(u, v))
             assert bool((buf[u.shape[0]:] == -5).all()) and bool((buf[:, v.shape[0]:] == -5).all())
+
+
+def test_layer_without_inputs(peat_gpu, h):
+    """No features in, or no tokens."""
+    import torch
+    layer = peat_gpu.Linear8(h, torch.zeros(48, 0, device="cuda"))
+    x, dy = torch.zeros(2, 3, 0, device="cuda"), torch.ones(2, 3, 48, device="cuda")
+    y, (dx, dw) = layer.forward(x), layer.backward(dy, x)
+    assert y.shape == (2, 3, 48) and not y.any() and dx.shape == (2, 3, 0) and dw.shape == (48, 0)
+    layer = peat_gpu.Linear8(h, torch.ones(48, 64, device="cuda"))
+    for shape in ((0,), (2, 0)):
+        x, dy = torch.zeros(*shape, 64, device="cuda"), torch.ones(*shape, 48, device="cuda")
+        y, (dx, dw) = layer.forward(x), layer.backward(dy, x)
+        assert y.shape == (*shape, 48) and dx.shape == (*shape, 64) and dw.shape == (48, 64) and not dw.any()
