@@ -348,14 +348,25 @@ def peat_grad_clip(h, grads, max_norm: float, norm_type: str = "2", unscale: flo
         return _grad_record(record, norms, stream)
 
 
+def _as_rows(t, K: int):
+    """t [..., K] as a matrix with rows of their own: t, a view of it or, where its strides are others (transposed or
+    expanded tensors), a copy."""
+    x = t if t.dim() == 2 else t.reshape(t.shape[:-1].numel(), K)
+    s0, s1 = x.stride()
+    return x if (s1 == 1 or K <= 1) and (s0 >= K or x.shape[0] <= 1) else x.contiguous()
+
+
 class Linear8:
     """y = x w^T with w [out, in] held in 8-bit integers, by row for the forward product and by column for the
     input gradient; x and the output gradient are rounded as they come (by row, or, for the weight gradient, by
-    column).  Inputs are float32, float16 or bfloat16 with any leading dimensions; the layer keeps none of them."""
+    column).  Inputs are float32, float16 or bfloat16 with any leading dimensions and strides; the layer keeps none of
+    them."""
 
     def __init__(self, h, weight, stream=None):
         self.h = h
         self.out_features, self.in_features = weight.shape
+        with _on(stream):
+            weight = _as_rows(weight, self.in_features)
         self.q, self.scale = peat_quantize_i8(h, weight, 0, stream)
         self.qt, self.scale_t = peat_quantize_i8(h, weight, 1, stream)
         self._w = _operand(h, self.q, 0, self.scale, "weight")
@@ -371,13 +382,12 @@ class Linear8:
         shape = t.shape
         if not shape or shape[-1] != K:
             raise ValueError(f"the last dimension of {name} must be {K}")
-        flat = len(shape) == 2
-        x = t if flat else t.reshape(shape[:-1].numel(), K)
+        x = _as_rows(t, K)
         a, M, _ = _operand(self.h, x, 0, None, name)
         out = torch.empty((M, N), dtype=x.dtype, device=x.device)
         _call(self.h, "peat_product_i8", ctypes.byref(a), ctypes.byref(op), _vector(self.h, bias, N, "bias"),
               out.data_ptr(), N, _code(out), _stream(self.h, None))
-        return out if flat else out.view(*shape[:-1], N)
+        return out if len(shape) == 2 else out.view(*shape[:-1], N)
 
     def forward(self, x, bias=None, stream=None):
         """x [..., in] -> [..., out] of x's type."""
@@ -394,8 +404,7 @@ class Linear8:
                 return self.weight_grad(grad, x)
         if grad.shape[-1:] != (self.out_features,) or x.shape[-1:] != (self.in_features,):
             raise ValueError(f"the last dimensions of grad and x must be {self.out_features} and {self.in_features}")
-        g = grad if grad.dim() == 2 else grad.reshape(grad.shape[:-1].numel(), self.out_features)
-        x = x if x.dim() == 2 else x.reshape(x.shape[:-1].numel(), self.in_features)
+        g, x = _as_rows(grad, self.out_features), _as_rows(x, self.in_features)
         if g.shape[0] != x.shape[0]:
             raise ValueError("grad and x differ in their leading dimensions")
         return peat_product_i8(self.h, g, x, 1, 1)

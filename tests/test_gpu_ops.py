@@ -881,6 +881,25 @@ def test_one_row_against_many(peat_gpu, h, K):
             assert bool((buf[u.shape[0]:] == -5).all()) and bool((buf[:, v.shape[0]:] == -5).all())
 
 
+def test_layer_takes_any_strides(peat_gpu, h):
+    """Transposed, sliced and expanded tensors (a broadcast sum's gradient among them) give what their copies give, two
+    dimensions like three."""
+    import torch
+    g = rng(31)
+    normal = lambda *shape: torch.randn(*shape, generator=g, device="cuda").to(torch.bfloat16)
+    xs = [normal(64, 40).t(), normal(5, 8, 128)[:, :, ::2], normal(40, 1).expand(40, 64), normal(64).expand(5, 8, 64),
+          normal(8, 5, 64).transpose(0, 1), normal(1, 1).expand(40, 64)]
+    gs = [normal(48, 40).t(), normal(5, 8, 96)[:, :, 48:], normal(48).expand(40, 48), normal(1, 1, 1).expand(5, 8, 48),
+          normal(8, 5, 48).transpose(0, 1), normal(48, 40).t()]
+    w = normal(64, 48).t()
+    layer, want = peat_gpu.Linear8(h, w), peat_gpu.Linear8(h, w.contiguous())
+    for x, dy in zip(xs, gs):
+        xc, dc = x.contiguous(), dy.contiguous()
+        assert same_bits(layer.forward(x), want.forward(xc))
+        for got, expected in zip(layer.backward(dy, x), want.backward(dc, xc)):
+            assert same_bits(got, expected)
+
+
 def test_layer_without_inputs(peat_gpu, h):
     """No features in, or no tokens."""
     import torch
