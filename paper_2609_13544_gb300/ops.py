@@ -273,8 +273,11 @@ class GradList:
                 raise ValueError("gradients and outputs must be CUDA tensors on one device")
             if o.dtype != t.dtype or o.shape != t.shape:
                 raise ValueError("an output differs from its gradient in type or shape")
-            dense = t.is_contiguous() or (t.dim() == 4 and t.is_contiguous(memory_format=torch.channels_last))
-            if not dense or (o is not t and o.stride() != t.stride()):
+            # (by order in memory: the strides of dimensions of size 1 tell nothing)
+            same = t.is_contiguous() and o.is_contiguous()
+            if not same and t.dim() == 4:
+                same = all(v.is_contiguous(memory_format=torch.channels_last) for v in (t, o))
+            if not same:
                 raise ValueError("gradients must be contiguous (or channels-last), outputs of the same layout")
             self.entries[i] = GradEntry(t.data_ptr(), o.data_ptr(), t.numel(), code, 0)
 

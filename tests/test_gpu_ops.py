@@ -912,3 +912,22 @@ def test_layer_without_inputs(peat_gpu, h):
         x, dy = torch.zeros(*shape, 64, device="cuda"), torch.ones(*shape, 48, device="cuda")
         y, (dx, dw) = layer.forward(x), layer.backward(dy, x)
         assert y.shape == (*shape, 48) and dx.shape == (*shape, 64) and dw.shape == (48, 64) and not dw.any()
+
+
+def test_grad_outputs_of_the_same_order(peat_gpu, h):
+    """An output lies in memory as its gradient does, whatever the strides of dimensions of size 1 say; another order is
+    refused."""
+    import torch
+    g = rng(8)
+    last = torch.channels_last
+    one = torch.randn(6, 5, 1, 1, generator=g, device="cuda").as_strided((6, 5, 1, 1), (5, 1, 5, 5))
+    full = torch.randn(6, 5, 3, 2, generator=g, device="cuda").to(memory_format=last)
+    deep = torch.randn(6, 1, 3, 2, generator=g, device="cuda").to(memory_format=last)
+    ts = [one, full, deep]
+    outs = [torch.empty(6, 5, 1, 1, device="cuda"), torch.empty_like(full), torch.empty(6, 1, 3, 2, device="cuda")]
+    r = peat_gpu.peat_grad_clip(h, peat_gpu.GradList(ts, outs), 0.5)
+    for t, o in zip(ts, outs):
+        assert torch.equal(o, t * np.float32(r["coef"]))
+    for t, o in ((full, torch.empty(6, 5, 3, 2, device="cuda")), (full.contiguous(), torch.empty_like(full))):
+        with pytest.raises(ValueError):
+            peat_gpu.GradList([t], [o])
