@@ -931,3 +931,26 @@ def test_grad_outputs_of_the_same_order(peat_gpu, h):
     for t, o in ((full, torch.empty(6, 5, 3, 2, device="cuda")), (full.contiguous(), torch.empty_like(full))):
         with pytest.raises(ValueError):
             peat_gpu.GradList([t], [o])
+
+
+@pytest.mark.parametrize("fill", ["low", "high", "gauss", "uniform"])
+@pytest.mark.parametrize("mnk", [(2500, 2500, 2000), (5000, 4700, 2100), (4800, 1000, 9000)])
+def test_matmul_long_sums_of_many_tiles(peat_gpu, h, fill, mnk):
+    """Sums that leave the accumulator in several pieces where no tile is split: one or two tiles a CTA pair, five of them
+    (more than are planned ahead), and pieces past the first 32 norm blocks."""
+    import torch
+    M, N, K = mnk
+    g = rng(M + K)
+    a, b = ints(M, K, fill, g, -K % 16), ints(N, K, fill, g, -K % 16)
+    if fill == "gauss":  # some rows and some stretches of k that need their pieces, others that do not
+        a[: M // 2].fill_(-128)
+        b[:, : K // 2].fill_(127)
+    want = sums(a, b)
+    sa, sb = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+    scaled = want.float() * (sa[:, None] * sb[None, :])
+    out = torch.empty(M, N, dtype=torch.int32, device="cuda")
+    for _ in range(2):
+        out.fill_(-1)
+        peat_gpu.peat_matmul_i8_raw(h, a, None, b, None, out)
+        assert torch.equal(out, want.int())
+    assert same_bits(peat_gpu.peat_matmul_i8(h, a, sa, b, sb), scaled)
