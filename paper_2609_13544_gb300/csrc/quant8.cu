@@ -6,8 +6,7 @@
 // without sign, which order as the magnitudes do, infinities and NaNs on top.
 //
 // Bound by memory: a row is read once and kept in registers between the
-// maximum and the rounding; columns are read twice, as far as they fit from L2
-// the second time.
+// maximum and the rounding; columns are read twice.
 #include <algorithm>
 
 #include "ops_internal.h"
@@ -286,7 +285,7 @@ __device__ __forceinline__ void put_row_vec(const QuantParams& p, uint4 v, int64
 // registers between the maximum and the rounding.  PACK: into a packed operand,
 // with zeros in its margins, and the largest sums of squares handed on once for
 // all rows.  16384 x 4096 bfloat16 with values take 49 us, 5.5 TB/s; 11590 x 1749
-// binary16 with values, rows off the grid, 27 (on it, x 1752: 13).
+// binary16 with values, rows off the grid, 40 (on it, x 1752: 17).
 template <int DT, int TPR, int NV, bool PACK, bool GRID>
 __global__ void __launch_bounds__(QT) quant_rows(QuantParams p, int each) {
   using L = Elem<DT>;
@@ -388,16 +387,16 @@ __global__ void __launch_bounds__(QT) quant_long_rows(QuantParams p) {
 // Columns, in two launches (one for few rows, QUANT_FEW_ROWS).  The first finds
 // each column's maximum: a thread has a 16-byte vector of columns and walks down
 // a share of the rows, the shares meet by atomic maxima of the patterns (order
-// makes no difference to a maximum).  The second reads the matrix again, last
-// rows first, so that it finds in L2 what the first read last, in tiles of 128
+// makes no difference to a maximum).  The second reads the matrix again (last
+// rows first, which L2 may still hold, it takes no less time), in tiles of 128
 // rows by 128 bytes, and writes the integers transposed through shared memory,
 // 128 contiguous ones of a column at a time.  16384 x 4096 bfloat16 with values
-// take 70 us, 5.7 TB/s of what the two launches read and write; with q alone 68.
+// take 73 us, 5.5 TB/s of what the two launches read and write; with q alone 71.
 // (One launch of clusters that keep a strip of columns to themselves, meet in
 // distributed shared memory and read the strip again from L2 took 101 us: its
 // phases wait for each other.)  Rows off the 16-byte grid take two aligned loads
 // for a vector in the second launch, and their values go through shared memory,
-// an element a lane: 16384 x 4095 take 173 us, with q alone 123, bound by
+// an element a lane: 16384 x 4095 take 173 us, with q alone 125, bound by
 // instructions (two elements a lane: 202; values from the registers: 232).
 template <int DT>
 __global__ void __launch_bounds__(QT, 4) quant_colmax(QuantParams p, int vl, int64_t rows_each) {
@@ -480,7 +479,7 @@ __global__ void __launch_bounds__(QT, 3) quant_cols(QuantParams p, int64_t rows_
   const int64_t c0 = (int64_t)blockIdx.x * CW, col = c0 + tx * L::E;
   const int64_t left = p.cols - col;  // may be <= 0
   // (a packed operand's k go on to a whole block: zeros)
-  const int64_t r0 = (int64_t)(gridDim.y - 1 - blockIdx.y) * rows_each,
+  const int64_t r0 = (int64_t)blockIdx.y * rows_each,
                 r1 = min(PACK ? (int64_t)p.kb * 64 : p.rows, r0 + rows_each);
   const typename L::T* x = static_cast<const typename L::T*>(p.x) + col;
   begin(p);
