@@ -128,8 +128,9 @@ __global__ void __launch_bounds__(RT) mm8_rows(Mm8Params p) {
 
 // ---- up to 64 rows of a and many of b: a stream over b ------------------------
 // The rows of a are turned into binary16 once per CTA, in the very registers'
-// order, and stay in shared memory (a run of 1024 k of them at a time where
-// they are longer); every warp then streams 16 rows of b past them, so a byte
+// order, and stay in shared memory (up to 4096 k of 8 rows, 2048 of 16 and 32, 1024
+// of 64; longer rows are turned piece by piece for every round of tiles); every
+// warp then streams 16 rows of b past them, so a byte
 // of b costs its load, its conversion and its share of the instructions.  Where
 // a CTA has few such tiles, 2 to 16 warps (`1 << shift`) share the runs of one
 // and meet in shared memory; not where that takes more rounds (two warps a tile

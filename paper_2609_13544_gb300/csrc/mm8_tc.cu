@@ -26,9 +26,11 @@
 // 768 k, normally distributed ones about every 16 000; up to 1024 k nothing can
 // add up to more, and no norms are made.
 //
-// 8192 x 8192 x 8192 to bfloat16 takes 575 us (1910 TFLOP/s, what the library's
-// bfloat16 product reaches), with extreme integers 727; 16384 x 4096 x 1024 83,
-// of which pack has 10; 2048 x 1024 x 4096, 32 tiles with k in two parts, 26.
+// 8192 x 8192 x 8192 to bfloat16 takes 590 us in bursts (1860 TFLOP/s) and 620 to
+// 635 without a pause, at the power limit (1690 to 1755 MHz; the library's
+// bfloat16 product of normal numbers 573 and 643), with extreme integers 716 to
+// 727 at 2070 MHz; 16384 x 4096 x 1024 88 to 92, of which pack has 10; 2048 x
+// 1024 x 4096, 32 tiles with k in two parts, 26.
 // pack is bound by memory: 52 million integers take 22 us, 7 TB/s.
 #include <cooperative_groups.h>
 #include <cuda.h>
