@@ -587,9 +587,11 @@ peat_status_t guarded(peat_handle_t h, F f) {
   if (!h) return PEAT_ERR_INVALID_ARG;
   try {
     return f();
-  } catch (const std::bad_alloc&) {
+  } catch (const std::bad_alloc&) {  // (texts that a string holds in itself: setting them throws nothing)
+    h->err = "out of memory";
     return PEAT_ERR_ALLOC;
   } catch (...) {
+    h->err = "internal error";
     return PEAT_ERR_INTERNAL;
   }
 }

@@ -10,6 +10,8 @@
 #include <cstdlib>
 #include <cstring>
 #include <map>
+#include <new>
+#include <string>
 #include <vector>
 
 #include "ops_internal.h"
@@ -20,6 +22,7 @@ namespace {
 struct Runtime {
   bool capturing = false;
   bool fail_memset = false;
+  bool fail_new = false;
   size_t largest = (size_t)-1;  // block that can be had
   int fail_pinned = 0;          // the pinned allocation from here on that fails (1: the next)
   int fail_step = -1;        // the quantiser's launch that fails
@@ -47,6 +50,14 @@ void check(bool ok, const char* what, int line) {
 #define CHECK(x) check((x), #x, __LINE__)
 
 }  // namespace
+
+void* operator new(size_t n) {
+  if (rt.fail_new) throw std::bad_alloc();
+  if (void* p = std::malloc(n ? n : 1)) return p;
+  throw std::bad_alloc();
+}
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, size_t) noexcept { std::free(p); }
 
 // ---- the runtime ----
 extern "C" {
@@ -264,6 +275,20 @@ void one_row_is_aligned() {
   CHECK(!aligned(0, 2, 1001, 5, 1008) && !aligned(0, 5, 1008, 2, 1001) && !aligned(8, 1, 1001, 5, 1008));
 }
 
+// Host memory that runs out is a status with a text of its own, and the handle works on.
+void host_memory() {
+  Host u;
+  CHECK(peat_quantize_i8(&u.h, nullptr, 1, 1, 1, PEAT_F32, 0, nullptr, 0, nullptr, nullptr, 0, nullptr) == PEAT_ERR_INVALID_ARG);
+  const std::string before = u.h.err;
+  std::vector<peat_grad_t> list(3, peat_grad_t{u.data(), nullptr, 3, PEAT_F32, 0});
+  rt.fail_new = true;
+  const peat_status_t st = peat_grad_norm(&u.h, list.data(), 3, PEAT_NORM_2, 1.0f, static_cast<peat_gradnorm_t*>(u.data()),
+                                          nullptr, nullptr);
+  rt.fail_new = false;
+  CHECK(st == PEAT_ERR_ALLOC && u.h.err != before && !u.h.err.empty());
+  CHECK(u.norm(3) == PEAT_OK);
+}
+
 const struct {
   const char* name;
   void (*run)();
@@ -273,6 +298,7 @@ const struct {
     {"growing_sizes", growing_sizes},
     {"lists_allocate_once", lists_allocate_once},
     {"one_row_is_aligned", one_row_is_aligned},
+    {"host_memory", host_memory},
 };
 
 }  // namespace

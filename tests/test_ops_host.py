@@ -19,7 +19,7 @@ def program(tmp_path_factory):
 
 
 @pytest.mark.parametrize("name", ["words_after_a_failed_launch", "words_after_a_failed_clear", "growing_sizes",
-                                  "lists_allocate_once", "one_row_is_aligned"])
+                                  "lists_allocate_once", "one_row_is_aligned", "host_memory"])
 def test_host(program, name):
     r = subprocess.run([str(program), name], capture_output=True, text=True)
     assert r.returncode == 0, r.stdout
