@@ -1,0 +1,159 @@
+// Matrices of float32, binary16 or bfloat16 by 16-byte vectors: element types,
+// magnitudes, loads and stores at any multiple of the element's size.
+#pragma once
+#include "vec16.cuh"
+
+namespace peat {
+
+template <int DT>
+struct Elem;
+template <>
+struct Elem<PEAT_F32> {
+  using T = float;
+  static constexpr int E = 4;  // elements of a 16-byte vector
+  static constexpr uint32_t INF = 0x7f800000u;
+  static __device__ __forceinline__ float mag(uint32_t b) { return __uint_as_float(b); }
+};
+template <>
+struct Elem<PEAT_F16> {
+  using T = __half;
+  static constexpr int E = 8;
+  static constexpr uint32_t INF = 0x7c00u;
+  static __device__ __forceinline__ float mag(uint32_t b) { return __half2float(__ushort_as_half((unsigned short)b)); }
+};
+template <>
+struct Elem<PEAT_BF16> {
+  using T = __nv_bfloat16;
+  static constexpr int E = 8;
+  static constexpr uint32_t INF = 0x7f80u;
+  static __device__ __forceinline__ float mag(uint32_t b) { return __uint_as_float(b << 16); }
+};
+
+// a 16-byte vector as its elements
+template <int DT>
+union Vec {
+  uint4 u;
+  typename Elem<DT>::T e[Elem<DT>::E];
+  __device__ Vec() {}
+};
+
+// elementwise maximum of the magnitudes; a NaN on either side stays (as a NaN
+// pattern, above every number's).  The types' own maxima: the packed integer
+// ones are several instructions each on this GPU.
+__device__ __forceinline__ uint32_t max_f32(uint32_t m, uint32_t v) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(m)), "f"(fabsf(__uint_as_float(v))));
+  return __float_as_uint(r) & 0x7fffffffu;
+}
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t m, uint32_t v) {
+  uint32_t r;
+  asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(v & 0x7fff7fffu));
+  return r;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t m, uint32_t v) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(v & 0x7fff7fffu));
+  return r;
+}
+template <int DT>
+__device__ __forceinline__ uint32_t max_word(uint32_t m, uint32_t v) {
+  return DT == PEAT_F32 ? max_f32(m, v) : (DT == PEAT_F16 ? max_f16x2(m, v) : max_bf16x2(m, v));
+}
+template <int DT>
+__device__ __forceinline__ uint4 mag_max(uint4 m, uint4 v) {
+  return make_uint4(max_word<DT>(m.x, v.x), max_word<DT>(m.y, v.y), max_word<DT>(m.z, v.z), max_word<DT>(m.w, v.w));
+}
+template <int DT>
+__device__ __forceinline__ uint32_t mag_fold(uint4 m) {  // the largest of the vector
+  const uint32_t a = max_word<DT>(max_word<DT>(m.x, m.y), max_word<DT>(m.z, m.w));
+  return DT == PEAT_F32 ? a : max(a & 0xffffu, a >> 16);
+}
+
+// Vectors of E elements at any multiple of the element's size.  On the 16-byte
+// grid one load; off it the two aligned vectors that hold it, shifted together.
+// A vector that is not whole (`left` elements exist), or whose aligned vectors
+// reach beyond the matrix, is left for load_edge.
+template <int DT, bool GRID>
+struct Source {
+  using T = typename Elem<DT>::T;
+  uintptr_t lo, hi;  // the matrix's bytes
+  __device__ Source(const void* at, int64_t rows, int64_t cols, int64_t ld) {
+    const T* x = static_cast<const T*>(at);
+    lo = reinterpret_cast<uintptr_t>(x);
+    hi = reinterpret_cast<uintptr_t>(x + (rows - 1) * ld + cols);
+  }
+  __device__ __forceinline__ bool whole(const T* p, int64_t left) const {
+    if (left < Elem<DT>::E) return false;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15;
+    return GRID || (a >= lo && a + 32 <= hi);
+  }
+  __device__ __forceinline__ uint4 load(const T* p) const {
+    if (GRID) return __ldg(reinterpret_cast<const uint4*>(p));
+    const uint4* a = on_grid(p);
+    return shifted(__ldg(a), __ldg(a + 1), (int)(reinterpret_cast<uintptr_t>(p) & 15));
+  }
+  static __device__ __forceinline__ const uint4* on_grid(const T* p) {
+    return reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
+  }
+};
+// the first `left` elements of a vector, one by one, zeros beyond
+template <int DT>
+__device__ __forceinline__ uint4 load_edge(const typename Elem<DT>::T* p, int64_t left) {
+  Vec<DT> v;
+  v.u = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::E; e++)
+    if (e < left) v.e[e] = p[e];
+  return v.u;
+}
+
+// A vector's values at o, of which `left` (any number) exist, by G lanes that
+// have consecutive vectors of a row.  Where the row is off the 16-byte grid a
+// lane writes the aligned vector that ends inside its own, the last elements of
+// the vector before in front: the lane before's, or for lane 0 `carry`, the last
+// lane's of the call before, unless this is the first.  What no vector of the
+// group precedes or follows goes one by one.  All lanes of a group call it.
+template <int DT, int G>
+__device__ __forceinline__ void store_values(typename Elem<DT>::T* o, const float (&y)[Elem<DT>::E], bool on_grid,
+                                             int64_t left, uint4& carry, bool first, bool last) {
+  constexpr int E = Elem<DT>::E, B = 16 / E;
+  Vec<DT> v;
+  v.u = pack<DT>(y);
+  if (on_grid) {
+    if (left >= E) {
+      __stcs(reinterpret_cast<uint4*>(o), v.u);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e++)
+        if (e < left) o[e] = v.e[e];
+    }
+    return;
+  }
+  const int lane = threadIdx.x % G;
+  // (a rotation: lane 0 receives the last lane's, for the next call)
+  auto turned = [&](uint32_t x, uint32_t& kept) {
+    const uint32_t t = __shfl_sync(0xffffffffu, x, (lane + G - 1) % G, G);
+    const uint32_t before = lane == 0 ? kept : t;
+    kept = t;
+    return before;
+  };
+  const uint4 before = make_uint4(turned(v.u.x, carry.x), turned(v.u.y, carry.y), turned(v.u.z, carry.z), turned(v.u.w, carry.w));
+  const int s = (int)(reinterpret_cast<uintptr_t>(o) & 15) / B;  // elements from the grid to o
+  const bool alone = first && lane == 0;
+  Vec<DT> w;
+  w.u = s ? shifted(before, v.u, 16 - s * B) : v.u;
+  if ((!alone || s == 0) && left >= E - s) {
+    __stcs(reinterpret_cast<uint4*>(o - s), w.u);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e++)
+      if ((!alone || e >= s) && e - s < left) o[e - s] = w.e[e];
+  }
+  if (last && lane == G - 1) {  // its own last elements
+#pragma unroll
+    for (int e = 0; e < E; e++)
+      if (e >= E - s && e < left) o[e] = v.e[e];
+  }
+}
+
+}  // namespace peat
