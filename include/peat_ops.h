@@ -112,6 +112,135 @@ typedef struct {
 peat_status_t peat_product_i8(peat_handle_t h, const peat_operand_t* a, const peat_operand_t* b, const float* bias,
                               void* out, int64_t ldo, peat_dtype_t out_dtype, peat_stream_t stream);
 
+/* ---- 4-bit floating point with a scale for each block ----
+ *
+ * A 4-bit value is +-0, 0.5, 1, 1.5, 2, 3, 4 or 6: one sign bit (bit 3 of its
+ * code), two exponent bits, one mantissa bit.  Blocks along the product's axis
+ * share a scale:
+ *   PEAT_MXFP4  32 values, a power of two 2^e in one byte, e + 127 (255: NaN)
+ *   PEAT_NVFP4  16 values, an 8-bit float (4 exponent bits, bias 7, 3 mantissa
+ *               bits, sign 0; 0x7f: NaN), below a float32 scale of the whole row
+ * Codes lie two to a byte, the first in the low half; a row is whole blocks and
+ * starts on a 16-byte boundary.  Block scales lie in tiles of 128 rows by 4
+ * blocks, 512 bytes: row r of a tile and block k at (r mod 32) * 16 + (r div 32) *
+ * 4 + k; the tiles of the first 128 rows come first, in the order of the blocks.
+ * A matrix of `rows` rows and `blocks` blocks a row has peat_f4_scale_bytes of
+ * them; what lies in the margins of the tiles is zero (or any scale but NaN). */
+typedef enum { PEAT_MXFP4 = 0, PEAT_NVFP4 = 1 } peat_f4_t;
+
+/* Bytes of a matrix's block scales: ceil(rows / 128) * ceil(blocks / 4) * 512. */
+static inline int64_t peat_f4_scale_bytes(int64_t rows, int64_t blocks) {
+  return (rows + 127) / 128 * ((blocks + 3) / 4) * 512;
+}
+
+/* Rounds a matrix x [rows, cols] (PEAT_F32, PEAT_F16 or PEAT_BF16; row r at x + r
+ * * ldx elements, ldx >= cols) to 4-bit values, with blocks along its rows (axis
+ * 0) or down its columns (axis 1).  E2M1(v) is the code nearest to v, ties to the
+ * even code, at most 6 in magnitude; all operations are float32 ones.
+ *   PEAT_MXFP4  amax = max |x| over the block; e = floor(log2(amax)) - 2, at least
+ *               -127 (amax = 0: -127); code = E2M1(x * 2^-e).  A block that holds
+ *               a NaN or an infinity has codes 0 and scale NaN.
+ *   PEAT_NVFP4  over the row (column): amax = max |x|, scale = amax / 2688, t =
+ *               2688 / amax; over the block: b = the 8-bit float nearest to (max
+ *               |x| * t) / 6, ties to even; code = E2M1((x * t) * (1 / b)), 0 where
+ *               b = 0.  Where t is not finite (amax = 0, or below about 7.9e-36)
+ *               scale, b and codes are 0; a row that holds a NaN or an infinity has
+ *               b and codes 0 and scale = NaN.
+ *
+ * Outputs, each optional (NULL), but for at least one of q and values; q needs
+ * block_scale, and with PEAT_NVFP4 scale:
+ *   q            axis 0: [rows, ceil(cols / block) * block / 2 bytes], row r at q +
+ *                r * ldq bytes; axis 1: the transpose, [cols, ceil(rows / block) *
+ *                block / 2 bytes].  ldq a multiple of 16; codes beyond the matrix
+ *                are 0.
+ *   block_scale  peat_f4_scale_bytes(rows of q, blocks of a row), margins 0.
+ *   scale        PEAT_NVFP4: float32 [rows] (axis 0) or [cols] (axis 1).
+ *   values       [rows, cols] of x's type, row r at values + r * ldv: the code's
+ *                value times 2^e, or times b, times scale (each product rounded),
+ *                rounded to the type.
+ * The outputs must not overlap x.  Fastest with 16-byte aligned rows. */
+peat_status_t peat_quantize_f4(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx,
+                               peat_dtype_t dtype, peat_f4_t format, int axis, uint8_t* q, int64_t ldq,
+                               uint8_t* block_scale, float* scale, void* values, int64_t ldv, peat_stream_t stream);
+
+/* out[m, n] = acc * (a_scale[m] * b_scale[n]) + bias[n], with acc the sum over k of
+ * the products of the operands' values (codes times block scales), in float32: the
+ * values' products are exact, the sum is rounded as it goes, in an order that
+ * depends on the sizes alone.  Scaling and bias are float32 operations, the result
+ * is rounded once more to a 16-bit type.  (A product of two block scales outside
+ * float32's range gives infinities, NaN or 0.)
+ * a: [M, K], b: [N, K], both of `format`, K whole blocks, rows lda and ldb BYTES
+ * apart (multiples of 16).  a_scale [M], b_scale [N] and bias [N] are float32; a
+ * NULL scale is 1, a NULL bias 0.  out: row m at out + m * ldo elements, ldo >= N;
+ * out_dtype PEAT_F32, PEAT_F16 or PEAT_BF16.  K = 0 gives 0 (plus the bias).  out
+ * must not overlap the inputs. */
+peat_status_t peat_matmul_f4(peat_handle_t h, peat_f4_t format, const uint8_t* a, int64_t lda,
+                             const uint8_t* a_block_scale, const float* a_scale, const uint8_t* b, int64_t ldb,
+                             const uint8_t* b_block_scale, const float* b_scale, const float* bias, int64_t M,
+                             int64_t N, int64_t K, void* out, int64_t ldo, peat_dtype_t out_dtype,
+                             peat_stream_t stream);
+
+/* An operand of peat_product_f4: a matrix [rows, cols].  dtype PEAT_F4: codes with
+ * their scales (scale: NULL is 1), axis 0, cols whole blocks, rows ld bytes apart.
+ * dtype PEAT_F32, PEAT_F16 or PEAT_BF16: rounded as peat_quantize_f4 does, along its
+ * rows (axis 0) or columns (axis 1, whose transpose is then the operand), rows ld
+ * elements apart; the scales are not read. */
+#define PEAT_F4 102
+typedef struct {
+  const void* data;
+  const uint8_t* block_scale;
+  const float* scale;
+  int64_t rows, cols, ld;
+  int32_t dtype;
+  int32_t axis;
+} peat_operand_f4_t;
+
+/* peat_matmul_f4 of two operands that are rounded on the way where they are not
+ * 4-bit values yet: a's M x K is rows x cols (axis 0) or cols x rows (axis 1), b's N
+ * x K likewise, the two K equal once they are filled up to whole blocks. */
+peat_status_t peat_product_f4(peat_handle_t h, peat_f4_t format, const peat_operand_f4_t* a,
+                              const peat_operand_f4_t* b, const float* bias, void* out, int64_t ldo,
+                              peat_dtype_t out_dtype, peat_stream_t stream);
+
+/* ---- root-mean-square norm ----
+ *
+ * The norm that precedes a sublayer's products, of the residual stream with what
+ * the sublayer before adds to it, and its output in 8 bits as peat_matmul_i8 takes
+ * it.  Over each row of x [rows, cols] (of type dtype), in float32 unless said
+ * otherwise,
+ *   s     = x + residual, rounded to dtype (no residual: x)
+ *   v     = (sum of s^2) / cols, summed in twice the precision, rounded once
+ *   rstd  = 1 / sqrt(v + eps)
+ *   y     = (s * rstd) * weight
+ *   scale = amax / 127 and q = the nearest integer of y * (127 / amax), amax = max
+ *           |y|, with all of peat_quantize_i8's rules (float32 y, not the rounded).
+ * weight [cols] is of type dtype or PEAT_F32.  A NaN or an infinity in a row goes
+ * where the formulas take it; no square overflows or underflows.
+ * Outputs, each optional (NULL), one at least: sum (s), y and values (q * scale)
+ * [rows, cols] of type dtype, q int8 [rows, cols], scale and rstd float32 [rows].
+ * sum may be x or residual itself (the same rows at the same distance); else no
+ * output overlaps an input or another output. */
+peat_status_t peat_rmsnorm(peat_handle_t h, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                           const void* weight, peat_dtype_t weight_dtype, int64_t rows, int64_t cols,
+                           peat_dtype_t dtype, float eps, void* sum, int64_t lds, void* y, int64_t ldy, int8_t* q,
+                           int64_t ldq, float* scale, void* values, int64_t ldv, float* rstd, peat_stream_t stream);
+
+/* The norm's gradients, of grad = dL/dy and, where the stream goes on beside the
+ * sublayer, grad_sum = dL/ds (NULL: none), from x = s (peat_rmsnorm's sum) and its
+ * rstd.  With n = x * rstd, g = grad * weight, c = (sum of g * n) / cols,
+ *   grad_x      = rstd * (g - n * c) + grad_sum, rounded to dtype: the gradient of
+ *                 x and of the residual alike
+ *   grad_weight = the sum over the rows of grad * n, float32 [cols].
+ * (Rounding to 8 bits passes gradients through: grad is then that of values.)  Sums
+ * are float32, in an order that depends on the sizes alone.  Each output may be
+ * NULL, not both; no rows give grad_weight 0.  grad_x may be grad or grad_sum itself
+ * (the same rows at the same distance), else no output overlaps an input. */
+peat_status_t peat_rmsnorm_backward(peat_handle_t h, const void* grad, int64_t ldg, const void* grad_sum,
+                                    int64_t ldr, const void* x, int64_t ldx, const void* weight,
+                                    peat_dtype_t weight_dtype, const float* rstd, int64_t rows, int64_t cols,
+                                    peat_dtype_t dtype, void* grad_x, int64_t ldo, float* grad_weight,
+                                    peat_stream_t stream);
+
 /* One tensor of a gradient list (a HOST array, copied before the call
  * returns): n contiguous elements of type dtype (PEAT_F32, PEAT_F16,
  * PEAT_BF16) at g.  out is peat_grad_clip's output: g itself (in place) or

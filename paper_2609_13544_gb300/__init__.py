@@ -22,6 +22,9 @@ from .buildlib import LIB, build  # noqa: F401
 from .ops import (GRADNORM_BYTES, OPS_EXPORTS, GradList, Linear8, peat_grad_clip, peat_grad_clip_raw,  # noqa: F401
                   peat_grad_norm, peat_grad_norm_raw, peat_matmul_i8, peat_matmul_i8_raw, peat_product_i8,
                   peat_product_i8_raw, peat_quantize_i8, peat_quantize_i8_raw)
+from .ops4 import (F4_BLOCK, F4_FORMATS, Float4, Linear4, RMSNorm8, f4_scale_bytes, peat_matmul_f4,  # noqa: F401
+                   peat_matmul_f4_raw, peat_product_f4, peat_product_f4_raw, peat_quantize_f4, peat_quantize_f4_raw,
+                   peat_rmsnorm, peat_rmsnorm_backward, peat_rmsnorm_backward_raw, peat_rmsnorm_raw)
 
 DTYPE_CODES = {"f32": 0, "f16": 1, "bf16": 2}
 CLASSES = ("exact", "within_tol", "mismatch", "nan_inf_asym", "sign_flip")

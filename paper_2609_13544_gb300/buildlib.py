@@ -21,10 +21,11 @@ OUT_DIR = PKG / "_build"
 LIB = OUT_DIR / "libpeat.so"
 LIB_CHECKED = OUT_DIR / "libpeat_checked.so"
 SOURCES = ["compare.cu", "compare8.cu", "compare64.cu", "topk.cu", "tstats.cu", "isclose.cu", "isclose64.cu", "inject.cu", "quant8.cu",
-           "matmul8.cu", "mm8_tc.cu", "gradnorm.cu", "peat_api.cpp", "ops_api.cpp"]
+           "matmul8.cu", "mm8_tc.cu", "gradnorm.cu", "quant4.cu", "mm4_tc.cu", "rmsnorm.cu", "peat_api.cpp", "ops_api.cpp",
+           "ops4_api.cpp"]
 HEADERS = [CSRC / "peat_internal.h", CSRC / "exact.cuh", CSRC / "meanvar.cuh", CSRC / "inject_models.cuh", CSRC / "tol_exact.cuh", CSRC / "exact64.cuh",
            CSRC / "peat_handle.h", CSRC / "ops_internal.h", CSRC / "ops_state.h", CSRC / "mm8_common.cuh",
-           CSRC / "tc_common.cuh", CSRC / "matrix_vec.cuh", CSRC / "vec16.cuh", ROOT / "include" / "peat.h",
+           CSRC / "tc_common.cuh", CSRC / "matrix_vec.cuh", CSRC / "f4.cuh", CSRC / "vec16.cuh", ROOT / "include" / "peat.h",
            ROOT / "include" / "peat_ops.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",

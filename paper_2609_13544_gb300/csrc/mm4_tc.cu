@@ -1,0 +1,365 @@
+// Products of 4-bit matrices on the fifth-generation tensor cores, which scale
+// each block of values by the bytes that go with it and add up in float32.
+//
+// A CTA makes tiles of 128 rows of one operand by `bn` rows of the other,
+// persistent over them.  A stage is 256 k: a 128-byte piece of every row, swizzled
+// by the copy, and the scales' tiles, which lie in memory as the instruction wants
+// them in tensor memory.  Warp roles: one thread issues the copies, one the moves
+// of scales and the matrix instructions, eight warps turn accumulators into
+// results while the other one fills.
+//
+// Few rows of a: the tile's 128 rows are b's (SWAP), so that the instruction
+// spends nothing on rows that a does not have.
+#include <algorithm>
+
+#include "f4.cuh"
+#include "peat_internal.h"
+#include "tc_common.cuh"
+
+namespace peat {
+namespace {
+
+constexpr int SK = 256;                 // k of a stage
+constexpr int P_BYTES = 128 * SK / 2;   // its rows on the 128-row side
+constexpr int PS_BYTES = 2048, QS_BYTES = 4096;  // its scales: tiles of 64 k or more, of up to two blocks of 128 rows
+constexpr int EPI_WARPS = 8, COPY_WARP = EPI_WARPS, MMA_WARP = COPY_WARP + 1, THREADS = (MMA_WARP + 1) * 32;
+constexpr int MOST_BN = 192, MOST_STAGES = 8;
+constexpr int EDGE = MOST_BN / 2;       // columns of a warp
+constexpr int EPI_BYTES = EPI_WARPS * EDGE * 2 * 4, BARS = 256;
+constexpr int SMEM = 227 * 1024;
+// tensor memory: two accumulators, then two sets of scales
+constexpr int AT_SCALES = 2 * MOST_BN, SCALES = 48, AT_QS = 16;
+static_assert(AT_SCALES + 2 * SCALES <= 512, "tensor memory has 512 columns");
+
+constexpr int stage_bytes(int bn) { return P_BYTES + bn * (SK / 2) + PS_BYTES + QS_BYTES; }
+
+struct Tc4Params {
+  const uint8_t* ps;  // scales of the 128-row side and of the other
+  const uint8_t* qs;
+  const float* sp;    // of their rows, or null
+  const float* sq;
+  const float* bias;
+  OutPlace out;
+  int64_t P, Q;       // rows
+  int64_t tiles;      // of scales along k
+  int steps;          // instructions of 64 k
+  int bn, pt, qt, stages;
+  unsigned int* status;
+  uint32_t wait_limit;
+};
+
+__device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, int x, int row, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(row), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// a tile of scales into four columns of tensor memory: 32 lanes of 16 bytes, the same for each quarter of the lanes
+__device__ __forceinline__ void scales_in(uint32_t col, uint32_t addr) {
+  const uint64_t d = (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(col), "l"(d) : "memory");
+}
+// 128 rows by bn, 64 k: 4-bit values, a scale for 32 (mxfp4: two of the four bytes of a tile, from `which` on) or for 16
+template <int FMT>
+__device__ __forceinline__ void mma4(uint32_t d, uint64_t a, uint64_t b, uint32_t bn, uint32_t which, uint32_t sa, uint32_t sb,
+                                     bool accumulate) {
+  const uint32_t idesc = (1u << 7) | (1u << 10) | ((bn / 8) << 17) | ((FMT == PEAT_MXFP4 ? 1u : 0u) << 23) |
+                         ((128u / 16) << 24) | (which << 4) | (which << 29);
+  if (FMT == PEAT_MXFP4)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+      : "r"(addr));
+}
+
+constexpr int GROUP = 8;
+struct Place4 {
+  int64_t p0, q0;
+};
+__device__ __forceinline__ Place4 place_of(const Tc4Params& p, int u) {
+  // groups of GROUP tiles of P, column by column: the CTAs at work at any time share few rows of either
+  const int64_t per = (int64_t)GROUP * p.qt;
+  const int g = (int)(u / per), in = (int)(u - g * per), wide = min(GROUP, p.pt - g * GROUP);
+  const int q = in / wide;
+  return Place4{(int64_t)(g * GROUP + in - q * wide) * 128, (int64_t)q * p.bn};
+}
+
+template <int OUT>
+__device__ __forceinline__ void put_one(void* out, int64_t at, float y) {
+  typename Mm8Out<OUT>::T* o = static_cast<typename Mm8Out<OUT>::T*>(out) + at;
+  if constexpr (OUT == PEAT_F32) *o = y;
+  else if constexpr (OUT == PEAT_F16) *o = __float2half_rn(y);
+  else *o = __float2bfloat16_rn(y);
+}
+
+template <int OUT, int FMT, bool SWAP>
+__global__ void __launch_bounds__(THREADS, 1)
+    mm4_tc(Tc4Params p, const __grid_constant__ CUtensorMap mp, const __grid_constant__ CUtensorMap mq) {
+  extern __shared__ char raw[];
+  char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  const int bn = p.bn, stage = stage_bytes(bn);
+  char* edges = smem + p.stages * stage;
+  const uint32_t full = sptr(edges + EPI_BYTES), empty = full + 8 * MOST_STAGES, acc_full = empty + 8 * MOST_STAGES,
+                 acc_empty = acc_full + 16, last = acc_empty + 16;
+  volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(edges + EPI_BYTES + 8 * (2 * MOST_STAGES + 5));
+  static_assert(8 * (2 * MOST_STAGES + 5) + 4 <= BARS, "the barriers fit");
+  constexpr int TILE_K = F4<FMT>::BLOCK * 4, PER = SK / TILE_K;  // k of a tile of scales; tiles of a stage
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int units = p.pt * p.qt, nk = (p.steps + 3) / 4;
+
+  if (threadIdx.x == 32) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mp) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mq) : "memory");
+  }
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < MOST_STAGES; i++) {
+      mbar_init(full + 8 * i, 1);
+      mbar_init(empty + 8 * i, 1);
+    }
+    for (int i = 0; i < 2; i++) {
+      mbar_init(acc_full + 8 * i, 1);
+      mbar_init(acc_empty + 8 * i, EPI_WARPS);
+    }
+    mbar_init(last, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == MMA_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sptr((const void*)tmem_at))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = *tmem_at;
+  pdl_trigger();
+
+  bool ok = true;
+  if (warp == COPY_WARP) {
+    if (elect_one()) {
+      pdl_wait();
+      int seq = 0;
+      for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
+        const Place4 t = place_of(p, u);
+        const int64_t pb = t.p0 >> 7, qb = t.q0 >> 7, q_end = min(t.q0 + bn, p.Q);
+        const int qbs = (int)(((q_end - 1) >> 7) - qb) + 1;  // blocks of 128 rows that the tile's lie in
+        for (int k = 0; k < nk; k++, seq++) {
+          const int s = seq % p.stages;
+          if (!(ok = mbar_wait(empty + 8 * s, (seq / p.stages & 1) ^ 1, p.wait_limit))) break;
+          const uint32_t dst = sptr(smem + s * stage), bar = full + 8 * s, qd = dst + P_BYTES, sd = qd + bn * (SK / 2);
+          const uint32_t n = (uint32_t)min((int64_t)PER, p.tiles - (int64_t)k * PER) * SCALE_TILE;
+          mbar_expect(bar, P_BYTES + bn * (SK / 2) + n * (1 + qbs));
+          tma_rows(dst, &mp, k * (SK / 2), (int)t.p0, bar);
+          tma_rows(qd, &mq, k * (SK / 2), (int)t.q0, bar);
+          bulk(sd, p.ps + (pb * p.tiles + (int64_t)k * PER) * SCALE_TILE, n, bar);
+          for (int i = 0; i < qbs; i++)
+            bulk(sd + PS_BYTES + i * (PER * SCALE_TILE), p.qs + ((qb + i) * p.tiles + (int64_t)k * PER) * SCALE_TILE, n, bar);
+        }
+      }
+      // a stage's copies have landed when its instructions are done with it
+      for (int j = 0; j < p.stages && j < seq; j++) {
+        const int q = seq - 1 - j;
+        mbar_wait(empty + 8 * (q % p.stages), q / p.stages & 1, END_LIMIT);
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    if (elect_one()) {
+      int seq = 0, i = 0;
+      for (int u = blockIdx.x; u < units && ok && nk; u += gridDim.x, i++) {
+        const Place4 t = place_of(p, u);
+        const int qbs = (int)(((min(t.q0 + bn, p.Q) - 1) >> 7) - (t.q0 >> 7)) + 1;
+        const uint32_t shift = (uint32_t)(t.q0 & 127) / 32;
+        if (!(ok = mbar_wait(acc_empty + 8 * (i & 1), (i / 2 & 1) ^ 1, p.wait_limit))) break;
+        const uint32_t d = tmem + (i & 1) * bn;
+        for (int k = 0; k < nk; k++, seq++) {
+          const int s = seq % p.stages;
+          if (!(ok = mbar_wait(full + 8 * s, seq / p.stages & 1, p.wait_limit))) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t base = sptr(smem + s * stage), qd = base + P_BYTES, sd = qd + bn * (SK / 2);
+          const uint32_t tp = tmem + AT_SCALES + (seq & 1) * SCALES, tq = tp + AT_QS;
+          const int here = min(4, p.steps - 4 * k);
+#pragma unroll
+          for (int j = 0; j < PER; j++) {
+            if (j * (4 / PER) >= here) break;
+            scales_in(tp + 4 * j, sd + j * SCALE_TILE);
+            for (int q = 0; q < qbs; q++) scales_in(tq + 8 * j + 4 * q, sd + PS_BYTES + (q * PER + j) * SCALE_TILE);
+          }
+          const uint64_t a = block_desc(base), b = block_desc(qd);
+#pragma unroll
+          for (int j = 0; j < 4; j++) {
+            if (j >= here) break;
+            const int tile = j * PER / 4;
+            mma4<FMT>(d, a + 2 * j, b + 2 * j, bn, FMT == PEAT_MXFP4 ? 2 * (j & 1) : 0, tp + 4 * tile, tq + 8 * tile + shift,
+                      k + j > 0);
+          }
+          commit(empty + 8 * s);
+          if (k == nk - 1) commit(acc_full + 8 * (i & 1));
+        }
+      }
+      // whatever was issued is done before the accumulators are given back
+      commit(last);
+      mbar_wait(last, 0, END_LIMIT);
+    }
+  } else {  // results: a warp has 32 of the 128 rows and half of the columns
+    pdl_wait();
+    int i = 0;
+    const int half = warp >> 2, quarter = warp & 3;
+    constexpr int STEP = SWAP ? 16 : 32;
+    const int chunks = bn / STEP, c0 = half ? (chunks + 1) / 2 : 0, c1 = half ? chunks : (chunks + 1) / 2;
+    float* sq = reinterpret_cast<float*>(edges) + warp * (EDGE * 2);
+    float* bias = sq + EDGE;
+    for (int u = blockIdx.x; u < units && ok; u += gridDim.x, i++) {
+      const Place4 t = place_of(p, u);
+      const int64_t row0 = t.p0 + quarter * 32, row = row0 + lane, col0 = t.q0 + c0 * STEP;
+      __syncwarp();
+      for (int c = lane; c < (c1 - c0) * STEP; c += 32) {
+        const int64_t col = col0 + c;
+        sq[c] = p.sq && col < p.Q ? __ldcg(p.sq + col) : 1.0f;
+        if (!SWAP) bias[c] = p.bias && col < p.Q ? __ldcg(p.bias + col) : 0.0f;
+      }
+      const float sp = p.sp && row < p.P ? __ldcg(p.sp + row) : 1.0f;
+      const float row_bias = SWAP && p.bias && row < p.P ? __ldcg(p.bias + row) : 0.0f;
+      __syncwarp();
+      if (nk) {
+        if (!(ok = warp_wait(acc_full + 8 * (i & 1), i / 2 & 1, p.wait_limit))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      }
+      const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1) * bn + c0 * STEP;
+      const int rows = (int)max((int64_t)0, min((int64_t)32, p.P - row0));
+      uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      for (int c = c0; c < c1; c++) {
+        uint32_t v[STEP];
+#pragma unroll
+        for (int j = 0; j < STEP; j++) v[j] = 0;
+        if (nk) {
+          if constexpr (SWAP) tmem_load16(taddr + (c - c0) * STEP, v);
+          else tmem_load32(taddr + (c - c0) * STEP, v);
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        }
+        if (c == c1 - 1) {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(acc_empty + 8 * (i & 1));
+        }
+        const int at = (c - c0) * STEP;
+        if constexpr (SWAP) {
+#pragma unroll
+          for (int j = 0; j < STEP; j++) {
+            const int64_t m = col0 + at + j;
+            float y = __uint_as_float(v[j]);
+            if (p.sp) y = __fmul_rn(y, __fmul_rn(sq[at + j], sp));
+            if (p.bias) y = __fadd_rn(y, row_bias);
+            if (m < p.Q && row < p.P) put_one<OUT>(p.out.out, m * p.out.ldo + row, y);
+          }
+        } else {
+          float f[32];
+#pragma unroll
+          for (int j = 0; j < 32; j++) f[j] = __uint_as_float(v[j]);
+          put_columns<OUT>(p.out, f, sp, sq + at, bias + at, row0, rows, col0 + at, c == c0, c == c1 - 1, carry);
+        }
+      }
+      if (c0 == c1) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(acc_empty + 8 * (i & 1));
+      }
+    }
+  }
+  __syncwarp();
+  if (!ok) atomicOr_system(p.status, 1u);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// rows of codes; a box is 128 bytes of `box` rows, swizzled
+bool rows_map(CUtensorMap* m, const uint8_t* base, int64_t rows, int64_t bytes, int64_t ld, int box) {
+  EncodeFn f = encode_fn();
+  if (!f) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? ld : (bytes + 15) / 16 * 16)};
+  const cuuint32_t size[2] = {128, (cuuint32_t)box}, elem[2] = {1, 1};
+  return f(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(base), dims, strides, size, elem,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int OUT, int FMT, bool SWAP>
+cudaError_t launch(const Tc4Params& p, const CUtensorMap& mp, const CUtensorMap& mq, int nsm, cudaStream_t s) {
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = allow_smem(mm4_tc<OUT, FMT, SWAP>, SMEM, allowed);
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = (int64_t)p.pt * p.qt;
+  // (one CTA an SM, which has all of tensor memory)
+  return launch_dependent(mm4_tc<OUT, FMT, SWAP>, (unsigned)std::min<int64_t>(tiles, nsm), THREADS, SMEM, s, p, mp, mq);
+}
+template <int OUT, int FMT>
+cudaError_t launch_side(bool swap, const Tc4Params& p, const CUtensorMap& mp, const CUtensorMap& mq, int nsm, cudaStream_t s) {
+  return swap ? launch<OUT, FMT, true>(p, mp, mq, nsm, s) : launch<OUT, FMT, false>(p, mp, mq, nsm, s);
+}
+template <int OUT>
+cudaError_t launch_out(int format, bool swap, const Tc4Params& p, const CUtensorMap& mp, const CUtensorMap& mq, int nsm,
+                       cudaStream_t s) {
+  return format == PEAT_MXFP4 ? launch_side<OUT, PEAT_MXFP4>(swap, p, mp, mq, nsm, s)
+                              : launch_side<OUT, PEAT_NVFP4>(swap, p, mp, mq, nsm, s);
+}
+
+}  // namespace
+
+cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned int* status, unsigned int wait_limit, int nsm,
+                       cudaStream_t s) {
+  const int block = format == PEAT_MXFP4 ? 32 : 16;
+  const bool swap = m.M <= MOST_BN;
+  Tc4Params p;
+  p.ps = swap ? m.b_block_scale : m.a_block_scale;
+  p.qs = swap ? m.a_block_scale : m.b_block_scale;
+  p.sp = swap ? m.sb : m.sa;
+  p.sq = swap ? m.sa : m.sb;
+  p.bias = m.bias;
+  p.P = swap ? m.N : m.M;
+  p.Q = swap ? m.M : m.N;
+  p.tiles = (m.K / block + 3) / 4;
+  p.steps = (int)((m.K + 63) / 64);
+  p.bn = swap ? (int)((m.M + 15) / 16 * 16) : 128;
+  p.pt = (int)((p.P + 127) / 128);
+  p.qt = (int)((p.Q + p.bn - 1) / p.bn);
+  p.stages = std::min(MOST_STAGES, (SMEM - 1024 - EPI_BYTES - BARS) / stage_bytes(p.bn));
+  const int size = out_dtype == PEAT_F32 ? 4 : 2;
+  p.out = OutPlace{m.out, m.ldo, m.N, m.bias != nullptr,
+                   reinterpret_cast<uintptr_t>(m.out) % 32 == 0 && m.ldo * size % 32 == 0};
+  p.status = status;
+  p.wait_limit = wait_limit;
+  CUtensorMap mp = {}, mq = {};
+  if (m.K > 0 && (!rows_map(&mp, swap ? m.b : m.a, p.P, m.K / 2, swap ? m.ldb : m.lda, 128) ||
+                  !rows_map(&mq, swap ? m.a : m.b, p.Q, m.K / 2, swap ? m.lda : m.ldb, p.bn)))
+    return cudaErrorNotSupported;
+  switch (out_dtype) {
+    case PEAT_F32: return launch_out<PEAT_F32>(format, swap, p, mp, mq, nsm, s);
+    case PEAT_F16: return launch_out<PEAT_F16>(format, swap, p, mp, mq, nsm, s);
+    default: return launch_out<PEAT_BF16>(format, swap, p, mp, mq, nsm, s);
+  }
+}
+
+}  // namespace peat

@@ -187,12 +187,6 @@ __device__ __forceinline__ int add_sum(int a, int b, bool exact) {
   return exact ? __float_as_int(__fadd_rn(__int_as_float(a), __int_as_float(b))) : a + b;
 }
 
-// Polls for what a CTA has under way before it ends, whether or not an earlier
-// wait of its expired.  A poll that finds nothing takes 4 us: a quarter of a
-// second for each of at most STAGES + 1 of them, for copies and instructions that
-// take microseconds.  (Where all went well nothing hangs on these: the cluster
-// meets only when the instructions are done.)
-constexpr uint32_t END_LIMIT = 1u << 16;
 constexpr int GROUP = 8;
 // a tile, and its part of the k range in blocks of 64
 struct Place {

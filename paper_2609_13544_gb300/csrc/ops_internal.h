@@ -143,4 +143,96 @@ inline int64_t gn_units(const void* g, int64_t n, int size) {
   return (int64_t)((a + (uint64_t)n * size + 15) / 16 - a / 16);
 }
 
+
+// ---- 4-bit rounding (quant4.cu) ----
+struct Quant4Params {
+  const void* x;
+  int64_t rows, cols, ldx;
+  uint8_t* q;  // or null; rows of ldq bytes on 16-byte boundaries
+  int64_t ldq;
+  int64_t width;         // elements of whole blocks along the product's axis
+  uint8_t* block_scale;  // or null
+  int64_t tiles;         // of four blocks along the product's axis
+  float* scale;          // or null
+  void* values;          // or null
+  int64_t ldv;
+  int vec_x, vec_v;  // rows start on 16-byte boundaries
+  int pairs;         // x's rows start on boundaries of two elements
+  // nvfp4 by column: the columns' largest patterns, and words to clear for a later call
+  const unsigned int* colmax;
+  unsigned int* zero;
+  int64_t zero_n;
+};
+cudaError_t launch_quant4(int dtype, int format, int axis, const Quant4Params& p, int nsm, cudaStream_t s);
+
+// ---- 4-bit products (mm4_tc.cu) ----
+struct Mm4Params {
+  const uint8_t* a;  // [M, K / 2 bytes]
+  const uint8_t* b;  // [N, K / 2 bytes]
+  int64_t lda, ldb;  // bytes
+  const uint8_t* a_block_scale;
+  const uint8_t* b_block_scale;
+  const float* sa;    // or null, both or none
+  const float* sb;
+  const float* bias;  // or null
+  void* out;
+  int64_t ldo;
+  int64_t M, N, K;
+};
+cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& p, unsigned int* status, unsigned int wait_limit, int nsm,
+                       cudaStream_t s);
+
+// ---- root-mean-square norm (rmsnorm.cu) ----
+struct RmsParams {
+  const void* x;
+  int64_t ldx;
+  const void* residual;  // or null
+  int64_t ldr;
+  const void* weight;
+  int weight_f32;  // of float32, else of x's type
+  int64_t rows, cols;
+  float eps;
+  void* sum;  // or null
+  int64_t lds;
+  void* y;  // or null
+  int64_t ldy;
+  int8_t* q;  // or null
+  int64_t ldq;
+  float* scale;  // or null
+  void* values;  // or null
+  int64_t ldv;
+  float* rstd;  // or null
+  int grid;     // x's and residual's rows start on 16-byte boundaries
+  int vec_w, vec_s, vec_y, vec_q, vec_v;  // the others'
+};
+cudaError_t launch_rmsnorm(int dtype, const RmsParams& p, cudaStream_t s);
+struct RmsBackParams {
+  const void* grad;
+  int64_t ldg;
+  const void* stream;  // the sum's own gradient, or null
+  int64_t ldr;
+  const void* x;
+  int64_t ldx;
+  const void* weight;
+  int weight_f32;
+  const float* rstd;
+  int64_t rows, cols;
+  void* grad_x;  // or null
+  int64_t ldo;
+  float* grad_weight;  // or null
+  float* parts;        // sums of the CTAs' rows [ctas, cols]
+  float* dots;         // of long rows
+  int ctas;
+  int64_t each;  // rows of a CTA's group
+  int grid, vec_w, vec_o;
+};
+// what a backward call needs: CTAs, and whether its rows are long ones
+struct RmsBackPlan {
+  int ctas;
+  int64_t each;
+  bool longer;
+};
+RmsBackPlan rms_back_plan(int dtype, int64_t rows, int64_t cols, int nsm);
+cudaError_t launch_rmsnorm_backward(int dtype, const RmsBackPlan& plan, const RmsBackParams& p, cudaStream_t s);
+
 }  // namespace peat

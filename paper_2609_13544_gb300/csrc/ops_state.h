@@ -50,6 +50,9 @@ struct OpsState {
   // products: packed operands and partial sums
   void* mm = nullptr;
   size_t mm_cap = 0;
+  // norm gradients: the CTAs' sums over their rows, long rows' means
+  void* norm = nullptr;
+  size_t norm_cap = 0;
 };
 
 constexpr int64_t MAX_DIM = ((int64_t)1 << 31) - 1;

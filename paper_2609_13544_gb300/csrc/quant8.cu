@@ -16,34 +16,6 @@
 namespace peat {
 namespace {
 
-// r and scale of a row from its largest pattern
-template <int DT>
-__device__ __forceinline__ void factors(uint32_t m, float& r, float& scale) {
-  if (m >= Elem<DT>::INF) {
-    r = 0.0f;
-    scale = __uint_as_float(0x7fc00000u);
-    return;
-  }
-  const float amax = Elem<DT>::mag(m);
-  r = __fdiv_rn(127.0f, amax);
-  scale = __fdiv_rn(amax, 127.0f);
-  if (!(r <= 3.402823466e38f)) r = scale = 0.0f;  // amax 0, or too small for a finite r
-}
-// The integer of x: the float32 product x r, added to 1.5 2^23, has it in its
-// low bits, rounded to nearest even (conversion instructions run at an eighth of
-// the additions' rate).  A row that is not finite has r = 0, and 0 x NaN must
-// not get through.
-constexpr float MAGIC = 12582912.0f;
-__device__ __forceinline__ float whole(float x, float r, bool finite) {
-  return finite ? __fadd_rn(__fmul_rn(x, r), MAGIC) : MAGIC;
-}
-__device__ __forceinline__ float number(float w) { return __fsub_rn(w, MAGIC); }
-__device__ __forceinline__ int8_t byte_of(float w) { return (int8_t)__float_as_uint(w); }
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
-  return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
-                     __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
-}
-
 // a vector's integers (in float32, see whole) from its row's factor
 template <int DT, bool FINITE>
 __device__ __forceinline__ void wholes(uint4 v, float r, float (&w)[Elem<DT>::E]) {

@@ -1,0 +1,541 @@
+// The root-mean-square norm of a residual stream, with the stream's addition
+// before it and the rounding to 8-bit integers behind it, and its gradients.
+//
+//   s = x + residual in the tensors' type, v = sum s^2 / n, rstd = 1 / sqrt(v + eps),
+//   y = (s rstd) weight; 8 bits: amax = max |y|, q = rint(y (127 / amax))
+//
+// The sum of squares is carried with its rounding errors (two float32 numbers,
+// good to 2^-40 or so), so that v is the 64-bit sum's float32 value: the integers
+// near a rounding border then do not depend on the order of the sum.  Rows whose
+// squares leave float32's range are summed in binary64.
+//
+// Bound by memory: a row is read once and kept in registers between the two
+// reductions; the gradients of the weights are summed in registers over a CTA's
+// rows, then over the CTAs in a fixed order.
+#include <algorithm>
+
+#include "matrix_vec.cuh"
+#include "ops_internal.h"
+#include "peat_internal.h"
+
+namespace peat {
+namespace {
+
+template <int TPR>
+constexpr int threads_of() { return TPR > 256 ? TPR : 256; }
+
+// (hi, lo) + x, the rounding error of the sum kept in lo
+__device__ __forceinline__ void add_kept(float& hi, float& lo, float x) {
+  const float t = __fadd_rn(hi, x), z = __fsub_rn(t, hi);
+  lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(t, z)), __fsub_rn(x, z)));
+  hi = t;
+}
+// Sums over the TPR threads of a row, the same bits in all of them.  `part`: a
+// place for each warp, read only after a barrier that all of the CTA meets.
+template <int TPR>
+__device__ __forceinline__ void sum_kept(float& hi, float& lo, float2* part) {
+#pragma unroll
+  for (int o = 16; o; o /= 2) {
+    const float h = __shfl_xor_sync(0xffffffffu, hi, o), l = __shfl_xor_sync(0xffffffffu, lo, o);
+    lo = __fadd_rn(lo, l);
+    add_kept(hi, lo, h);
+  }
+  if (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = make_float2(hi, lo);
+    __syncthreads();
+    const float2* p = part + threadIdx.x / TPR * (TPR / 32);
+    hi = p[0].x, lo = p[0].y;
+#pragma unroll
+    for (int w = 1; w < TPR / 32; w++) {
+      lo = __fadd_rn(lo, p[w].y);
+      add_kept(hi, lo, p[w].x);
+    }
+  }
+}
+template <int TPR>
+__device__ __forceinline__ double sum_wide(double x, double* part) {
+#pragma unroll
+  for (int o = 16; o; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+    __syncthreads();
+    const double* p = part + threadIdx.x / TPR * (TPR / 32);
+    x = p[0];
+#pragma unroll
+    for (int w = 1; w < TPR / 32; w++) x += p[w];
+  }
+  return x;
+}
+template <int TPR>
+__device__ __forceinline__ float sum_plain(float x, float* part) {
+#pragma unroll
+  for (int o = 16; o; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+    __syncthreads();
+    const float* p = part + threadIdx.x / TPR * (TPR / 32);
+    x = p[0];
+#pragma unroll
+    for (int w = 1; w < TPR / 32; w++) x += p[w];
+  }
+  return x;
+}
+template <int TPR>
+__device__ __forceinline__ uint32_t most_of(uint32_t top, uint32_t* part) {
+  top = __reduce_max_sync(0xffffffffu, top);
+  if (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
+    __syncthreads();
+    const uint32_t* p = part + threadIdx.x / TPR * (TPR / 32);
+#pragma unroll
+    for (int w = 0; w < TPR / 32; w++) top = max(top, p[w]);
+  }
+  return top;
+}
+
+template <int DT, bool GRID>
+__device__ __forceinline__ uint4 load_vec(const Source<DT, GRID>& s, const typename Elem<DT>::T* p, int64_t left) {
+  if (s.whole(p, left)) return s.load(p);
+  return left > 0 ? load_edge<DT>(p, left) : make_uint4(0, 0, 0, 0);
+}
+// a vector of a matrix that this kernel has written (the thread's own elements)
+template <int DT>
+__device__ __forceinline__ uint4 load_own(const typename Elem<DT>::T* p, int64_t left, bool on_grid) {
+  Vec<DT> v;
+  v.u = make_uint4(0, 0, 0, 0);
+  if (on_grid && left >= Elem<DT>::E) {
+    v.u = *reinterpret_cast<const uint4*>(p);
+  } else {
+#pragma unroll
+    for (int e = 0; e < Elem<DT>::E; e++)
+      if (e < left) v.e[e] = p[e];
+  }
+  return v.u;
+}
+// E weights from column col on
+template <int DT>
+__device__ __forceinline__ void weights(const void* w, int f32, bool vec, int64_t col, int64_t cols, float (&x)[Elem<DT>::E]) {
+  constexpr int E = Elem<DT>::E;
+  if (DT != PEAT_F32 && !f32) {
+    const typename Elem<DT>::T* p = static_cast<const typename Elem<DT>::T*>(w) + col;
+    const int64_t left = cols - col;
+    unpack<DT>(vec && left >= E ? __ldg(reinterpret_cast<const uint4*>(p)) : left > 0 ? load_edge<DT>(p, left) : make_uint4(0, 0, 0, 0), x);
+    return;
+  }
+  const float* p = static_cast<const float*>(w) + col;
+  if (vec && col + E <= cols) {
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      const float4 f = __ldg(reinterpret_cast<const float4*>(p + e));
+      x[e] = f.x, x[e + 1] = f.y, x[e + 2] = f.z, x[e + 3] = f.w;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e++) x[e] = col + e < cols ? __ldg(p + e) : 0.0f;
+  }
+}
+
+// ---- forward ------------------------------------------------------------------
+// TPR threads have a row, NV vectors each; LONG: rows that these do not hold, read
+// again for each of the three passes.
+template <int DT, int TPR, int NV, bool GRID, bool LONG>
+__global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
+  using L = Elem<DT>;
+  using T = typename L::T;
+  constexpr int E = L::E, QT = threads_of<TPR>();
+  constexpr int64_t PIECE = (int64_t)TPR * NV * E;
+  __shared__ float2 sums[QT / 32];
+  __shared__ double wide[QT / 32];
+  __shared__ uint32_t tops[QT / 32];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t row = (int64_t)blockIdx.x * (QT / TPR) + threadIdx.x / TPR;
+  const int lane = threadIdx.x % TPR;
+  const bool live = row < p.rows;
+  const int64_t cols = live ? p.cols : 0, end = LONG ? p.cols : 1;
+  const Source<DT, GRID> sx(p.x, p.rows, p.cols, p.ldx), sr(p.residual, p.rows, p.cols, p.ldr);
+  const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+  const T* res = p.residual ? static_cast<const T*>(p.residual) + row * p.ldr : nullptr;
+  T* sum = p.sum ? static_cast<T*>(p.sum) + row * p.lds : nullptr;
+  uint4 s[NV];
+  auto column = [&](int64_t at, int i) { return at + (int64_t)(i * TPR + lane) * E; };
+  auto load = [&](int64_t at) {  // s = x + residual, rounded to the type
+    uint4 u[NV];
+#pragma unroll
+    for (int i = 0; i < NV; i++) s[i] = load_vec(sx, x + column(at, i), cols - column(at, i));
+    if (!res) return;
+#pragma unroll
+    for (int i = 0; i < NV; i++) u[i] = load_vec(sr, res + column(at, i), cols - column(at, i));
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      float a[E], b[E];
+      unpack<DT>(s[i], a);
+      unpack<DT>(u[i], b);
+#pragma unroll
+      for (int e = 0; e < E; e++) a[e] = __fadd_rn(a[e], b[e]);
+      s[i] = pack<DT>(a);
+    }
+  };
+  auto again = [&](int64_t at) {  // of a long row: from where the first pass left it
+    if (!LONG) return;
+    if (!sum) return load(at);
+#pragma unroll
+    for (int i = 0; i < NV; i++) s[i] = load_own<DT>(sum + column(at, i), cols - column(at, i), p.vec_s);
+  };
+
+  float hi = 0.0f, lo = 0.0f;
+  for (int64_t at = 0; at < end; at += PIECE) {
+    load(at);
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      float a[E];
+      unpack<DT>(s[i], a);
+      if (sum) {
+        uint4 none = make_uint4(0, 0, 0, 0);
+        store_values<DT, 32>(sum + column(at, i), a, p.vec_s, live ? cols - column(at, i) : -16, none, true, true);
+      }
+#pragma unroll
+      for (int e = 0; e < E; e++) {
+        const float sq = __fmul_rn(a[e], a[e]);
+        if (DT == PEAT_F32) lo = __fadd_rn(lo, __fmaf_rn(a[e], a[e], -sq));  // (16-bit: exact)
+        add_kept(hi, lo, sq);
+      }
+    }
+  }
+  sum_kept<TPR>(hi, lo, sums);
+  const float n = (float)p.cols;
+  // (hi + lo) / n, rounded once: the quotient and what it leaves
+  const float quotient = __fdiv_rn(hi, n);
+  float v = __fadd_rn(quotient, __fdiv_rn(__fadd_rn(__fmaf_rn(-quotient, n, hi), lo), n));
+  const bool fine = hi < 0x1p126f && hi > 0x1p-70f && p.cols < (1 << 24);
+  // (all of a CTA that meets at barriers)
+  if (TPR > 32 ? !__syncthreads_and(fine || !live) : !fine) {
+    double t = 0.0;
+    for (int64_t at = 0; at < end; at += PIECE) {
+      again(at);
+#pragma unroll
+      for (int i = 0; i < NV; i++) {
+        float a[E];
+        unpack<DT>(s[i], a);
+#pragma unroll
+        for (int e = 0; e < E; e++)
+          if (a[e] != 0.0f) t += (double)a[e] * (double)a[e];
+      }
+    }
+    t = sum_wide<TPR>(t, wide);
+    if (!fine) v = (float)(t / (double)p.cols);
+  }
+  const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(v, p.eps)));
+  if (p.rstd && lane == 0 && live) p.rstd[row] = rstd;
+  const bool round = p.q || p.values || p.scale;
+  if (!p.y && !round) return;
+
+  float y[NV][E];
+  auto normed = [&](int64_t at) {
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      float w[E];
+      weights<DT>(p.weight, p.weight_f32, p.vec_w, column(at, i), p.cols, w);
+      unpack<DT>(s[i], y[i]);
+#pragma unroll
+      for (int e = 0; e < E; e++) y[i][e] = __fmul_rn(__fmul_rn(y[i][e], rstd), w[e]);
+    }
+  };
+  float r = 0.0f, scale = 0.0f;
+  bool finite = true;
+  if (round) {
+    uint32_t top = 0;
+    for (int64_t at = 0; at < end; at += PIECE) {
+      again(at);
+      normed(at);
+#pragma unroll
+      for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int e = 0; e < E; e++) {
+          // (what lies beyond the row's end: infinite rows make it 0 x inf)
+          const bool in = column(at, i) + e < cols;
+          top = in ? max_f32(top, __float_as_uint(y[i][e])) : top;
+        }
+    }
+    top = most_of<TPR>(top & 0x7fffffffu, tops);
+    finite = top < Elem<PEAT_F32>::INF;
+    factors<PEAT_F32>(top, r, scale);
+    if (p.scale && lane == 0 && live) p.scale[row] = scale;
+  }
+  for (int64_t at = 0; at < end; at += PIECE) {
+    if (LONG || !round) {
+      again(at);
+      normed(at);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int64_t col = column(at, i), left = live ? p.cols - col : -16;
+      uint4 none = make_uint4(0, 0, 0, 0);
+      if (p.y) store_values<DT, 32>(static_cast<T*>(p.y) + row * p.ldy + col, y[i], p.vec_y, left, none, true, true);
+      if (!p.q && !p.values) continue;
+      float w[E];
+#pragma unroll
+      for (int e = 0; e < E; e++) w[e] = whole(y[i][e], r, finite);
+      if (p.q) {
+        int8_t* q = p.q + row * p.ldq + col;
+        if (p.vec_q && left >= E) {
+          if (E == 8)
+            *reinterpret_cast<uint2*>(q) = make_uint2(pack4(w[0], w[1], w[2], w[3]), pack4(w[4 % E], w[5 % E], w[6 % E], w[7 % E]));
+          else
+            *reinterpret_cast<uint32_t*>(q) = pack4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; e++)
+            if (e < left) q[e] = byte_of(w[e]);
+        }
+      }
+      if (p.values) {
+        float z[E];
+#pragma unroll
+        for (int e = 0; e < E; e++) z[e] = __fmul_rn(number(w[e]), scale);
+        store_values<DT, 32>(static_cast<T*>(p.values) + row * p.ldv + col, z, p.vec_v, left, none, true, true);
+      }
+    }
+  }
+}
+
+// ---- backward -----------------------------------------------------------------
+//   n = s rstd, g = grad weight, c = sum (g n) / cols,
+//   grad_x = rstd (g - n c) + stream, grad_weight = sum over rows of grad n
+// A CTA has `each` rows for each of its groups of TPR threads, one after another; a
+// thread keeps its columns' sums over them.  LONG: the CTAs of blockIdx.y have a
+// piece of the columns, and c is there already (rms_dots).
+template <int DT, int TPR, int NV, bool GRID, bool LONG>
+__global__ void __launch_bounds__(threads_of<TPR>()) rms_backward(RmsBackParams p) {
+  using L = Elem<DT>;
+  using T = typename L::T;
+  constexpr int E = L::E, QT = threads_of<TPR>(), GROUPS = QT / TPR;
+  __shared__ float dots[2][QT / 32];
+  __shared__ float met[GROUPS > 1 ? TPR * NV * E : 1];
+  pdl_wait();
+  pdl_trigger();
+  const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+  const int64_t at = LONG ? (int64_t)blockIdx.y * TPR * NV * E : 0;
+  const int64_t row0 = ((int64_t)blockIdx.x * GROUPS + group) * p.each;
+  const Source<DT, GRID> sg(p.grad, p.rows, p.cols, p.ldg), sx(p.x, p.rows, p.cols, p.ldx), st(p.stream, p.rows, p.cols, p.ldr);
+  auto column = [&](int i) { return at + (int64_t)(i * TPR + lane) * E; };
+  float dw[NV][E];
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int e = 0; e < E; e++) dw[i][e] = 0.0f;
+  for (int64_t it = 0; it < p.each; it++) {
+    const int64_t row = row0 + it;
+    const bool live = row < p.rows;
+    const int64_t cols = live ? p.cols : 0;
+    const float rstd = live ? __ldg(p.rstd + row) : 0.0f;
+    uint4 d[NV], s[NV];
+    const T* dp = static_cast<const T*>(p.grad) + row * p.ldg;
+    const T* xp = static_cast<const T*>(p.x) + row * p.ldx;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      d[i] = load_vec(sg, dp + column(i), cols - column(i));
+      s[i] = load_vec(sx, xp + column(i), cols - column(i));
+    }
+    float c = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      float a[E], b[E], w[E];
+      unpack<DT>(d[i], a);
+      unpack<DT>(s[i], b);
+      if (!LONG) weights<DT>(p.weight, p.weight_f32, p.vec_w, column(i), p.cols, w);
+#pragma unroll
+      for (int e = 0; e < E; e++) {
+        const float n = __fmul_rn(b[e], rstd);
+        if (column(i) + e < cols) dw[i][e] = __fmaf_rn(a[e], n, dw[i][e]);
+        if (!LONG) c = __fmaf_rn(__fmul_rn(a[e], w[e]), n, c);
+      }
+    }
+    if (!p.grad_x) continue;
+    if (LONG) c = live ? __ldg(p.dots + row) : 0.0f;
+    else c = sum_plain<TPR>(c, dots[it & 1]) / (float)p.cols;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      float a[E], b[E], w[E], t[E];
+      unpack<DT>(d[i], a);
+      unpack<DT>(s[i], b);
+      weights<DT>(p.weight, p.weight_f32, p.vec_w, column(i), p.cols, w);
+#pragma unroll
+      for (int e = 0; e < E; e++) b[e] = __fmul_rn(rstd, __fmaf_rn(-__fmul_rn(b[e], rstd), c, __fmul_rn(a[e], w[e])));
+      if (p.stream) {
+        unpack<DT>(load_vec(st, static_cast<const T*>(p.stream) + row * p.ldr + column(i), cols - column(i)), t);
+#pragma unroll
+        for (int e = 0; e < E; e++) b[e] = __fadd_rn(b[e], t[e]);
+      }
+      uint4 none = make_uint4(0, 0, 0, 0);
+      store_values<DT, 32>(static_cast<T*>(p.grad_x) + row * p.ldo + column(i), b, p.vec_o, live ? cols - column(i) : -16, none,
+                           true, true);
+    }
+  }
+  if (!p.grad_weight) return;
+  if (GROUPS > 1) {  // the groups' sums, one after the other
+    for (int g = 0; g < GROUPS; g++) {
+      if (group == g) {
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+#pragma unroll
+          for (int e = 0; e < E; e++) {
+            float* m = met + (i * E + e) * TPR + lane;
+            dw[i][e] = g ? *m + dw[i][e] : dw[i][e];
+            *m = dw[i][e];
+          }
+      }
+      __syncthreads();
+    }
+    if (group != GROUPS - 1) return;
+  }
+  float* o = p.parts + (int64_t)blockIdx.x * p.cols;
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int e = 0; e < E; e++)
+      if (column(i) + e < p.cols) o[column(i) + e] = dw[i][e];
+}
+
+// sum (g n) / cols of each row, by a CTA
+template <int DT, bool GRID>
+__global__ void __launch_bounds__(256) rms_dots(RmsBackParams p) {
+  using T = typename Elem<DT>::T;
+  constexpr int E = Elem<DT>::E;
+  __shared__ float parts[8];
+  pdl_wait();
+  pdl_trigger();
+  const int64_t row = blockIdx.x;
+  const Source<DT, GRID> sg(p.grad, p.rows, p.cols, p.ldg), sx(p.x, p.rows, p.cols, p.ldx);
+  const T* dp = static_cast<const T*>(p.grad) + row * p.ldg;
+  const T* xp = static_cast<const T*>(p.x) + row * p.ldx;
+  const float rstd = __ldg(p.rstd + row);
+  float c = 0.0f;
+  for (int64_t col = (int64_t)threadIdx.x * E; col < p.cols; col += 256 * E) {
+    float a[E], b[E], w[E];
+    unpack<DT>(load_vec(sg, dp + col, p.cols - col), a);
+    unpack<DT>(load_vec(sx, xp + col, p.cols - col), b);
+    weights<DT>(p.weight, p.weight_f32, p.vec_w, col, p.cols, w);
+    float part = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; e++) part = __fmaf_rn(__fmul_rn(a[e], w[e]), __fmul_rn(b[e], rstd), part);
+    c += part;
+  }
+  c = sum_plain<256>(c, parts);
+  if (threadIdx.x == 0) p.dots[row] = c / (float)p.cols;
+}
+
+// the CTAs' sums of each column, in their order: 8 lanes of rows, then over the lanes
+__global__ void __launch_bounds__(256) rms_weight_sums(const float* parts, int ctas, int64_t cols, float* out) {
+  pdl_wait();
+  pdl_trigger();
+  __shared__ float met[8][32];
+  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int64_t col = (int64_t)blockIdx.x * 32 + lane;
+  float hi = 0.0f, lo = 0.0f;
+  if (col < cols)
+    for (int i = part; i < ctas; i += 8) add_kept(hi, lo, __ldcg(parts + (int64_t)i * cols + col));
+  met[part][lane] = __fadd_rn(hi, lo);
+  __syncthreads();
+  if (part || col >= cols) return;
+  float t = met[0][lane];
+#pragma unroll
+  for (int i = 1; i < 8; i++) t += met[i][lane];
+  out[col] = t;
+}
+
+template <int DT, int TPR, int NV, bool LONG = false>
+cudaError_t forward(const RmsParams& p, cudaStream_t s) {
+  constexpr int QT = threads_of<TPR>();
+  const unsigned grid = (unsigned)((p.rows + QT / TPR - 1) / (QT / TPR));
+  if (p.grid) return launch_dependent(rms_forward<DT, TPR, NV, true, LONG>, grid, QT, 0, s, p);
+  return launch_dependent(rms_forward<DT, TPR, NV, false, LONG>, grid, QT, 0, s, p);
+}
+template <int DT>
+cudaError_t forward_of(const RmsParams& p, cudaStream_t s) {
+  const int64_t vecs = (p.cols + Elem<DT>::E - 1) / Elem<DT>::E;
+  if (vecs <= 32) return forward<DT, 32, 1>(p, s);
+  if (vecs <= 128) return forward<DT, 32, 4>(p, s);
+  if (vecs <= 512) return forward<DT, 128, 4>(p, s);
+  if (vecs <= 1024) return forward<DT, 256, 4>(p, s);
+  if (vecs <= 2048) return forward<DT, 512, 4>(p, s);
+  return forward<DT, 512, 4, true>(p, s);
+}
+
+struct Shape {  // of the backward kernel
+  int tpr, nv;
+  bool longer;
+};
+Shape shape_of(int64_t vecs) {
+  if (vecs <= 32) return {32, 1, false};
+  if (vecs <= 128) return {32, 4, false};
+  if (vecs <= 256) return {64, 4, false};
+  if (vecs <= 512) return {128, 4, false};
+  if (vecs <= 1024) return {256, 4, false};
+  return {256, 4, true};
+}
+template <int DT, int TPR, int NV, bool LONG = false>
+cudaError_t backward(const RmsBackParams& p, cudaStream_t s) {
+  constexpr int QT = threads_of<TPR>();
+  cudaError_t e = cudaSuccess;
+  if (LONG && p.rows && p.grad_x) {
+    e = p.grid ? launch_dependent(rms_dots<DT, true>, (unsigned)p.rows, 256, 0, s, p)
+               : launch_dependent(rms_dots<DT, false>, (unsigned)p.rows, 256, 0, s, p);
+    if (e != cudaSuccess) return e;
+  }
+  if (p.ctas) {
+    constexpr int64_t PIECE = (int64_t)TPR * NV * Elem<DT>::E;
+    const dim3 grid((unsigned)p.ctas, LONG ? (unsigned)((p.cols + PIECE - 1) / PIECE) : 1u);
+    e = p.grid ? launch_dependent(rms_backward<DT, TPR, NV, true, LONG>, grid, QT, 0, s, p)
+               : launch_dependent(rms_backward<DT, TPR, NV, false, LONG>, grid, QT, 0, s, p);
+    if (e != cudaSuccess) return e;
+  }
+  if (!p.grad_weight) return e;
+  return launch_dependent(rms_weight_sums, (unsigned)((p.cols + 31) / 32), 256, 0, s, (const float*)p.parts, p.ctas, p.cols, p.grad_weight);
+}
+template <int DT>
+cudaError_t backward_of(const RmsBackParams& p, cudaStream_t s) {
+  const Shape k = shape_of((p.cols + Elem<DT>::E - 1) / Elem<DT>::E);
+  if (k.longer) return backward<DT, 256, 4, true>(p, s);
+  if (k.tpr == 32) return k.nv == 1 ? backward<DT, 32, 1>(p, s) : backward<DT, 32, 4>(p, s);
+  if (k.tpr == 64) return backward<DT, 64, 4>(p, s);
+  if (k.tpr == 128) return backward<DT, 128, 4>(p, s);
+  return backward<DT, 256, 4>(p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_rmsnorm(int dtype, const RmsParams& p, cudaStream_t s) {
+  switch (dtype) {
+    case PEAT_F32: return forward_of<PEAT_F32>(p, s);
+    case PEAT_F16: return forward_of<PEAT_F16>(p, s);
+    default: return forward_of<PEAT_BF16>(p, s);
+  }
+}
+
+RmsBackPlan rms_back_plan(int dtype, int64_t rows, int64_t cols, int nsm) {
+  const int e = dtype == PEAT_F32 ? 4 : 8;
+  const Shape k = shape_of((cols + e - 1) / e);
+  const int64_t groups = std::max(256, k.tpr) / k.tpr;  // of a CTA
+  // two CTAs an SM; a long row's pieces fill the SMs already where there are several
+  const int64_t pieces = k.longer ? (cols + (int64_t)k.tpr * k.nv * e - 1) / ((int64_t)k.tpr * k.nv * e) : 1;
+  const int64_t most = std::max<int64_t>(1, 3 * (int64_t)nsm / pieces);
+  RmsBackPlan r;
+  r.longer = k.longer;
+  r.each = std::max<int64_t>(1, (rows + most * groups - 1) / (most * groups));
+  r.ctas = (int)((rows + r.each * groups - 1) / (r.each * groups));
+  return r;
+}
+
+cudaError_t launch_rmsnorm_backward(int dtype, const RmsBackPlan& plan, const RmsBackParams& in, cudaStream_t s) {
+  RmsBackParams p = in;
+  p.ctas = plan.ctas;
+  p.each = plan.each;
+  switch (dtype) {
+    case PEAT_F32: return backward_of<PEAT_F32>(p, s);
+    case PEAT_F16: return backward_of<PEAT_F16>(p, s);
+    default: return backward_of<PEAT_BF16>(p, s);
+  }
+}
+
+}  // namespace peat

@@ -233,6 +233,13 @@ __device__ __forceinline__ void put_columns(const OutPlace& p, const float (&v)[
   }
 }
 
+// Polls for what a CTA has under way before it ends, whether or not an earlier
+// wait of its expired.  A poll that finds nothing takes 4 us: a quarter of a
+// second for each copy stage, for copies and instructions that
+// take microseconds.  (Where all went well nothing hangs on these: the cluster
+// meets only when the instructions are done.)
+constexpr uint32_t END_LIMIT = 1u << 16;
+
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);

@@ -23,7 +23,8 @@ GRADNORM_BYTES = 16
 NORM_TYPES = {"2": 0, "1": 1, "inf": 2}
 BAD_MODES = {"propagate": 0, "zero": 1, "keep": 2}
 
-OPS_EXPORTS = ("peat_quantize_i8", "peat_matmul_i8", "peat_product_i8", "peat_grad_norm", "peat_grad_clip")
+OPS_EXPORTS = ("peat_quantize_i8", "peat_matmul_i8", "peat_product_i8", "peat_grad_norm", "peat_grad_clip",
+               "peat_quantize_f4", "peat_matmul_f4", "peat_product_f4", "peat_rmsnorm", "peat_rmsnorm_backward")
 INT8 = 101
 
 
@@ -37,6 +38,12 @@ class Operand8(ctypes.Structure):
                 ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("axis", ctypes.c_int32)]
 
 
+class OperandF4(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("block_scale", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("axis", ctypes.c_int32)]
+
+
 def register(L) -> None:
     """Argument types of the entry points in a loaded library."""
     vp, i64, i32, f32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float
@@ -46,6 +53,13 @@ def register(L) -> None:
     L.peat_product_i8.argtypes = [vp, op, op, vp, vp, i64, i32, vp]
     L.peat_grad_norm.argtypes = [vp, vp, i64, i32, f32, vp, vp, vp]
     L.peat_grad_clip.argtypes = [vp, vp, i64, i32, f32, f32, f32, i32, vp, vp, vp]
+    L.peat_quantize_f4.argtypes = [vp, vp, i64, i64, i64, i32, i32, i32, vp, i64, vp, vp, vp, i64, vp]
+    L.peat_matmul_f4.argtypes = [vp, i32, vp, i64, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, vp, i64, i32, vp]
+    op4 = ctypes.POINTER(OperandF4)
+    L.peat_product_f4.argtypes = [vp, i32, op4, op4, vp, vp, i64, i32, vp]
+    L.peat_rmsnorm.argtypes = [vp, vp, i64, vp, i64, vp, i32, i64, i64, i32, f32, vp, i64, vp, i64, vp, i64, vp, vp, i64,
+                               vp, vp]
+    L.peat_rmsnorm_backward.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i32, vp, i64, i64, i32, vp, i64, vp, vp]
     for name in OPS_EXPORTS:
         getattr(L, name).restype = i32
 
@@ -359,21 +373,18 @@ def _as_rows(t, K: int):
     return x if (s1 == 1 or K <= 1) and (s0 >= K or x.shape[0] <= 1) else x.contiguous()
 
 
-class Linear8:
-    """y = x w^T with w [out, in] held in 8-bit integers, by row for the forward product and by column for the
-    input gradient; x and the output gradient are rounded as they come (by row, or, for the weight gradient, by
-    column).  Inputs are float32, float16 or bfloat16 with any leading dimensions and strides; the layer keeps none of
-    them."""
+class LinearBase:
+    """y = x w^T of a weight [out, in] that is held at a lower precision, by row for the forward product and by column
+    for the input gradient; what comes in is rounded on the way.  A kind of layer says how (``_hold``: the weight's
+    operand along an axis; ``_take``: an incoming matrix's operand; ``_multiply``)."""
 
     def __init__(self, h, weight, stream=None):
         self.h = h
         self.out_features, self.in_features = weight.shape
         with _on(stream):
             weight = _as_rows(weight, self.in_features)
-        self.q, self.scale = peat_quantize_i8(h, weight, 0, stream)
-        self.qt, self.scale_t = peat_quantize_i8(h, weight, 1, stream)
-        self._w = _operand(h, self.q, 0, self.scale, "weight")
-        self._wt = _operand(h, self.qt, 0, self.scale_t, "weight")
+        self._w = self._hold(weight, 0, stream), self.out_features, self.in_features
+        self._wt = self._hold(weight, 1, stream), self.in_features, self.out_features
 
     def _product(self, t, w, name: str, bias=None, stream=None):
         """t [..., K] by row times a weight operand -> [..., N] of t's type."""
@@ -386,10 +397,9 @@ class Linear8:
         if not shape or shape[-1] != K:
             raise ValueError(f"the last dimension of {name} must be {K}")
         x = _as_rows(t, K)
-        a, M, _ = _operand(self.h, x, 0, None, name)
-        out = torch.empty((M, N), dtype=x.dtype, device=x.device)
-        _call(self.h, "peat_product_i8", ctypes.byref(a), ctypes.byref(op), _vector(self.h, bias, N, "bias"),
-              out.data_ptr(), N, _code(out), _stream(self.h, None))
+        a = self._take(x, name)
+        out = torch.empty((x.shape[0], N), dtype=x.dtype, device=x.device)
+        self._multiply(a, op, _vector(self.h, bias, N, "bias"), out.data_ptr(), N, _code(out), _stream(self.h, None))
         return out if len(shape) == 2 else out.view(*shape[:-1], N)
 
     def forward(self, x, bias=None, stream=None):
@@ -410,8 +420,51 @@ class Linear8:
         g, x = _as_rows(grad, self.out_features), _as_rows(x, self.in_features)
         if g.shape[0] != x.shape[0]:
             raise ValueError("grad and x differ in their leading dimensions")
-        return peat_product_i8(self.h, g, x, 1, 1)
+        return self._columns(g, x)
 
     def backward(self, grad, x, stream=None):
         """(dL/dx, dL/dw)."""
         return self.input_grad(grad, stream), self.weight_grad(grad, x, stream)
+
+
+class Linear8(LinearBase):
+    """y = x w^T with w [out, in] held in 8-bit integers, by row for the forward product and by column for the
+    input gradient; x and the output gradient are rounded as they come (by row, or, for the weight gradient, by
+    column).  Inputs are float32, float16 or bfloat16 with any leading dimensions and strides; the layer keeps none of
+    them."""
+
+    def __init__(self, h, weight, stream=None):
+        super().__init__(h, weight, stream)
+        (self.q, self.scale), (self.qt, self.scale_t) = self._w[0][1], self._wt[0][1]
+        self._w, self._wt = (self._w[0][0], *self._w[1:]), (self._wt[0][0], *self._wt[1:])
+
+    def _hold(self, weight, axis: int, stream):
+        q, scale = peat_quantize_i8(self.h, weight, axis, stream)
+        return _operand(self.h, q, 0, scale, "weight")[0], (q, scale)
+
+    def _take(self, x, name: str):
+        return _operand(self.h, x, 0, None, name)[0]
+
+    def _multiply(self, a, b, *rest) -> None:
+        _call(self.h, "peat_product_i8", ctypes.byref(a), ctypes.byref(b), *rest)
+
+    def _columns(self, g, x):
+        return peat_product_i8(self.h, g, x, 1, 1)
+
+    def forward_rounded(self, q, scale, out_dtype=None, bias=None, stream=None):
+        """forward of an input that is 8-bit integers already, q int8 [..., in] and scale float32 [...], as
+        ``peat_rmsnorm`` leaves them -> [..., out] of out_dtype (float32 unless given)."""
+        if stream is not None:
+            with _on(stream):
+                return self.forward_rounded(q, scale, out_dtype, bias)
+        import torch
+        if q.dtype != torch.int8 or q.shape[-1:] != (self.in_features,):
+            raise ValueError(f"q must be int8, its last dimension {self.in_features}")
+        if scale.shape != q.shape[:-1]:
+            raise ValueError("scale must have one element for each row of q")
+        x = _as_rows(q, self.in_features)
+        a = _operand(self.h, x, 0, scale.reshape(-1), "q")[0]
+        out = torch.empty((x.shape[0], self.out_features), dtype=out_dtype or torch.float32, device=x.device)
+        self._multiply(a, self._w[0], _vector(self.h, bias, self.out_features, "bias"), out.data_ptr(), self.out_features,
+                       _code(out), _stream(self.h, None))
+        return out if q.dim() == 2 else out.view(*q.shape[:-1], self.out_features)
