@@ -30,26 +30,14 @@ __device__ __forceinline__ void add_kept(float& hi, float& lo, float x) {
   lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(t, z)), __fsub_rn(x, z)));
   hi = t;
 }
-// Sums over the TPR threads of a row, the same bits in all of them.  `part`: a
-// place for each warp, read only after a barrier that all of the CTA meets.
-template <int TPR>
-__device__ __forceinline__ void sum_kept(float& hi, float& lo, float2* part) {
+// (hi, lo) over the lanes of a group of N, the same bits in all of them
+template <int N>
+__device__ __forceinline__ void lanes_kept(float& hi, float& lo) {
 #pragma unroll
-  for (int o = 16; o; o /= 2) {
+  for (int o = N / 2; o; o /= 2) {
     const float h = __shfl_xor_sync(0xffffffffu, hi, o), l = __shfl_xor_sync(0xffffffffu, lo, o);
     lo = __fadd_rn(lo, l);
     add_kept(hi, lo, h);
-  }
-  if (TPR > 32) {
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = make_float2(hi, lo);
-    __syncthreads();
-    const float2* p = part + threadIdx.x / TPR * (TPR / 32);
-    hi = p[0].x, lo = p[0].y;
-#pragma unroll
-    for (int w = 1; w < TPR / 32; w++) {
-      lo = __fadd_rn(lo, p[w].y);
-      add_kept(hi, lo, p[w].x);
-    }
   }
 }
 template <int TPR>
@@ -80,19 +68,6 @@ __device__ __forceinline__ float sum_plain(float x, float* part) {
   }
   return x;
 }
-template <int TPR>
-__device__ __forceinline__ uint32_t most_of(uint32_t top, uint32_t* part) {
-  top = __reduce_max_sync(0xffffffffu, top);
-  if (TPR > 32) {
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = top;
-    __syncthreads();
-    const uint32_t* p = part + threadIdx.x / TPR * (TPR / 32);
-#pragma unroll
-    for (int w = 0; w < TPR / 32; w++) top = max(top, p[w]);
-  }
-  return top;
-}
-
 template <int DT, bool GRID>
 __device__ __forceinline__ uint4 load_vec(const Source<DT, GRID>& s, const typename Elem<DT>::T* p, int64_t left) {
   if (s.whole(p, left)) return s.load(p);
@@ -139,12 +114,12 @@ __device__ __forceinline__ void weights(const void* w, int f32, bool vec, int64_
 // TPR threads have a row, NV vectors each; LONG: rows that these do not hold, read
 // again for each of the three passes.
 template <int DT, int TPR, int NV, bool GRID, bool LONG>
-__global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
+__global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 4) rms_forward(RmsParams p) {
   using L = Elem<DT>;
   using T = typename L::T;
   constexpr int E = L::E, QT = threads_of<TPR>();
   constexpr int64_t PIECE = (int64_t)TPR * NV * E;
-  __shared__ float2 sums[QT / 32];
+  __shared__ float2 sums[QT / 32], found[QT / TPR], factor[QT / TPR];
   __shared__ double wide[QT / 32];
   __shared__ uint32_t tops[QT / 32];
   pdl_wait();
@@ -186,6 +161,13 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
   float hi = 0.0f, lo = 0.0f;
   for (int64_t at = 0; at < end; at += PIECE) {
     load(at);
+    // Squares on top of one that none exceeds: what a sum's rounding leaves of a
+    // square is then the difference of two sums away (Dekker's short form)
+    uint4 m = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NV; i++) m = mag_max<DT>(m, s[i]);
+    const float most = L::mag(mag_fold<DT>(m)), base = __fmul_ru(most, most);
+    float t = base, rest = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       float a[E];
@@ -196,20 +178,54 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
       }
 #pragma unroll
       for (int e = 0; e < E; e++) {
-        const float sq = __fmul_rn(a[e], a[e]);
-        if (DT == PEAT_F32) lo = __fadd_rn(lo, __fmaf_rn(a[e], a[e], -sq));  // (16-bit: exact)
-        add_kept(hi, lo, sq);
+        const float u = __fmaf_rn(a[e], a[e], t);
+        rest = __fadd_rn(rest, __fmaf_rn(a[e], a[e], __fsub_rn(t, u)));
+        t = u;
       }
     }
+    lo = __fadd_rn(lo, rest);
+    if (LONG) {
+      add_kept(hi, lo, t);
+      add_kept(hi, lo, -base);
+    } else {
+      hi = t;
+      add_kept(hi, lo, -base);
+    }
   }
-  sum_kept<TPR>(hi, lo, sums);
-  const float n = (float)p.cols;
-  // (hi + lo) / n, rounded once: the quotient and what it leaves
-  const float quotient = __fdiv_rn(hi, n);
-  float v = __fadd_rn(quotient, __fdiv_rn(__fadd_rn(__fmaf_rn(-quotient, n, hi), lo), n));
-  const bool fine = hi < 0x1p126f && hi > 0x1p-70f && p.cols < (1 << 24);
-  // (all of a CTA that meets at barriers)
-  if (TPR > 32 ? !__syncthreads_and(fine || !live) : !fine) {
+  lanes_kept<32>(hi, lo);
+  // One warp adds up the warps' sums and finds the row's factor for all: the
+  // divisions would be a quarter of every thread's instructions.
+  if (TPR > 32) {
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = make_float2(hi, lo);
+    __syncthreads();
+  }
+  constexpr int WARPS = TPR / 32, FIRST = TPR > 32 ? 32 : TPR;
+  bool fine = true;
+  float rstd = 0.0f;
+  if (lane < FIRST) {
+    if (TPR > 32) {
+      const float2 f = sums[threadIdx.x / TPR * WARPS + (lane & (WARPS - 1))];
+      hi = f.x, lo = f.y;
+      lanes_kept<WARPS>(hi, lo);
+    }
+    // (hi + lo) / n, rounded once: the quotient and what it leaves
+    const float n = (float)(int)p.cols, quotient = __fdiv_rn(hi, n);
+    const float v = __fadd_rn(quotient, __fdiv_rn(__fadd_rn(__fmaf_rn(-quotient, n, hi), lo), n));
+    fine = (hi < 0x1p126f && hi > 0x1p-70f && p.cols < (1 << 24)) || !live;
+    rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(v, p.eps)));
+    if (TPR > 32 && lane == 0) found[threadIdx.x / TPR] = make_float2(rstd, fine ? 1.0f : 0.0f);
+  }
+  bool wide_row = !fine;  // of the whole CTA where it meets at barriers
+  if (TPR > 32) {
+    __syncthreads();
+    const float2 f = found[threadIdx.x / TPR];
+    rstd = f.x;
+    fine = f.y != 0.0f;
+    wide_row = false;
+#pragma unroll
+    for (int g = 0; g < QT / TPR; g++) wide_row |= found[g].y == 0.0f;
+  }
+  if (wide_row) {
     double t = 0.0;
     for (int64_t at = 0; at < end; at += PIECE) {
       again(at);
@@ -223,9 +239,8 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
       }
     }
     t = sum_wide<TPR>(t, wide);
-    if (!fine) v = (float)(t / (double)p.cols);
+    if (!fine) rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn((float)(t / (double)p.cols), p.eps)));
   }
-  const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(v, p.eps)));
   if (p.rstd && lane == 0 && live) p.rstd[row] = rstd;
   const bool round = p.q || p.values || p.scale;
   if (!p.y && !round) return;
@@ -242,8 +257,8 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
     }
   };
   float r = 0.0f, scale = 0.0f;
-  bool finite = true;
   if (round) {
+    // (beyond the row's end y is 0, or NaN where all of the row is)
     uint32_t top = 0;
     for (int64_t at = 0; at < end; at += PIECE) {
       again(at);
@@ -251,17 +266,26 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
 #pragma unroll
       for (int i = 0; i < NV; i++)
 #pragma unroll
-        for (int e = 0; e < E; e++) {
-          // (what lies beyond the row's end: infinite rows make it 0 x inf)
-          const bool in = column(at, i) + e < cols;
-          top = in ? max_f32(top, __float_as_uint(y[i][e])) : top;
-        }
+        for (int e = 0; e < E; e++) top = max_f32(top, __float_as_uint(y[i][e]));
     }
-    top = most_of<TPR>(top & 0x7fffffffu, tops);
-    finite = top < Elem<PEAT_F32>::INF;
-    factors<PEAT_F32>(top, r, scale);
-    if (p.scale && lane == 0 && live) p.scale[row] = scale;
+    top = __reduce_max_sync(0xffffffffu, top & 0x7fffffffu);
+    if (TPR > 32) {
+      if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+      __syncthreads();
+    }
+    if (lane < FIRST) {
+      if (TPR > 32) top = __reduce_max_sync(0xffffffffu, tops[threadIdx.x / TPR * WARPS + (lane & (WARPS - 1))]);
+      factors<PEAT_F32>(top, r, scale);
+      if (p.scale && lane == 0 && live) p.scale[row] = scale;
+      if (TPR > 32 && lane == 0) factor[threadIdx.x / TPR] = make_float2(r, scale);
+    }
+    if (TPR > 32) {
+      __syncthreads();
+      r = factor[threadIdx.x / TPR].x;
+      scale = factor[threadIdx.x / TPR].y;
+    }
   }
+  const bool finite = scale == scale;
   for (int64_t at = 0; at < end; at += PIECE) {
     if (LONG || !round) {
       again(at);
@@ -274,8 +298,13 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
       if (p.y) store_values<DT, 32>(static_cast<T*>(p.y) + row * p.ldy + col, y[i], p.vec_y, left, none, true, true);
       if (!p.q && !p.values) continue;
       float w[E];
+      if (finite) {
 #pragma unroll
-      for (int e = 0; e < E; e++) w[e] = whole(y[i][e], r, finite);
+        for (int e = 0; e < E; e++) w[e] = whole(y[i][e], r, true);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; e++) w[e] = MAGIC;
+      }
       if (p.q) {
         int8_t* q = p.q + row * p.ldq + col;
         if (p.vec_q && left >= E) {
@@ -306,7 +335,7 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_forward(RmsParams p) {
 // thread keeps its columns' sums over them.  LONG: the CTAs of blockIdx.y have a
 // piece of the columns, and c is there already (rms_dots).
 template <int DT, int TPR, int NV, bool GRID, bool LONG>
-__global__ void __launch_bounds__(threads_of<TPR>()) rms_backward(RmsBackParams p) {
+__global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) rms_backward(RmsBackParams p) {
   using L = Elem<DT>;
   using T = typename L::T;
   constexpr int E = L::E, QT = threads_of<TPR>(), GROUPS = QT / TPR;
@@ -315,6 +344,7 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_backward(RmsBackParams 
   pdl_wait();
   pdl_trigger();
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+  const float n_cols = (float)(int)p.cols;
   const int64_t at = LONG ? (int64_t)blockIdx.y * TPR * NV * E : 0;
   const int64_t row0 = ((int64_t)blockIdx.x * GROUPS + group) * p.each;
   const Source<DT, GRID> sg(p.grad, p.rows, p.cols, p.ldg), sx(p.x, p.rows, p.cols, p.ldx), st(p.stream, p.rows, p.cols, p.ldr);
@@ -329,7 +359,7 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_backward(RmsBackParams 
     const bool live = row < p.rows;
     const int64_t cols = live ? p.cols : 0;
     const float rstd = live ? __ldg(p.rstd + row) : 0.0f;
-    uint4 d[NV], s[NV];
+    uint4 d[NV], s[NV], u[NV];
     const T* dp = static_cast<const T*>(p.grad) + row * p.ldg;
     const T* xp = static_cast<const T*>(p.x) + row * p.ldx;
 #pragma unroll
@@ -337,6 +367,10 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_backward(RmsBackParams 
       d[i] = load_vec(sg, dp + column(i), cols - column(i));
       s[i] = load_vec(sx, xp + column(i), cols - column(i));
     }
+    if (p.stream && p.grad_x)
+#pragma unroll
+      for (int i = 0; i < NV; i++)
+        u[i] = load_vec(st, static_cast<const T*>(p.stream) + row * p.ldr + column(i), cols - column(i));
     float c = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
@@ -347,13 +381,13 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_backward(RmsBackParams 
 #pragma unroll
       for (int e = 0; e < E; e++) {
         const float n = __fmul_rn(b[e], rstd);
-        if (column(i) + e < cols) dw[i][e] = __fmaf_rn(a[e], n, dw[i][e]);
+        dw[i][e] = __fmaf_rn(a[e], n, dw[i][e]);
         if (!LONG) c = __fmaf_rn(__fmul_rn(a[e], w[e]), n, c);
       }
     }
     if (!p.grad_x) continue;
     if (LONG) c = live ? __ldg(p.dots + row) : 0.0f;
-    else c = sum_plain<TPR>(c, dots[it & 1]) / (float)p.cols;
+    else c = sum_plain<TPR>(c, dots[it & 1]) / n_cols;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       float a[E], b[E], w[E], t[E];
@@ -363,7 +397,7 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_backward(RmsBackParams 
 #pragma unroll
       for (int e = 0; e < E; e++) b[e] = __fmul_rn(rstd, __fmaf_rn(-__fmul_rn(b[e], rstd), c, __fmul_rn(a[e], w[e])));
       if (p.stream) {
-        unpack<DT>(load_vec(st, static_cast<const T*>(p.stream) + row * p.ldr + column(i), cols - column(i)), t);
+        unpack<DT>(u[i], t);
 #pragma unroll
         for (int e = 0; e < E; e++) b[e] = __fadd_rn(b[e], t[e]);
       }
@@ -397,6 +431,7 @@ __global__ void __launch_bounds__(threads_of<TPR>()) rms_backward(RmsBackParams 
       if (column(i) + e < p.cols) o[column(i) + e] = dw[i][e];
 }
 
+// (beyond a row's end grad, x and weight are 0)
 // sum (g n) / cols of each row, by a CTA
 template <int DT, bool GRID>
 __global__ void __launch_bounds__(256) rms_dots(RmsBackParams p) {
@@ -422,7 +457,7 @@ __global__ void __launch_bounds__(256) rms_dots(RmsBackParams p) {
     c += part;
   }
   c = sum_plain<256>(c, parts);
-  if (threadIdx.x == 0) p.dots[row] = c / (float)p.cols;
+  if (threadIdx.x == 0) p.dots[row] = c / (float)(int)p.cols;
 }
 
 // the CTAs' sums of each column, in their order: 8 lanes of rows, then over the lanes
@@ -455,9 +490,11 @@ template <int DT>
 cudaError_t forward_of(const RmsParams& p, cudaStream_t s) {
   const int64_t vecs = (p.cols + Elem<DT>::E - 1) / Elem<DT>::E;
   if (vecs <= 32) return forward<DT, 32, 1>(p, s);
-  if (vecs <= 128) return forward<DT, 32, 4>(p, s);
-  if (vecs <= 512) return forward<DT, 128, 4>(p, s);
-  if (vecs <= 1024) return forward<DT, 256, 4>(p, s);
+  if (vecs <= 64) return forward<DT, 32, 2>(p, s);
+  if (vecs <= 128) return forward<DT, 64, 2>(p, s);
+  if (vecs <= 256) return forward<DT, 128, 2>(p, s);
+  if (vecs <= 512) return forward<DT, 256, 2>(p, s);
+  if (vecs <= 1024) return forward<DT, 512, 2>(p, s);
   if (vecs <= 2048) return forward<DT, 512, 4>(p, s);
   return forward<DT, 512, 4, true>(p, s);
 }
@@ -468,10 +505,11 @@ struct Shape {  // of the backward kernel
 };
 Shape shape_of(int64_t vecs) {
   if (vecs <= 32) return {32, 1, false};
-  if (vecs <= 128) return {32, 4, false};
-  if (vecs <= 256) return {64, 4, false};
-  if (vecs <= 512) return {128, 4, false};
-  if (vecs <= 1024) return {256, 4, false};
+  if (vecs <= 64) return {32, 2, false};
+  if (vecs <= 128) return {64, 2, false};
+  if (vecs <= 256) return {128, 2, false};
+  if (vecs <= 512) return {256, 2, false};
+  if (vecs <= 1024) return {512, 2, false};
   return {256, 4, true};
 }
 template <int DT, int TPR, int NV, bool LONG = false>
@@ -497,10 +535,13 @@ template <int DT>
 cudaError_t backward_of(const RmsBackParams& p, cudaStream_t s) {
   const Shape k = shape_of((p.cols + Elem<DT>::E - 1) / Elem<DT>::E);
   if (k.longer) return backward<DT, 256, 4, true>(p, s);
-  if (k.tpr == 32) return k.nv == 1 ? backward<DT, 32, 1>(p, s) : backward<DT, 32, 4>(p, s);
-  if (k.tpr == 64) return backward<DT, 64, 4>(p, s);
-  if (k.tpr == 128) return backward<DT, 128, 4>(p, s);
-  return backward<DT, 256, 4>(p, s);
+  switch (k.tpr) {
+    case 32: return k.nv == 1 ? backward<DT, 32, 1>(p, s) : backward<DT, 32, 2>(p, s);
+    case 64: return backward<DT, 64, 2>(p, s);
+    case 128: return backward<DT, 128, 2>(p, s);
+    case 256: return backward<DT, 256, 2>(p, s);
+    default: return backward<DT, 512, 2>(p, s);
+  }
 }
 
 }  // namespace
