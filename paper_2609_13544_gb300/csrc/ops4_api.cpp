@@ -299,13 +299,14 @@ peat_status_t rmsnorm(peat_handle_t h, const void* x, int64_t ldx, const void* r
   p.values = values;
   p.ldv = ldv;
   p.rstd = rstd;
-  p.grid = vec(x, ldx, rows, B) && (!residual || vec(residual, ldr, rows, B));
   p.vec_w = aligned(weight, 16);
-  p.vec_s = vec(sum, lds, rows, B);
-  p.vec_y = vec(y, ldy, rows, B);
-  p.vec_q = aligned(q, E) && (ldq % E == 0 || rows <= 1);
-  p.vec_v = vec(values, ldv, rows, B);
-  cudaError_t e = peat::launch_rmsnorm(dtype, p, st);
+  p.vec_s = !sum || vec(sum, lds, rows, B);
+  p.vec_y = !y || vec(y, ldy, rows, B);
+  p.vec_q = !q || (aligned(q, E) && (ldq % E == 0 || rows <= 1));
+  p.vec_v = !values || vec(values, ldv, rows, B);
+  p.grid = cols % E == 0 && vec(x, ldx, rows, B) && (!residual || vec(residual, ldr, rows, B)) && p.vec_w && p.vec_s && p.vec_y &&
+           p.vec_q && p.vec_v;
+  cudaError_t e = peat::launch_rmsnorm(dtype, p, h->nsm, st);
   return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "norm launch");
 }
 
@@ -352,9 +353,10 @@ peat_status_t rmsnorm_backward(peat_handle_t h, const void* grad, int64_t ldg, c
   p.grad_weight = grad_weight;
   p.parts = static_cast<float*>(s->norm);
   p.dots = reinterpret_cast<float*>(static_cast<char*>(s->norm) + at);
-  p.grid = vec(grad, ldg, rows, B) && vec(x, ldx, rows, B) && (!grad_sum || vec(grad_sum, ldr, rows, B));
   p.vec_w = aligned(weight, 16);
-  p.vec_o = vec(grad_x, ldo, rows, B);
+  p.vec_o = !grad_x || vec(grad_x, ldo, rows, B);
+  p.grid = cols % (16 / B) == 0 && vec(grad, ldg, rows, B) && vec(x, ldx, rows, B) && (!grad_sum || vec(grad_sum, ldr, rows, B)) &&
+           p.vec_w && p.vec_o;
   cudaError_t e = peat::launch_rmsnorm_backward(dtype, plan, p, st);
   return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "norm gradient launch");
 }

@@ -202,10 +202,10 @@ struct RmsParams {
   void* values;  // or null
   int64_t ldv;
   float* rstd;  // or null
-  int grid;     // x's and residual's rows start on 16-byte boundaries
-  int vec_w, vec_s, vec_y, vec_q, vec_v;  // the others'
+  int grid;     // all matrices' rows start on 16-byte boundaries and are whole vectors
+  int vec_w, vec_s, vec_y, vec_q, vec_v;  // each output's rows and the weight start on them
 };
-cudaError_t launch_rmsnorm(int dtype, const RmsParams& p, cudaStream_t s);
+cudaError_t launch_rmsnorm(int dtype, const RmsParams& p, int nsm, cudaStream_t s);
 struct RmsBackParams {
   const void* grad;
   int64_t ldg;

@@ -13,6 +13,7 @@
 // reductions; the gradients of the weights are summed in registers over a CTA's
 // rows, then over the CTAs in a fixed order.
 #include <algorithm>
+#include <type_traits>
 
 #include "matrix_vec.cuh"
 #include "ops_internal.h"
@@ -68,10 +69,21 @@ __device__ __forceinline__ float sum_plain(float x, float* part) {
   }
   return x;
 }
+// GRID: every matrix's rows start on 16-byte boundaries and are whole vectors
 template <int DT, bool GRID>
 __device__ __forceinline__ uint4 load_vec(const Source<DT, GRID>& s, const typename Elem<DT>::T* p, int64_t left) {
+  if constexpr (GRID) return left > 0 ? s.load(p) : make_uint4(0, 0, 0, 0);
   if (s.whole(p, left)) return s.load(p);
   return left > 0 ? load_edge<DT>(p, left) : make_uint4(0, 0, 0, 0);
+}
+template <int DT, bool GRID>
+__device__ __forceinline__ void put_vec(typename Elem<DT>::T* o, const float (&y)[Elem<DT>::E], bool on_grid, int64_t left) {
+  if constexpr (GRID) {
+    if (left > 0) __stcs(reinterpret_cast<uint4*>(o), pack<DT>(y));
+  } else {
+    uint4 none = make_uint4(0, 0, 0, 0);
+    store_values<DT, 32>(o, y, on_grid, left, none, true, true);
+  }
 }
 // a vector of a matrix that this kernel has written (the thread's own elements)
 template <int DT>
@@ -88,17 +100,19 @@ __device__ __forceinline__ uint4 load_own(const typename Elem<DT>::T* p, int64_t
   return v.u;
 }
 // E weights from column col on
-template <int DT>
+template <int DT, bool GRID>
 __device__ __forceinline__ void weights(const void* w, int f32, bool vec, int64_t col, int64_t cols, float (&x)[Elem<DT>::E]) {
   constexpr int E = Elem<DT>::E;
+  const int64_t left = cols - col;
   if (DT != PEAT_F32 && !f32) {
     const typename Elem<DT>::T* p = static_cast<const typename Elem<DT>::T*>(w) + col;
-    const int64_t left = cols - col;
-    unpack<DT>(vec && left >= E ? __ldg(reinterpret_cast<const uint4*>(p)) : left > 0 ? load_edge<DT>(p, left) : make_uint4(0, 0, 0, 0), x);
+    unpack<DT>((GRID ? left > 0 : vec && left >= E) ? __ldg(reinterpret_cast<const uint4*>(p))
+               : !GRID && left > 0                  ? load_edge<DT>(p, left)
+                                                    : make_uint4(0, 0, 0, 0), x);
     return;
   }
   const float* p = static_cast<const float*>(w) + col;
-  if (vec && col + E <= cols) {
+  if (GRID ? left > 0 : vec && left >= E) {
 #pragma unroll
     for (int e = 0; e < E; e += 4) {
       const float4 f = __ldg(reinterpret_cast<const float4*>(p + e));
@@ -106,223 +120,235 @@ __device__ __forceinline__ void weights(const void* w, int f32, bool vec, int64_
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < E; e++) x[e] = col + e < cols ? __ldg(p + e) : 0.0f;
+    for (int e = 0; e < E; e++) x[e] = !GRID && e < left ? __ldg(p + e) : 0.0f;
   }
 }
 
 // ---- forward ------------------------------------------------------------------
-// TPR threads have a row, NV vectors each; LONG: rows that these do not hold, read
-// again for each of the three passes.
+// TPR threads have a row, NV vectors each, one row after another; the next row's
+// loads are under way while this one's factors are found.  LONG: rows that these
+// threads do not hold, read again for each of the three passes.
 template <int DT, int TPR, int NV, bool GRID, bool LONG>
-__global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 4) rms_forward(RmsParams p) {
+__global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) rms_forward(RmsParams p) {
   using L = Elem<DT>;
   using T = typename L::T;
-  constexpr int E = L::E, QT = threads_of<TPR>();
+  using Col = std::conditional_t<LONG, int64_t, int>;
+  constexpr int E = L::E, QT = threads_of<TPR>(), GROUPS = QT / TPR;
   constexpr int64_t PIECE = (int64_t)TPR * NV * E;
-  __shared__ float2 sums[QT / 32], found[QT / TPR], factor[QT / TPR];
+  constexpr int WARPS = TPR / 32;
+  __shared__ float2 sums[QT / 32], found[GROUPS], factor[GROUPS];
   __shared__ double wide[QT / 32];
   __shared__ uint32_t tops[QT / 32];
   pdl_wait();
   pdl_trigger();
-  const int64_t row = (int64_t)blockIdx.x * (QT / TPR) + threadIdx.x / TPR;
-  const int lane = threadIdx.x % TPR;
-  const bool live = row < p.rows;
-  const int64_t cols = live ? p.cols : 0, end = LONG ? p.cols : 1;
+  const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
+  const Col end = LONG ? (Col)p.cols : 1;
   const Source<DT, GRID> sx(p.x, p.rows, p.cols, p.ldx), sr(p.residual, p.rows, p.cols, p.ldr);
-  const T* x = static_cast<const T*>(p.x) + row * p.ldx;
-  const T* res = p.residual ? static_cast<const T*>(p.residual) + row * p.ldr : nullptr;
-  T* sum = p.sum ? static_cast<T*>(p.sum) + row * p.lds : nullptr;
-  uint4 s[NV];
-  auto column = [&](int64_t at, int i) { return at + (int64_t)(i * TPR + lane) * E; };
-  auto load = [&](int64_t at) {  // s = x + residual, rounded to the type
-    uint4 u[NV];
+  const bool round = p.q || p.values || p.scale;
+  uint4 s[NV], u[NV];
+  auto column = [&](Col at, int i) { return at + (i * TPR + lane) * E; };
+  auto fetch = [&](int64_t row, Col at) {
+    const Col cols = row < p.rows ? (Col)p.cols : 0;
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx;
 #pragma unroll
-    for (int i = 0; i < NV; i++) s[i] = load_vec(sx, x + column(at, i), cols - column(at, i));
-    if (!res) return;
+    for (int i = 0; i < NV; i++) s[i] = load_vec<DT, GRID>(sx, x + column(at, i), cols - column(at, i));
+    if (!p.residual) return;
+    const T* r = static_cast<const T*>(p.residual) + row * p.ldr;
 #pragma unroll
-    for (int i = 0; i < NV; i++) u[i] = load_vec(sr, res + column(at, i), cols - column(at, i));
+    for (int i = 0; i < NV; i++) u[i] = load_vec<DT, GRID>(sr, r + column(at, i), cols - column(at, i));
+  };
+  auto added = [&](uint4 (&v)[NV]) {  // s = x + residual, rounded to the type
 #pragma unroll
     for (int i = 0; i < NV; i++) {
+      v[i] = s[i];
+      if (!p.residual) continue;
       float a[E], b[E];
       unpack<DT>(s[i], a);
       unpack<DT>(u[i], b);
 #pragma unroll
       for (int e = 0; e < E; e++) a[e] = __fadd_rn(a[e], b[e]);
-      s[i] = pack<DT>(a);
+      v[i] = pack<DT>(a);
     }
   };
-  auto again = [&](int64_t at) {  // of a long row: from where the first pass left it
-    if (!LONG) return;
-    if (!sum) return load(at);
-#pragma unroll
-    for (int i = 0; i < NV; i++) s[i] = load_own<DT>(sum + column(at, i), cols - column(at, i), p.vec_s);
-  };
-
-  float hi = 0.0f, lo = 0.0f;
-  for (int64_t at = 0; at < end; at += PIECE) {
-    load(at);
-    // Squares on top of one that none exceeds: what a sum's rounding leaves of a
-    // square is then the difference of two sums away (Dekker's short form)
-    uint4 m = make_uint4(0, 0, 0, 0);
-#pragma unroll
-    for (int i = 0; i < NV; i++) m = mag_max<DT>(m, s[i]);
-    const float most = L::mag(mag_fold<DT>(m)), base = __fmul_ru(most, most);
-    float t = base, rest = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-      float a[E];
-      unpack<DT>(s[i], a);
-      if (sum) {
-        uint4 none = make_uint4(0, 0, 0, 0);
-        store_values<DT, 32>(sum + column(at, i), a, p.vec_s, live ? cols - column(at, i) : -16, none, true, true);
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  if (!LONG) fetch((int64_t)blockIdx.x * GROUPS + group, 0);
+  for (int64_t row0 = (int64_t)blockIdx.x * GROUPS; row0 < p.rows; row0 += step) {
+    const int64_t row = row0 + group;
+    const bool live = row < p.rows;
+    const Col cols = live ? (Col)p.cols : 0;
+    T* sum = p.sum ? static_cast<T*>(p.sum) + row * p.lds : nullptr;
+    uint4 v[NV];
+    auto again = [&](Col at) {  // a piece of a long row, from where the first pass left it
+      if (!LONG) return;
+      if (!sum) {
+        fetch(row, at);
+        added(v);
+        return;
       }
 #pragma unroll
-      for (int e = 0; e < E; e++) {
-        const float u = __fmaf_rn(a[e], a[e], t);
-        rest = __fadd_rn(rest, __fmaf_rn(a[e], a[e], __fsub_rn(t, u)));
-        t = u;
-      }
-    }
-    lo = __fadd_rn(lo, rest);
-    if (LONG) {
-      add_kept(hi, lo, t);
-      add_kept(hi, lo, -base);
-    } else {
-      hi = t;
-      add_kept(hi, lo, -base);
-    }
-  }
-  lanes_kept<32>(hi, lo);
-  // One warp adds up the warps' sums and finds the row's factor for all: the
-  // divisions would be a quarter of every thread's instructions.
-  if (TPR > 32) {
-    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = make_float2(hi, lo);
-    __syncthreads();
-  }
-  constexpr int WARPS = TPR / 32, FIRST = TPR > 32 ? 32 : TPR;
-  bool fine = true;
-  float rstd = 0.0f;
-  if (lane < FIRST) {
-    if (TPR > 32) {
-      const float2 f = sums[threadIdx.x / TPR * WARPS + (lane & (WARPS - 1))];
-      hi = f.x, lo = f.y;
-      lanes_kept<WARPS>(hi, lo);
-    }
-    // (hi + lo) / n, rounded once: the quotient and what it leaves
-    const float n = (float)(int)p.cols, quotient = __fdiv_rn(hi, n);
-    const float v = __fadd_rn(quotient, __fdiv_rn(__fadd_rn(__fmaf_rn(-quotient, n, hi), lo), n));
-    fine = (hi < 0x1p126f && hi > 0x1p-70f && p.cols < (1 << 24)) || !live;
-    rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(v, p.eps)));
-    if (TPR > 32 && lane == 0) found[threadIdx.x / TPR] = make_float2(rstd, fine ? 1.0f : 0.0f);
-  }
-  bool wide_row = !fine;  // of the whole CTA where it meets at barriers
-  if (TPR > 32) {
-    __syncthreads();
-    const float2 f = found[threadIdx.x / TPR];
-    rstd = f.x;
-    fine = f.y != 0.0f;
-    wide_row = false;
+      for (int i = 0; i < NV; i++) v[i] = load_own<DT>(sum + column(at, i), cols - column(at, i), p.vec_s);
+    };
+    float hi = 0.0f, lo = 0.0f;
+    for (Col at = 0; at < end; at += (Col)PIECE) {
+      if (LONG) fetch(row, at);
+      added(v);
+      if (!LONG && row0 + step < p.rows) fetch(row + step, 0);
+      // Squares on top of one that none exceeds: what a sum's rounding leaves of a
+      // square is then the difference of two sums away (Dekker's short form)
+      uint4 m = make_uint4(0, 0, 0, 0);
 #pragma unroll
-    for (int g = 0; g < QT / TPR; g++) wide_row |= found[g].y == 0.0f;
-  }
-  if (wide_row) {
-    double t = 0.0;
-    for (int64_t at = 0; at < end; at += PIECE) {
-      again(at);
+      for (int i = 0; i < NV; i++) m = mag_max<DT>(m, v[i]);
+      const float most = L::mag(mag_fold<DT>(m)), base = __fmul_ru(most, most);
+      float t = base, rest = 0.0f;
 #pragma unroll
       for (int i = 0; i < NV; i++) {
         float a[E];
-        unpack<DT>(s[i], a);
+        unpack<DT>(v[i], a);
+        if (sum) put_vec<DT, GRID>(sum + column(at, i), a, p.vec_s, live ? cols - column(at, i) : -16);
 #pragma unroll
-        for (int e = 0; e < E; e++)
-          if (a[e] != 0.0f) t += (double)a[e] * (double)a[e];
-      }
-    }
-    t = sum_wide<TPR>(t, wide);
-    if (!fine) rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn((float)(t / (double)p.cols), p.eps)));
-  }
-  if (p.rstd && lane == 0 && live) p.rstd[row] = rstd;
-  const bool round = p.q || p.values || p.scale;
-  if (!p.y && !round) return;
-
-  float y[NV][E];
-  auto normed = [&](int64_t at) {
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-      float w[E];
-      weights<DT>(p.weight, p.weight_f32, p.vec_w, column(at, i), p.cols, w);
-      unpack<DT>(s[i], y[i]);
-#pragma unroll
-      for (int e = 0; e < E; e++) y[i][e] = __fmul_rn(__fmul_rn(y[i][e], rstd), w[e]);
-    }
-  };
-  float r = 0.0f, scale = 0.0f;
-  if (round) {
-    // (beyond the row's end y is 0, or NaN where all of the row is)
-    uint32_t top = 0;
-    for (int64_t at = 0; at < end; at += PIECE) {
-      again(at);
-      normed(at);
-#pragma unroll
-      for (int i = 0; i < NV; i++)
-#pragma unroll
-        for (int e = 0; e < E; e++) top = max_f32(top, __float_as_uint(y[i][e]));
-    }
-    top = __reduce_max_sync(0xffffffffu, top & 0x7fffffffu);
-    if (TPR > 32) {
-      if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
-      __syncthreads();
-    }
-    if (lane < FIRST) {
-      if (TPR > 32) top = __reduce_max_sync(0xffffffffu, tops[threadIdx.x / TPR * WARPS + (lane & (WARPS - 1))]);
-      factors<PEAT_F32>(top, r, scale);
-      if (p.scale && lane == 0 && live) p.scale[row] = scale;
-      if (TPR > 32 && lane == 0) factor[threadIdx.x / TPR] = make_float2(r, scale);
-    }
-    if (TPR > 32) {
-      __syncthreads();
-      r = factor[threadIdx.x / TPR].x;
-      scale = factor[threadIdx.x / TPR].y;
-    }
-  }
-  const bool finite = scale == scale;
-  for (int64_t at = 0; at < end; at += PIECE) {
-    if (LONG || !round) {
-      again(at);
-      normed(at);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; i++) {
-      const int64_t col = column(at, i), left = live ? p.cols - col : -16;
-      uint4 none = make_uint4(0, 0, 0, 0);
-      if (p.y) store_values<DT, 32>(static_cast<T*>(p.y) + row * p.ldy + col, y[i], p.vec_y, left, none, true, true);
-      if (!p.q && !p.values) continue;
-      float w[E];
-      if (finite) {
-#pragma unroll
-        for (int e = 0; e < E; e++) w[e] = whole(y[i][e], r, true);
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; e++) w[e] = MAGIC;
-      }
-      if (p.q) {
-        int8_t* q = p.q + row * p.ldq + col;
-        if (p.vec_q && left >= E) {
-          if (E == 8)
-            *reinterpret_cast<uint2*>(q) = make_uint2(pack4(w[0], w[1], w[2], w[3]), pack4(w[4 % E], w[5 % E], w[6 % E], w[7 % E]));
-          else
-            *reinterpret_cast<uint32_t*>(q) = pack4(w[0], w[1], w[2], w[3]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < E; e++)
-            if (e < left) q[e] = byte_of(w[e]);
+        for (int e = 0; e < E; e++) {
+          const float w = __fmaf_rn(a[e], a[e], t);
+          rest = __fadd_rn(rest, __fmaf_rn(a[e], a[e], __fsub_rn(t, w)));
+          t = w;
         }
       }
-      if (p.values) {
-        float z[E];
+      lo = __fadd_rn(lo, rest);
+      if (LONG) {
+        add_kept(hi, lo, t);
+        add_kept(hi, lo, -base);
+      } else {
+        hi = t;
+        add_kept(hi, lo, -base);
+      }
+    }
+    lanes_kept<32>(hi, lo);
+    // One warp adds up the warps' sums and finds the row's factor for all: the
+    // divisions would be a quarter of every thread's instructions.
+    if (TPR > 32) {
+      if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = make_float2(hi, lo);
+      __syncthreads();
+    }
+    bool fine = true;
+    float rstd = 0.0f;
+    if (lane < 32) {
+      if (TPR > 32) {
+        const float2 f = sums[group * WARPS + (lane & (WARPS - 1))];
+        hi = f.x, lo = f.y;
+        lanes_kept<WARPS>(hi, lo);
+      }
+      // (hi + lo) / n, rounded once: the quotient and what it leaves
+      const float n = (float)(int)p.cols, quotient = __fdiv_rn(hi, n);
+      const float mean = __fadd_rn(quotient, __fdiv_rn(__fadd_rn(__fmaf_rn(-quotient, n, hi), lo), n));
+      fine = (hi < 0x1p126f && hi > 0x1p-70f && p.cols < (1 << 24)) || !live;
+      rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(mean, p.eps)));
+      if (TPR > 32 && lane == 0) found[group] = make_float2(rstd, fine ? 1.0f : 0.0f);
+    }
+    bool widely = !fine;  // by the whole CTA where it meets at barriers
+    if (TPR > 32) {
+      __syncthreads();
+      rstd = found[group].x;
+      fine = found[group].y != 0.0f;
+      widely = false;
 #pragma unroll
-        for (int e = 0; e < E; e++) z[e] = __fmul_rn(number(w[e]), scale);
-        store_values<DT, 32>(static_cast<T*>(p.values) + row * p.ldv + col, z, p.vec_v, left, none, true, true);
+      for (int g = 0; g < GROUPS; g++) widely |= found[g].y == 0.0f;
+    }
+    if (widely) {
+      double t = 0.0;
+      for (Col at = 0; at < end; at += (Col)PIECE) {
+        again(at);
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+          float a[E];
+          unpack<DT>(v[i], a);
+#pragma unroll
+          for (int e = 0; e < E; e++)
+            if (a[e] != 0.0f) t += (double)a[e] * (double)a[e];
+        }
+      }
+      t = sum_wide<TPR>(t, wide);
+      if (!fine) rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn((float)(t / (double)p.cols), p.eps)));
+    }
+    if (p.rstd && lane == 0 && live) p.rstd[row] = rstd;
+    if (!p.y && !round) continue;
+
+    float y[NV][E];
+    auto normed = [&](Col at) {
+#pragma unroll
+      for (int i = 0; i < NV; i++) {
+        float w[E];
+        weights<DT, GRID>(p.weight, p.weight_f32, p.vec_w, column(at, i), p.cols, w);
+        unpack<DT>(v[i], y[i]);
+#pragma unroll
+        for (int e = 0; e < E; e++) y[i][e] = __fmul_rn(__fmul_rn(y[i][e], rstd), w[e]);
+      }
+    };
+    float r = 0.0f, scale = 0.0f;
+    if (round) {
+      // (beyond the row's end y is 0, or NaN where all of the row is)
+      uint32_t top = 0;
+      for (Col at = 0; at < end; at += (Col)PIECE) {
+        again(at);
+        normed(at);
+#pragma unroll
+        for (int i = 0; i < NV; i++)
+#pragma unroll
+          for (int e = 0; e < E; e++) top = max_f32(top, __float_as_uint(y[i][e]));
+      }
+      top = __reduce_max_sync(0xffffffffu, top & 0x7fffffffu);
+      if (TPR > 32) {
+        if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+        __syncthreads();
+      }
+      if (lane < 32) {
+        if (TPR > 32) top = __reduce_max_sync(0xffffffffu, tops[group * WARPS + (lane & (WARPS - 1))]);
+        factors<PEAT_F32>(top, r, scale);
+        if (p.scale && lane == 0 && live) p.scale[row] = scale;
+        if (TPR > 32 && lane == 0) factor[group] = make_float2(r, scale);
+      }
+      if (TPR > 32) {
+        __syncthreads();
+        r = factor[group].x;
+        scale = factor[group].y;
+      }
+    }
+    const bool finite = scale == scale;
+    for (Col at = 0; at < end; at += (Col)PIECE) {
+      if (LONG || !round) {
+        again(at);
+        normed(at);
+      }
+#pragma unroll
+      for (int i = 0; i < NV; i++) {
+        const Col col = column(at, i), left = live ? (Col)p.cols - col : -16;
+        if (p.y) put_vec<DT, GRID>(static_cast<T*>(p.y) + row * p.ldy + col, y[i], p.vec_y, left);
+        if (!p.q && !p.values) continue;
+        float w[E];
+        if (finite) {
+#pragma unroll
+          for (int e = 0; e < E; e++) w[e] = whole(y[i][e], r, true);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; e++) w[e] = MAGIC;
+        }
+        if (p.q) {
+          int8_t* q = p.q + row * p.ldq + col;
+          if (GRID ? left > 0 : p.vec_q && left >= E) {
+            if (E == 8)
+              *reinterpret_cast<uint2*>(q) = make_uint2(pack4(w[0], w[1], w[2], w[3]), pack4(w[4 % E], w[5 % E], w[6 % E], w[7 % E]));
+            else
+              *reinterpret_cast<uint32_t*>(q) = pack4(w[0], w[1], w[2], w[3]);
+          } else if (!GRID) {
+#pragma unroll
+            for (int e = 0; e < E; e++)
+              if (e < left) q[e] = byte_of(w[e]);
+          }
+        }
+        if (p.values) {
+          float z[E];
+#pragma unroll
+          for (int e = 0; e < E; e++) z[e] = __fmul_rn(number(w[e]), scale);
+          put_vec<DT, GRID>(static_cast<T*>(p.values) + row * p.ldv + col, z, p.vec_v, left);
+        }
       }
     }
   }
@@ -331,13 +357,15 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 4) 
 // ---- backward -----------------------------------------------------------------
 //   n = s rstd, g = grad weight, c = sum (g n) / cols,
 //   grad_x = rstd (g - n c) + stream, grad_weight = sum over rows of grad n
-// A CTA has `each` rows for each of its groups of TPR threads, one after another; a
-// thread keeps its columns' sums over them.  LONG: the CTAs of blockIdx.y have a
-// piece of the columns, and c is there already (rms_dots).
+// A CTA has `each` rows for each of its groups of TPR threads, one after another,
+// the next one's loads under way; a thread keeps its columns' weights and sums.
+// LONG: the CTAs of blockIdx.y have a piece of the columns, and c is there already
+// (rms_dots).  Beyond a row's end grad, x and weight are 0.
 template <int DT, int TPR, int NV, bool GRID, bool LONG>
-__global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) rms_backward(RmsBackParams p) {
+__global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_backward(RmsBackParams p) {
   using L = Elem<DT>;
   using T = typename L::T;
+  using Col = std::conditional_t<LONG, int64_t, int>;
   constexpr int E = L::E, QT = threads_of<TPR>(), GROUPS = QT / TPR;
   __shared__ float dots[2][QT / 32];
   __shared__ float met[GROUPS > 1 ? TPR * NV * E : 1];
@@ -345,44 +373,54 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
   pdl_trigger();
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float n_cols = (float)(int)p.cols;
-  const int64_t at = LONG ? (int64_t)blockIdx.y * TPR * NV * E : 0;
+  const Col at = LONG ? (Col)blockIdx.y * (TPR * NV * E) : 0;
   const int64_t row0 = ((int64_t)blockIdx.x * GROUPS + group) * p.each;
   const Source<DT, GRID> sg(p.grad, p.rows, p.cols, p.ldg), sx(p.x, p.rows, p.cols, p.ldx), st(p.stream, p.rows, p.cols, p.ldr);
-  auto column = [&](int i) { return at + (int64_t)(i * TPR + lane) * E; };
-  float dw[NV][E];
+  auto column = [&](int i) { return at + (i * TPR + lane) * E; };
+  float dw[NV][E], w[NV][E];
 #pragma unroll
-  for (int i = 0; i < NV; i++)
+  for (int i = 0; i < NV; i++) {
+    weights<DT, GRID>(p.weight, p.weight_f32, p.vec_w, column(i), p.cols, w[i]);
 #pragma unroll
     for (int e = 0; e < E; e++) dw[i][e] = 0.0f;
+  }
+  uint4 d[NV], s[NV], u[NV];
+  float rstd_next;
+  auto fetch = [&](int64_t row) {
+    const Col cols = row < p.rows ? (Col)p.cols : 0;
+    const T* dp = static_cast<const T*>(p.grad) + row * p.ldg;
+    const T* xp = static_cast<const T*>(p.x) + row * p.ldx;
+    rstd_next = row < p.rows ? __ldg(p.rstd + row) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      d[i] = load_vec<DT, GRID>(sg, dp + column(i), cols - column(i));
+      s[i] = load_vec<DT, GRID>(sx, xp + column(i), cols - column(i));
+    }
+    if (!p.stream || !p.grad_x) return;
+    const T* tp = static_cast<const T*>(p.stream) + row * p.ldr;
+#pragma unroll
+    for (int i = 0; i < NV; i++) u[i] = load_vec<DT, GRID>(st, tp + column(i), cols - column(i));
+  };
+  fetch(row0);
   for (int64_t it = 0; it < p.each; it++) {
     const int64_t row = row0 + it;
     const bool live = row < p.rows;
-    const int64_t cols = live ? p.cols : 0;
-    const float rstd = live ? __ldg(p.rstd + row) : 0.0f;
-    uint4 d[NV], s[NV], u[NV];
-    const T* dp = static_cast<const T*>(p.grad) + row * p.ldg;
-    const T* xp = static_cast<const T*>(p.x) + row * p.ldx;
+    const float rstd = rstd_next;
+    uint4 dv[NV], sv[NV], uv[NV];
 #pragma unroll
-    for (int i = 0; i < NV; i++) {
-      d[i] = load_vec(sg, dp + column(i), cols - column(i));
-      s[i] = load_vec(sx, xp + column(i), cols - column(i));
-    }
-    if (p.stream && p.grad_x)
-#pragma unroll
-      for (int i = 0; i < NV; i++)
-        u[i] = load_vec(st, static_cast<const T*>(p.stream) + row * p.ldr + column(i), cols - column(i));
+    for (int i = 0; i < NV; i++) dv[i] = d[i], sv[i] = s[i], uv[i] = u[i];
+    if (it + 1 < p.each) fetch(row + 1);
     float c = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-      float a[E], b[E], w[E];
-      unpack<DT>(d[i], a);
-      unpack<DT>(s[i], b);
-      if (!LONG) weights<DT>(p.weight, p.weight_f32, p.vec_w, column(i), p.cols, w);
+      float a[E], b[E];
+      unpack<DT>(dv[i], a);
+      unpack<DT>(sv[i], b);
 #pragma unroll
       for (int e = 0; e < E; e++) {
         const float n = __fmul_rn(b[e], rstd);
         dw[i][e] = __fmaf_rn(a[e], n, dw[i][e]);
-        if (!LONG) c = __fmaf_rn(__fmul_rn(a[e], w[e]), n, c);
+        if (!LONG) c = __fmaf_rn(__fmul_rn(a[e], w[i][e]), n, c);
       }
     }
     if (!p.grad_x) continue;
@@ -390,20 +428,17 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
     else c = sum_plain<TPR>(c, dots[it & 1]) / n_cols;
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-      float a[E], b[E], w[E], t[E];
-      unpack<DT>(d[i], a);
-      unpack<DT>(s[i], b);
-      weights<DT>(p.weight, p.weight_f32, p.vec_w, column(i), p.cols, w);
+      float a[E], b[E], t[E];
+      unpack<DT>(dv[i], a);
+      unpack<DT>(sv[i], b);
 #pragma unroll
-      for (int e = 0; e < E; e++) b[e] = __fmul_rn(rstd, __fmaf_rn(-__fmul_rn(b[e], rstd), c, __fmul_rn(a[e], w[e])));
+      for (int e = 0; e < E; e++) b[e] = __fmul_rn(rstd, __fmaf_rn(-__fmul_rn(b[e], rstd), c, __fmul_rn(a[e], w[i][e])));
       if (p.stream) {
-        unpack<DT>(u[i], t);
+        unpack<DT>(uv[i], t);
 #pragma unroll
         for (int e = 0; e < E; e++) b[e] = __fadd_rn(b[e], t[e]);
       }
-      uint4 none = make_uint4(0, 0, 0, 0);
-      store_values<DT, 32>(static_cast<T*>(p.grad_x) + row * p.ldo + column(i), b, p.vec_o, live ? cols - column(i) : -16, none,
-                           true, true);
+      put_vec<DT, GRID>(static_cast<T*>(p.grad_x) + row * p.ldo + column(i), b, p.vec_o, live ? (Col)p.cols - column(i) : -16);
     }
   }
   if (!p.grad_weight) return;
@@ -431,7 +466,6 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
       if (column(i) + e < p.cols) o[column(i) + e] = dw[i][e];
 }
 
-// (beyond a row's end grad, x and weight are 0)
 // sum (g n) / cols of each row, by a CTA
 template <int DT, bool GRID>
 __global__ void __launch_bounds__(256) rms_dots(RmsBackParams p) {
@@ -448,9 +482,9 @@ __global__ void __launch_bounds__(256) rms_dots(RmsBackParams p) {
   float c = 0.0f;
   for (int64_t col = (int64_t)threadIdx.x * E; col < p.cols; col += 256 * E) {
     float a[E], b[E], w[E];
-    unpack<DT>(load_vec(sg, dp + col, p.cols - col), a);
-    unpack<DT>(load_vec(sx, xp + col, p.cols - col), b);
-    weights<DT>(p.weight, p.weight_f32, p.vec_w, col, p.cols, w);
+    unpack<DT>(load_vec<DT, GRID>(sg, dp + col, p.cols - col), a);
+    unpack<DT>(load_vec<DT, GRID>(sx, xp + col, p.cols - col), b);
+    weights<DT, GRID>(p.weight, p.weight_f32, p.vec_w, col, p.cols, w);
     float part = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; e++) part = __fmaf_rn(__fmul_rn(a[e], w[e]), __fmul_rn(b[e], rstd), part);
@@ -480,23 +514,24 @@ __global__ void __launch_bounds__(256) rms_weight_sums(const float* parts, int c
 }
 
 template <int DT, int TPR, int NV, bool LONG = false>
-cudaError_t forward(const RmsParams& p, cudaStream_t s) {
+cudaError_t forward(const RmsParams& p, int nsm, cudaStream_t s) {
   constexpr int QT = threads_of<TPR>();
-  const unsigned grid = (unsigned)((p.rows + QT / TPR - 1) / (QT / TPR));
+  // as many CTAs as are at work at once
+  const unsigned grid = (unsigned)std::min<int64_t>((p.rows + QT / TPR - 1) / (QT / TPR), (int64_t)nsm * (TPR > 256 ? 2 : 3));
   if (p.grid) return launch_dependent(rms_forward<DT, TPR, NV, true, LONG>, grid, QT, 0, s, p);
   return launch_dependent(rms_forward<DT, TPR, NV, false, LONG>, grid, QT, 0, s, p);
 }
 template <int DT>
-cudaError_t forward_of(const RmsParams& p, cudaStream_t s) {
+cudaError_t forward_of(const RmsParams& p, int nsm, cudaStream_t s) {
   const int64_t vecs = (p.cols + Elem<DT>::E - 1) / Elem<DT>::E;
-  if (vecs <= 32) return forward<DT, 32, 1>(p, s);
-  if (vecs <= 64) return forward<DT, 32, 2>(p, s);
-  if (vecs <= 128) return forward<DT, 64, 2>(p, s);
-  if (vecs <= 256) return forward<DT, 128, 2>(p, s);
-  if (vecs <= 512) return forward<DT, 256, 2>(p, s);
-  if (vecs <= 1024) return forward<DT, 512, 2>(p, s);
-  if (vecs <= 2048) return forward<DT, 512, 4>(p, s);
-  return forward<DT, 512, 4, true>(p, s);
+  if (vecs <= 32) return forward<DT, 32, 1>(p, nsm, s);
+  if (vecs <= 64) return forward<DT, 32, 2>(p, nsm, s);
+  if (vecs <= 128) return forward<DT, 64, 2>(p, nsm, s);
+  if (vecs <= 256) return forward<DT, 128, 2>(p, nsm, s);
+  if (vecs <= 512) return forward<DT, 256, 2>(p, nsm, s);
+  if (vecs <= 1024) return forward<DT, 512, 2>(p, nsm, s);
+  if (vecs <= 2048) return forward<DT, 512, 4>(p, nsm, s);
+  return forward<DT, 512, 4, true>(p, nsm, s);
 }
 
 struct Shape {  // of the backward kernel
@@ -510,7 +545,7 @@ Shape shape_of(int64_t vecs) {
   if (vecs <= 256) return {128, 2, false};
   if (vecs <= 512) return {256, 2, false};
   if (vecs <= 1024) return {512, 2, false};
-  return {256, 4, true};
+  return {256, 2, true};
 }
 template <int DT, int TPR, int NV, bool LONG = false>
 cudaError_t backward(const RmsBackParams& p, cudaStream_t s) {
@@ -534,7 +569,7 @@ cudaError_t backward(const RmsBackParams& p, cudaStream_t s) {
 template <int DT>
 cudaError_t backward_of(const RmsBackParams& p, cudaStream_t s) {
   const Shape k = shape_of((p.cols + Elem<DT>::E - 1) / Elem<DT>::E);
-  if (k.longer) return backward<DT, 256, 4, true>(p, s);
+  if (k.longer) return backward<DT, 256, 2, true>(p, s);
   switch (k.tpr) {
     case 32: return k.nv == 1 ? backward<DT, 32, 1>(p, s) : backward<DT, 32, 2>(p, s);
     case 64: return backward<DT, 64, 2>(p, s);
@@ -546,11 +581,11 @@ cudaError_t backward_of(const RmsBackParams& p, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_rmsnorm(int dtype, const RmsParams& p, cudaStream_t s) {
+cudaError_t launch_rmsnorm(int dtype, const RmsParams& p, int nsm, cudaStream_t s) {
   switch (dtype) {
-    case PEAT_F32: return forward_of<PEAT_F32>(p, s);
-    case PEAT_F16: return forward_of<PEAT_F16>(p, s);
-    default: return forward_of<PEAT_BF16>(p, s);
+    case PEAT_F32: return forward_of<PEAT_F32>(p, nsm, s);
+    case PEAT_F16: return forward_of<PEAT_F16>(p, nsm, s);
+    default: return forward_of<PEAT_BF16>(p, nsm, s);
   }
 }
 
@@ -560,7 +595,7 @@ RmsBackPlan rms_back_plan(int dtype, int64_t rows, int64_t cols, int nsm) {
   const int64_t groups = std::max(256, k.tpr) / k.tpr;  // of a CTA
   // two CTAs an SM; a long row's pieces fill the SMs already where there are several
   const int64_t pieces = k.longer ? (cols + (int64_t)k.tpr * k.nv * e - 1) / ((int64_t)k.tpr * k.nv * e) : 1;
-  const int64_t most = std::max<int64_t>(1, 3 * (int64_t)nsm / pieces);
+  const int64_t most = std::max<int64_t>(1, 2 * (int64_t)nsm / pieces);
   RmsBackPlan r;
   r.longer = k.longer;
   r.each = std::max<int64_t>(1, (rows + most * groups - 1) / (most * groups));
