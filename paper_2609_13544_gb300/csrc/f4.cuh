@@ -85,27 +85,56 @@ __device__ __forceinline__ Row4 row4(float amax, bool finite) {
   if (!(t <= 3.402823466e38f)) return Row4{0.0f, 0.0f, true};  // amax 0, or too small for a finite t
   return Row4{t, __fdiv_rn(amax, F4_TOP), true};
 }
+// the reciprocals of the 8-bit floats by their bytes, of 0 and NaN 0: a look-up a
+// block in place of a division; all threads of the CTA
+constexpr int RECIPROCALS = 128;
+__device__ __forceinline__ void make_reciprocals(float* table) {
+  for (int i = threadIdx.x; i < RECIPROCALS; i += blockDim.x)
+    table[i] = i == 0 || i == RECIPROCALS - 1 ? 0.0f : __fdiv_rn(1.0f, e4m3_value((uint32_t)i));
+}
+// x / 6, rounded once, for x >= 2^-100: by the divisor's reciprocal in two parts
+// (Brisebarre, Muller and Raina 2004; checked for every such x up to 2^12)
+__device__ __forceinline__ float sixth(float x) {
+  constexpr float HI = 0x1.555556p-3f, LO = -0x1.555556p-28f;
+  return __fmaf_rn(x, HI, __fmul_rn(x, LO));
+}
 // amax: of the block (mxfp4: NaN or infinite where finite is not set)
 template <int FMT>
-__device__ __forceinline__ Block4 block4(float amax, bool finite, const Row4& row) {
+__device__ __forceinline__ Block4 block4(float amax, bool finite, const Row4& row, const float* reciprocals) {
   if (FMT == PEAT_MXFP4) {
-    if (!finite) return Block4{0.0f, __uint_as_float(0x7fc00000u), 255};
-    const int e = max((int)(__float_as_uint(amax) >> 23) - 129, -127);
-    return Block4{__uint_as_float((uint32_t)(127 - e) << 23),
-                  e > -127 ? __uint_as_float((uint32_t)(e + 127) << 23) : 0x1p-127f, (uint32_t)(e + 127)};
+    const int e = max((int)(__float_as_uint(amax) >> 23), 2);  // + 129
+    return finite ? Block4{__uint_as_float((uint32_t)(256 - e) << 23),
+                           e > 2 ? __uint_as_float((uint32_t)(e - 2) << 23) : 0x1p-127f, (uint32_t)(e - 2)}
+                  : Block4{0.0f, __uint_as_float(0x7fc00000u), 255};
   }
-  if (!row.finite) return Block4{0.0f, 0.0f, 0};
-  const uint32_t b = e4m3(__fdiv_rn(__fmul_rn(amax, row.t), 6.0f));
-  const float f = e4m3_value(b);
-  return Block4{b ? __fdiv_rn(1.0f, f) : 0.0f, f, b};
+  const uint32_t b = row.finite ? e4m3(sixth(__fmul_rn(amax, row.t))) : 0;
+  return Block4{reciprocals[b], 0.0f, b};
 }
 template <int FMT>
 __device__ __forceinline__ float scaled4(float x, const Row4& row, const Block4& b) {
   return FMT == PEAT_MXFP4 ? __fmul_rn(x, b.r) : __fmul_rn(__fmul_rn(x, row.t), b.r);
 }
+// whether a block's codes are those of its numbers, not zeros
 template <int FMT>
-__device__ __forceinline__ float value4(float code, const Row4& row, const Block4& b) {
-  return FMT == PEAT_MXFP4 ? __fmul_rn(code, b.f) : __fmul_rn(__fmul_rn(code, b.f), row.s);
+__device__ __forceinline__ bool coded(bool finite, const Block4& b) { return FMT == PEAT_MXFP4 ? finite : b.byte != 0; }
+// the values of four codes; nvfp4: a code times its block's scale fits binary16 exactly
+template <int FMT>
+__device__ __forceinline__ void decoded4(uint32_t c, const Row4& row, const Block4& b, float (&v)[4]) {
+  if (FMT == PEAT_MXFP4) {
+    values4(c, v);
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = __fmul_rn(v[i], b.f);
+    return;
+  }
+  uint32_t lo, hi, f;
+  asm("{\n .reg .b8 a, b;\n mov.b16 {a, b}, %3;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+      " cvt.rn.f16x2.e4m3x2 %2, %4;\n}"
+      : "=r"(lo), "=r"(hi), "=r"(f)
+      : "h"((uint16_t)c), "h"((uint16_t)(b.byte * 0x101u)));
+  const __half2 h = *reinterpret_cast<const __half2*>(&f);
+  const float2 x = __half22float2(__hmul2(*reinterpret_cast<const __half2*>(&lo), h));
+  const float2 y = __half22float2(__hmul2(*reinterpret_cast<const __half2*>(&hi), h));
+  v[0] = __fmul_rn(x.x, row.s), v[1] = __fmul_rn(x.y, row.s), v[2] = __fmul_rn(y.x, row.s), v[3] = __fmul_rn(y.y, row.s);
 }
 
 }  // namespace peat
