@@ -5,7 +5,7 @@
 // persistent over them.  A stage is 256 k: a 128-byte piece of every row, swizzled
 // by the copy, and the scales' tiles, which lie in memory as the instruction wants
 // them in tensor memory.  Warp roles: one thread issues the copies, one the moves
-// of scales and the matrix instructions, eight warps turn accumulators into
+// of scales and the matrix instructions, sixteen warps turn accumulators into
 // results while the other one fills.
 //
 // Few rows of a: the tile's 128 rows are b's (SWAP), so that the instruction
@@ -22,9 +22,9 @@ namespace {
 constexpr int SK = 256;                 // k of a stage
 constexpr int P_BYTES = 128 * SK / 2;   // its rows on the 128-row side
 constexpr int PS_BYTES = 2048, QS_BYTES = 4096;  // its scales: tiles of 64 k or more, of up to two blocks of 128 rows
-constexpr int EPI_WARPS = 8, COPY_WARP = EPI_WARPS, MMA_WARP = COPY_WARP + 1, THREADS = (MMA_WARP + 1) * 32;
+constexpr int PARTS = 4, EPI_WARPS = 4 * PARTS, COPY_WARP = EPI_WARPS, MMA_WARP = COPY_WARP + 1, THREADS = (MMA_WARP + 1) * 32;
 constexpr int MOST_BN = 192, MOST_STAGES = 8;
-constexpr int EDGE = MOST_BN / 2;       // columns of a warp
+constexpr int EDGE = MOST_BN / PARTS;   // columns of a warp
 constexpr int EPI_BYTES = EPI_WARPS * EDGE * 2 * 4, BARS = 256;
 constexpr int SMEM = 227 * 1024;
 // tensor memory: two accumulators, then two sets of scales
@@ -63,16 +63,13 @@ __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 // a tile of scales into four columns of tensor memory: 32 lanes of 16 bytes, the same for each quarter of the lanes
-__device__ __forceinline__ void scales_in(uint32_t col, uint32_t addr) {
-  const uint64_t d = (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+__device__ __forceinline__ void scales_in(uint32_t col, uint64_t d) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(col), "l"(d) : "memory");
 }
-// 128 rows by bn, 64 k: 4-bit values, a scale for 32 (mxfp4: two of the four bytes of a tile, from `which` on) or for 16
+// 128 rows by bn, 64 k: 4-bit values, a scale for 32 (mxfp4: two of the four bytes of a tile, from the byte on that the
+// instruction's descriptor names) or for 16
 template <int FMT>
-__device__ __forceinline__ void mma4(uint32_t d, uint64_t a, uint64_t b, uint32_t bn, uint32_t which, uint32_t sa, uint32_t sb,
-                                     bool accumulate) {
-  const uint32_t idesc = (1u << 7) | (1u << 10) | ((bn / 8) << 17) | ((FMT == PEAT_MXFP4 ? 1u : 0u) << 23) |
-                         ((128u / 16) << 24) | (which << 4) | (which << 29);
+__device__ __forceinline__ void mma4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool accumulate) {
   if (FMT == PEAT_MXFP4)
     asm volatile(
         "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
@@ -94,6 +91,14 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&v)[16]) {
       : "r"(addr));
 }
 
+// a ring's slot and the parity of its round
+struct Turn {
+  int s = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int n) {
+    if (++s == n) s = 0, phase ^= 1;
+  }
+};
 constexpr int GROUP = 8;
 struct Place4 {
   int64_t p0, q0;
@@ -114,6 +119,41 @@ __device__ __forceinline__ void put_one(void* out, int64_t at, float y) {
   else *o = __float2bfloat16_rn(y);
 }
 
+// 32 columns of the lane's row, not scaled, in whole sectors
+template <int OUT>
+__device__ __forceinline__ void put_sums(const OutPlace& p, float (&v)[32], const float* bias, int64_t row, int64_t col0, bool in) {
+  using T = typename Mm8Out<OUT>::T;
+  constexpr int B = (int)sizeof(T), E = 32 / B;
+  T* o = static_cast<T*>(p.out) + row * p.ldo + col0;
+  if (p.biased) {
+#pragma unroll
+    for (int c = 0; c < 32; c += 4) {
+      const float4 b = *reinterpret_cast<const float4*>(bias + c);
+      v[c] = __fadd_rn(v[c], b.x);
+      v[c + 1] = __fadd_rn(v[c + 1], b.y);
+      v[c + 2] = __fadd_rn(v[c + 2], b.z);
+      v[c + 3] = __fadd_rn(v[c + 3], b.w);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 32; c += E) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      if constexpr (OUT == PEAT_F32) {
+        w[i] = __float_as_uint(v[c + i]);
+      } else if constexpr (OUT == PEAT_BF16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[c + 2 * i], v[c + 2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      } else {
+        const __half2 h = __floats2half2_rn(v[c + 2 * i], v[c + 2 * i + 1]);
+        w[i] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+    }
+    if (in) store_sector(o + c, w);
+  }
+}
+
 template <int OUT, int FMT, bool SWAP>
 __global__ void __launch_bounds__(THREADS, 1)
     mm4_tc(Tc4Params p, const __grid_constant__ CUtensorMap mp, const __grid_constant__ CUtensorMap mq) {
@@ -125,9 +165,11 @@ __global__ void __launch_bounds__(THREADS, 1)
                  acc_empty = acc_full + 16, last = acc_empty + 16;
   volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(edges + EPI_BYTES + 8 * (2 * MOST_STAGES + 5));
   static_assert(8 * (2 * MOST_STAGES + 5) + 4 <= BARS, "the barriers fit");
+  constexpr int STEP = SWAP ? 16 : 32;  // columns of a chunk of results
   constexpr int TILE_K = F4<FMT>::BLOCK * 4, PER = SK / TILE_K;  // k of a tile of scales; tiles of a stage
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int units = p.pt * p.qt, nk = (p.steps + 3) / 4;
+  const uint32_t base = sptr(smem);
 
   if (threadIdx.x == 32) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mp) : "memory");
@@ -160,127 +202,175 @@ __global__ void __launch_bounds__(THREADS, 1)
   if (warp == COPY_WARP) {
     if (elect_one()) {
       pdl_wait();
-      int seq = 0;
+      Turn at;
+      int64_t seq = 0;
       for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
         const Place4 t = place_of(p, u);
         const int64_t pb = t.p0 >> 7, qb = t.q0 >> 7, q_end = min(t.q0 + bn, p.Q);
         const int qbs = (int)(((q_end - 1) >> 7) - qb) + 1;  // blocks of 128 rows that the tile's lie in
-        for (int k = 0; k < nk; k++, seq++) {
-          const int s = seq % p.stages;
-          if (!(ok = mbar_wait(empty + 8 * s, (seq / p.stages & 1) ^ 1, p.wait_limit))) break;
-          const uint32_t dst = sptr(smem + s * stage), bar = full + 8 * s, qd = dst + P_BYTES, sd = qd + bn * (SK / 2);
-          const uint32_t n = (uint32_t)min((int64_t)PER, p.tiles - (int64_t)k * PER) * SCALE_TILE;
+        const uint8_t* ps = p.ps + pb * p.tiles * SCALE_TILE;
+        const uint8_t* qs = p.qs + qb * p.tiles * SCALE_TILE;
+        int left = (int)p.tiles;
+        for (int k = 0; k < nk; k++, seq++, left -= PER, ps += PER * SCALE_TILE, qs += PER * SCALE_TILE) {
+          if (!(ok = mbar_wait(empty + 8 * at.s, at.phase ^ 1, p.wait_limit))) break;
+          const uint32_t dst = base + at.s * stage, bar = full + 8 * at.s, qd = dst + P_BYTES, sd = qd + bn * (SK / 2);
+          const uint32_t n = (uint32_t)min(PER, left) * SCALE_TILE;
           mbar_expect(bar, P_BYTES + bn * (SK / 2) + n * (1 + qbs));
           tma_rows(dst, &mp, k * (SK / 2), (int)t.p0, bar);
           tma_rows(qd, &mq, k * (SK / 2), (int)t.q0, bar);
-          bulk(sd, p.ps + (pb * p.tiles + (int64_t)k * PER) * SCALE_TILE, n, bar);
-          for (int i = 0; i < qbs; i++)
-            bulk(sd + PS_BYTES + i * (PER * SCALE_TILE), p.qs + ((qb + i) * p.tiles + (int64_t)k * PER) * SCALE_TILE, n, bar);
+          bulk(sd, ps, n, bar);
+          bulk(sd + PS_BYTES, qs, n, bar);
+          if (qbs > 1) bulk(sd + PS_BYTES + PER * SCALE_TILE, qs + p.tiles * SCALE_TILE, n, bar);
+          at.next(p.stages);
         }
       }
       // a stage's copies have landed when its instructions are done with it
       for (int j = 0; j < p.stages && j < seq; j++) {
-        const int q = seq - 1 - j;
-        mbar_wait(empty + 8 * (q % p.stages), q / p.stages & 1, END_LIMIT);
+        const int64_t q = seq - 1 - j;
+        mbar_wait(empty + 8 * (int)(q % p.stages), (uint32_t)(q / p.stages & 1), END_LIMIT);
       }
     }
   } else if (warp == MMA_WARP) {
     if (elect_one()) {
-      int seq = 0, i = 0;
-      for (int u = blockIdx.x; u < units && ok && nk; u += gridDim.x, i++) {
-        const Place4 t = place_of(p, u);
-        const int qbs = (int)(((min(t.q0 + bn, p.Q) - 1) >> 7) - (t.q0 >> 7)) + 1;
-        const uint32_t shift = (uint32_t)(t.q0 & 127) / 32;
-        if (!(ok = mbar_wait(acc_empty + 8 * (i & 1), (i / 2 & 1) ^ 1, p.wait_limit))) break;
-        const uint32_t d = tmem + (i & 1) * bn;
-        for (int k = 0; k < nk; k++, seq++) {
-          const int s = seq % p.stages;
-          if (!(ok = mbar_wait(full + 8 * s, seq / p.stages & 1, p.wait_limit))) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t base = sptr(smem + s * stage), qd = base + P_BYTES, sd = qd + bn * (SK / 2);
-          const uint32_t tp = tmem + AT_SCALES + (seq & 1) * SCALES, tq = tp + AT_QS;
-          const int here = min(4, p.steps - 4 * k);
+      // A stage's scales are moved while the stage before is multiplied.  (The loop is
+      // one thread's: what it does for an instruction has to fit into the one before.)
+      const int mine = units > (int)blockIdx.x ? (units - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+      int64_t total = (int64_t)mine * nk;
+      const uint64_t desc = block_desc(0), scale_desc = (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+      const uint32_t at_q = P_BYTES >> 4, at_s = (P_BYTES + bn * (SK / 2)) >> 4, tall = bn > 128;
+      const uint32_t idesc = (1u << 7) | (1u << 10) | ((bn / 8) << 17) | ((FMT == PEAT_MXFP4 ? 1u : 0u) << 23) | ((128u / 16) << 24);
+      Turn in, at;  // of the scales, of the instructions
+      uint32_t set = 0;
+      auto scales = [&]() {
+        if (!(ok = mbar_wait(full + 8 * in.s, in.phase, p.wait_limit))) return;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t sd = scale_desc + ((base + in.s * stage) >> 4) + at_s;
+        const uint32_t tp = tmem + AT_SCALES + set * SCALES, tq = tp + AT_QS;
 #pragma unroll
-          for (int j = 0; j < PER; j++) {
-            if (j * (4 / PER) >= here) break;
-            scales_in(tp + 4 * j, sd + j * SCALE_TILE);
-            for (int q = 0; q < qbs; q++) scales_in(tq + 8 * j + 4 * q, sd + PS_BYTES + (q * PER + j) * SCALE_TILE);
-          }
-          const uint64_t a = block_desc(base), b = block_desc(qd);
+        for (int j = 0; j < PER; j++) {
+          scales_in(tp + 4 * j, sd + j * (SCALE_TILE >> 4));
+          scales_in(tq + 8 * j, sd + ((PS_BYTES + j * SCALE_TILE) >> 4));
+          if (tall) scales_in(tq + 8 * j + 4, sd + ((PS_BYTES + (PER + j) * SCALE_TILE) >> 4));
+        }
+        in.next(p.stages);
+        set ^= 1;
+      };
+      uint32_t acc = 0, acc_phase = 1;
+      if (total) scales();
+      for (int u = blockIdx.x; u < units && ok && nk; u += gridDim.x) {
+        const uint32_t shift = (uint32_t)(place_of(p, u).q0 & 127) / 32;
+        if (!(ok = mbar_wait(acc_empty + 8 * acc, acc_phase, p.wait_limit))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem + acc * bn;
+        for (int k = 0; k < nk && ok; k++) {
+          const uint32_t tp = tmem + AT_SCALES + (set ^ 1) * SCALES, tq = tp + AT_QS + shift;
+          if (--total > 0) scales();
+          if (!ok) break;
+          const uint64_t a = desc + ((base + at.s * stage) >> 4), b = a + at_q;
+          const int here = p.steps - 4 * k;
 #pragma unroll
           for (int j = 0; j < 4; j++) {
             if (j >= here) break;
-            const int tile = j * PER / 4;
-            mma4<FMT>(d, a + 2 * j, b + 2 * j, bn, FMT == PEAT_MXFP4 ? 2 * (j & 1) : 0, tp + 4 * tile, tq + 8 * tile + shift,
-                      k + j > 0);
+            constexpr int TILE_STEPS = 4 / PER;
+            mma4<FMT>(d, a + 2 * j, b + 2 * j, idesc | (FMT == PEAT_MXFP4 ? (2u * (j & 1)) * 0x20000010u : 0u),
+                      tp + 4 * (j / TILE_STEPS), tq + 8 * (j / TILE_STEPS), k + j > 0);
           }
-          commit(empty + 8 * s);
-          if (k == nk - 1) commit(acc_full + 8 * (i & 1));
+          commit(empty + 8 * at.s);
+          at.next(p.stages);
         }
+        if (ok) commit(acc_full + 8 * acc);
+        acc ^= 1;
+        acc_phase ^= acc == 0;
       }
       // whatever was issued is done before the accumulators are given back
       commit(last);
       mbar_wait(last, 0, END_LIMIT);
     }
-  } else {  // results: a warp has 32 of the 128 rows and half of the columns
+  } else {  // results: a warp has 32 of the 128 rows, and every fourth chunk of columns
     pdl_wait();
     int i = 0;
-    const int half = warp >> 2, quarter = warp & 3;
-    constexpr int STEP = SWAP ? 16 : 32;
-    const int chunks = bn / STEP, c0 = half ? (chunks + 1) / 2 : 0, c1 = half ? chunks : (chunks + 1) / 2;
+    const int part = warp >> 2, quarter = warp & 3, chunks = bn / STEP;
     float* sq = reinterpret_cast<float*>(edges) + warp * (EDGE * 2);
     float* bias = sq + EDGE;
+    const bool scaled = p.sp || p.sq;
+    // scales and bias of a tile, fetched while the one before is at work
+    constexpr int MINE = EDGE / STEP;
+    float sq_next[MINE], bias_next[MINE], sp_next = 1.0f, row_bias_next = 0.0f;
+    auto fetch = [&](int u) {
+      if (u >= units) return;
+      const Place4 t = place_of(p, u);
+      const int64_t row = t.p0 + quarter * 32 + lane;
+      if (p.sp && row < p.P) sp_next = __ldcg(p.sp + row);
+      if (SWAP && p.bias && row < p.P) row_bias_next = __ldcg(p.bias + row);
+#pragma unroll
+      for (int k = 0; k < MINE; k++) {
+        const int64_t col = t.q0 + (part + PARTS * k) * STEP + lane;
+        const bool in = lane < STEP && part + PARTS * k < chunks && col < p.Q;
+        sq_next[k] = p.sq && in ? __ldcg(p.sq + col) : 1.0f;
+        bias_next[k] = !SWAP && p.bias && in ? __ldcg(p.bias + col) : 0.0f;
+      }
+    };
+    fetch(blockIdx.x);
     for (int u = blockIdx.x; u < units && ok; u += gridDim.x, i++) {
       const Place4 t = place_of(p, u);
-      const int64_t row0 = t.p0 + quarter * 32, row = row0 + lane, col0 = t.q0 + c0 * STEP;
+      const int64_t row0 = t.p0 + quarter * 32, row = row0 + lane;
+      const float sp = sp_next, row_bias = row_bias_next;
       __syncwarp();
-      for (int c = lane; c < (c1 - c0) * STEP; c += 32) {
-        const int64_t col = col0 + c;
-        sq[c] = p.sq && col < p.Q ? __ldcg(p.sq + col) : 1.0f;
-        if (!SWAP) bias[c] = p.bias && col < p.Q ? __ldcg(p.bias + col) : 0.0f;
-      }
-      const float sp = p.sp && row < p.P ? __ldcg(p.sp + row) : 1.0f;
-      const float row_bias = SWAP && p.bias && row < p.P ? __ldcg(p.bias + row) : 0.0f;
+#pragma unroll
+      for (int k = 0; k < MINE; k++)
+        if (lane < STEP) {
+          sq[k * STEP + lane] = sq_next[k];
+          if (!SWAP) bias[k * STEP + lane] = bias_next[k];
+        }
       __syncwarp();
+      fetch(u + gridDim.x);
       if (nk) {
         if (!(ok = warp_wait(acc_full + 8 * (i & 1), i / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
-      const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1) * bn + c0 * STEP;
+      const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1) * bn;
       const int rows = (int)max((int64_t)0, min((int64_t)32, p.P - row0));
-      uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      for (int c = c0; c < c1; c++) {
-        uint32_t v[STEP];
 #pragma unroll
-        for (int j = 0; j < STEP; j++) v[j] = 0;
+      for (int k = 0; k < MINE; k++) {
+        const int c = part + PARTS * k;
+        if (c >= chunks) break;
+        uint32_t v[STEP];
         if (nk) {
-          if constexpr (SWAP) tmem_load16(taddr + (c - c0) * STEP, v);
-          else tmem_load32(taddr + (c - c0) * STEP, v);
+          if constexpr (SWAP) tmem_load16(taddr + c * STEP, v);
+          else tmem_load32(taddr + c * STEP, v);
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+        } else {
+#pragma unroll
+          for (int j = 0; j < STEP; j++) v[j] = 0;
         }
-        if (c == c1 - 1) {
+        if (c + PARTS >= chunks) {
           asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
           __syncwarp();
           if (lane == 0) mbar_arrive(acc_empty + 8 * (i & 1));
         }
-        const int at = (c - c0) * STEP;
+        const int at = k * STEP;
+        const int64_t col0 = t.q0 + c * STEP;
         if constexpr (SWAP) {
 #pragma unroll
           for (int j = 0; j < STEP; j++) {
-            const int64_t m = col0 + at + j;
             float y = __uint_as_float(v[j]);
-            if (p.sp) y = __fmul_rn(y, __fmul_rn(sq[at + j], sp));
+            if (scaled) y = __fmul_rn(y, __fmul_rn(sq[at + j], sp));
             if (p.bias) y = __fadd_rn(y, row_bias);
-            if (m < p.Q && row < p.P) put_one<OUT>(p.out.out, m * p.out.ldo + row, y);
+            if (col0 + j < p.Q && row < p.P) put_one<OUT>(p.out.out, (col0 + j) * p.out.ldo + row, y);
           }
         } else {
           float f[32];
 #pragma unroll
           for (int j = 0; j < 32; j++) f[j] = __uint_as_float(v[j]);
-          put_columns<OUT>(p.out, f, sp, sq + at, bias + at, row0, rows, col0 + at, c == c0, c == c1 - 1, carry);
+          if (p.out.vec && !scaled && p.out.N - col0 >= 32) {  // no scales, whole sectors
+            put_sums<OUT>(p.out, f, bias + at, row, col0, lane < rows);
+          } else {
+            uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            put_columns<OUT>(p.out, f, sp, sq + at, bias + at, row0, rows, col0, true, true, carry);
+          }
         }
       }
-      if (c0 == c1) {
+      if (part >= chunks) {
         __syncwarp();
         if (lane == 0) mbar_arrive(acc_empty + 8 * (i & 1));
       }
