@@ -1,8 +1,9 @@
 // Products of 4-bit matrices on the fifth-generation tensor cores, which scale
 // each block of values by the bytes that go with it and add up in float32.
 //
-// A CTA makes tiles of 128 rows of one operand by `bn` rows of the other,
-// persistent over them.  A stage is 256 k: a 128-byte piece of every row, swizzled
+// A CTA makes tiles of 128 rows of one operand by `bn` rows of the other, or a pair
+// of CTAs tiles of 256 by `bn` (each holds 128 rows and half of the others), which
+// needs fewer bytes for an instruction; persistent over the tiles.  A stage is 256 k: a 128-byte piece of every row, swizzled
 // by the copy, and the scales' tiles, which lie in memory as the instruction wants
 // them in tensor memory.  Warp roles: one thread issues the copies, one the moves
 // of scales and the matrix instructions, sixteen warps turn accumulators into
@@ -10,11 +11,15 @@
 //
 // Few rows of a: the tile's 128 rows are b's (SWAP), so that the instruction
 // spends nothing on rows that a does not have.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
 #include "f4.cuh"
 #include "peat_internal.h"
 #include "tc_common.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace peat {
 namespace {
@@ -22,16 +27,21 @@ namespace {
 constexpr int SK = 256;                 // k of a stage
 constexpr int P_BYTES = 128 * SK / 2;   // its rows on the 128-row side
 constexpr int PS_BYTES = 2048, QS_BYTES = 4096;  // its scales: tiles of 64 k or more, of up to two blocks of 128 rows
-constexpr int PARTS = 4, EPI_WARPS = 4 * PARTS, COPY_WARP = EPI_WARPS, MMA_WARP = COPY_WARP + 1, THREADS = (MMA_WARP + 1) * 32;
 constexpr int MOST_BN = 192, MOST_STAGES = 8;
-constexpr int EDGE = MOST_BN / PARTS;   // columns of a warp
-constexpr int EPI_BYTES = EPI_WARPS * EDGE * 2 * 4, BARS = 256;
+// warps for results, by the CTAs that share a tile: they take its chunks of columns in turn
+template <int CG>
+struct Warps {
+  static constexpr int PARTS = CG == 2 ? 3 : 4, EPI = 4 * PARTS, COPY = EPI, MMA = COPY + 1, THREADS = (MMA + 1) * 32;
+  static constexpr int EDGE = MOST_BN / PARTS;  // columns of a warp
+};
+constexpr int EPI_BYTES = 12 * 64 * 2 * 4, BARS = 256;
+static_assert(EPI_BYTES == Warps<1>::EPI * Warps<1>::EDGE * 8 && EPI_BYTES == Warps<2>::EPI * Warps<2>::EDGE * 8, "scales and bias");
 constexpr int SMEM = 227 * 1024;
 // tensor memory: two accumulators, then two sets of scales
 constexpr int AT_SCALES = 2 * MOST_BN, SCALES = 48, AT_QS = 16;
 static_assert(AT_SCALES + 2 * SCALES <= 512, "tensor memory has 512 columns");
 
-constexpr int stage_bytes(int bn) { return P_BYTES + bn * (SK / 2) + PS_BYTES + QS_BYTES; }
+constexpr int stage_bytes(int rows) { return P_BYTES + rows * (SK / 2) + PS_BYTES + QS_BYTES; }
 
 struct Tc4Params {
   const uint8_t* ps;  // scales of the 128-row side and of the other
@@ -54,34 +64,46 @@ __device__ __forceinline__ void tma_rows(uint32_t dst, const CUtensorMap* map, i
       "l"(map), "r"(x), "r"(row), "r"(bar)
       : "memory");
 }
+// the same, its bytes counted on a barrier of the pair's even CTA
+__device__ __forceinline__ void tma_pair(uint32_t dst, const CUtensorMap* map, int x, int row, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, "
+      "%3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(row), "r"(bar)
+      : "memory");
+}
 __device__ __forceinline__ void bulk(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
                "r"(bytes), "r"(bar)
                : "memory");
 }
+// arrives on the barrier (of both CTAs of a pair) once the instructions issued so far are done
+template <int CG>
 __device__ __forceinline__ void commit(uint32_t bar) {
+  if (CG == 2) return commit_both(bar, 3);
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 // a tile of scales into four columns of tensor memory: 32 lanes of 16 bytes, the same for each quarter of the lanes
+// (of a pair: each CTA's own)
+template <int CG>
 __device__ __forceinline__ void scales_in(uint32_t col, uint64_t d) {
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(col), "l"(d) : "memory");
+  if (CG == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(col), "l"(d) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(col), "l"(d) : "memory");
 }
-// 128 rows by bn, 64 k: 4-bit values, a scale for 32 (mxfp4: two of the four bytes of a tile, from the byte on that the
-// instruction's descriptor names) or for 16
-template <int FMT>
+// 128 rows (of a pair: 256) by bn, 64 k: 4-bit values, a scale for 32 (mxfp4: two of the four bytes of a tile, from the
+// byte on that the instruction's descriptor names) or for 16
+template <int FMT, int CG>
 __device__ __forceinline__ void mma4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, bool accumulate) {
-  if (FMT == PEAT_MXFP4)
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)accumulate)
-        : "memory");
-  else
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)accumulate)
-        : "memory");
+#define PEAT_MMA4(GROUP, SCALES)                                                                                      \
+  asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %6, 0;\n tcgen05.mma.cta_group::" GROUP                            \
+               ".kind::mxf4nvf4.block_scale.scale_vec::" SCALES " [%0], %1, %2, %3, [%4], [%5], p;\n}" ::"r"(d),      \
+               "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"((uint32_t)accumulate)                                \
+               : "memory")
+  if constexpr (FMT == PEAT_MXFP4 && CG == 1) PEAT_MMA4("1", "2X");
+  if constexpr (FMT == PEAT_MXFP4 && CG == 2) PEAT_MMA4("2", "2X");
+  if constexpr (FMT == PEAT_NVFP4 && CG == 1) PEAT_MMA4("1", "4X");
+  if constexpr (FMT == PEAT_NVFP4 && CG == 2) PEAT_MMA4("2", "4X");
+#undef PEAT_MMA4
 }
 __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&v)[16]) {
   asm volatile(
@@ -103,12 +125,13 @@ constexpr int GROUP = 8;
 struct Place4 {
   int64_t p0, q0;
 };
+template <int CG>
 __device__ __forceinline__ Place4 place_of(const Tc4Params& p, int u) {
   // groups of GROUP tiles of P, column by column: the CTAs at work at any time share few rows of either
   const int64_t per = (int64_t)GROUP * p.qt;
   const int g = (int)(u / per), in = (int)(u - g * per), wide = min(GROUP, p.pt - g * GROUP);
   const int q = in / wide;
-  return Place4{(int64_t)(g * GROUP + in - q * wide) * 128, (int64_t)q * p.bn};
+  return Place4{(int64_t)(g * GROUP + in - q * wide) * (CG * 128), (int64_t)q * p.bn};
 }
 
 template <int OUT>
@@ -154,12 +177,20 @@ __device__ __forceinline__ void put_sums(const OutPlace& p, float (&v)[32], cons
   }
 }
 
-template <int OUT, int FMT, bool SWAP>
-__global__ void __launch_bounds__(THREADS, 1)
-    mm4_tc(Tc4Params p, const __grid_constant__ CUtensorMap mp, const __grid_constant__ CUtensorMap mq) {
+// mp, mq: the codes; sp, sq: the tiles of scales, where a pair copies them
+template <int OUT, int FMT, bool SWAP, int CG>
+__global__ void __launch_bounds__(Warps<CG>::THREADS, 1)
+    mm4_tc(Tc4Params p, const __grid_constant__ CUtensorMap mp, const __grid_constant__ CUtensorMap mq,
+           const __grid_constant__ CUtensorMap msp, const __grid_constant__ CUtensorMap msq) {
+  constexpr int PARTS = Warps<CG>::PARTS, EPI_WARPS = Warps<CG>::EPI, COPY_WARP = Warps<CG>::COPY, MMA_WARP = Warps<CG>::MMA,
+                EDGE = Warps<CG>::EDGE;
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  const int bn = p.bn, stage = stage_bytes(bn);
+  const int bn = p.bn, half = bn / CG, stage = stage_bytes(half);  // rows of the other operand: the tile's, this CTA's
+  // a pair's CTAs differ in their rank; the even one issues the instructions
+  uint32_t rank = 0;
+  if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int first = blockIdx.x / CG, apart = gridDim.x / CG;
   char* edges = smem + p.stages * stage;
   const uint32_t full = sptr(edges + EPI_BYTES), empty = full + 8 * MOST_STAGES, acc_full = empty + 8 * MOST_STAGES,
                  acc_empty = acc_full + 16, last = acc_empty + 16;
@@ -182,18 +213,25 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     for (int i = 0; i < 2; i++) {
       mbar_init(acc_full + 8 * i, 1);
-      mbar_init(acc_empty + 8 * i, EPI_WARPS);
+      mbar_init(acc_empty + 8 * i, CG * EPI_WARPS);
     }
     mbar_init(last, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == MMA_WARP) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sptr((const void*)tmem_at))
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (CG == 2) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sptr((const void*)tmem_at))
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sptr((const void*)tmem_at))
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  __syncthreads();
+  if (CG == 2) cg::this_cluster().sync();
+  else __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_at;
   pdl_trigger();
@@ -204,8 +242,8 @@ __global__ void __launch_bounds__(THREADS, 1)
       pdl_wait();
       Turn at;
       int64_t seq = 0;
-      for (int u = blockIdx.x; u < units && ok; u += gridDim.x) {
-        const Place4 t = place_of(p, u);
+      for (int u = first; u < units && ok; u += apart) {
+        const Place4 t = place_of<CG>(p, u);
         const int64_t pb = t.p0 >> 7, qb = t.q0 >> 7, q_end = min(t.q0 + bn, p.Q);
         const int qbs = (int)(((q_end - 1) >> 7) - qb) + 1;  // blocks of 128 rows that the tile's lie in
         const uint8_t* ps = p.ps + pb * p.tiles * SCALE_TILE;
@@ -213,7 +251,20 @@ __global__ void __launch_bounds__(THREADS, 1)
         int left = (int)p.tiles;
         for (int k = 0; k < nk; k++, seq++, left -= PER, ps += PER * SCALE_TILE, qs += PER * SCALE_TILE) {
           if (!(ok = mbar_wait(empty + 8 * at.s, at.phase ^ 1, p.wait_limit))) break;
-          const uint32_t dst = base + at.s * stage, bar = full + 8 * at.s, qd = dst + P_BYTES, sd = qd + bn * (SK / 2);
+          const uint32_t dst = base + at.s * stage, bar = full + 8 * at.s, qd = dst + P_BYTES, sd = qd + half * (SK / 2);
+          if constexpr (CG == 2) {  // all bytes of both CTAs count on the even one's barrier
+            const uint32_t even = mapa(bar, 0);
+            if (rank == 0) mbar_expect(bar, 2 * (P_BYTES + half * (SK / 2) + 3 * PER * SCALE_TILE));
+            tma_pair(dst, &mp, k * (SK / 2), (int)(t.p0 + rank * 128), even);
+            tma_pair(qd, &mq, k * (SK / 2), (int)(t.q0 + rank * half), even);
+            // (past a row's last tile lie the next row's, which no instruction takes; past all of them zeros)
+            const int64_t kt = (int64_t)k * PER;
+            tma_pair(sd, &msp, 0, (int)((pb + rank) * p.tiles + kt), even);
+            tma_pair(sd + PS_BYTES, &msq, 0, (int)(qb * p.tiles + kt), even);
+            tma_pair(sd + PS_BYTES + PER * SCALE_TILE, &msq, 0, (int)((qb + 1) * p.tiles + kt), even);
+            at.next(p.stages);
+            continue;
+          }
           const uint32_t n = (uint32_t)min(PER, left) * SCALE_TILE;
           mbar_expect(bar, P_BYTES + bn * (SK / 2) + n * (1 + qbs));
           tma_rows(dst, &mp, k * (SK / 2), (int)t.p0, bar);
@@ -231,14 +282,14 @@ __global__ void __launch_bounds__(THREADS, 1)
       }
     }
   } else if (warp == MMA_WARP) {
-    if (elect_one()) {
+    if (rank == 0 && elect_one()) {
       // A stage's scales are moved while the stage before is multiplied.  (The loop is
       // one thread's: what it does for an instruction has to fit into the one before.)
-      const int mine = units > (int)blockIdx.x ? (units - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+      const int mine = units > first ? (units - first + apart - 1) / apart : 0;
       int64_t total = (int64_t)mine * nk;
       const uint64_t desc = block_desc(0), scale_desc = (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
-      const uint32_t at_q = P_BYTES >> 4, at_s = (P_BYTES + bn * (SK / 2)) >> 4, tall = bn > 128;
-      const uint32_t idesc = (1u << 7) | (1u << 10) | ((bn / 8) << 17) | ((FMT == PEAT_MXFP4 ? 1u : 0u) << 23) | ((128u / 16) << 24);
+      const uint32_t at_q = P_BYTES >> 4, at_s = (P_BYTES + half * (SK / 2)) >> 4, tall = CG == 2 || bn > 128;
+      const uint32_t idesc = (1u << 7) | (1u << 10) | ((bn / 8) << 17) | ((FMT == PEAT_MXFP4 ? 1u : 0u) << 23) | ((CG * 128u / 16) << 24);
       Turn in, at;  // of the scales, of the instructions
       uint32_t set = 0;
       auto scales = [&]() {
@@ -248,17 +299,17 @@ __global__ void __launch_bounds__(THREADS, 1)
         const uint32_t tp = tmem + AT_SCALES + set * SCALES, tq = tp + AT_QS;
 #pragma unroll
         for (int j = 0; j < PER; j++) {
-          scales_in(tp + 4 * j, sd + j * (SCALE_TILE >> 4));
-          scales_in(tq + 8 * j, sd + ((PS_BYTES + j * SCALE_TILE) >> 4));
-          if (tall) scales_in(tq + 8 * j + 4, sd + ((PS_BYTES + (PER + j) * SCALE_TILE) >> 4));
+          scales_in<CG>(tp + 4 * j, sd + j * (SCALE_TILE >> 4));
+          scales_in<CG>(tq + 8 * j, sd + ((PS_BYTES + j * SCALE_TILE) >> 4));
+          if (tall) scales_in<CG>(tq + 8 * j + 4, sd + ((PS_BYTES + (PER + j) * SCALE_TILE) >> 4));
         }
         in.next(p.stages);
         set ^= 1;
       };
       uint32_t acc = 0, acc_phase = 1;
       if (total) scales();
-      for (int u = blockIdx.x; u < units && ok && nk; u += gridDim.x) {
-        const uint32_t shift = (uint32_t)(place_of(p, u).q0 & 127) / 32;
+      for (int u = first; u < units && ok && nk; u += apart) {
+        const uint32_t shift = (uint32_t)(place_of<CG>(p, u).q0 & 127) / 32;
         if (!(ok = mbar_wait(acc_empty + 8 * acc, acc_phase, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + acc * bn;
@@ -272,18 +323,18 @@ __global__ void __launch_bounds__(THREADS, 1)
           for (int j = 0; j < 4; j++) {
             if (j >= here) break;
             constexpr int TILE_STEPS = 4 / PER;
-            mma4<FMT>(d, a + 2 * j, b + 2 * j, idesc | (FMT == PEAT_MXFP4 ? (2u * (j & 1)) * 0x20000010u : 0u),
+            mma4<FMT, CG>(d, a + 2 * j, b + 2 * j, idesc | (FMT == PEAT_MXFP4 ? (2u * (j & 1)) * 0x20000010u : 0u),
                       tp + 4 * (j / TILE_STEPS), tq + 8 * (j / TILE_STEPS), k + j > 0);
           }
-          commit(empty + 8 * at.s);
+          commit<CG>(empty + 8 * at.s);
           at.next(p.stages);
         }
-        if (ok) commit(acc_full + 8 * acc);
+        if (ok) commit<CG>(acc_full + 8 * acc);
         acc ^= 1;
         acc_phase ^= acc == 0;
       }
       // whatever was issued is done before the accumulators are given back
-      commit(last);
+      commit<CG>(last);
       mbar_wait(last, 0, END_LIMIT);
     }
   } else {  // results: a warp has 32 of the 128 rows, and every fourth chunk of columns
@@ -298,8 +349,8 @@ __global__ void __launch_bounds__(THREADS, 1)
     float sq_next[MINE], bias_next[MINE], sp_next = 1.0f, row_bias_next = 0.0f;
     auto fetch = [&](int u) {
       if (u >= units) return;
-      const Place4 t = place_of(p, u);
-      const int64_t row = t.p0 + quarter * 32 + lane;
+      const Place4 t = place_of<CG>(p, u);
+      const int64_t row = t.p0 + rank * 128 + quarter * 32 + lane;
       if (p.sp && row < p.P) sp_next = __ldcg(p.sp + row);
       if (SWAP && p.bias && row < p.P) row_bias_next = __ldcg(p.bias + row);
 #pragma unroll
@@ -310,10 +361,18 @@ __global__ void __launch_bounds__(THREADS, 1)
         bias_next[k] = !SWAP && p.bias && in ? __ldcg(p.bias + col) : 0.0f;
       }
     };
-    fetch(blockIdx.x);
-    for (int u = blockIdx.x; u < units && ok; u += gridDim.x, i++) {
-      const Place4 t = place_of(p, u);
-      const int64_t row0 = t.p0 + quarter * 32, row = row0 + lane;
+    const uint32_t release = CG == 2 ? mapa(acc_empty, 0) : acc_empty;
+    auto released = [&](int b) {
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane) return;
+      if (CG == 2) mbar_arrive_cluster(release + 8 * b);
+      else mbar_arrive(release + 8 * b);
+    };
+    fetch(first);
+    for (int u = first; u < units && ok; u += apart, i++) {
+      const Place4 t = place_of<CG>(p, u);
+      const int64_t row0 = t.p0 + rank * 128 + quarter * 32, row = row0 + lane;
       const float sp = sp_next, row_bias = row_bias_next;
       __syncwarp();
 #pragma unroll
@@ -323,7 +382,7 @@ __global__ void __launch_bounds__(THREADS, 1)
           if (!SWAP) bias[k * STEP + lane] = bias_next[k];
         }
       __syncwarp();
-      fetch(u + gridDim.x);
+      fetch(u + apart);
       if (nk) {
         if (!(ok = warp_wait(acc_full + 8 * (i & 1), i / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -343,11 +402,7 @@ __global__ void __launch_bounds__(THREADS, 1)
 #pragma unroll
           for (int j = 0; j < STEP; j++) v[j] = 0;
         }
-        if (c + PARTS >= chunks) {
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(acc_empty + 8 * (i & 1));
-        }
+        if (c + PARTS >= chunks) released(i & 1);
         const int at = k * STEP;
         const int64_t col0 = t.q0 + c * STEP;
         if constexpr (SWAP) {
@@ -370,18 +425,24 @@ __global__ void __launch_bounds__(THREADS, 1)
           }
         }
       }
-      if (part >= chunks) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(acc_empty + 8 * (i & 1));
-      }
+      if (part >= chunks) released(i & 1);
     }
   }
   __syncwarp();
   if (!ok) atomicOr_system(p.status, 1u);
+  __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  __syncthreads();
+  if (CG == 2) cg::this_cluster().sync();
+  else __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  if (CG == 2) {
+    // (the last arrival in the odd CTA's shared memory, before it goes)
+    if (warp == MMA_WARP && rank) warp_wait(last, 0, END_LIMIT);
+    __syncwarp();
+    if (warp == MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  } else if (warp == MMA_WARP) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
 }
 
 // rows of codes; a box is 128 bytes of `box` rows, swizzled
@@ -396,24 +457,74 @@ bool rows_map(CUtensorMap* m, const uint8_t* base, int64_t rows, int64_t bytes, 
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int OUT, int FMT, bool SWAP>
-cudaError_t launch(const Tc4Params& p, const CUtensorMap& mp, const CUtensorMap& mq, int nsm, cudaStream_t s) {
+// tiles of scales, `per` of them a box
+bool scales_map(CUtensorMap* m, const uint8_t* base, int64_t tiles, int per) {
+  EncodeFn f = encode_fn();
+  if (!f) return false;
+  const cuuint64_t dims[2] = {SCALE_TILE / 4, (cuuint64_t)tiles}, strides[1] = {SCALE_TILE};
+  const cuuint32_t size[2] = {SCALE_TILE / 4, (cuuint32_t)per}, elem[2] = {1, 1};
+  return f(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<uint8_t*>(base), dims, strides, size, elem,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Maps {
+  CUtensorMap p, q, sp, sq;
+};
+template <int OUT, int FMT, bool SWAP, int CG>
+cudaError_t launch(const Tc4Params& p, const Maps& m, int nsm, cudaStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  cudaError_t e = allow_smem(mm4_tc<OUT, FMT, SWAP>, SMEM, allowed);
+  cudaError_t e = allow_smem(mm4_tc<OUT, FMT, SWAP, CG>, SMEM, allowed);
   if (e != cudaSuccess) return e;
   const int64_t tiles = (int64_t)p.pt * p.qt;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = CG;
+  at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
   // (one CTA an SM, which has all of tensor memory)
-  return launch_dependent(mm4_tc<OUT, FMT, SWAP>, (unsigned)std::min<int64_t>(tiles, nsm), THREADS, SMEM, s, p, mp, mq);
+  cfg.gridDim = dim3((unsigned)(CG * std::min<int64_t>(tiles, nsm / CG)));
+  cfg.blockDim = dim3(Warps<CG>::THREADS);
+  cfg.dynamicSmemBytes = SMEM;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = CG == 2 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, mm4_tc<OUT, FMT, SWAP, CG>, p, m.p, m.q, m.sp, m.sq);
 }
+enum Kind { FEW, ONE, PAIR };  // few rows of a; tiles of a CTA; of a pair
 template <int OUT, int FMT>
-cudaError_t launch_side(bool swap, const Tc4Params& p, const CUtensorMap& mp, const CUtensorMap& mq, int nsm, cudaStream_t s) {
-  return swap ? launch<OUT, FMT, true>(p, mp, mq, nsm, s) : launch<OUT, FMT, false>(p, mp, mq, nsm, s);
+cudaError_t launch_kind(Kind kind, const Tc4Params& p, const Maps& m, int nsm, cudaStream_t s) {
+  if (kind == FEW) return launch<OUT, FMT, true, 1>(p, m, nsm, s);
+  return kind == ONE ? launch<OUT, FMT, false, 1>(p, m, nsm, s) : launch<OUT, FMT, false, 2>(p, m, nsm, s);
 }
 template <int OUT>
-cudaError_t launch_out(int format, bool swap, const Tc4Params& p, const CUtensorMap& mp, const CUtensorMap& mq, int nsm,
-                       cudaStream_t s) {
-  return format == PEAT_MXFP4 ? launch_side<OUT, PEAT_MXFP4>(swap, p, mp, mq, nsm, s)
-                              : launch_side<OUT, PEAT_NVFP4>(swap, p, mp, mq, nsm, s);
+cudaError_t launch_out(int format, Kind kind, const Tc4Params& p, const Maps& m, int nsm, cudaStream_t s) {
+  return format == PEAT_MXFP4 ? launch_kind<OUT, PEAT_MXFP4>(kind, p, m, nsm, s) : launch_kind<OUT, PEAT_NVFP4>(kind, p, m, nsm, s);
+}
+
+// How a product is cut into tiles: by the cycles of its waves, an instruction of 64
+// k and what each tile costs once.
+struct Cut {
+  Kind kind;
+  int bn;
+};
+Cut cut_of(int64_t M, int64_t N, int64_t steps, int nsm) {
+  if (M <= MOST_BN) return {FEW, (int)((M + 15) / 16 * 16)};
+  Cut best{ONE, 128};
+  double least = 0.0;
+  const struct {
+    Cut cut;
+    int cycles;
+  } ways[] = {{{ONE, 128}, 140}, {{PAIR, 128}, 100}, {{PAIR, 192}, 115}};
+  for (const auto& w : ways) {
+    const int64_t rows = w.cut.kind == PAIR ? 256 : 128, at_once = w.cut.kind == PAIR ? nsm / 2 : nsm;
+    const int64_t tiles = ((M + rows - 1) / rows) * ((N + w.cut.bn - 1) / w.cut.bn);
+    const double t = (double)((tiles + at_once - 1) / at_once) * (steps * w.cycles + 8.0 * w.cut.bn);
+    if (least == 0.0 || t < least) best = w.cut, least = t;
+  }
+  return best;
 }
 
 }  // namespace
@@ -421,8 +532,14 @@ cudaError_t launch_out(int format, bool swap, const Tc4Params& p, const CUtensor
 cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned int* status, unsigned int wait_limit, int nsm,
                        cudaStream_t s) {
   const int block = format == PEAT_MXFP4 ? 32 : 16;
-  const bool swap = m.M <= MOST_BN;
   Tc4Params p;
+  p.steps = (int)((m.K + 63) / 64);
+  Cut cut = cut_of(m.M, m.N, p.steps, nsm);
+  p.tiles = (m.K / block + 3) / 4;
+  // (a pair's copies count tiles of scales in 32 bits)
+  const int64_t tall = (std::max(m.M, m.N) + 127) / 128 * p.tiles;
+  if (cut.kind == PAIR && tall >= ((int64_t)1 << 31) - 1024 - 2 * p.tiles) cut = {ONE, 128};
+  const bool swap = cut.kind == FEW;
   p.ps = swap ? m.b_block_scale : m.a_block_scale;
   p.qs = swap ? m.a_block_scale : m.b_block_scale;
   p.sp = swap ? m.sb : m.sa;
@@ -430,25 +547,28 @@ cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned i
   p.bias = m.bias;
   p.P = swap ? m.N : m.M;
   p.Q = swap ? m.M : m.N;
-  p.tiles = (m.K / block + 3) / 4;
-  p.steps = (int)((m.K + 63) / 64);
-  p.bn = swap ? (int)((m.M + 15) / 16 * 16) : 128;
-  p.pt = (int)((p.P + 127) / 128);
+  p.bn = cut.bn;
+  const int cg = cut.kind == PAIR ? 2 : 1;
+  p.pt = (int)((p.P + 128 * cg - 1) / (128 * cg));
   p.qt = (int)((p.Q + p.bn - 1) / p.bn);
-  p.stages = std::min(MOST_STAGES, (SMEM - 1024 - EPI_BYTES - BARS) / stage_bytes(p.bn));
+  p.stages = std::min(MOST_STAGES, (SMEM - 1024 - EPI_BYTES - BARS) / stage_bytes(p.bn / cg));
   const int size = out_dtype == PEAT_F32 ? 4 : 2;
   p.out = OutPlace{m.out, m.ldo, m.N, m.bias != nullptr,
                    reinterpret_cast<uintptr_t>(m.out) % 32 == 0 && m.ldo * size % 32 == 0};
   p.status = status;
   p.wait_limit = wait_limit;
-  CUtensorMap mp = {}, mq = {};
-  if (m.K > 0 && (!rows_map(&mp, swap ? m.b : m.a, p.P, m.K / 2, swap ? m.ldb : m.lda, 128) ||
-                  !rows_map(&mq, swap ? m.a : m.b, p.Q, m.K / 2, swap ? m.lda : m.ldb, p.bn)))
+  Maps maps = {};
+  const int per = SK / (4 * block);
+  if (m.K > 0 && (!rows_map(&maps.p, swap ? m.b : m.a, p.P, m.K / 2, swap ? m.ldb : m.lda, 128) ||
+                  !rows_map(&maps.q, swap ? m.a : m.b, p.Q, m.K / 2, swap ? m.lda : m.ldb, p.bn / cg)))
+    return cudaErrorNotSupported;
+  if (m.K > 0 && cut.kind == PAIR && (!scales_map(&maps.sp, p.ps, (p.P + 127) / 128 * p.tiles, per) ||
+                                      !scales_map(&maps.sq, p.qs, (p.Q + 127) / 128 * p.tiles, per)))
     return cudaErrorNotSupported;
   switch (out_dtype) {
-    case PEAT_F32: return launch_out<PEAT_F32>(format, swap, p, mp, mq, nsm, s);
-    case PEAT_F16: return launch_out<PEAT_F16>(format, swap, p, mp, mq, nsm, s);
-    default: return launch_out<PEAT_BF16>(format, swap, p, mp, mq, nsm, s);
+    case PEAT_F32: return launch_out<PEAT_F32>(format, cut.kind, p, maps, nsm, s);
+    case PEAT_F16: return launch_out<PEAT_F16>(format, cut.kind, p, maps, nsm, s);
+    default: return launch_out<PEAT_BF16>(format, cut.kind, p, maps, nsm, s);
   }
 }
 
