@@ -28,14 +28,16 @@ constexpr int SK = 256;                 // k of a stage
 constexpr int P_BYTES = 128 * SK / 2;   // its rows on the 128-row side
 constexpr int PS_BYTES = 2048, QS_BYTES = 4096;  // its scales: tiles of 64 k or more, of up to two blocks of 128 rows
 constexpr int MOST_BN = 192, MOST_STAGES = 8;
-// warps for results, by the CTAs that share a tile: they take its chunks of columns in turn
-template <int CG>
+// Warps for results: they take a tile's chunks of columns in turn, 32 rows each.
+template <int CG, bool SWAP>
 struct Warps {
-  static constexpr int PARTS = CG == 2 ? 3 : 4, EPI = 4 * PARTS, COPY = EPI, MMA = COPY + 1, THREADS = (MMA + 1) * 32;
-  static constexpr int EDGE = MOST_BN / PARTS;  // columns of a warp
+  static constexpr int PARTS = SWAP ? 4 : (CG == 2 ? 3 : 2), EPI = 4 * PARTS, COPY = EPI, MMA = COPY + 1, THREADS = (MMA + 1) * 32;
+  static constexpr int STEP = SWAP ? 16 : 64;           // columns of a chunk
+  static constexpr int EDGE = SWAP ? MOST_BN / PARTS : STEP;  // columns of a warp
+  // a place where a warp's results wait for their copy out, and its columns' scales and bias
+  static constexpr int BOX = SWAP ? 0 : 4096, BYTES = EPI * (BOX + EDGE * 2 * 4);
 };
-constexpr int EPI_BYTES = 12 * 64 * 2 * 4, BARS = 256;
-static_assert(EPI_BYTES == Warps<1>::EPI * Warps<1>::EDGE * 8 && EPI_BYTES == Warps<2>::EPI * Warps<2>::EDGE * 8, "scales and bias");
+constexpr int BARS = 256;
 constexpr int SMEM = 227 * 1024;
 // tensor memory: two accumulators, then two sets of scales
 constexpr int AT_SCALES = 2 * MOST_BN, SCALES = 48, AT_QS = 16;
@@ -142,48 +144,58 @@ __device__ __forceinline__ void put_one(void* out, int64_t at, float y) {
   else *o = __float2bfloat16_rn(y);
 }
 
-// 32 columns of the lane's row, not scaled, in whole sectors
+// 16 bytes of results from v[c] on
 template <int OUT>
-__device__ __forceinline__ void put_sums(const OutPlace& p, float (&v)[32], const float* bias, int64_t row, int64_t col0, bool in) {
-  using T = typename Mm8Out<OUT>::T;
-  constexpr int B = (int)sizeof(T), E = 32 / B;
-  T* o = static_cast<T*>(p.out) + row * p.ldo + col0;
-  if (p.biased) {
+__device__ __forceinline__ uint4 packed(const float* v) {
+  if constexpr (OUT == PEAT_F32) return *reinterpret_cast<const uint4*>(v);
+  uint32_t w[4];
 #pragma unroll
-    for (int c = 0; c < 32; c += 4) {
-      const float4 b = *reinterpret_cast<const float4*>(bias + c);
-      v[c] = __fadd_rn(v[c], b.x);
-      v[c + 1] = __fadd_rn(v[c + 1], b.y);
-      v[c + 2] = __fadd_rn(v[c + 2], b.z);
-      v[c + 3] = __fadd_rn(v[c + 3], b.w);
+  for (int i = 0; i < 4; i++) {
+    if constexpr (OUT == PEAT_BF16) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    } else {
+      const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
   }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// 64 columns of a warp's 32 rows, a row a lane, through shared memory (128-byte
+// rows, swizzled) and out by copies of 32 rows, which write whole lines and leave
+// out what lies beyond the matrix.  (Sectors straight from the lanes, 32 rows a
+// store, took 1.3 us a tile of 128 x 128, twice its instructions' time.)
+template <int OUT>
+__device__ __forceinline__ void put_boxes(char* box, const CUtensorMap* map, float (&v)[64], int64_t row0, int64_t col0,
+                                          int64_t N) {
+  constexpr int B = (int)sizeof(typename Mm8Out<OUT>::T), COLS = 128 / B;
+  const int lane = threadIdx.x & 31;
+  const uint32_t at = sptr(box);
 #pragma unroll
-  for (int c = 0; c < 32; c += E) {
-    uint32_t w[8];
+  for (int c0 = 0; c0 < 64; c0 += COLS) {
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the place is free
+    __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-      if constexpr (OUT == PEAT_F32) {
-        w[i] = __float_as_uint(v[c + i]);
-      } else if constexpr (OUT == PEAT_BF16) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(v[c + 2 * i], v[c + 2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-      } else {
-        const __half2 h = __floats2half2_rn(v[c + 2 * i], v[c + 2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&h);
-      }
+    for (int c = 0; c < 8; c++)
+      *reinterpret_cast<uint4*>(box + lane * 128 + ((c ^ (lane & 7)) * 16)) = packed<OUT>(v + c0 + c * (16 / B));
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0 && col0 + c0 < N) {
+      asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map),
+                   "r"((int)(col0 + c0)), "r"((int)row0), "r"(at)
+                   : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
-    if (in) store_sector(o + c, w);
   }
 }
 
-// mp, mq: the codes; sp, sq: the tiles of scales, where a pair copies them
+// mp, mq: the codes; msp, msq: the tiles of scales, where a pair copies them; mo: out, where it can be copied to
 template <int OUT, int FMT, bool SWAP, int CG>
-__global__ void __launch_bounds__(Warps<CG>::THREADS, 1)
+__global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
     mm4_tc(Tc4Params p, const __grid_constant__ CUtensorMap mp, const __grid_constant__ CUtensorMap mq,
-           const __grid_constant__ CUtensorMap msp, const __grid_constant__ CUtensorMap msq) {
-  constexpr int PARTS = Warps<CG>::PARTS, EPI_WARPS = Warps<CG>::EPI, COPY_WARP = Warps<CG>::COPY, MMA_WARP = Warps<CG>::MMA,
-                EDGE = Warps<CG>::EDGE;
+           const __grid_constant__ CUtensorMap msp, const __grid_constant__ CUtensorMap msq, const __grid_constant__ CUtensorMap mo) {
+  using W = Warps<CG, SWAP>;
+  constexpr int PARTS = W::PARTS, EPI_WARPS = W::EPI, COPY_WARP = W::COPY, MMA_WARP = W::MMA, EDGE = W::EDGE, STEP = W::STEP;
   extern __shared__ char raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   const int bn = p.bn, half = bn / CG, stage = stage_bytes(half);  // rows of the other operand: the tile's, this CTA's
@@ -192,11 +204,10 @@ __global__ void __launch_bounds__(Warps<CG>::THREADS, 1)
   if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const int first = blockIdx.x / CG, apart = gridDim.x / CG;
   char* edges = smem + p.stages * stage;
-  const uint32_t full = sptr(edges + EPI_BYTES), empty = full + 8 * MOST_STAGES, acc_full = empty + 8 * MOST_STAGES,
+  const uint32_t full = sptr(edges + W::BYTES), empty = full + 8 * MOST_STAGES, acc_full = empty + 8 * MOST_STAGES,
                  acc_empty = acc_full + 16, last = acc_empty + 16;
-  volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(edges + EPI_BYTES + 8 * (2 * MOST_STAGES + 5));
+  volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(edges + W::BYTES + 8 * (2 * MOST_STAGES + 5));
   static_assert(8 * (2 * MOST_STAGES + 5) + 4 <= BARS, "the barriers fit");
-  constexpr int STEP = SWAP ? 16 : 32;  // columns of a chunk of results
   constexpr int TILE_K = F4<FMT>::BLOCK * 4, PER = SK / TILE_K;  // k of a tile of scales; tiles of a stage
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int units = p.pt * p.qt, nk = (p.steps + 3) / 4;
@@ -337,16 +348,18 @@ __global__ void __launch_bounds__(Warps<CG>::THREADS, 1)
       commit<CG>(last);
       mbar_wait(last, 0, END_LIMIT);
     }
-  } else {  // results: a warp has 32 of the 128 rows, and every fourth chunk of columns
+  } else {  // results: a warp has 32 of the 128 rows, and every PARTS-th chunk of columns
     pdl_wait();
     int i = 0;
     const int part = warp >> 2, quarter = warp & 3, chunks = bn / STEP;
-    float* sq = reinterpret_cast<float*>(edges) + warp * (EDGE * 2);
+    char* box = edges + warp * W::BOX;
+    float* sq = reinterpret_cast<float*>(edges + EPI_WARPS * W::BOX) + warp * (EDGE * 2);
     float* bias = sq + EDGE;
     const bool scaled = p.sp || p.sq;
     // scales and bias of a tile, fetched while the one before is at work
-    constexpr int MINE = EDGE / STEP;
-    float sq_next[MINE], bias_next[MINE], sp_next = 1.0f, row_bias_next = 0.0f;
+    constexpr int MINE = EDGE / STEP, KEPT = (EDGE + 31) / 32;
+    float sq_next[KEPT], bias_next[KEPT], sp_next = 1.0f, row_bias_next = 0.0f;
+    auto column = [&](int c) { return (part + PARTS * (c / STEP)) * STEP + c % STEP; };  // the warp's c-th, of the tile
     auto fetch = [&](int u) {
       if (u >= units) return;
       const Place4 t = place_of<CG>(p, u);
@@ -354,11 +367,11 @@ __global__ void __launch_bounds__(Warps<CG>::THREADS, 1)
       if (p.sp && row < p.P) sp_next = __ldcg(p.sp + row);
       if (SWAP && p.bias && row < p.P) row_bias_next = __ldcg(p.bias + row);
 #pragma unroll
-      for (int k = 0; k < MINE; k++) {
-        const int64_t col = t.q0 + (part + PARTS * k) * STEP + lane;
-        const bool in = lane < STEP && part + PARTS * k < chunks && col < p.Q;
-        sq_next[k] = p.sq && in ? __ldcg(p.sq + col) : 1.0f;
-        bias_next[k] = !SWAP && p.bias && in ? __ldcg(p.bias + col) : 0.0f;
+      for (int k = 0; k < KEPT; k++) {
+        const int c = k * 32 + lane;
+        const bool in = c < EDGE && column(c) < bn && t.q0 + column(c) < p.Q;
+        sq_next[k] = p.sq && in ? __ldcg(p.sq + t.q0 + column(c)) : 1.0f;
+        bias_next[k] = !SWAP && p.bias && in ? __ldcg(p.bias + t.q0 + column(c)) : 0.0f;
       }
     };
     const uint32_t release = CG == 2 ? mapa(acc_empty, 0) : acc_empty;
@@ -376,10 +389,10 @@ __global__ void __launch_bounds__(Warps<CG>::THREADS, 1)
       const float sp = sp_next, row_bias = row_bias_next;
       __syncwarp();
 #pragma unroll
-      for (int k = 0; k < MINE; k++)
-        if (lane < STEP) {
-          sq[k * STEP + lane] = sq_next[k];
-          if (!SWAP) bias[k * STEP + lane] = bias_next[k];
+      for (int k = 0; k < KEPT; k++)
+        if (k * 32 + lane < EDGE) {
+          sq[k * 32 + lane] = sq_next[k];
+          if (!SWAP) bias[k * 32 + lane] = bias_next[k];
         }
       __syncwarp();
       fetch(u + apart);
@@ -393,14 +406,18 @@ __global__ void __launch_bounds__(Warps<CG>::THREADS, 1)
       for (int k = 0; k < MINE; k++) {
         const int c = part + PARTS * k;
         if (c >= chunks) break;
-        uint32_t v[STEP];
+        float v[STEP];
         if (nk) {
-          if constexpr (SWAP) tmem_load16(taddr + c * STEP, v);
-          else tmem_load32(taddr + c * STEP, v);
+          if constexpr (SWAP) {
+            tmem_load16(taddr + c * STEP, reinterpret_cast<uint32_t(&)[16]>(v));
+          } else {
+            tmem_load32(taddr + c * STEP, reinterpret_cast<uint32_t(&)[32]>(v[0]));
+            tmem_load32(taddr + c * STEP + 32, reinterpret_cast<uint32_t(&)[32]>(v[32]));
+          }
           asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
         } else {
 #pragma unroll
-          for (int j = 0; j < STEP; j++) v[j] = 0;
+          for (int j = 0; j < STEP; j++) v[j] = 0.0f;
         }
         if (c + PARTS >= chunks) released(i & 1);
         const int at = k * STEP;
@@ -408,25 +425,47 @@ __global__ void __launch_bounds__(Warps<CG>::THREADS, 1)
         if constexpr (SWAP) {
 #pragma unroll
           for (int j = 0; j < STEP; j++) {
-            float y = __uint_as_float(v[j]);
+            float y = v[j];
             if (scaled) y = __fmul_rn(y, __fmul_rn(sq[at + j], sp));
             if (p.bias) y = __fadd_rn(y, row_bias);
             if (col0 + j < p.Q && row < p.P) put_one<OUT>(p.out.out, (col0 + j) * p.out.ldo + row, y);
           }
-        } else {
-          float f[32];
+        } else if (p.out.vec) {
+          if (row0 >= p.P) continue;
+          if (scaled) {
 #pragma unroll
-          for (int j = 0; j < 32; j++) f[j] = __uint_as_float(v[j]);
-          if (p.out.vec && !scaled && p.out.N - col0 >= 32) {  // no scales, whole sectors
-            put_sums<OUT>(p.out, f, bias + at, row, col0, lane < rows);
-          } else {
-            uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            put_columns<OUT>(p.out, f, sp, sq + at, bias + at, row0, rows, col0, true, true, carry);
+            for (int j = 0; j < STEP; j += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(sq + j);
+              v[j] = __fmul_rn(v[j], __fmul_rn(sp, f.x));
+              v[j + 1] = __fmul_rn(v[j + 1], __fmul_rn(sp, f.y));
+              v[j + 2] = __fmul_rn(v[j + 2], __fmul_rn(sp, f.z));
+              v[j + 3] = __fmul_rn(v[j + 3], __fmul_rn(sp, f.w));
+            }
           }
+          if (p.out.biased) {
+#pragma unroll
+            for (int j = 0; j < STEP; j += 4) {
+              const float4 f = *reinterpret_cast<const float4*>(bias + j);
+              v[j] = __fadd_rn(v[j], f.x);
+              v[j + 1] = __fadd_rn(v[j + 1], f.y);
+              v[j + 2] = __fadd_rn(v[j + 2], f.z);
+              v[j + 3] = __fadd_rn(v[j + 3], f.w);
+            }
+          }
+          put_boxes<OUT>(box, &mo, v, row0, col0, p.out.N);
+        } else {  // rows off the 16-byte grid
+          uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          const OutPlace off_grid{p.out.out, p.out.ldo, p.out.N, p.out.biased, false};
+#pragma unroll
+          for (int j = 0; j < STEP; j += 32)
+            put_columns<OUT>(off_grid, reinterpret_cast<const float(&)[32]>(v[j]), sp, sq + j, bias + j, row0, rows, col0 + j, j == 0,
+                             j + 32 == STEP, carry);
         }
       }
       if (part >= chunks) released(i & 1);
     }
+    // (the boxes are read before the CTA ends, and written before the next kernel reads them)
+    if (!SWAP && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   __syncwarp();
   if (!ok) atomicOr_system(p.status, 1u);
@@ -468,8 +507,22 @@ bool scales_map(CUtensorMap* m, const uint8_t* base, int64_t tiles, int per) {
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// results: boxes of 32 rows of 128 bytes, swizzled
+bool out_map(CUtensorMap* m, void* out, int64_t rows, int64_t cols, int64_t ld, int dtype) {
+  EncodeFn f = encode_fn();
+  if (!f) return false;
+  const int size = dtype == PEAT_F32 ? 4 : 2;
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(rows > 1 ? ld * size : (cols * size + 15) / 16 * 16)};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / size), 32}, elem[2] = {1, 1};
+  const CUtensorMapDataType type = dtype == PEAT_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == PEAT_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  return f(m, type, 2, out, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+           CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct Maps {
-  CUtensorMap p, q, sp, sq;
+  CUtensorMap p, q, sp, sq, out;
 };
 template <int OUT, int FMT, bool SWAP, int CG>
 cudaError_t launch(const Tc4Params& p, const Maps& m, int nsm, cudaStream_t s) {
@@ -486,12 +539,12 @@ cudaError_t launch(const Tc4Params& p, const Maps& m, int nsm, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   // (one CTA an SM, which has all of tensor memory)
   cfg.gridDim = dim3((unsigned)(CG * std::min<int64_t>(tiles, nsm / CG)));
-  cfg.blockDim = dim3(Warps<CG>::THREADS);
+  cfg.blockDim = dim3(Warps<CG, SWAP>::THREADS);
   cfg.dynamicSmemBytes = SMEM;
   cfg.stream = s;
   cfg.attrs = at;
   cfg.numAttrs = CG == 2 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, mm4_tc<OUT, FMT, SWAP, CG>, p, m.p, m.q, m.sp, m.sq);
+  return cudaLaunchKernelEx(&cfg, mm4_tc<OUT, FMT, SWAP, CG>, p, m.p, m.q, m.sp, m.sq, m.out);
 }
 enum Kind { FEW, ONE, PAIR };  // few rows of a; tiles of a CTA; of a pair
 template <int OUT, int FMT>
@@ -551,10 +604,11 @@ cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned i
   const int cg = cut.kind == PAIR ? 2 : 1;
   p.pt = (int)((p.P + 128 * cg - 1) / (128 * cg));
   p.qt = (int)((p.Q + p.bn - 1) / p.bn);
-  p.stages = std::min(MOST_STAGES, (SMEM - 1024 - EPI_BYTES - BARS) / stage_bytes(p.bn / cg));
+  const int results = swap ? Warps<1, true>::BYTES : (cg == 2 ? Warps<2, false>::BYTES : Warps<1, false>::BYTES);
+  p.stages = std::min(MOST_STAGES, (SMEM - 1024 - results - BARS) / stage_bytes(p.bn / cg));
   const int size = out_dtype == PEAT_F32 ? 4 : 2;
-  p.out = OutPlace{m.out, m.ldo, m.N, m.bias != nullptr,
-                   reinterpret_cast<uintptr_t>(m.out) % 32 == 0 && m.ldo * size % 32 == 0};
+  const bool grid = reinterpret_cast<uintptr_t>(m.out) % 16 == 0 && (m.ldo * size % 16 == 0 || m.M <= 1) && m.ldo * size < ((int64_t)1 << 40);
+  p.out = OutPlace{m.out, m.ldo, m.N, m.bias != nullptr, grid};
   p.status = status;
   p.wait_limit = wait_limit;
   Maps maps = {};
@@ -565,6 +619,7 @@ cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned i
   if (m.K > 0 && cut.kind == PAIR && (!scales_map(&maps.sp, p.ps, (p.P + 127) / 128 * p.tiles, per) ||
                                       !scales_map(&maps.sq, p.qs, (p.Q + 127) / 128 * p.tiles, per)))
     return cudaErrorNotSupported;
+  if (!swap && grid && !out_map(&maps.out, m.out, m.M, m.N, m.ldo, out_dtype)) return cudaErrorNotSupported;
   switch (out_dtype) {
     case PEAT_F32: return launch_out<PEAT_F32>(format, cut.kind, p, maps, nsm, s);
     case PEAT_F16: return launch_out<PEAT_F16>(format, cut.kind, p, maps, nsm, s);
