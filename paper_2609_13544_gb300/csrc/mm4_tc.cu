@@ -27,21 +27,25 @@ namespace {
 constexpr int SK = 256;                 // k of a stage
 constexpr int P_BYTES = 128 * SK / 2;   // its rows on the 128-row side
 constexpr int PS_BYTES = 2048, QS_BYTES = 4096;  // its scales: tiles of 64 k or more, of up to two blocks of 128 rows
-constexpr int MOST_BN = 192, MOST_STAGES = 8;
+constexpr int FEW_ROWS = 192, MOST_STAGES = 8;  // rows of a up to which the tile's 128 rows may be b's
 // Warps for results: they take a tile's chunks of columns in turn, 32 rows each.
 template <int CG, bool SWAP>
 struct Warps {
-  static constexpr int PARTS = SWAP ? 4 : (CG == 2 ? 3 : 2), EPI = 4 * PARTS, COPY = EPI, MMA = COPY + 1, THREADS = (MMA + 1) * 32;
+  static constexpr int PARTS = SWAP || CG == 2 ? 4 : 2, EPI = 4 * PARTS, COPY = EPI, MMA = COPY + 1, THREADS = (MMA + 1) * 32;
   static constexpr int STEP = SWAP ? 16 : 64;           // columns of a chunk
-  static constexpr int EDGE = SWAP ? MOST_BN / PARTS : STEP;  // columns of a warp
+  static constexpr int EDGE = SWAP ? FEW_ROWS / PARTS : STEP;  // columns of a warp
   // a place where a warp's results wait for their copy out, and its columns' scales and bias
   static constexpr int BOX = SWAP ? 0 : 4096, BYTES = EPI * (BOX + EDGE * 2 * 4);
 };
 constexpr int BARS = 256;
 constexpr int SMEM = 227 * 1024;
-// tensor memory: two accumulators, then two sets of scales
-constexpr int AT_SCALES = 2 * MOST_BN, SCALES = 48, AT_QS = 16;
-static_assert(AT_SCALES + 2 * SCALES <= 512, "tensor memory has 512 columns");
+// Tensor memory: two accumulators, then a stage's scales.  A pair's accumulators have
+// 256 columns and share 48 of them: the next tile's instructions wait until the warps
+// that have these have read them, not for the whole tile.
+template <int CG>
+struct Tmem {
+  static constexpr int APART = CG == 2 ? 208 : FEW_ROWS, SCALES = CG == 2 ? 464 : 2 * FEW_ROWS;
+};
 
 constexpr int stage_bytes(int rows) { return P_BYTES + rows * (SK / 2) + PS_BYTES + QS_BYTES; }
 
@@ -161,31 +165,53 @@ __device__ __forceinline__ uint4 packed(const float* v) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// 64 columns of a warp's 32 rows, a row a lane, through shared memory (128-byte
-// rows, swizzled) and out by copies of 32 rows, which write whole lines and leave
-// out what lies beyond the matrix.  (Sectors straight from the lanes, 32 rows a
-// store, took 1.3 us a tile of 128 x 128, twice its instructions' time.)
+// Half h of 64 columns of a warp's 32 rows, a row a lane, scaled and biased, through
+// shared memory (128-byte rows, swizzled) and out by copies of 32 rows, which write
+// whole lines and leave out what lies beyond the matrix.  (Sectors straight from the
+// lanes, 32 rows a store, took 1.3 us a tile of 128 x 128, twice its instructions'
+// time.)
 template <int OUT>
-__device__ __forceinline__ void put_boxes(char* box, const CUtensorMap* map, float (&v)[64], int64_t row0, int64_t col0,
-                                          int64_t N) {
-  constexpr int B = (int)sizeof(typename Mm8Out<OUT>::T), COLS = 128 / B;
+__device__ __forceinline__ void put_box(char* box, const CUtensorMap* map, float (&v)[32], int h, bool scaled, float sp,
+                                        const float* sq, bool biased, const float* bias, int64_t row0, int64_t col0, int64_t N) {
+  constexpr int B = (int)sizeof(typename Mm8Out<OUT>::T), HALVES = B == 2 ? 2 : 1;  // that a box holds
   const int lane = threadIdx.x & 31;
-  const uint32_t at = sptr(box);
+  if (scaled) {
 #pragma unroll
-  for (int c0 = 0; c0 < 64; c0 += COLS) {
+    for (int j = 0; j < 32; j += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(sq + 32 * h + j);
+      v[j] = __fmul_rn(v[j], __fmul_rn(sp, f.x));
+      v[j + 1] = __fmul_rn(v[j + 1], __fmul_rn(sp, f.y));
+      v[j + 2] = __fmul_rn(v[j + 2], __fmul_rn(sp, f.z));
+      v[j + 3] = __fmul_rn(v[j + 3], __fmul_rn(sp, f.w));
+    }
+  }
+  if (biased) {
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(bias + 32 * h + j);
+      v[j] = __fadd_rn(v[j], f.x);
+      v[j + 1] = __fadd_rn(v[j + 1], f.y);
+      v[j + 2] = __fadd_rn(v[j + 2], f.z);
+      v[j + 3] = __fadd_rn(v[j + 3], f.w);
+    }
+  }
+  if (h % HALVES == 0) {
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the place is free
     __syncwarp();
+  }
+  const int c0 = HALVES == 2 ? 4 * h : 0;
 #pragma unroll
-    for (int c = 0; c < 8; c++)
-      *reinterpret_cast<uint4*>(box + lane * 128 + ((c ^ (lane & 7)) * 16)) = packed<OUT>(v + c0 + c * (16 / B));
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncwarp();
-    if (lane == 0 && col0 + c0 < N) {
-      asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map),
-                   "r"((int)(col0 + c0)), "r"((int)row0), "r"(at)
-                   : "memory");
-      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-    }
+  for (int c = 0; c < 8 / HALVES; c++)
+    *reinterpret_cast<uint4*>(box + lane * 128 + (((c0 + c) ^ (lane & 7)) * 16)) = packed<OUT>(v + c * (16 / B));
+  if (h % HALVES != HALVES - 1) return;
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  const int64_t col = HALVES == 2 ? col0 : col0 + 32 * h;
+  if (lane == 0 && col < N) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"((int)col),
+                 "r"((int)row0), "r"(sptr(box))
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
 
@@ -205,9 +231,9 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
   const int first = blockIdx.x / CG, apart = gridDim.x / CG;
   char* edges = smem + p.stages * stage;
   const uint32_t full = sptr(edges + W::BYTES), empty = full + 8 * MOST_STAGES, acc_full = empty + 8 * MOST_STAGES,
-                 acc_empty = acc_full + 16, last = acc_empty + 16;
-  volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(edges + W::BYTES + 8 * (2 * MOST_STAGES + 5));
-  static_assert(8 * (2 * MOST_STAGES + 5) + 4 <= BARS, "the barriers fit");
+                 acc_empty = acc_full + 16, shared_empty = acc_empty + 16, last = shared_empty + 8;
+  volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(edges + W::BYTES + 8 * (2 * MOST_STAGES + 6));
+  static_assert(8 * (2 * MOST_STAGES + 6) + 4 <= BARS, "the barriers fit");
   constexpr int TILE_K = F4<FMT>::BLOCK * 4, PER = SK / TILE_K;  // k of a tile of scales; tiles of a stage
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int units = p.pt * p.qt, nk = (p.steps + 3) / 4;
@@ -226,6 +252,7 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
       mbar_init(acc_full + 8 * i, 1);
       mbar_init(acc_empty + 8 * i, CG * EPI_WARPS);
     }
+    mbar_init(shared_empty, CG * 4);  // the warps of one chunk of columns
     mbar_init(last, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -294,48 +321,40 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
     }
   } else if (warp == MMA_WARP) {
     if (rank == 0 && elect_one()) {
-      // A stage's scales are moved while the stage before is multiplied.  (The loop is
-      // one thread's: what it does for an instruction has to fit into the one before.)
-      const int mine = units > first ? (units - first + apart - 1) / apart : 0;
-      int64_t total = (int64_t)mine * nk;
+      // (The loop is one thread's: what it does for an instruction has to fit into the
+      // one before.)
       const uint64_t desc = block_desc(0), scale_desc = (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
       const uint32_t at_q = P_BYTES >> 4, at_s = (P_BYTES + half * (SK / 2)) >> 4, tall = CG == 2 || bn > 128;
       const uint32_t idesc = (1u << 7) | (1u << 10) | ((bn / 8) << 17) | ((FMT == PEAT_MXFP4 ? 1u : 0u) << 23) | ((CG * 128u / 16) << 24);
-      Turn in, at;  // of the scales, of the instructions
-      uint32_t set = 0;
-      auto scales = [&]() {
-        if (!(ok = mbar_wait(full + 8 * in.s, in.phase, p.wait_limit))) return;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint64_t sd = scale_desc + ((base + in.s * stage) >> 4) + at_s;
-        const uint32_t tp = tmem + AT_SCALES + set * SCALES, tq = tp + AT_QS;
-#pragma unroll
-        for (int j = 0; j < PER; j++) {
-          scales_in<CG>(tp + 4 * j, sd + j * (SCALE_TILE >> 4));
-          scales_in<CG>(tq + 8 * j, sd + ((PS_BYTES + j * SCALE_TILE) >> 4));
-          if (tall) scales_in<CG>(tq + 8 * j + 4, sd + ((PS_BYTES + (PER + j) * SCALE_TILE) >> 4));
-        }
-        in.next(p.stages);
-        set ^= 1;
-      };
-      uint32_t acc = 0, acc_phase = 1;
-      if (total) scales();
+      const uint32_t tp = tmem + Tmem<CG>::SCALES, tq = tp + 4 * PER;  // 4 and 8 columns for a tile
+      static_assert(Tmem<CG>::SCALES + 12 * PER <= 512, "tensor memory has 512 columns");
+      Turn at;
+      uint32_t acc = 0, acc_phase = 1, shared_phase = 1;
       for (int u = first; u < units && ok && nk; u += apart) {
         const uint32_t shift = (uint32_t)(place_of<CG>(p, u).q0 & 127) / 32;
         if (!(ok = mbar_wait(acc_empty + 8 * acc, acc_phase, p.wait_limit))) break;
+        if (CG == 2 && !(ok = mbar_wait(shared_empty, shared_phase, p.wait_limit))) break;
+        shared_phase ^= 1;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + acc * bn;
-        for (int k = 0; k < nk && ok; k++) {
-          const uint32_t tp = tmem + AT_SCALES + (set ^ 1) * SCALES, tq = tp + AT_QS + shift;
-          if (--total > 0) scales();
-          if (!ok) break;
-          const uint64_t a = desc + ((base + at.s * stage) >> 4), b = a + at_q;
+        const uint32_t d = tmem + acc * Tmem<CG>::APART;
+        for (int k = 0; k < nk; k++) {
+          if (!(ok = mbar_wait(full + 8 * at.s, at.phase, p.wait_limit))) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t from = (base + at.s * stage) >> 4;
+          const uint64_t a = desc + from, b = a + at_q, sd = scale_desc + from + at_s;
+#pragma unroll
+          for (int j = 0; j < PER; j++) {
+            scales_in<CG>(tp + 4 * j, sd + j * (SCALE_TILE >> 4));
+            scales_in<CG>(tq + 8 * j, sd + ((PS_BYTES + j * SCALE_TILE) >> 4));
+            if (tall) scales_in<CG>(tq + 8 * j + 4, sd + ((PS_BYTES + (PER + j) * SCALE_TILE) >> 4));
+          }
           const int here = p.steps - 4 * k;
 #pragma unroll
           for (int j = 0; j < 4; j++) {
             if (j >= here) break;
             constexpr int TILE_STEPS = 4 / PER;
             mma4<FMT, CG>(d, a + 2 * j, b + 2 * j, idesc | (FMT == PEAT_MXFP4 ? (2u * (j & 1)) * 0x20000010u : 0u),
-                      tp + 4 * (j / TILE_STEPS), tq + 8 * (j / TILE_STEPS), k + j > 0);
+                          tp + 4 * (j / TILE_STEPS), tq + shift + 8 * (j / TILE_STEPS), k + j > 0);
           }
           commit<CG>(empty + 8 * at.s);
           at.next(p.stages);
@@ -374,19 +393,20 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
         bias_next[k] = !SWAP && p.bias && in ? __ldcg(p.bias + t.q0 + column(c)) : 0.0f;
       }
     };
-    const uint32_t release = CG == 2 ? mapa(acc_empty, 0) : acc_empty;
-    auto released = [&](int b) {
+    const uint32_t release = CG == 2 ? mapa(acc_empty, 0) : acc_empty, release_shared = CG == 2 ? mapa(shared_empty, 0) : 0;
+    auto released = [&](uint32_t bar) {
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
       if (lane) return;
-      if (CG == 2) mbar_arrive_cluster(release + 8 * b);
-      else mbar_arrive(release + 8 * b);
+      if (CG == 2) mbar_arrive_cluster(bar);
+      else mbar_arrive(bar);
     };
     fetch(first);
     for (int u = first; u < units && ok; u += apart, i++) {
       const Place4 t = place_of<CG>(p, u);
       const int64_t row0 = t.p0 + rank * 128 + quarter * 32, row = row0 + lane;
       const float sp = sp_next, row_bias = row_bias_next;
+      const int acc = i & 1;
       __syncwarp();
 #pragma unroll
       for (int k = 0; k < KEPT; k++)
@@ -397,72 +417,62 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
       __syncwarp();
       fetch(u + apart);
       if (nk) {
-        if (!(ok = warp_wait(acc_full + 8 * (i & 1), i / 2 & 1, p.wait_limit))) break;
+        if (!(ok = warp_wait(acc_full + 8 * acc, i / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
-      const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (i & 1) * bn;
+      const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + acc * Tmem<CG>::APART;
       const int rows = (int)max((int64_t)0, min((int64_t)32, p.P - row0));
 #pragma unroll
       for (int k = 0; k < MINE; k++) {
         const int c = part + PARTS * k;
         if (c >= chunks) break;
-        float v[STEP];
-        if (nk) {
-          if constexpr (SWAP) {
-            tmem_load16(taddr + c * STEP, reinterpret_cast<uint32_t(&)[16]>(v));
-          } else {
-            tmem_load32(taddr + c * STEP, reinterpret_cast<uint32_t(&)[32]>(v[0]));
-            tmem_load32(taddr + c * STEP + 32, reinterpret_cast<uint32_t(&)[32]>(v[32]));
-          }
-          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-        } else {
-#pragma unroll
-          for (int j = 0; j < STEP; j++) v[j] = 0.0f;
-        }
-        if (c + PARTS >= chunks) released(i & 1);
         const int at = k * STEP;
         const int64_t col0 = t.q0 + c * STEP;
         if constexpr (SWAP) {
+          float v[16];
+          if (nk) {
+            tmem_load16(taddr + c * STEP, reinterpret_cast<uint32_t(&)[16]>(v));
+            asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          } else {
 #pragma unroll
-          for (int j = 0; j < STEP; j++) {
+            for (int j = 0; j < 16; j++) v[j] = 0.0f;
+          }
+          if (c + PARTS >= chunks) released(release + 8 * acc);
+#pragma unroll
+          for (int j = 0; j < 16; j++) {
             float y = v[j];
             if (scaled) y = __fmul_rn(y, __fmul_rn(sq[at + j], sp));
             if (p.bias) y = __fadd_rn(y, row_bias);
             if (col0 + j < p.Q && row < p.P) put_one<OUT>(p.out.out, (col0 + j) * p.out.ldo + row, y);
           }
-        } else if (p.out.vec) {
-          if (row0 >= p.P) continue;
-          if (scaled) {
-#pragma unroll
-            for (int j = 0; j < STEP; j += 4) {
-              const float4 f = *reinterpret_cast<const float4*>(sq + j);
-              v[j] = __fmul_rn(v[j], __fmul_rn(sp, f.x));
-              v[j + 1] = __fmul_rn(v[j + 1], __fmul_rn(sp, f.y));
-              v[j + 2] = __fmul_rn(v[j + 2], __fmul_rn(sp, f.z));
-              v[j + 3] = __fmul_rn(v[j + 3], __fmul_rn(sp, f.w));
-            }
-          }
-          if (p.out.biased) {
-#pragma unroll
-            for (int j = 0; j < STEP; j += 4) {
-              const float4 f = *reinterpret_cast<const float4*>(bias + j);
-              v[j] = __fadd_rn(v[j], f.x);
-              v[j + 1] = __fadd_rn(v[j + 1], f.y);
-              v[j + 2] = __fadd_rn(v[j + 2], f.z);
-              v[j + 3] = __fadd_rn(v[j + 3], f.w);
-            }
-          }
-          put_boxes<OUT>(box, &mo, v, row0, col0, p.out.N);
-        } else {  // rows off the 16-byte grid
+        } else {
           uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-          const OutPlace off_grid{p.out.out, p.out.ldo, p.out.N, p.out.biased, false};
+#pragma unroll 1
+          for (int h = 0; h < 2; h++) {  // 32 columns at a time
+            float v[32];
+            if (nk) {
+              tmem_load32(taddr + c * STEP + 32 * h, reinterpret_cast<uint32_t(&)[32]>(v));
+              asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+            } else {
 #pragma unroll
-          for (int j = 0; j < STEP; j += 32)
-            put_columns<OUT>(off_grid, reinterpret_cast<const float(&)[32]>(v[j]), sp, sq + j, bias + j, row0, rows, col0 + j, j == 0,
-                             j + 32 == STEP, carry);
+              for (int j = 0; j < 32; j++) v[j] = 0.0f;
+            }
+            if (h == 1) {
+              // (of a pair's accumulators the first ends with the shared columns, the second starts with them)
+              if (CG == 2 && part == (acc ? 0 : 3)) released(release_shared);
+              if (c + PARTS >= chunks) released(release + 8 * acc);
+            }
+            if (p.out.vec) {
+              if (row0 >= p.P) continue;
+              put_box<OUT>(box, &mo, v, h, scaled, sp, sq, p.out.biased, bias, row0, col0, p.out.N);
+            } else {  // rows off the 16-byte grid
+              const OutPlace off_grid{p.out.out, p.out.ldo, p.out.N, p.out.biased, false};
+              put_columns<OUT>(off_grid, v, sp, sq + 32 * h, bias + 32 * h, row0, rows, col0 + 32 * h, h == 0, h == 1, carry);
+            }
+          }
         }
       }
-      if (part >= chunks) released(i & 1);
+      if (part >= chunks) released(release + 8 * acc);
     }
     // (the boxes are read before the CTA ends, and written before the next kernel reads them)
     if (!SWAP && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
@@ -557,25 +567,27 @@ cudaError_t launch_out(int format, Kind kind, const Tc4Params& p, const Maps& m,
   return format == PEAT_MXFP4 ? launch_kind<OUT, PEAT_MXFP4>(kind, p, m, nsm, s) : launch_kind<OUT, PEAT_NVFP4>(kind, p, m, nsm, s);
 }
 
-// How a product is cut into tiles: by the cycles of its waves, an instruction of 64
-// k and what each tile costs once.
+// How a product is cut into tiles.  An instruction takes as long for 16 columns as
+// for 256 (its 128 rows' loads), so a pair's tile does twice a CTA's work in the time,
+// where there are tiles enough and k is long enough to hide the results' way out.
 struct Cut {
   Kind kind;
   int bn;
 };
 Cut cut_of(int64_t M, int64_t N, int64_t steps, int nsm) {
-  if (M <= MOST_BN) return {FEW, (int)((M + 15) / 16 * 16)};
-  Cut best{ONE, 128};
-  double least = 0.0;
+  if (M <= FEW_ROWS) return {FEW, (int)((M + 15) / 16 * 16)};
   const struct {
     Cut cut;
-    int cycles;
-  } ways[] = {{{ONE, 128}, 140}, {{PAIR, 128}, 100}, {{PAIR, 192}, 115}};
+    int fixed, least, tile, step;  // nanoseconds: of a call; of a wave, and with its instructions
+  } ways[] = {{{ONE, 64}, 3500, 800, 450, 65}, {{ONE, 128}, 3600, 1150, 600, 70}, {{PAIR, 256}, 4400, 1500, 900, 75}};
+  Cut best = ways[0].cut;
+  double shortest = 0.0;
   for (const auto& w : ways) {
     const int64_t rows = w.cut.kind == PAIR ? 256 : 128, at_once = w.cut.kind == PAIR ? nsm / 2 : nsm;
     const int64_t tiles = ((M + rows - 1) / rows) * ((N + w.cut.bn - 1) / w.cut.bn);
-    const double t = (double)((tiles + at_once - 1) / at_once) * (steps * w.cycles + 8.0 * w.cut.bn);
-    if (least == 0.0 || t < least) best = w.cut, least = t;
+    const double waves = (double)((tiles + at_once - 1) / at_once);
+    const double t = w.fixed + waves * std::max<double>(w.least, w.tile + (double)w.step * steps);
+    if (shortest == 0.0 || t < shortest) best = w.cut, shortest = t;
   }
   return best;
 }
