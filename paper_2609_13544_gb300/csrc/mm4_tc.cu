@@ -567,26 +567,33 @@ cudaError_t launch_out(int format, Kind kind, const Tc4Params& p, const Maps& m,
   return format == PEAT_MXFP4 ? launch_kind<OUT, PEAT_MXFP4>(kind, p, m, nsm, s) : launch_kind<OUT, PEAT_NVFP4>(kind, p, m, nsm, s);
 }
 
-// How a product is cut into tiles.  An instruction takes as long for 16 columns as
-// for 256 (its 128 rows' loads), so a pair's tile does twice a CTA's work in the time,
-// where there are tiles enough and k is long enough to hide the results' way out.
+// How a product is cut into tiles: by its expected time, fitted to those measured
+// for M from 1 to 16384, N to 50257 and K to 8192 (see the figures in each row).  An
+// instruction takes as long for 16 columns as for 256 (its 128 rows' loads): what
+// tells the ways apart are the waves, and the results' way out, which takes the
+// longer of it and the instructions.
 struct Cut {
   Kind kind;
   int bn;
 };
-Cut cut_of(int64_t M, int64_t N, int64_t steps, int nsm) {
-  if (M <= FEW_ROWS) return {FEW, (int)((M + 15) / 16 * 16)};
+Cut cut_of(int64_t M, int64_t N, int64_t steps, bool grid, int nsm) {
+  const int few = (int)((std::min<int64_t>(M, FEW_ROWS) + 15) / 16 * 16);
+  if (M <= 48) return {FEW, few};  // (16 x 8192 x 8192: 12.0 us, with a's rows on the 128-row side 17.9)
   const struct {
     Cut cut;
-    int fixed, least, tile, step;  // nanoseconds: of a call; of a wave, and with its instructions
-  } ways[] = {{{ONE, 64}, 3500, 800, 450, 65}, {{ONE, 128}, 3600, 1150, 600, 70}, {{PAIR, 256}, 4400, 1500, 900, 75}};
-  Cut best = ways[0].cut;
+    // nanoseconds: of a call; of a wave, on the 16-byte grid and off it, at least; with instructions: and of each
+    int fixed, least, least_off, tile, step;
+  } ways[] = {{{FEW, few}, 3400, 0, 0, 350 + 19 * few, 60},   // 16 x 50257 x 1024: 8.4 us, 192 x: 18.9
+              {{ONE, 128}, 3300, 1350, 3900, 450, 65},        // 2048 x 1024 x 4096: 7.1 us (a pair's 9.8)
+              {{PAIR, 256}, 4200, 1800, 5800, 1100, 81}};     // 16384 x 4096 x 1024: 37.6 us (a CTA's 43.2)
+  Cut best = ways[1].cut;
   double shortest = 0.0;
   for (const auto& w : ways) {
+    if (w.cut.kind == FEW && M > FEW_ROWS) continue;
     const int64_t rows = w.cut.kind == PAIR ? 256 : 128, at_once = w.cut.kind == PAIR ? nsm / 2 : nsm;
-    const int64_t tiles = ((M + rows - 1) / rows) * ((N + w.cut.bn - 1) / w.cut.bn);
+    const int64_t tiles = w.cut.kind == FEW ? (N + 127) / 128 : ((M + rows - 1) / rows) * ((N + w.cut.bn - 1) / w.cut.bn);
     const double waves = (double)((tiles + at_once - 1) / at_once);
-    const double t = w.fixed + waves * std::max<double>(w.least, w.tile + (double)w.step * steps);
+    const double t = w.fixed + waves * std::max<double>(grid ? w.least : w.least_off, w.tile + (double)w.step * steps);
     if (shortest == 0.0 || t < shortest) best = w.cut, shortest = t;
   }
   return best;
@@ -599,7 +606,9 @@ cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned i
   const int block = format == PEAT_MXFP4 ? 32 : 16;
   Tc4Params p;
   p.steps = (int)((m.K + 63) / 64);
-  Cut cut = cut_of(m.M, m.N, p.steps, nsm);
+  const int size = out_dtype == PEAT_F32 ? 4 : 2;
+  const bool grid = reinterpret_cast<uintptr_t>(m.out) % 16 == 0 && (m.ldo * size % 16 == 0 || m.M <= 1) && m.ldo * size < ((int64_t)1 << 40);
+  Cut cut = cut_of(m.M, m.N, p.steps, grid, nsm);
   p.tiles = (m.K / block + 3) / 4;
   // (a pair's copies count tiles of scales in 32 bits)
   const int64_t tall = (std::max(m.M, m.N) + 127) / 128 * p.tiles;
@@ -618,8 +627,6 @@ cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned i
   p.qt = (int)((p.Q + p.bn - 1) / p.bn);
   const int results = swap ? Warps<1, true>::BYTES : (cg == 2 ? Warps<2, false>::BYTES : Warps<1, false>::BYTES);
   p.stages = std::min(MOST_STAGES, (SMEM - 1024 - results - BARS) / stage_bytes(p.bn / cg));
-  const int size = out_dtype == PEAT_F32 ? 4 : 2;
-  const bool grid = reinterpret_cast<uintptr_t>(m.out) % 16 == 0 && (m.ldo * size % 16 == 0 || m.M <= 1) && m.ldo * size < ((int64_t)1 << 40);
   p.out = OutPlace{m.out, m.ldo, m.N, m.bias != nullptr, grid};
   p.status = status;
   p.wait_limit = wait_limit;

@@ -84,13 +84,15 @@ __device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Ou
   }
 }
 
+// (16384 x 4096 bfloat16 to codes: mxfp4 36 us, nvfp4 44, bound by the bytes under way:
+// two vectors a thread and twice the threads took 43 and 51.)
 // Rows: TPR threads have a unit, NV vectors each, one unit after another with the
 // next one's loads under way.  A unit is a row, or with mxfp4, which needs nothing
 // of the row beyond its blocks, one of `pieces` of it.  LONG (nvfp4): rows that
 // these threads do not hold, read twice, from L2 the second time.  GRID: x's and
 // values' rows start on 16-byte boundaries and are whole vectors.
 template <int DT, int FMT, int TPR, int NV, bool GRID, bool LONG>
-__global__ void __launch_bounds__(QT) quant4_rows(Quant4Params p, int64_t rows, int pieces, int64_t step_row, int step_piece) {
+__global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p, int64_t rows, int pieces, int64_t step_row, int step_piece) {
   using L = Elem<DT>;
   using T = typename L::T;
   using Col = std::conditional_t<LONG, int64_t, int>;
@@ -299,11 +301,11 @@ cudaError_t rows(const Quant4Params& p, int nsm, cudaStream_t s) {
   const int64_t vecs = p.tiles * 4 * F4<FMT>::BLOCK / Elem<DT>::E;
   if (vecs <= 16) return rows_of<DT, FMT, 16, 1>(p, nsm, s);
   if (vecs <= 32) return rows_of<DT, FMT, 32, 1>(p, nsm, s);
-  if (FMT == PEAT_MXFP4 || vecs <= 64) return rows_of<DT, FMT, 32, 2>(p, nsm, s);
+  if (vecs <= 64) return rows_of<DT, FMT, 32, 2>(p, nsm, s);
+  if (FMT == PEAT_MXFP4 || vecs <= 128) return rows_of<DT, FMT, 32, 4>(p, nsm, s);
   if constexpr (FMT == PEAT_NVFP4) {
-    if (vecs <= 128) return rows_of<DT, FMT, 64, 2>(p, nsm, s);
-    if (vecs <= 256) return rows_of<DT, FMT, 128, 2>(p, nsm, s);
-    if (vecs <= 512) return rows_of<DT, FMT, 256, 2>(p, nsm, s);
+    if (vecs <= 256) return rows_of<DT, FMT, 64, 4>(p, nsm, s);
+    if (vecs <= 512) return rows_of<DT, FMT, 128, 4>(p, nsm, s);
     if (vecs <= 1024) return rows_of<DT, FMT, 256, 4>(p, nsm, s);
     return rows_of<DT, FMT, 256, 4, true>(p, nsm, s);
   }
