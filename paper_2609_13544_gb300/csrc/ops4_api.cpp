@@ -70,38 +70,20 @@ peat_status_t quant_params(peat_handle_t h, const void* x, int64_t rows, int64_t
   p->vec_x = aligned(x, 16) && (ldx % E == 0 || rows <= 1);
   p->vec_v = values && aligned(values, 16) && (ldv % E == 0 || rows <= 1);
   p->pairs = aligned(x, 2 * B) && (ldx % 2 == 0 || rows <= 1);
+  p->pairs_v = aligned(values, 2 * B) && (ldv % 2 == 0 || rows <= 1);
   return PEAT_OK;
 }
 
-// By column, nvfp4 needs the columns' maxima first.
-peat_status_t column_maxima(peat_handle_t h, int dtype, peat::Quant4Params* p, cudaStream_t st) {
-  OpsState* s = nullptr;
-  peat::QuantParams m;
-  std::memset(&m, 0, sizeof(m));
-  m.x = p->x;
-  m.rows = p->rows;
-  m.cols = p->cols;
-  m.ldx = p->ldx;
-  m.vec_x = p->vec_x;
-  peat_status_t ps = peat::ops_state(h, st, &s);
-  if (ps == PEAT_OK) ps = peat::take(h, &s->colmax, p->cols, 8192, &m.colmax, &p->zero, &p->zero_n, st);
-  if (ps != PEAT_OK) return ps;
-  p->colmax = m.colmax;
-  cudaError_t e = peat::launch_quant8(dtype, peat::QUANT_MAXIMA, m, h->nsm, st);
-  if (e == cudaSuccess) return PEAT_OK;
-  s->colmax.lost = true;
-  return cuda_fail(h, e, "4-bit quantisation launch");
-}
-
 peat_status_t round4(peat_handle_t h, int dtype, int format, int axis, peat::Quant4Params* p, cudaStream_t st) {
-  if (axis && format == PEAT_NVFP4) {
-    peat_status_t ps = column_maxima(h, dtype, p, st);
+  if (axis && format == PEAT_NVFP4) {  // the columns' maxima first
+    OpsState* s = nullptr;
+    peat_status_t ps = peat::ops_state(h, st, &s);
+    if (ps == PEAT_OK) ps = peat::grow(h, &s->tops, &s->tops_cap, sizeof(unsigned int) * (size_t)peat::QUANT4_CHUNKS * (size_t)p->cols);
     if (ps != PEAT_OK) return ps;
+    p->tops = static_cast<unsigned int*>(s->tops);
   }
   cudaError_t e = peat::launch_quant4(dtype, format, axis, *p, h->nsm, st);
-  if (e == cudaSuccess) return PEAT_OK;
-  if (h->ops) h->ops->colmax.lost = true;
-  return cuda_fail(h, e, "4-bit quantisation launch");
+  return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "4-bit quantisation launch");
 }
 
 peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int format, int axis,

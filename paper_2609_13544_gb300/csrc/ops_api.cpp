@@ -19,6 +19,7 @@ void ops_destroy(OpsState* s) {
   if (s->colmax.p) cudaFree(s->colmax.p);
   if (s->mm) cudaFree(s->mm);
   if (s->rounded) cudaFree(s->rounded);
+  if (s->tops) cudaFree(s->tops);
   if (s->norm) cudaFree(s->norm);
   if (s->norms.p) cudaFree(s->norms.p);
   for (void* p : s->kept) cudaFree(p);

@@ -157,12 +157,10 @@ struct Quant4Params {
   void* values;          // or null
   int64_t ldv;
   int vec_x, vec_v;  // rows start on 16-byte boundaries
-  int pairs;         // x's rows start on boundaries of two elements
-  // nvfp4 by column: the columns' largest patterns, and words to clear for a later call
-  const unsigned int* colmax;
-  unsigned int* zero;
-  int64_t zero_n;
+  int pairs, pairs_v;  // x's and values' rows start on boundaries of two elements
+  unsigned int* tops;  // nvfp4 by column: place for QUANT4_CHUNKS words a column
 };
+constexpr int64_t QUANT4_CHUNKS = 32;
 cudaError_t launch_quant4(int dtype, int format, int axis, const Quant4Params& p, int nsm, cudaStream_t s);
 
 // ---- 4-bit products (mm4_tc.cu) ----

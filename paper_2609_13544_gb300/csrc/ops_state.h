@@ -50,6 +50,9 @@ struct OpsState {
   // products: packed operands and partial sums
   void* mm = nullptr;
   size_t mm_cap = 0;
+  // 4-bit rounding by column: the columns' maxima over parts of the rows
+  void* tops = nullptr;
+  size_t tops_cap = 0;
   // norm gradients: the CTAs' sums over their rows, long rows' means
   void* norm = nullptr;
   size_t norm_cap = 0;

@@ -195,91 +195,187 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
   }
 }
 
-// Columns: a warp has 32 rows of 32 columns (16-bit types by pairs: 64), a thread
-// the blocks of its own, 16 bytes of codes each.
-template <int DT, int FMT, bool PAIRS>
-__global__ void __launch_bounds__(QT) quant4_columns(Quant4Params p, int64_t wide) {
+// ---- columns ------------------------------------------------------------------
+// A warp has C columns a lane (16-bit types by pairs, where rows allow it).
+template <int DT, bool PAIRS>
+__device__ __forceinline__ uint32_t column_word(const typename Elem<DT>::T* x, int64_t cols) {
+  if (cols <= 0) return 0;
+  if (DT == PEAT_F32 || (PAIRS && cols > 1)) return __ldg(reinterpret_cast<const uint32_t*>(x));
+  return __ldg(reinterpret_cast<const uint16_t*>(x));
+}
+
+// nvfp4: the largest patterns of each column over one of the parts of the rows,
+// [parts, cols].  A lane has a vector of a row, off the 16-byte grid a word.
+template <int DT, bool GRID, bool PAIRS>
+__global__ void __launch_bounds__(QT) quant4_maxima(Quant4Params p, int64_t wide, int64_t each) {
   using L = Elem<DT>;
   using T = typename L::T;
   pdl_wait();
   pdl_trigger();
-  for (int64_t i = (int64_t)blockIdx.x * QT + threadIdx.x; i < p.zero_n; i += (int64_t)gridDim.x * QT) p.zero[i] = 0;
+  constexpr int C = GRID ? L::E : (PAIRS ? 2 : 1), W = GRID ? 4 : 1, U = GRID ? 4 : 8, ROWS = QT / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t c0 = ((int64_t)blockIdx.x % wide) * (32 * C) + lane * C, chunk = (int64_t)blockIdx.x / wide;
+  const int64_t r0 = chunk * each, r1 = min(p.rows, r0 + each), cols = p.cols - c0;
+  const T* x = static_cast<const T*>(p.x) + c0;
+  uint32_t m[W];
+#pragma unroll
+  for (int k = 0; k < W; k++) m[k] = 0;
+  auto load = [&](int64_t row, uint32_t (&w)[W]) {
+    if constexpr (GRID) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(x + row * p.ldx));
+      w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    } else {
+      w[0] = column_word<DT, PAIRS>(x + row * p.ldx, cols);
+    }
+  };
+  int64_t r = r0 + warp;
+  if (cols > 0) {
+    for (; r + (U - 1) * ROWS < r1; r += U * ROWS) {  // (without a condition on each load, or they wait for one another)
+      uint32_t w[U][W];
+#pragma unroll
+      for (int u = 0; u < U; u++) load(r + u * ROWS, w[u]);
+#pragma unroll
+      for (int u = 0; u < U; u++)
+#pragma unroll
+        for (int k = 0; k < W; k++) m[k] = max_word<DT>(m[k], w[u][k]);
+    }
+    for (; r < r1; r += ROWS) {
+      uint32_t w[W];
+      load(r, w);
+#pragma unroll
+      for (int k = 0; k < W; k++) m[k] = max_word<DT>(m[k], w[k]);
+    }
+  }
+  __shared__ uint32_t part[ROWS][W][32];
+#pragma unroll
+  for (int k = 0; k < W; k++) part[warp][k][lane] = m[k];
+  __syncthreads();
+  if (warp) return;
+  unsigned int* top = p.tops + chunk * p.cols + c0;
+#pragma unroll
+  for (int k = 0; k < W; k++) {
+#pragma unroll
+    for (int j = 1; j < ROWS; j++) m[k] = max_word<DT>(m[k], part[j][k][lane]);
+    constexpr int PER = C / W;  // columns of a word
+#pragma unroll
+    for (int c = 0; c < PER; c++)
+      if (k * PER + c < cols) top[k * PER + c] = DT == PEAT_F32 ? m[k] & 0x7fffffffu : (c ? m[k] >> 16 : m[k]) & 0x7fffu;
+  }
+}
+
+// A warp has 32 rows, a thread the blocks of its columns, 16 bytes of codes each.
+// (4096 x 4096 bfloat16 to codes: mxfp4 11.6 us.)
+template <int DT, int FMT, bool PAIRS, bool VALUES>
+__global__ void __launch_bounds__(QT) quant4_columns(Quant4Params p, int64_t wide, int chunks) {
+  using L = Elem<DT>;
+  using T = typename L::T;
+  pdl_wait();
+  pdl_trigger();
   constexpr int C = PAIRS ? 2 : 1, BLOCK = F4<FMT>::BLOCK, NB = 32 / BLOCK;
   __shared__ float reciprocals[FMT == PEAT_NVFP4 ? RECIPROCALS : 1];
-  if (FMT == PEAT_NVFP4) {
-    make_reciprocals(reciprocals);
-    __syncthreads();
-  }
+  __shared__ uint32_t most[FMT == PEAT_NVFP4 ? QT : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t c0 = ((int64_t)blockIdx.x % wide) * (32 * C) + lane * C;
-  const int64_t r0 = ((int64_t)blockIdx.x / wide) * (QT / 32 * 32) + warp * 32;
+  const int64_t r0 = ((int64_t)blockIdx.x / wide) * QT + warp * 32;
   const T* x = static_cast<const T*>(p.x) + r0 * p.ldx + c0;
   uint32_t w[32];  // (16-bit: of C columns)
   const int64_t rows = min((int64_t)32, p.rows - r0), cols = p.cols - c0;
+  if (rows == 32 && cols >= C) {  // (without a condition on each load, or they wait for one another)
 #pragma unroll
-  for (int i = 0; i < 32; i++) {
-    w[i] = 0;
-    if (i >= rows || cols <= 0) continue;
-    if (DT == PEAT_F32) w[i] = __ldg(reinterpret_cast<const uint32_t*>(x + i * p.ldx));
-    else if (PAIRS && cols > 1) w[i] = __ldg(reinterpret_cast<const uint32_t*>(x + i * p.ldx));
-    else w[i] = __ldg(reinterpret_cast<const uint16_t*>(x + i * p.ldx));
+    for (int i = 0; i < 32; i++) {
+      if constexpr (DT == PEAT_F32 || PAIRS) w[i] = __ldg(reinterpret_cast<const uint32_t*>(x + i * p.ldx));
+      else w[i] = __ldg(reinterpret_cast<const uint16_t*>(x + i * p.ldx));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; i++) w[i] = i < rows ? column_word<DT, PAIRS>(x + i * p.ldx, cols) : 0;
   }
+  if (FMT == PEAT_NVFP4) {
+    // the columns' maxima over the parts, by all threads: a column's by every (32 C)-th
+    make_reciprocals(reciprocals);
+    constexpr int WIDE = 32 * C;
+    const int64_t col = ((int64_t)blockIdx.x % wide) * WIDE + threadIdx.x % WIDE;
+    uint32_t top = 0;
+    if (col < p.cols)
+      for (int k = threadIdx.x / WIDE; k < chunks; k += QT / WIDE) top = max(top, __ldcg(p.tops + k * p.cols + col));
+    most[threadIdx.x] = top;
+    __syncthreads();
+  }
+  Row4 r[C];
+  Block4 b[C][NB];
+  uint32_t code[C][4];
 #pragma unroll
   for (int c = 0; c < C; c++) {
     const int64_t col = c0 + c;
-    Row4 r = row4<FMT>(0.0f, true);
+    r[c] = row4<FMT>(0.0f, true);
     if (FMT == PEAT_NVFP4) {
-      const uint32_t top = col < p.cols ? __ldcg(p.colmax + col) : 0;
-      r = row4<FMT>(L::mag(top), top < L::INF);
-      if (p.scale && r0 == 0 && col < p.cols) p.scale[col] = r.s;
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < QT / (32 * C); k++) top = max(top, most[k * (32 * C) + lane * C + c]);
+      r[c] = row4<FMT>(L::mag(top), top < L::INF);
+      if (p.scale && r0 == 0 && col < p.cols) p.scale[col] = r[c].s;
     }
     auto bits = [&](int i) { return DT == PEAT_F32 ? w[i] : (c ? w[i] >> 16 : w[i] & 0xffffu); };
     auto number = [&](int i) {
-      const uint32_t b = bits(i);
-      if (DT == PEAT_F32) return __uint_as_float(b);
-      if (DT == PEAT_BF16) return __uint_as_float(b << 16);
-      return __half2float(__ushort_as_half((unsigned short)b));
+      if (DT == PEAT_F32) return __uint_as_float(w[i]);
+      if (DT == PEAT_BF16) return __uint_as_float(c ? w[i] & 0xffff0000u : w[i] << 16);
+      return __half2float(__ushort_as_half((unsigned short)bits(i)));
     };
-    uint32_t code[4];
 #pragma unroll
     for (int n = 0; n < NB; n++) {
       uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < BLOCK; i++) top = max(top, bits(n * BLOCK + i) & (DT == PEAT_F32 ? 0x7fffffffu : 0x7fffu));
       const bool finite = top < L::INF;
-      const Block4 b = block4<FMT>(L::mag(top), finite, r, reciprocals);
+      b[c][n] = block4<FMT>(L::mag(top), finite, r[c], reciprocals);
 #pragma unroll
       for (int j = 0; j < BLOCK / 8; j++) {
         float y[8];
 #pragma unroll
-        for (int e = 0; e < 8; e++) y[e] = scaled4<FMT>(number(n * BLOCK + j * 8 + e), r, b);
-        code[n * (BLOCK / 8) + j] = coded<FMT>(finite, b) ? codes8(y) : 0;
+        for (int e = 0; e < 8; e++) y[e] = scaled4<FMT>(number(n * BLOCK + j * 8 + e), r[c], b[c][n]);
+        code[c][n * (BLOCK / 8) + j] = coded<FMT>(finite, b[c][n]) ? codes8(y) : 0;
       }
       const int64_t block = r0 / BLOCK + n;
-      if (p.block_scale && block < p.tiles * 4) p.block_scale[scale_at(col, block, p.tiles)] = (uint8_t)b.byte;
-      if (p.values && col < p.cols) {
-        T* o = static_cast<T*>(p.values) + (r0 + n * BLOCK) * p.ldv + col;
-#pragma unroll
-        for (int j = 0; j < BLOCK; j += 4) {
-          float v[4];
-          decoded4<FMT>(code[(n * BLOCK + j) / 8] >> (4 * (j & 4)), r, b, v);
-#pragma unroll
-          for (int e = 0; e < 4; e++)
-            if (n * BLOCK + j + e < rows) {
-              const float y = v[e];
-              if constexpr (DT == PEAT_F32) o[(j + e) * p.ldv] = y;
-              else if constexpr (DT == PEAT_F16) o[(j + e) * p.ldv] = __float2half_rn(y);
-              else o[(j + e) * p.ldv] = __float2bfloat16_rn(y);
-            }
-        }
-      }
+      if (p.block_scale && block < p.tiles * 4) p.block_scale[scale_at(col, block, p.tiles)] = (uint8_t)b[c][n].byte;
     }
     // whole blocks: 16 or 8 bytes of a 16-byte unit
     const int64_t left = (p.width - r0) / 2;
     if (p.q && col < p.cols && left > 0) {
       uint8_t* q = p.q + col * p.ldq + r0 / 2;
-      if (left >= 16) *reinterpret_cast<uint4*>(q) = make_uint4(code[0], code[1], code[2], code[3]);
-      else *reinterpret_cast<uint2*>(q) = make_uint2(code[0], code[1]);
+      if (left >= 16) *reinterpret_cast<uint4*>(q) = make_uint4(code[c][0], code[c][1], code[c][2], code[c][3]);
+      else *reinterpret_cast<uint2*>(q) = make_uint2(code[c][0], code[c][1]);
+    }
+  }
+  if (!VALUES || cols <= 0) return;
+  T* o = static_cast<T*>(p.values) + r0 * p.ldv + c0;
+  const bool both = PAIRS && cols > 1 && p.pairs_v;
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    float v[C][4];
+#pragma unroll
+    for (int c = 0; c < C; c++) decoded4<FMT>(code[c][i / 8] >> (4 * (i & 4)), r[c], b[c][i / BLOCK], v[c]);
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      if (i + e >= rows) break;
+      T* at = o + (i + e) * p.ldv;
+      if constexpr (DT == PEAT_F32) {
+        *at = v[0][e];
+      } else {
+        uint32_t two;
+        if constexpr (DT == PEAT_F16) {
+          const __half2 h = __floats2half2_rn(v[0][e], v[C - 1][e]);
+          two = *reinterpret_cast<const uint32_t*>(&h);
+        } else {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(v[0][e], v[C - 1][e]);
+          two = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        if (both) {
+          *reinterpret_cast<uint32_t*>(at) = two;
+        } else {
+          *reinterpret_cast<uint16_t*>(at) = (uint16_t)two;
+          if (C == 2 && cols > 1) *reinterpret_cast<uint16_t*>(at + 1) = (uint16_t)(two >> 16);
+        }
+      }
     }
   }
 }
@@ -311,20 +407,35 @@ cudaError_t rows(const Quant4Params& p, int nsm, cudaStream_t s) {
   }
   return cudaErrorNotSupported;
 }
-template <int DT, int FMT>
-cudaError_t columns(const Quant4Params& p, cudaStream_t s) {
-  constexpr bool SMALL = DT != PEAT_F32;
-  const bool pairs = SMALL && p.pairs;
+template <int DT, int FMT, bool PAIRS>
+cudaError_t columns_by(const Quant4Params& p, int nsm, cudaStream_t s) {
+  constexpr int WIDE = PAIRS ? 64 : 32;
+  int chunks = 0;
+  if (FMT == PEAT_NVFP4) {
+    // parts of the rows for the maxima: until the SMs have four CTAs each, 64 rows or more
+    const bool grid = p.vec_x && p.cols % Elem<DT>::E == 0;
+    const int64_t broad = grid ? 32 * Elem<DT>::E : WIDE, groups = (p.cols + broad - 1) / broad;
+    chunks = (int)std::max<int64_t>(1, std::min<int64_t>({QUANT4_CHUNKS, p.rows / 64, 4 * (int64_t)nsm / groups}));
+    const int64_t each = (p.rows + chunks - 1) / chunks;
+    cudaError_t e = launch_dependent(grid ? quant4_maxima<DT, true, PAIRS> : quant4_maxima<DT, false, PAIRS>,
+                                     (unsigned)(groups * chunks), QT, 0, s, p, groups, each);
+    if (e != cudaSuccess) return e;
+  }
   const int64_t cols = p.block_scale ? (p.cols + 127) / 128 * 128 : p.cols;
-  const int64_t height = p.tiles * 4 * F4<FMT>::BLOCK, wide = (cols + (pairs ? 63 : 31)) / (pairs ? 64 : 32);
-  const dim3 grid((unsigned)(wide * ((height + QT - 1) / QT)));
-  if (pairs) return launch_dependent(quant4_columns<DT, FMT, SMALL>, grid, QT, 0, s, p, wide);
-  return launch_dependent(quant4_columns<DT, FMT, false>, grid, QT, 0, s, p, wide);
+  const int64_t height = p.tiles * 4 * F4<FMT>::BLOCK, wide = (cols + WIDE - 1) / WIDE;
+  return launch_dependent(p.values ? quant4_columns<DT, FMT, PAIRS, true> : quant4_columns<DT, FMT, PAIRS, false>,
+                          (unsigned)(wide * ((height + QT - 1) / QT)), QT, 0, s, p, wide, chunks);
+}
+template <int DT, int FMT>
+cudaError_t columns(const Quant4Params& p, int nsm, cudaStream_t s) {
+  if constexpr (DT != PEAT_F32)
+    if (p.pairs) return columns_by<DT, FMT, true>(p, nsm, s);
+  return columns_by<DT, FMT, false>(p, nsm, s);
 }
 template <int DT>
 cudaError_t of_type(int format, int axis, const Quant4Params& p, int nsm, cudaStream_t s) {
-  if (format == PEAT_MXFP4) return axis ? columns<DT, PEAT_MXFP4>(p, s) : rows<DT, PEAT_MXFP4>(p, nsm, s);
-  return axis ? columns<DT, PEAT_NVFP4>(p, s) : rows<DT, PEAT_NVFP4>(p, nsm, s);
+  if (format == PEAT_MXFP4) return axis ? columns<DT, PEAT_MXFP4>(p, nsm, s) : rows<DT, PEAT_MXFP4>(p, nsm, s);
+  return axis ? columns<DT, PEAT_NVFP4>(p, nsm, s) : rows<DT, PEAT_NVFP4>(p, nsm, s);
 }
 
 }  // namespace
