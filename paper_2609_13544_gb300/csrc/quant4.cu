@@ -113,6 +113,11 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
   auto load = [&](int64_t row, Col at) {
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
     const Col cols = row < p.rows ? (Col)p.cols : 0;
+    if (GRID && at + PIECE <= cols) {  // (without a condition on each load, or they wait for one another)
+#pragma unroll
+      for (int i = 0; i < NV; i++) v[i] = source.load(x + at + (i * TPR + lane) * L::E);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       const Col col = at + (i * TPR + lane) * L::E;

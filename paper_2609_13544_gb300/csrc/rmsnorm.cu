@@ -150,6 +150,15 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
   auto fetch = [&](int64_t row, Col at) {
     const Col cols = row < p.rows ? (Col)p.cols : 0;
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    if (GRID && at + (Col)PIECE <= cols) {  // (without a condition on each load, or they wait for one another)
+#pragma unroll
+      for (int i = 0; i < NV; i++) s[i] = sx.load(x + column(at, i));
+      if (!p.residual) return;
+      const T* r = static_cast<const T*>(p.residual) + row * p.ldr;
+#pragma unroll
+      for (int i = 0; i < NV; i++) u[i] = sr.load(r + column(at, i));
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NV; i++) s[i] = load_vec<DT, GRID>(sx, x + column(at, i), cols - column(at, i));
     if (!p.residual) return;
@@ -391,6 +400,18 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
     const T* dp = static_cast<const T*>(p.grad) + row * p.ldg;
     const T* xp = static_cast<const T*>(p.x) + row * p.ldx;
     rstd_next = row < p.rows ? __ldg(p.rstd + row) : 0.0f;
+    if (GRID && at + TPR * NV * E <= cols) {  // (without a condition on each load, or they wait for one another)
+#pragma unroll
+      for (int i = 0; i < NV; i++) {
+        d[i] = sg.load(dp + column(i));
+        s[i] = sx.load(xp + column(i));
+      }
+      if (!p.stream || !p.grad_x) return;
+      const T* tp = static_cast<const T*>(p.stream) + row * p.ldr;
+#pragma unroll
+      for (int i = 0; i < NV; i++) u[i] = st.load(tp + column(i));
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       d[i] = load_vec<DT, GRID>(sg, dp + column(i), cols - column(i));
