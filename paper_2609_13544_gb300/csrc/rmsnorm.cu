@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
   constexpr int E = L::E, QT = threads_of<TPR>(), GROUPS = QT / TPR;
   constexpr int64_t PIECE = (int64_t)TPR * NV * E;
   constexpr int WARPS = TPR / 32;
-  __shared__ float2 sums[QT / 32], found[GROUPS], factor[GROUPS];
+  __shared__ float2 sums[TPR > 32 ? QT : 1], found[GROUPS], factor[GROUPS];
   __shared__ double wide[QT / 32];
   __shared__ uint32_t tops[QT / 32];
   pdl_wait();
@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
       unpack<DT>(s[i], a);
       unpack<DT>(u[i], b);
 #pragma unroll
-      for (int e = 0; e < E; e++) a[e] = __fadd_rn(a[e], b[e]);
+      for (int e = 0; e < E / 2; e++) put_pair(a, e, add2(pair(a, e), pair(b, e)));
       v[i] = pack<DT>(a);
     }
   };
@@ -208,43 +208,42 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
 #pragma unroll
       for (int i = 0; i < NV; i++) m = mag_max<DT>(m, v[i]);
       const float most = L::mag(mag_fold<DT>(m)), base = __fmul_ru(most, most);
-      float t = base, rest = 0.0f;
+      float2 t = both(base), rest = both(0.0f);
 #pragma unroll
       for (int i = 0; i < NV; i++) {
         float a[E];
         unpack<DT>(v[i], a);
         if (sum) put_vec<DT, GRID>(sum + column(at, i), a, p.vec_s, live ? cols - column(at, i) : -16);
 #pragma unroll
-        for (int e = 0; e < E; e++) {
-          const float w = __fmaf_rn(a[e], a[e], t);
-          rest = __fadd_rn(rest, __fmaf_rn(a[e], a[e], __fsub_rn(t, w)));
+        for (int e = 0; e < E / 2; e++) {
+          const float2 x = pair(a, e), w = fma2(x, x, t);
+          rest = add2(rest, fma2(x, x, add2(t, minus(w))));
           t = w;
         }
       }
-      lo = __fadd_rn(lo, rest);
-      if (LONG) {
-        add_kept(hi, lo, t);
-        add_kept(hi, lo, -base);
-      } else {
-        hi = t;
-        add_kept(hi, lo, -base);
-      }
+      lo = __fadd_rn(lo, __fadd_rn(rest.x, rest.y));
+      if (LONG) add_kept(hi, lo, t.x);
+      else hi = t.x;
+      add_kept(hi, lo, -base);
+      add_kept(hi, lo, t.y);
+      add_kept(hi, lo, -base);
     }
-    lanes_kept<32>(hi, lo);
     // One warp adds up the warps' sums and finds the row's factor for all: the
     // divisions would be a quarter of every thread's instructions.
     if (TPR > 32) {
-      if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = make_float2(hi, lo);
+      sums[threadIdx.x] = make_float2(hi, lo);
       __syncthreads();
     }
     bool fine = true;
     float rstd = 0.0f;
     if (lane < 32) {
-      if (TPR > 32) {
-        const float2 f = sums[group * WARPS + (lane & (WARPS - 1))];
-        hi = f.x, lo = f.y;
-        lanes_kept<WARPS>(hi, lo);
+#pragma unroll
+      for (int k = 1; k < WARPS; k++) {
+        const float2 f = sums[group * TPR + k * 32 + lane];
+        lo = __fadd_rn(lo, f.y);
+        add_kept(hi, lo, f.x);
       }
+      lanes_kept<32>(hi, lo);
       // (hi + lo) / n, rounded once: the quotient and what it leaves
       const float n = (float)(int)p.cols, quotient = __fdiv_rn(hi, n);
       const float mean = __fadd_rn(quotient, __fdiv_rn(__fadd_rn(__fmaf_rn(-quotient, n, hi), lo), n));
@@ -288,7 +287,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
         weights<DT, GRID>(p.weight, p.weight_f32, p.vec_w, column(at, i), p.cols, w);
         unpack<DT>(v[i], y[i]);
 #pragma unroll
-        for (int e = 0; e < E; e++) y[i][e] = __fmul_rn(__fmul_rn(y[i][e], rstd), w[e]);
+        for (int e = 0; e < E / 2; e++) put_pair(y[i], e, mul2(mul2(pair(y[i], e), both(rstd)), pair(w, e)));
       }
     };
     float r = 0.0f, scale = 0.0f;
@@ -334,7 +333,9 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
         float w[E];
         if (finite) {
 #pragma unroll
-          for (int e = 0; e < E; e++) w[e] = whole(y[i][e], r, true);
+          for (int e = 0; e < E; e++) w[e] = __fmul_rn(y[i][e], r);  // (a pair's product and sum become one rounding)
+#pragma unroll
+          for (int e = 0; e < E / 2; e++) put_pair(w, e, add2(pair(w, e), both(MAGIC)));
         } else {
 #pragma unroll
           for (int e = 0; e < E; e++) w[e] = MAGIC;
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
         if (p.values) {
           float z[E];
 #pragma unroll
-          for (int e = 0; e < E; e++) z[e] = __fmul_rn(number(w[e]), scale);
+          for (int e = 0; e < E / 2; e++) put_pair(z, e, mul2(add2(pair(w, e), both(-MAGIC)), both(scale)));
           put_vec<DT, GRID>(static_cast<T*>(p.values) + row * p.ldv + col, z, p.vec_v, left);
         }
       }
@@ -431,20 +432,21 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
 #pragma unroll
     for (int i = 0; i < NV; i++) dv[i] = d[i], sv[i] = s[i], uv[i] = u[i];
     if (it + 1 < p.each) fetch(row + 1);
-    float c = 0.0f;
+    float2 c2 = both(0.0f);
 #pragma unroll
     for (int i = 0; i < NV; i++) {
       float a[E], b[E];
       unpack<DT>(dv[i], a);
       unpack<DT>(sv[i], b);
 #pragma unroll
-      for (int e = 0; e < E; e++) {
-        const float n = __fmul_rn(b[e], rstd);
-        dw[i][e] = __fmaf_rn(a[e], n, dw[i][e]);
-        if (!LONG) c = __fmaf_rn(__fmul_rn(a[e], w[i][e]), n, c);
+      for (int e = 0; e < E / 2; e++) {
+        const float2 x = pair(a, e), n = mul2(pair(b, e), both(rstd));
+        put_pair(dw[i], e, fma2(x, n, pair(dw[i], e)));
+        if (!LONG) c2 = fma2(mul2(x, pair(w[i], e)), n, c2);
       }
     }
     if (!p.grad_x) continue;
+    float c = c2.x + c2.y;
     if (LONG) c = live ? __ldg(p.dots + row) : 0.0f;
     else c = sum_plain<TPR>(c, dots[it & 1]) / n_cols;
 #pragma unroll
@@ -453,11 +455,12 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
       unpack<DT>(dv[i], a);
       unpack<DT>(sv[i], b);
 #pragma unroll
-      for (int e = 0; e < E; e++) b[e] = __fmul_rn(rstd, __fmaf_rn(-__fmul_rn(b[e], rstd), c, __fmul_rn(a[e], w[i][e])));
+      for (int e = 0; e < E / 2; e++)
+        put_pair(b, e, mul2(both(rstd), fma2(minus(mul2(pair(b, e), both(rstd))), both(c), mul2(pair(a, e), pair(w[i], e)))));
       if (p.stream) {
         unpack<DT>(uv[i], t);
 #pragma unroll
-        for (int e = 0; e < E; e++) b[e] = __fadd_rn(b[e], t[e]);
+        for (int e = 0; e < E / 2; e++) put_pair(b, e, add2(pair(b, e), pair(t, e)));
       }
       put_vec<DT, GRID>(static_cast<T*>(p.grad_x) + row * p.ldo + column(i), b, p.vec_o, live ? (Col)p.cols - column(i) : -16);
     }
@@ -515,22 +518,31 @@ __global__ void __launch_bounds__(256) rms_dots(RmsBackParams p) {
   if (threadIdx.x == 0) p.dots[row] = c / (float)(int)p.cols;
 }
 
-// the CTAs' sums of each column, in their order: 8 lanes of rows, then over the lanes
-__global__ void __launch_bounds__(256) rms_weight_sums(const float* parts, int ctas, int64_t cols, float* out) {
+// the CTAs' sums of each column, in their order: some by each warp, then over the warps
+__global__ void __launch_bounds__(1024) rms_weight_sums(const float* parts, int ctas, int64_t cols, float* out) {
   pdl_wait();
   pdl_trigger();
-  __shared__ float met[8][32];
-  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+  __shared__ float met[32][32];
+  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const int64_t col = (int64_t)blockIdx.x * 32 + lane;
   float hi = 0.0f, lo = 0.0f;
-  if (col < cols)
-    for (int i = part; i < ctas; i += 8) add_kept(hi, lo, __ldcg(parts + (int64_t)i * cols + col));
+  if (col < cols) {
+    constexpr int U = 5;
+    int i = part;
+    for (; i + (U - 1) * warps < ctas; i += U * warps) {
+      float x[U];
+#pragma unroll
+      for (int u = 0; u < U; u++) x[u] = __ldcg(parts + (int64_t)(i + u * warps) * cols + col);
+#pragma unroll
+      for (int u = 0; u < U; u++) add_kept(hi, lo, x[u]);
+    }
+    for (; i < ctas; i += warps) add_kept(hi, lo, __ldcg(parts + (int64_t)i * cols + col));
+  }
   met[part][lane] = __fadd_rn(hi, lo);
   __syncthreads();
   if (part || col >= cols) return;
   float t = met[0][lane];
-#pragma unroll
-  for (int i = 1; i < 8; i++) t += met[i][lane];
+  for (int k = 1; k < warps; k++) t += met[k][lane];
   out[col] = t;
 }
 
@@ -585,7 +597,7 @@ cudaError_t backward(const RmsBackParams& p, cudaStream_t s) {
     if (e != cudaSuccess) return e;
   }
   if (!p.grad_weight) return e;
-  return launch_dependent(rms_weight_sums, (unsigned)((p.cols + 31) / 32), 256, 0, s, (const float*)p.parts, p.ctas, p.cols, p.grad_weight);
+  return launch_dependent(rms_weight_sums, (unsigned)((p.cols + 31) / 32), p.ctas > 80 ? 1024 : 256, 0, s, (const float*)p.parts, p.ctas, p.cols, p.grad_weight);
 }
 template <int DT>
 cudaError_t backward_of(const RmsBackParams& p, cudaStream_t s) {

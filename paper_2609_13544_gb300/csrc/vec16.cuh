@@ -57,4 +57,36 @@ __device__ __forceinline__ uint4 pack(const float (&x)[DT == PEAT_F32 ? 4 : 8]) 
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Two float32 operations in one instruction, each rounded to nearest as the single
+// ones; but the compiler makes one fma of a mul2 whose result only an add2 takes.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, w;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mul.rn.f32x2 w, x, y;\n mov.b64 {%0, %1}, w;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, w;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n add.rn.f32x2 w, x, y;\n mov.b64 {%0, %1}, w;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n .reg .b64 x, y, z, w;\n mov.b64 x, {%2, %3};\n mov.b64 y, {%4, %5};\n mov.b64 z, {%6, %7};\n"
+      " fma.rn.f32x2 w, x, y, z;\n mov.b64 {%0, %1}, w;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 minus(float2 a) { return make_float2(-a.x, -a.y); }
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+// elements 2 i and 2 i + 1
+template <int N>
+__device__ __forceinline__ float2 pair(const float (&x)[N], int i) { return make_float2(x[2 * i], x[2 * i + 1]); }
+template <int N>
+__device__ __forceinline__ void put_pair(float (&x)[N], int i, float2 v) { x[2 * i] = v.x, x[2 * i + 1] = v.y; }
+
 }  // namespace peat
