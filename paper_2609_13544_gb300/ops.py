@@ -131,11 +131,14 @@ def _is_int32(t) -> bool:
 
 def _matrix(h, t, name: str) -> int:
     """The row distance of a matrix whose rows are contiguous, on the handle's device."""
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError(f"{name} must have two dimensions")
     if t.get_device() != h.device:
         raise ValueError(f"{name} must be a CUDA tensor on the handle's device")
-    rows, cols = t.shape
+    rows, cols = shape
+    if t.is_contiguous():
+        return cols
     s0, s1 = t.stride()
     if s1 != 1 and cols > 1:
         raise ValueError(f"the rows of {name} must be contiguous")

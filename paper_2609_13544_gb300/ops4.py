@@ -35,9 +35,15 @@ def f4_scale_bytes(rows: int, blocks: int) -> int:
     return -(-rows // 128) * -(-blocks // 4) * 512
 
 
+_uint8 = None
+
+
 def _is_bytes(t) -> bool:
-    import torch
-    return t.dtype == torch.uint8
+    global _uint8
+    if _uint8 is None:
+        import torch
+        _uint8 = torch.uint8
+    return t.dtype is _uint8
 
 
 class Float4:
@@ -145,7 +151,7 @@ def peat_matmul_f4_raw(h, a: Float4, b: Float4, out, bias=None, stream=None) -> 
     if a.cols != b.cols:
         raise ValueError("a and b differ in their row length")
     ldo = _matrix(h, out, "out")
-    if out.shape[0] != a.rows or out.shape[1] != b.rows:
+    if out.shape != (a.rows, b.rows):
         raise ValueError("out must be [rows of a, rows of b]")
     _call(h, "peat_matmul_f4", a.code, *a.args, *b.args, _vector(h, bias, b.rows, "bias"), a.rows, b.rows, a.cols,
           out.data_ptr(), ldo, _code(out), _stream(h, stream))
@@ -245,22 +251,21 @@ class Linear4(LinearBase):
 # ---------------------------------------------------------------------------
 # root-mean-square norm
 # ---------------------------------------------------------------------------
-def _like(h, t, x, name: str):
+def _like(h, t, shape, dtype, name: str):
     """(pointer, row distance) of an optional matrix of x's shape and type."""
     if t is None:
-        return None, x.shape[1]
-    if t.dtype != x.dtype or t.shape != x.shape:
+        return None, shape[1]
+    if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must have x's shape and type")
     return t.data_ptr(), _matrix(h, t, name)
 
 
-def _norm_weight(h, weight, x):
+def _norm_weight(h, weight, cols: int, dtype):
     """(pointer, type code) of a norm's weights."""
-    if (weight.dim() != 1 or weight.shape[0] != x.shape[1] or not weight.is_contiguous()
-            or weight.get_device() != h.device):
-        raise ValueError(f"weight must be a contiguous vector of {x.shape[1]} elements on the handle's device")
+    if weight.shape != (cols,) or not weight.is_contiguous() or weight.get_device() != h.device:
+        raise ValueError(f"weight must be a contiguous vector of {cols} elements on the handle's device")
     code = _code(weight)
-    if code != 0 and weight.dtype != x.dtype:
+    if code != 0 and weight.dtype is not dtype:
         raise TypeError("weight must be of x's type or float32")
     return weight.data_ptr(), code
 
@@ -271,17 +276,17 @@ def peat_rmsnorm_raw(h, x, weight, eps: float = 1e-6, residual=None, sum=None, y
     type, q int8 of x's shape, scale and rstd float32 [rows]; each may be None, but not all.  sum may be x or residual
     itself."""
     ldx = _matrix(h, x, "x")
-    rows, cols = x.shape
-    w, wcode = _norm_weight(h, weight, x)
-    ldq = cols
+    shape, dtype = x.shape, x.dtype
+    rows, cols = shape
+    ldq, qp = cols, None
     if q is not None:
-        ldq = _matrix(h, q, "q")
-        if _code_or_int8(q) != INT8 or q.shape != x.shape:
+        ldq, qp = _matrix(h, q, "q"), q.data_ptr()
+        if _code_or_int8(q) != INT8 or q.shape != shape:
             raise ValueError("q must be int8 of x's shape")
-    _call(h, "peat_rmsnorm", x.data_ptr(), ldx, *_like(h, residual, x, "residual"), w, wcode, rows, cols, _code(x), eps,
-          *_like(h, sum, x, "sum"), *_like(h, y, x, "y"), None if q is None else q.data_ptr(), ldq,
-          _vector(h, scale, rows, "scale"), *_like(h, values, x, "values"), _vector(h, rstd, rows, "rstd"),
-          _stream(h, stream))
+    _call(h, "peat_rmsnorm", x.data_ptr(), ldx, *_like(h, residual, shape, dtype, "residual"),
+          *_norm_weight(h, weight, cols, dtype), rows, cols, _code(x), eps, *_like(h, sum, shape, dtype, "sum"),
+          *_like(h, y, shape, dtype, "y"), qp, ldq, _vector(h, scale, rows, "scale"),
+          *_like(h, values, shape, dtype, "values"), _vector(h, rstd, rows, "rstd"), _stream(h, stream))
 
 
 def peat_rmsnorm(h, x, weight, eps: float = 1e-6, residual=None, rounded: bool = True, stream=None) -> dict:
@@ -307,14 +312,14 @@ def peat_rmsnorm(h, x, weight, eps: float = 1e-6, residual=None, rounded: bool =
 def peat_rmsnorm_backward_raw(h, grad, x, weight, rstd, grad_x=None, grad_weight=None, grad_sum=None, stream=None) -> None:
     """peat_rmsnorm_backward from grad = dL/dy, x (the norm's sum) and rstd on preallocated outputs: grad_x of x's shape
     and type (grad or grad_sum itself, if need be), grad_weight float32 [cols]; not both None."""
-    ldx = _matrix(h, x, "x")
-    rows, cols = x.shape
-    w, wcode = _norm_weight(h, weight, x)
     if rstd is None or grad is None:
         raise ValueError("grad and rstd are needed")
-    _call(h, "peat_rmsnorm_backward", *_like(h, grad, x, "grad"), *_like(h, grad_sum, x, "grad_sum"), x.data_ptr(), ldx, w,
-          wcode, _vector(h, rstd, rows, "rstd"), rows, cols, _code(x), *_like(h, grad_x, x, "grad_x"),
-          _vector(h, grad_weight, cols, "grad_weight"), _stream(h, stream))
+    ldx = _matrix(h, x, "x")
+    shape, dtype = x.shape, x.dtype
+    rows, cols = shape
+    _call(h, "peat_rmsnorm_backward", *_like(h, grad, shape, dtype, "grad"), *_like(h, grad_sum, shape, dtype, "grad_sum"),
+          x.data_ptr(), ldx, *_norm_weight(h, weight, cols, dtype), _vector(h, rstd, rows, "rstd"), rows, cols, _code(x),
+          *_like(h, grad_x, shape, dtype, "grad_x"), _vector(h, grad_weight, cols, "grad_weight"), _stream(h, stream))
 
 
 def peat_rmsnorm_backward(h, grad, x, weight, rstd, grad_sum=None, stream=None):
