@@ -38,6 +38,7 @@ struct Warps {
   static constexpr int BOX = SWAP ? 0 : 4096, BYTES = EPI * (BOX + EDGE * 2 * 4);
 };
 constexpr int BARS = 256;
+constexpr int SUM_ROW = 132;  // words from one row of sums to the next
 constexpr int SMEM = 227 * 1024;
 // Tensor memory: two accumulators, then a stage's scales.  A pair's accumulators have
 // 256 columns and share 48 of them: the next tile's instructions wait until the warps
@@ -60,6 +61,7 @@ struct Tc4Params {
   int64_t tiles;      // of scales along k
   int steps;          // instructions of 64 k
   int bn, pt, qt, stages;
+  int splits;         // CTAs of a cluster that share a tile's k range: 1, 2, 4 or 8 (then a cluster has one tile)
   unsigned int* status;
   uint32_t wait_limit;
 };
@@ -140,6 +142,11 @@ __device__ __forceinline__ Place4 place_of(const Tc4Params& p, int u) {
   return Place4{(int64_t)(g * GROUP + in - q * wide) * (CG * 128), (int64_t)q * p.bn};
 }
 
+__device__ __forceinline__ float4 load_cluster_float4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+  return v;
+}
 template <int OUT>
 __device__ __forceinline__ void put_one(void* out, int64_t at, float y) {
   typename Mm8Out<OUT>::T* o = static_cast<typename Mm8Out<OUT>::T*>(out) + at;
@@ -228,7 +235,12 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
   // a pair's CTAs differ in their rank; the even one issues the instructions
   uint32_t rank = 0;
   if (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  const int first = blockIdx.x / CG, apart = gridDim.x / CG;
+  // parts of a tile's k range, in stages
+  uint32_t part_k = 0;
+  if (CG == 1 && p.splits > 1) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(part_k));
+  const bool split = CG == 1 && p.splits > 1;
+  const int together = CG == 1 ? p.splits : 2, first = blockIdx.x / together, apart = gridDim.x / together;
+  const int all_k = (p.steps + 3) / 4, k0 = (int)((int64_t)all_k * part_k / p.splits), k1 = (int)((int64_t)all_k * (part_k + 1) / p.splits);
   char* edges = smem + p.stages * stage;
   const uint32_t full = sptr(edges + W::BYTES), empty = full + 8 * MOST_STAGES, acc_full = empty + 8 * MOST_STAGES,
                  acc_empty = acc_full + 16, shared_empty = acc_empty + 16, last = shared_empty + 8;
@@ -236,7 +248,7 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
   static_assert(8 * (2 * MOST_STAGES + 6) + 4 <= BARS, "the barriers fit");
   constexpr int TILE_K = F4<FMT>::BLOCK * 4, PER = SK / TILE_K;  // k of a tile of scales; tiles of a stage
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int units = p.pt * p.qt, nk = (p.steps + 3) / 4;
+  const int units = p.pt * p.qt, nk = k1 - k0;
   const uint32_t base = sptr(smem);
 
   if (threadIdx.x == 32) {
@@ -284,10 +296,10 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
         const Place4 t = place_of<CG>(p, u);
         const int64_t pb = t.p0 >> 7, qb = t.q0 >> 7, q_end = min(t.q0 + bn, p.Q);
         const int qbs = (int)(((q_end - 1) >> 7) - qb) + 1;  // blocks of 128 rows that the tile's lie in
-        const uint8_t* ps = p.ps + pb * p.tiles * SCALE_TILE;
-        const uint8_t* qs = p.qs + qb * p.tiles * SCALE_TILE;
-        int left = (int)p.tiles;
-        for (int k = 0; k < nk; k++, seq++, left -= PER, ps += PER * SCALE_TILE, qs += PER * SCALE_TILE) {
+        const uint8_t* ps = p.ps + (pb * p.tiles + (int64_t)k0 * PER) * SCALE_TILE;
+        const uint8_t* qs = p.qs + (qb * p.tiles + (int64_t)k0 * PER) * SCALE_TILE;
+        int left = (int)p.tiles - k0 * PER;
+        for (int k = k0; k < k1; k++, seq++, left -= PER, ps += PER * SCALE_TILE, qs += PER * SCALE_TILE) {
           if (!(ok = mbar_wait(empty + 8 * at.s, at.phase ^ 1, p.wait_limit))) break;
           const uint32_t dst = base + at.s * stage, bar = full + 8 * at.s, qd = dst + P_BYTES, sd = qd + half * (SK / 2);
           if constexpr (CG == 2) {  // all bytes of both CTAs count on the even one's barrier
@@ -337,7 +349,7 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
         shared_phase ^= 1;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint32_t d = tmem + acc * Tmem<CG>::APART;
-        for (int k = 0; k < nk; k++) {
+        for (int k = k0; k < k1; k++) {
           if (!(ok = mbar_wait(full + 8 * at.s, at.phase, p.wait_limit))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t from = (base + at.s * stage) >> 4;
@@ -354,7 +366,7 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
             if (j >= here) break;
             constexpr int TILE_STEPS = 4 / PER;
             mma4<FMT, CG>(d, a + 2 * j, b + 2 * j, idesc | (FMT == PEAT_MXFP4 ? (2u * (j & 1)) * 0x20000010u : 0u),
-                          tp + 4 * (j / TILE_STEPS), tq + shift + 8 * (j / TILE_STEPS), k + j > 0);
+                          tp + 4 * (j / TILE_STEPS), tq + shift + 8 * (j / TILE_STEPS), k + j > k0);
           }
           commit<CG>(empty + 8 * at.s);
           at.next(p.stages);
@@ -421,6 +433,26 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
       const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + acc * Tmem<CG>::APART;
+      if (split) {
+        // The sums go to the stages' place (the last instruction is done with it), where
+        // the cluster's other parts find them: contiguous along the output's rows.
+        float* sums = reinterpret_cast<float*>(smem);
+        const int r = quarter * 32 + lane;
+        for (int c = part * 16; c < bn; c += PARTS * 16) {
+          float v[16];
+          tmem_load16(taddr + c, reinterpret_cast<uint32_t(&)[16]>(v));
+          asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+          if (SWAP) {
+#pragma unroll
+            for (int j = 0; j < 16; j++) sums[(c + j) * SUM_ROW + r] = v[j];
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4)
+              *reinterpret_cast<float4*>(sums + r * SUM_ROW + c + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+          }
+        }
+        break;
+      }
       const int rows = (int)max((int64_t)0, min((int64_t)32, p.P - row0));
 #pragma unroll
       for (int k = 0; k < MINE; k++) {
@@ -478,6 +510,51 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
     if (!SWAP && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   __syncwarp();
+  if (split) {
+    // The parts meet: each CTA adds up its share of the columns, in the parts' order.
+    cg::this_cluster().sync();
+    if (warp < EPI_WARPS && ok && first < units) {
+      const Place4 t = place_of<CG>(p, first);
+      // four of a row of the output at a time: of a column of sums (SWAP), or of a row's share
+      const int c0 = bn * (int)part_k / p.splits, nc = bn * ((int)part_k + 1) / p.splits - c0;
+      const int per = SWAP ? 5 : 5 - (__ffs(p.splits) - 1);  // (not SWAP: 128 columns)
+      const uint32_t sums = sptr(smem);
+      // (a thread's place along the rows is the same in all its turns)
+      const int along = (threadIdx.x & ((1 << per) - 1)) * 4;
+      const int64_t from = SWAP ? t.p0 + along : t.q0 + c0 + along, limit = SWAP ? p.P : p.Q;
+      const float *mine = SWAP ? p.sp : p.sq, *others = SWAP ? p.sq : p.sp;
+      float scale[4], bias[4];
+#pragma unroll
+      for (int j = 0; j < 4; j++) {
+        scale[j] = mine && from + j < limit ? __ldcg(mine + from + j) : 1.0f;
+        bias[j] = p.bias && from + j < limit ? __ldcg(p.bias + from + j) : 0.0f;
+      }
+#pragma unroll 2
+      for (int i = threadIdx.x; i < 32 * nc; i += EPI_WARPS * 32) {
+        const int over = i >> per;
+        const int64_t m = SWAP ? t.q0 + c0 + over : t.p0 + over;  // the output's row
+        if (m >= (SWAP ? p.Q : p.P)) continue;
+        const uint32_t at = sums + ((SWAP ? c0 + over : over) * SUM_ROW + (SWAP ? along : c0 + along)) * 4;
+        const float other = others ? __ldcg(others + m) : 1.0f;
+        float4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; k++)
+          if (k < p.splits) x[k] = load_cluster_float4(mapa(at, k));
+        float y[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
+#pragma unroll
+        for (int k = 1; k < 8; k++)
+          if (k < p.splits) y[0] += x[k].x, y[1] += x[k].y, y[2] += x[k].z, y[3] += x[k].w;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+          if (from + j >= limit) break;
+          if (p.sp || p.sq) y[j] = __fmul_rn(y[j], __fmul_rn(other, scale[j]));
+          if (p.bias) y[j] = __fadd_rn(y[j], bias[j]);
+          put_one<OUT>(p.out.out, m * p.out.ldo + from + j, y[j]);
+        }
+      }
+    }
+    cg::this_cluster().sync();  // the others may still read this CTA's sums
+  }
   if (!ok) atomicOr_system(p.status, 1u);
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -544,16 +621,16 @@ cudaError_t launch(const Tc4Params& p, const Maps& m, int nsm, cudaStream_t s) {
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
   at[1].id = cudaLaunchAttributeClusterDimension;
-  at[1].val.clusterDim.x = CG;
+  at[1].val.clusterDim.x = (unsigned)(CG == 2 ? 2 : p.splits);
   at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   // (one CTA an SM, which has all of tensor memory)
-  cfg.gridDim = dim3((unsigned)(CG * std::min<int64_t>(tiles, nsm / CG)));
+  cfg.gridDim = dim3((unsigned)(p.splits > 1 ? p.splits * tiles : CG * std::min<int64_t>(tiles, nsm / CG)));
   cfg.blockDim = dim3(Warps<CG, SWAP>::THREADS);
   cfg.dynamicSmemBytes = SMEM;
   cfg.stream = s;
   cfg.attrs = at;
-  cfg.numAttrs = CG == 2 ? 2 : 1;
+  cfg.numAttrs = CG == 2 || p.splits > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, mm4_tc<OUT, FMT, SWAP, CG>, p, m.p, m.q, m.sp, m.sq, m.out);
 }
 enum Kind { FEW, ONE, PAIR };  // few rows of a; tiles of a CTA; of a pair
@@ -568,33 +645,39 @@ cudaError_t launch_out(int format, Kind kind, const Tc4Params& p, const Maps& m,
 }
 
 // How a product is cut into tiles: by its expected time, fitted to those measured
-// for M from 1 to 16384, N to 50257 and K to 8192 (see the figures in each row).  An
+// for M from 1 to 16384, N to 50257 and K to 16384 (see the figures in each row).  An
 // instruction takes as long for 16 columns as for 256 (its 128 rows' loads): what
 // tells the ways apart are the waves, and the results' way out, which takes the
-// longer of it and the instructions.
+// longer of it and the instructions.  Few tiles of long rows have a cluster each,
+// whose CTAs share the k range.
 struct Cut {
   Kind kind;
-  int bn;
+  int bn, splits;
 };
 Cut cut_of(int64_t M, int64_t N, int64_t steps, bool grid, int nsm) {
   const int few = (int)((std::min<int64_t>(M, FEW_ROWS) + 15) / 16 * 16);
-  if (M <= 48) return {FEW, few};  // (16 x 8192 x 8192: 12.0 us, with a's rows on the 128-row side 17.9)
   const struct {
     Cut cut;
     // nanoseconds: of a call; of a wave, on the 16-byte grid and off it, at least; with instructions: and of each
     int fixed, least, least_off, tile, step;
-  } ways[] = {{{FEW, few}, 3400, 0, 0, 350 + 19 * few, 60},   // 16 x 50257 x 1024: 8.4 us, 192 x: 18.9
-              {{ONE, 128}, 3300, 1350, 3900, 450, 65},        // 2048 x 1024 x 4096: 7.1 us (a pair's 9.8)
-              {{PAIR, 256}, 4200, 1800, 5800, 1100, 81}};     // 16384 x 4096 x 1024: 37.6 us (a CTA's 43.2)
+  } ways[] = {{{FEW, few, 1}, 3400, 0, 0, 350 + 19 * few, 60},   // 16 x 50257 x 1024: 8.4 us, 192 x: 18.9
+              {{ONE, 128, 1}, 3300, 1350, 3900, 450, 65},        // 2048 x 1024 x 4096: 7.1 us (a pair's 9.8)
+              {{PAIR, 256, 1}, 4200, 1800, 5800, 1100, 81}};     // 16384 x 4096 x 1024: 37.6 us (a CTA's 43.2)
   Cut best = ways[1].cut;
   double shortest = 0.0;
   for (const auto& w : ways) {
     if (w.cut.kind == FEW && M > FEW_ROWS) continue;
+    if (w.cut.kind != FEW && M <= 48) continue;  // (16 x 8192 x 8192: 12.0 us, with a's rows on the 128-row side 17.9)
     const int64_t rows = w.cut.kind == PAIR ? 256 : 128, at_once = w.cut.kind == PAIR ? nsm / 2 : nsm;
     const int64_t tiles = w.cut.kind == FEW ? (N + 127) / 128 : ((M + rows - 1) / rows) * ((N + w.cut.bn - 1) / w.cut.bn);
-    const double waves = (double)((tiles + at_once - 1) / at_once);
-    const double t = w.fixed + waves * std::max<double>(grid ? w.least : w.least_off, w.tile + (double)w.step * steps);
-    if (shortest == 0.0 || t < shortest) best = w.cut, shortest = t;
+    for (int s = 1; s <= (w.cut.kind == PAIR ? 1 : 8); s *= 2) {
+      // (a cluster of 8 finds place on some of the GPU's parts only; a part has two stages or more)
+      if (s > 1 && (tiles > (s == 2 ? nsm / 2 : s == 4 ? nsm / 4 - 2 : nsm / 10) || steps < 8 * s)) break;
+      const double waves = s > 1 ? 1.0 : (double)((tiles + at_once - 1) / at_once);
+      double t = w.fixed + waves * std::max<double>(grid || s > 1 ? w.least : w.least_off, w.tile + (double)w.step * ((steps + s - 1) / s));
+      if (s > 1) t += w.cut.kind == FEW ? 1600 + 3 * few : 4300;  // the parts' meeting
+      if (shortest == 0.0 || t < shortest) best = Cut{w.cut.kind, w.cut.bn, s}, shortest = t;
+    }
   }
   return best;
 }
@@ -612,7 +695,7 @@ cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned i
   p.tiles = (m.K / block + 3) / 4;
   // (a pair's copies count tiles of scales in 32 bits)
   const int64_t tall = (std::max(m.M, m.N) + 127) / 128 * p.tiles;
-  if (cut.kind == PAIR && tall >= ((int64_t)1 << 31) - 1024 - 2 * p.tiles) cut = {ONE, 128};
+  if (cut.kind == PAIR && tall >= ((int64_t)1 << 31) - 1024 - 2 * p.tiles) cut = {ONE, 128, 1};
   const bool swap = cut.kind == FEW;
   p.ps = swap ? m.b_block_scale : m.a_block_scale;
   p.qs = swap ? m.a_block_scale : m.b_block_scale;
@@ -622,6 +705,7 @@ cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned i
   p.P = swap ? m.N : m.M;
   p.Q = swap ? m.M : m.N;
   p.bn = cut.bn;
+  p.splits = cut.splits;
   const int cg = cut.kind == PAIR ? 2 : 1;
   p.pt = (int)((p.P + 128 * cg - 1) / (128 * cg));
   p.qt = (int)((p.Q + p.bn - 1) / p.bn);
