@@ -75,15 +75,12 @@ peat_status_t quant_params(peat_handle_t h, const void* x, int64_t rows, int64_t
 }
 
 peat_status_t round4(peat_handle_t h, int dtype, int format, int axis, peat::Quant4Params* p, cudaStream_t st) {
-  if (axis && format == PEAT_NVFP4) {  // the columns' maxima first
-    OpsState* s = nullptr;
-    peat_status_t ps = peat::ops_state(h, st, &s);
-    if (ps == PEAT_OK) ps = peat::grow(h, &s->tops, &s->tops_cap, sizeof(unsigned int) * (size_t)peat::QUANT4_CHUNKS * (size_t)p->cols);
-    if (ps != PEAT_OK) return ps;
-    p->tops = static_cast<unsigned int*>(s->tops);
-  }
   cudaError_t e = peat::launch_quant4(dtype, format, axis, *p, h->nsm, st);
   return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "4-bit quantisation launch");
+}
+// the columns' maxima over parts of the rows, which nvfp4 by column needs
+size_t tops_bytes(int format, int axis, int64_t cols) {
+  return axis && format == PEAT_NVFP4 ? sizeof(unsigned int) * (size_t)peat::QUANT4_CHUNKS * (size_t)cols : 0;
 }
 
 peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx, int dtype, int format, int axis,
@@ -98,6 +95,13 @@ peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t col
   if (p.tiles == 0) {  // rows of nothing
     cudaError_t e = cudaMemsetAsync(scale, 0, sizeof(float) * (size_t)across, st);
     return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "cudaMemsetAsync(scale)");
+  }
+  if (const size_t need = tops_bytes(format, axis, cols)) {
+    OpsState* s = nullptr;
+    ps = peat::ops_state(h, st, &s);
+    if (ps == PEAT_OK) ps = peat::grow(h, &s->tops, &s->tops_cap, need);
+    if (ps != PEAT_OK) return ps;
+    p.tops = static_cast<unsigned int*>(s->tops);
   }
   return round4(h, dtype, format, axis, &p, st);
 }
@@ -212,8 +216,14 @@ peat_status_t product(peat_handle_t h, int format, const peat_operand_f4_t* a, c
   OpsState* s = nullptr;
   ps = peat::ops_state(h, st, &s);
   if (ps == PEAT_OK) ps = peat::grow(h, &s->rounded, &s->rounded_cap, need);
+  // (each operand's maxima have a place of their own: the second is rounded beside the first)
+  size_t tops[2] = {0, 0};
+  for (int i = 0; i < 2; i++)
+    if (in[i]->dtype != PEAT_F4) tops[i] = tops_bytes(format, in[i]->axis, in[i]->cols);
+  if (ps == PEAT_OK && tops[0] + tops[1]) ps = peat::grow(h, &s->tops, &s->tops_cap, tops[0] + tops[1]);
   if (ps != PEAT_OK) return ps;
   size_t at = 0;
+  bool beside = false;
   for (int i = 0; i < 2; i++) {
     op[i] = operand_of(*in[i], format, static_cast<char*>(s->rounded), &at);
     if (in[i]->dtype == PEAT_F4 || K == 0) continue;
@@ -221,6 +231,9 @@ peat_status_t product(peat_handle_t h, int format, const peat_operand_f4_t* a, c
     ps = quant_params(h, in[i]->data, in[i]->rows, in[i]->cols, in[i]->ld, in[i]->dtype, format, in[i]->axis,
                       const_cast<uint8_t*>(op[i].q), op[i].ld, const_cast<uint8_t*>(op[i].block_scale),
                       const_cast<float*>(op[i].scale), nullptr, 0, &q);
+    q.tops = reinterpret_cast<unsigned int*>(static_cast<char*>(s->tops) + (i ? tops[0] : 0));
+    q.overlap = beside;
+    beside = true;
     if (ps == PEAT_OK) ps = round4(h, in[i]->dtype, format, in[i]->axis, &q, st);
     if (ps != PEAT_OK) return ps;
   }

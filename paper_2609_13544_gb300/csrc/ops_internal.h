@@ -159,6 +159,7 @@ struct Quant4Params {
   int vec_x, vec_v;  // rows start on 16-byte boundaries
   int pairs, pairs_v;  // x's and values' rows start on boundaries of two elements
   unsigned int* tops;  // nvfp4 by column: place for QUANT4_CHUNKS words a column
+  int overlap;         // the kernel before this one on the stream is nothing to it
 };
 constexpr int64_t QUANT4_CHUNKS = 32;
 cudaError_t launch_quant4(int dtype, int format, int axis, const Quant4Params& p, int nsm, cudaStream_t s);

@@ -18,6 +18,17 @@ namespace {
 
 constexpr int QT = 256;  // threads of a CTA
 
+// A kernel that needs nothing of the one before it (Quant4Params::overlap) runs
+// beside it, and waits for it at its end, so that whoever waits for this one has
+// waited for both.
+__device__ __forceinline__ void begin(const Quant4Params& p) {
+  if (!p.overlap) pdl_wait();
+  pdl_trigger();
+}
+__device__ __forceinline__ void end(const Quant4Params& p) {
+  if (p.overlap) pdl_wait();
+}
+
 // the largest of two magnitudes' patterns of a vector
 template <int DT>
 __device__ __forceinline__ uint32_t vec_top(uint4 v) {
@@ -96,8 +107,7 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
   using L = Elem<DT>;
   using T = typename L::T;
   using Col = std::conditional_t<LONG, int64_t, int>;
-  pdl_wait();
-  pdl_trigger();
+  begin(p);
   constexpr int G = TPR < 32 ? TPR : 32, GROUPS = QT / TPR;
   constexpr Col PIECE = TPR * NV * L::E;
   __shared__ uint32_t part[2][QT / 32];
@@ -198,6 +208,7 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
       }
     }
   }
+  end(p);
 }
 
 // ---- columns ------------------------------------------------------------------
@@ -215,8 +226,7 @@ template <int DT, bool GRID, bool PAIRS>
 __global__ void __launch_bounds__(QT) quant4_maxima(Quant4Params p, int64_t wide, int64_t each) {
   using L = Elem<DT>;
   using T = typename L::T;
-  pdl_wait();
-  pdl_trigger();
+  begin(p);
   constexpr int C = GRID ? L::E : (PAIRS ? 2 : 1), W = GRID ? 4 : 1, U = GRID ? 4 : 8, ROWS = QT / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t c0 = ((int64_t)blockIdx.x % wide) * (32 * C) + lane * C, chunk = (int64_t)blockIdx.x / wide;
@@ -266,6 +276,7 @@ __global__ void __launch_bounds__(QT) quant4_maxima(Quant4Params p, int64_t wide
     for (int c = 0; c < PER; c++)
       if (k * PER + c < cols) top[k * PER + c] = DT == PEAT_F32 ? m[k] & 0x7fffffffu : (c ? m[k] >> 16 : m[k]) & 0x7fffu;
   }
+  end(p);
 }
 
 // A warp has 32 rows, a thread the blocks of its columns, 16 bytes of codes each.
@@ -274,8 +285,7 @@ template <int DT, int FMT, bool PAIRS, bool VALUES>
 __global__ void __launch_bounds__(QT) quant4_columns(Quant4Params p, int64_t wide, int chunks) {
   using L = Elem<DT>;
   using T = typename L::T;
-  pdl_wait();
-  pdl_trigger();
+  begin(p);
   constexpr int C = PAIRS ? 2 : 1, BLOCK = F4<FMT>::BLOCK, NB = 32 / BLOCK;
   __shared__ float reciprocals[FMT == PEAT_NVFP4 ? RECIPROCALS : 1];
   __shared__ uint32_t most[FMT == PEAT_NVFP4 ? QT : 1];
@@ -351,6 +361,7 @@ __global__ void __launch_bounds__(QT) quant4_columns(Quant4Params p, int64_t wid
       else *reinterpret_cast<uint2*>(q) = make_uint2(code[c][0], code[c][1]);
     }
   }
+  end(p);  // (mxfp4; nvfp4 needs its maxima first)
   if (!VALUES || cols <= 0) return;
   T* o = static_cast<T*>(p.values) + r0 * p.ldv + c0;
   const bool both = PAIRS && cols > 1 && p.pairs_v;
@@ -413,7 +424,7 @@ cudaError_t rows(const Quant4Params& p, int nsm, cudaStream_t s) {
   return cudaErrorNotSupported;
 }
 template <int DT, int FMT, bool PAIRS>
-cudaError_t columns_by(const Quant4Params& p, int nsm, cudaStream_t s) {
+cudaError_t columns_by(Quant4Params p, int nsm, cudaStream_t s) {
   constexpr int WIDE = PAIRS ? 64 : 32;
   int chunks = 0;
   if (FMT == PEAT_NVFP4) {
@@ -425,6 +436,7 @@ cudaError_t columns_by(const Quant4Params& p, int nsm, cudaStream_t s) {
     cudaError_t e = launch_dependent(grid ? quant4_maxima<DT, true, PAIRS> : quant4_maxima<DT, false, PAIRS>,
                                      (unsigned)(groups * chunks), QT, 0, s, p, groups, each);
     if (e != cudaSuccess) return e;
+    p.overlap = 0;
   }
   const int64_t cols = p.block_scale ? (p.cols + 127) / 128 * 128 : p.cols;
   const int64_t height = p.tiles * 4 * F4<FMT>::BLOCK, wide = (cols + WIDE - 1) / WIDE;
