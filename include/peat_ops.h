@@ -233,7 +233,7 @@ peat_status_t peat_rmsnorm(peat_handle_t h, const void* x, int64_t ldx, const vo
  *   grad_weight = the sum over the rows of grad * n, float32 [cols].
  * (Rounding to 8 bits passes gradients through: grad is then that of values.)  Sums
  * are float32, in an order that depends on the sizes alone.  Each output may be
- * NULL, not both; no rows give grad_weight 0.  grad_x may be grad or grad_sum itself
+ * NULL, not both; no rows give grad_weight 0.  cols <= 2^27.  grad_x may be grad or grad_sum itself
  * (the same rows at the same distance), else no output overlaps an input. */
 peat_status_t peat_rmsnorm_backward(peat_handle_t h, const void* grad, int64_t ldg, const void* grad_sum,
                                     int64_t ldr, const void* x, int64_t ldx, const void* weight,

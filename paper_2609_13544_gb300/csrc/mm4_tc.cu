@@ -61,6 +61,7 @@ struct Tc4Params {
   int64_t tiles;      // of scales along k
   int steps;          // instructions of 64 k
   int bn, pt, qt, stages;
+  int units;          // the output's rows are whole 16-byte units
   int splits;         // CTAs of a cluster that share a tile's k range: 1, 2, 4 or 8 (then a cluster has one tile)
   unsigned int* status;
   uint32_t wait_limit;
@@ -479,6 +480,8 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
           }
         } else {
           uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+          // (a copy out writes whole 16-byte units: the row's last columns go by themselves if they are not)
+          const bool boxed = p.out.vec && (p.units || col0 + STEP <= p.out.N);
 #pragma unroll 1
           for (int h = 0; h < 2; h++) {  // 32 columns at a time
             float v[32];
@@ -494,10 +497,10 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
               if (CG == 2 && part == (acc ? 0 : 3)) released(release_shared);
               if (c + PARTS >= chunks) released(release + 8 * acc);
             }
-            if (p.out.vec) {
+            if (boxed) {
               if (row0 >= p.P) continue;
               put_box<OUT>(box, &mo, v, h, scaled, sp, sq, p.out.biased, bias, row0, col0, p.out.N);
-            } else {  // rows off the 16-byte grid
+            } else {
               const OutPlace off_grid{p.out.out, p.out.ldo, p.out.N, p.out.biased, false};
               put_columns<OUT>(off_grid, v, sp, sq + 32 * h, bias + 32 * h, row0, rows, col0 + 32 * h, h == 0, h == 1, carry);
             }
@@ -712,6 +715,7 @@ cudaError_t launch_mm4(int format, int out_dtype, const Mm4Params& m, unsigned i
   const int results = swap ? Warps<1, true>::BYTES : (cg == 2 ? Warps<2, false>::BYTES : Warps<1, false>::BYTES);
   p.stages = std::min(MOST_STAGES, (SMEM - 1024 - results - BARS) / stage_bytes(p.bn / cg));
   p.out = OutPlace{m.out, m.ldo, m.N, m.bias != nullptr, grid};
+  p.units = m.N * size % 16 == 0;
   p.status = status;
   p.wait_limit = wait_limit;
   Maps maps = {};

@@ -313,6 +313,7 @@ peat_status_t rmsnorm_backward(peat_handle_t h, const void* grad, int64_t ldg, c
   const int B = type_bytes(dtype);
   if (ldg < cols || ldx < cols || (grad_sum && ldr < cols) || (grad_x && ldo < cols))
     return fail(h, PEAT_ERR_INVALID_ARG, "a matrix's row distance is less than a row");
+  if (cols > ((int64_t)1 << 27)) return fail(h, PEAT_ERR_UNSUPPORTED, "cols above 2^27");
   if (cols == 0) return PEAT_OK;
   if (rows > 0 && (!grad || !x || !weight || !rstd)) return fail(h, PEAT_ERR_INVALID_ARG, "grad, x, weight or rstd is NULL");
   if (rows > 0 && !grad_x && !grad_weight) return fail(h, PEAT_ERR_INVALID_ARG, "grad_x and grad_weight are both NULL");

@@ -285,6 +285,13 @@ void operands() {
         take(q.q, rows[i] * q.ldq);
         take(q.block_scale, (rows[i] + 127) / 128 * tiles * 512);
         if (format == PEAT_NVFP4) take(q.scale, rows[i] * 4);
+        if (format == PEAT_NVFP4 && (axes >> i & 1)) {  // the operands' maxima do not meet
+          const uintptr_t lo = reinterpret_cast<uintptr_t>(q.tops);
+          const size_t n = sizeof(unsigned int) * peat::QUANT4_CHUNKS * rows[i];
+          for (const Range& r : used) CHECK(lo >= r.hi || lo + n <= r.lo);
+          used.push_back({lo, lo + n});
+        }
+        CHECK(q.overlap == (i == 1));
         CHECK(q.tiles == tiles && q.ldq % 16 == 0 && q.ldq >= q.width / 2 && (format == PEAT_NVFP4 || !q.scale));
         CHECK((i ? rt.product.b : rt.product.a) == q.q && (i ? rt.product.sb : rt.product.sa) == q.scale);
       }
@@ -413,6 +420,7 @@ void norm_refusals() {
   CHECK(rt.launches == 0);
   CHECK(back(0, 16, nullptr, nullptr, u.floats(), nullptr, 16) == PEAT_OK && rt.launches == 1);  // no rows: the sums are 0
   CHECK(back(0, 16, nullptr, nullptr, nullptr, nullptr, 16) == PEAT_OK && rt.launches == 1);
+  CHECK(back(9, (int64_t)1 << 28, u.data(), u.data(), u.floats(), u.floats(), (int64_t)1 << 28) == PEAT_ERR_UNSUPPORTED);
 }
 
 }  // namespace

@@ -432,13 +432,15 @@ def test_product_refusals(peat_gpu, h):
     torch.cuda.synchronize()
 
 
-def test_expired_wait_is_reported(peat_gpu, h):
-    """A handle whose bounded waits give up at once: the product returns, the next one reports it, and other handles
-    go on."""
+@pytest.mark.parametrize("mnk", [(700, 300, 1024), (16, 700, 512), (16, 500, 8192), (300, 500, 16384), (4096, 4096, 512)])
+def test_expired_wait_is_reported(peat_gpu, h, mnk):
+    """A handle whose bounded waits give up at once: the product returns, the next one reports it, and other handles go
+    on; tiles of a CTA, of few rows, of clusters that share k, of a pair."""
     import torch
     g = rng(3)
-    a, b = random_f4(peat_gpu, 700, 1024, "nvfp4", g), random_f4(peat_gpu, 300, 1024, "nvfp4", g)
-    out = torch.empty(700, 300, device="cuda")
+    M, N, K = mnk
+    a, b = random_f4(peat_gpu, M, K, "nvfp4", g), random_f4(peat_gpu, N, K, "nvfp4", g)
+    out = torch.empty(M, N, device="cuda")
     bad = peat_gpu.Handle(0, flags=peat_gpu.PEAT_FLAG_TEST_EXPIRE_WAITS)
     for _ in range(2):
         peat_gpu.peat_matmul_f4_raw(bad, a, b, out)
@@ -448,7 +450,81 @@ def test_expired_wait_is_reported(peat_gpu, h):
         assert e.value.status == 5
     bad.close()
     peat_gpu.peat_matmul_f4_raw(h, a, b, out)
-    check_product(out, values64(a), values64(b), 1024, "nvfp4")
+    check_product(out, values64(a), values64(b), K, "nvfp4")
+
+
+# tiles by pairs, clusters of two, four and eight that share k, with rows and columns that end inside a tile, and sums
+# that the accumulators' shared columns, several waves and odd tiles go through
+WAYS = [(4096, 4096, 512), (5000, 3001, 96), (2049, 8200, 1056), (16384, 300, 64), (1, 4096, 8192), (16, 4095, 4128),
+        (48, 1000, 8192), (130, 500, 16384), (192, 512, 16384), (500, 520, 8192), (200, 300, 4096), (3, 100, 32768),
+        (33, 9000, 4096), (17, 130, 520 * 32)]
+
+
+@pytest.mark.parametrize("format", FORMATS)
+@pytest.mark.parametrize("mnk", WAYS)
+def test_matmul_ways(peat_gpu, h, format, mnk):
+    import torch
+    M, N, K = mnk
+    g = rng(M + 3 * N + 7 * K)
+    a, b = random_f4(peat_gpu, M, K, format, g), random_f4(peat_gpu, N, K, format, g)
+    x, y = values64(a), values64(b)
+    bias = torch.randn(N, generator=g, device="cuda") * K ** 0.5
+    for bv, out, ldo in ((bias, torch.float32, N), (None, torch.bfloat16, (N + 7) // 8 * 8), (bias, torch.bfloat16, N + 1)):
+        buf = torch.full((M, ldo), 7.0, device="cuda", dtype=out)
+        peat_gpu.peat_matmul_f4_raw(h, a, b, buf[:, :N], bv)
+        check_product(buf[:, :N], x, y, K, format, bv)
+        assert bool((buf[:, N:] == 7).all())
+        again = torch.empty(M, N, device="cuda", dtype=out)
+        peat_gpu.peat_matmul_f4_raw(h, a, b, again, bv)
+        if (ldo * again.element_size() % 16 == 0) == (N * again.element_size() % 16 == 0):
+            assert same_bits(again, buf[:, :N])
+
+
+@pytest.mark.parametrize("n", [1, 2, 3, 5, 9, 33])
+def test_matmul_narrow_outputs(peat_gpu, h, n):
+    """Fewer columns than a 16-byte unit, in rows on that grid."""
+    import torch
+    a, b = random_f4(peat_gpu, 300, 128, "mxfp4", rng(n)), random_f4(peat_gpu, n, 128, "mxfp4", rng(n + 1))
+    for t in (torch.float32, torch.float16, torch.bfloat16):
+        buf = torch.full((301, 40), 7.0, device="cuda", dtype=t)
+        peat_gpu.peat_matmul_f4_raw(h, a, b, buf[:300, :n])
+        if t != torch.float16 or float((values64(a) @ values64(b).t()).abs().max()) < 3e4:
+            check_product(buf[:300, :n], values64(a), values64(b), 128, "mxfp4")
+        assert bool((buf[:, n:] == 7).all()) and bool((buf[300:] == 7).all())
+
+
+@pytest.mark.parametrize("format", FORMATS)
+@pytest.mark.parametrize("m", [5, 300, 3000])
+def test_matmul_scales_of_nan_and_zero(peat_gpu, h, format, m):
+    """A block scale that is NaN makes its row NaN, one that is 0 (nvfp4) or the least (mxfp4) adds nothing."""
+    import torch
+    g = rng(m)
+    a, b = random_f4(peat_gpu, m, 512, format, g), random_f4(peat_gpu, 260, 512, format, g)
+    at = lambda r, k: ((r // 128) * (a.cols // BLOCK[format] // 4) + k // 4) * 512 + r % 32 * 16 + r % 128 // 32 * 4 + k % 4
+    nan = 255 if format == "mxfp4" else 127
+    a.block_scale[at(m - 1, 3)] = nan
+    b.block_scale[at(200, 1)] = nan
+    a.block_scale[at(1, 0)] = 0
+    y = peat_gpu.peat_matmul_f4(h, a, b)
+    bad = torch.isnan(y)
+    assert bool(bad[m - 1].all()) and bool(bad[:, 200].all()) and int(bad.sum()) == m + 260 - 1
+    # (a copy without the NaN, for the rest)
+    a.block_scale[at(m - 1, 3)] = 127 if format == "mxfp4" else 56
+    b.block_scale[at(200, 1)] = 127 if format == "mxfp4" else 56
+    z = peat_gpu.peat_matmul_f4(h, a, b)
+    check_product(z, values64(a), values64(b), 512, format)
+    assert same_bits(z[: m - 1, :200], y[: m - 1, :200])
+
+
+def test_small_and_large_scales(peat_gpu, h):
+    """mxfp4's powers of two over float32's range: sums come out where they fit it, far apart ones too."""
+    import torch
+    for M in (4, 300):
+        a, b = random_f4(peat_gpu, M, 128, "mxfp4", rng(1), 0), random_f4(peat_gpu, 40, 128, "mxfp4", rng(2), 0)
+        for ea, eb in ((-120, 100), (110, -125), (-60, -60), (55, 60), (-100, 0)):
+            a.block_scale.copy_(torch.where(a.block_scale > 0, 127 + ea, 0))
+            b.block_scale.copy_(torch.where(b.block_scale > 0, 127 + eb, 0))
+            check_product(peat_gpu.peat_matmul_f4(h, a, b), values64(a), values64(b), 128, "mxfp4")
 
 
 # ---------------------------------------------------------------------------
