@@ -1,6 +1,7 @@
 /*
  * peat_ops.h -- the operators of libpeat that a playback step runs beside the
- * compare: a linear layer's products in 8-bit integers, and the norm and the
+ * compare: a linear layer's products in 8-bit integers or in 4-bit floating
+ * point, the root-mean-square norm in front of such a layer, and the norm and the
  * clipping of a list of gradients.
  *
  * Playback FI (Alg. 1) computes a layer's forward output, its input gradient
@@ -8,9 +9,12 @@
  * (activation, weight, output gradient), and scores them against the golden
  * ones.  Here the lower precision is 8-bit integers with one scale for each
  * row of either operand: peat_quantize_i8 makes the operands,
- * peat_matmul_i8 multiplies them, peat_product_i8 does both.  A training step
- * ends with the norm over all its gradient tensors, by which they are clipped:
- * peat_grad_norm and peat_grad_clip.
+ * peat_matmul_i8 multiplies them, peat_product_i8 does both.  Or it is 4-bit
+ * floating point with a scale for each short block: peat_quantize_f4,
+ * peat_matmul_f4, peat_product_f4.  What comes into the layer is a norm's output:
+ * peat_rmsnorm makes it, rounded to 8 bits on the way, peat_rmsnorm_backward its
+ * gradients.  A training step ends with the norm over all its gradient tensors,
+ * by which they are clipped: peat_grad_norm and peat_grad_clip.
  *
  * The conventions of peat.h hold: device pointers unless said otherwise,
  * every call asynchronous on `stream`, errors as peat_status_t with the text
@@ -23,8 +27,13 @@
  * calls of this header do not allocate.  A product of many rows takes, with M and
  * N rounded up to 256 and K to 64, 2 (M + N) K bytes, and for K above 1024 20 MB,
  * or where that is more 4 M N bytes for each of the 1, 2 or 4 parts in which K is
- * taken; operands that peat_product_i8 rounds add a byte for each element.  A
- * gradient list takes 32 bytes for each tensor and 100 KB; one of more than 800
+ * taken; operands that peat_product_i8 rounds add a byte for each element.
+ * Operands that peat_product_f4 rounds take 9/16 of a byte for each element (4
+ * bytes a row with PEAT_NVFP4; rounded down the columns, there or in
+ * peat_quantize_f4, 128 bytes for each column more); peat_matmul_f4 and
+ * peat_rmsnorm take none, peat_rmsnorm_backward at most 4 bytes for each column and
+ * each of two CTAs an SM, and 4 a row of more than 8192 elements (float32: 4096).
+ * A gradient list takes 32 bytes for each tensor and 100 KB; one of more than 800
  * takes 40 more for each, and 160 of pinned host memory.
  *
  * The calls can be captured into a CUDA graph, once such a first call has been
@@ -33,9 +42,9 @@
  * The graph uses the handle's workspace: it lives as long as the handle, and its
  * launches and the handle's calls stay in order on the GPU.
  *
- * The waits inside a product of many rows are bounded; should one expire, that
- * call's outputs are invalid, and the next product or compare on the handle
- * returns PEAT_ERR_TIMEOUT once.
+ * The waits inside an 8-bit product of many rows and a 4-bit product are bounded;
+ * should one expire, that call's outputs are invalid, and the next product or
+ * compare on the handle returns PEAT_ERR_TIMEOUT once.
  */
 #ifndef PEAT_OPS_H
 #define PEAT_OPS_H
