@@ -29,10 +29,20 @@ __device__ __forceinline__ void end(const Quant4Params& p) {
   if (p.overlap) pdl_wait();
 }
 
-// the largest of two magnitudes' patterns of a vector
+// the larger magnitude, under some sign; a NaN stays
+template <int DT>
+__device__ __forceinline__ uint32_t max_abs(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (DT == PEAT_F32) asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(*reinterpret_cast<float*>(&r)) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
+  else if (DT == PEAT_F16) asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// the largest magnitude's pattern of a vector
 template <int DT>
 __device__ __forceinline__ uint32_t vec_top(uint4 v) {
-  return mag_fold<DT>(mag_max<DT>(make_uint4(0, 0, 0, 0), v));
+  const uint32_t m = max_abs<DT>(max_abs<DT>(v.x, v.y), max_abs<DT>(v.z, v.w));
+  return DT == PEAT_F32 ? m & 0x7fffffffu : max(m & 0x7fffu, m >> 16 & 0x7fffu);
 }
 
 // where a row's outputs lie
@@ -51,10 +61,11 @@ __device__ __forceinline__ Out4<DT> out_of(const Quant4Params& p, int64_t row, b
   return o;
 }
 
-// one vector of a row: codes, block scale, values; all lanes of a warp together
-template <int DT, int FMT, int G, bool GRID, typename Col>
-__device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Out4<DT>& o, Col col, Col left, const Row4& r,
-                                        const float* reciprocals) {
+// one vector of a row: codes, block scale (at), values; all lanes of a warp together.
+// FULL: the whole group's vectors lie inside the matrix.
+template <int DT, int FMT, int G, bool GRID, bool FULL, typename Col>
+__device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Out4<DT>& o, Col col, Col left, uint8_t* at,
+                                        const Row4& r, const float* reciprocals) {
   using L = Elem<DT>;
   constexpr int LANES = F4<FMT>::BLOCK / L::E;  // that have a block
   uint32_t top = vec_top<DT>(v);
@@ -64,20 +75,21 @@ __device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Ou
   const Block4 b = block4<FMT>(L::mag(top), finite, r, reciprocals);
   float x[L::E];
   unpack<DT>(v, x);
+  if (FMT == PEAT_NVFP4) {
 #pragma unroll
-  for (int e = 0; e < L::E; e++) x[e] = scaled4<FMT>(x[e], r, b);
+    for (int e = 0; e < L::E / 2; e++) put_pair(x, e, mul2(pair(x, e), both(r.t)));
+  }
+#pragma unroll
+  for (int e = 0; e < L::E / 2; e++) put_pair(x, e, mul2(pair(x, e), both(b.r)));
   uint32_t c;
   if constexpr (L::E == 8) c = codes8(x);
   else c = codes4(x[0], x[1], x[2], x[3]);
   c = coded<FMT>(finite, b) ? c : 0;
-  if (o.q && col < (Col)p.width) {
+  if (o.q && (FULL || col < (Col)p.width)) {
     if (L::E == 8) *reinterpret_cast<uint32_t*>(o.q + col / 2) = c;
     else *reinterpret_cast<uint16_t*>(o.q + col / 2) = (uint16_t)c;
   }
-  if (o.block_scale && (threadIdx.x & (LANES - 1)) == 0 && col < (Col)(p.tiles * 4 * F4<FMT>::BLOCK)) {
-    const Col block = col / F4<FMT>::BLOCK;
-    o.block_scale[(int64_t)(block >> 2) * SCALE_TILE + (block & 3)] = (uint8_t)b.byte;
-  }
+  if (o.block_scale && (threadIdx.x & (LANES - 1)) == 0 && (FULL || col < (Col)(p.tiles * 4 * F4<FMT>::BLOCK))) *at = (uint8_t)b.byte;
   if (o.values) {
     float y[L::E], four[4];
 #pragma unroll
@@ -87,7 +99,7 @@ __device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Ou
       for (int i = 0; i < 4; i++) y[e + i] = four[i];
     }
     if constexpr (GRID) {
-      if (left > 0) __stcs(reinterpret_cast<uint4*>(o.values + col), pack<DT>(y));
+      if (FULL || left > 0) __stcs(reinterpret_cast<uint4*>(o.values + col), pack<DT>(y));
     } else {
       uint4 none = make_uint4(0, 0, 0, 0);
       store_values<DT, G>(o.values + col, y, p.vec_v, left, none, true, true);
@@ -201,10 +213,23 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
 #pragma unroll
         for (int i = 0; i < NV; i++) w[i] = v[i];
       }
+      // where the lane's block scales go: a vector further on, whole tiles further (or there is one vector)
+      constexpr int TILE = 4 * F4<FMT>::BLOCK, NEXT = TPR * L::E / TILE;
+      static_assert(NV == 1 || TPR * L::E % TILE == 0, "tiles of scales");
+      const Col block = (at + lane * L::E) / F4<FMT>::BLOCK;
+      uint8_t* scales = o.block_scale + (int64_t)(block >> 2) * SCALE_TILE + (block & 3);
+      if (GRID && at + PIECE <= (Col)p.cols && here < p.rows) {
 #pragma unroll
-      for (int i = 0; i < NV; i++) {
-        const Col begin = at + i * TPR * L::E, col = begin + lane * L::E;
-        if (begin < wide) put_vec<DT, FMT, G, GRID, Col>(p, w[i], o, col, here < p.rows ? cols - col : -16, r, reciprocals);
+        for (int i = 0; i < NV; i++)
+          put_vec<DT, FMT, G, GRID, true, Col>(p, w[i], o, at + (i * TPR + lane) * L::E, 1, scales + i * (NEXT * SCALE_TILE), r, reciprocals);
+      } else {
+#pragma unroll
+        for (int i = 0; i < NV; i++) {
+          const Col begin = at + i * TPR * L::E, col = begin + lane * L::E;
+          if (begin < wide)
+            put_vec<DT, FMT, G, GRID, false, Col>(p, w[i], o, col, here < p.rows ? cols - col : -16, scales + i * (NEXT * SCALE_TILE), r,
+                                                  reciprocals);
+        }
       }
     }
   }
