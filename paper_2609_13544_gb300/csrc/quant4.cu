@@ -29,22 +29,6 @@ __device__ __forceinline__ void end(const Quant4Params& p) {
   if (p.overlap) pdl_wait();
 }
 
-// the larger magnitude, under some sign; a NaN stays
-template <int DT>
-__device__ __forceinline__ uint32_t max_abs(uint32_t a, uint32_t b) {
-  uint32_t r;
-  if (DT == PEAT_F32) asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(*reinterpret_cast<float*>(&r)) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)));
-  else if (DT == PEAT_F16) asm("max.NaN.xorsign.abs.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  else asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// the largest magnitude's pattern of a vector
-template <int DT>
-__device__ __forceinline__ uint32_t vec_top(uint4 v) {
-  const uint32_t m = max_abs<DT>(max_abs<DT>(v.x, v.y), max_abs<DT>(v.z, v.w));
-  return DT == PEAT_F32 ? m & 0x7fffffffu : max(m & 0x7fffu, m >> 16 & 0x7fffu);
-}
-
 // where a row's outputs lie
 template <int DT>
 struct Out4 {

@@ -204,10 +204,10 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) 
       if (!LONG && row0 + step < p.rows) fetch(row + step, 0);
       // Squares on top of one that none exceeds: what a sum's rounding leaves of a
       // square is then the difference of two sums away (Dekker's short form)
-      uint4 m = make_uint4(0, 0, 0, 0);
+      uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < NV; i++) m = mag_max<DT>(m, v[i]);
-      const float most = L::mag(mag_fold<DT>(m)), base = __fmul_ru(most, most);
+      for (int i = 0; i < NV; i++) top = max(top, vec_top<DT>(v[i]));
+      const float most = L::mag(top), base = __fmul_ru(most, most);
       float2 t = both(base), rest = both(0.0f);
 #pragma unroll
       for (int i = 0; i < NV; i++) {
