@@ -129,7 +129,7 @@ __device__ __forceinline__ void weights(const void* w, int f32, bool vec, int64_
 // loads are under way while this one's factors are found.  LONG: rows that these
 // threads do not hold, read again for each of the three passes.
 template <int DT, int TPR, int NV, bool GRID, bool LONG>
-__global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : 3) rms_forward(RmsParams p) {
+__global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR <= 64 ? 3 : 4) rms_forward(RmsParams p) {
   using L = Elem<DT>;
   using T = typename L::T;
   using Col = std::conditional_t<LONG, int64_t, int>;
@@ -549,8 +549,11 @@ __global__ void __launch_bounds__(1024) rms_weight_sums(const float* parts, int 
 template <int DT, int TPR, int NV, bool LONG = false>
 cudaError_t forward(const RmsParams& p, int nsm, cudaStream_t s) {
   constexpr int QT = threads_of<TPR>();
-  // as many CTAs as are at work at once
-  const unsigned grid = (unsigned)std::min<int64_t>((p.rows + QT / TPR - 1) / (QT / TPR), (int64_t)nsm * (TPR > 256 ? 2 : 3));
+  // As many CTAs as are at work at once; without the rounding, which is bound by its
+  // instructions, one less (16384 x 4096 bfloat16 with the residual: 8 bits 88 us, with
+  // three CTAs an SM 96; y 82 to 85, with four 90).
+  const unsigned grid = (unsigned)std::min<int64_t>((p.rows + QT / TPR - 1) / (QT / TPR),
+                                                    (int64_t)nsm * (TPR > 256 ? 2 : p.q || p.values ? 4 : 3));
   if (p.grid) return launch_dependent(rms_forward<DT, TPR, NV, true, LONG>, grid, QT, 0, s, p);
   return launch_dependent(rms_forward<DT, TPR, NV, false, LONG>, grid, QT, 0, s, p);
 }

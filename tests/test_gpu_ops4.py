@@ -937,7 +937,9 @@ def test_rows_past_32_bit_offsets(peat_gpu, h):
         t = peat_gpu.peat_quantize_f4(h, tail, format)
         assert torch.equal(a.q[-200:], t.q)
         y = peat_gpu.peat_matmul_f4(h, a, b)
-        assert same_bits(y[-200:], peat_gpu.peat_matmul_f4(h, t, b)) and not bool(y[:-200].any())
+        # (against the 64-bit product: a call of other sizes may add in another order)
+        check_product(y[-200:], values64(t), values64(b), cols, format)
+        assert not bool(y[:-200].any())
         del a, y
     one = torch.ones(cols, device="cuda")
     got = peat_gpu.peat_rmsnorm(h, x, one)
