@@ -2,6 +2,8 @@
 // magnitudes, rounding to 8-bit integers, loads and stores at any multiple of the
 // element's size.
 #pragma once
+#include <type_traits>
+
 #include "vec16.cuh"
 
 namespace peat {
@@ -200,6 +202,64 @@ __device__ __forceinline__ void store_values(typename Elem<DT>::T* o, const floa
     for (int e = 0; e < E; e++)
       if (e >= E - s && e < left) o[e] = v.e[e];
   }
+}
+
+// E elements of a row, APART columns from one to the next, as a vector; and back.  A
+// warp's are side by side, whatever the row's alignment.
+template <int DT, int APART, typename Col>
+__device__ __forceinline__ uint4 load_apart(const typename Elem<DT>::T* row, Col col, Col cols) {
+  using U = std::conditional_t<DT == PEAT_F32, uint32_t, uint16_t>;
+  constexpr int E = Elem<DT>::E, PER = DT == PEAT_F32 ? 1 : 2;
+  uint32_t w[4] = {0, 0, 0, 0};
+  const U* p = reinterpret_cast<const U*>(row + col);
+  U x[E];
+  if (col + (E - 1) * APART < cols) {  // (without a condition on each load, or they wait for one another)
+#pragma unroll
+    for (int e = 0; e < E; e++) x[e] = p[e * APART];
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e++) x[e] = col + e * APART < cols ? p[e * APART] : (U)0;
+  }
+#pragma unroll
+  for (int e = 0; e < E; e++) w[e / PER] |= (uint32_t)x[e] << (e % PER * 16);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+template <int DT, int APART, typename Col>
+__device__ __forceinline__ void put_apart(typename Elem<DT>::T* row, uint4 u, Col col, Col cols) {
+  Vec<DT> v;
+  v.u = u;
+  typename Elem<DT>::T* o = row + col;
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::E; e++)
+    if (col + e * APART < cols) o[e * APART] = v.e[e];
+}
+// Between such vectors and those of consecutive elements, G lanes' at a time, by way
+// of `place` (16 bytes a lane of the warp); all lanes of the warp together.
+template <int DT, int G>
+__device__ __forceinline__ uint4 gathered(uint4 u, uint4* place) {
+  using T = typename Elem<DT>::T;
+  const int lane = threadIdx.x & (G - 1);
+  uint4* mine = place + (threadIdx.x & 31 & ~(G - 1));
+  Vec<DT> v;
+  v.u = u;
+  __syncwarp();
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::E; e++) reinterpret_cast<T*>(mine)[e * G + lane] = v.e[e];
+  __syncwarp();
+  return mine[lane];
+}
+template <int DT, int G>
+__device__ __forceinline__ uint4 spread(uint4 u, uint4* place) {
+  using T = typename Elem<DT>::T;
+  const int lane = threadIdx.x & (G - 1);
+  uint4* mine = place + (threadIdx.x & 31 & ~(G - 1));
+  __syncwarp();
+  mine[lane] = u;
+  __syncwarp();
+  Vec<DT> v;
+#pragma unroll
+  for (int e = 0; e < Elem<DT>::E; e++) v.e[e] = reinterpret_cast<const T*>(mine)[e * G + lane];
+  return v.u;
 }
 
 }  // namespace peat

@@ -69,59 +69,58 @@ __device__ __forceinline__ float sum_plain(float x, float* part) {
   }
   return x;
 }
-// GRID: every matrix's rows start on 16-byte boundaries and are whole vectors
-template <int DT, bool GRID>
-__device__ __forceinline__ uint4 load_vec(const Source<DT, GRID>& s, const typename Elem<DT>::T* p, int64_t left) {
-  if constexpr (GRID) return left > 0 ? s.load(p) : make_uint4(0, 0, 0, 0);
-  if (s.whole(p, left)) return s.load(p);
-  return left > 0 ? load_edge<DT>(p, left) : make_uint4(0, 0, 0, 0);
-}
-template <int DT, bool GRID>
-__device__ __forceinline__ void put_vec(typename Elem<DT>::T* o, const float (&y)[Elem<DT>::E], bool on_grid, int64_t left) {
+// A thread's E elements of a row of `cols`.  GRID (every matrix's rows start on
+// 16-byte boundaries and are whole vectors): a vector from column `col` on.  Off the
+// grid: elements `APART` columns apart, so that a warp's are side by side, whatever
+// the alignment (10273 x 3863 bfloat16, 8-bit values with the residual: 104 us; by
+// vectors shifted together from aligned ones 142).
+template <int DT, bool GRID, int APART, typename Col>
+__device__ __forceinline__ uint4 load_vec(const typename Elem<DT>::T* row, Col col, Col cols) {
   if constexpr (GRID) {
-    if (left > 0) __stcs(reinterpret_cast<uint4*>(o), pack<DT>(y));
+    return col < cols ? __ldg(reinterpret_cast<const uint4*>(row + col)) : make_uint4(0, 0, 0, 0);
   } else {
-    uint4 none = make_uint4(0, 0, 0, 0);
-    store_values<DT, 32>(o, y, on_grid, left, none, true, true);
+    return load_apart<DT, APART>(row, col, cols);
   }
 }
-// a vector of a matrix that this kernel has written (the thread's own elements)
-template <int DT>
-__device__ __forceinline__ uint4 load_own(const typename Elem<DT>::T* p, int64_t left, bool on_grid) {
-  Vec<DT> v;
-  v.u = make_uint4(0, 0, 0, 0);
-  if (on_grid && left >= Elem<DT>::E) {
-    v.u = *reinterpret_cast<const uint4*>(p);
+template <int DT, bool GRID, int APART, typename Col>
+__device__ __forceinline__ void put_vec(typename Elem<DT>::T* row, const float (&y)[Elem<DT>::E], Col col, Col cols) {
+  if constexpr (GRID) {
+    if (col < cols) __stcs(reinterpret_cast<uint4*>(row + col), pack<DT>(y));
   } else {
-#pragma unroll
-    for (int e = 0; e < Elem<DT>::E; e++)
-      if (e < left) v.e[e] = p[e];
+    put_apart<DT, APART>(row, pack<DT>(y), col, cols);
   }
-  return v.u;
 }
-// E weights from column col on
-template <int DT, bool GRID>
-__device__ __forceinline__ void weights(const void* w, int f32, bool vec, int64_t col, int64_t cols, float (&x)[Elem<DT>::E]) {
+// the weights of these columns
+template <int DT, bool GRID, int APART, typename Col>
+__device__ __forceinline__ void weights(const void* w, int f32, Col col, Col cols, float (&x)[Elem<DT>::E]) {
   constexpr int E = Elem<DT>::E;
-  const int64_t left = cols - col;
   if (DT != PEAT_F32 && !f32) {
-    const typename Elem<DT>::T* p = static_cast<const typename Elem<DT>::T*>(w) + col;
-    unpack<DT>((GRID ? left > 0 : vec && left >= E) ? __ldg(reinterpret_cast<const uint4*>(p))
-               : !GRID && left > 0                  ? load_edge<DT>(p, left)
-                                                    : make_uint4(0, 0, 0, 0), x);
+    unpack<DT>(load_vec<DT, GRID, APART>(static_cast<const typename Elem<DT>::T*>(w), col, cols), x);
     return;
   }
-  const float* p = static_cast<const float*>(w) + col;
-  if (GRID ? left > 0 : vec && left >= E) {
+  const float* p = static_cast<const float*>(w);
+  if constexpr (GRID) {
 #pragma unroll
     for (int e = 0; e < E; e += 4) {
-      const float4 f = __ldg(reinterpret_cast<const float4*>(p + e));
+      const float4 f = col < cols ? __ldg(reinterpret_cast<const float4*>(p + col + e)) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       x[e] = f.x, x[e + 1] = f.y, x[e + 2] = f.z, x[e + 3] = f.w;
     }
   } else {
+    if (col + (E - 1) * APART < cols) {
 #pragma unroll
-    for (int e = 0; e < E; e++) x[e] = !GRID && e < left ? __ldg(p + e) : 0.0f;
+      for (int e = 0; e < E; e++) x[e] = __ldg(p + col + e * APART);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e++) x[e] = col + e * APART < cols ? __ldg(p + col + e * APART) : 0.0f;
+    }
   }
+}
+
+// a vector of a matrix that this kernel has written (the thread's own elements)
+template <int DT, bool GRID, int APART, typename Col>
+__device__ __forceinline__ uint4 load_own(const typename Elem<DT>::T* row, Col col, Col cols) {
+  if constexpr (GRID) return col < cols ? *reinterpret_cast<const uint4*>(row + col) : make_uint4(0, 0, 0, 0);
+  else return load_vec<DT, GRID, APART>(row, col, cols);
 }
 
 // ---- forward ------------------------------------------------------------------
@@ -143,28 +142,26 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR
   pdl_trigger();
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const Col end = LONG ? (Col)p.cols : 1;
-  const Source<DT, GRID> sx(p.x, p.rows, p.cols, p.ldx), sr(p.residual, p.rows, p.cols, p.ldr);
   const bool round = p.q || p.values || p.scale;
   uint4 s[NV], u[NV];
-  auto column = [&](Col at, int i) { return at + (i * TPR + lane) * E; };
+  auto column = [&](Col at, int i) { return at + (GRID ? (i * TPR + lane) * E : i * TPR * E + lane); };
   auto fetch = [&](int64_t row, Col at) {
     const Col cols = row < p.rows ? (Col)p.cols : 0;
     const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+    const T* r = static_cast<const T*>(p.residual) + row * p.ldr;
     if (GRID && at + (Col)PIECE <= cols) {  // (without a condition on each load, or they wait for one another)
 #pragma unroll
-      for (int i = 0; i < NV; i++) s[i] = sx.load(x + column(at, i));
+      for (int i = 0; i < NV; i++) s[i] = __ldg(reinterpret_cast<const uint4*>(x + column(at, i)));
       if (!p.residual) return;
-      const T* r = static_cast<const T*>(p.residual) + row * p.ldr;
 #pragma unroll
-      for (int i = 0; i < NV; i++) u[i] = sr.load(r + column(at, i));
+      for (int i = 0; i < NV; i++) u[i] = __ldg(reinterpret_cast<const uint4*>(r + column(at, i)));
       return;
     }
 #pragma unroll
-    for (int i = 0; i < NV; i++) s[i] = load_vec<DT, GRID>(sx, x + column(at, i), cols - column(at, i));
+    for (int i = 0; i < NV; i++) s[i] = load_vec<DT, GRID, TPR>(x, column(at, i), cols);
     if (!p.residual) return;
-    const T* r = static_cast<const T*>(p.residual) + row * p.ldr;
 #pragma unroll
-    for (int i = 0; i < NV; i++) u[i] = load_vec<DT, GRID>(sr, r + column(at, i), cols - column(at, i));
+    for (int i = 0; i < NV; i++) u[i] = load_vec<DT, GRID, TPR>(r, column(at, i), cols);
   };
   auto added = [&](uint4 (&v)[NV]) {  // s = x + residual, rounded to the type
 #pragma unroll
@@ -195,7 +192,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR
         return;
       }
 #pragma unroll
-      for (int i = 0; i < NV; i++) v[i] = load_own<DT>(sum + column(at, i), cols - column(at, i), p.vec_s);
+      for (int i = 0; i < NV; i++) v[i] = load_own<DT, GRID, TPR>(sum, column(at, i), cols);
     };
     float hi = 0.0f, lo = 0.0f;
     for (Col at = 0; at < end; at += (Col)PIECE) {
@@ -213,7 +210,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR
       for (int i = 0; i < NV; i++) {
         float a[E];
         unpack<DT>(v[i], a);
-        if (sum) put_vec<DT, GRID>(sum + column(at, i), a, p.vec_s, live ? cols - column(at, i) : -16);
+        if (sum) put_vec<DT, GRID, TPR>(sum, a, column(at, i), cols);
 #pragma unroll
         for (int e = 0; e < E / 2; e++) {
           const float2 x = pair(a, e), w = fma2(x, x, t);
@@ -284,7 +281,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR
 #pragma unroll
       for (int i = 0; i < NV; i++) {
         float w[E];
-        weights<DT, GRID>(p.weight, p.weight_f32, p.vec_w, column(at, i), p.cols, w);
+        weights<DT, GRID, TPR>(p.weight, p.weight_f32, column(at, i), (Col)p.cols, w);
         unpack<DT>(v[i], y[i]);
 #pragma unroll
         for (int e = 0; e < E / 2; e++) put_pair(y[i], e, mul2(mul2(pair(y[i], e), both(rstd)), pair(w, e)));
@@ -327,8 +324,8 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR
       }
 #pragma unroll
       for (int i = 0; i < NV; i++) {
-        const Col col = column(at, i), left = live ? (Col)p.cols - col : -16;
-        if (p.y) put_vec<DT, GRID>(static_cast<T*>(p.y) + row * p.ldy + col, y[i], p.vec_y, left);
+        const Col col = column(at, i);
+        if (p.y) put_vec<DT, GRID, TPR>(static_cast<T*>(p.y) + row * p.ldy, y[i], col, cols);
         if (!p.q && !p.values) continue;
         float w[E];
         if (finite) {
@@ -342,22 +339,24 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR
         }
         if (p.q) {
           int8_t* q = p.q + row * p.ldq + col;
-          if (GRID ? left > 0 : p.vec_q && left >= E) {
-            if (E == 8)
-              *reinterpret_cast<uint2*>(q) = make_uint2(pack4(w[0], w[1], w[2], w[3]), pack4(w[4 % E], w[5 % E], w[6 % E], w[7 % E]));
-            else
-              *reinterpret_cast<uint32_t*>(q) = pack4(w[0], w[1], w[2], w[3]);
-          } else if (!GRID) {
+          if constexpr (GRID) {
+            if (col < cols) {
+              if (E == 8)
+                *reinterpret_cast<uint2*>(q) = make_uint2(pack4(w[0], w[1], w[2], w[3]), pack4(w[4 % E], w[5 % E], w[6 % E], w[7 % E]));
+              else
+                *reinterpret_cast<uint32_t*>(q) = pack4(w[0], w[1], w[2], w[3]);
+            }
+          } else {
 #pragma unroll
             for (int e = 0; e < E; e++)
-              if (e < left) q[e] = byte_of(w[e]);
+              if (col + e * TPR < cols) q[e * TPR] = byte_of(w[e]);
           }
         }
         if (p.values) {
           float z[E];
 #pragma unroll
           for (int e = 0; e < E / 2; e++) put_pair(z, e, mul2(add2(pair(w, e), both(-MAGIC)), both(scale)));
-          put_vec<DT, GRID>(static_cast<T*>(p.values) + row * p.ldv + col, z, p.vec_v, left);
+          put_vec<DT, GRID, TPR>(static_cast<T*>(p.values) + row * p.ldv, z, col, cols);
         }
       }
     }
@@ -385,12 +384,12 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
   const float n_cols = (float)(int)p.cols;
   const Col at = LONG ? (Col)blockIdx.y * (TPR * NV * E) : 0;
   const int64_t row0 = ((int64_t)blockIdx.x * GROUPS + group) * p.each;
-  const Source<DT, GRID> sg(p.grad, p.rows, p.cols, p.ldg), sx(p.x, p.rows, p.cols, p.ldx), st(p.stream, p.rows, p.cols, p.ldr);
-  auto column = [&](int i) { return at + (i * TPR + lane) * E; };
+  constexpr int STEP = GRID ? 1 : TPR;  // columns from one element of a vector to the next
+  auto column = [&](int i) { return at + (GRID ? (i * TPR + lane) * E : i * TPR * E + lane); };
   float dw[NV][E], w[NV][E];
 #pragma unroll
   for (int i = 0; i < NV; i++) {
-    weights<DT, GRID>(p.weight, p.weight_f32, p.vec_w, column(i), p.cols, w[i]);
+    weights<DT, GRID, TPR>(p.weight, p.weight_f32, column(i), (Col)p.cols, w[i]);
 #pragma unroll
     for (int e = 0; e < E; e++) dw[i][e] = 0.0f;
   }
@@ -401,27 +400,27 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
     const T* dp = static_cast<const T*>(p.grad) + row * p.ldg;
     const T* xp = static_cast<const T*>(p.x) + row * p.ldx;
     rstd_next = row < p.rows ? __ldg(p.rstd + row) : 0.0f;
+    const bool streams = p.stream && p.grad_x;
+    const T* tp = static_cast<const T*>(p.stream) + row * p.ldr;
     if (GRID && at + TPR * NV * E <= cols) {  // (without a condition on each load, or they wait for one another)
 #pragma unroll
       for (int i = 0; i < NV; i++) {
-        d[i] = sg.load(dp + column(i));
-        s[i] = sx.load(xp + column(i));
+        d[i] = __ldg(reinterpret_cast<const uint4*>(dp + column(i)));
+        s[i] = __ldg(reinterpret_cast<const uint4*>(xp + column(i)));
       }
-      if (!p.stream || !p.grad_x) return;
-      const T* tp = static_cast<const T*>(p.stream) + row * p.ldr;
+      if (!streams) return;
 #pragma unroll
-      for (int i = 0; i < NV; i++) u[i] = st.load(tp + column(i));
+      for (int i = 0; i < NV; i++) u[i] = __ldg(reinterpret_cast<const uint4*>(tp + column(i)));
       return;
     }
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-      d[i] = load_vec<DT, GRID>(sg, dp + column(i), cols - column(i));
-      s[i] = load_vec<DT, GRID>(sx, xp + column(i), cols - column(i));
+      d[i] = load_vec<DT, GRID, TPR>(dp, column(i), cols);
+      s[i] = load_vec<DT, GRID, TPR>(xp, column(i), cols);
     }
-    if (!p.stream || !p.grad_x) return;
-    const T* tp = static_cast<const T*>(p.stream) + row * p.ldr;
+    if (!streams) return;
 #pragma unroll
-    for (int i = 0; i < NV; i++) u[i] = load_vec<DT, GRID>(st, tp + column(i), cols - column(i));
+    for (int i = 0; i < NV; i++) u[i] = load_vec<DT, GRID, TPR>(tp, column(i), cols);
   };
   fetch(row0);
   for (int64_t it = 0; it < p.each; it++) {
@@ -462,7 +461,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
 #pragma unroll
         for (int e = 0; e < E / 2; e++) put_pair(b, e, add2(pair(b, e), pair(t, e)));
       }
-      put_vec<DT, GRID>(static_cast<T*>(p.grad_x) + row * p.ldo + column(i), b, p.vec_o, live ? (Col)p.cols - column(i) : -16);
+      put_vec<DT, GRID, TPR>(static_cast<T*>(p.grad_x) + row * p.ldo, b, column(i), live ? (Col)p.cols : (Col)0);
     }
   }
   if (!p.grad_weight) return;
@@ -487,7 +486,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
   for (int i = 0; i < NV; i++)
 #pragma unroll
     for (int e = 0; e < E; e++)
-      if (column(i) + e < p.cols) o[column(i) + e] = dw[i][e];
+      if (column(i) + e * STEP < p.cols) o[column(i) + e * STEP] = dw[i][e];
 }
 
 // sum (g n) / cols of each row, by a CTA
@@ -499,21 +498,35 @@ __global__ void __launch_bounds__(256) rms_dots(RmsBackParams p) {
   pdl_wait();
   pdl_trigger();
   const int64_t row = blockIdx.x;
-  const Source<DT, GRID> sg(p.grad, p.rows, p.cols, p.ldg), sx(p.x, p.rows, p.cols, p.ldx);
   const T* dp = static_cast<const T*>(p.grad) + row * p.ldg;
   const T* xp = static_cast<const T*>(p.x) + row * p.ldx;
   const float rstd = __ldg(p.rstd + row);
   float c = 0.0f;
-  for (int64_t col = (int64_t)threadIdx.x * E; col < p.cols; col += 256 * E) {
+  auto place = [&](int64_t at) { return at + (GRID ? threadIdx.x * E : threadIdx.x); };
+  auto add = [&](uint4 d, uint4 x, int64_t at) {
     float a[E], b[E], w[E];
-    unpack<DT>(load_vec<DT, GRID>(sg, dp + col, p.cols - col), a);
-    unpack<DT>(load_vec<DT, GRID>(sx, xp + col, p.cols - col), b);
-    weights<DT, GRID>(p.weight, p.weight_f32, p.vec_w, col, p.cols, w);
+    unpack<DT>(d, a);
+    unpack<DT>(x, b);
+    weights<DT, GRID, 256>(p.weight, p.weight_f32, place(at), p.cols, w);
     float part = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; e++) part = __fmaf_rn(__fmul_rn(a[e], w[e]), __fmul_rn(b[e], rstd), part);
     c += part;
+  };
+  constexpr int U = GRID ? 4 : 1, PIECE = 256 * E;
+  int64_t at = 0;
+  for (; at + U * PIECE <= p.cols; at += U * PIECE) {  // (whole pieces: loads in a batch)
+    uint4 d[U], x[U];
+#pragma unroll
+    for (int k = 0; k < U; k++) {
+      d[k] = load_vec<DT, GRID, 256>(dp, place(at + k * PIECE), p.cols);
+      x[k] = load_vec<DT, GRID, 256>(xp, place(at + k * PIECE), p.cols);
+    }
+#pragma unroll
+    for (int k = 0; k < U; k++) add(d[k], x[k], at + k * PIECE);
   }
+  for (; at < p.cols; at += PIECE)
+    add(load_vec<DT, GRID, 256>(dp, place(at), p.cols), load_vec<DT, GRID, 256>(xp, place(at), p.cols), at);
   c = sum_plain<256>(c, parts);
   if (threadIdx.x == 0) p.dots[row] = c / (float)(int)p.cols;
 }
