@@ -49,9 +49,10 @@ __device__ __forceinline__ Out4<DT> out_of(const Quant4Params& p, int64_t row, b
 // FULL: the whole group's vectors lie inside the matrix.
 template <int DT, int FMT, int G, bool GRID, bool FULL, typename Col>
 __device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Out4<DT>& o, Col col, Col left, uint8_t* at,
-                                        const Row4& r, const float* reciprocals) {
+                                        const Row4& r, const float* reciprocals, uint4* place) {
   using L = Elem<DT>;
   constexpr int LANES = F4<FMT>::BLOCK / L::E;  // that have a block
+  if (!GRID) v = gathered<DT, G>(v, place);
   uint32_t top = vec_top<DT>(v);
 #pragma unroll
   for (int n = 1; n < LANES; n *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, n));
@@ -85,8 +86,9 @@ __device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Ou
     if constexpr (GRID) {
       if (FULL || left > 0) __stcs(reinterpret_cast<uint4*>(o.values + col), pack<DT>(y));
     } else {
-      uint4 none = make_uint4(0, 0, 0, 0);
-      store_values<DT, G>(o.values + col, y, p.vec_v, left, none, true, true);
+      // (the group's first column, its lanes' elements side by side)
+      const Col lane = threadIdx.x & (G - 1);
+      put_apart<DT, G>(o.values + (col - lane * L::E), spread<DT, G>(pack<DT>(y), place), lane, left + lane * L::E);
     }
   }
 }
@@ -107,6 +109,8 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
   constexpr int G = TPR < 32 ? TPR : 32, GROUPS = QT / TPR;
   constexpr Col PIECE = TPR * NV * L::E;
   __shared__ uint32_t part[2][QT / 32];
+  __shared__ uint4 places[GRID ? 1 : QT];
+  uint4* place = places + (GRID ? 0 : threadIdx.x & ~31);
   __shared__ float reciprocals[FMT == PEAT_NVFP4 ? RECIPROCALS : 1];
   if (FMT == PEAT_NVFP4) {
     make_reciprocals(reciprocals);
@@ -126,13 +130,12 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
     }
 #pragma unroll
     for (int i = 0; i < NV; i++) {
-      const Col col = at + (i * TPR + lane) * L::E;
-      v[i] = make_uint4(0, 0, 0, 0);
       if constexpr (GRID) {
-        if (col < cols) v[i] = source.load(x + col);
-      } else {
-        if (source.whole(x + col, cols - col)) v[i] = source.load(x + col);
-        else if (col < cols) v[i] = load_edge<DT>(x + col, cols - col);
+        const Col col = at + (i * TPR + lane) * L::E;
+        v[i] = col < cols ? source.load(x + col) : make_uint4(0, 0, 0, 0);
+      } else {  // a group's elements side by side; gathered before their use
+        const Col begin = at + (i * TPR + lane / G * G) * L::E;
+        v[i] = load_apart<DT, G, Col>(x, begin + (lane & (G - 1)), cols);
       }
     }
   };
@@ -190,7 +193,8 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
       if (p.scale && lane == 0 && here < p.rows) p.scale[here] = r.s;
     }
     const Out4<DT> o = out_of<DT>(p, here, margin);
-    const Col cols = here < p.rows ? (Col)p.cols : -16;
+    const Col cols = (Col)p.cols;
+    constexpr Col NONE = -(1 << 28);  // elements left of a row that is not the matrix's, seen from any lane's column
     for (Col at = at0; at < (LONG ? wide : at0 + 1); at += PIECE) {
       if (LONG) {
         load(here, at);
@@ -205,14 +209,14 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
       if (GRID && at + PIECE <= (Col)p.cols && here < p.rows) {
 #pragma unroll
         for (int i = 0; i < NV; i++)
-          put_vec<DT, FMT, G, GRID, true, Col>(p, w[i], o, at + (i * TPR + lane) * L::E, 1, scales + i * (NEXT * SCALE_TILE), r, reciprocals);
+          put_vec<DT, FMT, G, GRID, true, Col>(p, w[i], o, at + (i * TPR + lane) * L::E, 1, scales + i * (NEXT * SCALE_TILE), r, reciprocals, place);
       } else {
 #pragma unroll
         for (int i = 0; i < NV; i++) {
           const Col begin = at + i * TPR * L::E, col = begin + lane * L::E;
           if (begin < wide)
-            put_vec<DT, FMT, G, GRID, false, Col>(p, w[i], o, col, here < p.rows ? cols - col : -16, scales + i * (NEXT * SCALE_TILE), r,
-                                                  reciprocals);
+            put_vec<DT, FMT, G, GRID, false, Col>(p, w[i], o, col, here < p.rows ? cols - col : NONE, scales + i * (NEXT * SCALE_TILE), r,
+                                                  reciprocals, place);
         }
       }
     }
