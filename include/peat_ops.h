@@ -167,7 +167,8 @@ static inline int64_t peat_f4_scale_bytes(int64_t rows, int64_t blocks) {
  *   values       [rows, cols] of x's type, row r at values + r * ldv: the code's
  *                value times 2^e, or times b, times scale (each product rounded),
  *                rounded to the type.
- * The outputs must not overlap x.  Fastest with 16-byte aligned rows. */
+ * The outputs must not overlap x; at most 2^30 along the product's axis.  Fastest
+ * with 16-byte aligned rows. */
 peat_status_t peat_quantize_f4(peat_handle_t h, const void* x, int64_t rows, int64_t cols, int64_t ldx,
                                peat_dtype_t dtype, peat_f4_t format, int axis, uint8_t* q, int64_t ldq,
                                uint8_t* block_scale, float* scale, void* values, int64_t ldv, peat_stream_t stream);
@@ -242,8 +243,9 @@ peat_status_t peat_rmsnorm(peat_handle_t h, const void* x, int64_t ldx, const vo
  *   grad_weight = the sum over the rows of grad * n, float32 [cols].
  * (Rounding to 8 bits passes gradients through: grad is then that of values.)  Sums
  * are float32, in an order that depends on the sizes alone.  Each output may be
- * NULL, not both; no rows give grad_weight 0.  cols <= 2^27.  grad_x may be grad or grad_sum itself
- * (the same rows at the same distance), else no output overlaps an input. */
+ * NULL, not both; no rows give grad_weight 0.  cols <= 2^27.  grad_x may be grad or
+ * grad_sum itself (the same rows at the same distance), else no output overlaps an
+ * input. */
 peat_status_t peat_rmsnorm_backward(peat_handle_t h, const void* grad, int64_t ldg, const void* grad_sum,
                                     int64_t ldr, const void* x, int64_t ldx, const void* weight,
                                     peat_dtype_t weight_dtype, const float* rstd, int64_t rows, int64_t cols,

@@ -21,6 +21,7 @@ using peat::type_bytes;
 
 // (rows are counted in 32 bits with their margins)
 constexpr int64_t MAX_ROWS = peat::MAX_DIM - 255;
+constexpr int64_t MAX_K = (int64_t)1 << 30;
 
 int64_t block_of(int format) { return format == PEAT_MXFP4 ? 32 : 16; }
 int64_t blocks_of(int format, int64_t k) { return (k + block_of(format) - 1) / block_of(format); }
@@ -40,6 +41,7 @@ peat_status_t quant_params(peat_handle_t h, const void* x, int64_t rows, int64_t
   if (ldx < cols) return fail(h, PEAT_ERR_INVALID_ARG, "ldx < cols");
   if (format == PEAT_MXFP4 && scale) return fail(h, PEAT_ERR_INVALID_ARG, "PEAT_MXFP4 has no float32 scales");
   const int64_t k = axis ? rows : cols, width = blocks_of(format, k) * block_of(format);
+  if (k > MAX_K) return fail(h, PEAT_ERR_UNSUPPORTED, "more than 2^30 along the product's axis");
   if (q && (ldq < width / 2 || (ldq % 16 && (axis ? cols : rows) > 1) || !aligned(q, 16)))
     return fail(h, PEAT_ERR_INVALID_ARG, "q's rows must hold whole blocks and start on 16-byte boundaries");
   if (block_scale && !aligned(block_scale, 16)) return fail(h, PEAT_ERR_INVALID_ARG, "block_scale must be 16-byte aligned");
@@ -107,12 +109,12 @@ peat_status_t quantize(peat_handle_t h, const void* x, int64_t rows, int64_t col
 }
 
 // checks of a product's output and sizes
-peat_status_t product_ok(peat_handle_t h, int format, const float* sa, const float* sb, const float* bias, int64_t M, int64_t N,
+peat_status_t product_ok(peat_handle_t h, const float* sa, const float* sb, const float* bias, int64_t M, int64_t N,
                          int64_t K, const void* out, int64_t ldo, int out_dtype) {
   const int B = type_bytes(out_dtype);
   if (!B) return fail(h, PEAT_ERR_INVALID_ARG, "out_dtype must be PEAT_F32, PEAT_F16 or PEAT_BF16");
   if (ldo < N) return fail(h, PEAT_ERR_INVALID_ARG, "ldo is less than a row");
-  if (M > MAX_ROWS || N > MAX_ROWS || K > ((int64_t)1 << 30))
+  if (M > MAX_ROWS || N > MAX_ROWS || K > MAX_K)
     return fail(h, PEAT_ERR_UNSUPPORTED, "M or N above 2^31 - 256, or K above 2^30");
   if (M == 0 || N == 0) return PEAT_OK;
   // tiles are counted in 32 bits
@@ -121,15 +123,13 @@ peat_status_t product_ok(peat_handle_t h, int format, const float* sa, const flo
   if (!out) return fail(h, PEAT_ERR_INVALID_ARG, "out is NULL");
   if (!aligned(out, B) || (sa && !aligned(sa, 4)) || (sb && !aligned(sb, 4)) || (bias && !aligned(bias, 4)))
     return fail(h, PEAT_ERR_INVALID_ARG, "a pointer is not aligned to its element type");
-  (void)format;
   return peat::expired(h);
 }
-peat_status_t operand_ok(peat_handle_t h, const uint8_t* q, int64_t ld, const uint8_t* block_scale, int64_t rows, int64_t K) {
+peat_status_t operand_ok(peat_handle_t h, const uint8_t* q, int64_t ld, const uint8_t* block_scale, int64_t rows) {
   if (!q || !block_scale) return fail(h, PEAT_ERR_INVALID_ARG, "an operand's codes or block scales are NULL");
   if (!aligned(q, 16) || (rows > 1 && ld % 16) || !aligned(block_scale, 16))
     return fail(h, PEAT_ERR_INVALID_ARG, "an operand's rows and block scales must start on 16-byte boundaries");
   if (ld > ((int64_t)1 << 39)) return fail(h, PEAT_ERR_UNSUPPORTED, "rows more than 2^39 bytes apart");
-  (void)K;
   return PEAT_OK;
 }
 peat_status_t multiply(peat_handle_t h, int format, const peat::Mm4Params& p, int out_dtype, cudaStream_t st) {
@@ -144,10 +144,10 @@ peat_status_t matmul(peat_handle_t h, int format, const uint8_t* a, int64_t lda,
   if (M < 0 || N < 0 || K < 0) return fail(h, PEAT_ERR_INVALID_ARG, "M, N or K < 0");
   if (K % block_of(format)) return fail(h, PEAT_ERR_INVALID_ARG, "K must be whole blocks (the quantiser fills a row's last one with zeros)");
   if (lda < K / 2 || ldb < K / 2) return fail(h, PEAT_ERR_INVALID_ARG, "lda or ldb is less than a row");
-  peat_status_t ps = product_ok(h, format, sa, sb, bias, M, N, K, out, ldo, out_dtype);
+  peat_status_t ps = product_ok(h, sa, sb, bias, M, N, K, out, ldo, out_dtype);
   if (ps != PEAT_OK || M == 0 || N == 0) return ps;
-  if (K > 0) ps = operand_ok(h, a, lda, abs, M, K);
-  if (K > 0 && ps == PEAT_OK) ps = operand_ok(h, b, ldb, bbs, N, K);
+  if (K > 0) ps = operand_ok(h, a, lda, abs, M);
+  if (K > 0 && ps == PEAT_OK) ps = operand_ok(h, b, ldb, bbs, N);
   if (ps != PEAT_OK) return ps;
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
@@ -203,12 +203,12 @@ peat_status_t product(peat_handle_t h, int format, const peat_operand_f4_t* a, c
   Operand op[2] = {operand_of(*a, format, nullptr, &need), operand_of(*b, format, nullptr, &need)};
   if (op[0].K != op[1].K) return fail(h, PEAT_ERR_INVALID_ARG, "the operands differ in K");
   const int64_t M = op[0].rows, N = op[1].rows, K = op[0].K;
-  peat_status_t ps = product_ok(h, format, a->dtype == PEAT_F4 ? a->scale : nullptr, b->dtype == PEAT_F4 ? b->scale : nullptr, bias,
+  peat_status_t ps = product_ok(h, a->dtype == PEAT_F4 ? a->scale : nullptr, b->dtype == PEAT_F4 ? b->scale : nullptr, bias,
                                 M, N, K, out, ldo, out_dtype);
   if (ps != PEAT_OK || M == 0 || N == 0) return ps;
   for (int i = 0; i < 2 && K > 0; i++) {
     if (!in[i]->data) return fail(h, PEAT_ERR_INVALID_ARG, "an operand's data is NULL");
-    if (in[i]->dtype == PEAT_F4) ps = operand_ok(h, op[i].q, op[i].ld, op[i].block_scale, op[i].rows, K);
+    if (in[i]->dtype == PEAT_F4) ps = operand_ok(h, op[i].q, op[i].ld, op[i].block_scale, op[i].rows);
     if (ps != PEAT_OK) return ps;
   }
   DeviceGuard dg(h->device);
@@ -294,13 +294,9 @@ peat_status_t rmsnorm(peat_handle_t h, const void* x, int64_t ldx, const void* r
   p.values = values;
   p.ldv = ldv;
   p.rstd = rstd;
-  p.vec_w = aligned(weight, 16);
-  p.vec_s = !sum || vec(sum, lds, rows, B);
-  p.vec_y = !y || vec(y, ldy, rows, B);
-  p.vec_q = !q || (aligned(q, E) && (ldq % E == 0 || rows <= 1));
-  p.vec_v = !values || vec(values, ldv, rows, B);
-  p.grid = cols % E == 0 && vec(x, ldx, rows, B) && (!residual || vec(residual, ldr, rows, B)) && p.vec_w && p.vec_s && p.vec_y &&
-           p.vec_q && p.vec_v;
+  p.grid = cols % E == 0 && aligned(weight, 16) && vec(x, ldx, rows, B) && (!residual || vec(residual, ldr, rows, B)) &&
+           (!sum || vec(sum, lds, rows, B)) && (!y || vec(y, ldy, rows, B)) && (!values || vec(values, ldv, rows, B)) &&
+           (!q || (aligned(q, E) && (ldq % E == 0 || rows <= 1)));
   cudaError_t e = peat::launch_rmsnorm(dtype, p, h->nsm, st);
   return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "norm launch");
 }
@@ -349,10 +345,8 @@ peat_status_t rmsnorm_backward(peat_handle_t h, const void* grad, int64_t ldg, c
   p.grad_weight = grad_weight;
   p.parts = static_cast<float*>(s->norm);
   p.dots = reinterpret_cast<float*>(static_cast<char*>(s->norm) + at);
-  p.vec_w = aligned(weight, 16);
-  p.vec_o = !grad_x || vec(grad_x, ldo, rows, B);
-  p.grid = cols % (16 / B) == 0 && vec(grad, ldg, rows, B) && vec(x, ldx, rows, B) && (!grad_sum || vec(grad_sum, ldr, rows, B)) &&
-           p.vec_w && p.vec_o;
+  p.grid = cols % (16 / B) == 0 && aligned(weight, 16) && vec(grad, ldg, rows, B) && vec(x, ldx, rows, B) &&
+           (!grad_sum || vec(grad_sum, ldr, rows, B)) && (!grad_x || vec(grad_x, ldo, rows, B));
   cudaError_t e = peat::launch_rmsnorm_backward(dtype, plan, p, st);
   return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "norm gradient launch");
 }

@@ -202,7 +202,6 @@ struct RmsParams {
   int64_t ldv;
   float* rstd;  // or null
   int grid;     // all matrices' rows start on 16-byte boundaries and are whole vectors
-  int vec_w, vec_s, vec_y, vec_q, vec_v;  // each output's rows and the weight start on them
 };
 cudaError_t launch_rmsnorm(int dtype, const RmsParams& p, int nsm, cudaStream_t s);
 struct RmsBackParams {
@@ -223,7 +222,7 @@ struct RmsBackParams {
   float* dots;         // of long rows
   int ctas;
   int64_t each;  // rows of a CTA's group
-  int grid, vec_w, vec_o;
+  int grid;  // as RmsParams'
 };
 // what a backward call needs: CTAs, and whether its rows are long ones
 struct RmsBackPlan {

@@ -174,6 +174,11 @@ void quantize_refusals() {
   Q big = good;
   big.rows = ((int64_t)1 << 31) - 200;
   CHECK(run(big) == PEAT_ERR_UNSUPPORTED);
+  big = good;  // (columns of blocks are counted in 32 bits with what a step reaches beyond)
+  big.rows = 1, big.cols = big.ldx = ((int64_t)1 << 30) + 32, big.ldq = big.cols / 2;
+  CHECK(run(big) == PEAT_ERR_UNSUPPORTED);
+  big.axis = 1, big.rows = big.cols, big.cols = 1;
+  CHECK(run(big) == PEAT_ERR_UNSUPPORTED);
   // one row needs no distance of its own; nothing to do is no error
   Q one = good;
   one.rows = 1, one.ldq = 24;
