@@ -4,8 +4,10 @@
 // The blocks lie along the product's axis: along the rows (axis 0), or down the
 // columns, whose codes come out transposed (axis 1).
 //
-// Bound by memory.  A lane holds one 16-byte vector of a row, so a block's
-// maximum is a few shuffles; down the columns a thread holds the whole block.
+// Bound by memory (16384 x 4096 bfloat16 to nvfp4 values by row: 46 us, 5.8 TB/s),
+// next to it by the instructions of a value's rounding.  A lane holds one 16-byte
+// vector of a row, so a block's maximum is a few shuffles; down the columns a thread
+// holds the whole block.
 #include <algorithm>
 #include <type_traits>
 
@@ -93,13 +95,17 @@ __device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Ou
   }
 }
 
-// (16384 x 4096 bfloat16 to codes: mxfp4 36 us, nvfp4 44, bound by the bytes under way:
-// two vectors a thread and twice the threads took 43 and 51.)
 // Rows: TPR threads have a unit, NV vectors each, one unit after another with the
 // next one's loads under way.  A unit is a row, or with mxfp4, which needs nothing
 // of the row beyond its blocks, one of `pieces` of it.  LONG (nvfp4): rows that
 // these threads do not hold, read twice, from L2 the second time.  GRID: x's and
-// values' rows start on 16-byte boundaries and are whole vectors.
+// values' rows start on 16-byte boundaries and are whole vectors; off it a warp's
+// elements are read side by side and change places in shared memory (10273 x 3863
+// bfloat16 to codes and values: mxfp4 67 us, nvfp4 78; by aligned vectors shifted
+// together 89 and 100).
+// (16384 x 4096 bfloat16 to codes: mxfp4 31 us, nvfp4 37, where the bytes take 25:
+// bound by the loads under way; two vectors a thread and twice the threads were a
+// fifth slower.)
 template <int DT, int FMT, int TPR, int NV, bool GRID, bool LONG>
 __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p, int64_t rows, int pieces, int64_t step_row, int step_piece) {
   using L = Elem<DT>;
@@ -234,7 +240,8 @@ __device__ __forceinline__ uint32_t column_word(const typename Elem<DT>::T* x, i
 }
 
 // nvfp4: the largest patterns of each column over one of the parts of the rows,
-// [parts, cols].  A lane has a vector of a row, off the 16-byte grid a word.
+// [parts, cols].  A lane has a vector of a row, off the 16-byte grid a word.  (16384 x
+// 4096 bfloat16: half of nvfp4's 63 us.)
 template <int DT, bool GRID, bool PAIRS>
 __global__ void __launch_bounds__(QT) quant4_maxima(Quant4Params p, int64_t wide, int64_t each) {
   using L = Elem<DT>;
@@ -292,8 +299,10 @@ __global__ void __launch_bounds__(QT) quant4_maxima(Quant4Params p, int64_t wide
   end(p);
 }
 
-// A warp has 32 rows, a thread the blocks of its columns, 16 bytes of codes each.
-// (4096 x 4096 bfloat16 to codes: mxfp4 11.6 us.)
+// A warp has 32 rows, a thread the blocks of its columns, 16 bytes of codes each: the
+// codes come out transposed without a way through shared memory, in units of half a
+// sector that L2 puts together.  (To codes: 4096 x 4096 bfloat16 mxfp4 9.0 us, 16384 x
+// 4096 31, the latter bound by memory.)
 template <int DT, int FMT, bool PAIRS, bool VALUES>
 __global__ void __launch_bounds__(QT) quant4_columns(Quant4Params p, int64_t wide, int chunks) {
   using L = Elem<DT>;
