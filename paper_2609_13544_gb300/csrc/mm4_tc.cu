@@ -1,17 +1,22 @@
 // Products of 4-bit matrices on the fifth-generation tensor cores, which scale
 // each block of values by the bytes that go with it and add up in float32.
 //
-// A CTA makes tiles of 128 rows of one operand by `bn` rows of the other, or a pair
-// of CTAs tiles of 256 by `bn` (each holds 128 rows and half of the others), which
-// needs fewer bytes for an instruction; persistent over the tiles.  An instruction of
-// 64 k takes about 128 cycles for any bn up to 256, so large products are bound by it
-// at 256 (8192 x 8192 x 8192 to bfloat16: mxfp4 170 us, 6.5 PFLOP/s, nvfp4 178), short
-// k by the results' way out (16384 x 4096 x 1024: 38 to 41 us, 21 of them bytes), small
-// ones by the chain of copy, instruction and result (1 x 4096 x 1024: 4.5 us).  A stage
-// is 256 k: a 128-byte piece of every row, swizzled by the copy, and the scales' tiles,
-// which lie in memory as the instruction wants them in tensor memory.  Warp roles: one thread issues the copies, one the moves
-// of scales and the matrix instructions, sixteen warps turn accumulators into
-// results while the other one fills.
+// A CTA makes tiles of 128 rows of one operand by `bn` rows of the other, or a pair of
+// CTAs tiles of 256 by `bn` (each holds 128 rows and half of the others), which needs
+// fewer bytes for an instruction; persistent over the tiles.  An instruction of 64 k
+// takes about 128 cycles for any bn up to 256, so large products are bound by it at 256
+// (8192 x 8192 x 8192 to bfloat16: mxfp4 171 us, 6.4 PFLOP/s, nvfp4 178), short k by
+// the results' way out (16384 x 4096 x 1024: 37 us, with a bias 40, 21 of them bytes),
+// small ones by the chain of copy, instruction and result (1 x 4096 x 1024: 4.5 us).
+// Two pairs in a cluster, each reading half of what both need of the other operand,
+// were no faster (178 us: 72 of 76 pairs find place, and reading is not what bounds
+// it).
+//
+// A stage is 256 k: a 128-byte piece of every row, swizzled by the copy, and the
+// scales' tiles, which lie in memory as the instruction wants them in tensor memory.
+// Warp roles: one thread issues the copies, one the moves of scales and the matrix
+// instructions, sixteen warps (eight for 128 x 128) turn accumulators into results
+// while the other one fills.
 //
 // Few rows of a: the tile's 128 rows are b's (SWAP), so that the instruction
 // spends nothing on rows that a does not have.
@@ -22,6 +27,7 @@
 #include "f4.cuh"
 #include "peat_internal.h"
 #include "tc_common.cuh"
+#include "vec16.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -45,11 +51,11 @@ constexpr int BARS = 256;
 constexpr int SUM_ROW = 132;  // words from one row of sums to the next
 constexpr int SMEM = 227 * 1024;
 // Tensor memory: two accumulators, then a stage's scales.  A pair's accumulators have
-// 256 columns and share 48 of them: the next tile's instructions wait until the warps
-// that have these have read them, not for the whole tile.
-template <int CG>
+// 256 columns and share 32 (mxfp4) or 48 of them: the next tile's instructions wait
+// until the warps that have these have read them, not for the whole tile.
+template <int CG, int FMT>
 struct Tmem {
-  static constexpr int APART = CG == 2 ? 208 : FEW_ROWS, SCALES = CG == 2 ? 464 : 2 * FEW_ROWS;
+  static constexpr int APART = CG == 2 ? (FMT == PEAT_MXFP4 ? 224 : 208) : FEW_ROWS, SCALES = CG == 2 ? APART + 256 : 2 * FEW_ROWS;
 };
 
 constexpr int stage_bytes(int rows) { return P_BYTES + rows * (SK / 2) + PS_BYTES + QS_BYTES; }
@@ -141,9 +147,9 @@ struct Place4 {
 template <int CG>
 __device__ __forceinline__ Place4 place_of(const Tc4Params& p, int u) {
   // groups of GROUP tiles of P, column by column: the CTAs at work at any time share few rows of either
-  const int64_t per = (int64_t)GROUP * p.qt;
-  const int g = (int)(u / per), in = (int)(u - g * per), wide = min(GROUP, p.pt - g * GROUP);
-  const int q = in / wide;
+  // (there are at most 2^27 tiles)
+  const unsigned per = GROUP * (unsigned)p.qt, g = (unsigned)u / per, in = (unsigned)u - g * per;
+  const unsigned wide = min(GROUP, p.pt - (int)g * GROUP), q = in / wide;
   return Place4{(int64_t)(g * GROUP + in - q * wide) * (CG * 128), (int64_t)q * p.bn};
 }
 
@@ -177,13 +183,13 @@ __device__ __forceinline__ uint4 packed(const float* v) {
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// Half h of 64 columns of a warp's 32 rows, a row a lane, scaled and biased, through
-// shared memory (128-byte rows, swizzled) and out by copies of 32 rows, which write
+// Half h of 64 columns of a warp's 32 rows, a row a lane, the first or the second one in
+// turn, scaled and biased, through shared memory (128-byte rows, swizzled) and out by copies of 32 rows, which write
 // whole lines and leave out what lies beyond the matrix.  (Sectors straight from the
 // lanes, 32 rows a store, took 1.3 us a tile of 128 x 128, twice its instructions'
 // time.)
 template <int OUT>
-__device__ __forceinline__ void put_box(char* box, const CUtensorMap* map, float (&v)[32], int h, bool scaled, float sp,
+__device__ __forceinline__ void put_box(char* box, const CUtensorMap* map, float (&v)[32], int h, int turn, bool scaled, float sp,
                                         const float* sq, bool biased, const float* bias, int64_t row0, int64_t col0, int64_t N) {
   constexpr int B = (int)sizeof(typename Mm8Out<OUT>::T), HALVES = B == 2 ? 2 : 1;  // that a box holds
   const int lane = threadIdx.x & 31;
@@ -191,23 +197,23 @@ __device__ __forceinline__ void put_box(char* box, const CUtensorMap* map, float
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
       const float4 f = *reinterpret_cast<const float4*>(sq + 32 * h + j);
-      v[j] = __fmul_rn(v[j], __fmul_rn(sp, f.x));
-      v[j + 1] = __fmul_rn(v[j + 1], __fmul_rn(sp, f.y));
-      v[j + 2] = __fmul_rn(v[j + 2], __fmul_rn(sp, f.z));
-      v[j + 3] = __fmul_rn(v[j + 3], __fmul_rn(sp, f.w));
+      const float2 lo = mul2(both(sp), make_float2(f.x, f.y)), hi = mul2(both(sp), make_float2(f.z, f.w));
+      // (one by one: a pair's product and the bias' sum would become one rounding)
+      v[j] = __fmul_rn(v[j], lo.x);
+      v[j + 1] = __fmul_rn(v[j + 1], lo.y);
+      v[j + 2] = __fmul_rn(v[j + 2], hi.x);
+      v[j + 3] = __fmul_rn(v[j + 3], hi.y);
     }
   }
   if (biased) {
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
       const float4 f = *reinterpret_cast<const float4*>(bias + 32 * h + j);
-      v[j] = __fadd_rn(v[j], f.x);
-      v[j + 1] = __fadd_rn(v[j + 1], f.y);
-      v[j + 2] = __fadd_rn(v[j + 2], f.z);
-      v[j + 3] = __fadd_rn(v[j + 3], f.w);
+      put_pair(v, j / 2, add2(pair(v, j / 2), make_float2(f.x, f.y)));
+      put_pair(v, j / 2 + 1, add2(pair(v, j / 2 + 1), make_float2(f.z, f.w)));
     }
   }
-  if (h % HALVES == 0) {
+  if (HALVES == 1 || turn == 0) {
     if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // the place is free
     __syncwarp();
   }
@@ -215,7 +221,7 @@ __device__ __forceinline__ void put_box(char* box, const CUtensorMap* map, float
 #pragma unroll
   for (int c = 0; c < 8 / HALVES; c++)
     *reinterpret_cast<uint4*>(box + lane * 128 + (((c0 + c) ^ (lane & 7)) * 16)) = packed<OUT>(v + c * (16 / B));
-  if (h % HALVES != HALVES - 1) return;
+  if (HALVES == 2 && turn == 0) return;
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
   const int64_t col = HALVES == 2 ? col0 : col0 + 32 * h;
@@ -343,8 +349,8 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
       const uint64_t desc = block_desc(0), scale_desc = (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
       const uint32_t at_q = P_BYTES >> 4, at_s = (P_BYTES + half * (SK / 2)) >> 4, tall = CG == 2 || bn > 128;
       const uint32_t idesc = (1u << 7) | (1u << 10) | ((bn / 8) << 17) | ((FMT == PEAT_MXFP4 ? 1u : 0u) << 23) | ((CG * 128u / 16) << 24);
-      const uint32_t tp = tmem + Tmem<CG>::SCALES, tq = tp + 4 * PER;  // 4 and 8 columns for a tile
-      static_assert(Tmem<CG>::SCALES + 12 * PER <= 512, "tensor memory has 512 columns");
+      const uint32_t tp = tmem + Tmem<CG, FMT>::SCALES, tq = tp + 4 * PER;  // 4 and 8 columns for a tile
+      static_assert(Tmem<CG, FMT>::SCALES + 12 * PER <= 512, "tensor memory has 512 columns");
       Turn at;
       uint32_t acc = 0, acc_phase = 1, shared_phase = 1;
       for (int u = first; u < units && ok && nk; u += apart) {
@@ -353,7 +359,7 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
         if (CG == 2 && !(ok = mbar_wait(shared_empty, shared_phase, p.wait_limit))) break;
         shared_phase ^= 1;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + acc * Tmem<CG>::APART;
+        const uint32_t d = tmem + acc * Tmem<CG, FMT>::APART;
         for (int k = k0; k < k1; k++) {
           if (!(ok = mbar_wait(full + 8 * at.s, at.phase, p.wait_limit))) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -437,7 +443,7 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
         if (!(ok = warp_wait(acc_full + 8 * acc, i / 2 & 1, p.wait_limit))) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
-      const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + acc * Tmem<CG>::APART;
+      const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + acc * Tmem<CG, FMT>::APART;
       if (split) {
         // The sums go to the stages' place (the last instruction is done with it), where
         // the cluster's other parts find them: contiguous along the output's rows.
@@ -486,8 +492,12 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
           uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
           // (a copy out writes whole 16-byte units: the row's last columns go by themselves if they are not)
           const bool boxed = p.out.vec && (p.units || col0 + STEP <= p.out.N);
+          // Of a pair's accumulators the first ends with the shared columns, the second starts with them: the first
+          // one's last half goes first (16384 x 4096 x 1024: mxfp4 37.5 us for 38.4).
+          const int half0 = CG == 2 && boxed && !acc, sharing = CG == 2 && part == (acc ? 0 : 3);
 #pragma unroll 1
-          for (int h = 0; h < 2; h++) {  // 32 columns at a time
+          for (int turn = 0; turn < 2; turn++) {  // 32 columns at a time
+            const int h = turn ^ half0;
             float v[32];
             if (nk) {
               tmem_load32(taddr + c * STEP + 32 * h, reinterpret_cast<uint32_t(&)[32]>(v));
@@ -496,14 +506,11 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
 #pragma unroll
               for (int j = 0; j < 32; j++) v[j] = 0.0f;
             }
-            if (h == 1) {
-              // (of a pair's accumulators the first ends with the shared columns, the second starts with them)
-              if (CG == 2 && part == (acc ? 0 : 3)) released(release_shared);
-              if (c + PARTS >= chunks) released(release + 8 * acc);
-            }
+            if (sharing && (FMT == PEAT_MXFP4 ? h != acc : turn == 1)) released(release_shared);
+            if (turn == 1 && c + PARTS >= chunks) released(release + 8 * acc);
             if (boxed) {
               if (row0 >= p.P) continue;
-              put_box<OUT>(box, &mo, v, h, scaled, sp, sq, p.out.biased, bias, row0, col0, p.out.N);
+              put_box<OUT>(box, &mo, v, h, turn, scaled, sp, sq, p.out.biased, bias, row0, col0, p.out.N);
             } else {
               const OutPlace off_grid{p.out.out, p.out.ldo, p.out.N, p.out.biased, false};
               put_columns<OUT>(off_grid, v, sp, sq + 32 * h, bias + 32 * h, row0, rows, col0 + 32 * h, h == 0, h == 1, carry);

@@ -152,7 +152,8 @@ def _matrix(h, t, name: str) -> int:
 def _vector(h, t, n: int, name: str) -> Optional[int]:
     if t is None:
         return None
-    if _code_or_int8(t) != 0 or t.numel() != n or not t.is_contiguous() or t.get_device() != h.device:
+    if (_codes.get(t.dtype) != 0 and _code_or_int8(t) != 0) or t.numel() != n or not t.is_contiguous() or (
+            t.get_device() != h.device):
         raise ValueError(f"{name} must be a contiguous float32 tensor of {n} elements on the handle's device")
     return t.data_ptr()
 

@@ -257,7 +257,7 @@ def _like(h, t, shape, dtype, name: str):
         return None, shape[1]
     if t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{name} must have x's shape and type")
-    return t.data_ptr(), _matrix(h, t, name)
+    return t.data_ptr(), shape[1] if t.is_contiguous() and t.get_device() == h.device else _matrix(h, t, name)
 
 
 def _norm_weight(h, weight, cols: int, dtype):
