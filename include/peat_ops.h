@@ -176,7 +176,7 @@ peat_status_t peat_quantize_f4(peat_handle_t h, const void* x, int64_t rows, int
 /* out[m, n] = acc * (a_scale[m] * b_scale[n]) + bias[n], with acc the sum over k of
  * the products of the operands' values (codes times block scales), in float32: the
  * values' products are exact, the sum is rounded as it goes, in an order that
- * depends on the sizes alone.  Scaling and bias are float32 operations, the result
+ * depends on the sizes and on whether out's rows start on 16-byte boundaries.  Scaling and bias are float32 operations, the result
  * is rounded once more to a 16-bit type.  (A product of two block scales outside
  * float32's range gives infinities, NaN or 0.)
  * a: [M, K], b: [N, K], both of `format`, K whole blocks, rows lda and ldb BYTES
@@ -242,7 +242,8 @@ peat_status_t peat_rmsnorm(peat_handle_t h, const void* x, int64_t ldx, const vo
  *                 x and of the residual alike
  *   grad_weight = the sum over the rows of grad * n, float32 [cols].
  * (Rounding to 8 bits passes gradients through: grad is then that of values.)  Sums
- * are float32, in an order that depends on the sizes alone.  Each output may be
+ * are float32, in an order that depends on the sizes and on whether all rows, and the
+ * weight, are whole 16-byte units on 16-byte boundaries.  Each output may be
  * NULL, not both; no rows give grad_weight 0.  cols <= 2^27.  grad_x may be grad or
  * grad_sum itself (the same rows at the same distance), else no output overlaps an
  * input. */
