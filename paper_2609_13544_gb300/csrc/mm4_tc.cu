@@ -489,16 +489,12 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
             if (col0 + j < p.Q && row < p.P) put_one<OUT>(p.out.out, (col0 + j) * p.out.ldo + row, y);
           }
         } else {
-          uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
           // (a copy out writes whole 16-byte units: the row's last columns go by themselves if they are not)
           const bool boxed = p.out.vec && (p.units || col0 + STEP <= p.out.N);
           // Of a pair's accumulators the first ends with the shared columns, the second starts with them: the first
           // one's last half goes first (16384 x 4096 x 1024: mxfp4 37.5 us for 38.4).
           const int half0 = CG == 2 && boxed && !acc, sharing = CG == 2 && part == (acc ? 0 : 3);
-#pragma unroll 1
-          for (int turn = 0; turn < 2; turn++) {  // 32 columns at a time
-            const int h = turn ^ half0;
-            float v[32];
+          auto take = [&](float (&v)[32], int h, int turn) {  // 32 columns at a time
             if (nk) {
               tmem_load32(taddr + c * STEP + 32 * h, reinterpret_cast<uint32_t(&)[32]>(v));
               asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
@@ -508,11 +504,22 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
             }
             if (sharing && (FMT == PEAT_MXFP4 ? h != acc : turn == 1)) released(release_shared);
             if (turn == 1 && c + PARTS >= chunks) released(release + 8 * acc);
-            if (boxed) {
-              if (row0 >= p.P) continue;
-              put_box<OUT>(box, &mo, v, h, turn, scaled, sp, sq, p.out.biased, bias, row0, col0, p.out.N);
-            } else {
-              const OutPlace off_grid{p.out.out, p.out.ldo, p.out.N, p.out.biased, false};
+          };
+          if (boxed) {
+#pragma unroll 1
+            for (int turn = 0; turn < 2; turn++) {
+              const int h = turn ^ half0;
+              float v[32];
+              take(v, h, turn);
+              if (row0 < p.P) put_box<OUT>(box, &mo, v, h, turn, scaled, sp, sq, p.out.biased, bias, row0, col0, p.out.N);
+            }
+          } else {
+            const OutPlace off_grid{p.out.out, p.out.ldo, p.out.N, p.out.biased, false};
+            uint32_t carry[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll 1
+            for (int h = 0; h < 2; h++) {
+              float v[32];
+              take(v, h, h);
               put_columns<OUT>(off_grid, v, sp, sq + 32 * h, bias + 32 * h, row0, rows, col0 + 32 * h, h == 0, h == 1, carry);
             }
           }
