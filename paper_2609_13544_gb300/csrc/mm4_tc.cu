@@ -5,7 +5,7 @@
 // CTAs tiles of 256 by `bn` (each holds 128 rows and half of the others), which needs
 // fewer bytes for an instruction; persistent over the tiles.  An instruction of 64 k
 // takes about 128 cycles for any bn up to 256, so large products are bound by it at 256
-// (8192 x 8192 x 8192 to bfloat16: mxfp4 171 us, 6.4 PFLOP/s, nvfp4 178), short k by
+// (8192 x 8192 x 8192 to bfloat16: mxfp4 170 us, 6.5 PFLOP/s, nvfp4 177), short k by
 // the results' way out (16384 x 4096 x 1024: 37 us, with a bias 40, 21 of them bytes),
 // small ones by the chain of copy, instruction and result (1 x 4096 x 1024: 4.5 us).
 // Two pairs in a cluster, each reading half of what both need of the other operand,
@@ -184,10 +184,10 @@ __device__ __forceinline__ uint4 packed(const float* v) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // Half h of 64 columns of a warp's 32 rows, a row a lane, the first or the second one in
-// turn, scaled and biased, through shared memory (128-byte rows, swizzled) and out by copies of 32 rows, which write
-// whole lines and leave out what lies beyond the matrix.  (Sectors straight from the
-// lanes, 32 rows a store, took 1.3 us a tile of 128 x 128, twice its instructions'
-// time.)
+// turn, scaled and biased, through shared memory (128-byte rows, swizzled) and out by
+// copies of 32 rows, which write whole lines and leave out what lies beyond the matrix.
+// (Sectors straight from the lanes, 32 rows a store, took 1.3 us a tile of 128 x 128,
+// twice its instructions' time.)
 template <int OUT>
 __device__ __forceinline__ void put_box(char* box, const CUtensorMap* map, float (&v)[32], int h, int turn, bool scaled, float sp,
                                         const float* sq, bool biased, const float* bias, int64_t row0, int64_t col0, int64_t N) {
