@@ -466,8 +466,9 @@ class Linear8(LinearBase):
             raise ValueError(f"q must be int8, its last dimension {self.in_features}")
         if scale.shape != q.shape[:-1]:
             raise ValueError("scale must have one element for each row of q")
-        x = _as_rows(q, self.in_features)
-        a = _operand(self.h, x, 0, scale.reshape(-1), "q")[0]
+        # (both may be copies, of which the operand holds pointers alone: they are kept until the call is made)
+        x, flat = _as_rows(q, self.in_features), scale.reshape(-1)
+        a = _operand(self.h, x, 0, flat, "q")[0]
         out = torch.empty((x.shape[0], self.out_features), dtype=out_dtype or torch.float32, device=x.device)
         self._multiply(a, self._w[0], _vector(self.h, bias, self.out_features, "bias"), out.data_ptr(), self.out_features,
                        _code(out), _stream(self.h, None))

@@ -1,0 +1,33 @@
+"""The 4-bit products, the 8-bit layer behind the norm, and the norm's gradients: strides, row counts, lengths and empty
+matrices at the edges of what the calls allow, against the definitions in 64 bits."""
+import pytest
+import test_gpu_ops4 as T
+
+pytestmark = pytest.mark.gpu
+
+EPS = T.EPS
+
+
+@pytest.fixture(scope="module")
+def h(peat_gpu):
+    handle = peat_gpu.Handle(0)
+    yield handle
+    handle.close()
+
+
+@pytest.mark.parametrize("lead,width,features,out", [((100, 3000), 32, 4, "bf16"), ((5, 26), 200, 1, "f32"), ((65, 2), 96, 40, "bf16"),
+                                                     ((60, 100), 64, 40, "f32")])
+def test_rounded_input_of_turned_dimensions(peat_gpu, h, lead, width, features, out):
+    """q and scale with their leading dimensions in another order than memory's give what contiguous ones give: the copy of
+    the scales outlives the call, also where the results would fit its place (300 000 rows, in several waves)."""
+    import torch
+    g = T.rng(width)
+    layer = peat_gpu.Linear8(h, torch.randn(features, width, generator=g, device="cuda"))
+    q = torch.randint(-127, 128, (*lead, width), generator=g, device="cuda", dtype=torch.int8)
+    scale = torch.rand(*lead, generator=g, device="cuda")
+    flat_q, flat_scale = q.transpose(0, 1).contiguous(), scale.transpose(0, 1).contiguous()
+    want = layer.forward_rounded(flat_q, flat_scale, T.dt(out))
+    for _ in range(3):
+        torch.cuda.empty_cache()  # (what a call frees is then the first place that its next tensor finds)
+        y = layer.forward_rounded(q.transpose(0, 1), scale.transpose(0, 1), T.dt(out))
+        assert y.shape == (lead[1], lead[0], features) and T.same_bits(y, want)
