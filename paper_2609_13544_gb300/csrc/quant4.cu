@@ -212,7 +212,10 @@ __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p
       static_assert(NV == 1 || TPR * L::E % TILE == 0, "tiles of scales");
       const Col block = (at + lane * L::E) / F4<FMT>::BLOCK;
       uint8_t* scales = o.block_scale + (int64_t)(block >> 2) * SCALE_TILE + (block & 3);
-      if (GRID && at + PIECE <= (Col)p.cols && here < p.rows) {
+      // (one way for a warp of two rows, of which the second may be beyond the last: its shuffles are all lanes')
+      bool whole = GRID && at + PIECE <= (Col)p.cols && here < p.rows;
+      if (GRID && TPR < 32) whole = __all_sync(0xffffffffu, whole);
+      if (whole) {
 #pragma unroll
         for (int i = 0; i < NV; i++)
           put_vec<DT, FMT, G, GRID, true, Col>(p, w[i], o, at + (i * TPR + lane) * L::E, 1, scales + i * (NEXT * SCALE_TILE), r, reciprocals, place);

@@ -31,3 +31,16 @@ def test_rounded_input_of_turned_dimensions(peat_gpu, h, lead, width, features, 
         torch.cuda.empty_cache()  # (what a call frees is then the first place that its next tensor finds)
         y = layer.forward_rounded(q.transpose(0, 1), scale.transpose(0, 1), T.dt(out))
         assert y.shape == (lead[1], lead[0], features) and T.same_bits(y, want)
+
+
+@pytest.mark.parametrize("dtype", T.DTYPES)
+@pytest.mark.parametrize("format", T.FORMATS)
+@pytest.mark.parametrize("rows", [1, 15, 77, 129, 4097])
+@pytest.mark.parametrize("cols", [64, 128])
+def test_quantize_rows_of_half_a_warp(peat_gpu, h, dtype, format, rows, cols):
+    """Rows of 16 vectors, two to a warp, and an odd number of them: the last warp has a row of the matrix and one that is
+    not."""
+    import torch
+    for pad in (0, 8):
+        x = torch.randn(rows, cols + pad, generator=T.rng(rows), device="cuda").to(T.dt(dtype))[:, :cols]
+        T.check_quant(peat_gpu, h, x, format, 0, 0, pad)
