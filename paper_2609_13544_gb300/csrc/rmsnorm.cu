@@ -372,9 +372,10 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR
 //   grad_x = rstd (g - n c) + stream, grad_weight = sum over rows of grad n
 // A CTA has `each` rows for each of its groups of TPR threads, one after another,
 // the next one's loads under way; a thread keeps its columns' weights and sums.
-// LONG: the CTAs of blockIdx.y have a piece of the columns, and c is there already
-// (rms_dots), which costs a second reading (4000 x 12800 bfloat16: 98 us, the bytes read
-// once 45).  Beyond a row's end grad, x and weight are 0.
+// LONG: CTA blockIdx.x has a piece of the columns (65536 pieces at most) of the rows of
+// blockIdx.y, and c is there already (rms_dots), which costs a second reading (4000 x
+// 12800 bfloat16: 98 us, the bytes read once 45).  Beyond a row's end grad, x and weight
+// are 0.
 template <int DT, int TPR, int NV, bool GRID, bool LONG>
 __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_backward(RmsBackParams p) {
   using L = Elem<DT>;
@@ -387,8 +388,8 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
   pdl_trigger();
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR;
   const float n_cols = (float)(int)p.cols;
-  const Col at = LONG ? (Col)blockIdx.y * (TPR * NV * E) : 0;
-  const int64_t row0 = ((int64_t)blockIdx.x * GROUPS + group) * p.each;
+  const Col at = LONG ? (Col)blockIdx.x * (TPR * NV * E) : 0;
+  const int64_t cta = LONG ? blockIdx.y : blockIdx.x, row0 = (cta * GROUPS + group) * p.each;
   constexpr int STEP = GRID ? 1 : TPR;  // columns from one element of a vector to the next
   auto column = [&](int i) { return at + (GRID ? (i * TPR + lane) * E : i * TPR * E + lane); };
   float dw[NV][E], w[NV][E];
@@ -486,7 +487,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_back
     }
     if (group != GROUPS - 1) return;
   }
-  float* o = p.parts + (int64_t)blockIdx.x * p.cols;
+  float* o = p.parts + cta * p.cols;
 #pragma unroll
   for (int i = 0; i < NV; i++)
 #pragma unroll
@@ -612,7 +613,8 @@ cudaError_t backward(const RmsBackParams& p, cudaStream_t s) {
   }
   if (p.ctas) {
     constexpr int64_t PIECE = (int64_t)TPR * NV * Elem<DT>::E;
-    const dim3 grid((unsigned)p.ctas, LONG ? (unsigned)((p.cols + PIECE - 1) / PIECE) : 1u);
+    // (a grid's y ends at 65535, the rows' CTAs at two an SM)
+    const dim3 grid = LONG ? dim3((unsigned)((p.cols + PIECE - 1) / PIECE), (unsigned)p.ctas) : dim3((unsigned)p.ctas);
     e = p.grid ? launch_dependent(rms_backward<DT, TPR, NV, true, LONG>, grid, QT, 0, s, p)
                : launch_dependent(rms_backward<DT, TPR, NV, false, LONG>, grid, QT, 0, s, p);
     if (e != cudaSuccess) return e;

@@ -44,3 +44,23 @@ def test_quantize_rows_of_half_a_warp(peat_gpu, h, dtype, format, rows, cols):
     for pad in (0, 8):
         x = torch.randn(rows, cols + pad, generator=T.rng(rows), device="cuda").to(T.dt(dtype))[:, :cols]
         T.check_quant(peat_gpu, h, x, format, 0, 0, pad)
+
+
+def test_rmsnorm_backward_of_the_widest_rows(peat_gpu, h):
+    """2^27 columns, the most that the call takes, in the type that has the most pieces a row."""
+    import torch
+    cols, g = 1 << 27, T.rng(27)
+    x, grad = torch.randn(1, cols, generator=g, device="cuda"), torch.rand(1, cols, generator=g, device="cuda")
+    w, rstd = torch.rand(cols, generator=g, device="cuda") + 0.5, torch.full((1,), 1.25, device="cuda")
+    dx, dw = peat_gpu.peat_rmsnorm_backward(h, grad, x, w, rstd)
+    n, d = x.double() * 1.25, grad.double()
+    assert bool(((dw.double() - (d * n)[0]).abs() <= 2 * EPS * (d * n)[0].abs()).all())
+    gn = d * w.double() * n
+    c, size = gn.mean(), gn.abs().mean()
+    del gn
+    # a product's 3 roundings and 4 more in its vector; 2^17 vectors a thread one after the other with their errors kept,
+    # to the square of 2^17 roundings; 13 partial sums and the division
+    off = ((3 + 4 + 2 + 14) * EPS + (2.0 ** 17 * EPS) ** 2) * size
+    want = 1.25 * (d * w.double() - n * c)
+    tol = 1.25 * (n.abs() * off + 5 * EPS * ((d * w.double()).abs() + (n * c).abs())) + EPS * want.abs()
+    assert bool(((dx.double() - want).abs() <= tol).all())
