@@ -58,9 +58,35 @@ def test_rmsnorm_backward_of_the_widest_rows(peat_gpu, h):
     gn = d * w.double() * n
     c, size = gn.mean(), gn.abs().mean()
     del gn
-    # a product's 3 roundings and 4 more in its vector; 2^17 vectors a thread one after the other with their errors kept,
-    # to the square of 2^17 roundings; 13 partial sums and the division
-    off = ((3 + 4 + 2 + 14) * EPS + (2.0 ** 17 * EPS) ** 2) * size
+    # a product's 3 roundings and 4 more in its vector, 64 vectors; 2^17 vectors a thread one after the other, those
+    # additions' errors kept, to the square of as many roundings; 13 partial sums and the division
+    off = ((3 + 4 + 64 + 14) * EPS + (2.0 ** 17 * EPS) ** 2) * size
     want = 1.25 * (d * w.double() - n * c)
     tol = 1.25 * (n.abs() * off + 5 * EPS * ((d * w.double()).abs() + (n * c).abs())) + EPS * want.abs()
     assert bool(((dx.double() - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("more,pad,off", [(3, 5, 0), (3, 5, 1), (8, 8, 0)])
+def test_rmsnorm_backward_sums_of_long_rows(peat_gpu, h, dtype, more, pad, off):
+    """A row's inner product over 2^24 elements of one sign, whose single additions all round the same way: grad_x is what
+    is left of g and of that mean, which cancel."""
+    import torch
+    cols = (1 << 24) + more
+    t, w = T.dt(dtype), torch.full((cols,), 0.7, device="cuda")
+    rstd = torch.ones(2, device="cuda")
+    buf = torch.ones(2 * (cols + pad) + off, device="cuda", dtype=t)
+    x = buf[off:].view(2, cols + pad)[:, :cols]
+    grad = torch.empty(2, cols, device="cuda", dtype=t)
+    grad[0], grad[1] = 0.1, 0.7
+    dx, dw = peat_gpu.peat_rmsnorm_backward(h, grad, x, w, rstd)
+    assert torch.equal(dw, grad.float()[0] + grad.float()[1])
+    # (g is constant and n = 1: c is that constant)  8 products of 2 roundings and an addition each in a vector; 2^13
+    # (float32 2^14) vectors a thread one after the other with their errors kept, to the square of as many roundings, or
+    # (float32 on the grid) 64 of them before that; 13 partial sums and the division; then g's own rounding, the
+    # difference, the product by rstd
+    g = 0.7 * grad[:, :1].double()
+    vectors = 2.0 ** (13 if dtype == "bf16" else 14) + 1
+    run = 64 if (dtype, more) == ("f32", 8) else 0
+    tol = ((8 + 2 + 2 + run + 14) * EPS + (vectors * EPS) ** 2) * g + 5 * EPS * g
+    assert float((dx.double().abs() - tol).max()) <= 0.0
