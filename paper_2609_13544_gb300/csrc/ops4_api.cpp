@@ -151,6 +151,7 @@ peat_status_t matmul(peat_handle_t h, int format, const uint8_t* a, int64_t lda,
   if (ps != PEAT_OK) return ps;
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
+  if (K == 0) sa = sb = nullptr;  // (nothing to scale, and 0 x NaN must not get through)
   return multiply(h, format, peat::Mm4Params{a, b, lda, ldb, abs, bbs, sa, sb, bias, out, ldo, M, N, K}, out_dtype, st);
 }
 

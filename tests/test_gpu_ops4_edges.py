@@ -90,3 +90,17 @@ def test_rmsnorm_backward_sums_of_long_rows(peat_gpu, h, dtype, more, pad, off):
     run = 64 if (dtype, more) == ("f32", 8) else 0
     tol = ((8 + 2 + 2 + run + 14) * EPS + (vectors * EPS) ** 2) * g + 5 * EPS * g
     assert float((dx.double().abs() - tol).max()) <= 0.0
+
+
+@pytest.mark.parametrize("m", [3, 300])
+def test_4_bit_products_of_no_k_look_at_no_scale(peat_gpu, h, m):
+    """Without k the results are 0, plus the bias, whatever the rows' scales hold."""
+    import torch
+    bad = torch.tensor([float("nan"), float("inf"), 1.0], device="cuda")
+    empty = lambda rows, scale: peat_gpu.Float4("nvfp4", torch.empty(rows, 0, dtype=torch.uint8, device="cuda"),
+                                                torch.empty(0, dtype=torch.uint8, device="cuda"), scale)
+    a, b = empty(m, bad.repeat(m // 3)), empty(300, bad.repeat(100))
+    bias = torch.randn(300, generator=T.rng(m), device="cuda")
+    for bv, want in ((bias, bias.expand(m, 300)), (None, torch.zeros(m, 300, device="cuda"))):
+        assert torch.equal(peat_gpu.peat_matmul_f4(h, a, b, bv), want)
+        assert torch.equal(peat_gpu.peat_product_f4(h, a, b, None, 0, 0, bv), want)
