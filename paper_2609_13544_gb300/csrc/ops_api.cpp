@@ -190,6 +190,7 @@ peat_status_t matmul(peat_handle_t h, const int8_t* a, int64_t lda, const float*
   if (K > 0 && (!a || !b)) return fail(h, PEAT_ERR_INVALID_ARG, "a or b is NULL");
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
+  if (K == 0) sa = sb = nullptr;  // (nothing to scale, and 0 x NaN must not get through)
   const peat::Mm8Params p{a, b, lda, ldb, sa, sb, bias, out, ldo, M, N, K};
   const peat::Mm8TcPlan plan = peat::mm8_tc_plan(M, N, K, h->nsm);
   cudaError_t e;

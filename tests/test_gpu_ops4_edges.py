@@ -104,3 +104,15 @@ def test_4_bit_products_of_no_k_look_at_no_scale(peat_gpu, h, m):
     for bv, want in ((bias, bias.expand(m, 300)), (None, torch.zeros(m, 300, device="cuda"))):
         assert torch.equal(peat_gpu.peat_matmul_f4(h, a, b, bv), want)
         assert torch.equal(peat_gpu.peat_product_f4(h, a, b, None, 0, 0, bv), want)
+
+
+@pytest.mark.parametrize("m", [3, 300])
+def test_8_bit_products_of_no_k_look_at_no_scale(peat_gpu, h, m):
+    import torch
+    bad = torch.tensor([float("nan"), float("inf"), 1.0], device="cuda")
+    sa, sb = bad.repeat(m // 3), bad.repeat(100)
+    a, b = (torch.empty(rows, 0, dtype=torch.int8, device="cuda") for rows in (m, 300))
+    bias = torch.randn(300, generator=T.rng(m), device="cuda")
+    for bv, want in ((bias, bias.expand(m, 300)), (None, torch.zeros(m, 300, device="cuda"))):
+        assert torch.equal(peat_gpu.peat_matmul_i8(h, a, sa, b, sb, bv), want)
+        assert torch.equal(peat_gpu.peat_product_i8(h, a, b, 0, 0, sa, sb, bv), want)
