@@ -225,7 +225,8 @@ peat_status_t peat_product_f4(peat_handle_t h, peat_f4_t format, const peat_oper
  *   scale = amax / 127 and q = the nearest integer of y * (127 / amax), amax = max
  *           |y|, with all of peat_quantize_i8's rules (float32 y, not the rounded).
  * weight [cols] is of type dtype or PEAT_F32.  A NaN or an infinity in a row goes
- * where the formulas take it; no square overflows or underflows.
+ * where the formulas take it; no square overflows or underflows.  Rows of no columns
+ * have scale 0 and rstd NaN (0 / 0).
  * Outputs, each optional (NULL), one at least: sum (s), y and values (q * scale)
  * [rows, cols] of type dtype, q int8 [rows, cols], scale and rstd float32 [rows].
  * sum may be x or residual itself (the same rows at the same distance); else no

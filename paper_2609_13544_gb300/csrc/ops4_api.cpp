@@ -266,15 +266,20 @@ peat_status_t rmsnorm(peat_handle_t h, const void* x, int64_t ldx, const void* r
   if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(h, PEAT_ERR_INVALID_ARG, "eps must be finite and >= 0");
   if (ldx < cols || (residual && ldr < cols) || (sum && lds < cols) || (y && ldy < cols) || (q && ldq < cols) || (values && ldv < cols))
     return fail(h, PEAT_ERR_INVALID_ARG, "a matrix's row distance is less than a row");
-  if (rows == 0 || cols == 0) return PEAT_OK;
-  if (!x || !weight) return fail(h, PEAT_ERR_INVALID_ARG, "x or weight is NULL");
-  if (!sum && !y && !q && !scale && !values && !rstd) return fail(h, PEAT_ERR_INVALID_ARG, "no output is asked for");
+  if (rows == 0) return PEAT_OK;
+  if (cols > 0 && (!x || !weight)) return fail(h, PEAT_ERR_INVALID_ARG, "x or weight is NULL");
+  if (cols > 0 && !sum && !y && !q && !scale && !values && !rstd) return fail(h, PEAT_ERR_INVALID_ARG, "no output is asked for");
   for (const void* p : {x, residual, (const void*)sum, (const void*)y, (const void*)values})
     if (!aligned(p, B)) return fail(h, PEAT_ERR_INVALID_ARG, "a pointer is not aligned to its element type");
   if (!aligned(weight, type_bytes(weight_dtype)) || !aligned(scale, 4) || !aligned(rstd, 4))
     return fail(h, PEAT_ERR_INVALID_ARG, "a pointer is not aligned to its element type");
   DeviceGuard dg(h->device);
   if (!dg.ok) return fail(h, PEAT_ERR_CUDA, "cudaSetDevice failed");
+  if (cols == 0) {  // rows of nothing: bytes of zeros, and of a NaN
+    cudaError_t e = scale ? cudaMemsetAsync(scale, 0, sizeof(float) * (size_t)rows, st) : cudaSuccess;
+    if (e == cudaSuccess && rstd) e = cudaMemsetAsync(rstd, 0xff, sizeof(float) * (size_t)rows, st);
+    return e == cudaSuccess ? PEAT_OK : cuda_fail(h, e, "cudaMemsetAsync(scale, rstd)");
+  }
   peat::RmsParams p;
   p.x = x;
   p.ldx = ldx;

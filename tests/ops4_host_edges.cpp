@@ -16,10 +16,26 @@ void no_k_no_scales() {
   CHECK(rt.launches == 1 && rt.product.K == 0 && !rt.product.sa && !rt.product.sb && rt.product.bias == u.floats());
 }
 
+// A norm's rows of nothing: every output that has elements is written.
+void norm_of_nothing() {
+  Host u;
+  float *scale = u.floats(), *rstd = u.floats() + 64;
+  for (int i = 0; i < 4; i++) scale[i] = rstd[i] = 5.0f;
+  auto run = [&](float* s, float* r, int8_t* q) {
+    return peat_rmsnorm(&u.h, nullptr, 0, nullptr, 0, nullptr, PEAT_F32, 3, 0, PEAT_BF16, 1e-6f, nullptr, 0, nullptr, 0, q, 0, s,
+                        nullptr, 0, r, nullptr);
+  };
+  CHECK(run(scale, rstd, nullptr) == PEAT_OK && rt.launches == 0);
+  for (int i = 0; i < 3; i++) CHECK(scale[i] == 0.0f && rstd[i] != rstd[i]);
+  CHECK(scale[3] == 5.0f && rstd[3] == 5.0f);
+  CHECK(run(nullptr, nullptr, reinterpret_cast<int8_t*>(u.data())) == PEAT_OK && rt.launches == 0);
+  CHECK(run(nullptr, nullptr, nullptr) == PEAT_OK && rt.launches == 0);  // (matrices of nothing may be NULL)
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
-  const std::map<std::string, void (*)()> checks = {{"no_k_no_scales", no_k_no_scales}};
+  const std::map<std::string, void (*)()> checks = {{"no_k_no_scales", no_k_no_scales}, {"norm_of_nothing", norm_of_nothing}};
   if (argc != 2 || !checks.count(argv[1])) return 2;
   checks.at(argv[1])();
   return failures ? 1 : 0;

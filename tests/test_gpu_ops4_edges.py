@@ -116,3 +116,17 @@ def test_8_bit_products_of_no_k_look_at_no_scale(peat_gpu, h, m):
     for bv, want in ((bias, bias.expand(m, 300)), (None, torch.zeros(m, 300, device="cuda"))):
         assert torch.equal(peat_gpu.peat_matmul_i8(h, a, sa, b, sb, bv), want)
         assert torch.equal(peat_gpu.peat_product_i8(h, a, b, 0, 0, sa, sb, bv), want)
+
+
+def test_norm_of_no_columns(peat_gpu, h):
+    """Rows of nothing: a mean of nothing is no number, a largest of nothing 0; the layer behind them gives its bias."""
+    import torch
+    x, w = torch.empty(5, 3, 0, device="cuda"), torch.empty(0, device="cuda")
+    scale, rstd = torch.full((15,), 7.0, device="cuda"), torch.full((15,), 7.0, device="cuda")
+    peat_gpu.peat_rmsnorm_raw(h, x.view(15, 0), w, scale=scale, rstd=rstd)
+    assert not bool(scale.any()) and bool(torch.isnan(rstd).all())
+    got = peat_gpu.RMSNorm8(h, w).forward(x)
+    assert got["q"].shape == x.shape and not bool(got["scale"].any()) and bool(torch.isnan(got["rstd"]).all())
+    bias = torch.randn(40, generator=T.rng(1), device="cuda")
+    y = peat_gpu.Linear8(h, torch.empty(40, 0, device="cuda")).forward_rounded(got["q"], got["scale"], bias=bias)
+    assert torch.equal(y, bias.expand(5, 3, 40))
