@@ -79,11 +79,12 @@ class Float4:
         import torch
         block = F4_BLOCK[self.format]
         blocks, tall = self.cols // block, -(-self.rows // 128)
+        wide = -(-blocks // 4)
         table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], device=self.q.device)
         code = torch.stack([self.q & 15, self.q >> 4], 2).view(self.rows, blocks, block).long()
         v = torch.where(code > 7, -table[code & 7], table[code & 7])
-        s = self.block_scale[: f4_scale_bytes(self.rows, blocks)].view(tall, -1, 32, 4, 4).permute(0, 3, 2, 1, 4)
-        s = s.reshape(tall * 128, -1)[: self.rows, :blocks]
+        s = self.block_scale[: f4_scale_bytes(self.rows, blocks)].view(tall, wide, 32, 4, 4).permute(0, 3, 2, 1, 4)
+        s = s.reshape(tall * 128, 4 * wide)[: self.rows, :blocks]
         if self.code == 0:
             bits = torch.where(s == 0, 1 << 22, torch.where(s == 255, 0x7fc00000, s.int() << 23)).int()
             return (v * bits.view(torch.float32)[:, :, None]).view(self.rows, self.cols)

@@ -130,3 +130,11 @@ def test_norm_of_no_columns(peat_gpu, h):
     bias = torch.randn(40, generator=T.rng(1), device="cuda")
     y = peat_gpu.Linear8(h, torch.empty(40, 0, device="cuda")).forward_rounded(got["q"], got["scale"], bias=bias)
     assert torch.equal(y, bias.expand(5, 3, 40))
+
+
+@pytest.mark.parametrize("format", T.FORMATS)
+def test_values_of_an_empty_matrix(peat_gpu, h, format):
+    import torch
+    for rows, cols in ((0, 64), (0, 0), (5, 0), (130, 0)):
+        f = peat_gpu.peat_quantize_f4(h, torch.empty(rows, cols, device="cuda"), format)
+        assert f.values().shape == (rows, cols) and f.values().dtype == torch.float32
