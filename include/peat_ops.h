@@ -180,10 +180,10 @@ peat_status_t peat_quantize_f4(peat_handle_t h, const void* x, int64_t rows, int
  * is rounded once more to a 16-bit type.  (A product of two block scales outside
  * float32's range gives infinities, NaN or 0.)
  * a: [M, K], b: [N, K], both of `format`, K whole blocks, rows lda and ldb BYTES
- * apart (multiples of 16).  a_scale [M], b_scale [N] and bias [N] are float32; a
- * NULL scale is 1, a NULL bias 0.  out: row m at out + m * ldo elements, ldo >= N;
- * out_dtype PEAT_F32, PEAT_F16 or PEAT_BF16.  K = 0 gives 0 (plus the bias).  out
- * must not overlap the inputs. */
+ * apart (multiples of 16).  a_scale [M], b_scale [N] (PEAT_NVFP4 alone) and bias [N]
+ * are float32; a NULL scale is 1, a NULL bias 0.  out: row m at out + m * ldo
+ * elements, ldo >= N; out_dtype PEAT_F32, PEAT_F16 or PEAT_BF16.  K = 0 gives 0 (plus
+ * the bias).  out must not overlap the inputs. */
 peat_status_t peat_matmul_f4(peat_handle_t h, peat_f4_t format, const uint8_t* a, int64_t lda,
                              const uint8_t* a_block_scale, const float* a_scale, const uint8_t* b, int64_t ldb,
                              const uint8_t* b_block_scale, const float* b_scale, const float* bias, int64_t M,
@@ -191,7 +191,7 @@ peat_status_t peat_matmul_f4(peat_handle_t h, peat_f4_t format, const uint8_t* a
                              peat_stream_t stream);
 
 /* An operand of peat_product_f4: a matrix [rows, cols].  dtype PEAT_F4: codes with
- * their scales (scale: NULL is 1), axis 0, cols whole blocks, rows ld bytes apart.
+ * their scales (scale: PEAT_NVFP4 alone, NULL is 1), axis 0, cols whole blocks, rows ld bytes apart.
  * dtype PEAT_F32, PEAT_F16 or PEAT_BF16: rounded as peat_quantize_f4 does, along its
  * rows (axis 0) or columns (axis 1, whose transpose is then the operand), rows ld
  * elements apart; the scales are not read. */

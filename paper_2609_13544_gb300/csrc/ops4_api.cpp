@@ -142,6 +142,7 @@ peat_status_t matmul(peat_handle_t h, int format, const uint8_t* a, int64_t lda,
                      int64_t K, void* out, int64_t ldo, int out_dtype, cudaStream_t st) {
   if (!format_ok(format)) return fail(h, PEAT_ERR_INVALID_ARG, "format must be PEAT_MXFP4 or PEAT_NVFP4");
   if (M < 0 || N < 0 || K < 0) return fail(h, PEAT_ERR_INVALID_ARG, "M, N or K < 0");
+  if (format == PEAT_MXFP4 && (sa || sb)) return fail(h, PEAT_ERR_INVALID_ARG, "PEAT_MXFP4 has no float32 scales");
   if (K % block_of(format)) return fail(h, PEAT_ERR_INVALID_ARG, "K must be whole blocks (the quantiser fills a row's last one with zeros)");
   if (lda < K / 2 || ldb < K / 2) return fail(h, PEAT_ERR_INVALID_ARG, "lda or ldb is less than a row");
   peat_status_t ps = product_ok(h, sa, sb, bias, M, N, K, out, ldo, out_dtype);

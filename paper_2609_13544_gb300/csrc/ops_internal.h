@@ -171,7 +171,7 @@ struct Mm4Params {
   int64_t lda, ldb;  // bytes
   const uint8_t* a_block_scale;
   const uint8_t* b_block_scale;
-  const float* sa;    // or null, both or none
+  const float* sa;    // or null: 1
   const float* sb;
   const float* bias;  // or null
   void* out;

@@ -32,10 +32,25 @@ void norm_of_nothing() {
   CHECK(run(nullptr, nullptr, nullptr) == PEAT_OK && rt.launches == 0);  // (matrices of nothing may be NULL)
 }
 
+// The format that has no float32 scales takes none, here as in the other calls.
+void mxfp4_has_no_scales() {
+  Host u;
+  auto run = [&](peat_f4_t format, const float* sa, const float* sb) {
+    u.h.err.clear();
+    return peat_matmul_f4(&u.h, format, u.bytes(), 64, u.bytes(), sa, u.bytes(), 64, u.bytes(), sb, nullptr, 5, 7, 128, u.data(), 7,
+                          PEAT_F32, nullptr);
+  };
+  CHECK(run(PEAT_MXFP4, u.floats(), nullptr) == PEAT_ERR_INVALID_ARG && !u.h.err.empty());
+  CHECK(run(PEAT_MXFP4, nullptr, u.floats()) == PEAT_ERR_INVALID_ARG && !u.h.err.empty());
+  CHECK(rt.launches == 0);
+  CHECK(run(PEAT_MXFP4, nullptr, nullptr) == PEAT_OK && run(PEAT_NVFP4, u.floats(), nullptr) == PEAT_OK && rt.launches == 2);
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
-  const std::map<std::string, void (*)()> checks = {{"no_k_no_scales", no_k_no_scales}, {"norm_of_nothing", norm_of_nothing}};
+  const std::map<std::string, void (*)()> checks = {{"no_k_no_scales", no_k_no_scales}, {"norm_of_nothing", norm_of_nothing},
+                                                    {"mxfp4_has_no_scales", mxfp4_has_no_scales}};
   if (argc != 2 || !checks.count(argv[1])) return 2;
   checks.at(argv[1])();
   return failures ? 1 : 0;
