@@ -240,7 +240,8 @@ peat_status_t peat_rmsnorm(peat_handle_t h, const void* x, int64_t ldx, const vo
  * sublayer, grad_sum = dL/ds (NULL: none), from x = s (peat_rmsnorm's sum) and its
  * rstd.  With n = x * rstd, g = grad * weight, c = (sum of g * n) / cols,
  *   grad_x      = rstd * (g - n * c) + grad_sum, rounded to dtype: the gradient of
- *                 x and of the residual alike
+ *                 x and of the residual alike (float32 operations, n * c and its
+ *                 subtraction one of them)
  *   grad_weight = the sum over the rows of grad * n, float32 [cols].
  * (Rounding to 8 bits passes gradients through: grad is then that of values.)  Sums
  * are float32, in an order that depends on the sizes and on whether all rows, and the

@@ -138,3 +138,19 @@ def test_values_of_an_empty_matrix(peat_gpu, h, format):
     for rows, cols in ((0, 64), (0, 0), (5, 0), (130, 0)):
         f = peat_gpu.peat_quantize_f4(h, torch.empty(rows, cols, device="cuda"), format)
         assert f.values().shape == (rows, cols) and f.values().dtype == torch.float32
+
+
+@pytest.mark.parametrize("dtype", T.DTYPES)
+@pytest.mark.parametrize("cols", [40, 1001, 4096, 20000])
+def test_rmsnorm_backward_rounds_as_documented(peat_gpu, h, dtype, cols):
+    """rstd (g - n c) + grad_sum: the first difference is one fused operation, the others are rounded one by one.  Where
+    x = 0 (c = 0) that leaves grad weight, its product by rstd and the sum, bit for bit."""
+    import torch
+    g = T.rng(cols)
+    grad, add = (torch.randn(64, cols, generator=g, device="cuda").to(T.dt(dtype)) for _ in range(2))
+    w, rstd = (torch.rand(n, generator=g, device="cuda") + 0.5 for n in (cols, 64))
+    dx, dw = peat_gpu.peat_rmsnorm_backward(h, grad, torch.zeros_like(grad), w, rstd, add)
+    want = T.single(T.single(grad.double() * w.double()) * rstd.double()[:, None])
+    assert T.same_values(dx, (want + add.double()).float().to(dx.dtype)) and not bool(dw.any())
+    alone = peat_gpu.peat_rmsnorm_backward(h, grad, torch.zeros_like(grad), w, rstd)[0]
+    assert T.same_values(alone, want.to(dx.dtype))
