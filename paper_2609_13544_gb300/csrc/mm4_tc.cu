@@ -70,7 +70,7 @@ struct Tc4Params {
   int64_t P, Q;       // rows
   int64_t tiles;      // of scales along k
   int steps;          // instructions of 64 k
-  int bn, pt, qt, stages;
+  int bn, pt, qt, stages;  // (tiles start on blocks of 128 rows of Q: bn is 128, 256, or all of them)
   int units;          // the output's rows are whole 16-byte units
   int splits;         // CTAs of a cluster that share a tile's k range: 1, 2, 4 or 8 (then a cluster has one tile)
   unsigned int* status;
@@ -354,7 +354,6 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
       Turn at;
       uint32_t acc = 0, acc_phase = 1, shared_phase = 1;
       for (int u = first; u < units && ok && nk; u += apart) {
-        const uint32_t shift = (uint32_t)(place_of<CG>(p, u).q0 & 127) / 32;
         if (!(ok = mbar_wait(acc_empty + 8 * acc, acc_phase, p.wait_limit))) break;
         if (CG == 2 && !(ok = mbar_wait(shared_empty, shared_phase, p.wait_limit))) break;
         shared_phase ^= 1;
@@ -377,7 +376,7 @@ __global__ void __launch_bounds__(Warps<CG, SWAP>::THREADS, 1)
             if (j >= here) break;
             constexpr int TILE_STEPS = 4 / PER;
             mma4<FMT, CG>(d, a + 2 * j, b + 2 * j, idesc | (FMT == PEAT_MXFP4 ? (2u * (j & 1)) * 0x20000010u : 0u),
-                          tp + 4 * (j / TILE_STEPS), tq + shift + 8 * (j / TILE_STEPS), k + j > k0);
+                          tp + 4 * (j / TILE_STEPS), tq + 8 * (j / TILE_STEPS), k + j > k0);
           }
           commit<CG>(empty + 8 * at.s);
           at.next(p.stages);
