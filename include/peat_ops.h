@@ -28,9 +28,11 @@
  * N rounded up to 256 and K to 64, 2 (M + N) K bytes, and for K above 1024 20 MB,
  * or where that is more 4 M N bytes for each of the 1, 2 or 4 parts in which K is
  * taken; operands that peat_product_i8 rounds add a byte for each element.
- * Operands that peat_product_f4 rounds take 9/16 of a byte for each element (4
- * bytes a row with PEAT_NVFP4; rounded down the columns, there or in
- * peat_quantize_f4, 128 bytes for each column more); peat_matmul_f4 and
+ * An operand of R rows and k along the product's axis that peat_product_f4 rounds
+ * takes R (k / 2) bytes for its codes (k rounded up to whole blocks, k / 2 to 16
+ * bytes), peat_f4_scale_bytes for its block scales, 4 R with PEAT_NVFP4, each of these
+ * rounded up to 256 bytes; with PEAT_NVFP4 down the columns, there or in
+ * peat_quantize_f4, 128 for each column besides.  peat_matmul_f4 and
  * peat_rmsnorm take none, peat_rmsnorm_backward at most 4 bytes for each column and
  * each of two CTAs an SM, and 4 a row of more than 8192 elements (float32: 4096).
  * A gradient list takes 32 bytes for each tensor and 100 KB; one of more than 800
@@ -129,6 +131,11 @@ peat_status_t peat_product_i8(peat_handle_t h, const peat_operand_t* a, const pe
  *   PEAT_MXFP4  32 values, a power of two 2^e in one byte, e + 127 (255: NaN)
  *   PEAT_NVFP4  16 values, an 8-bit float (4 exponent bits, bias 7, 3 mantissa
  *               bits, sign 0; 0x7f: NaN), below a float32 scale of the whole row
+ *               (the row's own, as peat_quantize_i8 has one; elsewhere the format
+ *               of this name often has one float32 scale for the whole matrix:
+ *               peat_matmul_f4 takes such a matrix with its scale on every row, but
+ *               peat_quantize_f4 does not round by a scale that it is given, and by
+ *               the rows' scales the blocks' come out otherwise)
  * Codes lie two to a byte, the first in the low half; a row is whole blocks and
  * starts on a 16-byte boundary.  Block scales lie in tiles of 128 rows by 4
  * blocks, 512 bytes: row r of a tile and block k at (r mod 32) * 16 + (r div 32) *

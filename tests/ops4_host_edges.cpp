@@ -46,11 +46,35 @@ void mxfp4_has_no_scales() {
   CHECK(run(PEAT_MXFP4, nullptr, nullptr) == PEAT_OK && run(PEAT_NVFP4, u.floats(), nullptr) == PEAT_OK && rt.launches == 2);
 }
 
+// What a product takes of the workspace is what the header says.
+void workspace() {
+  for (int format : {PEAT_MXFP4, PEAT_NVFP4})
+    for (int axes = 0; axes < 4; axes++)
+      for (int64_t K : {1, 16, 32, 33, 1000})
+        for (int64_t rows : {1, 3, 128, 129, 1000}) {
+          Host u;
+          auto up = [](int64_t n, int64_t to) { return (n + to - 1) / to * to; };
+          const int64_t R[2] = {rows, 77}, block = format == PEAT_MXFP4 ? 32 : 16;
+          int64_t held = 0, tops = 0;
+          peat_operand_f4_t op[2];
+          for (int i = 0; i < 2; i++) {
+            const bool down = axes >> i & 1;
+            op[i] = peat_operand_f4_t{u.data(), nullptr, nullptr, down ? K : R[i], down ? R[i] : K, down ? R[i] : K, PEAT_BF16, down};
+            held += up(R[i] * up(up(K, block) / 2, 16), 256) + up(peat_f4_scale_bytes(R[i], up(K, block) / block), 256);
+            if (format == PEAT_NVFP4) held += up(4 * R[i], 256);
+            if (format == PEAT_NVFP4 && down) tops += 128 * R[i];
+          }
+          CHECK(peat_product_f4(&u.h, (peat_f4_t)format, &op[0], &op[1], nullptr, u.data(), 77, PEAT_F32, nullptr) == PEAT_OK);
+          CHECK((int64_t)u.h.ops->rounded_cap == held && (int64_t)u.h.ops->tops_cap == tops);
+        }
+}
+
 }  // namespace
 
 int main(int argc, char** argv) {
   const std::map<std::string, void (*)()> checks = {{"no_k_no_scales", no_k_no_scales}, {"norm_of_nothing", norm_of_nothing},
-                                                    {"mxfp4_has_no_scales", mxfp4_has_no_scales}};
+                                                    {"mxfp4_has_no_scales", mxfp4_has_no_scales},
+                                                    {"workspace", workspace}};
   if (argc != 2 || !checks.count(argv[1])) return 2;
   checks.at(argv[1])();
   return failures ? 1 : 0;

@@ -7,7 +7,7 @@ import pytest
 
 ROOT = Path(__file__).resolve().parents[1]
 CSRC = ROOT / "paper_2609_13544_gb300" / "csrc"
-CHECKS = ["no_k_no_scales", "norm_of_nothing", "mxfp4_has_no_scales"]
+CHECKS = ["no_k_no_scales", "norm_of_nothing", "mxfp4_has_no_scales", "workspace"]
 
 
 @pytest.fixture(scope="module")
