@@ -5,12 +5,13 @@
 // CTAs tiles of 256 by `bn` (each holds 128 rows and half of the others), which needs
 // fewer bytes for an instruction; persistent over the tiles.  An instruction of 64 k
 // takes about 128 cycles for any bn up to 256, so large products are bound by it at 256
-// (8192 x 8192 x 8192 to bfloat16: mxfp4 170 us, 6.5 PFLOP/s, nvfp4 177), short k by
-// the results' way out (16384 x 4096 x 1024: 37 us, with a bias 40, 21 of them bytes),
-// small ones by the chain of copy, instruction and result (1 x 4096 x 1024: 4.5 us).
-// Two pairs in a cluster, each reading half of what both need of the other operand,
-// were no faster (178 us: 72 of 76 pairs find place, and reading is not what bounds
-// it).
+// (8192 x 8192 x 8192 to bfloat16: mxfp4 168 us, 6.5 PFLOP/s, nvfp4 180; the chip's
+// form of 96 k, of 1.5 times that rate, is not used: a stage's 256 k are no multiple of
+// it), short k by the results' way out (16384 x 4096 x 1024: 36.5 us, with a bias 39.3,
+// 21 of them bytes), small ones by the chain of copy, instruction and result (1 x 4096 x
+// 1024: 4.5 us).  Two pairs in a cluster, each reading half of what both need of the
+// other operand, were no faster (178 us where one pair took 171: 72 of 76 pairs find
+// place, and reading is not what bounds it).
 //
 // A stage is 256 k: a 128-byte piece of every row, swizzled by the copy, and the
 // scales' tiles, which lie in memory as the instruction wants them in tensor memory.
@@ -680,9 +681,9 @@ Cut cut_of(int64_t M, int64_t N, int64_t steps, bool grid, int nsm) {
     Cut cut;
     // nanoseconds: of a call; of a wave, on the 16-byte grid and off it, at least; with instructions: and of each
     int fixed, least, least_off, tile, step;
-  } ways[] = {{{FEW, few, 1}, 3400, 0, 0, 350 + 19 * few, 60},   // 16 x 50257 x 1024: 8.4 us, 192 x: 18.9
-              {{ONE, 128, 1}, 3300, 1350, 3900, 450, 65},        // 2048 x 1024 x 4096: 7.1 us (a pair's 9.8)
-              {{PAIR, 256, 1}, 4200, 1800, 5800, 1100, 81}};     // 16384 x 4096 x 1024: 37.6 us (a CTA's 43.2)
+  } ways[] = {{{FEW, few, 1}, 3400, 0, 0, 350 + 19 * few, 60},   // 16 x 50257 x 1024: 8.5 us, 192 x: 18.9
+              {{ONE, 128, 1}, 3300, 1350, 3900, 450, 65},        // 2048 x 1024 x 4096: 7.7 us (a pair's 9.8)
+              {{PAIR, 256, 1}, 4200, 1800, 5800, 1100, 81}};     // 16384 x 4096 x 1024: 36.5 us (a CTA's 43.2)
   Cut best = ways[1].cut;
   double shortest = 0.0;
   for (const auto& w : ways) {

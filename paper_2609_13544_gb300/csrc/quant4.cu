@@ -101,11 +101,10 @@ __device__ __forceinline__ void put_vec(const Quant4Params& p, uint4 v, const Ou
 // these threads do not hold, read twice, from L2 the second time.  GRID: x's and
 // values' rows start on 16-byte boundaries and are whole vectors; off it a warp's
 // elements are read side by side and change places in shared memory (10273 x 3863
-// bfloat16 to codes and values: mxfp4 67 us, nvfp4 78; by aligned vectors shifted
-// together 89 and 100).
-// (16384 x 4096 bfloat16 to codes: mxfp4 31 us, nvfp4 37, where the bytes take 25:
-// bound by the loads under way; two vectors a thread and twice the threads were a
-// fifth slower.)
+// bfloat16 to values: mxfp4 67 us, nvfp4 78, with the codes 69 and 81; by aligned
+// vectors shifted together about a third more).
+// (16384 x 4096 bfloat16 to codes: mxfp4 31 us, nvfp4 37, where the bytes take 25;
+// two vectors a thread and twice the threads were a fifth slower.)
 template <int DT, int FMT, int TPR, int NV, bool GRID, bool LONG>
 __global__ void __launch_bounds__(QT, NV > 2 ? 2 : 4) quant4_rows(Quant4Params p, int64_t rows, int pieces, int64_t step_row, int step_piece) {
   using L = Elem<DT>;

@@ -9,7 +9,7 @@
 // near a rounding border then do not depend on the order of the sum.  Rows whose
 // squares leave float32's range are summed in binary64.
 //
-// Bound by memory (16384 x 4096 bfloat16 with residual and 8-bit values: 88 us, 6.1
+// Bound by memory (16384 x 4096 bfloat16 with residual and 8-bit values: 87 us, 6.1
 // TB/s; gradients with the stream's 90 us, 5.9 TB/s), next to it by the instructions
 // of the sum's kept errors and of the rounding: a row is read once and kept in
 // registers between the two reductions; the gradients of the weights are summed in
@@ -74,7 +74,7 @@ __device__ __forceinline__ float sum_plain(float x, float* part) {
 // A thread's E elements of a row of `cols`.  GRID (every matrix's rows start on
 // 16-byte boundaries and are whole vectors): a vector from column `col` on.  Off the
 // grid: elements `APART` columns apart, so that a warp's are side by side, whatever
-// the alignment (10273 x 3863 bfloat16, 8-bit values with the residual: 104 us; by
+// the alignment (10273 x 3863 bfloat16, 8-bit values with the residual: 101 us; by
 // vectors shifted together from aligned ones 142).
 template <int DT, bool GRID, int APART, typename Col>
 __device__ __forceinline__ uint4 load_vec(const typename Elem<DT>::T* row, Col col, Col cols) {
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(threads_of<TPR>(), LONG || TPR > 256 ? 1 : TPR
 // the next one's loads under way; a thread keeps its columns' weights and sums.
 // LONG: CTA blockIdx.x has a piece of the columns (65536 pieces at most) of the rows of
 // blockIdx.y, and c is there already (rms_dots), which costs a second reading (4000 x
-// 12800 bfloat16: 98 us, the bytes read once 45).  Beyond a row's end grad, x and weight
+// 12800 bfloat16: 99 us, the bytes read once 45).  Beyond a row's end grad, x and weight
 // are 0.
 template <int DT, int TPR, int NV, bool GRID, bool LONG>
 __global__ void __launch_bounds__(threads_of<TPR>(), TPR > 256 ? 1 : 2) rms_backward(RmsBackParams p) {

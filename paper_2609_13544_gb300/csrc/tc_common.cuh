@@ -177,7 +177,8 @@ __device__ __forceinline__ void sector_at(const uint32_t (&x)[16], int s, uint32
 #pragma unroll
   for (int i = 0; i < 8; i++) w[i] = y[8 + i];
 }
-// where results go: rows of ldo elements, N columns; vec: rows start on 32-byte boundaries
+// where results go: rows of ldo elements, N columns; vec: rows start on boundaries of the
+// units that the caller stores (put_columns: 32 bytes; copies out of shared memory: 16)
 struct OutPlace {
   void* out;
   int64_t ldo, N;
